@@ -239,6 +239,124 @@ typedef struct iodf_kernel_stat {
 int iodf_profile_begin(iodf_ctx* ctx, int max_launches);
 int iodf_profile_end(iodf_ctx* ctx, iodf_kernel_stat* stats, int max_stats, int* n_stats);
 
+/*
+ * Training operators of residual blocks, for fitting a network such as a prior head to the latents that iodf_forward gives. They
+ * need no context: they work on the current device of the calling thread, only enqueue on `stream`, allocate nothing and keep
+ * nothing between calls; scratch is the caller's (iodf_join_workspace, iodf_weight_grad_workspace). All pointers are device
+ * memory. A tensor is rows x cols with consecutive columns; strides count elements from row to row and are at least the columns.
+ * Any element address will do. rows may be 0 (no work; gradients that sum over rows are then 0); 0 <= rows <= 2^30,
+ * 1 <= cols <= 65536. `live` (may be NULL) holds a byte for each row, 0 where the row is padding: its entries in tensors may be
+ * anything, NaN included, and add nothing to any gradient.
+ *
+ * What the backward pass needs is kept as a checkpoint in 8 bits. For rows x cols values, with pitch = cols rounded up to 32:
+ * q int8 [rows][pitch] (16-byte aligned) and e uint8 [rows][pitch / 32], one exponent for 32 columns; q * 2^(e - 133) is the value.
+ * e is the biased exponent of the group's largest magnitude, or one more where that would round to 128 steps, limited to
+ * 16..254; q is rounded to nearest, ties to even, limited to -127..127. e = 255: the group held a NaN or an infinity and reads
+ * as NaN throughout. Columns past cols are written as 0. Padded rows are written as 0.
+ */
+enum { IODF_T_F32 = 0, IODF_T_BF16 = 1, IODF_T_F16 = 2 };
+enum { IODF_ACT_RELU = 0, IODF_ACT_SILU = 1, IODF_ACT_GELU = 2 /* the tanh form */ };
+
+/* x [rows][cols] of x_type -> checkpoint, and a checkpoint -> y of y_type (F32 or BF16, in both of which it is exact). */
+int iodf_pack(const void* x, int x_type, int64_t x_stride, int64_t rows, int cols, const uint8_t* live, int8_t* q, uint8_t* e,
+              void* stream);
+int iodf_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int cols, void* y, int y_type, int64_t y_stride, void* stream);
+
+/*
+ * The join of two blocks of a residual network: the norm behind a block's output f, its gate and residual scale, the addition
+ * to the stream h, and the norm before the next block, in one pass.
+ *   n = f / rms(f),  h' = h + alpha * gate * w_post * n,  x = h' / rms(h'),  u = w_pre * x      rms(v) = sqrt(mean(v^2) + eps)
+ * Sums and everything between loads and stores are 32-bit floats; x is taken from h' before it is rounded to the stream's type.
+ * w_post NULL: no norm behind the block, n = f. w_pre NULL: none before the next, no x and no u. gate NULL and alpha NULL: 1.
+ * Row t reads gate row t / gate_rows (gate_rows 1: a gate for each row; gate_rows >= rows: one gate for all). In a padded row
+ * h' = h and u = 0. out_stream may be in_stream (same stride); otherwise outputs overlap no inputs.
+ * The stream's type is F32 or the block's type; 1 <= cols <= 16384; eps > 0.
+ *
+ * iodf_join_forward: in_stream = h, in_block = f -> out_stream = h', out_block = u; with xq, not NULL, also the checkpoints of
+ *   x and n and the factors inv_pre = 1 / rms(h'), inv_post = 1 / rms(f) of each row (0 in padded rows).
+ * iodf_join_backward: in_stream = dL/dh', in_block = dL/du and the checkpoint -> out_stream = dL/dh, out_block = dL/df
+ *   (rounded to those types; may not overlap anything) and the sums dalpha [1], dgate [gate rows][cols], dw_post [cols], dw_pre [cols] (each NULL
+ *   exactly where its parameter is). x and n stand for what the checkpoint holds. The result is the same bits on every call.
+ */
+typedef struct iodf_join {
+    int64_t rows, gate_rows;
+    int32_t cols, stream_type, block_type;
+    float eps;
+    const float* alpha;
+    const float* gate;
+    const float* w_post;
+    const float* w_pre;
+    const uint8_t* live;
+    const void* in_stream;
+    const void* in_block;
+    void* out_stream;
+    void* out_block;
+    int64_t in_stream_stride, in_block_stride, out_stream_stride, out_block_stride;
+    int8_t* xq;
+    uint8_t* xe;
+    int8_t* nq;
+    uint8_t* ne;
+    float* inv_pre;
+    float* inv_post;
+    float* dalpha;
+    float* dgate;
+    float* dw_post;
+    float* dw_pre;
+} iodf_join;
+int iodf_join_forward(const iodf_join* args, void* stream);
+int iodf_join_backward(const iodf_join* args, void* work, int64_t work_bytes, void* stream);
+int iodf_join_workspace(const iodf_join* args, int64_t* bytes);
+
+/*
+ * The gated activation y = act(a) * b of a block's hidden layer.
+ * iodf_glu_forward: a, b -> y; with aq not NULL also the checkpoints of a and b.
+ * iodf_glu_backward: the checkpoints and dy = dL/dy -> a_out = dL/da, b_out = dL/db and, with yq not NULL, the checkpoint of
+ *   y as the checkpoints of a and b give it: the input of the projection behind, for that one's weight gradient.
+ * One type for a, b, y, dy and the gradients.
+ */
+typedef struct iodf_glu {
+    int64_t rows;
+    int32_t cols, type, act;
+    const uint8_t* live;
+    const void* a;
+    const void* b;
+    void* y;
+    const void* dy;
+    void* da;
+    void* db;
+    int64_t a_stride, b_stride, y_stride, dy_stride, da_stride, db_stride;
+    int8_t* aq;
+    uint8_t* ae;
+    int8_t* bq;
+    uint8_t* be;
+    int8_t* yq;
+    uint8_t* ye;
+} iodf_glu;
+int iodf_glu_forward(const iodf_glu* args, void* stream);
+int iodf_glu_backward(const iodf_glu* args, void* stream);
+
+/*
+ * Gradient of a linear layer's weight W [out][cols] from the checkpoint of its input:
+ *   dw[o][c] = (accumulate ? dw[o][c] : 0) + col_scale[c] * sum_t dy[t][o] * X[t][c]
+ * dy [rows][out] of dy_type, X what the checkpoint stands for, dw F32 with rows dw_stride apart. col_scale (may be NULL): the
+ * weight of the norm between the checkpoint and the layer (w_pre of iodf_join). Products are exact for every dy_type,
+ * sums are 32-bit floats, in an order that depends on the sizes alone. 1 <= out <= 65536.
+ */
+typedef struct iodf_wgrad {
+    int64_t rows;
+    int32_t cols, out, dy_type, accumulate;
+    const void* dy;
+    int64_t dy_stride;
+    const int8_t* q;
+    const uint8_t* e;
+    const float* col_scale;
+    const uint8_t* live;
+    float* dw;
+    int64_t dw_stride;
+} iodf_wgrad;
+int iodf_weight_grad(const iodf_wgrad* args, void* work, int64_t work_bytes, void* stream);
+int iodf_weight_grad_workspace(const iodf_wgrad* args, int64_t* bytes);
+
 /* Read one IODF_Q_* quantity into *out (host). */
 int iodf_query(iodf_ctx* ctx, int what, int64_t* out);
 

@@ -24,12 +24,40 @@ IODF_Q_Z_ELEMS, IODF_Q_CODE_BYTES, IODF_Q_WORKSPACE_BYTES, IODF_Q_MACS_FORWARD, 
 EXPORTS = ["iodf_init", "iodf_forward", "iodf_inverse", "iodf_query", "iodf_free", "iodf_strerror",
            "iodf_last_hip_error", "iodf_profile_begin", "iodf_profile_end", "iodf_prior_cf", "iodf_encode",
            "iodf_decode", "iodf_codec_tables", "iodf_tile_patches", "iodf_untile_patches",
-           "iodf_conv_probe", "iodf_encode_noalloc", "iodf_conv_probe_timeline"]
+           "iodf_conv_probe", "iodf_encode_noalloc", "iodf_conv_probe_timeline", "iodf_pack", "iodf_unpack",
+           "iodf_join_forward", "iodf_join_backward", "iodf_join_workspace", "iodf_glu_forward", "iodf_glu_backward",
+           "iodf_weight_grad", "iodf_weight_grad_workspace"]
+
+IODF_T_F32, IODF_T_BF16, IODF_T_F16 = range(3)
+IODF_ACT_RELU, IODF_ACT_SILU, IODF_ACT_GELU = range(3)
 
 
 class KernelStat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 48), ("launches", ctypes.c_int64), ("total_ms", ctypes.c_double),
                 ("macs", ctypes.c_int64), ("bytes", ctypes.c_int64), ("issued_macs", ctypes.c_int64)]
+
+
+class JoinArgs(ctypes.Structure):
+    _fields_ = ([("rows", ctypes.c_int64), ("gate_rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("stream_type", ctypes.c_int32),
+                 ("block_type", ctypes.c_int32), ("eps", ctypes.c_float)] +
+                [(n, ctypes.c_void_p) for n in ("alpha", "gate", "w_post", "w_pre", "live", "in_stream", "in_block", "out_stream",
+                                                "out_block")] +
+                [(n, ctypes.c_int64) for n in ("in_stream_stride", "in_block_stride", "out_stream_stride", "out_block_stride")] +
+                [(n, ctypes.c_void_p) for n in ("xq", "xe", "nq", "ne", "inv_pre", "inv_post", "dalpha", "dgate", "dw_post", "dw_pre")])
+
+
+class GluArgs(ctypes.Structure):
+    _fields_ = ([("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("type", ctypes.c_int32), ("act", ctypes.c_int32)] +
+                [(n, ctypes.c_void_p) for n in ("live", "a", "b", "y", "dy", "da", "db")] +
+                [(n, ctypes.c_int64) for n in ("a_stride", "b_stride", "y_stride", "dy_stride", "da_stride", "db_stride")] +
+                [(n, ctypes.c_void_p) for n in ("aq", "ae", "bq", "be", "yq", "ye")])
+
+
+class WgradArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("out", ctypes.c_int32), ("dy_type", ctypes.c_int32),
+                ("accumulate", ctypes.c_int32), ("dy", ctypes.c_void_p), ("dy_stride", ctypes.c_int64), ("q", ctypes.c_void_p),
+                ("e", ctypes.c_void_p), ("col_scale", ctypes.c_void_p), ("live", ctypes.c_void_p), ("dw", ctypes.c_void_p),
+                ("dw_stride", ctypes.c_int64)]
 
 
 class IodfError(RuntimeError):
@@ -112,6 +140,20 @@ def load_library(build_if_missing=True):
     L.iodf_tile_patches.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp]
     L.iodf_untile_patches.restype = ci
     L.iodf_untile_patches.argtypes = [vp, vp, ci, ci, vp, ci, ci, vp]
+    i64, args = ctypes.c_int64, ctypes.POINTER
+    L.iodf_pack.restype = ci
+    L.iodf_pack.argtypes = [vp, ci, i64, i64, ci, vp, vp, vp, vp]
+    L.iodf_unpack.restype = ci
+    L.iodf_unpack.argtypes = [vp, vp, i64, ci, vp, ci, i64, vp]
+    for name, kind in (("iodf_join_forward", JoinArgs), ("iodf_glu_forward", GluArgs), ("iodf_glu_backward", GluArgs)):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [args(kind), vp]
+    for name, kind in (("iodf_join_backward", JoinArgs), ("iodf_weight_grad", WgradArgs)):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [args(kind), vp, i64, vp]
+    for name, kind in (("iodf_join_workspace", JoinArgs), ("iodf_weight_grad_workspace", WgradArgs)):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [args(kind), args(i64)]
     _LIB = L
     return L
 
@@ -205,6 +247,46 @@ def iodf_conv_probe_timeline(x, w, bias, m, shift, relu=True, iters=20, max_tile
                                                    p(x), p(w), p(bias), p(m), p(shift), p(y), int(iters),
                                                    ctypes.byref(us), p(tl), int(max_tiles), ctypes.byref(n)))
     return y, float(us.value), tl[:n.value]
+
+
+def iodf_pack(x_ptr, x_type, x_stride, rows, cols, live_ptr, q_ptr, e_ptr, stream):
+    _check(load_library().iodf_pack(x_ptr, x_type, x_stride, rows, cols, live_ptr, q_ptr, e_ptr, stream))
+
+
+def iodf_unpack(q_ptr, e_ptr, rows, cols, y_ptr, y_type, y_stride, stream):
+    _check(load_library().iodf_unpack(q_ptr, e_ptr, rows, cols, y_ptr, y_type, y_stride, stream))
+
+
+def iodf_join_forward(args, stream):
+    _check(load_library().iodf_join_forward(args, stream))
+
+
+def iodf_join_workspace(args):
+    n = ctypes.c_int64(0)
+    _check(load_library().iodf_join_workspace(args, n))
+    return n.value
+
+
+def iodf_join_backward(args, work_ptr, work_bytes, stream):
+    _check(load_library().iodf_join_backward(args, work_ptr, work_bytes, stream))
+
+
+def iodf_glu_forward(args, stream):
+    _check(load_library().iodf_glu_forward(args, stream))
+
+
+def iodf_glu_backward(args, stream):
+    _check(load_library().iodf_glu_backward(args, stream))
+
+
+def iodf_weight_grad_workspace(args):
+    n = ctypes.c_int64(0)
+    _check(load_library().iodf_weight_grad_workspace(args, n))
+    return n.value
+
+
+def iodf_weight_grad(args, work_ptr, work_bytes, stream):
+    _check(load_library().iodf_weight_grad(args, work_ptr, work_bytes, stream))
 
 
 def iodf_codec_tables():

@@ -16,6 +16,7 @@
 #include <string>
 #include <vector>
 
+#include "block.h"
 #include "chain.h"
 #include "codec_kernels.h"
 #include "conv.h"
@@ -1175,6 +1176,12 @@ int run_net(iodf_ctx* ctx, const DevNet& N, int batch, int mode_sign, int8_t* co
 static const int32_t* partial_of(const iodf_ctx* ctx) { return ctx->raw; }
 
 }  // namespace
+
+int iodf::report_hip(hipError_t e) {
+    if (e == hipSuccess) return IODF_OK;
+    g_last_hip = (int)e;
+    return IODF_E_HIP;
+}
 
 extern "C" {
 
