@@ -155,9 +155,27 @@ __device__ __forceinline__ u32x2 encode8(const float v[8], uint32_t& e) {
     return finite ? u32x2{w[0], w[1]} : u32x2{0, 0};
 }
 
+// Two instructions a value: with its sign bit turned a code is a byte 128 above its value, which one instruction takes out of the word
+// and makes a float; (q + 128) step - 128 step is exact.
 __device__ __forceinline__ void decode8(u32x2 q, float step, float v[8]) {
+    const float low = -128.f * step;
+    const uint32_t w[2] = {q[0] ^ 0x80808080u, q[1] ^ 0x80808080u};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(q[i >> 2] >> (8 * (i & 3))) * step;
+    for (int i = 0; i < 8; ++i) v[i] = fmaf((float)((w[i >> 2] >> (8 * (i & 3))) & 0xffu), step, low);
+}
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+
+// Rounded to bfloat16, two to a register.
+__device__ __forceinline__ bf8 narrow8(const float v[8]) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    union { uint32_t w[4]; bf8 all; } u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bf2 p = {(__bf16)v[2 * i], (__bf16)v[2 * i + 1]};
+        u.w[i] = __builtin_bit_cast(uint32_t, p);
+    }
+    return u.all;
 }
 
 // One row's codes at columns c0.. (a multiple of 8) of a checkpoint with `pitch` columns.

@@ -8,12 +8,12 @@
 #include "block_dev.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace iodf {
 
 namespace {
 
-typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -23,11 +23,12 @@ constexpr int KT = 32;  // rows of a tile: two matrix instructions deep
 template <typename T> constexpr int parts_of() { return sizeof(T) == 4 ? 3 : 1; }
 template <> constexpr int parts_of<_Float16>() { return 2; }
 
-// Sixteen-byte chunk of column chunk c8 of row r of a tile W columns wide. The four rows that sixteen lanes read together would lie on
-// the same banks; moved by 64 bytes a row they cover 256 bytes.
+// Where column chunk c8 (sixteen bytes) of row r of a tile W columns wide lies. The four rows that sixteen lanes read together would be on
+// the same banks; moved by 64 bytes a row they cover 256 bytes. Every other eight chunks change places in pairs, for the lanes that
+// write two chunks each and so every second one at a time.
 template <int W>
 __device__ __forceinline__ int chunk_at(int r, int c8) {
-    return r * (W / 8) + (W >= 128 ? c8 ^ ((r & 3) << 2) : c8 ^ ((r & 2) << 1));
+    return r * (W / 8) + (W >= 128 ? c8 ^ ((r & 3) << 2) ^ (c8 >> 3 & 1) : c8 ^ ((r & 2) << 1));
 }
 
 template <int W>
@@ -39,18 +40,34 @@ __device__ __forceinline__ bf8 fragment(const __bf16* tile, int off, int step) {
     return f.v;
 }
 
+struct Tiles {
+    int m, n, splits, slice;  // tiles of outputs, slices of the rows and rows of a slice
+};
+
+// Which tile and slice a workgroup takes. Workgroups go round the eight dies (each with an L2 of its own) in turn; a die gets neighbours: the
+// tiles of one slice, in blocks four tiles high, so that a panel of either operand is fetched into as few L2s as may be.
+__device__ __forceinline__ void place(const Tiles& t, int& m, int& n, int& split) {
+    const unsigned all = gridDim.x, share = all / 8, b = blockIdx.x;
+    const unsigned l = b < share * 8 ? b % 8 * share + b / 8 : b, tiles = t.m * t.n;
+    split = (int)(l / tiles);
+    const unsigned k = l - split * tiles, band = k / (4 * t.n), in = k - band * 4 * t.n;
+    const unsigned high = min(4u, t.m - band * 4);
+    m = (int)(band * 4 + in % high);
+    n = (int)(in / high);
+}
+
 template <typename TY, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_wgrad(const iodf_wgrad a, int tiles_m, int tiles_n, int slice,
-                                                                     float* partial) {
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_wgrad(const iodf_wgrad a, const Tiles tiles, float* partial) {
     constexpr int THREADS = (BM / WM) * (BN / WN) * 64, P = parts_of<TY>(), MT = WM / 32, NT = WN / 32;
     constexpr int AL = KT * BM / 8 / THREADS, BL = KT * BN / 8 / THREADS;
     __shared__ __bf16 at[2][P][KT * BM];
     __shared__ __bf16 bt[2][KT * BN];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int tile = blockIdx.x % (tiles_m * tiles_n), split = blockIdx.x / (tiles_m * tiles_n);
-    const int m0 = tile / tiles_n * BM, n0 = tile % tiles_n * BN;
+    int m0, n0, split;
+    place(tiles, m0, n0, split);
+    m0 *= BM, n0 *= BN;
     const int pitch = (a.cols + 31) / 32 * 32;
-    const long long t0 = (long long)split * slice, t1 = min((long long)a.rows, t0 + slice);
+    const long long t0 = (long long)split * tiles.slice, t1 = min((long long)a.rows, t0 + tiles.slice);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
 
     int a_off[MT], b_off[NT];
@@ -107,10 +124,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_wgrad(const iodf
             const int k = threadIdx.x + i * THREADS, at16 = chunk_at<BN>(k / (BN / 8), k % (BN / 8)) * 8;
             float v[8];
             decode8(bq[i], bs[i], v);
-            bf8 w;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = (__bf16)v[j];
-            *(bf8*)&bt[buf][at16] = w;
+            *(bf8*)&bt[buf][at16] = narrow8(v);
         }
     };
 
@@ -172,45 +186,311 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_wgrad(const iodf
     }
 }
 
-// The slices' sums, in the order of the slices.
-__global__ __launch_bounds__(256) void k_wgrad_join(const iodf_wgrad a, int splits, const float* partial) {
-    const long long n = (long long)a.out * a.cols, i = blockIdx.x * 256ll + threadIdx.x;
-    if (i >= n) return;
-    float s = 0.f;
-    for (int k = 0; k < splits; ++k) s += partial[k * n + i];
-    const int o = (int)(i / a.cols), c = (int)(i - (long long)o * a.cols);
-    float* const d = a.dw + o * a.dw_stride + c;
-    *d = (a.accumulate ? *d : 0.f) + (a.col_scale ? a.col_scale[c] : 1.f) * s;
+// ---- large layers, dy in bfloat16 ----
+// 256 x 256 outputs to a workgroup of eight waves, 128 x 64 to a wave, two waves to a SIMD. A product keeps a SIMD's matrix core for 32
+// clocks and lets about four plain vector instructions of the same wave pass beside it, so all else is dealt out between the products.
+// Tile i takes two phases of eight products a wave, one for each step:
+//   A  products of step 0, held in registers; reads step 1; widens the second half of tile i + 1's codes
+//   the one barrier of a tile
+//   B  products of step 1; reads step 0 of tile i + 1; widens the first half of tile i + 2's codes; starts dy of tile i + 4 and codes of tile i + 5
+// All loads go straight to LDS, dy to a ring of four tiles, codes to a ring in which every lane has its own places, from which
+// it takes them a phase before it widens them. No load lands in a register, so that no wait is the compiler's; wait_loads leaves the loads
+// of a tile and a half in flight.
+// 16384 rows, 4096 x 4096 weights: 460 to 470 us, 1170 to 1195 TFLOP/s, 1690 clocks a tile where the products alone take 1024; the clock
+// sinks from 2.2 to 1.83 GHz under it, so that clocks saved come back as time only in part (the products alone, without loads, widening or
+// LDS writes: 361 us). Four waves of 128 x 128, which read a third less from LDS: 487; codes and dy through registers: 505.
+//
+// Loads carry no bounds checks except near a slice's end: a chunk of dy that sticks out of its row reads the next one's start, and
+// chunks past the last column repeat the first; both only reach outputs that are not stored.
+constexpr int WIDE = 256, RING = 4;
+constexpr int kLiveRows = 1 << 17;  // of a slice, whose padding is kept as bits in LDS
+
+// Sixteen bytes or one byte (as a word) a lane from memory to LDS, lane after lane from `lds` on. Written out because the compiler, where it
+// knows of such a load, waits for all of them before any LDS access that may meet one.
+__device__ __forceinline__ void start_lds16(uint32_t lds, const void* base, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void start_lds16(uint32_t lds, const void* p) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+__device__ __forceinline__ void start_lds1(uint32_t lds, const void* base, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
 }
 
-struct Plan {
-    int tile, tiles_m, tiles_n, slice, splits;
+__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};  // what a padded row of dy is read from
+
+template <bool LIVE>
+__global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const Tiles tiles, float* partial) {
+    constexpr int THREADS = 512, NT = 2;
+    constexpr int LOADS = 4;  // of a thread and tile: sixteen codes, an exponent, two chunks of dy
+    __shared__ __bf16 at[RING][KT * WIDE];
+    __shared__ __bf16 bt[2][KT * WIDE];
+    __shared__ u32x4 raw[RING][512];
+    __shared__ uint32_t raw_e[RING][512];
+    __shared__ uint32_t alive[LIVE ? kLiveRows / 32 : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int m0, n0, split;
+    place(tiles, m0, n0, split);
+    m0 *= WIDE, n0 *= WIDE;
+    const int pitch = (a.cols + 31) / 32 * 32, epitch = pitch / 32;
+    const long long t0 = (long long)split * tiles.slice, t1 = min((long long)a.rows, t0 + tiles.slice);
+    const int wm = wave / 4 * 128, wn = wave % 4 * 64;
+
+    // what this thread loads: chunks of eight of dy in rows ar and ar + 16, sixteen codes in row br, an exponent (each one twice a wave). A
+    // chunk of dy goes to the place in LDS that its lane has, so the lane takes the chunk that belongs there.
+    const int ar = tid / 32, slot = (tid % 32) ^ ((ar & 3) << 2), ac = slot ^ (slot >> 3 & 1);
+    const int br = tid / 16, bc = tid % 16, er = wave * 4 + (lane >> 3 & 3), ec = n0 / 32 + (lane & 7);
+    const int acol = m0 + ac * 8 < a.out ? m0 + ac * 8 : 0, bcol = n0 + bc * 16 < pitch ? n0 + bc * 16 : 0;
+    const unsigned a_voff = (unsigned)(ar * (unsigned)a.dy_stride + acol) * 2, a_step = 16 * (unsigned)a.dy_stride * 2;
+    const unsigned b_voff = (unsigned)(br * pitch + bcol), e_voff = (unsigned)(er * epitch + (ec < epitch ? ec : 0));
+    auto lds_of = [](const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; };
+    const uint32_t at0 = lds_of(&at[0][0]) + wave * 1024, raw0 = lds_of(&raw[0][0]) + wave * 1024, rawe0 = lds_of(&raw_e[0][0]) + wave * 256;
+
+    if (LIVE) {  // bit r of word k: row t0 + 32 k + r is no padding
+        const int words = (int)((t1 - t0 + 31) / 32);
+        for (int k = tid; k < words; k += THREADS) {
+            uint32_t w = 0;
+            for (int r = 0; r < 32; ++r) {
+                const long long row = t0 + k * 32ll + r;
+                if (row < t1 && a.live[row]) w |= 1u << r;
+            }
+            alive[k] = w;
+        }
+        __syncthreads();
+    }
+
+    auto start_dy = [&](int to, long long t, auto guarded) {
+        const char* const ab = (const char*)a.dy + t * a.dy_stride * 2;
+        const uint32_t live = LIVE && !guarded ? alive[(t - t0) / 32] : 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = ar + 16 * i;
+            if (!guarded) {
+                const uint32_t lds = at0 + to * (KT * WIDE * 2) + i * (THREADS * 16);
+                if (LIVE) start_lds16(lds, live >> r & 1 ? ab + (a_voff + i * a_step) : (const char*)kZeros);
+                else start_lds16(lds, ab, a_voff + i * a_step);
+            } else {
+                const int n = t + r < t1 && (!LIVE || a.live[t + r]) ? a.out - acol : 0;
+                const __bf16* const p = (const __bf16*)(ab + (a_voff + i * a_step));
+                u32x4 w;
+                if (n >= 8) {
+                    w = *(const u32x4_any*)p;
+                } else {
+                    __bf16 v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (__bf16)0.f;
+                    __builtin_memcpy(&w, v, 16);
+                }
+                *(u32x4*)&at[to][(i * THREADS + tid) * 8] = w;
+            }
+        }
+    };
+    auto start_codes = [&](int to, long long t, auto guarded) {
+        const char* const bb = (const char*)a.q + t * pitch;
+        const uint8_t* const eb = a.e + t * epitch;
+        if (!guarded) {
+            start_lds16(raw0 + to * 8192, bb, b_voff);
+            start_lds1(rawe0 + to * 2048, eb, e_voff);
+        } else {
+            raw[to][tid] = t + br < t1 ? *(const u32x4*)(bb + b_voff) : u32x4{0, 0, 0, 0};
+            raw_e[to][tid] = t + er < t1 ? eb[e_voff] : 16;
+        }
+    };
+    // a thread widens eight of its sixteen codes in either phase
+    u32x2 codes[2];
+    uint32_t ex[2];
+    auto take_codes = [&](int half, int from) {
+        codes[half] = ((const u32x2*)&raw[from][tid])[half];
+        ex[half] = raw_e[from][wave * 64 + (br & 3) * 8 + bc / 2];
+    };
+    auto widen = [&](int half, int to) {
+        float v[8];
+        decode8(codes[half], code_step(ex[half]), v);
+        *(bf8*)&bt[to][chunk_at<WIDE>(br, bc * 2 + half) * 8] = narrow8(v);
+    };
+
+    int a_off[4], b_off[NT];
+    const int fr = (lane >> 5) * 8 + ((lane >> 2) & 3), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) a_off[m] = chunk_at<WIDE>(fr, (wm + m * 32 + fc) / 8) * 8 + (fc & 7);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) b_off[n] = chunk_at<WIDE>(fr, (wn + n * 32 + fc) / 8) * 8 + (fc & 7);
+    f32x16 acc[4][NT];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.f;
+    bf8 fa[2][4], fb[2][NT];
+    auto read = [&](int set, int abuf, int bbuf, int step) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) fb[set][n] = fragment<WIDE>(bt[bbuf], b_off[n], step);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) fa[set][m] = fragment<WIDE>(at[abuf], a_off[m], step);
+    };
+    auto multiply = [&](int set, int half) {
+#pragma unroll
+        for (int m = 2 * half; m < 2 * half + 2; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[set][m], fb[set][n], acc[m][n], 0, 0, 0);
+    };
+    auto barrier = [&] {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    const std::true_type checked;
+    const std::false_type whole;
+    // the loads of a tile count LOADS and follow one another as in phase B
+    auto begin = [&](auto guarded) {
+        start_codes(0, t0, guarded);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            start_codes(k + 1, t0 + (k + 1) * KT, guarded);
+            start_dy(k, t0 + k * KT, guarded);
+        }
+        wait_loads<guarded ? 0 : 2 * LOADS>();
+        take_codes(0, 0), take_codes(1, 0);
+        widen(0, 0), widen(1, 0);
+        take_codes(0, 1), take_codes(1, 1);
+        widen(0, 1);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        start_codes(0, t0 + 4 * KT, guarded);
+        start_dy(3, t0 + 3 * KT, guarded);
+    };
+    if (t0 + 6 * KT < t1) begin(whole);
+    else begin(checked);
+    barrier();
+    read(0, 0, 0, 0);
+
+    // Half a phase: left to itself the compiler gathers reads and writes behind the products.
+    auto deal = [](auto reads) {
+#pragma unroll
+        for (int k = 0; k < 2 * NT; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (reads) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto four_tiles = [&](long long t, auto guarded) {
+#pragma unroll
+        for (int h = 0; h < RING; ++h, t += KT) {
+            const int now = h & 1, next = now ^ 1;
+            read(1, h, now, 1);
+            take_codes(0, (h + 2) % RING);
+            widen(1, next);
+            multiply(0, 0);
+            deal(std::true_type());
+            multiply(0, 1);
+            deal(std::false_type());
+            wait_loads<guarded ? 0 : 2 + LOADS>();  // dy of tile i + 1 and codes of tile i + 3 have landed
+            barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            start_codes((h + 1) % RING, t + 5 * KT, guarded);
+            read(0, (h + 1) % RING, next, 0);
+            take_codes(1, (h + 2) % RING);
+            widen(0, now);
+            multiply(1, 0);
+            deal(std::true_type());
+            start_dy(h, t + 4 * KT, guarded);
+            multiply(1, 1);
+            deal(std::false_type());
+        }
+    };
+    long long t = t0;
+    for (; t + 9 * KT < t1; t += RING * KT) four_tiles(t, whole);
+    for (; t < t1; t += RING * KT) four_tiles(t, checked);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int c = n0 + wn + n * 32 + (lane & 31);
+        if (c >= a.cols) continue;
+        const float scale = !partial && a.col_scale ? a.col_scale[c] : 1.f;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int o = m0 + wm + m * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+                if (o >= a.out) continue;
+                if (partial) {
+                    partial[((long long)split * a.out + o) * a.cols + c] = acc[m][n][i];
+                } else {
+                    float* const d = a.dw + o * a.dw_stride + c;
+                    *d = (a.accumulate ? *d : 0.f) + scale * acc[m][n][i];
+                }
+            }
+    }
+}
+
+// The slices' sums, in an order that their number alone decides: JL threads to an output, or to four neighbours (VEC).
+constexpr int JL = 8;
+
+template <int VEC>
+__global__ __launch_bounds__(256) void k_wgrad_join(const iodf_wgrad a, int splits, const float* partial) {
+    typedef float vec __attribute__((ext_vector_type(VEC)));
+    __shared__ vec meet[JL][256 / JL];
+    const int lane = threadIdx.x / (256 / JL), at = threadIdx.x % (256 / JL);
+    const long long n = (long long)a.out * a.cols, i = (blockIdx.x * (256ll / JL) + at) * VEC;
+    vec s = 0.f;
+    if (i < n) {
+        int k = lane;
+        for (; k + 3 * JL < splits; k += 4 * JL) {
+            vec v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = *(const vec*)(partial + (k + u * JL) * n + i);
+            s += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        for (; k < splits; k += JL) s += *(const vec*)(partial + k * n + i);
+    }
+    meet[lane][at] = s;
+    __syncthreads();
+    if (lane || i >= n) return;
+#pragma unroll
+    for (int k = 1; k < JL; ++k) s += meet[k][at];
+    const int o = (int)(i / a.cols), c = (int)(i - (long long)o * a.cols);
+    float* const d = a.dw + o * a.dw_stride + c;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) d[j] = (a.accumulate ? d[j] : 0.f) + (a.col_scale ? a.col_scale[c + j] : 1.f) * s[j];
+}
+
+struct Plan : Tiles {
+    int tile;  // its edge
 };
 
 Plan plan_of(const iodf_wgrad& a) {
     Plan p;
     auto tiles = [&](int b) { return (long long)((a.out + b - 1) / b) * ((a.cols + b - 1) / b); };
     p.tile = tiles(128) * ((a.rows + 255) / 256) >= 256 ? 128 : 64;
-    if (a.dy_type == IODF_T_BF16 && a.out > 128 && a.cols > 128 && tiles(256) * ((a.rows + 1023) / 1024) >= 256) p.tile = 256;
-    p.tiles_m = (a.out + p.tile - 1) / p.tile;
-    p.tiles_n = (a.cols + p.tile - 1) / p.tile;
-    const long long n = (long long)p.tiles_m * p.tiles_n;
+    if (a.dy_type == IODF_T_BF16 && a.dy_stride <= (1 << 24) && a.out > 128 && a.cols > 128 && tiles(256) * ((a.rows + 1023) / 1024) >= 256)
+        p.tile = 256;
+    p.m = (a.out + p.tile - 1) / p.tile;
+    p.n = (a.cols + p.tile - 1) / p.tile;
+    const long long n = (long long)p.m * p.n;
     long long splits = std::max<long long>(1, 256 / n);
     splits = std::min<long long>(splits, std::max<long long>(1, a.rows / 128));
-    p.slice = (int)(((a.rows + splits - 1) / splits + KT - 1) / KT * KT);
+    if (a.live) splits = std::max<long long>(splits, (a.rows + kLiveRows - 1) / kLiveRows);
+    const int unit = p.tile == WIDE ? RING * KT : KT;  // what the loop takes at a time
+    p.slice = (int)(((a.rows + splits - 1) / splits + unit - 1) / unit * unit);
     p.splits = p.slice ? (int)((a.rows + p.slice - 1) / p.slice) : 1;
     return p;
 }
 
 template <typename TY>
 hipError_t run(const iodf_wgrad& a, const Plan& p, float* partial, hipStream_t st) {
-    const unsigned blocks = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
+    const unsigned blocks = (unsigned)(p.m * p.n * p.splits);
     if (p.tile == 256) {
-        if constexpr (parts_of<TY>() == 1) k_wgrad<TY, 256, 256, 128, 64><<<blocks, 512, 0, st>>>(a, p.tiles_m, p.tiles_n, p.slice, partial);
+        if (a.live) k_wgrad_wide<true><<<blocks, 512, 0, st>>>(a, p, partial);
+        else k_wgrad_wide<false><<<blocks, 512, 0, st>>>(a, p, partial);
     } else if (p.tile == 128) {
-        k_wgrad<TY, 128, 128, 64, 64><<<blocks, 256, 0, st>>>(a, p.tiles_m, p.tiles_n, p.slice, partial);
+        k_wgrad<TY, 128, 128, 64, 64><<<blocks, 256, 0, st>>>(a, p, partial);
     } else {
-        k_wgrad<TY, 64, 64, 32, 32><<<blocks, 256, 0, st>>>(a, p.tiles_m, p.tiles_n, p.slice, partial);
+        k_wgrad<TY, 64, 64, 32, 32><<<blocks, 256, 0, st>>>(a, p, partial);
     }
     return hipGetLastError();
 }
@@ -230,7 +510,8 @@ hipError_t launch_weight_grad(const iodf_wgrad& a, void* work, hipStream_t st) {
                                                     : run<_Float16>(a, p, partial, st);
     if (e != hipSuccess || !partial) return e;
     const long long n = (long long)a.out * a.cols;
-    k_wgrad_join<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(a, p.splits, partial);
+    if (a.cols % 4 == 0) k_wgrad_join<4><<<(unsigned)((n / 4 + 31) / 32), 256, 0, st>>>(a, p.splits, partial);
+    else k_wgrad_join<1><<<(unsigned)((n + 31) / 32), 256, 0, st>>>(a, p.splits, partial);
     return hipGetLastError();
 }
 
