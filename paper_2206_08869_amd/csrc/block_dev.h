@@ -13,49 +13,53 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ float f32_of(float v) { return v; }
-__device__ __forceinline__ float f32_of(__bf16 v) { return (float)v; }
-__device__ __forceinline__ float f32_of(_Float16 v) { return (float)v; }
-
+// Eight elements as they lie in memory: what a load that is not waited for yet holds.
 template <typename T>
-__device__ __forceinline__ void widen8(const T* p, float v[8]);
+struct Raw8 {
+    uint32_t w[2 * sizeof(T)];
+};
 
-template <>
-__device__ __forceinline__ void widen8<float>(const float* p, float v[8]) {
-    const u32x4_any a = *(const u32x4_any*)p, b = *(const u32x4_any*)(p + 4);
+// From p on, of which the first n exist (n <= 0: none); the others are 0.
+template <typename T>
+__device__ __forceinline__ Raw8<T> fetch8(const T* p, int n) {
+    Raw8<T> r;
+    if (n >= 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const u32x4_any a = *(const u32x4_any*)((const char*)p + 16 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.w[4 * i + j] = a[j];
+        }
+    } else {
+        T t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = i < n ? p[i] : (T)0.f;
+        __builtin_memcpy(r.w, t, sizeof(t));
+    }
+    return r;
+}
+
+__device__ __forceinline__ void widen8(const Raw8<float>& r, float v[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+}
+__device__ __forceinline__ void widen8(const Raw8<__bf16>& r, float v[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        v[i] = __uint_as_float(a[i]);
-        v[4 + i] = __uint_as_float(b[i]);
+        v[2 * i] = __uint_as_float(r.w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
     }
 }
-template <>
-__device__ __forceinline__ void widen8<__bf16>(const __bf16* p, float v[8]) {
-    const u32x4_any a = *(const u32x4_any*)p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(a[i] << 16);
-        v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-    }
-}
-template <>
-__device__ __forceinline__ void widen8<_Float16>(const _Float16* p, float v[8]) {
-    const u32x4_any a = *(const u32x4_any*)p;
+__device__ __forceinline__ void widen8(const Raw8<_Float16>& r, float v[8]) {
     _Float16 h[8];
-    __builtin_memcpy(h, &a, 16);
+    __builtin_memcpy(h, r.w, 16);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
 }
 
-// Eight elements from p on, of which the first n exist (n <= 0: none); the others read as 0.
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, int n, float v[8]) {
-    if (n >= 8) {
-        widen8(p, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? f32_of(p[i]) : 0.f;
-    }
+    widen8(fetch8(p, n), v);
 }
 
 // Rounded to nearest, ties to even.
@@ -87,8 +91,8 @@ constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIR
 // Sum over aligned runs of LPR lanes, the same in each of them.
 template <int LPR>
 __device__ __forceinline__ float lanes_sum(float v) {
-    v += __uint_as_float(dpp<DPP_XOR1>(__float_as_uint(v)));
-    v += __uint_as_float(dpp<DPP_XOR2>(__float_as_uint(v)));
+    if (LPR >= 2) v += __uint_as_float(dpp<DPP_XOR1>(__float_as_uint(v)));
+    if (LPR >= 4) v += __uint_as_float(dpp<DPP_XOR2>(__float_as_uint(v)));
     if (LPR >= 8) v += __uint_as_float(dpp<DPP_HALF_MIRROR>(__float_as_uint(v)));
     if (LPR >= 16) v += __uint_as_float(dpp<DPP_MIRROR>(__float_as_uint(v)));
     if (LPR >= 32) {
@@ -102,21 +106,30 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return v;
 }
 
-// Sum over the LPR threads of a row. Past a wave the sums meet in LDS: `slot` [waves] is the caller's, a slot of its own for each sum
-// that a row takes, so that one barrier a sum is enough (the next row's first write lies behind this row's last barrier as
-// long as a row takes at least two sums; rows with one alternate between two slots).
-template <int LPR>
-__device__ __forceinline__ float row_sum(float v, float* slot) {
-    v = lanes_sum<(LPR < 64 ? LPR : 64)>(v);
-    if (LPR > 64) {
-        constexpr int W = LPR > 64 ? LPR / 64 : 1;
-        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.f;
+// N sums over the LPR threads of a row. Past a wave they meet in LDS, in two places by turns (`turn` counts the calls): with one barrier a
+// call, nobody writes a place again before everybody has read it.
+template <int LPR, int N>
+struct RowSums {
+    static constexpr int WAVES = LPR > 64 ? LPR / 64 : 1, W = WAVES <= 2 ? WAVES : WAVES <= 4 ? 4 : WAVES <= 8 ? 8 : 16;
+    float at[2][N][W];
+};
+template <int LPR, int N>
+__device__ __forceinline__ void row_sums(float v[N], RowSums<LPR, N>& meet, int& turn) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) v += slot[i];
+    for (int k = 0; k < N; ++k) v[k] = lanes_sum<(LPR < 64 ? LPR : 64)>(v[k]);
+    if (LPR > 64) {
+        constexpr int W = RowSums<LPR, N>::W;
+        float* const at = &meet.at[turn++ & 1][0][0];
+        const int lane = threadIdx.x & 63;
+        if (lane == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) at[k * W + (threadIdx.x >> 6)] = v[k];
+        __syncthreads();
+        // W lanes to a sum: one read, and the results in scalar registers
+        const float mine = lanes_sum<W>(lane < N * W && lane % W < RowSums<LPR, N>::WAVES ? at[lane] : 0.f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), k * W));
     }
-    return v;
 }
 
 // ---- checkpoint ----
@@ -155,13 +168,9 @@ __device__ __forceinline__ u32x2 encode8(const float v[8], uint32_t& e) {
     return finite ? u32x2{w[0], w[1]} : u32x2{0, 0};
 }
 
-// Two instructions a value: with its sign bit turned a code is a byte 128 above its value, which one instruction takes out of the word
-// and makes a float; (q + 128) step - 128 step is exact.
 __device__ __forceinline__ void decode8(u32x2 q, float step, float v[8]) {
-    const float low = -128.f * step;
-    const uint32_t w[2] = {q[0] ^ 0x80808080u, q[1] ^ 0x80808080u};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf((float)((w[i >> 2] >> (8 * (i & 3))) & 0xffu), step, low);
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int)__builtin_amdgcn_sbfe((int)q[i >> 2], 8 * (i & 3), 8) * step;  // two instructions a value
 }
 
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
@@ -187,15 +196,32 @@ __device__ __forceinline__ void store_codes(int8_t* q, uint8_t* e, long long row
         if ((c0 & 31) == 0) e[row * (pitch / 32) + c0 / 32] = (uint8_t)ex;
     }
 }
-__device__ __forceinline__ void load_codes(const int8_t* q, const uint8_t* e, long long row, int pitch, int c0, float v[8]) {
+// Eight codes and their exponent as they lie in memory (none past the pitch: zeros).
+struct RawCodes {
+    u32x2 q;
+    uint32_t e;
+};
+__device__ __forceinline__ RawCodes fetch_codes(const int8_t* q, const uint8_t* e, long long row, int pitch, int c0) {
+    RawCodes r = {u32x2{0, 0}, 16};
     if (c0 < pitch) {
-        const u32x2 w = *(const u32x2*)(q + row * pitch + c0);
-        decode8(w, code_step(e[row * (pitch / 32) + c0 / 32]), v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        r.q = *(const u32x2*)(q + row * pitch + c0);
+        r.e = e[row * (pitch / 32) + c0 / 32];
     }
+    return r;
 }
+__device__ __forceinline__ void load_codes(const int8_t* q, const uint8_t* e, long long row, int pitch, int c0, float v[8]) {
+    const RawCodes r = fetch_codes(q, e, row, pitch, c0);
+    decode8(r.q, code_step(r.e), v);
+}
+
+// Makes the compiler forget what it has widened from these, so that it is widened again where it is used next and not held in four times the
+// registers until then.
+template <typename T>
+__device__ __forceinline__ void forget(Raw8<T>& r) {
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) asm volatile("" : "+v"(r.w[i]));
+}
+__device__ __forceinline__ void forget(RawCodes& r) { asm volatile("" : "+v"(r.q), "+v"(r.e)); }
 
 // ---- activations ----
 

@@ -11,10 +11,9 @@ namespace iodf {
 
 namespace {
 
-constexpr int TPB = 256;
-
+// Threads of a workgroup: several rows to a workgroup up to a wave a row, one row past that, whose sums meet in LDS.
 template <int LPR>
-constexpr int threads_of() { return LPR > TPB ? LPR : TPB; }
+constexpr int threads_of() { return LPR > 64 ? LPR : 256; }
 
 // coef[c] = alpha * gate[c] * w_post[c]
 __device__ __forceinline__ void load_params(const float* p, int c0, int cols, float v[8], float absent) {
@@ -30,7 +29,8 @@ __device__ __forceinline__ void load_params(const float* p, int c0, int cols, fl
 template <typename TH, typename TF, int LPR, int NV>
 __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_join a) {
     constexpr int TEAMS = threads_of<LPR>() / LPR;
-    __shared__ float sums[2][LPR > 64 ? LPR / 64 : 1];
+    __shared__ RowSums<LPR, 1> meet;
+    int turn = 0;
     const int team = threadIdx.x / LPR, tid = threadIdx.x % LPR;
     const int cols = a.cols, pitch = (cols + 31) / 32 * 32;
     const float inv_cols = 1.f / (float)cols;
@@ -40,7 +40,23 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
     for (int v = 0; v < NV; ++v) load_params(a.w_pre, (v * LPR + tid) * 8, cols, wq[v], 0.f);
     int group = -1;
     const int rows = (int)a.rows, gate_rows = a.gate && a.gate_rows < a.rows ? (int)a.gate_rows : 0;
-    for (int row = blockIdx.x * TEAMS + team; row < rows; row += gridDim.x * TEAMS) {
+    Raw8<TH> hr[NV];
+    Raw8<TF> fr[NV];
+    bool live = true;
+    auto fetch = [&](int row) {
+        live = !a.live || a.live[row];
+        const TH* const h = (const TH*)a.in_stream + (long long)row * a.in_stream_stride;
+        const TF* const f = (const TF*)a.in_block + (long long)row * a.in_block_stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c0 = (v * LPR + tid) * 8;
+            hr[v] = fetch8(h + c0, cols - c0);
+            fr[v] = fetch8(f + c0, live ? cols - c0 : 0);
+        }
+    };
+    int row = blockIdx.x * TEAMS + team;
+    if (row < rows) fetch(row);
+    while (row < rows) {
         const int g = gate_rows ? row / gate_rows : 0;
         if (g != group) {
             group = g;
@@ -54,16 +70,15 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
                 for (int i = 0; i < 8; ++i) coef[v][i] = c0 + i < cols ? alpha * coef[v][i] * wp[i] : 0.f;
             }
         }
-        const bool live = !a.live || a.live[row];
-        const TH* const h = (const TH*)a.in_stream + (long long)row * a.in_stream_stride;
-        const TF* const f = (const TF*)a.in_block + (long long)row * a.in_block_stride;
         float z[NV][8], n[NV][8];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            load8(h + c0, cols - c0, z[v]);
-            load8(f + c0, live ? cols - c0 : 0, n[v]);
+            widen8(hr[v], z[v]);
+            widen8(fr[v], n[v]);
         }
+        const bool now = live;
+        const int next = row + gridDim.x * TEAMS;
+        if (next < rows) fetch(next);  // on its way while this row's sums are taken
         float ip = 1.f;
         if (a.w_post) {
             float s = 0.f;
@@ -71,7 +86,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s += n[v][i] * n[v][i];
-            ip = 1.f / sqrtf(row_sum<LPR>(s, sums[0]) * inv_cols + a.eps);
+            row_sums<LPR, 1>(&s, meet, turn);
+            ip = 1.f / sqrtf(s * inv_cols + a.eps);
         }
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -87,14 +103,15 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
             store8(ho + c0, cols - c0, z[v]);
             if (a.nq) store_codes(a.nq, a.ne, row, pitch, c0, n[v]);
         }
-        if (a.inv_post && tid == 0) a.inv_post[row] = live ? ip : 0.f;
+        if (a.inv_post && tid == 0) a.inv_post[row] = now ? ip : 0.f;
         if (a.w_pre) {
             float s = 0.f;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s += z[v][i] * z[v][i];
-            const float iq = 1.f / sqrtf(row_sum<LPR>(s, sums[1]) * inv_cols + a.eps);
+            row_sums<LPR, 1>(&s, meet, turn);
+            const float iq = 1.f / sqrtf(s * inv_cols + a.eps);
             TF* const u = (TF*)a.out_block + (long long)row * a.out_block_stride;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -102,15 +119,15 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    z[v][i] = live ? z[v][i] * iq : 0.f;
+                    z[v][i] = now ? z[v][i] * iq : 0.f;
                     o[i] = z[v][i] * wq[v][i];
                 }
                 store8(u + c0, cols - c0, o);
                 if (a.xq) store_codes(a.xq, a.xe, row, pitch, c0, z[v]);
             }
-            if (a.inv_pre && tid == 0) a.inv_pre[row] = live ? iq : 0.f;
+            if (a.inv_pre && tid == 0) a.inv_pre[row] = now ? iq : 0.f;
         }
-        if (LPR > 64) __syncthreads();  // a row with one norm would otherwise meet the next row's sums in the same slot
+        row = next;
     }
 }
 
@@ -122,22 +139,25 @@ struct Runs {
 
 // dx = du * w_pre, dz = dh' + inv_pre (dx - x mean(dx x)), dn = coef dz, df = inv_post (dn - n mean(dn n)); sums over the run's rows of
 // du x and of dz n (where every row has a gate of its own: of gate dz n, and dgate is written at once).
-template <typename TH, typename TF, int LPR, int NV>
-__global__ __launch_bounds__(threads_of<LPR>()) void k_join_backward(const iodf_join a, const Runs runs, float* sum_pre, float* sum_post,
+// The second mean needs the first one, but it is linear in dz: with m = coef n,
+//   sum(dn n) = sum(m dh') + inv_pre (sum(m dx) - mean(dx x) sum(m x)),
+// so that a row meets once, for four sums, and not twice.
+template <typename TH, typename TF, int LPR, int NV, bool OWN>
+__global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 ? 3 : 4) void k_join_backward(const iodf_join a, const Runs runs, float* sum_pre, float* sum_post,
                                                                      unsigned* ticket) {
     constexpr int THREADS = threads_of<LPR>(), TEAMS = THREADS / LPR;
-    __shared__ float sums[2][LPR > 64 ? LPR / 64 : 1];
+    __shared__ RowSums<LPR, 4> meet;
+    int turn = 0;
     __shared__ float joined[TEAMS > 1 ? THREADS * 8 : 1];
     const int team = threadIdx.x / LPR, tid = threadIdx.x % LPR;
     const int cols = a.cols, pitch = (cols + 31) / 32 * 32, wide = (cols + 7) / 8 * 8;
     const float inv_cols = 1.f / (float)cols;
     const float alpha = a.alpha ? a.alpha[0] : 1.f;
-    const bool own_gate = runs.gate_rows == 1;
     if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
-    const int group = own_gate ? 0 : blockIdx.x / runs.per_group, part = own_gate ? blockIdx.x : blockIdx.x % runs.per_group;
+    const int group = OWN ? 0 : blockIdx.x / runs.per_group, part = OWN ? blockIdx.x : blockIdx.x % runs.per_group;
     const int rows = (int)a.rows;
-    const int group_end = own_gate ? rows : min((long long)rows, (long long)(group + 1) * runs.gate_rows);
-    const int first = (own_gate ? 0 : group * runs.gate_rows) + part * runs.chunk;
+    const int group_end = OWN ? rows : min((long long)rows, (long long)(group + 1) * runs.gate_rows);
+    const int first = (OWN ? 0 : group * runs.gate_rows) + part * runs.chunk;
     const int last = min((long long)group_end, (long long)first + runs.chunk);
     float coef[NV][8], wq[NV][8], pre[NV][8], post[NV][8];
 #pragma unroll
@@ -146,86 +166,97 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_backward(const iodf_
         float wp[8];
         load_params(a.w_pre, c0, cols, wq[v], 0.f);
         load_params(a.w_post, c0, cols, wp, 1.f);
-        load_params(a.gate && !own_gate ? a.gate + (long long)group * cols : nullptr, c0, cols, coef[v], 1.f);
+        load_params(a.gate && !OWN ? a.gate + (long long)group * cols : nullptr, c0, cols, coef[v], 1.f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             coef[v][i] *= alpha * wp[i];
             pre[v][i] = post[v][i] = 0.f;
         }
     }
-    for (int row = first + team; row < last; row += TEAMS) {
-        const bool live = !a.live || a.live[row];
+    struct Row {
+        Raw8<TH> h[NV];
+        Raw8<TF> u[NV];
+        RawCodes x[NV], n[NV];
+        Raw8<float> gate[OWN ? NV : 1];
+        float iq, ip;
+        bool live;
+    };
+    auto fetch = [&](int row) {
+        Row r;
+        r.live = !a.live || a.live[row];
         const TH* const dh = (const TH*)a.in_stream + (long long)row * a.in_stream_stride;
         const TF* const du = (const TF*)a.in_block + (long long)row * a.in_block_stride;
-        TH* const dho = (TH*)a.out_stream + (long long)row * a.out_stream_stride;
-        TF* const df = (TF*)a.out_block + (long long)row * a.out_block_stride;
-        float dz[NV][8], n[NV][8];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c0 = (v * LPR + tid) * 8;
-            load8(dh + c0, cols - c0, dz[v]);
-            load_codes(a.nq, a.ne, row, pitch, live ? c0 : pitch, n[v]);
+            r.h[v] = fetch8(dh + c0, cols - c0);
+            r.n[v] = fetch_codes(a.nq, a.ne, row, pitch, r.live ? c0 : pitch);
+            r.u[v] = fetch8(du + c0, a.w_pre && r.live ? cols - c0 : 0);
+            r.x[v] = fetch_codes(a.xq, a.xe, row, pitch, a.w_pre && r.live ? c0 : pitch);
+            if (OWN) r.gate[v] = fetch8(a.gate + (long long)row * cols + c0, cols - c0);
         }
-        if (a.w_pre) {
-            float x[NV][8], dx[NV][8], s = 0.f;
-            const float iq = live ? a.inv_pre[row] : 0.f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c0 = (v * LPR + tid) * 8;
-                load8(du + c0, live ? cols - c0 : 0, dx[v]);
-                load_codes(a.xq, a.xe, row, pitch, live ? c0 : pitch, x[v]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    pre[v][i] += dx[v][i] * x[v][i];
-                    dx[v][i] *= wq[v][i];
-                    s += dx[v][i] * x[v][i];
-                }
-            }
-            s = row_sum<LPR>(s, sums[0]) * inv_cols;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dz[v][i] += iq * (dx[v][i] - x[v][i] * s);
-        }
-        float s = 0.f;
-        float dn[NV][8];
+        r.iq = a.w_pre && r.live ? a.inv_pre[row] : 0.f;
+        r.ip = !a.w_post ? 1.f : r.live ? a.inv_post[row] : 0.f;
+        return r;
+    };
+    Row next;
+    int row = first + team;
+    if (row < last) next = fetch(row);
+    for (; row < last; row += TEAMS) {
+        Row r = next;
+        if (row + TEAMS < last) next = fetch(row + TEAMS);  // on its way while this row's sums are taken
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};  // of dx x, m dh', m dx, m x
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            store8(dho + c0, cols - c0, dz[v]);
-            float gate[8];
-            if (own_gate) load8(a.gate + (long long)row * cols + c0, cols - c0, gate);
-            float share[8];
+            float dh[8], du[8], x[8], n[8], gate[8];
+            widen8(r.h[v], dh);
+            widen8(r.u[v], du);
+            decode8(r.x[v].q, code_step(r.x[v].e), x);
+            decode8(r.n[v].q, code_step(r.n[v].e), n);
+            if (OWN) widen8(r.gate[v], gate);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = live ? dz[v][i] : 0.f;  // padding goes to dL/dh as it came, and nowhere else
-                share[i] = d * n[v][i];
-                dn[v][i] = coef[v][i] * d;
-                if (own_gate) {
-                    dn[v][i] *= gate[i];
+                const float m = coef[v][i] * n[i] * (OWN ? gate[i] : 1.f), dx = du[i] * wq[v][i];
+                pre[v][i] += du[i] * x[i];
+                sum[0] += dx * x[i];
+                sum[1] += m * (r.live ? dh[i] : 0.f);  // padding goes to dL/dh as it came, and nowhere else
+                sum[2] += m * dx;
+                sum[3] += m * x[i];
+            }
+            forget(r.h[v]), forget(r.u[v]), forget(r.x[v]), forget(r.n[v]);
+        }
+        row_sums<LPR, 4>(sum, meet, turn);
+        const float mean_x = sum[0] * inv_cols, mean_n = a.w_post ? (sum[1] + r.iq * (sum[2] - mean_x * sum[3])) * inv_cols : 0.f;
+        TH* const dho = (TH*)a.out_stream + (long long)row * a.out_stream_stride;
+        TF* const df = (TF*)a.out_block + (long long)row * a.out_block_stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c0 = (v * LPR + tid) * 8;
+            float dz[8], du[8], x[8], n[8], gate[8], share[8], dn[8];
+            widen8(r.h[v], dz);
+            widen8(r.u[v], du);
+            decode8(r.x[v].q, code_step(r.x[v].e), x);
+            decode8(r.n[v].q, code_step(r.n[v].e), n);
+            if (OWN) widen8(r.gate[v], gate);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dz[i] += r.iq * (du[i] * wq[v][i] - x[i] * mean_x);
+                const float d = r.live ? dz[i] : 0.f;
+                share[i] = d * n[i];
+                dn[i] = coef[v][i] * d;
+                if (OWN) {
+                    dn[i] *= gate[i];
                     post[v][i] += gate[i] * share[i];
                     share[i] *= coef[v][i];
                 } else {
                     post[v][i] += share[i];
                 }
-                s += dn[v][i] * n[v][i];
+                dn[i] = r.ip * (dn[i] - n[i] * mean_n);
             }
-            if (own_gate) store8(a.dgate + (long long)row * cols + c0, cols - c0, share);
+            store8(dho + c0, cols - c0, dz);
+            store8(df + c0, cols - c0, dn);
+            if (OWN) store8(a.dgate + (long long)row * cols + c0, cols - c0, share);
         }
-        if (a.w_post) {
-            s = row_sum<LPR>(s, sums[1]) * inv_cols;
-            const float ip = live ? a.inv_post[row] : 0.f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dn[v][i] = ip * (dn[v][i] - n[v][i] * s);
-        }
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            store8(df + c0, cols - c0, dn[v]);
-        }
-        if (LPR > 64) __syncthreads();
     }
     // the teams' sums meet in the order of the teams
     float* const to[2] = {sum_pre + (long long)blockIdx.x * wide, sum_post + (long long)blockIdx.x * wide};
@@ -251,19 +282,18 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_backward(const iodf_
         }
 }
 
-// The parameters' gradients from the runs' sums. A workgroup has FC columns and FR threads for each, which share the runs: dw_pre over
-// all, and group by group dgate = alpha w_post S, dw_post = alpha sum gate S, S a group's sum. The workgroup that ends last
+// The parameters' gradients from the runs' sums. A workgroup has FC columns and FR threads for each, which share the runs: in the second row
+// of workgroups for dw_pre, over all, in the first one group by group for dgate = alpha w_post S, dw_post = alpha sum gate S, S a group's sum. The workgroup that ends last
 // adds the workgroups' parts of dalpha = sum gate w_post S, in their order.
 constexpr int FC = 16, FR = 64;
 
 __device__ __forceinline__ float column_sum(const float* p, int n, int wide, int lane, int lanes) {
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    int r = lane;
-    for (; r + 3 * lanes < n; r += 4 * lanes)
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int r = lane; r < n; r += 8 * lanes)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] += p[(long long)(r + k * lanes) * wide];
-    for (; r < n; r += lanes) s[0] += p[(long long)r * wide];
-    return (s[0] + s[1]) + (s[2] + s[3]);
+        for (int k = 0; k < 8; ++k)
+            if (r + k * lanes < n) s[k] += p[(long long)(r + k * lanes) * wide];
+    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
 }
 
 __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const Runs runs, int n_runs, const float* sum_pre,
@@ -275,7 +305,7 @@ __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const
     const bool there = c < cols;
     const float alpha = a.alpha ? a.alpha[0] : 1.f;
     const float wp = there && a.w_post ? a.w_post[c] : 1.f;
-    if (a.dw_pre) {
+    if (blockIdx.y) {
         meet[lane][col] = there ? column_sum(sum_pre + c, n_runs, wide, lane, FR) : 0.f;
         __syncthreads();
         if (lane == 0 && there) {
@@ -283,13 +313,13 @@ __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const
             for (int k = 0; k < FR; ++k) s += meet[k][col];
             a.dw_pre[c] = (float)s;
         }
-        __syncthreads();
+        return;
     }
     // FR threads of a column are cut into `teams` for as many groups at a time
     const bool own_gate = runs.gate_rows == 1;
     const int per_group = own_gate ? n_runs : runs.per_group, groups = own_gate ? 1 : runs.groups;
-    int lanes = 1;
-    while (lanes < per_group && lanes < FR) lanes *= 2;
+    int lanes = 1;  // of a group: as many as leave every group a team of its own, where there are that many
+    while (lanes < per_group && 2 * lanes * groups <= FR) lanes *= 2;
     const int teams = FR / lanes, team = lane / lanes, sub = lane % lanes;
     double weighted = 0;  // sum over this thread's groups of gate * S
     for (int g0 = 0; g0 < groups; g0 += teams) {
@@ -319,16 +349,20 @@ __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const
         total[0][col] = there ? wp * s : 0;
     }
     __syncthreads();
-    if (a.dalpha && threadIdx.x == 0) {
+    if (!a.dalpha) return;
+    __shared__ bool is_last;
+    if (threadIdx.x == 0) {
         double s = 0;
         for (int k = 0; k < FC; ++k) s += total[0][k];
         __hip_atomic_store(&parts[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (__hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1) {
-            s = 0;
-            for (int k = 0; k < (int)gridDim.x; ++k) s += __hip_atomic_load(&parts[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            a.dalpha[0] = (float)s;
-        }
+        is_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
     }
+    __syncthreads();
+    if (!is_last || threadIdx.x >= 64) return;
+    double s = 0;
+    for (int k = threadIdx.x; k < (int)gridDim.x; k += 64) s += __hip_atomic_load(&parts[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
+    if (threadIdx.x == 0) a.dalpha[0] = (float)s;
 }
 
 template <typename TH, typename TF, int LPR, int NV>
@@ -336,31 +370,42 @@ hipError_t forward_of(const iodf_join& a, hipStream_t st) {
     constexpr int TEAMS = threads_of<LPR>() / LPR;
     const long long blocks = (a.rows + TEAMS - 1) / TEAMS;
     // a workgroup keeps the parameters of its columns in registers over several rows
-    k_join_forward<TH, TF, LPR, NV><<<(unsigned)std::min<long long>(blocks, 256 * 8), threads_of<LPR>(), 0, st>>>(a);
+    const long long most = 256 * (2048 / threads_of<LPR>());
+    k_join_forward<TH, TF, LPR, NV><<<(unsigned)std::min(blocks, most), threads_of<LPR>(), 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <typename TH, typename TF>
 hipError_t forward_types(const iodf_join& a, hipStream_t st) {
-    if (a.cols <= 64) return forward_of<TH, TF, 8, 1>(a, st);
-    if (a.cols <= 128) return forward_of<TH, TF, 16, 1>(a, st);
-    if (a.cols <= 256) return forward_of<TH, TF, 32, 1>(a, st);
-    if (a.cols <= 512) return forward_of<TH, TF, 64, 1>(a, st);
-    if (a.cols <= 1024) return forward_of<TH, TF, 64, 2>(a, st);
-    if (a.cols <= 2048) return forward_of<TH, TF, 256, 1>(a, st);
-    if (a.cols <= 4096) return forward_of<TH, TF, 256, 2>(a, st);
-    if (a.cols <= 8192) return forward_of<TH, TF, 512, 2>(a, st);
+    if (a.cols <= 8 * 8) return forward_of<TH, TF, 8, 1>(a, st);
+    if (a.cols <= 8 * 16) return forward_of<TH, TF, 16, 1>(a, st);
+    if (a.cols <= 8 * 32) return forward_of<TH, TF, 32, 1>(a, st);
+    if (a.cols <= 8 * 64) return forward_of<TH, TF, 64, 1>(a, st);
+    if (a.cols <= 8 * 128) return forward_of<TH, TF, 64, 2>(a, st);
+    if (a.cols <= 8 * 192) return forward_of<TH, TF, 192, 1>(a, st);
+    if (a.cols <= 8 * 256) return forward_of<TH, TF, 256, 1>(a, st);
+    if (a.cols <= 8 * 384) return forward_of<TH, TF, 384, 1>(a, st);
+    if (a.cols <= 8 * 512) return forward_of<TH, TF, 512, 1>(a, st);
+    if (a.cols <= 8 * 768) return forward_of<TH, TF, 768, 1>(a, st);
+    if (a.cols <= 8 * 1024) return forward_of<TH, TF, 1024, 1>(a, st);
     return forward_of<TH, TF, 1024, 2>(a, st);
 }
 
-int backward_teams(int cols) { return cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1; }
+// Threads to a row of the backward pass, one vector to each: a power of two up to a wave, then whole waves in steps of a half of the power below.
+int backward_lanes(int cols) {
+    for (int lanes : {8, 16, 32, 64, 128, 192, 256, 384, 512, 768})
+        if (cols <= 8 * lanes) return lanes;
+    return 1024;
+}
+int backward_teams(int cols) { return backward_lanes(cols) > 64 ? 1 : 256 / backward_lanes(cols); }
 
-// Runs of rows: about four workgroups to a compute unit, each with at least two rows to a team.
+// Runs of rows: a thousand threads to a compute unit, but at least four rows to a team while every unit has a workgroup: a run's sums cost as
+// much as two rows of 16 bits.
 Runs runs_of(long long rows, int cols, long long gate_rows) {
     Runs r;
     if (gate_rows > rows || gate_rows < 1) gate_rows = rows;
     const int teams = backward_teams(cols);
-    const long long want = 1024;
+    const long long most = 256 * (1024 / (backward_lanes(cols) > 64 ? backward_lanes(cols) : 256)), want = std::min(most, std::max(256ll, rows / (4 * teams)));
     r.gate_rows = (int)gate_rows;
     if (gate_rows == 1 && rows > 1) {
         r.groups = (int)rows;
@@ -393,27 +438,33 @@ hipError_t backward_of(const iodf_join& a, void* work, hipStream_t st) {
     float* const post = pre + n * wide;
     hipError_t e = hipSuccess;
     if (n) {
-        k_join_backward<TH, TF, LPR, NV><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, pre, post, ticket);
+        if (r.gate_rows == 1) k_join_backward<TH, TF, LPR, NV, true><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, pre, post, ticket);
+        else k_join_backward<TH, TF, LPR, NV, false><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, pre, post, ticket);
         e = hipGetLastError();
     } else {
         e = launch_fill_zero(ticket, 16, st);
     }
     if (e != hipSuccess) return e;
-    k_join_params<<<(unsigned)parts, FC * FR, 0, st>>>(a, r, (int)n, pre, post, part, ticket);
+    k_join_params<<<dim3((unsigned)parts, a.dw_pre ? 2 : 1), FC * FR, 0, st>>>(a, r, (int)n, pre, post, part, ticket);
     return hipGetLastError();
 }
 
 template <typename TH, typename TF>
 hipError_t backward_types(const iodf_join& a, void* w, hipStream_t st) {
-    if (a.cols <= 64) return backward_of<TH, TF, 8, 1>(a, w, st);
-    if (a.cols <= 128) return backward_of<TH, TF, 16, 1>(a, w, st);
-    if (a.cols <= 256) return backward_of<TH, TF, 32, 1>(a, w, st);
-    if (a.cols <= 512) return backward_of<TH, TF, 64, 1>(a, w, st);
-    if (a.cols <= 1024) return backward_of<TH, TF, 64, 2>(a, w, st);
-    if (a.cols <= 2048) return backward_of<TH, TF, 256, 1>(a, w, st);
-    if (a.cols <= 4096) return backward_of<TH, TF, 256, 2>(a, w, st);
-    if (a.cols <= 8192) return backward_of<TH, TF, 512, 2>(a, w, st);
-    return backward_of<TH, TF, 1024, 2>(a, w, st);
+    if (a.cols > 8 * 1024) return backward_of<TH, TF, 1024, 2>(a, w, st);
+    switch (backward_lanes(a.cols)) {
+        case 8: return backward_of<TH, TF, 8, 1>(a, w, st);
+        case 16: return backward_of<TH, TF, 16, 1>(a, w, st);
+        case 32: return backward_of<TH, TF, 32, 1>(a, w, st);
+        case 64: return backward_of<TH, TF, 64, 1>(a, w, st);
+        case 128: return backward_of<TH, TF, 128, 1>(a, w, st);
+        case 192: return backward_of<TH, TF, 192, 1>(a, w, st);
+        case 256: return backward_of<TH, TF, 256, 1>(a, w, st);
+        case 384: return backward_of<TH, TF, 384, 1>(a, w, st);
+        case 512: return backward_of<TH, TF, 512, 1>(a, w, st);
+        case 768: return backward_of<TH, TF, 768, 1>(a, w, st);
+        default: return backward_of<TH, TF, 1024, 1>(a, w, st);
+    }
 }
 
 }  // namespace
