@@ -15,6 +15,7 @@ struct Grid {
     long long rows;
     int cols, pitch;
     unsigned vectors, magic;  // vectors of a row, and floor(2^32 / vectors) + 1
+    long long over[2];        // rows of the inputs whose last vector may be read past its row
 };
 
 // Row and first column of this thread's vector k. Within a workgroup the vectors are counted from the row in which it starts, a
@@ -35,21 +36,24 @@ template <typename T>
 __global__ __launch_bounds__(TPB) void k_pack(const Grid g, const T* x, long long stride, const uint8_t* live, int8_t* q, uint8_t* e) {
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
-    float v[VECS][8];
+    Raw8<T> r[VECS];
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
         if (live && n > 0 && !live[row]) n = 0;
-        load8(x + row * stride + c0, n, v[k]);
+        r[k] = fetch8(x + row * stride + c0, n, row < g.over[0]);
     }
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
-        put_codes(g, q, e, row, c0, v[k]);
+        cut8(r[k], n);
+        float v[8];
+        widen8(r[k], v);
+        put_codes(g, q, e, row, c0, v);
     }
 }
 
@@ -57,20 +61,22 @@ template <typename T>
 __global__ __launch_bounds__(TPB) void k_unpack(const Grid g, const int8_t* q, const uint8_t* e, T* y, long long stride) {
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
-    float v[VECS][8];
+    RawCodes r[VECS];
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
-        load_codes(q, e, row, g.pitch, n > 0 ? c0 : g.pitch, v[k]);
+        r[k] = fetch_codes(q, e, row, g.pitch, n > 0 ? c0 : g.pitch);
     }
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
-        store8(y + row * stride + c0, n, v[k]);
+        float v[8];
+        decode8(r[k].q, code_step(r[k].e), v);
+        store8(y + row * stride + c0, n, v);
     }
 }
 
@@ -78,29 +84,32 @@ template <typename T, int ACT>
 __global__ __launch_bounds__(TPB) void k_glu_forward(const Grid g, const iodf_glu a) {
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
-    float x[VECS][8], y[VECS][8];
+    Raw8<T> ra[VECS], rb[VECS];
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
         if (a.live && n > 0 && !a.live[row]) n = 0;
-        load8((const T*)a.a + row * a.a_stride + c0, n, x[k]);
-        load8((const T*)a.b + row * a.b_stride + c0, n, y[k]);
+        ra[k] = fetch8((const T*)a.a + row * a.a_stride + c0, n, row < g.over[0]);
+        rb[k] = fetch8((const T*)a.b + row * a.b_stride + c0, n, row < g.over[1]);
     }
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
+        cut8(ra[k], n), cut8(rb[k], n);
+        float x[8], y[8], slope;
+        widen8(ra[k], x);
+        widen8(rb[k], y);
         if (a.aq) {
-            put_codes(g, a.aq, a.ae, row, c0, x[k]);
-            put_codes(g, a.bq, a.be, row, c0, y[k]);
+            put_codes(g, a.aq, a.ae, row, c0, x);
+            put_codes(g, a.bq, a.be, row, c0, y);
         }
-        float slope;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[k][i] *= activate<ACT>(x[k][i], slope);
-        store8((T*)a.y + row * a.y_stride + c0, n, y[k]);
+        for (int i = 0; i < 8; ++i) y[i] *= activate<ACT>(x[i], slope);
+        store8((T*)a.y + row * a.y_stride + c0, n, y);
     }
 }
 
@@ -108,30 +117,35 @@ template <typename T, int ACT>
 __global__ __launch_bounds__(TPB) void k_glu_backward(const Grid g, const iodf_glu a) {
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
-    float x[VECS][8], b[VECS][8], d[VECS][8];
+    Raw8<T> rd[VECS];
+    RawCodes ra[VECS], rb[VECS];
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
         if (a.live && n > 0 && !a.live[row]) n = 0;
-        load8((const T*)a.dy + row * a.dy_stride + c0, n, d[k]);
-        load_codes(a.aq, a.ae, row, g.pitch, n > 0 ? c0 : g.pitch, x[k]);
-        load_codes(a.bq, a.be, row, g.pitch, n > 0 ? c0 : g.pitch, b[k]);
+        rd[k] = fetch8((const T*)a.dy + row * a.dy_stride + c0, n, row < g.over[0]);
+        ra[k] = fetch_codes(a.aq, a.ae, row, g.pitch, n > 0 ? c0 : g.pitch);
+        rb[k] = fetch_codes(a.bq, a.be, row, g.pitch, n > 0 ? c0 : g.pitch);
     }
 #pragma unroll
     for (int k = 0; k < VECS; ++k) {
         long long row;
         int c0, n;
         place(g, row0, rem, k, row, c0, n);
-        float da[8], db[8], y[8];
+        cut8(rd[k], n);
+        float d[8], x[8], b[8], da[8], db[8], y[8];
+        widen8(rd[k], d);
+        decode8(ra[k].q, code_step(ra[k].e), x);
+        decode8(rb[k].q, code_step(rb[k].e), b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float slope;
-            const float act = activate<ACT>(x[k][i], slope);
-            da[i] = d[k][i] * b[k][i] * slope;
-            db[i] = d[k][i] * act;
-            y[i] = act * b[k][i];
+            const float act = activate<ACT>(x[i], slope);
+            da[i] = d[i] * b[i] * slope;
+            db[i] = d[i] * act;
+            y[i] = act * b[i];
         }
         store8((T*)a.da + row * a.da_stride + c0, n, da);
         store8((T*)a.db + row * a.db_stride + c0, n, db);
@@ -139,13 +153,15 @@ __global__ __launch_bounds__(TPB) void k_glu_backward(const Grid g, const iodf_g
     }
 }
 
-Grid grid_of(long long rows, int cols, unsigned& blocks) {
+Grid grid_of(long long rows, int cols, unsigned& blocks, long long stride0 = 0, long long stride1 = 0) {
     Grid g;
     g.rows = rows;
     g.cols = cols;
     g.pitch = code_pitch(cols);
     g.vectors = (unsigned)g.pitch / 8;
     g.magic = (unsigned)((1ull << 32) / g.vectors) + 1;
+    g.over[0] = stride0 ? over_rows(rows, cols, stride0) : 0;
+    g.over[1] = stride1 ? over_rows(rows, cols, stride1) : 0;
     blocks = (unsigned)((rows * g.vectors + TPB * VECS - 1) / (TPB * VECS));
     return g;
 }
@@ -153,7 +169,7 @@ Grid grid_of(long long rows, int cols, unsigned& blocks) {
 template <typename T>
 hipError_t glu_forward_of(const iodf_glu& a, hipStream_t st) {
     unsigned blocks;
-    const Grid g = grid_of(a.rows, a.cols, blocks);
+    const Grid g = grid_of(a.rows, a.cols, blocks, a.a_stride, a.b_stride);
     if (a.act == IODF_ACT_RELU) k_glu_forward<T, IODF_ACT_RELU><<<blocks, TPB, 0, st>>>(g, a);
     else if (a.act == IODF_ACT_SILU) k_glu_forward<T, IODF_ACT_SILU><<<blocks, TPB, 0, st>>>(g, a);
     else k_glu_forward<T, IODF_ACT_GELU><<<blocks, TPB, 0, st>>>(g, a);
@@ -163,7 +179,7 @@ hipError_t glu_forward_of(const iodf_glu& a, hipStream_t st) {
 template <typename T>
 hipError_t glu_backward_of(const iodf_glu& a, hipStream_t st) {
     unsigned blocks;
-    const Grid g = grid_of(a.rows, a.cols, blocks);
+    const Grid g = grid_of(a.rows, a.cols, blocks, a.dy_stride);
     if (a.act == IODF_ACT_RELU) k_glu_backward<T, IODF_ACT_RELU><<<blocks, TPB, 0, st>>>(g, a);
     else if (a.act == IODF_ACT_SILU) k_glu_backward<T, IODF_ACT_SILU><<<blocks, TPB, 0, st>>>(g, a);
     else k_glu_backward<T, IODF_ACT_GELU><<<blocks, TPB, 0, st>>>(g, a);
@@ -175,7 +191,7 @@ hipError_t glu_backward_of(const iodf_glu& a, hipStream_t st) {
 hipError_t launch_pack(const void* x, int type, long long stride, long long rows, int cols, const uint8_t* live, int8_t* q,
                        uint8_t* e, hipStream_t st) {
     unsigned blocks;
-    const Grid g = grid_of(rows, cols, blocks);
+    const Grid g = grid_of(rows, cols, blocks, stride);
     if (type == IODF_T_F32) k_pack<float><<<blocks, TPB, 0, st>>>(g, (const float*)x, stride, live, q, e);
     else if (type == IODF_T_BF16) k_pack<__bf16><<<blocks, TPB, 0, st>>>(g, (const __bf16*)x, stride, live, q, e);
     else k_pack<_Float16><<<blocks, TPB, 0, st>>>(g, (const _Float16*)x, stride, live, q, e);

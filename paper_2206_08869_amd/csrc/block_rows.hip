@@ -15,6 +15,13 @@ namespace {
 template <int LPR>
 constexpr int threads_of() { return LPR > 64 ? LPR : 256; }
 
+// Which of a workgroup's rows a thread has a part in. Where a wave lies within one row, its number, and with it every address that hangs on
+// it, is kept in scalar registers.
+template <int LPR>
+__device__ __forceinline__ int team_of() {
+    return LPR > 64 ? 0 : LPR == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : threadIdx.x / LPR;
+}
+
 // coef[c] = alpha * gate[c] * w_post[c]
 __device__ __forceinline__ void load_params(const float* p, int c0, int cols, float v[8], float absent) {
     if (p) {
@@ -27,31 +34,34 @@ __device__ __forceinline__ void load_params(const float* p, int c0, int cols, fl
 
 // n = f / rms(f), h' = h + coef * n, x = h' / rms(h'), u = w_pre * x.
 template <typename TH, typename TF, int LPR, int NV>
-__global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_join a) {
+__global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_join a, const int over_h, const int over_f) {
     constexpr int TEAMS = threads_of<LPR>() / LPR;
     __shared__ RowSums<LPR, 1> meet;
     int turn = 0;
-    const int team = threadIdx.x / LPR, tid = threadIdx.x % LPR;
+    const int team = team_of<LPR>(), tid = threadIdx.x % LPR;
     const int cols = a.cols, pitch = (cols + 31) / 32 * 32;
     const float inv_cols = 1.f / (float)cols;
     const float alpha = a.alpha ? a.alpha[0] : 1.f;
+    Columns c[NV];
     float coef[NV][8], wq[NV][8];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_params(a.w_pre, (v * LPR + tid) * 8, cols, wq[v], 0.f);
+    for (int v = 0; v < NV; ++v) {
+        c[v] = columns_at((v * LPR + tid) * 8, cols);
+        load_params(a.w_pre, c[v].c0, cols, wq[v], 0.f);
+    }
     int group = -1;
     const int rows = (int)a.rows, gate_rows = a.gate && a.gate_rows < a.rows ? (int)a.gate_rows : 0;
     Raw8<TH> hr[NV];
     Raw8<TF> fr[NV];
     bool live = true;
     auto fetch = [&](int row) {
-        live = !a.live || a.live[row];
+        if (a.live) live = a.live[row];
         const TH* const h = (const TH*)a.in_stream + (long long)row * a.in_stream_stride;
         const TF* const f = (const TF*)a.in_block + (long long)row * a.in_block_stride;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            hr[v] = fetch8(h + c0, cols - c0);
-            fr[v] = fetch8(f + c0, live ? cols - c0 : 0);
+            hr[v] = fetch_row(h, c[v], row < over_h);
+            fr[v] = fetch_row(f, c[v], row < over_f);
         }
     };
     int row = blockIdx.x * TEAMS + team;
@@ -62,68 +72,86 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
             group = g;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int c0 = (v * LPR + tid) * 8;
                 float wp[8];
-                load_params(a.gate ? a.gate + (long long)g * cols : nullptr, c0, cols, coef[v], 1.f);
-                load_params(a.w_post, c0, cols, wp, 1.f);
+                load_params(a.gate ? a.gate + (long long)g * cols : nullptr, c[v].c0, cols, coef[v], 1.f);
+                load_params(a.w_post, c[v].c0, cols, wp, 1.f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) coef[v][i] = c0 + i < cols ? alpha * coef[v][i] * wp[i] : 0.f;
+                for (int i = 0; i < 8; ++i) coef[v][i] = c[v].c0 + i < cols ? alpha * coef[v][i] * wp[i] : 0.f;
             }
         }
         float z[NV][8], n[NV][8];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            c[v].cut(hr[v]), c[v].cut(fr[v]);
             widen8(hr[v], z[v]);
             widen8(fr[v], n[v]);
         }
         const bool now = live;
         const int next = row + gridDim.x * TEAMS;
         if (next < rows) fetch(next);  // on its way while this row's sums are taken
+        if (!now)
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) n[v][i] = 0.f;
         float ip = 1.f;
         if (a.w_post) {
             float s = 0.f;
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+            for (int v = 0; v < NV; ++v) {
+                float part = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += n[v][i] * n[v][i];
+                for (int i = 0; i < 8; ++i) part += n[v][i] * n[v][i];
+                s += c[v].n ? part : 0.f;
+            }
             row_sums<LPR, 1>(&s, meet, turn);
-            ip = 1.f / sqrtf(s * inv_cols + a.eps);
+            ip = __builtin_amdgcn_rsqf(s * inv_cols + a.eps);
         }
+        const long long out = (long long)row * a.out_stream_stride;
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 n[v][i] *= ip;
                 z[v][i] += coef[v][i] * n[v][i];
             }
-        TH* const ho = (TH*)a.out_stream + (long long)row * a.out_stream_stride;
+            store8((TH*)a.out_stream + out + c[v].c0, c[v].n, z[v]);
+            if (a.nq) {
+                if (!c[v].n)
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            store8(ho + c0, cols - c0, z[v]);
-            if (a.nq) store_codes(a.nq, a.ne, row, pitch, c0, n[v]);
+                    for (int i = 0; i < 8; ++i) n[v][i] = 0.f;  // past the last column the checkpoint holds 0
+                store_codes(a.nq, a.ne, row, pitch, c[v].c0, n[v]);
+            }
         }
         if (a.inv_post && tid == 0) a.inv_post[row] = now ? ip : 0.f;
         if (a.w_pre) {
             float s = 0.f;
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+            for (int v = 0; v < NV; ++v) {
+                float part = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += z[v][i] * z[v][i];
+                for (int i = 0; i < 8; ++i) part += z[v][i] * z[v][i];
+                s += c[v].n ? part : 0.f;
+            }
             row_sums<LPR, 1>(&s, meet, turn);
-            const float iq = 1.f / sqrtf(s * inv_cols + a.eps);
-            TF* const u = (TF*)a.out_block + (long long)row * a.out_block_stride;
+            const float iq = __builtin_amdgcn_rsqf(s * inv_cols + a.eps);
+            const long long uo = (long long)row * a.out_block_stride;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int c0 = (v * LPR + tid) * 8;
                 float o[8];
+                if (!now || !c[v].n)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[v][i] = 0.f;  // what stands in a padded row may be no number
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    z[v][i] = now ? z[v][i] * iq : 0.f;
+                    z[v][i] *= iq;
                     o[i] = z[v][i] * wq[v][i];
                 }
-                store8(u + c0, cols - c0, o);
-                if (a.xq) store_codes(a.xq, a.xe, row, pitch, c0, z[v]);
+                if (!now)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[v][i] = o[i] = 0.f;
+                store8((TF*)a.out_block + uo + c[v].c0, c[v].n, o);
+                if (a.xq) store_codes(a.xq, a.xe, row, pitch, c[v].c0, z[v]);
             }
             if (a.inv_pre && tid == 0) a.inv_pre[row] = now ? iq : 0.f;
         }
@@ -143,13 +171,13 @@ struct Runs {
 //   sum(dn n) = sum(m dh') + inv_pre (sum(m dx) - mean(dx x) sum(m x)),
 // so that a row meets once, for four sums, and not twice.
 template <typename TH, typename TF, int LPR, int NV, bool OWN>
-__global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 ? 3 : 4) void k_join_backward(const iodf_join a, const Runs runs, float* sum_pre, float* sum_post,
-                                                                     unsigned* ticket) {
+__global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR <= 64 ? 3 : 4) void k_join_backward(const iodf_join a, const Runs runs, const int over_h, const int over_u,
+                                                                     float* sum_pre, float* sum_post, unsigned* ticket) {
     constexpr int THREADS = threads_of<LPR>(), TEAMS = THREADS / LPR;
     __shared__ RowSums<LPR, 4> meet;
     int turn = 0;
     __shared__ float joined[TEAMS > 1 ? THREADS * 8 : 1];
-    const int team = threadIdx.x / LPR, tid = threadIdx.x % LPR;
+    const int team = team_of<LPR>(), tid = threadIdx.x % LPR;
     const int cols = a.cols, pitch = (cols + 31) / 32 * 32, wide = (cols + 7) / 8 * 8;
     const float inv_cols = 1.f / (float)cols;
     const float alpha = a.alpha ? a.alpha[0] : 1.f;
@@ -173,6 +201,9 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 ? 3 : 
             pre[v][i] = post[v][i] = 0.f;
         }
     }
+    Columns c[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) c[v] = columns_at((v * LPR + tid) * 8, cols);
     struct Row {
         Raw8<TH> h[NV];
         Raw8<TF> u[NV];
@@ -183,67 +214,107 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 ? 3 : 
     };
     auto fetch = [&](int row) {
         Row r;
-        r.live = !a.live || a.live[row];
+        r.live = true;
+        if (a.live) r.live = a.live[row];
         const TH* const dh = (const TH*)a.in_stream + (long long)row * a.in_stream_stride;
         const TF* const du = (const TF*)a.in_block + (long long)row * a.in_block_stride;
+        const long long q = (long long)row * pitch, e = (long long)row * (pitch / 32);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            r.h[v] = fetch8(dh + c0, cols - c0);
-            r.n[v] = fetch_codes(a.nq, a.ne, row, pitch, r.live ? c0 : pitch);
-            r.u[v] = fetch8(du + c0, a.w_pre && r.live ? cols - c0 : 0);
-            r.x[v] = fetch_codes(a.xq, a.xe, row, pitch, a.w_pre && r.live ? c0 : pitch);
-            if (OWN) r.gate[v] = fetch8(a.gate + (long long)row * cols + c0, cols - c0);
+            r.h[v] = fetch_row(dh, c[v], row < over_h);
+            r.n[v] = {*(const u32x2*)(a.nq + q + c[v].at), (a.ne + e)[c[v].at / 32]};
+            if (a.w_pre) {
+                r.u[v] = fetch_row(du, c[v], row < over_u);
+                r.x[v] = {*(const u32x2*)(a.xq + q + c[v].at), (a.xe + e)[c[v].at / 32]};
+            }
+            if (OWN) r.gate[v] = fetch_row(a.gate + (long long)row * cols, c[v], false);
         }
-        r.iq = a.w_pre && r.live ? a.inv_pre[row] : 0.f;
-        r.ip = !a.w_post ? 1.f : r.live ? a.inv_post[row] : 0.f;
+        r.iq = a.w_pre ? a.inv_pre[row] : 0.f;
+        r.ip = a.w_post ? a.inv_post[row] : 1.f;
         return r;
     };
+    constexpr bool AHEAD = NV == 1;  // two vectors to a thread leave no registers for another row
     Row next;
     int row = first + team;
-    if (row < last) next = fetch(row);
+    if (AHEAD && row < last) next = fetch(row);
     for (; row < last; row += TEAMS) {
-        Row r = next;
-        if (row + TEAMS < last) next = fetch(row + TEAMS);  // on its way while this row's sums are taken
+        Row r = AHEAD ? next : fetch(row);
+        if (AHEAD && row + TEAMS < last) next = fetch(row + TEAMS);  // on its way while this row's sums are taken
+        TH* const dho = (TH*)a.out_stream + (long long)row * a.out_stream_stride;
+        TF* const df = (TF*)a.out_block + (long long)row * a.out_block_stride;
+        float* const dgate = OWN ? a.dgate + (long long)row * cols : nullptr;
+        if (!r.live) {  // padding goes to dL/dh as it came, and nowhere else
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                float dz[8];
+                const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                widen8(r.h[v], dz);
+                store8(dho + c[v].c0, c[v].n, dz);
+                store8(df + c[v].c0, c[v].n, none);
+                if (OWN) store8(dgate + c[v].c0, c[v].n, none);
+            }
+            continue;
+        }
+        // a lane's eight columns have one step: the codes are used as numbers, and sums get their steps at the end
         float sum[4] = {0.f, 0.f, 0.f, 0.f};  // of dx x, m dh', m dx, m x
+        float sx[NV], sn[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float dh[8], du[8], x[8], n[8], gate[8];
+            float dh[8], du[8], x[8], n[8], gate[8], part[4] = {0.f, 0.f, 0.f, 0.f};
+            c[v].cut(r.h[v]);
+            if (a.w_pre) c[v].cut(r.u[v]);
             widen8(r.h[v], dh);
-            widen8(r.u[v], du);
-            decode8(r.x[v].q, code_step(r.x[v].e), x);
-            decode8(r.n[v].q, code_step(r.n[v].e), n);
+            numbers8(r.n[v].q, n);
+            sn[v] = code_step(r.n[v].e);
             if (OWN) widen8(r.gate[v], gate);
+            if (a.w_pre) {
+                widen8(r.u[v], du);
+                numbers8(r.x[v].q, x);
+                sx[v] = code_step(r.x[v].e);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float m = coef[v][i] * n[i] * (OWN ? gate[i] : 1.f), dx = du[i] * wq[v][i];
-                pre[v][i] += du[i] * x[i];
-                sum[0] += dx * x[i];
-                sum[1] += m * (r.live ? dh[i] : 0.f);  // padding goes to dL/dh as it came, and nowhere else
-                sum[2] += m * dx;
-                sum[3] += m * x[i];
+                float m = coef[v][i] * n[i];
+                if (OWN) m *= gate[i];
+                part[1] += m * dh[i];
+                if (a.w_pre) {
+                    const float dx = du[i] * wq[v][i];
+                    pre[v][i] += du[i] * sx[v] * x[i];
+                    part[0] += dx * x[i];
+                    part[2] += m * dx;
+                    part[3] += m * x[i];
+                }
             }
-            forget(r.h[v]), forget(r.u[v]), forget(r.x[v]), forget(r.n[v]);
+            sum[1] += c[v].n ? part[1] * sn[v] : 0.f;
+            if (a.w_pre) {
+                sum[0] += c[v].n ? part[0] * sx[v] : 0.f;
+                sum[2] += c[v].n ? part[2] * sn[v] : 0.f;
+                sum[3] += c[v].n ? part[3] * sn[v] * sx[v] : 0.f;
+            }
+            forget(r.h[v]), forget(r.n[v]);
+            if (a.w_pre) forget(r.u[v]), forget(r.x[v]);
         }
         row_sums<LPR, 4>(sum, meet, turn);
         const float mean_x = sum[0] * inv_cols, mean_n = a.w_post ? (sum[1] + r.iq * (sum[2] - mean_x * sum[3])) * inv_cols : 0.f;
-        TH* const dho = (TH*)a.out_stream + (long long)row * a.out_stream_stride;
-        TF* const df = (TF*)a.out_block + (long long)row * a.out_block_stride;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            float dz[8], du[8], x[8], n[8], gate[8], share[8], dn[8];
+            float dz[8], n[8], gate[8], share[8], dn[8];
             widen8(r.h[v], dz);
-            widen8(r.u[v], du);
-            decode8(r.x[v].q, code_step(r.x[v].e), x);
-            decode8(r.n[v].q, code_step(r.n[v].e), n);
+            numbers8(r.n[v].q, n);
             if (OWN) widen8(r.gate[v], gate);
+            if (a.w_pre) {
+                float du[8], x[8];
+                widen8(r.u[v], du);
+                numbers8(r.x[v].q, x);
+                const float back = r.iq * mean_x * sx[v];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dz[i] = fmaf(r.iq, du[i] * wq[v][i], fmaf(-back, x[i], dz[i]));
+            }
+            const float back = r.ip * mean_n * sn[v];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                dz[i] += r.iq * (du[i] * wq[v][i] - x[i] * mean_x);
-                const float d = r.live ? dz[i] : 0.f;
-                share[i] = d * n[i];
-                dn[i] = coef[v][i] * d;
+                share[i] = dz[i] * sn[v] * n[i];
+                dn[i] = coef[v][i] * dz[i];
                 if (OWN) {
                     dn[i] *= gate[i];
                     post[v][i] += gate[i] * share[i];
@@ -251,11 +322,11 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 ? 3 : 
                 } else {
                     post[v][i] += share[i];
                 }
-                dn[i] = r.ip * (dn[i] - n[i] * mean_n);
+                dn[i] = fmaf(r.ip, dn[i], -back * n[i]);
             }
-            store8(dho + c0, cols - c0, dz);
-            store8(df + c0, cols - c0, dn);
-            if (OWN) store8(a.dgate + (long long)row * cols + c0, cols - c0, share);
+            store8(dho + c[v].c0, c[v].n, dz);
+            store8(df + c[v].c0, c[v].n, dn);
+            if (OWN) store8(dgate + c[v].c0, c[v].n, share);
         }
     }
     // the teams' sums meet in the order of the teams
@@ -365,13 +436,23 @@ __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const
     if (threadIdx.x == 0) a.dalpha[0] = (float)s;
 }
 
+// Workgroups of a kernel that the chip holds at once.
+template <typename K>
+int resident(K kernel, int threads) {
+    int per_cu = 0, cus = 0, device = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kernel, threads, 0) != hipSuccess || per_cu < 1) per_cu = 1;
+    if (hipGetDevice(&device) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || cus < 1) cus = 256;
+    return per_cu * cus;
+}
+
 template <typename TH, typename TF, int LPR, int NV>
 hipError_t forward_of(const iodf_join& a, hipStream_t st) {
     constexpr int TEAMS = threads_of<LPR>() / LPR;
-    const long long blocks = (a.rows + TEAMS - 1) / TEAMS;
-    // a workgroup keeps the parameters of its columns in registers over several rows
-    const long long most = 256 * (2048 / threads_of<LPR>());
-    k_join_forward<TH, TF, LPR, NV><<<(unsigned)std::min(blocks, most), threads_of<LPR>(), 0, st>>>(a);
+    // as many workgroups as run at once: each keeps its columns' parameters in registers over all its rows
+    static const int most = resident(k_join_forward<TH, TF, LPR, NV>, threads_of<LPR>());
+    const long long blocks = std::min<long long>((a.rows + TEAMS - 1) / TEAMS, most);
+    k_join_forward<TH, TF, LPR, NV><<<(unsigned)blocks, threads_of<LPR>(), 0, st>>>(a, (int)over_rows(a.rows, a.cols, a.in_stream_stride),
+                                                                                     (int)over_rows(a.rows, a.cols, a.in_block_stride));
     return hipGetLastError();
 }
 
@@ -399,13 +480,13 @@ int backward_lanes(int cols) {
 }
 int backward_teams(int cols) { return backward_lanes(cols) > 64 ? 1 : 256 / backward_lanes(cols); }
 
-// Runs of rows: a thousand threads to a compute unit, but at least four rows to a team while every unit has a workgroup: a run's sums cost as
+// Runs of rows: as many workgroups as run at once, but at least four rows to a team while every unit has a workgroup: a run's sums cost as
 // much as two rows of 16 bits.
 Runs runs_of(long long rows, int cols, long long gate_rows) {
     Runs r;
     if (gate_rows > rows || gate_rows < 1) gate_rows = rows;
     const int teams = backward_teams(cols);
-    const long long most = 256 * (1024 / (backward_lanes(cols) > 64 ? backward_lanes(cols) : 256)), want = std::min(most, std::max(256ll, rows / (4 * teams)));
+    const long long most = 256 * (backward_lanes(cols) > 64 ? 1024 / backward_lanes(cols) : 3), want = std::min(most, std::max(256ll, rows / (4 * teams)));
     r.gate_rows = (int)gate_rows;
     if (gate_rows == 1 && rows > 1) {
         r.groups = (int)rows;
@@ -436,10 +517,11 @@ hipError_t backward_of(const iodf_join& a, void* work, hipStream_t st) {
     double* const part = (double*)((char*)work + 16);
     float* const pre = (float*)((char*)part + up16(parts * 8));
     float* const post = pre + n * wide;
+    const int over_h = (int)over_rows(a.rows, a.cols, a.in_stream_stride), over_u = a.w_pre ? (int)over_rows(a.rows, a.cols, a.in_block_stride) : 0;
     hipError_t e = hipSuccess;
     if (n) {
-        if (r.gate_rows == 1) k_join_backward<TH, TF, LPR, NV, true><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, pre, post, ticket);
-        else k_join_backward<TH, TF, LPR, NV, false><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, pre, post, ticket);
+        if (r.gate_rows == 1) k_join_backward<TH, TF, LPR, NV, true><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, ticket);
+        else k_join_backward<TH, TF, LPR, NV, false><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, ticket);
         e = hipGetLastError();
     } else {
         e = launch_fill_zero(ticket, 16, st);
