@@ -56,19 +56,50 @@ __device__ __forceinline__ void place(const Tiles& t, int& m, int& n, int& split
     n = (int)(in / high);
 }
 
-template <typename TY, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_wgrad(const iodf_wgrad a, const Tiles tiles, float* partial) {
-    constexpr int THREADS = (BM / WM) * (BN / WN) * 64, P = parts_of<TY>(), MT = WM / 32, NT = WN / 32;
-    constexpr int AL = KT * BM / 8 / THREADS, BL = KT * BN / 8 / THREADS;
+// A wave's MT x NT blocks of 32 x 32 outputs from row o0 and column c0 on: lane l holds column l % 32, rows 8 * (i / 4) + 4 * (l / 32) + i % 4 of
+// each. Row addresses are scalar, a lane adds its own offset.
+template <int MT, int NT>
+__device__ __forceinline__ void store_outputs(const f32x16 (&acc)[MT][NT], const iodf_wgrad& a, int o0, int c0, int split, float* partial) {
+    const int lane = threadIdx.x & 63, high = 4 * (lane >> 5), low = lane & 31;
+    o0 = __builtin_amdgcn_readfirstlane(o0), c0 = __builtin_amdgcn_readfirstlane(c0);
+    const long long ld = partial ? a.cols : a.dw_stride;
+    float* const base = (partial ? partial + (long long)split * a.out * a.cols : a.dw) + o0 * ld + c0;
+    const bool add = !partial && a.accumulate, inside = o0 + MT * 32 <= a.out && c0 + NT * 32 <= a.cols;
+    float scale[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) scale[n] = !partial && a.col_scale && c0 + n * 32 + low < a.cols ? a.col_scale[c0 + n * 32 + low] : 1.f;
+    const long long off = high * ld + low;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = m * 32 + 8 * (i / 4) + i % 4;
+            float* const row = base + r * ld;
+            if (inside && !add) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) row[off + n * 32] = scale[n] * acc[m][n][i];
+            } else if (o0 + r + high < a.out) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    if (c0 + n * 32 + low < a.cols) row[off + n * 32] = (add ? row[off + n * 32] : 0.f) + scale[n] * acc[m][n][i];
+            }
+        }
+}
+
+// BM x BN outputs to a workgroup of four waves, a quarter to each. Operands come through registers, two tiles ahead.
+template <typename TY, int BM, int BN>
+__global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles tiles, float* partial) {
+    constexpr int THREADS = 256, P = parts_of<TY>(), WM = BM / 2, WN = BN / 2, MT = WM / 32, NT = WN / 32;
+    constexpr int AL = KT * BM / 8 / THREADS, BL = KT * BN / 8 / THREADS;  // chunks of eight of dy and of codes that a thread loads
     __shared__ __bf16 at[2][P][KT * BM];
     __shared__ __bf16 bt[2][KT * BN];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int m0, n0, split;
     place(tiles, m0, n0, split);
     m0 *= BM, n0 *= BN;
-    const int pitch = (a.cols + 31) / 32 * 32;
+    const int pitch = (a.cols + 31) / 32 * 32, epitch = pitch / 32;
     const long long t0 = (long long)split * tiles.slice, t1 = min((long long)a.rows, t0 + tiles.slice);
-    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int wm = wave / 2 * WM, wn = wave % 2 * WN;
 
     int a_off[MT], b_off[NT];
     const int fr = (lane >> 5) * 8 + ((lane >> 2) & 3), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
@@ -77,54 +108,80 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_wgrad(const iodf
 #pragma unroll
     for (int n = 0; n < NT; ++n) b_off[n] = chunk_at<BN>(fr, (wn + n * 32 + fc) / 8) * 8 + (fc & 7);
 
-    float av[AL][8];
-    u32x2 bq[BL];
-    float bs[BL];
-    auto fetch = [&](long long t) {
+    // Chunks past the last column repeat the first, and one that sticks out of its row reads on: both only reach outputs that are not stored.
+    // Rows past the slice's end repeat its last one and are put as zeros. Only in the eight rows before dy's end, where reading on could leave
+    // it, is a chunk that sticks out taken element by element.
+    const int ar = tid / (BM / 8), ac = tid % (BM / 8) * 8, br = tid / (BN / 8), bc = tid % (BN / 8) * 8;
+    const int acol = m0 + ac < a.out ? m0 + ac : 0, bcol = n0 + bc < pitch ? n0 + bc : 0;
+    const TY* const dy = (const TY*)a.dy + ar * a.dy_stride + acol;
+    const long long a_step = THREADS * 8 / BM * a.dy_stride;
+    const int b_off0 = br * pitch + bcol, e_off0 = br * epitch + bcol / 32, b_step = THREADS * 8 / BN * pitch, e_step = THREADS * 8 / BN * epitch;
+    struct Stage {
+        Raw8<TY> a[AL];
+        RawCodes b[BL];
+        bool live[AL], there[BL];
+    };
+    auto fetch = [&](Stage& s, long long t, auto guarded) {
+        if (!guarded) {
 #pragma unroll
-        for (int i = 0; i < AL; ++i) {
-            const int k = threadIdx.x + i * THREADS, c = m0 + k % (BM / 8) * 8;
-            const long long row = t + k / (BM / 8);
-            const bool there = row < t1 && (!a.live || a.live[row]);
-            load8((const TY*)a.dy + row * a.dy_stride + c, there ? a.out - c : 0, av[i]);
-        }
+            for (int i = 0; i < AL; ++i) {
+                s.a[i] = fetch8(dy + t * a.dy_stride + i * a_step, 8, true);
+                s.live[i] = true;
+                if (a.live) s.live[i] = (a.live + t)[ar + i * (THREADS * 8 / BM)];
+            }
 #pragma unroll
-        for (int i = 0; i < BL; ++i) {
-            const int k = threadIdx.x + i * THREADS, c = n0 + k % (BN / 8) * 8;
-            const long long row = t + k / (BN / 8);
-            bq[i] = u32x2{0, 0};
-            bs[i] = 0.f;
-            if (row < t1 && c < pitch && (!a.live || a.live[row])) {
-                bq[i] = *(const u32x2*)(a.q + row * pitch + c);
-                bs[i] = code_step(a.e[row * (pitch / 32) + c / 32]);
+            for (int i = 0; i < BL; ++i) {
+                s.b[i] = {*(const u32x2*)(a.q + t * pitch + (b_off0 + i * b_step)), (a.e + t * epitch)[e_off0 + i * e_step]};
+                s.there[i] = true;
+            }
+        } else {
+            const bool apart = t1 + 8 > a.rows && a.out % 8 != 0;
+#pragma unroll
+            for (int i = 0; i < AL; ++i) {
+                const long long row = t + ar + i * (THREADS * 8 / BM), at = row < t1 ? row : t1 - 1;
+                const TY* const p = (const TY*)a.dy + at * a.dy_stride + acol;
+                s.a[i] = apart ? fetch8(p, a.out - acol, false) : fetch8(p, 8, true);
+                s.live[i] = row < t1;
+                if (a.live) s.live[i] = row < t1 && a.live[at];
+            }
+#pragma unroll
+            for (int i = 0; i < BL; ++i) {
+                const long long row = t + br + i * (THREADS * 8 / BN), at = row < t1 ? row : t1 - 1;
+                s.b[i] = {*(const u32x2*)(a.q + at * pitch + bcol), a.e[at * epitch + bcol / 32]};
+                s.there[i] = row < t1;
             }
         }
     };
-    auto put = [&](int buf) {
+    auto put = [&](const Stage& s, int buf) {
 #pragma unroll
         for (int i = 0; i < AL; ++i) {
-            const int k = threadIdx.x + i * THREADS, at16 = chunk_at<BM>(k / (BM / 8), k % (BM / 8)) * 8;
-            float rest[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) rest[j] = av[i][j];
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
+            const int to = chunk_at<BM>(ar + i * (THREADS * 8 / BM), ac / 8) * 8;
+            if (P == 1) {
                 bf8 w;
+                __builtin_memcpy(&w, s.a[i].w, 16);
+                *(bf8*)&at[buf][0][to] = s.live[i] ? w : bf8{};
+            } else {
+                float rest[8];
+                widen8(s.a[i], rest);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    w[j] = (__bf16)rest[j];
-                    const float got = (float)w[j];
-                    rest[j] = fabsf(got) < __builtin_inff() ? rest[j] - got : 0.f;
+                for (int j = 0; j < 8; ++j) rest[j] = s.live[i] ? rest[j] : 0.f;
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const bf8 w = narrow8(rest);
+                    *(bf8*)&at[buf][p][to] = w;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float got = (float)w[j];
+                        rest[j] = fabsf(got) < __builtin_inff() ? rest[j] - got : 0.f;
+                    }
                 }
-                *(bf8*)&at[buf][p][at16] = w;
             }
         }
 #pragma unroll
         for (int i = 0; i < BL; ++i) {
-            const int k = threadIdx.x + i * THREADS, at16 = chunk_at<BN>(k / (BN / 8), k % (BN / 8)) * 8;
             float v[8];
-            decode8(bq[i], bs[i], v);
-            *(bf8*)&bt[buf][at16] = narrow8(v);
+            decode8(s.there[i] ? s.b[i].q : u32x2{0, 0}, code_step(s.there[i] ? s.b[i].e : 16), v);
+            *(bf8*)&bt[buf][chunk_at<BN>(br + i * (THREADS * 8 / BN), bc / 8) * 8] = narrow8(v);
         }
     };
 
@@ -136,54 +193,43 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_wgrad(const iodf
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.f;
 
+    const std::true_type checked;
+    const std::false_type whole;
+    Stage st[2];
     if (t0 < t1) {
-        fetch(t0);
-        put(0);
+        fetch(st[0], t0, checked);
+        fetch(st[1], t0 + KT, checked);
+        put(st[0], 0);
+        fetch(st[0], t0 + 2 * KT, checked);
     }
     __syncthreads();
-    int buf = 0;
-    for (long long t = t0; t < t1; t += KT) {
-        const bool more = t + KT < t1;
-        if (more) fetch(t + KT);
+    auto two_tiles = [&](long long t, auto guarded) {
 #pragma unroll
-        for (int s = 0; s < KT / 16; ++s) {
-            bf8 bf[NT];
+        for (int h = 0; h < 2; ++h) {
+            if (guarded && h && t + KT >= t1) break;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) bf[n] = fragment<BN>(bt[buf], b_off[n], s);
+            for (int s = 0; s < KT / 16; ++s) {
+                bf8 bf[NT];
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+                for (int n = 0; n < NT; ++n) bf[n] = fragment<BN>(bt[h], b_off[n], s);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const bf8 af = fragment<BM>(at[buf][p], a_off[m], s);
+                for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af, bf[n], acc[m][n], 0, 0, 0);
-                }
-        }
-        if (more) put(buf ^ 1);
-        __syncthreads();
-        buf ^= 1;
-    }
-
-    // lane l holds column l % 32, rows 8 * (i / 4) + 4 * (l / 32) + i % 4 of each 32 x 32 block
+                    for (int m = 0; m < MT; ++m) {
+                        const bf8 af = fragment<BM>(at[h][p], a_off[m], s);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int c = n0 + wn + n * 32 + (lane & 31);
-        if (c >= a.cols) continue;
-        const float scale = !partial && a.col_scale ? a.col_scale[c] : 1.f;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int o = m0 + wm + m * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-                if (o >= a.out) continue;
-                if (partial) {
-                    partial[((long long)split * a.out + o) * a.cols + c] = acc[m][n][i];
-                } else {
-                    float* const d = a.dw + o * a.dw_stride + c;
-                    *d = (a.accumulate ? *d : 0.f) + scale * acc[m][n][i];
-                }
+                        for (int n = 0; n < NT; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af, bf[n], acc[m][n], 0, 0, 0);
+                    }
             }
-    }
+            if (!guarded || t + (h + 1) * KT < t1) put(st[h ^ 1], h ^ 1);
+            if (!guarded || t + (h + 3) * KT < t1) fetch(st[h ^ 1], t + (h + 3) * KT, guarded);
+            __syncthreads();
+        }
+    };
+    long long t = t0;
+    for (; t + 5 * KT + 8 <= t1; t += 2 * KT) two_tiles(t, whole);
+    for (; t < t1; t += 2 * KT) two_tiles(t, checked);
+    store_outputs<MT, NT>(acc, a, m0 + wm, n0 + wn, split, partial);
 }
 
 // ---- large layers, dy in bfloat16 ----
@@ -407,25 +453,7 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
     long long t = t0;
     for (; t + 9 * KT < t1; t += RING * KT) four_tiles(t, whole);
     for (; t < t1; t += RING * KT) four_tiles(t, checked);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int c = n0 + wn + n * 32 + (lane & 31);
-        if (c >= a.cols) continue;
-        const float scale = !partial && a.col_scale ? a.col_scale[c] : 1.f;
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int o = m0 + wm + m * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-                if (o >= a.out) continue;
-                if (partial) {
-                    partial[((long long)split * a.out + o) * a.cols + c] = acc[m][n][i];
-                } else {
-                    float* const d = a.dw + o * a.dw_stride + c;
-                    *d = (a.accumulate ? *d : 0.f) + scale * acc[m][n][i];
-                }
-            }
-    }
+    store_outputs<4, NT>(acc, a, m0 + wm, n0 + wn, split, partial);
 }
 
 // The slices' sums, in an order that their number alone decides: JL threads to an output, or to four neighbours (VEC).
@@ -460,37 +488,42 @@ __global__ __launch_bounds__(256) void k_wgrad_join(const iodf_wgrad a, int spli
 }
 
 struct Plan : Tiles {
-    int tile;  // its edge
+    int bm, bn;  // a tile's edges
 };
 
 Plan plan_of(const iodf_wgrad& a) {
     Plan p;
-    auto tiles = [&](int b) { return (long long)((a.out + b - 1) / b) * ((a.cols + b - 1) / b); };
-    p.tile = tiles(128) * ((a.rows + 255) / 256) >= 256 ? 128 : 64;
-    if (a.dy_type == IODF_T_BF16 && a.dy_stride <= (1 << 24) && a.out > 128 && a.cols > 128 && tiles(256) * ((a.rows + 1023) / 1024) >= 256)
-        p.tile = 256;
-    p.m = (a.out + p.tile - 1) / p.tile;
-    p.n = (a.cols + p.tile - 1) / p.tile;
-    const long long n = (long long)p.m * p.n;
-    long long splits = std::max<long long>(1, 256 / n);
+    auto up = [](long long n, long long d) { return (n + d - 1) / d; };
+    if (a.dy_type == IODF_T_BF16 && a.dy_stride <= (1 << 24) && a.out > 128 && a.cols > 128 && up(a.out, WIDE) * up(a.cols, WIDE) * up(a.rows, 1024) >= 256) {
+        p.bm = p.bn = WIDE;
+    } else {
+        p.bm = a.out > 64 ? 128 : 64;
+        p.bn = a.cols > 64 ? 128 : 64;
+    }
+    const int unit = p.bm == WIDE ? RING * KT : KT;  // what the loop takes at a time
+    p.m = (int)up(a.out, p.bm);
+    p.n = (int)up(a.cols, p.bn);
+    const long long n = (long long)p.m * p.n, at_once = p.bm == WIDE ? 256 : 512;
+    long long splits = std::max<long long>(1, at_once / n);
     splits = std::min<long long>(splits, std::max<long long>(1, a.rows / 128));
-    if (a.live) splits = std::max<long long>(splits, (a.rows + kLiveRows - 1) / kLiveRows);
-    const int unit = p.tile == WIDE ? RING * KT : KT;  // what the loop takes at a time
-    p.slice = (int)(((a.rows + splits - 1) / splits + unit - 1) / unit * unit);
-    p.splits = p.slice ? (int)((a.rows + p.slice - 1) / p.slice) : 1;
+    if (a.live) splits = std::max<long long>(splits, up(a.rows, kLiveRows));
+    p.slice = (int)(up(up(a.rows, splits), unit) * unit);
+    p.splits = p.slice ? (int)up(a.rows, p.slice) : 1;
     return p;
 }
 
 template <typename TY>
 hipError_t run(const iodf_wgrad& a, const Plan& p, float* partial, hipStream_t st) {
     const unsigned blocks = (unsigned)(p.m * p.n * p.splits);
-    if (p.tile == 256) {
+    if (p.bm == WIDE) {
         if (a.live) k_wgrad_wide<true><<<blocks, 512, 0, st>>>(a, p, partial);
         else k_wgrad_wide<false><<<blocks, 512, 0, st>>>(a, p, partial);
-    } else if (p.tile == 128) {
-        k_wgrad<TY, 128, 128, 64, 64><<<blocks, 256, 0, st>>>(a, p, partial);
+    } else if (p.bm == 128) {
+        if (p.bn == 128) k_wgrad<TY, 128, 128><<<blocks, 256, 0, st>>>(a, p, partial);
+        else k_wgrad<TY, 128, 64><<<blocks, 256, 0, st>>>(a, p, partial);
     } else {
-        k_wgrad<TY, 64, 64, 32, 32><<<blocks, 256, 0, st>>>(a, p, partial);
+        if (p.bn == 128) k_wgrad<TY, 64, 128><<<blocks, 256, 0, st>>>(a, p, partial);
+        else k_wgrad<TY, 64, 64><<<blocks, 256, 0, st>>>(a, p, partial);
     }
     return hipGetLastError();
 }
