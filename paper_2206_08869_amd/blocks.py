@@ -6,21 +6,59 @@ allocator supplies outputs and scratch. Parameters (alpha, gate, norm weights) a
 are not padding. `joined`, `projection` and `gated_projection` are the same operators as differentiable calls.
 """
 import ctypes
+import struct
 from typing import NamedTuple, Optional
 
 from . import binding as _b
 
 _ACTS = {"relu": _b.IODF_ACT_RELU, "silu": _b.IODF_ACT_SILU, "gelu": _b.IODF_ACT_GELU}
-_torch, _types = None, None
+_torch = _types = _f32 = _Tensor = _stream_of = None
+_native = {}
+
+# The argument blocks as one pack() each, a few microseconds less a call than filling a ctypes.Structure field by field.
+_JOIN, _GLU, _WGRAD = struct.Struct("@qq3if9P4q10P"), struct.Struct("@q3i7P6q6P"), struct.Struct("@q4iPq5Pq")
 
 
-def _t():
-    global _torch, _types
-    if _torch is None:
-        import torch
-        _types = {torch.float32: _b.IODF_T_F32, torch.bfloat16: _b.IODF_T_BF16, torch.float16: _b.IODF_T_F16}
-        _torch = torch
-    return _torch
+def _setup():
+    """torch, and the library's entry points: on first use, since importing the package loads neither."""
+    global _torch, _types, _f32, _Tensor, _stream_of
+    import torch
+    lib = _b.load_library()
+    for block, kind in ((_JOIN, _b.JoinArgs), (_GLU, _b.GluArgs), (_WGRAD, _b.WgradArgs)):
+        assert block.size == ctypes.sizeof(kind)
+    ci, args, vp, i64 = ctypes.c_int, ctypes.c_char_p, ctypes.c_void_p, ctypes.c_int64
+    for name, more in (("join_forward", ()), ("glu_forward", ()), ("glu_backward", ()), ("join_backward", (vp, i64)), ("weight_grad", (vp, i64))):
+        _native[name] = ctypes.CFUNCTYPE(ci, args, *more, vp)(("iodf_" + name, lib))
+    _native["pack"] = ctypes.CFUNCTYPE(ci, vp, ci, i64, i64, ci, vp, vp, vp, vp)(("iodf_pack", lib))
+    _native["unpack"] = ctypes.CFUNCTYPE(ci, vp, vp, i64, ci, vp, ci, i64, vp)(("iodf_unpack", lib))
+    for name in ("join_workspace", "weight_grad_workspace"):
+        _native[name] = ctypes.CFUNCTYPE(ci, args, ctypes.POINTER(i64))(("iodf_" + name, lib))
+    _types = {torch.float32: _b.IODF_T_F32, torch.bfloat16: _b.IODF_T_BF16, torch.float16: _b.IODF_T_F16}
+    _f32, _Tensor = torch.float32, torch.Tensor
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _stream_of = raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    _torch = torch
+    return torch
+
+
+def _call(name, device, *args):
+    """An entry point on the current stream of `device`, with that device current."""
+    index = device.index
+    if _torch.cuda.current_device() == index:
+        rc = _native[name](*args, _stream_of(index))
+    else:
+        with _torch.cuda.device(device):
+            rc = _native[name](*args, _stream_of(index))
+    if rc:
+        _b._check(rc)
+
+
+def _workspace(name, block, device):
+    need = ctypes.c_int64(0)
+    rc = _native[name](block, need)
+    if rc:
+        _b._check(rc)
+    return _torch.empty((need.value,), dtype=_torch.uint8, device=device), need.value
 
 
 class Codes(NamedTuple):
@@ -58,38 +96,40 @@ def _refuse(what):
     raise ValueError("iodf: " + what)
 
 
-def _matrix(x, name, rows=None, cols=None, dtype=None):
+def _matrix(x, name, shape=None, dtype=None, device=None):
     """Element type and row stride of a [rows, cols] tensor that the kernels take."""
-    t = _t()
-    if not isinstance(x, t.Tensor) or not x.is_cuda or x.dim() != 2 or x.dtype not in _types:
+    if not isinstance(x, _Tensor) or x.dim() != 2 or x.dtype not in _types or not x.is_cuda:
         _refuse("%s has to be a float32, bfloat16 or float16 [rows, cols] tensor on the GPU" % name)
     r, c = x.shape
-    if c < 1 or (r > 0 and c > 1 and x.stride(1) != 1):
-        _refuse("%s has to have one column or more, consecutive in memory" % name)
-    if (rows is not None and r != rows) or (cols is not None and c != cols):
-        _refuse("%s is %s, not [%s, %s]" % (name, list(x.shape), "rows" if rows is None else rows, "cols" if cols is None else cols))
+    if shape is not None and (r, c) != shape:
+        _refuse("%s is %s, not %s" % (name, [r, c], list(shape)))
     if dtype is not None and x.dtype != dtype:
         _refuse("%s is %s, not %s" % (name, x.dtype, dtype))
-    stride = x.stride(0) if r > 1 else c
-    if stride < c:
+    if device is not None and x.device != device:
+        _refuse("%s is on %s, the rest on %s" % (name, x.device, device))
+    stride, step = x.stride()
+    if c < 1 or (r > 0 and c > 1 and step != 1):
+        _refuse("%s has to have one column or more, consecutive in memory" % name)
+    if r <= 1:
+        stride = c
+    elif stride < c:
         _refuse("the rows of %s overlap" % name)
     return _types[x.dtype], stride
 
 
-def _vector(x, name, shape, device, dtype=None):
-    t = _t()
+def _vector(x, name, n, device):
+    """Address of a contiguous float32 tensor of n values (0: none)."""
     if x is None:
-        return None
-    if not isinstance(x, t.Tensor) or x.dtype != (dtype or t.float32) or tuple(x.shape) != shape or x.device != device or not x.is_contiguous():
-        _refuse("%s has to be a contiguous %s tensor of shape %s on %s" % (name, dtype or t.float32, list(shape), device))
+        return 0
+    if not isinstance(x, _Tensor) or x.dtype != _f32 or x.numel() != n or x.device != device or not x.is_contiguous():
+        _refuse("%s has to be a contiguous float32 tensor of %d values on %s" % (name, n, device))
     return x.data_ptr()
 
 
 def _live(live, rows, device):
-    t = _t()
     if live is None:
-        return None
-    if not isinstance(live, t.Tensor) or live.dtype not in (t.bool, t.uint8) or tuple(live.shape) != (rows,) or live.device != device \
+        return 0
+    if not isinstance(live, _Tensor) or live.dtype not in (_torch.bool, _torch.uint8) or tuple(live.shape) != (rows,) or live.device != device \
             or not live.is_contiguous():
         _refuse("live has to be a contiguous bool or uint8 tensor [rows] on the rows' GPU")
     return live.data_ptr()
@@ -100,63 +140,39 @@ def _pitch(cols):
 
 
 def _codes(c, name, rows, cols, device):
-    t = _t()
     if not isinstance(c, Codes):
         _refuse("%s has to be Codes" % name)
     pitch = _pitch(cols)
-    q, e = c.q, c.e
-    if c.cols != cols or q.dtype != t.int8 or e.dtype != t.uint8 or tuple(q.shape) != (rows, pitch) or tuple(e.shape) != (rows, pitch // 32) \
+    q, e, _ = c
+    if c.cols != cols or q.dtype != _torch.int8 or e.dtype != _torch.uint8 or q.shape != (rows, pitch) or e.shape != (rows, pitch // 32) \
             or q.device != device or e.device != device or not q.is_contiguous() or not e.is_contiguous():
         _refuse("%s has to be the codes of %d x %d values on %s" % (name, rows, cols, device))
     return q.data_ptr(), e.data_ptr()
 
 
 def _new_codes(rows, cols, device):
-    t = _t()
     pitch = _pitch(cols)
-    return Codes(t.empty((rows, pitch), dtype=t.int8, device=device), t.empty((rows, pitch // 32), dtype=t.uint8, device=device), cols)
-
-
-class _On:
-    """The device of a call made current, and its stream."""
-
-    def __init__(self, device):
-        cuda = _t().cuda
-        self.guard = cuda.device(device) if cuda.current_device() != device.index else None
-        self.device = device
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return ctypes.c_void_p(_torch.cuda.current_stream(self.device).cuda_stream)
-
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
-
-
-def _same_device(device, **tensors):
-    for name, x in tensors.items():
-        if x is not None and x.device != device:
-            _refuse("%s is on %s, the rest on %s" % (name, x.device, device))
+    return Codes(_torch.empty((rows, pitch), dtype=_torch.int8, device=device),
+                 _torch.empty((rows, pitch // 32), dtype=_torch.uint8, device=device), cols)
 
 
 # ---- checkpoints ----
 
 def pack(x, live=None):
     """x -> Codes."""
+    _torch or _setup()
     kind, stride = _matrix(x, "x")
     rows, cols = x.shape
-    lp = _live(live, rows, x.device)
-    out = _new_codes(rows, cols, x.device)
-    with _On(x.device) as st:
-        _b.iodf_pack(x.data_ptr(), kind, stride, rows, cols, lp, out.q.data_ptr(), out.e.data_ptr(), st)
+    device = x.device
+    lp = _live(live, rows, device)
+    out = _new_codes(rows, cols, device)
+    _call("pack", device, x.data_ptr(), kind, stride, rows, cols, lp, out.q.data_ptr(), out.e.data_ptr())
     return out
 
 
 def unpack(codes, dtype=None):
     """What Codes stand for, as bfloat16 (default) or float32: exact in both."""
-    t = _t()
+    t = _torch or _setup()
     dtype = t.bfloat16 if dtype is None else dtype
     if dtype not in (t.bfloat16, t.float32):
         _refuse("codes are unpacked to bfloat16 or float32")
@@ -167,25 +183,22 @@ def unpack(codes, dtype=None):
     if device.type != "cuda":
         _refuse("codes have to be on the GPU")
     y = t.empty((rows, cols), dtype=dtype, device=device)
-    with _On(device) as st:
-        _b.iodf_unpack(qp, ep, rows, cols, y.data_ptr(), _types[dtype], cols, st)
+    _call("unpack", device, qp, ep, rows, cols, y.data_ptr(), _types[dtype], cols)
     return y
 
 
 # ---- join ----
 
-def _join_params(h, alpha, gate, w_post, w_pre, live):
-    rows, cols = h.shape
-    device = h.device
-    gate_rows = rows
+def _join_params(rows, cols, device, alpha, gate, w_post, w_pre, live):
+    gate_rows, gp = rows, 0
     if gate is not None:
         groups = 1 if gate.dim() == 1 else gate.shape[0]
-        if groups < 1 and rows or groups > 1 and rows % groups:
-            _refuse("gate has %d rows, which do not divide the %d rows" % (groups, rows))
+        if gate.dim() not in (1, 2) or gate.shape[-1] != cols or groups < 1 and rows or groups > 1 and rows % groups:
+            _refuse("gate is %s: [cols] or [groups, cols] is wanted, groups that divide the %d rows" % (list(gate.shape), rows))
         gate_rows = rows // groups if groups else 0
-        gate_shape = (cols,) if gate.dim() == 1 else (groups, cols)
-    return (max(gate_rows, 1), _vector(alpha, "alpha", (1,), device), None if gate is None else _vector(gate, "gate", gate_shape, device),
-            _vector(w_post, "w_post", (cols,), device), _vector(w_pre, "w_pre", (cols,), device), _live(live, rows, device))
+        gp = _vector(gate, "gate", groups * cols, device)
+    return (gate_rows or 1, _vector(alpha, "alpha", 1, device), gp, _vector(w_post, "w_post", cols, device), _vector(w_pre, "w_pre", cols, device),
+            _live(live, rows, device))
 
 
 def join(h, f, alpha=None, gate=None, w_post=None, w_pre=None, live=None, eps=1e-6, save=True, h_out=None):
@@ -193,57 +206,53 @@ def join(h, f, alpha=None, gate=None, w_post=None, w_pre=None, live=None, eps=1e
 
     gate is [cols] or [groups, cols], rows in groups of equal length. w_post None: no norm behind the block; w_pre None: no u (None).
     save=False keeps nothing (None), for inference. h_out may be h."""
-    t = _t()
+    t = _torch or _setup()
     th, sh = _matrix(h, "h")
-    rows, cols = h.shape
-    tf, sf = _matrix(f, "f", rows, cols)
-    _same_device(h.device, f=f, h_out=h_out)
-    gate_rows, ap, gp, wop, wip, lp = _join_params(h, alpha, gate, w_post, w_pre, live)
+    shape = rows, cols = tuple(h.shape)
+    device = h.device
+    tf, sf = _matrix(f, "f", shape, None, device)
+    gate_rows, ap, gp, wop, wip, lp = _join_params(rows, cols, device, alpha, gate, w_post, w_pre, live)
     if h_out is None:
-        h_out = t.empty((rows, cols), dtype=h.dtype, device=h.device)
-    _, so = _matrix(h_out, "h_out", rows, cols, h.dtype)
-    u = t.empty((rows, cols), dtype=f.dtype, device=h.device) if w_pre is not None else None
-    saved, c = None, (None,) * 6
+        h_out, so = t.empty(shape, dtype=h.dtype, device=device), cols
+    else:
+        _, so = _matrix(h_out, "h_out", shape, h.dtype, device)
+    u = t.empty(shape, dtype=f.dtype, device=device) if w_pre is not None else None
+    saved, c = None, (0, 0, 0, 0, 0, 0)
     if save:
-        x, n = _new_codes(rows, cols, h.device) if w_pre is not None else None, _new_codes(rows, cols, h.device)
-        inv = t.empty((2, rows), dtype=t.float32, device=h.device)
+        x, n = _new_codes(rows, cols, device) if w_pre is not None else None, _new_codes(rows, cols, device)
+        inv = t.empty((2, rows), dtype=_f32, device=device)
         saved = JoinSaved(x, n, inv[0] if w_pre is not None else None, inv[1] if w_post is not None else None)
-        c = (x and x.q.data_ptr(), x and x.e.data_ptr(), n.q.data_ptr(), n.e.data_ptr(), inv.data_ptr(), inv.data_ptr() + 4 * rows)
-    args = _b.JoinArgs(rows, gate_rows, cols, th, tf, eps, ap, gp, wop, wip, lp, h.data_ptr(), f.data_ptr(), h_out.data_ptr(),
-                       u.data_ptr() if u is not None else None, sh, sf, so, cols, *c)
-    with _On(h.device) as st:
-        _b.iodf_join_forward(args, st)
+        c = (x.q.data_ptr() if x else 0, x.e.data_ptr() if x else 0, n.q.data_ptr(), n.e.data_ptr(), inv.data_ptr(), inv.data_ptr() + 4 * rows)
+    _call("join_forward", device, _JOIN.pack(rows, gate_rows, cols, th, tf, eps, ap, gp, wop, wip, lp, h.data_ptr(), f.data_ptr(), h_out.data_ptr(),
+                                             u.data_ptr() if u is not None else 0, sh, sf, so, cols, *c, 0, 0, 0, 0))
     return h_out, u, saved
 
 
 def join_backward(saved, dh, du, alpha=None, gate=None, w_post=None, w_pre=None, live=None, block_dtype=None):
     """dL/dh' and dL/du (None where join gave no u) -> JoinGrads; df has du's type, or block_dtype."""
-    t = _t()
+    t = _torch or _setup()
     th, sh = _matrix(dh, "dh")
-    rows, cols = dh.shape
+    shape = rows, cols = tuple(dh.shape)
     device = dh.device
     if (du is None) != (w_pre is None):
         _refuse("du belongs to w_pre: both or none")
     block_dtype = du.dtype if du is not None else block_dtype or dh.dtype
-    tf, sf = _matrix(du, "du", rows, cols, block_dtype) if du is not None else (_types[block_dtype], cols)
-    _same_device(device, du=du)
-    gate_rows, ap, gp, wop, wip, lp = _join_params(dh, alpha, gate, w_post, w_pre, live)
-    xq, xe = _codes(saved.x, "saved.x", rows, cols, device) if w_pre is not None else (None, None)
+    tf, sf = _matrix(du, "du", shape, block_dtype, device) if du is not None else (_types[block_dtype], cols)
+    gate_rows, ap, gp, wop, wip, lp = _join_params(rows, cols, device, alpha, gate, w_post, w_pre, live)
+    xq, xe = _codes(saved.x, "saved.x", rows, cols, device) if w_pre is not None else (0, 0)
     nq, ne = _codes(saved.n, "saved.n", rows, cols, device)
-    ipre = _vector(saved.inv_pre, "saved.inv_pre", (rows,), device) if w_pre is not None else None
-    ipost = _vector(saved.inv_post, "saved.inv_post", (rows,), device) if w_post is not None else None
-    if (w_pre is not None and ipre is None and rows) or (w_post is not None and ipost is None and rows):
+    ipre = _vector(saved.inv_pre, "saved.inv_pre", rows, device) if w_pre is not None else 0
+    ipost = _vector(saved.inv_post, "saved.inv_post", rows, device) if w_post is not None else 0
+    if rows and (w_pre is not None and saved.inv_pre is None or w_post is not None and saved.inv_post is None):
         _refuse("saved lacks a norm's factors")
-    dh_out = t.empty((rows, cols), dtype=dh.dtype, device=device)
-    df = t.empty((rows, cols), dtype=block_dtype, device=device)
+    dh_out = t.empty(shape, dtype=dh.dtype, device=device)
+    df = t.empty(shape, dtype=block_dtype, device=device)
     grads = [None if p is None else t.empty_like(p) for p in (alpha, gate, w_post, w_pre)]
-    args = _b.JoinArgs(rows, gate_rows, cols, th, tf, 1.0, ap, gp, wop, wip, lp, dh.data_ptr(), du.data_ptr() if du is not None else None,
+    block = _JOIN.pack(rows, gate_rows, cols, th, tf, 1.0, ap, gp, wop, wip, lp, dh.data_ptr(), du.data_ptr() if du is not None else 0,
                        dh_out.data_ptr(), df.data_ptr(), sh, sf, cols, cols, xq, xe, nq, ne, ipre, ipost,
-                       *[None if g is None else g.data_ptr() for g in grads])
-    with _On(device) as st:
-        need = _b.iodf_join_workspace(args)
-        work = t.empty((need,), dtype=t.uint8, device=device)
-        _b.iodf_join_backward(args, work.data_ptr(), need, st)
+                       *[0 if g is None else g.data_ptr() for g in grads])
+    work, need = _workspace("join_workspace", block, device)
+    _call("join_backward", device, block, work.data_ptr(), need)
     return JoinGrads(dh_out, df, *grads)
 
 
@@ -257,26 +266,24 @@ def _act(act):
 
 def glu(a, b, act="silu", live=None, save=True):
     """y = act(a) * b -> (y, GluSaved or None)."""
-    t = _t()
+    t = _torch or _setup()
     kind, sa = _matrix(a, "a")
-    rows, cols = a.shape
-    _, sb = _matrix(b, "b", rows, cols, a.dtype)
-    _same_device(a.device, b=b)
-    code, lp = _act(act), _live(live, rows, a.device)
-    y = t.empty((rows, cols), dtype=a.dtype, device=a.device)
-    saved, c = None, (None,) * 4
+    shape = rows, cols = tuple(a.shape)
+    device = a.device
+    _, sb = _matrix(b, "b", shape, a.dtype, device)
+    code, lp = _act(act), _live(live, rows, device)
+    y = t.empty(shape, dtype=a.dtype, device=device)
+    saved, c = None, (0, 0, 0, 0)
     if save:
-        saved = GluSaved(_new_codes(rows, cols, a.device), _new_codes(rows, cols, a.device))
+        saved = GluSaved(_new_codes(rows, cols, device), _new_codes(rows, cols, device))
         c = (saved.a.q.data_ptr(), saved.a.e.data_ptr(), saved.b.q.data_ptr(), saved.b.e.data_ptr())
-    args = _b.GluArgs(rows, cols, kind, code, lp, a.data_ptr(), b.data_ptr(), y.data_ptr(), None, None, None, sa, sb, cols, 0, 0, 0, *c)
-    with _On(a.device) as st:
-        _b.iodf_glu_forward(args, st)
+    _call("glu_forward", device, _GLU.pack(rows, cols, kind, code, lp, a.data_ptr(), b.data_ptr(), y.data_ptr(), 0, 0, 0, sa, sb, cols, 0, 0, 0, *c, 0, 0))
     return y, saved
 
 
 def glu_backward(saved, dy, act="silu", live=None, rebuild=True):
     """dL/dy -> (dL/da, dL/db, Codes of y or None). The two gradients are the halves of one [rows, 2 cols] tensor."""
-    t = _t()
+    t = _torch or _setup()
     kind, sd = _matrix(dy, "dy")
     rows, cols = dy.shape
     device = dy.device
@@ -286,10 +293,8 @@ def glu_backward(saved, dy, act="silu", live=None, rebuild=True):
     dab = t.empty((rows, 2 * cols), dtype=dy.dtype, device=device)
     da, db = dab[:, :cols], dab[:, cols:]
     y = _new_codes(rows, cols, device) if rebuild else None
-    args = _b.GluArgs(rows, cols, kind, code, lp, None, None, None, dy.data_ptr(), da.data_ptr(), db.data_ptr(), 0, 0, 0, sd, 2 * cols,
-                      2 * cols, aq, ae, bq, be, y and y.q.data_ptr(), y and y.e.data_ptr())
-    with _On(device) as st:
-        _b.iodf_glu_backward(args, st)
+    _call("glu_backward", device, _GLU.pack(rows, cols, kind, code, lp, 0, 0, 0, dy.data_ptr(), da.data_ptr(), db.data_ptr(), 0, 0, 0, sd, 2 * cols,
+                                            2 * cols, aq, ae, bq, be, y.q.data_ptr() if y else 0, y.e.data_ptr() if y else 0))
     return da, db, y
 
 
@@ -297,28 +302,24 @@ def glu_backward(saved, dy, act="silu", live=None, rebuild=True):
 
 def weight_grad(codes, dy, col_scale=None, live=None, out=None, accumulate=False):
     """float32 [dy's columns, codes' columns]: (accumulate: out +) dy^T X * col_scale, X what the codes stand for."""
-    t = _t()
+    t = _torch or _setup()
     kind, sd = _matrix(dy, "dy")
     rows, n_out = dy.shape
     device = dy.device
     if not isinstance(codes, Codes):
         _refuse("codes has to be Codes")
-    qp, ep = _codes(codes, "codes", rows, codes.cols, device)
     cols = codes.cols
-    sp, lp = _vector(col_scale, "col_scale", (cols,), device), _live(live, rows, device)
+    qp, ep = _codes(codes, "codes", rows, cols, device)
+    sp, lp = _vector(col_scale, "col_scale", cols, device), _live(live, rows, device)
     if out is None:
         if accumulate:
             _refuse("accumulate adds to out: pass it")
-        out = t.empty((n_out, cols), dtype=t.float32, device=device)
-    _, so = _matrix(out, "out", n_out, cols, t.float32)
-    _same_device(device, out=out)
-    if n_out > 1 and out.stride(0) < cols:
-        _refuse("the rows of out overlap")
-    args = _b.WgradArgs(rows, cols, n_out, kind, 1 if accumulate else 0, dy.data_ptr(), sd, qp, ep, sp, lp, out.data_ptr(), so)
-    with _On(device) as st:
-        need = _b.iodf_weight_grad_workspace(args)
-        work = t.empty((need,), dtype=t.uint8, device=device) if need else None
-        _b.iodf_weight_grad(args, work.data_ptr() if need else None, need, st)
+        out, so = t.empty((n_out, cols), dtype=_f32, device=device), cols
+    else:
+        _, so = _matrix(out, "out", (n_out, cols), _f32, device)
+    block = _WGRAD.pack(rows, cols, n_out, kind, 1 if accumulate else 0, dy.data_ptr(), sd, qp, ep, sp, lp, out.data_ptr(), so)
+    work, need = _workspace("weight_grad_workspace", block, device)
+    _call("weight_grad", device, block, work.data_ptr(), need)
     return out
 
 
@@ -332,7 +333,7 @@ def _make_functions():
     global _functions
     if _functions is not None:
         return _functions
-    t = _t()
+    t = _torch or _setup()
 
     def rows_first(x):
         return x if x.stride(-1) == 1 and (x.shape[0] <= 1 or x.stride(0) >= x.shape[1]) else x.contiguous()

@@ -393,7 +393,7 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
 
     const std::true_type checked;
     const std::false_type whole;
-    // the loads of a tile count LOADS and follow one another as in phase B
+    // the loads of a tile count LOADS and follow one another as in phase B: codes two, dy two
     auto begin = [&](auto guarded) {
         start_codes(0, t0, guarded);
 #pragma unroll
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
             start_codes(k + 1, t0 + (k + 1) * KT, guarded);
             start_dy(k, t0 + k * KT, guarded);
         }
-        wait_loads<guarded ? 0 : 2 * LOADS>();
+        wait_loads<guarded ? 0 : 2 + LOADS>();  // codes of tiles 0, 1 and 2 (whose first half phase A of tile 0 takes) and dy of tile 0 have landed
         take_codes(0, 0), take_codes(1, 0);
         widen(0, 0), widen(1, 0);
         take_codes(0, 1), take_codes(1, 1);
@@ -491,25 +491,48 @@ struct Plan : Tiles {
     int bm, bn;  // a tile's edges
 };
 
+// What a kind of tile costs, in microseconds: everything but the loop, a step of KT rows when a compute unit has one workgroup of the kind, and
+// what each of several adds to a step. Measured with dy in bfloat16; parts of dy are multiplied one after the other.
+struct TileCost {
+    int bm, bn;
+    float base, step, each;
+};
+constexpr TileCost kTiles[] = {{64, 64, 4.3f, 0.26f, 0.17f}, {64, 128, 6.3f, 0.30f, 0.24f}, {128, 64, 6.3f, 0.30f, 0.24f}, {128, 128, 8.3f, 0.36f, 0.33f},
+                               {WIDE, WIDE, 14.f, 0.84f, 0.84f}};
+
+// The tile and the number of slices of least estimated time. Large tiles read operands less often, small ones fill the chip with few outputs and
+// end sooner; slices do so with few tiles, at the price of their sums' way through memory (about 0.36 us a megabyte there and back) and of a second
+// launch. Over 18 shapes from 64 x 512 x 512 to 131072 x 512 x 512, timed with every tile and slices in powers of two, the choice is at most 8 %
+// behind the best of them; one fixed rule (the largest tile that fills the chip, slices for 512 workgroups) was up to 2.7 times behind (512 x 2048
+// x 2048: 44 us against 16).
 Plan plan_of(const iodf_wgrad& a) {
-    Plan p;
     auto up = [](long long n, long long d) { return (n + d - 1) / d; };
-    if (a.dy_type == IODF_T_BF16 && a.dy_stride <= (1 << 24) && a.out > 128 && a.cols > 128 && up(a.out, WIDE) * up(a.cols, WIDE) * up(a.rows, 1024) >= 256) {
-        p.bm = p.bn = WIDE;
-    } else {
-        p.bm = a.out > 64 ? 128 : 64;
-        p.bn = a.cols > 64 ? 128 : 64;
+    const float parts = a.dy_type == IODF_T_BF16 ? 1.f : a.dy_type == IODF_T_F16 ? 1.9f : 2.7f;
+    Plan best{};
+    float least = 0.f;
+    for (const TileCost& k : kTiles) {
+        // the wide kernel has dy in bfloat16 only and 32-bit offsets within a tile; no tile is twice as large as the layer
+        if (k.bm == WIDE && (a.dy_type != IODF_T_BF16 || a.dy_stride > (1 << 24) || a.out <= 128 || a.cols <= 128)) continue;
+        if ((k.bm == 128 && a.out <= 64) || (k.bn == 128 && a.cols <= 64)) continue;
+        const int unit = k.bm == WIDE ? RING * KT : KT;  // rows that its loop takes at a time
+        const long long m = up(a.out, k.bm), n = up(a.cols, k.bn);
+        const long long fill = std::max<long long>(1, 256 / (m * n));  // slices that give every unit one workgroup at most
+        for (int k2 = -1; k2 <= 10; ++k2) {
+            long long splits = k2 < 0 ? fill : 1ll << k2;
+            if (splits > 1 && (splits > 1024 || a.rows / splits < KT)) continue;
+            if (a.live) splits = std::max<long long>(splits, up(a.rows, kLiveRows));
+            const long long slice = up(up(a.rows, splits), unit) * unit;
+            splits = slice ? up(a.rows, slice) : 1;
+            const float steps = (float)(slice / KT), a_unit = (float)up(m * n * splits, 256), outputs = 4e-6f * a.out * a.cols;
+            float t = k.base + steps * parts * std::max(k.step, a_unit * k.each);
+            t += splits > 1 ? 3.f + 0.36f * outputs * splits : 0.2f * outputs;
+            if (!best.bm || t < least) {
+                least = t;
+                best.m = (int)m, best.n = (int)n, best.splits = (int)splits, best.slice = (int)slice, best.bm = k.bm, best.bn = k.bn;
+            }
+        }
     }
-    const int unit = p.bm == WIDE ? RING * KT : KT;  // what the loop takes at a time
-    p.m = (int)up(a.out, p.bm);
-    p.n = (int)up(a.cols, p.bn);
-    const long long n = (long long)p.m * p.n, at_once = p.bm == WIDE ? 256 : 512;
-    long long splits = std::max<long long>(1, at_once / n);
-    splits = std::min<long long>(splits, std::max<long long>(1, a.rows / 128));
-    if (a.live) splits = std::max<long long>(splits, up(a.rows, kLiveRows));
-    p.slice = (int)(up(up(a.rows, splits), unit) * unit);
-    p.splits = p.slice ? (int)up(a.rows, p.slice) : 1;
-    return p;
+    return best;
 }
 
 template <typename TY>

@@ -398,6 +398,31 @@ def test_weight_grad_of_32_bits_loses_no_bit_of_dy():
     assert np.array_equal(host(got), dy.astype(np.float64).T @ x)
 
 
+@pytest.mark.parametrize("rows,cols,out,name", [(40960, 512, 512, "bf16"), (8192, 1024, 1024, "bf16"), (30000, 136, 264, "bf16"), (20000, 64, 200, "f16")])
+def test_weight_grad_of_operands_that_come_late(rows, cols, out, name):
+    """Operands that other data has driven out of every cache, call after call without a wait between, against operands that a call has
+    just read: the same bits, whatever the order in which loads land."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(5)
+    sets = []
+    for _ in range(3):
+        x = t.randn((rows, cols), generator=gen, device="cuda")
+        d = t.randn((rows, out), generator=gen, device="cuda").to(dtype(name))
+        codes = iodf.pack(x)
+        want = iodf.weight_grad(codes, d)
+        t.cuda.synchronize()
+        want = iodf.weight_grad(codes, d)
+        exact = t.matmul(d.double().t(), iodf.unpack(codes).double())
+        assert (want.double() - exact).norm() <= 1e-5 * exact.norm()
+        sets.append((codes, d, want))
+    other = t.empty(1 << 29, dtype=t.uint8, device="cuda")   # twice the largest cache
+    for _ in range(6):
+        other.add_(1)
+        got = [iodf.weight_grad(codes, d) for codes, d, _ in sets]
+        for g, (_, _, want) in zip(got, sets):
+            assert t.equal(g, want)
+
+
 def test_weight_grad_spreads_an_infinity_no_further_than_its_column():
     rng, codes, x, dy, d0, _ = wgrad_case(100, 64, 40, "f32", "all")
     dy[17, 5] = np.inf
