@@ -398,6 +398,30 @@ def test_weight_grad_of_32_bits_loses_no_bit_of_dy():
     assert np.array_equal(host(got), dy.astype(np.float64).T @ x)
 
 
+@pytest.mark.parametrize("rows,cols,out", [(40001, 520, 1031), (33000, 1000, 257), (16384, 2048, 2048), (131073, 264, 392), (20000, 4095, 520),
+                                           (9001, 2050, 2100)])
+@pytest.mark.parametrize("mode", ["all", "some"])
+def test_weight_grad_of_large_layers(rows, cols, out, mode):
+    """Against a 64-bit product on the GPU: many rows, sides that are multiples of nothing, padding, a scale, added to what is there."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(rows)
+    live = t.rand(rows, generator=gen, device="cuda") < 0.8 if mode == "some" else None
+    x = t.randn((rows, cols), generator=gen, device="cuda")
+    d = (t.randn((rows, out), generator=gen, device="cuda") + 0.1).bfloat16()
+    scale, before = (t.randn(n, generator=gen, device="cuda") for n in ((cols,), (out, cols)))
+    d0 = d.double()
+    if live is not None:
+        d0[~live] = 0
+        d[~live] = float("nan")
+    codes = iodf.pack(x, live=live)
+    v = iodf.unpack(codes).double()
+    got = iodf.weight_grad(codes, d, col_scale=scale, live=live, out=before.clone(), accumulate=True).double()
+    want = before.double() + scale.double() * (d0.t().contiguous() @ v)
+    mass = before.double().abs() + scale.double().abs() * (d0.abs().t().contiguous() @ v.abs())
+    # the sum of a slice takes sixteen rows at a time and may round at each step, slices are added in runs of a few
+    assert ((got - want).abs() <= (min(rows, 1 << 14) / 16 + SLACK) * U * mass).all()
+
+
 @pytest.mark.parametrize("rows,cols,out,name", [(40960, 512, 512, "bf16"), (8192, 1024, 1024, "bf16"), (30000, 136, 264, "bf16"), (20000, 64, 200, "f16")])
 def test_weight_grad_of_operands_that_come_late(rows, cols, out, name):
     """Operands that other data has driven out of every cache, call after call without a wait between, against operands that a call has
