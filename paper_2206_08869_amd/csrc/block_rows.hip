@@ -3,7 +3,6 @@
 // A row is held in the registers of LPR threads, NV vectors of eight columns each, so that it is read once although its two norms are
 // sums over it. All row types are widened to 32-bit floats on the way in and rounded once on the way out.
 #include "block_dev.h"
-#include "flow_kernels.h"
 
 #include <algorithm>
 
@@ -165,14 +164,14 @@ struct Runs {
     int per_group, chunk, groups, gate_rows;
 };
 
-// dx = du * w_pre, dz = dh' + inv_pre (dx - x mean(dx x)), dn = coef dz, df = inv_post (dn - n mean(dn n)); sums over the run's rows of
-// du x and of dz n (where every row has a gate of its own: of gate dz n, and dgate is written at once).
-// The second mean needs the first one, but it is linear in dz: with m = coef n,
-//   sum(dn n) = sum(m dh') + inv_pre (sum(m dx) - mean(dx x) sum(m x)),
-// so that a row meets once, for four sums, and not twice.
+// dx = du * w_pre, dz = dh' + inv_pre (dx - x mean(dx x)), dn = alpha gate w_post dz, df = inv_post (dn - n mean(dn n)); sums over the run's rows
+// of du x and of dz n (where every row has a gate of its own: of gate dz n, and dgate is written at once).
+// The second mean needs the first one, but it is linear in dz: with m = gate w_post n,
+//   sum(m dz) = sum(m dh') + inv_pre (sum(m dx) - mean(dx x) sum(m x)),
+// so that a row meets once, for four sums, and not twice. That sum is also the row's part of dalpha (and alpha may be 0).
 template <typename TH, typename TF, int LPR, int NV, bool OWN>
 __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR <= 64 ? 3 : 4) void k_join_backward(const iodf_join a, const Runs runs, const int over_h, const int over_u,
-                                                                     float* sum_pre, float* sum_post, unsigned* ticket) {
+                                                                     float* sum_pre, float* sum_post, double* sum_alpha) {
     constexpr int THREADS = threads_of<LPR>(), TEAMS = THREADS / LPR;
     __shared__ RowSums<LPR, 4> meet;
     int turn = 0;
@@ -181,7 +180,6 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
     const int cols = a.cols, pitch = (cols + 31) / 32 * 32, wide = (cols + 7) / 8 * 8;
     const float inv_cols = 1.f / (float)cols;
     const float alpha = a.alpha ? a.alpha[0] : 1.f;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
     const int group = OWN ? 0 : blockIdx.x / runs.per_group, part = OWN ? blockIdx.x : blockIdx.x % runs.per_group;
     const int rows = (int)a.rows;
     const int group_end = OWN ? rows : min((long long)rows, (long long)(group + 1) * runs.gate_rows);
@@ -197,7 +195,7 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
         load_params(a.gate && !OWN ? a.gate + (long long)group * cols : nullptr, c0, cols, coef[v], 1.f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            coef[v][i] *= alpha * wp[i];
+            coef[v][i] *= wp[i];
             pre[v][i] = post[v][i] = 0.f;
         }
     }
@@ -233,6 +231,7 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
         r.ip = a.w_post ? a.inv_post[row] : 1.f;
         return r;
     };
+    double to_alpha = 0;
     constexpr bool AHEAD = NV == 1;  // two vectors to a thread leave no registers for another row
     Row next;
     int row = first + team;
@@ -295,7 +294,9 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
             if (a.w_pre) forget(r.u[v]), forget(r.x[v]);
         }
         row_sums<LPR, 4>(sum, meet, turn);
-        const float mean_x = sum[0] * inv_cols, mean_n = a.w_post ? (sum[1] + r.iq * (sum[2] - mean_x * sum[3])) * inv_cols : 0.f;
+        const float mean_x = sum[0] * inv_cols, part_alpha = sum[1] + r.iq * (sum[2] - mean_x * sum[3]);
+        const float mean_n = a.w_post ? alpha * part_alpha * inv_cols : 0.f, scale_n = alpha * r.ip;
+        to_alpha += part_alpha;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             float dz[8], n[8], gate[8], share[8], dn[8];
@@ -318,11 +319,11 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
                 if (OWN) {
                     dn[i] *= gate[i];
                     post[v][i] += gate[i] * share[i];
-                    share[i] *= coef[v][i];
+                    share[i] *= alpha * coef[v][i];
                 } else {
                     post[v][i] += share[i];
                 }
-                dn[i] = fmaf(r.ip, dn[i], -back * n[i]);
+                dn[i] = fmaf(scale_n, dn[i], -back * n[i]);
             }
             store8(dho + c[v].c0, c[v].n, dz);
             store8(df + c[v].c0, c[v].n, dn);
@@ -330,6 +331,14 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
         }
     }
     // the teams' sums meet in the order of the teams
+    if (TEAMS > 1) {
+        __shared__ double alphas[TEAMS];
+        if (tid == 0) alphas[team] = to_alpha;
+        __syncthreads();
+        to_alpha = 0;
+        for (int m = 0; m < TEAMS; ++m) to_alpha += alphas[m];
+    }
+    if (threadIdx.x == 0) sum_alpha[blockIdx.x] = to_alpha;
     float* const to[2] = {sum_pre + (long long)blockIdx.x * wide, sum_post + (long long)blockIdx.x * wide};
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -353,37 +362,57 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
         }
 }
 
-// The parameters' gradients from the runs' sums. A workgroup has FC columns and FR threads for each, which share the runs: in the second row
-// of workgroups for dw_pre, over all, in the first one group by group for dgate = alpha w_post S, dw_post = alpha sum gate S, S a group's sum. The workgroup that ends last
-// adds the workgroups' parts of dalpha = sum gate w_post S, in their order.
-constexpr int FC = 16, FR = 64;
+// The parameters' gradients from the runs' sums. A workgroup has FC columns and FR threads for each, which share the runs: in the first row of
+// workgroups group by group for dgate = alpha w_post S and dw_post = alpha sum gate S, S a group's sum, in the second one over all runs for
+// dw_pre; a workgroup of the third one adds the runs' parts of dalpha.
+constexpr int FC = 16, FR = 64;  // a wave has four threads of each column
 
 __device__ __forceinline__ float column_sum(const float* p, int n, int wide, int lane, int lanes) {
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int r = lane; r < n; r += 8 * lanes)
+    float s[16] = {};
+    for (int r = lane; r < n; r += 16 * lanes)
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (r + k * lanes < n) s[k] += p[(long long)(r + k * lanes) * wide];
-    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+        for (int k = 0; k < 16; ++k) s[k] += r + k * lanes < n ? p[(long long)(r + k * lanes) * wide] : 0.f;
+#pragma unroll
+    for (int d = 8; d; d /= 2)
+#pragma unroll
+        for (int k = 0; k < d; ++k) s[k] += s[k + d];
+    return s[0];
 }
 
 __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const Runs runs, int n_runs, const float* sum_pre,
-                                                        const float* sum_post, double* parts, unsigned* ticket) {
-    __shared__ float meet[FR][FC];
-    __shared__ double total[FR][FC];
+                                                        const float* sum_post, const double* sum_alpha) {
+    __shared__ double meet[FR / 4][FC];
     const int col = threadIdx.x % FC, lane = threadIdx.x / FC, c = blockIdx.x * FC + col;
     const int cols = a.cols, wide = (cols + 7) / 8 * 8;
     const bool there = c < cols;
     const float alpha = a.alpha ? a.alpha[0] : 1.f;
     const float wp = there && a.w_post ? a.w_post[c] : 1.f;
-    if (blockIdx.y) {
-        meet[lane][col] = there ? column_sum(sum_pre + c, n_runs, wide, lane, FR) : 0.f;
-        __syncthreads();
-        if (lane == 0 && there) {
-            double s = 0;
-            for (int k = 0; k < FR; ++k) s += meet[k][col];
-            a.dw_pre[c] = (float)s;
+    // the sum over `lanes` neighbouring lanes of a column, for the first of them: four are in a wave, then through LDS
+    auto over_lanes = [&](double v, int lanes) {
+        if (lanes >= 2) v += __shfl_xor(v, FC);
+        if (lanes >= 4) v += __shfl_xor(v, 2 * FC);
+        if (lanes > 4) {
+            if (lane % 4 == 0) meet[lane / 4][col] = v;
+            __syncthreads();
+            if (lane % lanes == 0)
+                for (int k = 1; k < lanes / 4; ++k) v += meet[lane / 4 + k][col];
+            __syncthreads();
         }
+        return v;
+    };
+    if (blockIdx.y == 2) {
+        if (blockIdx.x) return;
+        double s = 0;
+        for (int k = threadIdx.x; k < n_runs; k += FC * FR) s += sum_alpha[k];
+        for (int k = 1; k < FC; k *= 2) s += __shfl_xor(s, k);
+        s = over_lanes(s, FR);
+        if (threadIdx.x == 0) a.dalpha[0] = (float)s;
+        return;
+    }
+    if (blockIdx.y) {
+        if (!a.dw_pre) return;
+        const double s = over_lanes(there ? column_sum(sum_pre + c, n_runs, wide, lane, FR) : 0.f, FR);
+        if (lane == 0 && there) a.dw_pre[c] = (float)s;
         return;
     }
     // FR threads of a column are cut into `teams` for as many groups at a time
@@ -396,11 +425,8 @@ __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const
     for (int g0 = 0; g0 < groups; g0 += teams) {
         const int g = g0 + team;
         const bool mine = there && g < groups;
-        meet[lane][col] = mine ? column_sum(sum_post + (long long)g * per_group * wide + c, per_group, wide, sub, lanes) : 0.f;
-        if (lanes > 1) __syncthreads();
+        const double s = over_lanes(mine ? column_sum(sum_post + (long long)g * per_group * wide + c, per_group, wide, sub, lanes) : 0.f, lanes);
         if (mine && sub == 0) {
-            double s = 0;
-            for (int k = 0; k < lanes; ++k) s += meet[lane + k][col];
             if (own_gate || !a.gate) {
                 weighted += s;  // the gates are in the sums already, or are 1
             } else {
@@ -409,31 +435,9 @@ __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const
                 a.dgate[at] = (float)(alpha * wp * s);
             }
         }
-        if (lanes > 1) __syncthreads();
     }
-    total[lane][col] = weighted;
-    __syncthreads();
-    if (lane == 0) {
-        double s = 0;
-        for (int k = 0; k < FR; ++k) s += total[k][col];
-        if (there && a.dw_post) a.dw_post[c] = (float)(alpha * s);
-        total[0][col] = there ? wp * s : 0;
-    }
-    __syncthreads();
-    if (!a.dalpha) return;
-    __shared__ bool is_last;
-    if (threadIdx.x == 0) {
-        double s = 0;
-        for (int k = 0; k < FC; ++k) s += total[0][k];
-        __hip_atomic_store(&parts[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        is_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!is_last || threadIdx.x >= 64) return;
-    double s = 0;
-    for (int k = threadIdx.x; k < (int)gridDim.x; k += 64) s += __hip_atomic_load(&parts[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
-    if (threadIdx.x == 0) a.dalpha[0] = (float)s;
+    weighted = over_lanes(weighted, FR);
+    if (lane == 0 && there && a.dw_post) a.dw_post[c] = (float)(alpha * weighted);
 }
 
 // Workgroups of a kernel that the chip holds at once.
@@ -512,22 +516,19 @@ template <typename TH, typename TF, int LPR, int NV>
 hipError_t backward_of(const iodf_join& a, void* work, hipStream_t st) {
     const Runs r = runs_of(a.rows, a.cols, a.gate ? a.gate_rows : a.rows);
     const long long n = n_runs(r, a.rows);
-    const size_t wide = (a.cols + 7) / 8 * 8, parts = (a.cols + FC - 1) / FC;
-    unsigned* const ticket = (unsigned*)work;
-    double* const part = (double*)((char*)work + 16);
-    float* const pre = (float*)((char*)part + up16(parts * 8));
+    const size_t wide = (a.cols + 7) / 8 * 8, tiles = (a.cols + FC - 1) / FC;
+    double* const to_alpha = (double*)work;
+    float* const pre = (float*)((char*)work + up16(n * 8));
     float* const post = pre + n * wide;
     const int over_h = (int)over_rows(a.rows, a.cols, a.in_stream_stride), over_u = a.w_pre ? (int)over_rows(a.rows, a.cols, a.in_block_stride) : 0;
-    hipError_t e = hipSuccess;
     if (n) {
-        if (r.gate_rows == 1) k_join_backward<TH, TF, LPR, NV, true><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, ticket);
-        else k_join_backward<TH, TF, LPR, NV, false><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, ticket);
-        e = hipGetLastError();
-    } else {
-        e = launch_fill_zero(ticket, 16, st);
+        if (r.gate_rows == 1) k_join_backward<TH, TF, LPR, NV, true><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, to_alpha);
+        else k_join_backward<TH, TF, LPR, NV, false><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, to_alpha);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    if (e != hipSuccess) return e;
-    k_join_params<<<dim3((unsigned)parts, a.dw_pre ? 2 : 1), FC * FR, 0, st>>>(a, r, (int)n, pre, post, part, ticket);
+    if (!a.dalpha && !a.dgate && !a.dw_post && !a.dw_pre) return hipSuccess;
+    k_join_params<<<dim3((unsigned)tiles, a.dalpha ? 3 : a.dw_pre ? 2 : 1), FC * FR, 0, st>>>(a, r, (int)n, pre, post, to_alpha);
     return hipGetLastError();
 }
 
@@ -560,8 +561,8 @@ hipError_t launch_join_forward(const iodf_join& a, hipStream_t st) {
 
 size_t join_workspace(long long rows, int cols, long long gate_rows) {
     const Runs r = runs_of(rows, cols, gate_rows);
-    const size_t wide = (cols + 7) / 8 * 8, parts = (cols + FC - 1) / FC;
-    return 16 + up16(parts * 8) + 2 * (size_t)n_runs(r, rows) * wide * 4;
+    const size_t wide = (cols + 7) / 8 * 8, n = (size_t)n_runs(r, rows);
+    return 16 + up16(n * 8) + 2 * n * wide * 4;
 }
 
 hipError_t launch_join_backward(const iodf_join& a, void* work, hipStream_t st) {

@@ -468,11 +468,11 @@ __global__ __launch_bounds__(256) void k_wgrad_join(const iodf_wgrad a, int spli
     vec s = 0.f;
     if (i < n) {
         int k = lane;
-        for (; k + 3 * JL < splits; k += 4 * JL) {
-            vec v[4];
+        for (; k + 7 * JL < splits; k += 8 * JL) {
+            vec v[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = *(const vec*)(partial + (k + u * JL) * n + i);
-            s += (v[0] + v[1]) + (v[2] + v[3]);
+            for (int u = 0; u < 8; ++u) v[u] = *(const vec*)(partial + (k + u * JL) * n + i);
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
         for (; k < splits; k += JL) s += *(const vec*)(partial + k * n + i);
     }

@@ -241,6 +241,21 @@ def test_join_backward(rows, cols, stream, block, groups, mode, what):
         assert (a is None) == (b is None) and (a is None or torch().equal(a, b))
 
 
+def test_join_backward_at_a_residual_scale_of_zero():
+    """Where residual scales start: nothing of the block is in the stream, its gradients are 0, the scale's own is not."""
+    rng, p, live = join_case(8, 60, 200, "f32", "bf16", 3, "some")
+    p["alpha"] = np.float32([0.0])
+    h2, u, saved = iodf.join(dev(p["h"]), dev(p["f"], "bf16"), *params_on_gpu(p), live=on_gpu(live))
+    assert np.array_equal(host(h2), p["h"].astype(np.float32))
+    dh, du = rng.standard_normal((60, 200)).astype(np.float32), as_type(rng.standard_normal((60, 200)), "bf16")
+    g = iodf.join_backward(saved, dev(dh), dev(du, "bf16"), *params_on_gpu(p), live=on_gpu(live))
+    x, n = (ref.decode(c.q.cpu().numpy(), c.e.cpu().numpy(), 200) for c in (saved.x, saved.n))
+    r = ref.join_backward(x, n, host(saved.inv_pre), host(saved.inv_post), dh, du, p["alpha"], p["gate"], p["w_post"], p["w_pre"], live)
+    assert not host(g.df).any() and not host(g.dgate).any() and not host(g.dw_post).any()
+    mass = (np.abs(r["dh"]) * ref.per_row(p["gate"], 60, 200) * np.abs(p["w_post"] * n)).sum()
+    assert abs(host(g.dalpha)[0] - r["dalpha"][0]) <= 2 * SLACK * U * mass and abs(r["dalpha"][0]) > 0
+
+
 def test_join_backward_keeps_what_stands_in_padded_rows_to_itself():
     """NaN in dL/dh' of a padded row comes out where it went in, and reaches no gradient of a parameter."""
     rng, p, live = join_case(3, 40, 72, "f32", "f32", 4, "some")
