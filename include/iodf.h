@@ -245,8 +245,8 @@ int iodf_profile_end(iodf_ctx* ctx, iodf_kernel_stat* stats, int max_stats, int*
  * nothing between calls; scratch is the caller's (iodf_join_workspace, iodf_weight_grad_workspace). All pointers are device
  * memory. A tensor is rows x cols with consecutive columns; strides count elements from row to row and are at least the columns.
  * Any element address will do. rows may be 0 (no work; gradients that sum over rows are then 0); 0 <= rows <= 2^30,
- * 1 <= cols <= 65536. `live` (may be NULL) holds a byte for each row, 0 where the row is padding: its entries in tensors may be
- * anything, NaN included, and add nothing to any gradient.
+ * 1 <= cols <= 65536, rows * (cols rounded up to 32) <= 2^35. `live` (may be NULL) holds a byte for each row, 0 where the row
+ * is padding: its entries in tensors may be anything, NaN included, and add nothing to any gradient.
  *
  * What the backward pass needs is kept as a checkpoint in 8 bits. For rows x cols values, with pitch = cols rounded up to 32:
  * q int8 [rows][pitch] (16-byte aligned) and e uint8 [rows][pitch / 32], one exponent for 32 columns; q * 2^(e - 133) is the value.
@@ -275,8 +275,9 @@ int iodf_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int cols, void*
  * iodf_join_forward: in_stream = h, in_block = f -> out_stream = h', out_block = u; with xq, not NULL, also the checkpoints of
  *   x and n and the factors inv_pre = 1 / rms(h'), inv_post = 1 / rms(f) of each row (0 in padded rows).
  * iodf_join_backward: in_stream = dL/dh', in_block = dL/du and the checkpoint -> out_stream = dL/dh, out_block = dL/df
- *   (rounded to those types; may not overlap anything) and the sums dalpha [1], dgate [gate rows][cols], dw_post [cols], dw_pre [cols] (each NULL
- *   exactly where its parameter is). x and n stand for what the checkpoint holds. The result is the same bits on every call.
+ *   (rounded to those types; may not overlap anything) and the sums dalpha [1], dgate [gate rows][cols], dw_post [cols],
+ *   dw_pre [cols] (each NULL exactly where its parameter is). x and n stand for what the checkpoint holds. At most 2^21 gate rows,
+ *   or one for each row. The result is the same bits on every call.
  */
 typedef struct iodf_join {
     int64_t rows, gate_rows;
@@ -340,7 +341,8 @@ int iodf_glu_backward(const iodf_glu* args, void* stream);
  *   dw[o][c] = (accumulate ? dw[o][c] : 0) + col_scale[c] * sum_t dy[t][o] * X[t][c]
  * dy [rows][out] of dy_type, X what the checkpoint stands for, dw F32 with rows dw_stride apart. col_scale (may be NULL): the
  * weight of the norm between the checkpoint and the layer (w_pre of iodf_join). Products are exact for every dy_type,
- * sums are 32-bit floats, in an order that depends on the sizes alone. 1 <= out <= 65536.
+ * sums are 32-bit floats, in an order that depends on the sizes alone. 1 <= out <= 65536,
+ * rows * (out rounded up to 32) <= 2^35.
  */
 typedef struct iodf_wgrad {
     int64_t rows;

@@ -7,7 +7,8 @@ using namespace iodf;
 
 namespace {
 
-constexpr int64_t kMaxRows = 1ll << 30, kMaxElems = 1ll << 36;
+// what a launch can count (less than 2^32 threads): the backward pass of a join has at least one workgroup for each shared gate
+constexpr int64_t kMaxRows = 1ll << 30, kMaxElems = 1ll << 35, kMaxGates = 1ll << 21;
 constexpr int kMaxCols = 65536;
 
 bool a_type(int t) { return t == IODF_T_F32 || t == IODF_T_BF16 || t == IODF_T_F16; }
@@ -34,7 +35,6 @@ int check_glu(const iodf_glu* a) {
 
 int check_wgrad(const iodf_wgrad* a) {
     if (!a || !a_shape(a->rows, a->cols, kMaxCols) || !a_shape(a->rows, a->out, kMaxCols) || !a_type(a->dy_type)) return IODF_E_ARG;
-    if ((int64_t)a->out * a->cols > (1ll << 32)) return IODF_E_ARG;
     return IODF_OK;
 }
 
@@ -81,7 +81,7 @@ int iodf_join_forward(const iodf_join* a, void* stream) {
 int iodf_join_workspace(const iodf_join* a, int64_t* bytes) {
     const int rc = check_join(a);
     if (rc != IODF_OK) return rc;
-    if (!bytes) return IODF_E_ARG;
+    if (!bytes || (a->gate && a->gate_rows > 1 && (a->rows - 1) / a->gate_rows >= kMaxGates)) return IODF_E_ARG;
     *bytes = (int64_t)join_workspace(a->rows, a->cols, a->gate ? a->gate_rows : a->rows);
     return IODF_OK;
 }

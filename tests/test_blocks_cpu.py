@@ -195,3 +195,14 @@ def test_plain_form_s_activation_slope(kind):
     a = np.linspace(-8, 8, 401) + 1e-3
     d = (ref.act(a + 1e-6, kind)[0] - ref.act(a - 1e-6, kind)[0]) / 2e-6
     assert np.abs(d - ref.act(a, kind)[1]).max() < 1e-8
+
+
+def test_more_than_a_launch_can_count_is_refused(lib, buf):
+    n = ctypes.c_int64(0)
+    a = join_args(buf[1], rows=1 << 24, gate_rows=8)  # 2^21 shared gates: the most that the backward pass takes
+    assert lib.iodf_join_workspace(a, n) == 0
+    a.gate_rows = 7
+    assert lib.iodf_join_workspace(a, n) == E_ARG
+    a.gate_rows = 1
+    assert lib.iodf_join_workspace(a, n) == 0
+    assert lib.iodf_pack(buf[1], 1, 65536, (1 << 19) + 1, 65536, None, buf[1], buf[1], None) == E_ARG
