@@ -281,8 +281,8 @@ def glu(a, b, act="silu", live=None, save=True):
     return y, saved
 
 
-def glu_backward(saved, dy, act="silu", live=None, rebuild=True):
-    """dL/dy -> (dL/da, dL/db, Codes of y or None). The two gradients are the halves of one [rows, 2 cols] tensor."""
+def _glu_backward(saved, dy, act, live, rebuild):
+    """The gradients of a and b side by side, [rows, 2 cols], and the Codes of y."""
     t = _torch or _setup()
     kind, sd = _matrix(dy, "dy")
     rows, cols = dy.shape
@@ -291,11 +291,18 @@ def glu_backward(saved, dy, act="silu", live=None, rebuild=True):
     bq, be = _codes(saved.b, "saved.b", rows, cols, device)
     code, lp = _act(act), _live(live, rows, device)
     dab = t.empty((rows, 2 * cols), dtype=dy.dtype, device=device)
-    da, db = dab[:, :cols], dab[:, cols:]
     y = _new_codes(rows, cols, device) if rebuild else None
-    _call("glu_backward", device, _GLU.pack(rows, cols, kind, code, lp, 0, 0, 0, dy.data_ptr(), da.data_ptr(), db.data_ptr(), 0, 0, 0, sd, 2 * cols,
-                                            2 * cols, aq, ae, bq, be, y.q.data_ptr() if y else 0, y.e.data_ptr() if y else 0))
-    return da, db, y
+    da = dab.data_ptr()
+    _call("glu_backward", device, _GLU.pack(rows, cols, kind, code, lp, 0, 0, 0, dy.data_ptr(), da, da + cols * dab.element_size(), 0, 0, 0, sd,
+                                            2 * cols, 2 * cols, aq, ae, bq, be, y.q.data_ptr() if y else 0, y.e.data_ptr() if y else 0))
+    return dab, y
+
+
+def glu_backward(saved, dy, act="silu", live=None, rebuild=True):
+    """dL/dy -> (dL/da, dL/db, Codes of y or None). The two gradients are the halves of one [rows, 2 cols] tensor."""
+    dab, y = _glu_backward(saved, dy, act, live, rebuild)
+    cols = dy.shape[1]
+    return dab[:, :cols], dab[:, cols:], y
 
 
 # ---- weight gradient ----
@@ -338,17 +345,21 @@ def _make_functions():
     def rows_first(x):
         return x if x.stride(-1) == 1 and (x.shape[0] <= 1 or x.stride(0) >= x.shape[1]) else x.contiguous()
 
+    once = t.autograd.function.once_differentiable
+
     class Joined(t.autograd.Function):
         @staticmethod
         def forward(ctx, h, f, alpha, gate, w_post, w_pre, live, eps, hold):
             h2, u, saved = join(h, f, alpha, gate, w_post, w_pre, live=live, eps=eps, save=True)
-            ctx.params, ctx.saved, ctx.live, ctx.block = (alpha, gate, w_post, w_pre), saved, live, f.dtype
+            ctx.save_for_backward(alpha, gate, w_post, w_pre)
+            ctx.saved, ctx.live, ctx.block = saved, live, f.dtype
             hold.append(saved)
             return (h2, u) if u is not None else h2
 
         @staticmethod
+        @once
         def backward(ctx, dh, du=None):
-            g = join_backward(ctx.saved, rows_first(dh), None if du is None else rows_first(du), *ctx.params, live=ctx.live,
+            g = join_backward(ctx.saved, rows_first(dh), None if du is None else rows_first(du), *ctx.saved_tensors, live=ctx.live,
                               block_dtype=ctx.block)
             return (*g, None, None, None)
 
@@ -356,14 +367,17 @@ def _make_functions():
         @staticmethod
         def forward(ctx, u, weight, codes, col_scale, live):
             w = weight.to(u.dtype)
-            ctx.w, ctx.codes, ctx.col_scale, ctx.live, ctx.dtype = w, codes, col_scale, live, weight.dtype
+            ctx.save_for_backward(w, col_scale)
+            ctx.codes, ctx.live, ctx.dtype = codes, live, weight.dtype
             return u @ w.t()
 
         @staticmethod
+        @once
         def backward(ctx, dy):
+            w, col_scale = ctx.saved_tensors
             dy = rows_first(dy)
-            dw = weight_grad(ctx.codes, dy, col_scale=ctx.col_scale, live=ctx.live).to(ctx.dtype)
-            return dy @ ctx.w, dw, None, None, None
+            dw = weight_grad(ctx.codes, dy, col_scale=col_scale, live=ctx.live).to(ctx.dtype)
+            return dy @ w, dw, None, None, None
 
     class GatedProjection(t.autograd.Function):
         @staticmethod
@@ -371,15 +385,17 @@ def _make_functions():
             cols = ab.shape[1] // 2
             y, saved = glu(ab[:, :cols], ab[:, cols:], act, live=live)
             w = weight.to(y.dtype)
-            ctx.w, ctx.saved, ctx.act, ctx.live, ctx.dtype = w, saved, act, live, weight.dtype
+            ctx.save_for_backward(w)
+            ctx.saved, ctx.act, ctx.live, ctx.dtype = saved, act, live, weight.dtype
             return y @ w.t()
 
         @staticmethod
+        @once
         def backward(ctx, do):
+            w, = ctx.saved_tensors
             do = rows_first(do)
-            da, db, y = glu_backward(ctx.saved, do @ ctx.w, ctx.act, live=ctx.live)
-            dw = weight_grad(y, do, live=ctx.live).to(ctx.dtype)
-            return da._base, dw, None, None
+            dab, y = _glu_backward(ctx.saved, do @ w, ctx.act, ctx.live, True)
+            return dab, weight_grad(y, do, live=ctx.live).to(ctx.dtype), None, None
 
     _functions = (Joined, Projection, GatedProjection)
     return _functions

@@ -579,3 +579,26 @@ def test_differentiable_calls():
     want = t.autograd.grad((((t.sigmoid(a) * a * b) @ w2.t()) * dy).sum() + (z * dy).sum(), wide)
     for g, w in zip(got, want):
         assert (g.double() - w).norm() <= 0.03 * w.norm()
+
+
+def test_differentiable_calls_refuse_changed_parameters_and_second_derivatives():
+    """The backward pass reads the parameters again, so a change in place between the passes is an error, as for torch's own operations; the
+    gradients have no gradients of their own."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(8)
+    h, f, w = (t.randn(s, generator=gen, device="cuda").requires_grad_() for s in ((40, 32), (40, 32), (48, 32)))
+    w_pre, w_out = t.ones(32, device="cuda", requires_grad=True), t.randn((32, 24), generator=gen, device="cuda").requires_grad_()
+
+    def run():
+        _, u, codes = iodf.joined(h, f, w_pre=w_pre)
+        return iodf.gated_projection(iodf.projection(u, w, codes, col_scale=w_pre.detach()), w_out).square().sum()
+
+    for changed in (w_pre, w, w_out):
+        out = run()
+        with t.no_grad():
+            changed.mul_(2.0)
+        with pytest.raises(RuntimeError, match="inplace"):
+            out.backward()
+    g, = t.autograd.grad(run(), f, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.sum().backward()
