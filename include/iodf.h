@@ -245,7 +245,7 @@ int iodf_profile_end(iodf_ctx* ctx, iodf_kernel_stat* stats, int max_stats, int*
  * nothing between calls; scratch is the caller's (iodf_join_workspace, iodf_weight_grad_workspace). All pointers are device
  * memory. A tensor is rows x cols with consecutive columns; strides count elements from row to row and are at least the columns.
  * Any element address will do. rows may be 0 (no work; gradients that sum over rows are then 0); 0 <= rows <= 2^30,
- * 1 <= cols <= 65536, rows * (cols rounded up to 32) <= 2^35. `live` (may be NULL) holds a byte for each row, 0 where the row
+ * 1 <= cols <= 65536, rows * (cols rounded up to 32) <= 2^34. `live` (may be NULL) holds a byte for each row, 0 where the row
  * is padding: its entries in tensors may be anything, NaN included, and add nothing to any gradient.
  *
  * What the backward pass needs is kept as a checkpoint in 8 bits. For rows x cols values, with pitch = cols rounded up to 32:
@@ -342,7 +342,7 @@ int iodf_glu_backward(const iodf_glu* args, void* stream);
  * dy [rows][out] of dy_type, X what the checkpoint stands for, dw F32 with rows dw_stride apart. col_scale (may be NULL): the
  * weight of the norm between the checkpoint and the layer (w_pre of iodf_join). Products are exact for every dy_type,
  * sums are 32-bit floats, in an order that depends on the sizes alone. 1 <= out <= 65536,
- * rows * (out rounded up to 32) <= 2^35.
+ * rows * (out rounded up to 32) <= 2^34.
  */
 typedef struct iodf_wgrad {
     int64_t rows;

@@ -11,7 +11,7 @@
 namespace iodf {
 
 constexpr int kCodeGroup = 32;          // columns that share an exponent
-constexpr int kJoinMaxCols = 16384;     // widest row that the join's workgroups hold in registers
+constexpr int kJoinMaxCols = 16384;     // widest row of a join: two vectors of eight columns to each of 1024 threads
 
 inline int code_pitch(int cols) { return (cols + kCodeGroup - 1) / kCodeGroup * kCodeGroup; }
 

@@ -8,7 +8,7 @@ using namespace iodf;
 namespace {
 
 // what a launch can count (less than 2^32 threads): the backward pass of a join has at least one workgroup for each shared gate
-constexpr int64_t kMaxRows = 1ll << 30, kMaxElems = 1ll << 35, kMaxGates = 1ll << 21;
+constexpr int64_t kMaxRows = 1ll << 30, kMaxElems = 1ll << 34, kMaxGates = 1ll << 21;
 constexpr int kMaxCols = 65536;
 
 bool a_type(int t) { return t == IODF_T_F32 || t == IODF_T_BF16 || t == IODF_T_F16; }

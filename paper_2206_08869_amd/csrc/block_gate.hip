@@ -1,6 +1,18 @@
 // Checkpoints of single tensors, and the gated activation of a block's hidden layer with its gradients out of a checkpoint: passes
-// over all elements, bound by memory. A thread takes VECS vectors of eight columns, a workgroup a run of neighbouring ones that
+// over all elements, bound by memory. A thread takes one or two vectors of eight columns, a workgroup a run of neighbouring ones that
 // goes on across row ends, so that narrow rows fill it too; a vector's four lanes are a group of the checkpoint.
+//
+// Two vectors a thread where it loads little (a checkpoint, or 16 bits of one tensor), one elsewhere. Microseconds for 2^26 elements, silu,
+// with one / two / four:          512 columns           1000 columns          floor (a copy's 5.1 TB/s)
+//   pack      16 bits             38.4 / 36.0 / 40.4    41.6 / 41.0 / 43.0    39.7
+//             32 bits             58.2 / 61.1 / 62.1    60.0 / 61.8 / 65.6    65.9
+//   unpack    to 16 bits          33.3 / 32.7 / 33.5    36.5 / 33.9 / 34.3    39.7
+//   glu       16 bits, saved      96.2 / 103 / 107      101 / 107 / 116       105
+//             32 bits, saved      163 / 167 / 170       165 / 180 / 176       184
+//   gradient  16 bits             113 / 119 / 120       115 / 122 / 131       119
+//             32 bits             188 / 191 / 196       192 / 198 / 205       198
+// Below the floor, since parts of tensors this size stay in the last-level cache from call to call. All are bound by memory; the arithmetic
+// of an activation, its slope and two codes hides behind it.
 #include "block_dev.h"
 
 #include <algorithm>
@@ -9,7 +21,11 @@ namespace iodf {
 
 namespace {
 
-constexpr int TPB = 256, VECS = 2;
+constexpr int TPB = 256;
+
+template <typename T>
+constexpr int pack_vecs() { return sizeof(T) == 2 ? 2 : 1; }
+constexpr int UNPACK_VECS = 2, GLU_VECS = 1;
 
 struct Grid {
     long long rows;
@@ -19,7 +35,7 @@ struct Grid {
 };
 
 // Row and first column of this thread's vector k. Within a workgroup the vectors are counted from the row in which it starts, a
-// number below vectors + TPB * VECS < 2^14, so the product with the reciprocal gives the exact quotient (vectors <= 2^13).
+// number below vectors + TPB * VECS <= 2^13 + 2^9, so the product with the reciprocal gives the exact quotient (vectors <= 2^13).
 __device__ __forceinline__ void place(const Grid& g, long long row0, unsigned rem, int k, long long& row, int& c0, int& n) {
     const unsigned t = rem + k * TPB + threadIdx.x;
     const unsigned q = __umulhi(t, g.magic);
@@ -34,6 +50,7 @@ __device__ __forceinline__ void put_codes(const Grid& g, int8_t* q, uint8_t* e, 
 
 template <typename T>
 __global__ __launch_bounds__(TPB) void k_pack(const Grid g, const T* x, long long stride, const uint8_t* live, int8_t* q, uint8_t* e) {
+    constexpr int VECS = pack_vecs<T>();
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
     Raw8<T> r[VECS];
@@ -59,6 +76,7 @@ __global__ __launch_bounds__(TPB) void k_pack(const Grid g, const T* x, long lon
 
 template <typename T>
 __global__ __launch_bounds__(TPB) void k_unpack(const Grid g, const int8_t* q, const uint8_t* e, T* y, long long stride) {
+    constexpr int VECS = UNPACK_VECS;
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
     RawCodes r[VECS];
@@ -82,6 +100,7 @@ __global__ __launch_bounds__(TPB) void k_unpack(const Grid g, const int8_t* q, c
 
 template <typename T, int ACT>
 __global__ __launch_bounds__(TPB) void k_glu_forward(const Grid g, const iodf_glu a) {
+    constexpr int VECS = GLU_VECS;
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
     Raw8<T> ra[VECS], rb[VECS];
@@ -115,6 +134,7 @@ __global__ __launch_bounds__(TPB) void k_glu_forward(const Grid g, const iodf_gl
 
 template <typename T, int ACT>
 __global__ __launch_bounds__(TPB) void k_glu_backward(const Grid g, const iodf_glu a) {
+    constexpr int VECS = GLU_VECS;
     const long long first = (long long)blockIdx.x * (TPB * VECS), row0 = first / g.vectors;
     const unsigned rem = (unsigned)(first - row0 * g.vectors);
     Raw8<T> rd[VECS];
@@ -153,7 +173,7 @@ __global__ __launch_bounds__(TPB) void k_glu_backward(const Grid g, const iodf_g
     }
 }
 
-Grid grid_of(long long rows, int cols, unsigned& blocks, long long stride0 = 0, long long stride1 = 0) {
+Grid grid_of(long long rows, int cols, int vecs, unsigned& blocks, long long stride0 = 0, long long stride1 = 0) {
     Grid g;
     g.rows = rows;
     g.cols = cols;
@@ -162,14 +182,14 @@ Grid grid_of(long long rows, int cols, unsigned& blocks, long long stride0 = 0, 
     g.magic = (unsigned)((1ull << 32) / g.vectors) + 1;
     g.over[0] = stride0 ? over_rows(rows, cols, stride0) : 0;
     g.over[1] = stride1 ? over_rows(rows, cols, stride1) : 0;
-    blocks = (unsigned)((rows * g.vectors + TPB * VECS - 1) / (TPB * VECS));
+    blocks = (unsigned)((rows * g.vectors + TPB * vecs - 1) / (TPB * vecs));
     return g;
 }
 
 template <typename T>
 hipError_t glu_forward_of(const iodf_glu& a, hipStream_t st) {
     unsigned blocks;
-    const Grid g = grid_of(a.rows, a.cols, blocks, a.a_stride, a.b_stride);
+    const Grid g = grid_of(a.rows, a.cols, GLU_VECS, blocks, a.a_stride, a.b_stride);
     if (a.act == IODF_ACT_RELU) k_glu_forward<T, IODF_ACT_RELU><<<blocks, TPB, 0, st>>>(g, a);
     else if (a.act == IODF_ACT_SILU) k_glu_forward<T, IODF_ACT_SILU><<<blocks, TPB, 0, st>>>(g, a);
     else k_glu_forward<T, IODF_ACT_GELU><<<blocks, TPB, 0, st>>>(g, a);
@@ -179,7 +199,7 @@ hipError_t glu_forward_of(const iodf_glu& a, hipStream_t st) {
 template <typename T>
 hipError_t glu_backward_of(const iodf_glu& a, hipStream_t st) {
     unsigned blocks;
-    const Grid g = grid_of(a.rows, a.cols, blocks, a.dy_stride);
+    const Grid g = grid_of(a.rows, a.cols, GLU_VECS, blocks, a.dy_stride);
     if (a.act == IODF_ACT_RELU) k_glu_backward<T, IODF_ACT_RELU><<<blocks, TPB, 0, st>>>(g, a);
     else if (a.act == IODF_ACT_SILU) k_glu_backward<T, IODF_ACT_SILU><<<blocks, TPB, 0, st>>>(g, a);
     else k_glu_backward<T, IODF_ACT_GELU><<<blocks, TPB, 0, st>>>(g, a);
@@ -191,7 +211,7 @@ hipError_t glu_backward_of(const iodf_glu& a, hipStream_t st) {
 hipError_t launch_pack(const void* x, int type, long long stride, long long rows, int cols, const uint8_t* live, int8_t* q,
                        uint8_t* e, hipStream_t st) {
     unsigned blocks;
-    const Grid g = grid_of(rows, cols, blocks, stride);
+    const Grid g = grid_of(rows, cols, type == IODF_T_F32 ? pack_vecs<float>() : pack_vecs<__bf16>(), blocks, stride);
     if (type == IODF_T_F32) k_pack<float><<<blocks, TPB, 0, st>>>(g, (const float*)x, stride, live, q, e);
     else if (type == IODF_T_BF16) k_pack<__bf16><<<blocks, TPB, 0, st>>>(g, (const __bf16*)x, stride, live, q, e);
     else k_pack<_Float16><<<blocks, TPB, 0, st>>>(g, (const _Float16*)x, stride, live, q, e);
@@ -201,7 +221,7 @@ hipError_t launch_pack(const void* x, int type, long long stride, long long rows
 hipError_t launch_unpack(const int8_t* q, const uint8_t* e, long long rows, int cols, void* y, int type, long long stride,
                          hipStream_t st) {
     unsigned blocks;
-    const Grid g = grid_of(rows, cols, blocks);
+    const Grid g = grid_of(rows, cols, UNPACK_VECS, blocks);
     if (type == IODF_T_F32) k_unpack<float><<<blocks, TPB, 0, st>>>(g, q, e, (float*)y, stride);
     else k_unpack<__bf16><<<blocks, TPB, 0, st>>>(g, q, e, (__bf16*)y, stride);
     return hipGetLastError();

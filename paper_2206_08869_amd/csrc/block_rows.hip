@@ -1,7 +1,7 @@
 // The join of two blocks of a residual network (norm behind, gate, residual scale, addition, norm before) and its gradients.
 //
-// A row is held in the registers of LPR threads, NV vectors of eight columns each, so that it is read once although its two norms are
-// sums over it. All row types are widened to 32-bit floats on the way in and rounded once on the way out.
+// A row is held in the registers of LPR threads, a vector or two of eight columns each, so that it is read once although its two norms are
+// sums over it. All row types are widened to 32-bit floats on the way in and rounded once on the way out. Both passes are bound by memory.
 #include "block_dev.h"
 
 #include <algorithm>
@@ -9,6 +9,8 @@
 namespace iodf {
 
 namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Threads of a workgroup: several rows to a workgroup up to a wave a row, one row past that, whose sums meet in LDS.
 template <int LPR>
@@ -32,6 +34,10 @@ __device__ __forceinline__ void load_params(const float* p, int c0, int cols, fl
 }
 
 // n = f / rms(f), h' = h + coef * n, x = h' / rms(h'), u = w_pre * x.
+// As many workgroups as the chip holds, each with its columns' parameters in registers over all its rows; the next row is on its way while a row's
+// two sums are taken. Where a wave has a whole row (up to 1024 columns, with two vectors a thread up from 512) no barrier is needed.
+// With a checkpoint, 131072 x 512: 192 us for a stream in 32 bits, 137 us in 16 (both 4.9 TB/s; a large copy reaches 5.1); 4.9 to 5.4 TB/s for
+// aligned widths from 512 to 16384, 5.3 at 128. Below 64 columns, with 8 threads a row, the time is the launch's and the rows' own (26 us).
 template <typename TH, typename TF, int LPR, int NV>
 __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_join a, const int over_h, const int over_f) {
     constexpr int TEAMS = threads_of<LPR>() / LPR;
@@ -164,14 +170,19 @@ struct Runs {
     int per_group, chunk, groups, gate_rows;
 };
 
+// The gradients of a join, from dh', du and the codes of x and n:
 // dx = du * w_pre, dz = dh' + inv_pre (dx - x mean(dx x)), dn = alpha gate w_post dz, df = inv_post (dn - n mean(dn n)); sums over the run's rows
 // of du x and of dz n (where every row has a gate of its own: of gate dz n, and dgate is written at once).
 // The second mean needs the first one, but it is linear in dz: with m = gate w_post n,
 //   sum(m dz) = sum(m dh') + inv_pre (sum(m dx) - mean(dx x) sum(m x)),
 // so that a row meets once, for four sums, and not twice. That sum is also the row's part of dalpha (and alpha may be 0).
-template <typename TH, typename TF, int LPR, int NV, bool OWN>
-__global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR <= 64 ? 3 : 4) void k_join_backward(const iodf_join a, const Runs runs, const int over_h, const int over_u,
-                                                                     float* sum_pre, float* sum_post, double* sum_alpha) {
+// One vector to a thread, kept as it was loaded and widened again behind the meeting: held as 32-bit floats it would spill. Registers for four
+// waves a SIMD where that spills little, three where rows are 32 bits or a wave's own.
+// 32768 x 4096 in bfloat16: 272 us for 1.35 GB (5.0 TB/s); aligned widths from 512 to 8192: 4.2 to 4.6 TB/s with inputs in 16 bits or a stream in 32;
+// 3.3 to 3.8 TB/s for odd widths, whose vectors straddle lines.
+template <typename TH, typename TF, int LPR, bool OWN>
+__global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR <= 64 ? 3 : 4) void k_join_backward(
+    const iodf_join a, const Runs runs, const int over_h, const int over_u, float* sum_pre, float* sum_post, double* sum_alpha) {
     constexpr int THREADS = threads_of<LPR>(), TEAMS = THREADS / LPR;
     __shared__ RowSums<LPR, 4> meet;
     int turn = 0;
@@ -185,28 +196,22 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
     const int group_end = OWN ? rows : min((long long)rows, (long long)(group + 1) * runs.gate_rows);
     const int first = (OWN ? 0 : group * runs.gate_rows) + part * runs.chunk;
     const int last = min((long long)group_end, (long long)first + runs.chunk);
-    float coef[NV][8], wq[NV][8], pre[NV][8], post[NV][8];
+    float coef[8], wq[8], pre[8], post[8];
+    float wp[8];
+    const Columns c = columns_at(tid * 8, cols);
+    load_params(a.w_pre, c.c0, cols, wq, 0.f);
+    load_params(a.w_post, c.c0, cols, wp, 1.f);
+    load_params(a.gate && !OWN ? a.gate + (long long)group * cols : nullptr, c.c0, cols, coef, 1.f);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c0 = (v * LPR + tid) * 8;
-        float wp[8];
-        load_params(a.w_pre, c0, cols, wq[v], 0.f);
-        load_params(a.w_post, c0, cols, wp, 1.f);
-        load_params(a.gate && !OWN ? a.gate + (long long)group * cols : nullptr, c0, cols, coef[v], 1.f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            coef[v][i] *= wp[i];
-            pre[v][i] = post[v][i] = 0.f;
-        }
+    for (int i = 0; i < 8; ++i) {
+        coef[i] *= wp[i];
+        pre[i] = post[i] = 0.f;
     }
-    Columns c[NV];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) c[v] = columns_at((v * LPR + tid) * 8, cols);
     struct Row {
-        Raw8<TH> h[NV];
-        Raw8<TF> u[NV];
-        RawCodes x[NV], n[NV];
-        Raw8<float> gate[OWN ? NV : 1];
+        Raw8<TH> h;
+        Raw8<TF> u;
+        RawCodes x, n;
+        Raw8<float> gate;
         float iq, ip;
         bool live;
     };
@@ -217,118 +222,105 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
         const TH* const dh = (const TH*)a.in_stream + (long long)row * a.in_stream_stride;
         const TF* const du = (const TF*)a.in_block + (long long)row * a.in_block_stride;
         const long long q = (long long)row * pitch, e = (long long)row * (pitch / 32);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            r.h[v] = fetch_row(dh, c[v], row < over_h);
-            r.n[v] = {*(const u32x2*)(a.nq + q + c[v].at), (a.ne + e)[c[v].at / 32]};
-            if (a.w_pre) {
-                r.u[v] = fetch_row(du, c[v], row < over_u);
-                r.x[v] = {*(const u32x2*)(a.xq + q + c[v].at), (a.xe + e)[c[v].at / 32]};
-            }
-            if (OWN) r.gate[v] = fetch_row(a.gate + (long long)row * cols, c[v], false);
+        r.h = fetch_row(dh, c, row < over_h);
+        r.n = {*(const u32x2*)(a.nq + q + c.at), (a.ne + e)[c.at / 32]};
+        if (a.w_pre) {
+            r.u = fetch_row(du, c, row < over_u);
+            r.x = {*(const u32x2*)(a.xq + q + c.at), (a.xe + e)[c.at / 32]};
         }
+        if (OWN) r.gate = fetch_row(a.gate + (long long)row * cols, c, false);
         r.iq = a.w_pre ? a.inv_pre[row] : 0.f;
         r.ip = a.w_post ? a.inv_post[row] : 1.f;
         return r;
     };
     double to_alpha = 0;
-    constexpr bool AHEAD = NV == 1;  // two vectors to a thread leave no registers for another row
     Row next;
     int row = first + team;
-    if (AHEAD && row < last) next = fetch(row);
+    if (row < last) next = fetch(row);
     for (; row < last; row += TEAMS) {
-        Row r = AHEAD ? next : fetch(row);
-        if (AHEAD && row + TEAMS < last) next = fetch(row + TEAMS);  // on its way while this row's sums are taken
+        Row r = next;
+        if (row + TEAMS < last) next = fetch(row + TEAMS);  // on its way while this row's sums are taken
         TH* const dho = (TH*)a.out_stream + (long long)row * a.out_stream_stride;
         TF* const df = (TF*)a.out_block + (long long)row * a.out_block_stride;
         float* const dgate = OWN ? a.dgate + (long long)row * cols : nullptr;
         if (!r.live) {  // padding goes to dL/dh as it came, and nowhere else
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                float dz[8];
-                const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                widen8(r.h[v], dz);
-                store8(dho + c[v].c0, c[v].n, dz);
-                store8(df + c[v].c0, c[v].n, none);
-                if (OWN) store8(dgate + c[v].c0, c[v].n, none);
-            }
+            float dz[8];
+            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            widen8(r.h, dz);
+            store8(dho + c.c0, c.n, dz);
+            store8(df + c.c0, c.n, none);
+            if (OWN) store8(dgate + c.c0, c.n, none);
             continue;
         }
         // a lane's eight columns have one step: the codes are used as numbers, and sums get their steps at the end
         float sum[4] = {0.f, 0.f, 0.f, 0.f};  // of dx x, m dh', m dx, m x
-        float sx[NV], sn[NV];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
+        const float sn = code_step(r.n.e), sx = a.w_pre ? code_step(r.x.e) : 0.f;
+        {
             float dh[8], du[8], x[8], n[8], gate[8], part[4] = {0.f, 0.f, 0.f, 0.f};
-            c[v].cut(r.h[v]);
-            if (a.w_pre) c[v].cut(r.u[v]);
-            widen8(r.h[v], dh);
-            numbers8(r.n[v].q, n);
-            sn[v] = code_step(r.n[v].e);
-            if (OWN) widen8(r.gate[v], gate);
+            c.cut(r.h);
+            if (a.w_pre) c.cut(r.u);
+            widen8(r.h, dh);
+            numbers8(r.n.q, n);
+            if (OWN) widen8(r.gate, gate);
             if (a.w_pre) {
-                widen8(r.u[v], du);
-                numbers8(r.x[v].q, x);
-                sx[v] = code_step(r.x[v].e);
+                widen8(r.u, du);
+                numbers8(r.x.q, x);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float m = coef[v][i] * n[i];
+                float m = coef[i] * n[i];
                 if (OWN) m *= gate[i];
                 part[1] += m * dh[i];
                 if (a.w_pre) {
-                    const float dx = du[i] * wq[v][i];
-                    pre[v][i] += du[i] * sx[v] * x[i];
+                    const float dx = du[i] * wq[i];
+                    pre[i] += du[i] * sx * x[i];
                     part[0] += dx * x[i];
                     part[2] += m * dx;
                     part[3] += m * x[i];
                 }
             }
-            sum[1] += c[v].n ? part[1] * sn[v] : 0.f;
+            sum[1] += c.n ? part[1] * sn : 0.f;
             if (a.w_pre) {
-                sum[0] += c[v].n ? part[0] * sx[v] : 0.f;
-                sum[2] += c[v].n ? part[2] * sn[v] : 0.f;
-                sum[3] += c[v].n ? part[3] * sn[v] * sx[v] : 0.f;
+                sum[0] += c.n ? part[0] * sx : 0.f;
+                sum[2] += c.n ? part[2] * sn : 0.f;
+                sum[3] += c.n ? part[3] * sn * sx : 0.f;
             }
-            forget(r.h[v]), forget(r.n[v]);
-            if (a.w_pre) forget(r.u[v]), forget(r.x[v]);
+            forget(r.h), forget(r.n);
+            if (a.w_pre) forget(r.u), forget(r.x);
         }
         row_sums<LPR, 4>(sum, meet, turn);
         const float mean_x = sum[0] * inv_cols, part_alpha = sum[1] + r.iq * (sum[2] - mean_x * sum[3]);
         const float mean_n = a.w_post ? alpha * part_alpha * inv_cols : 0.f, scale_n = alpha * r.ip;
         to_alpha += part_alpha;
+        float dz[8], n[8], gate[8], share[8], dn[8];
+        widen8(r.h, dz);
+        numbers8(r.n.q, n);
+        if (OWN) widen8(r.gate, gate);
+        if (a.w_pre) {
+            float du[8], x[8];
+            widen8(r.u, du);
+            numbers8(r.x.q, x);
+            const float back = r.iq * mean_x * sx;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            float dz[8], n[8], gate[8], share[8], dn[8];
-            widen8(r.h[v], dz);
-            numbers8(r.n[v].q, n);
-            if (OWN) widen8(r.gate[v], gate);
-            if (a.w_pre) {
-                float du[8], x[8];
-                widen8(r.u[v], du);
-                numbers8(r.x[v].q, x);
-                const float back = r.iq * mean_x * sx[v];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dz[i] = fmaf(r.iq, du[i] * wq[v][i], fmaf(-back, x[i], dz[i]));
-            }
-            const float back = r.ip * mean_n * sn[v];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                share[i] = dz[i] * sn[v] * n[i];
-                dn[i] = coef[v][i] * dz[i];
-                if (OWN) {
-                    dn[i] *= gate[i];
-                    post[v][i] += gate[i] * share[i];
-                    share[i] *= alpha * coef[v][i];
-                } else {
-                    post[v][i] += share[i];
-                }
-                dn[i] = fmaf(scale_n, dn[i], -back * n[i]);
-            }
-            store8(dho + c[v].c0, c[v].n, dz);
-            store8(df + c[v].c0, c[v].n, dn);
-            if (OWN) store8(dgate + c[v].c0, c[v].n, share);
+            for (int i = 0; i < 8; ++i) dz[i] = fmaf(r.iq, du[i] * wq[i], fmaf(-back, x[i], dz[i]));
         }
+        const float back = r.ip * mean_n * sn;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            share[i] = dz[i] * sn * n[i];
+            dn[i] = coef[i] * dz[i];
+            if (OWN) {
+                dn[i] *= gate[i];
+                post[i] += gate[i] * share[i];
+                share[i] *= alpha * coef[i];
+            } else {
+                post[i] += share[i];
+            }
+            dn[i] = fmaf(scale_n, dn[i], -back * n[i]);
+        }
+        store8(dho + c.c0, c.n, dz);
+        store8(df + c.c0, c.n, dn);
+        if (OWN) store8(dgate + c.c0, c.n, share);
     }
     // the teams' sums meet in the order of the teams
     if (TEAMS > 1) {
@@ -341,30 +333,181 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
     if (threadIdx.x == 0) sum_alpha[blockIdx.x] = to_alpha;
     float* const to[2] = {sum_pre + (long long)blockIdx.x * wide, sum_post + (long long)blockIdx.x * wide};
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k) {
+        float t[8];
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c0 = (v * LPR + tid) * 8;
-            float t[8];
+        for (int i = 0; i < 8; ++i) t[i] = k ? post[i] : pre[i];
+        if (TEAMS > 1) {
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = k ? post[v][i] : pre[v][i];
-            if (TEAMS > 1) {
-                __syncthreads();
+            for (int i = 0; i < 8; ++i) joined[i * THREADS + threadIdx.x] = t[i];
+            __syncthreads();
+            if (team == 0)
+                for (int m = 1; m < TEAMS; ++m)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) joined[i * THREADS + threadIdx.x] = t[i];
-                __syncthreads();
-                if (team == 0)
-                    for (int m = 1; m < TEAMS; ++m)
+                    for (int i = 0; i < 8; ++i) t[i] += joined[i * THREADS + m * LPR + tid];
+        }
+        if (team == 0 && c.c0 < wide) store8(to[k] + c.c0, 8, t);
+    }
+}
+
+// The same for rows of more than 8192 columns, two vectors to each of 1024 threads: with 128 registers to a thread (64 KB of a row, its parameters
+// and sums in 256 KB), nothing of a row is held. The vectors are taken one after the other, each fetched while the one before is worked on, once
+// for the sums over the row and once more, out of L2, for the gradients; the columns' sums are in LDS and the parameters are read again.
+// 4096 x 16384: 275 us in bfloat16, 329 us with a stream in 32 bits (2.5 and 2.9 TB/s); rows held in registers, which spilled: 575 and 785.
+template <typename TH, typename TF, bool OWN>
+__global__ __launch_bounds__(1024) void k_join_backward_far(const iodf_join a, const Runs runs, const int over_h, const int over_u, float* sum_pre,
+                                                            float* sum_post, double* sum_alpha) {
+    constexpr int THREADS = 1024, NV = kJoinMaxCols / (8 * THREADS);
+    __shared__ RowSums<THREADS, 4> meet;
+    __shared__ f32x4 sums[2][NV][2][THREADS];
+    int turn = 0;
+    const int tid = threadIdx.x, cols = a.cols, pitch = (cols + 31) / 32 * 32, wide = (cols + 7) / 8 * 8;
+    const float inv_cols = 1.f / (float)cols;
+    const float alpha = a.alpha ? a.alpha[0] : 1.f;
+    const int group = OWN ? 0 : blockIdx.x / runs.per_group, part = OWN ? blockIdx.x : blockIdx.x % runs.per_group;
+    const int rows = (int)a.rows;
+    const int group_end = OWN ? rows : min((long long)rows, (long long)(group + 1) * runs.gate_rows);
+    const int first = (OWN ? 0 : group * runs.gate_rows) + part * runs.chunk;
+    const int last = min((long long)group_end, (long long)first + runs.chunk);
+    for (int v = 0; v < NV; ++v)
+        for (int k = 0; k < 2; ++k) sums[k][v][0][tid] = sums[k][v][1][tid] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](int k, int v, const float (&s)[8]) {  // a thread's own place: no barrier
+        sums[k][v][0][tid] += f32x4{s[0], s[1], s[2], s[3]};
+        sums[k][v][1][tid] += f32x4{s[4], s[5], s[6], s[7]};
+    };
+    struct Vector {
+        Raw8<TH> h;
+        Raw8<TF> u;
+        RawCodes x, n;
+    };
+    auto fetch = [&](int row, int v) {
+        Vector r;
+        const Columns c = columns_at((v * THREADS + tid) * 8, cols);
+        r.h = fetch_row((const TH*)a.in_stream + (long long)row * a.in_stream_stride, c, row < over_h);
+        r.n = {*(const u32x2*)(a.nq + (long long)row * pitch + c.at), (a.ne + (long long)row * (pitch / 32))[c.at / 32]};
+        if (a.w_pre) {
+            r.u = fetch_row((const TF*)a.in_block + (long long)row * a.in_block_stride, c, row < over_u);
+            r.x = {*(const u32x2*)(a.xq + (long long)row * pitch + c.at), (a.xe + (long long)row * (pitch / 32))[c.at / 32]};
+        }
+        return r;
+    };
+    double to_alpha = 0;
+    Vector next;
+    if (first < last) next = fetch(first, 0);
+    for (int row = first; row < last; ++row) {
+        const bool live = !a.live || a.live[row];
+        const float iq = a.w_pre ? a.inv_pre[row] : 0.f, ip = a.w_post ? a.inv_post[row] : 1.f;
+        const float* const gate = a.gate ? a.gate + (long long)(OWN ? row : group) * cols : nullptr;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};  // of dx x, m dh', m dx, m x
+        if (live) {
+#pragma unroll 1
+            for (int v = 0; v < NV; ++v) {
+                Vector r = next;
+                next = fetch(row, v + 1 < NV ? v + 1 : 0);
+                const Columns c = columns_at((v * THREADS + tid) * 8, cols);
+                float dh[8], n[8], m[8], by[8], part[4] = {0.f, 0.f, 0.f, 0.f};
+                load_params(a.w_post, c.c0, cols, m, 1.f);
+                load_params(gate, c.c0, cols, by, 1.f);
+                c.cut(r.h);
+                widen8(r.h, dh);
+                numbers8(r.n.q, n);
+                const float sn = code_step(r.n.e);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) t[i] += joined[i * THREADS + m * LPR + tid];
+                for (int i = 0; i < 8; ++i) {
+                    m[i] *= by[i] * n[i];
+                    part[1] += m[i] * dh[i];
+                }
+                sum[1] += c.n ? part[1] * sn : 0.f;
+                if (a.w_pre) {
+                    float du[8], x[8], to_pre[8];
+                    load_params(a.w_pre, c.c0, cols, by, 0.f);
+                    c.cut(r.u);
+                    widen8(r.u, du);
+                    numbers8(r.x.q, x);
+                    const float sx = code_step(r.x.e);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        to_pre[i] = du[i] * sx * x[i];
+                        part[0] += du[i] * by[i] * x[i];
+                        part[2] += m[i] * (du[i] * by[i]);
+                        part[3] += m[i] * x[i];
+                    }
+                    add(0, v, to_pre);
+                    sum[0] += c.n ? part[0] * sx : 0.f;
+                    sum[2] += c.n ? part[2] * sn : 0.f;
+                    sum[3] += c.n ? part[3] * sn * sx : 0.f;
+                }
             }
-            if (team == 0 && c0 < wide) store8(to[k] + c0, 8, t);
+            row_sums<THREADS, 4>(sum, meet, turn);
+        }
+        const float mean_x = sum[0] * inv_cols, part_alpha = sum[1] + iq * (sum[2] - mean_x * sum[3]);
+        const float mean_n = a.w_post ? alpha * part_alpha * inv_cols : 0.f, scale_n = alpha * ip;
+        if (live) to_alpha += part_alpha;
+        TH* const dho = (TH*)a.out_stream + (long long)row * a.out_stream_stride;
+        TF* const df = (TF*)a.out_block + (long long)row * a.out_block_stride;
+        float* const dgate = OWN ? a.dgate + (long long)row * cols : nullptr;
+#pragma unroll 1
+        for (int v = 0; v < NV; ++v) {
+            Vector r = next;
+            if (v + 1 < NV) next = fetch(row, v + 1);
+            else if (row + 1 < last) next = fetch(row + 1, 0);
+            const Columns c = columns_at((v * THREADS + tid) * 8, cols);
+            float dz[8], dn[8];
+            if (!live) {  // padding goes to dL/dh as it came, and nowhere else
+                widen8(r.h, dz);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dn[i] = 0.f;
+                store8(dho + c.c0, c.n, dz);
+                store8(df + c.c0, c.n, dn);
+                if (OWN) store8(dgate + c.c0, c.n, dn);
+                continue;
+            }
+            float n[8], coef[8], by[8];
+            c.cut(r.h);
+            widen8(r.h, dz);
+            if (a.w_pre) {
+                float du[8], x[8];
+                load_params(a.w_pre, c.c0, cols, by, 0.f);
+                c.cut(r.u);
+                widen8(r.u, du);
+                numbers8(r.x.q, x);
+                const float back = iq * mean_x * code_step(r.x.e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dz[i] = fmaf(iq, du[i] * by[i], fmaf(-back, x[i], dz[i]));
+            }
+            load_params(a.w_post, c.c0, cols, coef, 1.f);
+            load_params(gate, c.c0, cols, by, 1.f);
+            numbers8(r.n.q, n);
+            const float sn = code_step(r.n.e), back = ip * mean_n * sn;
+            float share[8], to_post[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                share[i] = dz[i] * sn * n[i];
+                to_post[i] = OWN ? by[i] * share[i] : share[i];
+                dn[i] = fmaf(scale_n, coef[i] * by[i] * dz[i], -back * n[i]);
+                share[i] *= alpha * coef[i];
+            }
+            add(1, v, to_post);
+            store8(dho + c.c0, c.n, dz);
+            store8(df + c.c0, c.n, dn);
+            if (OWN) store8(dgate + c.c0, c.n, share);
+        }
+    }
+    if (tid == 0) sum_alpha[blockIdx.x] = to_alpha;
+    for (int k = 0; k < 2; ++k)
+        for (int v = 0; v < NV; ++v) {
+            const int c0 = (v * THREADS + tid) * 8;
+            float* const to = (k ? sum_post : sum_pre) + (long long)blockIdx.x * wide + c0;
+            if (c0 < wide)
+                for (int half = 0; half < 2; ++half) *(f32x4*)(to + 4 * half) = sums[k][v][half][tid];
         }
 }
 
 // The parameters' gradients from the runs' sums. A workgroup has FC columns and FR threads for each, which share the runs: in the first row of
 // workgroups group by group for dgate = alpha w_post S and dw_post = alpha sum gate S, S a group's sum, in the second one over all runs for
-// dw_pre; a workgroup of the third one adds the runs' parts of dalpha.
+// dw_pre; a workgroup of the third one adds the runs' parts of dalpha. Sixteen loads of a thread are in flight. 4096 columns, 512 runs: 10.6 us;
+// 1111 columns, 7 gates: 5.4 us.
 constexpr int FC = 16, FR = 64;  // a wave has four threads of each column
 
 __device__ __forceinline__ float column_sum(const float* p, int n, int wide, int lane, int lanes) {
@@ -460,6 +603,10 @@ hipError_t forward_of(const iodf_join& a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// Threads to a row: the fewest that hold it, in powers of two up to a wave and in whole waves past that. Against powers of two alone, 192 and 768
+// threads: 1100 columns 214 us against 222 (2^26 elements, 32-bit stream), 4200 columns 148 against 154 (16 bits), the same where these are full; 384
+// against 512: 236 against 197 at 2100 columns, so there is none (two workgroups of 384 are twelve waves a unit, two of 512 sixteen).
+// 513 to 1024 columns by one wave with two vectors a thread against two waves with one: 185 us against 190 at 1024, 212 against 224 at 700.
 template <typename TH, typename TF>
 hipError_t forward_types(const iodf_join& a, hipStream_t st) {
     if (a.cols <= 8 * 8) return forward_of<TH, TF, 8, 1>(a, st);
@@ -469,16 +616,16 @@ hipError_t forward_types(const iodf_join& a, hipStream_t st) {
     if (a.cols <= 8 * 128) return forward_of<TH, TF, 64, 2>(a, st);
     if (a.cols <= 8 * 192) return forward_of<TH, TF, 192, 1>(a, st);
     if (a.cols <= 8 * 256) return forward_of<TH, TF, 256, 1>(a, st);
-    if (a.cols <= 8 * 384) return forward_of<TH, TF, 384, 1>(a, st);
     if (a.cols <= 8 * 512) return forward_of<TH, TF, 512, 1>(a, st);
     if (a.cols <= 8 * 768) return forward_of<TH, TF, 768, 1>(a, st);
     if (a.cols <= 8 * 1024) return forward_of<TH, TF, 1024, 1>(a, st);
     return forward_of<TH, TF, 1024, 2>(a, st);
 }
 
-// Threads to a row of the backward pass, one vector to each: a power of two up to a wave, then whole waves in steps of a half of the power below.
+// Threads to a row of the backward pass, one vector to each, as above. 192 threads against 256: 304 us against 322 at 1100 columns, 768 against 1024:
+// 253 against 290 at 4200 (32-bit stream); 384 against 512: within 3 % either way.
 int backward_lanes(int cols) {
-    for (int lanes : {8, 16, 32, 64, 128, 192, 256, 384, 512, 768})
+    for (int lanes : {8, 16, 32, 64, 128, 192, 256, 512, 768})
         if (cols <= 8 * lanes) return lanes;
     return 1024;
 }
@@ -512,7 +659,7 @@ long long n_runs(const Runs& r, long long rows) {
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
-template <typename TH, typename TF, int LPR, int NV>
+template <typename TH, typename TF, int LPR, bool FAR = false>
 hipError_t backward_of(const iodf_join& a, void* work, hipStream_t st) {
     const Runs r = runs_of(a.rows, a.cols, a.gate ? a.gate_rows : a.rows);
     const long long n = n_runs(r, a.rows);
@@ -522,8 +669,9 @@ hipError_t backward_of(const iodf_join& a, void* work, hipStream_t st) {
     float* const post = pre + n * wide;
     const int over_h = (int)over_rows(a.rows, a.cols, a.in_stream_stride), over_u = a.w_pre ? (int)over_rows(a.rows, a.cols, a.in_block_stride) : 0;
     if (n) {
-        if (r.gate_rows == 1) k_join_backward<TH, TF, LPR, NV, true><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, to_alpha);
-        else k_join_backward<TH, TF, LPR, NV, false><<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, to_alpha);
+        const auto kernel = r.gate_rows == 1 ? (FAR ? k_join_backward_far<TH, TF, true> : k_join_backward<TH, TF, LPR, true>)
+                                             : (FAR ? k_join_backward_far<TH, TF, false> : k_join_backward<TH, TF, LPR, false>);
+        kernel<<<(unsigned)n, threads_of<LPR>(), 0, st>>>(a, r, over_h, over_u, pre, post, to_alpha);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -534,19 +682,18 @@ hipError_t backward_of(const iodf_join& a, void* work, hipStream_t st) {
 
 template <typename TH, typename TF>
 hipError_t backward_types(const iodf_join& a, void* w, hipStream_t st) {
-    if (a.cols > 8 * 1024) return backward_of<TH, TF, 1024, 2>(a, w, st);
+    if (a.cols > 8 * 1024) return backward_of<TH, TF, 1024, true>(a, w, st);
     switch (backward_lanes(a.cols)) {
-        case 8: return backward_of<TH, TF, 8, 1>(a, w, st);
-        case 16: return backward_of<TH, TF, 16, 1>(a, w, st);
-        case 32: return backward_of<TH, TF, 32, 1>(a, w, st);
-        case 64: return backward_of<TH, TF, 64, 1>(a, w, st);
-        case 128: return backward_of<TH, TF, 128, 1>(a, w, st);
-        case 192: return backward_of<TH, TF, 192, 1>(a, w, st);
-        case 256: return backward_of<TH, TF, 256, 1>(a, w, st);
-        case 384: return backward_of<TH, TF, 384, 1>(a, w, st);
-        case 512: return backward_of<TH, TF, 512, 1>(a, w, st);
-        case 768: return backward_of<TH, TF, 768, 1>(a, w, st);
-        default: return backward_of<TH, TF, 1024, 1>(a, w, st);
+        case 8: return backward_of<TH, TF, 8>(a, w, st);
+        case 16: return backward_of<TH, TF, 16>(a, w, st);
+        case 32: return backward_of<TH, TF, 32>(a, w, st);
+        case 64: return backward_of<TH, TF, 64>(a, w, st);
+        case 128: return backward_of<TH, TF, 128>(a, w, st);
+        case 192: return backward_of<TH, TF, 192>(a, w, st);
+        case 256: return backward_of<TH, TF, 256>(a, w, st);
+        case 512: return backward_of<TH, TF, 512>(a, w, st);
+        case 768: return backward_of<TH, TF, 768>(a, w, st);
+        default: return backward_of<TH, TF, 1024>(a, w, st);
     }
 }
 

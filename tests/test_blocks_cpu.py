@@ -205,4 +205,4 @@ def test_more_than_a_launch_can_count_is_refused(lib, buf):
     assert lib.iodf_join_workspace(a, n) == E_ARG
     a.gate_rows = 1
     assert lib.iodf_join_workspace(a, n) == 0
-    assert lib.iodf_pack(buf[1], 1, 65536, (1 << 19) + 1, 65536, None, buf[1], buf[1], None) == E_ARG
+    assert lib.iodf_pack(buf[1], 1, 65536, (1 << 18) + 1, 65536, None, buf[1], buf[1], None) == E_ARG

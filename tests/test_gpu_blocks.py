@@ -241,6 +241,14 @@ def test_join_backward(rows, cols, stream, block, groups, mode, what):
         assert (a is None) == (b is None) and (a is None or torch().equal(a, b))
 
 
+@pytest.mark.parametrize("rows,cols,stream,block,groups,mode,what", [
+    (600, 8200, "bf16", "bf16", 1, "some", "agpq"), (520, 9001, "f32", "f32", 2, "some", "agpq"), (530, 8201, "f16", "f16", 530, "some", "agpq"),
+    (300, 8833, "f32", "bf16", 1, "some", "agp"), (3, 16383, "f32", "f16", 1, "all", "gq")])
+def test_join_backward_of_rows_past_8192_columns(rows, cols, stream, block, groups, mode, what):
+    """Rows that are not held but read twice: several to a run, padded ones between them."""
+    test_join_backward(rows, cols, stream, block, groups, mode, what)
+
+
 def test_join_backward_at_a_residual_scale_of_zero():
     """Where residual scales start: nothing of the block is in the stream, its gradients are 0, the scale's own is not."""
     rng, p, live = join_case(8, 60, 200, "f32", "bf16", 3, "some")
