@@ -254,13 +254,13 @@ constexpr int kLiveRows = 1 << 17;  // of a slice, whose padding is kept as bits
 // Sixteen bytes or one byte (as a word) a lane from memory to LDS, lane after lane from `lds` on. Written out because the compiler, where it
 // knows of such a load, waits for all of them before any LDS access that may meet one.
 __device__ __forceinline__ void start_lds16(uint32_t lds, const void* base, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void start_lds16(uint32_t lds, const void* p) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
 __device__ __forceinline__ void start_lds1(uint32_t lds, const void* base, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() {
@@ -464,32 +464,27 @@ __global__ __launch_bounds__(256) void k_wgrad_join(const iodf_wgrad a, int spli
     typedef float vec __attribute__((ext_vector_type(VEC)));
     __shared__ vec meet[JL][256 / JL];
     const int lane = threadIdx.x / (256 / JL), at = threadIdx.x % (256 / JL);
-    const long long n = (long long)a.out * a.cols, stride = gridDim.x * (256ll / JL) * VEC;
-    for (long long i0 = blockIdx.x * (256ll / JL) * VEC; i0 < n; i0 += stride) {
-        const long long i = i0 + at * VEC;
-        vec s = 0.f;
-        if (i < n) {
-            int k = lane;
-            for (; k + 7 * JL < splits; k += 8 * JL) {
-                vec v[8];
+    const long long n = (long long)a.out * a.cols, i = (((long long)blockIdx.y * gridDim.x + blockIdx.x) * (256 / JL) + at) * VEC;
+    vec s = 0.f;
+    if (i < n) {
+        int k = lane;
+        for (; k + 7 * JL < splits; k += 8 * JL) {
+            vec v[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = *(const vec*)(partial + (k + u * JL) * n + i);
-                s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-            }
-            for (; k < splits; k += JL) s += *(const vec*)(partial + k * n + i);
+            for (int u = 0; u < 8; ++u) v[u] = *(const vec*)(partial + (k + u * JL) * n + i);
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
-        meet[lane][at] = s;
-        __syncthreads();
-        if (lane == 0 && i < n) {
-#pragma unroll
-            for (int k = 1; k < JL; ++k) s += meet[k][at];
-            const int o = (int)(i / a.cols), c = (int)(i - (long long)o * a.cols);
-            float* const d = a.dw + o * a.dw_stride + c;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) d[j] = (a.accumulate ? d[j] : 0.f) + (a.col_scale ? a.col_scale[c + j] : 1.f) * s[j];
-        }
-        __syncthreads();
+        for (; k < splits; k += JL) s += *(const vec*)(partial + k * n + i);
     }
+    meet[lane][at] = s;
+    __syncthreads();
+    if (lane || i >= n) return;
+#pragma unroll
+    for (int k = 1; k < JL; ++k) s += meet[k][at];
+    const int o = (int)(i / a.cols), c = (int)(i - (long long)o * a.cols);
+    float* const d = a.dw + o * a.dw_stride + c;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) d[j] = (a.accumulate ? d[j] : 0.f) + (a.col_scale ? a.col_scale[c + j] : 1.f) * s[j];
 }
 
 struct Plan : Tiles {
@@ -570,9 +565,12 @@ hipError_t launch_weight_grad(const iodf_wgrad& a, void* work, hipStream_t st) {
                          : a.dy_type == IODF_T_BF16 ? run<__bf16>(a, p, partial, st)
                                                     : run<_Float16>(a, p, partial, st);
     if (e != hipSuccess || !partial) return e;
-    const long long n = (long long)a.out * a.cols, most = 1 << 20;
-    if (a.cols % 4 == 0) k_wgrad_join<4><<<(unsigned)std::min((n / 4 + 31) / 32, most), 256, 0, st>>>(a, p.splits, partial);
-    else k_wgrad_join<1><<<(unsigned)std::min((n + 31) / 32, most), 256, 0, st>>>(a, p.splits, partial);
+    // a grid of two dimensions: one holds less than 2^32 threads
+    const bool fours = a.cols % 4 == 0;
+    const long long n = ((long long)a.out * a.cols / (fours ? 4 : 1) + 31) / 32, x = std::min(n, 1ll << 20);
+    const dim3 grid((unsigned)x, (unsigned)((n + x - 1) / x));
+    if (fours) k_wgrad_join<4><<<grid, 256, 0, st>>>(a, p.splits, partial);
+    else k_wgrad_join<1><<<grid, 256, 0, st>>>(a, p.splits, partial);
     return hipGetLastError();
 }
 
