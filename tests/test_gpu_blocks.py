@@ -559,6 +559,44 @@ def test_refusals_on_the_gpu():
         assert e.value.code == -1
 
 
+@pytest.mark.parametrize("rows,cols,stream,block", [(37, 40, "f32", "bf16"), (20, 77, "bf16", "bf16"), (9, 1111, "f32", "f32"), (7, 600, "f16", "f16"),
+                                                   (5, 8205, "f32", "f16")])
+def test_join_and_glu_take_strided_rows_at_any_element(rows, cols, stream, block):
+    """The columns of wider tensors, from an odd element on and up to the last one: the same bits as from tensors of their own, and what lies
+    around an output stays."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(cols)
+
+    def apart(x, odd):
+        wide = t.full((rows, cols + odd + 3), 7.0, dtype=x.dtype, device="cuda")
+        part = wide.flatten()[odd + 3:].as_strided((rows, cols), (cols + odd + 3, 1), odd + 3)
+        part.copy_(x)
+        return wide, part
+
+    def normal(name):
+        return t.randn((rows, cols), generator=gen, device="cuda").to(dtype(name))
+
+    def same(got, want):
+        assert len(got) == len(want)
+        for a, b in zip(got, want):
+            assert t.equal(a, b)
+
+    h, f, dh, du = normal(stream), normal(block), normal(stream), normal(block)
+    par = [t.randn(n, generator=gen, device="cuda") for n in (1, cols, cols, cols)]
+    h2, u, saved = iodf.join(h, f, *par)
+    wide, out = apart(t.zeros_like(h), 8)
+    g2, v, kept = iodf.join(apart(h, 0)[1], apart(f, 2)[1], *par, h_out=out)
+    assert g2 is out and (wide[:, :11] == 7.0).all()
+    same((out, v, *kept.x[:2], *kept.n[:2], kept.inv_pre, kept.inv_post), (h2, u, *saved.x[:2], *saved.n[:2], saved.inv_pre, saved.inv_post))
+    same(iodf.join_backward(saved, apart(dh, 4)[1], apart(du, 6)[1], *par), iodf.join_backward(saved, dh, du, *par))
+    y, gated = iodf.glu(f, du)
+    z, kept = iodf.glu(apart(f, 2)[1], apart(du, 5)[1])
+    same((z, *kept.a[:2], *kept.b[:2]), (y, *gated.a[:2], *gated.b[:2]))
+    da, db, codes = iodf.glu_backward(gated, f)
+    ea, eb, others = iodf.glu_backward(gated, apart(f, 3)[1])
+    same((ea, eb, *others[:2]), (da, db, *codes[:2]))
+
+
 # ---- as they are used together ----
 
 def test_differentiable_calls():
