@@ -340,7 +340,8 @@ int iodf_glu_backward(const iodf_glu* args, void* stream);
  * Gradient of a linear layer's weight W [out][cols] from the checkpoint of its input:
  *   dw[o][c] = (accumulate ? dw[o][c] : 0) + col_scale[c] * sum_t dy[t][o] * X[t][c]
  * dy [rows][out] of dy_type, X what the checkpoint stands for, dw F32 with rows dw_stride apart. col_scale (may be NULL): the
- * weight of the norm between the checkpoint and the layer (w_pre of iodf_join). Products are exact for every dy_type,
+ * weight of the norm between the checkpoint and the layer (w_pre of iodf_join). In a padded row neither dy nor the checkpoint adds
+ * anything, whether the checkpoint was packed with `live` or without. Products are exact for every dy_type,
  * sums are 32-bit floats, in an order that depends on the sizes alone. 1 <= out <= 65536,
  * rows * (out rounded up to 32) <= 2^34.
  */

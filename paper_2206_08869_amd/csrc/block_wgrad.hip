@@ -19,6 +19,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int KT = 32;  // rows of a tile: two matrix instructions deep
+constexpr int kLiveRows = 1 << 17;  // of a slice, whose padding is kept as bits in LDS, a word for a tile
 
 template <typename T> constexpr int parts_of() { return sizeof(T) == 4 ? 3 : 1; }
 template <> constexpr int parts_of<_Float16>() { return 2; }
@@ -90,12 +91,15 @@ __device__ __forceinline__ void store_outputs(const f32x16 (&acc)[MT][NT], const
 // layers too small for tiles of 256, and for narrow ones, which are bound by memory. 100000 rows, 1000 x 37 weights: 40 us, 5.1 TB/s;
 // 4096 rows, 1024 x 1024: 30 us and 8 us for the slices' sums; 16384 rows, 4096 x 4096, dy in 32 bits: 1777 us, 930 TFLOP/s of the three
 // parts' products. Tiles of 64 rows instead of 32, half as many barriers: the same within 1 %, 8 % behind for the smallest.
-template <typename TY, int BM, int BN>
+// Padding (LIVE) is bits in LDS and costs 4 to 9 %: 40.5 us instead of 38.4 at 4096 rows, 1024 x 1024; a byte loaded beside each chunk of dy and of
+// codes cost up to 140 % (20000 rows, 1030 x 1100, 32 bits: 247 us against 566, 229 without padding).
+template <typename TY, int BM, int BN, bool LIVE>
 __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles tiles, float* partial) {
     constexpr int THREADS = 256, P = parts_of<TY>(), WM = BM / 2, WN = BN / 2, MT = WM / 32, NT = WN / 32;
     constexpr int AL = KT * BM / 8 / THREADS, BL = KT * BN / 8 / THREADS;  // chunks of eight of dy and of codes that a thread loads
     __shared__ __bf16 at[2][P][KT * BM];
     __shared__ __bf16 bt[2][KT * BN];
+    __shared__ uint32_t alive[LIVE ? kLiveRows / KT : 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int m0, n0, split;
     place(tiles, m0, n0, split);
@@ -103,6 +107,13 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
     const int pitch = (a.cols + 31) / 32 * 32, epitch = pitch / 32;
     const long long t0 = (long long)split * tiles.slice, t1 = min((long long)a.rows, t0 + tiles.slice);
     const int wm = wave / 2 * WM, wn = wave % 2 * WN;
+    if (LIVE) {  // bit r of word k: row t0 + 32 k + r is no padding
+        for (int k = wave * 64; k < (int)(t1 - t0); k += THREADS) {
+            const unsigned long long bits = __builtin_amdgcn_ballot_w64(t0 + k + lane < t1 && a.live[t0 + k + lane]);
+            if (lane < 2) alive[k / 32 + lane] = (uint32_t)(bits >> 32 * lane);
+        }
+        __syncthreads();
+    }
 
     int a_off[MT], b_off[NT];
     const int fr = (lane >> 5) * 8 + ((lane >> 2) & 3), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
@@ -112,8 +123,8 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
     for (int n = 0; n < NT; ++n) b_off[n] = chunk_at<BN>(fr, (wn + n * 32 + fc) / 8) * 8 + (fc & 7);
 
     // Chunks past the last column repeat the first, and one that sticks out of its row reads on: both only reach outputs that are not stored.
-    // Rows past the slice's end repeat its last one and are put as zeros. Only in the eight rows before dy's end, where reading on could leave
-    // it, is a chunk that sticks out taken element by element.
+    // Rows past the slice's end repeat its last one. Only in the eight rows before dy's end, where reading on could leave it, is a chunk that sticks
+    // out taken element by element.
     const int ar = tid / (BM / 8), ac = tid % (BM / 8) * 8, br = tid / (BN / 8), bc = tid % (BN / 8) * 8;
     const int acol = m0 + ac < a.out ? m0 + ac : 0, bcol = n0 + bc < pitch ? n0 + bc : 0;
     const TY* const dy = (const TY*)a.dy + ar * a.dy_stride + acol;
@@ -122,21 +133,13 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
     struct Stage {
         Raw8<TY> a[AL];
         RawCodes b[BL];
-        bool live[AL], there[BL];
     };
     auto fetch = [&](Stage& s, long long t, auto guarded) {
         if (!guarded) {
 #pragma unroll
-            for (int i = 0; i < AL; ++i) {
-                s.a[i] = fetch8(dy + t * a.dy_stride + i * a_step, 8, true);
-                s.live[i] = true;
-                if (a.live) s.live[i] = (a.live + t)[ar + i * (THREADS * 8 / BM)];
-            }
+            for (int i = 0; i < AL; ++i) s.a[i] = fetch8(dy + t * a.dy_stride + i * a_step, 8, true);
 #pragma unroll
-            for (int i = 0; i < BL; ++i) {
-                s.b[i] = {*(const u32x2*)(a.q + t * pitch + (b_off0 + i * b_step)), (a.e + t * epitch)[e_off0 + i * e_step]};
-                s.there[i] = true;
-            }
+            for (int i = 0; i < BL; ++i) s.b[i] = {*(const u32x2*)(a.q + t * pitch + (b_off0 + i * b_step)), (a.e + t * epitch)[e_off0 + i * e_step]};
         } else {
             const bool apart = t1 + 8 > a.rows && a.out % 8 != 0;
 #pragma unroll
@@ -144,30 +147,37 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
                 const long long row = t + ar + i * (THREADS * 8 / BM), at = row < t1 ? row : t1 - 1;
                 const TY* const p = (const TY*)a.dy + at * a.dy_stride + acol;
                 s.a[i] = apart ? fetch8(p, a.out - acol, false) : fetch8(p, 8, true);
-                s.live[i] = row < t1;
-                if (a.live) s.live[i] = row < t1 && a.live[at];
             }
 #pragma unroll
             for (int i = 0; i < BL; ++i) {
                 const long long row = t + br + i * (THREADS * 8 / BN), at = row < t1 ? row : t1 - 1;
                 s.b[i] = {*(const u32x2*)(a.q + at * pitch + bcol), a.e[at * epitch + bcol / 32]};
-                s.there[i] = row < t1;
             }
         }
     };
-    auto put = [&](const Stage& s, int buf) {
+    // bit r: row r of the tile at t adds something; asked for with rows of the slice in it only
+    auto rows_of = [&](long long t, auto guarded) {
+        uint32_t rows = LIVE ? alive[(int)(t - t0) / KT] : ~0u;
+        if (guarded && t1 - t < KT) rows &= (1u << (int)(t1 - t)) - 1;
+        return rows;
+    };
+    // What adds nothing goes in as zeros of dy and as codes of an exponent with which they are finite (they may stand for NaN, which would outlast
+    // the zeros).
+    auto put = [&](const Stage& s, int buf, uint32_t rows, auto guarded) {
+        const bool some = LIVE || guarded;
 #pragma unroll
         for (int i = 0; i < AL; ++i) {
-            const int to = chunk_at<BM>(ar + i * (THREADS * 8 / BM), ac / 8) * 8;
+            const int r = ar + i * (THREADS * 8 / BM), to = chunk_at<BM>(r, ac / 8) * 8;
+            const bool there = !some || rows >> r & 1;
             if (P == 1) {
                 bf8 w;
                 __builtin_memcpy(&w, s.a[i].w, 16);
-                *(bf8*)&at[buf][0][to] = s.live[i] ? w : bf8{};
+                *(bf8*)&at[buf][0][to] = there ? w : bf8{};
             } else {
                 float rest[8];
                 widen8(s.a[i], rest);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) rest[j] = s.live[i] ? rest[j] : 0.f;
+                for (int j = 0; j < 8; ++j) rest[j] = there ? rest[j] : 0.f;
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     const bf8 w = narrow8(rest);
@@ -182,9 +192,10 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
         }
 #pragma unroll
         for (int i = 0; i < BL; ++i) {
+            const int r = br + i * (THREADS * 8 / BN);
             float v[8];
-            decode8(s.there[i] ? s.b[i].q : u32x2{0, 0}, code_step(s.there[i] ? s.b[i].e : 16), v);
-            *(bf8*)&bt[buf][chunk_at<BN>(br + i * (THREADS * 8 / BN), bc / 8) * 8] = narrow8(v);
+            decode8(s.b[i].q, code_step(!some || rows >> r & 1 ? s.b[i].e : 16), v);
+            *(bf8*)&bt[buf][chunk_at<BN>(r, bc / 8) * 8] = narrow8(v);
         }
     };
 
@@ -202,7 +213,7 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
     if (t0 < t1) {
         fetch(st[0], t0, checked);
         fetch(st[1], t0 + KT, checked);
-        put(st[0], 0);
+        put(st[0], 0, rows_of(t0, checked), checked);
         fetch(st[0], t0 + 2 * KT, checked);
     }
     __syncthreads();
@@ -210,6 +221,8 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if (guarded && h && t + KT >= t1) break;
+            const bool more = !guarded || t + (h + 1) * KT < t1;
+            const uint32_t rows = more ? rows_of(t + (h + 1) * KT, guarded) : 0;
 #pragma unroll
             for (int s = 0; s < KT / 16; ++s) {
                 bf8 bf[NT];
@@ -224,7 +237,8 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
                         for (int n = 0; n < NT; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af, bf[n], acc[m][n], 0, 0, 0);
                     }
             }
-            if (!guarded || t + (h + 1) * KT < t1) put(st[h ^ 1], h ^ 1);
+            if (more) put(st[h ^ 1], h ^ 1, rows, guarded);
+            __builtin_amdgcn_sched_barrier(0);  // one region a tile: over two the compiler reads each operand just before its product
             if (!guarded || t + (h + 3) * KT < t1) fetch(st[h ^ 1], t + (h + 3) * KT, guarded);
             __syncthreads();
         }
@@ -253,7 +267,6 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
 // Loads carry no bounds checks except near a slice's end: a chunk of dy that sticks out of its row reads the next one's start, and
 // chunks past the last column repeat the first; both only reach outputs that are not stored.
 constexpr int WIDE = 256, RING = 4;
-constexpr int kLiveRows = 1 << 17;  // of a slice, whose padding is kept as bits in LDS
 
 // Sixteen bytes or one byte (as a word) a lane from memory to LDS, lane after lane from `lds` on. Written out because the compiler, where it
 // knows of such a load, waits for all of them before any LDS access that may meet one.
@@ -281,7 +294,7 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
     __shared__ __bf16 bt[2][KT * WIDE];
     __shared__ u32x4 raw[RING][512];
     __shared__ uint32_t raw_e[RING][512];
-    __shared__ uint32_t alive[LIVE ? kLiveRows / 32 : 1];
+    __shared__ uint32_t alive[LIVE ? kLiveRows / 32 + RING + 2 : 1];  // and of the tiles past the slice that its loop takes too
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int m0, n0, split;
     place(tiles, m0, n0, split);
@@ -300,8 +313,8 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
     auto lds_of = [](const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; };
     const uint32_t at0 = lds_of(&at[0][0]) + wave * 1024, raw0 = lds_of(&raw[0][0]) + wave * 1024, rawe0 = lds_of(&raw_e[0][0]) + wave * 256;
 
-    if (LIVE) {  // bit r of word k: row t0 + 32 k + r is no padding
-        const int words = (int)((t1 - t0 + 31) / 32);
+    if (LIVE) {  // bit r of word k: row t0 + 32 k + r is there and no padding
+        const int words = (int)((t1 - t0 + 31) / 32) + RING + 2;
         for (int k = tid; k < words; k += THREADS) {
             uint32_t w = 0;
             for (int r = 0; r < 32; ++r) {
@@ -350,12 +363,14 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
             raw_e[to][tid] = t + er < t1 ? eb[e_voff] : 16;
         }
     };
-    // a thread widens eight of its sixteen codes in either phase
+    // A thread widens eight of its sixteen codes in either phase. Those of a padded row may stand for NaN, which would outlast the zeros that its
+    // dy is: with another exponent they are finite.
     u32x2 codes[2];
     uint32_t ex[2];
-    auto take_codes = [&](int half, int from) {
+    auto take_codes = [&](int half, int from, long long t) {
         codes[half] = ((const u32x2*)&raw[from][tid])[half];
         ex[half] = raw_e[from][wave * 64 + (br & 3) * 8 + bc / 2];
+        if (LIVE) ex[half] = alive[(int)(t - t0) / 32] >> br & 1 ? ex[half] : 16;
     };
     auto widen = [&](int half, int to) {
         float v[8];
@@ -406,9 +421,9 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
             start_dy(k, t0 + k * KT, guarded);
         }
         wait_loads<guarded ? 0 : 2 + LOADS>();  // codes of tiles 0, 1 and 2 (whose first half phase A of tile 0 takes) and dy of tile 0 have landed
-        take_codes(0, 0), take_codes(1, 0);
+        take_codes(0, 0, t0), take_codes(1, 0, t0);
         widen(0, 0), widen(1, 0);
-        take_codes(0, 1), take_codes(1, 1);
+        take_codes(0, 1, t0 + KT), take_codes(1, 1, t0 + KT);
         widen(0, 1);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         start_codes(0, t0 + 4 * KT, guarded);
@@ -434,7 +449,7 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
         for (int h = 0; h < RING; ++h, t += KT) {
             const int now = h & 1, next = now ^ 1;
             read(1, h, now, 1);
-            take_codes(0, (h + 2) % RING);
+            take_codes(0, (h + 2) % RING, t + 2 * KT);
             widen(1, next);
             multiply(0, 0);
             deal(std::true_type());
@@ -445,7 +460,7 @@ __global__ __launch_bounds__(512, 1) void k_wgrad_wide(const iodf_wgrad a, const
             __builtin_amdgcn_sched_barrier(0);
             start_codes((h + 1) % RING, t + 5 * KT, guarded);
             read(0, (h + 1) % RING, next, 0);
-            take_codes(1, (h + 2) % RING);
+            take_codes(1, (h + 2) % RING, t + 2 * KT);
             widen(0, now);
             multiply(1, 0);
             deal(std::true_type());
@@ -540,18 +555,23 @@ Plan plan_of(const iodf_wgrad& a) {
     return best;
 }
 
+template <typename TY, bool LIVE>
+void run_tile(const iodf_wgrad& a, const Plan& p, float* partial, hipStream_t st) {
+    const unsigned blocks = (unsigned)(p.m * p.n * p.splits);
+    if (p.bm == 128 && p.bn == 128) k_wgrad<TY, 128, 128, LIVE><<<blocks, 256, 0, st>>>(a, p, partial);
+    else if (p.bm == 128) k_wgrad<TY, 128, 64, LIVE><<<blocks, 256, 0, st>>>(a, p, partial);
+    else if (p.bn == 128) k_wgrad<TY, 64, 128, LIVE><<<blocks, 256, 0, st>>>(a, p, partial);
+    else k_wgrad<TY, 64, 64, LIVE><<<blocks, 256, 0, st>>>(a, p, partial);
+}
+
 template <typename TY>
 hipError_t run(const iodf_wgrad& a, const Plan& p, float* partial, hipStream_t st) {
     const unsigned blocks = (unsigned)(p.m * p.n * p.splits);
     if (p.bm == WIDE) {
         if (a.live) k_wgrad_wide<true><<<blocks, 512, 0, st>>>(a, p, partial);
         else k_wgrad_wide<false><<<blocks, 512, 0, st>>>(a, p, partial);
-    } else if (p.bm == 128) {
-        if (p.bn == 128) k_wgrad<TY, 128, 128><<<blocks, 256, 0, st>>>(a, p, partial);
-        else k_wgrad<TY, 128, 64><<<blocks, 256, 0, st>>>(a, p, partial);
     } else {
-        if (p.bn == 128) k_wgrad<TY, 64, 128><<<blocks, 256, 0, st>>>(a, p, partial);
-        else k_wgrad<TY, 64, 64><<<blocks, 256, 0, st>>>(a, p, partial);
+        a.live ? run_tile<TY, true>(a, p, partial, st) : run_tile<TY, false>(a, p, partial, st);
     }
     return hipGetLastError();
 }
