@@ -277,7 +277,7 @@ int iodf_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int cols, void*
  * iodf_join_backward: in_stream = dL/dh', in_block = dL/du and the checkpoint -> out_stream = dL/dh, out_block = dL/df
  *   (rounded to those types; may not overlap anything) and the sums dalpha [1], dgate [gate rows][cols], dw_post [cols],
  *   dw_pre [cols] (each NULL exactly where its parameter is). x and n stand for what the checkpoint holds. At most 2^21 gate rows,
- *   or one for each row. The result is the same bits on every call.
+ *   or one for each row; with no rows dgate is one row. The result is the same bits on every call.
  */
 typedef struct iodf_join {
     int64_t rows, gate_rows;

@@ -256,7 +256,8 @@ def join_backward(saved, dh, du, alpha=None, gate=None, w_post=None, w_pre=None,
         _refuse("saved lacks a norm's factors")
     dh_out = _rows_like(dh, sh)
     df = t.empty(rows, cols, dtype=block_dtype, device=device) if du is None else _rows_like(du, sf)
-    grads = [None if p is None else t.empty_like(p) for p in (alpha, gate, w_post, w_pre)]
+    fresh = t.empty_like if rows else t.zeros_like  # of no rows the kernels fill one gate's gradient, however many gates there are
+    grads = [None if p is None else fresh(p) for p in (alpha, gate, w_post, w_pre)]
     block = _JOIN.pack(rows, gate_rows, cols, th, tf, 1.0, ap, gp, wop, wip, lp, dh.data_ptr(), du.data_ptr() if du is not None else 0,
                        dh_out.data_ptr(), df.data_ptr(), sh, sf, cols, cols, xq, xe, nq, ne, ipre, ipost,
                        *[0 if g is None else g.data_ptr() for g in grads])

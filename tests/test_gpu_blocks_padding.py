@@ -54,3 +54,18 @@ def test_projection_leaves_padded_rows_out_of_its_weight_s_gradient():
     x[~live, 40:] = float("inf")
     got, = t.autograd.grad(iodf.projection(x, w, iodf.pack(x), live=live), w, dy)
     assert np.isfinite(want.cpu().numpy()).all() and t.equal(got, want)
+
+
+@pytest.mark.parametrize("groups", [1, 3, 200])
+@pytest.mark.parametrize("cols", [5, 72, 9000])
+def test_join_backward_of_no_rows_gives_zeros(groups, cols):
+    """For every gate there is, in memory that held other numbers just before."""
+    t = torch()
+    h = t.empty((0, cols), device="cuda")
+    par = [t.ones(s, device="cuda") for s in ((1,), (groups, cols), (cols,), (cols,))]
+    _, u, saved = iodf.join(h, h, *par)
+    junk = [t.full((groups, cols), float("nan"), device="cuda") for _ in range(8)]
+    del junk
+    g = iodf.join_backward(saved, h, u, *par)
+    for got, p in zip(g[2:], par):
+        assert t.equal(got, t.zeros_like(p))
