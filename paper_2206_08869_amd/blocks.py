@@ -357,36 +357,45 @@ def _make_functions():
 
     once = t.autograd.function.once_differentiable
 
+    # Checkpoints and the mask are kept as saved tensors, which the backward pass lets go and in which a change in place is an error.
+
     class Joined(t.autograd.Function):
         @staticmethod
         def forward(ctx, h, f, alpha, gate, w_post, w_pre, live, eps, hold):
             h2, u, saved = join(h, f, alpha, gate, w_post, w_pre, live=live, eps=eps, save=True)
-            ctx.save_for_backward(alpha, gate, w_post, w_pre)
-            ctx.saved, ctx.live, ctx.block = saved, live, f.dtype
+            x, n, inv_pre, inv_post = saved
+            ctx.save_for_backward(alpha, gate, w_post, w_pre, live, *(x[:2] if x else (None, None)), *n[:2], inv_pre, inv_post)
+            ctx.block = f.dtype
             hold.append(saved)
             return (h2, u) if u is not None else h2
 
         @staticmethod
         @once
         def backward(ctx, dh, du=None):
-            g = join_backward(ctx.saved, rows_first(dh), None if du is None else rows_first(du), *ctx.saved_tensors, live=ctx.live,
-                              block_dtype=ctx.block)
+            *params, live, xq, xe, nq, ne, inv_pre, inv_post = ctx.saved_tensors
+            cols = dh.shape[1]
+            saved = JoinSaved(None if xq is None else Codes(xq, xe, cols), Codes(nq, ne, cols), inv_pre, inv_post)
+            g = join_backward(saved, rows_first(dh), None if du is None else rows_first(du), *params, live=live, block_dtype=ctx.block)
             return (*g, None, None, None)
 
     class Projection(t.autograd.Function):
         @staticmethod
         def forward(ctx, u, weight, codes, col_scale, live):
             w = weight.to(u.dtype)
-            ctx.save_for_backward(w, col_scale)
-            ctx.codes, ctx.live, ctx.dtype = codes, live, weight.dtype
+            if not isinstance(codes, Codes):
+                if ctx.needs_input_grad[1]:
+                    _refuse("codes has to be Codes")
+                codes = Codes(None, None, u.shape[-1])
+            ctx.save_for_backward(w, col_scale, live, *codes[:2])
+            ctx.cols, ctx.dtype = codes.cols, weight.dtype
             return u @ w.t()
 
         @staticmethod
         @once
         def backward(ctx, dy):
-            w, col_scale = ctx.saved_tensors
+            w, col_scale, live, q, e = ctx.saved_tensors
             dy = rows_first(dy)
-            dw = weight_grad(ctx.codes, dy, col_scale=col_scale, live=ctx.live).to(ctx.dtype)
+            dw = weight_grad(Codes(q, e, ctx.cols), dy, col_scale=col_scale, live=live).to(ctx.dtype)
             return dy @ w, dw, None, None, None
 
     class GatedProjection(t.autograd.Function):
@@ -395,17 +404,18 @@ def _make_functions():
             cols = ab.shape[1] // 2
             y, saved = glu(ab[:, :cols], ab[:, cols:], act, live=live)
             w = weight.to(y.dtype)
-            ctx.save_for_backward(w)
-            ctx.saved, ctx.act, ctx.live, ctx.dtype = saved, act, live, weight.dtype
+            ctx.save_for_backward(w, live, *saved.a[:2], *saved.b[:2])
+            ctx.cols, ctx.act, ctx.dtype = cols, act, weight.dtype
             return y @ w.t()
 
         @staticmethod
         @once
         def backward(ctx, do):
-            w, = ctx.saved_tensors
+            w, live, aq, ae, bq, be = ctx.saved_tensors
             do = rows_first(do)
-            dab, y = _glu_backward(ctx.saved, do @ w, ctx.act, ctx.live, True)
-            return dab, weight_grad(y, do, live=ctx.live).to(ctx.dtype), None, None
+            saved = GluSaved(Codes(aq, ae, ctx.cols), Codes(bq, be, ctx.cols))
+            dab, y = _glu_backward(saved, do @ w, ctx.act, live, True)
+            return dab, weight_grad(y, do, live=live).to(ctx.dtype), None, None
 
     _functions = (Joined, Projection, GatedProjection)
     return _functions

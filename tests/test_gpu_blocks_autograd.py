@@ -1,0 +1,130 @@
+"""The differentiable calls as autograd sees them: what they keep, how long, what they notice, and with padded rows."""
+import pytest
+
+import paper_2206_08869_amd as iodf
+
+pytestmark = pytest.mark.gpu
+
+
+def torch():
+    import torch as t
+    return t
+
+
+class Block:
+    """A stream of `rows` rows through two joins with a gated block between them, as an example of all three calls."""
+
+    def __init__(self, rows=512, cols=96, hid=160, live=None):
+        t = torch()
+        gen = t.Generator("cuda").manual_seed(rows)
+
+        def leaf(*shape, by=1.0, plus=0.0):
+            return (by * t.randn(shape, generator=gen, device="cuda") + plus).requires_grad_()
+
+        self.h, self.f = leaf(rows, cols), leaf(rows, cols)
+        self.w1, self.w2 = leaf(2 * hid, cols, by=0.1), leaf(cols, hid, by=0.1)
+        self.joins = [[leaf(1, plus=0.5, by=0.0), leaf(cols, by=0.1, plus=0.7), leaf(cols, by=0.1, plus=1.0), leaf(cols, by=0.1, plus=1.0)]
+                      for _ in range(2)]
+        self.dy = t.randn((rows, cols), generator=gen, device="cuda")
+        self.live, self.rows = live, None if live is None else live.clone()  # the loss has a mask of its own
+
+    def leaves(self):
+        return [self.h, self.f, self.w1, self.w2, *self.joins[0], *self.joins[1]]
+
+    def loss(self, seen=None):
+        first, second = self.joins
+        h, u, codes = iodf.joined(self.h, self.f, *first, live=self.live)
+        ab = iodf.projection(u, self.w1, codes, col_scale=first[3].detach(), live=self.live)
+        f = iodf.gated_projection(ab, self.w2, live=self.live)
+        h, u, last = iodf.joined(h, f, *second, live=self.live)
+        if seen is not None:
+            seen += [codes, last]
+        out = (h + u) * self.dy
+        return (out if self.rows is None else out[self.rows]).sum()
+
+
+def test_the_backward_pass_lets_checkpoints_go():
+    """While the loss, and with it the graph, is still held, as in a training loop until the next step's loss takes its place."""
+    t = torch()
+    rows, cols, hid = 8192, 512, 1024
+    block = Block(rows, cols, hid)
+    t.autograd.grad(block.loss(), block.leaves())  # what the libraries allocate once
+    t.cuda.synchronize()
+    before = t.cuda.memory_allocated()
+    loss = block.loss()
+    kept = t.cuda.memory_allocated() - before
+    codes = rows * (4 * cols + 2 * hid) * 33 // 32  # of two joins and of a gated activation
+    assert kept >= codes
+    loss.backward()
+    for x in block.leaves():
+        x.grad = None
+    t.cuda.synchronize()
+    assert t.cuda.memory_allocated() - before < codes // 16 and loss.requires_grad
+
+
+def test_saved_tensor_hooks_see_the_checkpoints():
+    """Offloading and the like work on saved tensors: every checkpoint passes through them, and what they give back is used."""
+    t = torch()
+    block = Block()
+    want = t.autograd.grad(block.loss(), block.leaves())
+    packed = []
+
+    def pack(x):
+        packed.append(x.dtype)
+        return x.cpu()
+
+    with t.autograd.graph.saved_tensors_hooks(pack, lambda x: x.cuda()):
+        loss = block.loss()
+    got = t.autograd.grad(loss, block.leaves())
+    assert packed.count(t.int8) == 7  # x and n of two joins, x for the projection, a and b
+    for a, b in zip(got, want):
+        assert t.equal(a, b)
+
+
+@pytest.mark.parametrize("what", ["live", "codes.q", "codes.e"])
+def test_what_is_changed_in_place_between_the_passes_is_an_error(what):
+    t = torch()
+    live = t.rand(512, device="cuda") < 0.8
+    block, seen = Block(live=live), []
+    loss = block.loss(seen)
+    if what == "live":
+        live.fill_(True)
+    else:
+        getattr(seen[0], what[-1]).add_(1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+
+
+def test_a_projection_whose_weight_learns_wants_codes():
+    t = torch()
+    u, w = t.randn((4, 32), device="cuda"), t.randn((8, 32), device="cuda").requires_grad_()
+    with pytest.raises(ValueError):
+        iodf.projection(u, w, None)
+    assert t.equal(iodf.projection(u, w.detach(), None), u @ w.detach().t())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_padded_rows_through_the_differentiable_calls(dtype):
+    """Gradients of a batch with padded rows are those of the batch without them, whatever stands in the padded rows; as near as sums over
+    other rows in another order and other kernels of the projections' library come to each other."""
+    t = torch()
+    rows = 640
+    live = t.rand(rows, generator=t.Generator("cuda").manual_seed(1), device="cuda") < 0.7
+    block = Block(rows, live=live)
+    whole = Block(rows)
+    for x in (block, whole):
+        x.h, x.f = (v.detach().to(getattr(t, dtype)) for v in (x.h, x.f))
+    whole.h, whole.f, whole.dy = whole.h[live], whole.f[live], whole.dy[live]
+    block.f[~live] = float("nan")
+    block.h[~live] = float("inf")
+    for x in (block, whole):
+        x.h.requires_grad_(), x.f.requires_grad_()
+    got = t.autograd.grad(block.loss(), block.leaves())
+    want = t.autograd.grad(whole.loss(), whole.leaves())
+    for k, (g, w) in enumerate(zip(got, want)):
+        if k < 2:
+            assert not g[~live].any()
+            g = g[live]
+        assert t.isfinite(g).all()
+        # activations in 32 bits: a code on a border may fall to either side; in 16: other products' roundings besides
+        assert (g - w).float().norm() <= (0.02 if dtype == "bfloat16" else 0.01) * w.float().norm()
