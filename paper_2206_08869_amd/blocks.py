@@ -219,7 +219,8 @@ def join(h, f, alpha=None, gate=None, w_post=None, w_pre=None, live=None, eps=1e
     device = h.device
     tf, sf = _matrix(f, "f", shape, None, device)
     gate_rows, ap, gp, wop, wip, lp = _join_params(rows, cols, device, alpha, gate, w_post, w_pre, live)
-    if h_out is None:
+    given = h_out is not None
+    if not given:
         h_out, so = _rows_like(h, sh), cols
     else:
         _, so = _matrix(h_out, "h_out", shape, h.dtype, device)
@@ -234,6 +235,8 @@ def join(h, f, alpha=None, gate=None, w_post=None, w_pre=None, live=None, eps=1e
              inv_post.data_ptr() if w_post is not None else 0)
     _call("join_forward", device, _JOIN.pack(rows, gate_rows, cols, th, tf, eps, ap, gp, wop, wip, lp, h.data_ptr(), f.data_ptr(), h_out.data_ptr(),
                                              u.data_ptr() if u is not None else 0, sh, sf, so, cols, *c, 0, 0, 0, 0))
+    if given:
+        t.autograd.graph.increment_version(h_out)
     return h_out, u, saved
 
 
@@ -328,7 +331,8 @@ def weight_grad(codes, dy, col_scale=None, live=None, out=None, accumulate=False
     cols = codes.cols
     qp, ep = _codes(codes, "codes", rows, cols, device)
     sp, lp = _vector(col_scale, "col_scale", cols, device), _live(live, rows, device)
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             _refuse("accumulate adds to out: pass it")
         out, so = t.empty(n_out, cols, dtype=_f32, device=device), cols
@@ -337,6 +341,8 @@ def weight_grad(codes, dy, col_scale=None, live=None, out=None, accumulate=False
     block = _WGRAD.pack(rows, cols, n_out, kind, 1 if accumulate else 0, dy.data_ptr(), sd, qp, ep, sp, lp, out.data_ptr(), so)
     work, need = _workspace("weight_grad_workspace", block, device)
     _call("weight_grad", device, block, work.data_ptr() if need else 0, need)
+    if given:
+        t.autograd.graph.increment_version(out)
     return out
 
 

@@ -128,3 +128,19 @@ def test_padded_rows_through_the_differentiable_calls(dtype):
         assert t.isfinite(g).all()
         # activations in 32 bits: a code on a border may fall to either side; in 16: other products' roundings besides
         assert (g - w).float().norm() <= (0.02 if dtype == "bfloat16" else 0.01) * w.float().norm()
+
+
+def test_outputs_that_are_given_are_known_to_have_changed():
+    """A tensor that autograd keeps for another operation, overwritten as h_out or out, is an error in that one's backward pass."""
+    t = torch()
+    h, f, w = (t.randn(s, device="cuda") for s in ((8, 32), (8, 32), (24, 32)))
+    other, codes, dy = t.randn((8, 32), device="cuda").requires_grad_(), iodf.pack(f), t.randn((8, 24), device="cuda")
+    for overwrite, kept in ((lambda: iodf.join(h, f, save=False, h_out=h), h), (lambda: iodf.join(f, f, h_out=h[:, :]), h),
+                            (lambda: iodf.weight_grad(codes, dy, out=w, accumulate=True), w)):
+        loss = (other * kept[:8]).sum()
+        overwrite()
+        with pytest.raises(RuntimeError, match="inplace"):
+            loss.backward()
+    with t.inference_mode():
+        x = t.ones((3, 32), device="cuda")
+        assert iodf.join(x, x, save=False, h_out=x)[0] is x and (x == 2).all()
