@@ -3,7 +3,8 @@ activation, and the gradients of both and of linear layers out of 8-bit activati
 
 Tensors are [rows, cols] on one GPU with consecutive columns (any row stride); work goes to the current stream of their device, whose
 allocator supplies outputs and scratch. Parameters (alpha, gate, norm weights) are float32. `live` (bool or uint8 [rows]) marks rows that
-are not padding. `joined`, `projection` and `gated_projection` are the same operators as differentiable calls.
+are not padding. `joined`, `projection` and `gated_projection` are the same operators as differentiable calls; the others record no graph, and
+refuse activations and gradients for which autograd would have to record one.
 """
 import ctypes
 import struct
@@ -96,10 +97,12 @@ def _refuse(what):
     raise ValueError("iodf: " + what)
 
 
-def _matrix(x, name, shape=None, dtype=None, device=None):
-    """Element type and row stride of a [rows, cols] tensor that the kernels take."""
+def _matrix(x, name, shape=None, dtype=None, device=None, recorded=True):
+    """Element type and row stride of a [rows, cols] tensor that the kernels take. `recorded`: autograd would record what is made of it."""
     if not isinstance(x, _Tensor) or x.dim() != 2 or x.dtype not in _types or not x.is_cuda:
         _refuse("%s has to be a float32, bfloat16 or float16 [rows, cols] tensor on the GPU" % name)
+    if x.requires_grad and recorded and _torch.is_grad_enabled():
+        _refuse("%s requires a gradient, and this call records no graph: take joined, projection or gated_projection, or torch.no_grad()" % name)
     r, c = x.shape
     if shape is not None and (r, c) != shape:
         _refuse("%s is %s, not %s" % (name, [r, c], list(shape)))
@@ -168,7 +171,7 @@ def _rows_like(x, stride):
 def pack(x, live=None):
     """x -> Codes."""
     _torch or _setup()
-    kind, stride = _matrix(x, "x")
+    kind, stride = _matrix(x, "x", recorded=False)  # whole numbers have no gradient
     rows, cols = x.shape
     device = x.device
     lp = _live(live, rows, device)

@@ -144,3 +144,23 @@ def test_outputs_that_are_given_are_known_to_have_changed():
     with t.inference_mode():
         x = t.ones((3, 32), device="cuda")
         assert iodf.join(x, x, save=False, h_out=x)[0] is x and (x == 2).all()
+
+
+def test_calls_that_record_no_graph_refuse_what_would_need_one():
+    """Activations and gradients that require a gradient, while autograd records. Parameters may require one; whole numbers have none."""
+    t = torch()
+    x, g = t.randn((8, 32), device="cuda"), t.randn((8, 32), device="cuda").requires_grad_()
+    w = t.ones(32, device="cuda").requires_grad_()
+    codes = iodf.pack(x)
+    _, _, saved = iodf.join(x, x, w_pre=w)
+    _, gated = iodf.glu(x, x)
+    calls = (lambda: iodf.join(g, x), lambda: iodf.join(x, g), lambda: iodf.join(x, x, h_out=g), lambda: iodf.join_backward(saved, g, x, w_pre=w),
+             lambda: iodf.join_backward(saved, x, g, w_pre=w), lambda: iodf.glu(g, x), lambda: iodf.glu(x, g),
+             lambda: iodf.glu_backward(gated, g), lambda: iodf.weight_grad(codes, g), lambda: iodf.weight_grad(codes, x, out=t.zeros_like(g).expand(
+                 8, 32).repeat(4, 1).requires_grad_()))
+    for call in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+        with t.no_grad():
+            call()
+    iodf.join_backward(saved, x, x, w_pre=w), iodf.weight_grad(codes, x, col_scale=w), iodf.pack(g)
