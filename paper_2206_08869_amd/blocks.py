@@ -391,30 +391,30 @@ def _make_functions():
         @staticmethod
         def forward(ctx, u, weight, codes, col_scale, live):
             w = weight.to(u.dtype)
-            if not isinstance(codes, Codes):
-                if ctx.needs_input_grad[1]:
-                    _refuse("codes has to be Codes")
-                codes = Codes(None, None, u.shape[-1])
-            ctx.save_for_backward(w, col_scale, live, *codes[:2])
-            ctx.cols, ctx.dtype = codes.cols, weight.dtype
+            learns = ctx.needs_input_grad[1]
+            if learns and not isinstance(codes, Codes):
+                _refuse("codes has to be Codes")
+            ctx.save_for_backward(w, col_scale, live, *(codes[:2] if learns else (None, None)))
+            ctx.cols, ctx.dtype = codes.cols if learns else 0, weight.dtype
             return u @ w.t()
 
         @staticmethod
         @once
         def backward(ctx, dy):
             w, col_scale, live, q, e = ctx.saved_tensors
-            dy = rows_first(dy)
-            dw = weight_grad(Codes(q, e, ctx.cols), dy, col_scale=col_scale, live=live).to(ctx.dtype)
-            return dy @ w, dw, None, None, None
+            dy, to_u, to_weight = rows_first(dy), *ctx.needs_input_grad[:2]
+            dw = weight_grad(Codes(q, e, ctx.cols), dy, col_scale=col_scale, live=live).to(ctx.dtype) if to_weight else None
+            return dy @ w if to_u else None, dw, None, None, None
 
     class GatedProjection(t.autograd.Function):
         @staticmethod
-        def forward(ctx, ab, weight, act, live):
+        def forward(ctx, ab, weight, act, live, recorded):
             cols = ab.shape[1] // 2
-            y, saved = glu(ab[:, :cols], ab[:, cols:], act, live=live)
+            y, saved = glu(ab[:, :cols], ab[:, cols:], act, live=live, save=recorded)
             w = weight.to(y.dtype)
-            ctx.save_for_backward(w, live, *saved.a[:2], *saved.b[:2])
-            ctx.cols, ctx.act, ctx.dtype = cols, act, weight.dtype
+            if recorded:
+                ctx.save_for_backward(w, live, *saved.a[:2], *saved.b[:2])
+                ctx.cols, ctx.act, ctx.dtype = cols, act, weight.dtype
             return y @ w.t()
 
         @staticmethod
@@ -423,15 +423,17 @@ def _make_functions():
             w, live, aq, ae, bq, be = ctx.saved_tensors
             do = rows_first(do)
             saved = GluSaved(Codes(aq, ae, ctx.cols), Codes(bq, be, ctx.cols))
-            dab, y = _glu_backward(saved, do @ w, ctx.act, live, True)
-            return dab, weight_grad(y, do, live=live).to(ctx.dtype), None, None
+            to_weight = ctx.needs_input_grad[1]
+            dab, y = _glu_backward(saved, do @ w, ctx.act, live, to_weight)
+            return dab, weight_grad(y, do, live=live).to(ctx.dtype) if to_weight else None, None, None, None
 
     _functions = (Joined, Projection, GatedProjection)
     return _functions
 
 
 def joined(h, f, alpha=None, gate=None, w_post=None, w_pre=None, live=None, eps=1e-6):
-    """join() as a differentiable call -> (h', u, Codes of x): the codes and w_pre go to the projection that reads u."""
+    """join() as a differentiable call -> (h', u, Codes of x): the codes and w_pre go to the projection that reads u. They are an answer of this
+    call and made in every case: join(save=False) is the form that keeps nothing."""
     hold = []
     out = _make_functions()[0].apply(h, f, alpha, gate, w_post, w_pre, live, eps, hold)
     return (*out, hold[0].x) if w_pre is not None else (out, None, None)
@@ -444,4 +446,5 @@ def projection(u, weight, codes, col_scale=None, live=None):
 
 def gated_projection(ab, weight, act="silu", live=None):
     """(act(a) * b) @ weight.T for the halves a, b of ab, differentiable, which keeps a and b in 8 bits and no product."""
-    return _make_functions()[2].apply(ab, weight, act, live)
+    call = _make_functions()[2].apply
+    return call(ab, weight, act, live, _torch.is_grad_enabled() and (ab.requires_grad or weight.requires_grad))

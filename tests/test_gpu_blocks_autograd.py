@@ -164,3 +164,37 @@ def test_calls_that_record_no_graph_refuse_what_would_need_one():
         with t.no_grad():
             call()
     iodf.join_backward(saved, x, x, w_pre=w), iodf.weight_grad(codes, x, col_scale=w), iodf.pack(g)
+
+
+def test_gradients_that_nobody_asked_for_are_not_computed(monkeypatch):
+    """A projection of data, and a frozen weight; nothing is kept where nothing is recorded."""
+    t = torch()
+    from paper_2206_08869_amd import blocks
+    rows, cols, out = 4096, 1024, 16
+    x, dy = t.randn((rows, cols), device="cuda"), t.randn((rows, out), device="cuda")
+    w = t.randn((out, cols), device="cuda")
+    codes = iodf.pack(x)
+    learning, data = w.clone().requires_grad_(), x.clone().requires_grad_()
+    y = iodf.projection(x, learning, codes)
+    want = iodf.weight_grad(codes, dy)
+    t.cuda.synchronize()
+    t.cuda.reset_peak_memory_stats()
+    before = t.cuda.memory_allocated()
+    got, = t.autograd.grad(y, learning, dy)
+    assert t.equal(got, want) and t.cuda.max_memory_allocated() - before < 4 * rows * cols  # no gradient of x
+
+    def never(*args, **more):
+        raise AssertionError("a weight gradient that nobody asked for")
+
+    a = t.randn((rows, 2 * out), device="cuda").requires_grad_()
+    frozen = t.randn((cols, out), device="cuda")
+    both = t.autograd.grad(iodf.gated_projection(a, frozen.clone().requires_grad_()), a, x)[0]
+    monkeypatch.setattr(blocks, "weight_grad", never)
+    assert t.equal(t.autograd.grad(iodf.projection(data, w, codes), data, dy)[0], dy @ w)
+    assert t.equal(t.autograd.grad(iodf.gated_projection(a, frozen), a, x)[0], both)
+    saves, glu = [], blocks.glu
+    monkeypatch.setattr(blocks, "glu", lambda *args, save=True, **more: saves.append(save) or glu(*args, save=save, **more))
+    with t.no_grad():
+        silent = iodf.gated_projection(a, frozen)
+    assert t.equal(silent, iodf.gated_projection(a, frozen).detach()) and not silent.requires_grad
+    assert t.equal(silent, iodf.gated_projection(a.detach(), frozen)) and saves == [False, True, False]
