@@ -344,8 +344,16 @@ __device__ __forceinline__ void forget(RawCodes& r) { asm volatile("" : "+v"(r.q
 
 // ---- activations ----
 
-// act(a), and its derivative. The logistic function is exp and a reciprocal (both to the last bit or so): both ends are exact (exp overflows to
-// infinity, 1 / inf = 0).
+// exp(x) within three units of its last bit or so. The product x log2(e), rounded, is off by as many units as it has whole bits, 60 at x = 80; what
+// was rounded off and the constant's own rest come in again as a factor. Both ends are exact: infinity, 0 (the clamp only meets what is no
+// number there).
+__device__ __forceinline__ float exponential(float x) {
+    const float p = x * 1.44269502f, rest = fmaf(x, 1.92596303e-8f, fmaf(x, 1.44269502f, -p));
+    return __builtin_amdgcn_exp2f(p) * fmaf(__builtin_amdgcn_fmed3f(rest, -1.f, 1.f), 0.693147181f, 1.f);
+}
+
+// act(a), and its derivative. Relative errors in units of 2^-24: the logistic function some ten, with gelu another four times its argument, which
+// is rounded as often. Below exp(-87), where its reciprocal leaves the normal numbers, it is 0.
 template <int ACT>
 __device__ __forceinline__ float activate(float a, float& slope) {
     if (ACT == IODF_ACT_RELU) {
@@ -354,7 +362,7 @@ __device__ __forceinline__ float activate(float a, float& slope) {
     }
     const float k = 1.5957691216057308f;  // 2 sqrt(2 / pi)
     const float arg = ACT == IODF_ACT_SILU ? a : k * (a + 0.044715f * a * a * a);
-    const float s = __builtin_amdgcn_rcpf(1.f + __expf(-arg));
+    const float s = __builtin_amdgcn_rcpf(1.f + exponential(-arg));
     const float bend = s * (1.f - s);
     if (ACT == IODF_ACT_SILU) slope = s + a * bend;
     else slope = bend == 0.f ? s : s + a * bend * k * (1.f + 0.134145f * a * a);  // far out a * a may be infinite

@@ -648,3 +648,29 @@ def test_differentiable_calls_refuse_changed_parameters_and_second_derivatives()
     g, = t.autograd.grad(run(), f, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         g.sum().backward()
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_activations_keep_their_precision_in_the_tail(kind):
+    """Where the logistic function is small, relative to the result itself: exp, a sum, a reciprocal and two products come to ten units of 2^-24 or
+    so, a few more are allowed; gelu's argument 2 sqrt(2 / pi) (a + 0.044715 a^3) is rounded six times on its way (constants among them), half a unit
+    of its last bit each, and exp turns that into as many units times the argument. A slope cancels near its zero: it is held to its terms."""
+    a = np.linspace(-85, 85, 20001) if kind == "silu" else np.linspace(-7.6, 7.6, 20001)  # the argument within +-85
+    a = a.astype(np.float32).reshape(-1, 1)
+    x, one = dev(a), dev(np.ones_like(a))
+    a = a.astype(np.float64)
+    arg = np.abs(a if kind == "silu" else 2 * np.sqrt(2 / np.pi) * (a + 0.044715 * a ** 3))
+    units = (16 + (0 if kind == "silu" else 6 * arg)) * U
+    sig = 1 / (1 + np.exp(-(a if kind == "silu" else 2 * np.sqrt(2 / np.pi) * (a + 0.044715 * a ** 3))))
+    y, _ = iodf.glu(x, one, kind)
+    near(y, a * sig, "f32", units * np.abs(a * sig), kind)
+    c = iodf.pack(x)
+    v = ref.decode(c.q.cpu().numpy(), c.e.cpu().numpy(), 1)   # one number to a group: seven bits of it
+    inner = v if kind == "silu" else 2 * np.sqrt(2 / np.pi) * (v + 0.044715 * v ** 3)
+    grow = np.ones_like(v) if kind == "silu" else 2 * np.sqrt(2 / np.pi) * (1 + 3 * 0.044715 * v * v)
+    up, down = 1 / (1 + np.exp(-inner)), 1 / (1 + np.exp(inner))
+    units = (24 + (0 if kind == "silu" else 6 * np.abs(inner))) * U
+    da, db, _ = iodf.glu_backward(iodf.GluSaved(c, iodf.pack(one)), one, kind)
+    near(db, v * up, "f32", units * np.abs(v * up), kind + " again")
+    # 1 - s is taken from s in 32 bits: where s is near 1 its own units count, not those of the small rest
+    near(da, up + v * up * down * grow, "f32", units * (up + np.abs(v) * up * np.maximum(down, U) * grow) + 2 * U * np.abs(v) * grow * up * up, kind + " slope")
