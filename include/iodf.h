@@ -341,7 +341,8 @@ int iodf_glu_backward(const iodf_glu* args, void* stream);
  *   dw[o][c] = (accumulate ? dw[o][c] : 0) + col_scale[c] * sum_t dy[t][o] * X[t][c]
  * dy [rows][out] of dy_type, X what the checkpoint stands for, dw F32 with rows dw_stride apart. col_scale (may be NULL): the
  * weight of the norm between the checkpoint and the layer (w_pre of iodf_join). In a padded row neither dy nor the checkpoint adds
- * anything, whether the checkpoint was packed with `live` or without. Products are exact for every dy_type,
+ * anything, whether the checkpoint was packed with `live` or without. Products are exact for every dy_type
+ * (in 32 bits of numbers from 2^-109 on; of smaller ones, what lies below 2^-133 may be lost),
  * sums are 32-bit floats, in an order that depends on the sizes alone. 1 <= out <= 65536,
  * rows * (out rounded up to 32) <= 2^34.
  */

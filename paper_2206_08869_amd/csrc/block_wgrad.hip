@@ -4,7 +4,8 @@
 // to a lane) is a transpose. Tiles of KT rows go to LDS as they lie in memory, codes widened to bfloat16 (exact: seven bits and a sign
 // times a power of two) on the way, and the transposing LDS read takes them from there.
 // dy of more than eight significant bits is the exact sum of two (half precision) or three (32 bits) bfloat16 parts, multiplied
-// one after the other into the same sums.
+// one after the other into the same sums. A part is what fits of the rest, cut off and not rounded: rounded, the largest 32-bit numbers would be
+// infinite.
 #include "block_dev.h"
 
 #include <algorithm>
@@ -180,12 +181,14 @@ __global__ __launch_bounds__(256) void k_wgrad(const iodf_wgrad a, const Tiles t
                 for (int j = 0; j < 8; ++j) rest[j] = there ? rest[j] : 0.f;
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    const bf8 w = narrow8(rest);
-                    *(bf8*)&at[buf][p][to] = w;
+                    u32x4 w;  // the upper halves, two to a word
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float got = (float)w[j];
-                        rest[j] = fabsf(got) < __builtin_inff() ? rest[j] - got : 0.f;
+                    for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * j + 1]), __float_as_uint(rest[2 * j]), 0x07060302u);
+                    *(u32x4*)&at[buf][p][to] = w;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {  // a NaN stays one, an infinity has no rest
+                        const float got = __uint_as_float(__float_as_uint(rest[j]) & 0xffff0000u);
+                        rest[j] = p || fabsf(rest[j]) != __builtin_inff() ? rest[j] - got : 0.f;
                     }
                 }
             }

@@ -674,3 +674,17 @@ def test_activations_keep_their_precision_in_the_tail(kind):
     near(db, v * up, "f32", units * np.abs(v * up), kind + " again")
     # 1 - s is taken from s in 32 bits: where s is near 1 its own units count, not those of the small rest
     near(da, up + v * up * down * grow, "f32", units * (up + np.abs(v) * up * np.maximum(down, U) * grow) + 2 * U * np.abs(v) * grow * up * up, kind + " slope")
+
+
+def test_weight_grad_of_the_largest_numbers_in_32_bits():
+    """Up to the type's last number, which bfloat16 rounds to infinity: one row, to the bit. Infinities and NaN of any payload come out as such."""
+    t = torch()
+    top = np.finfo(np.float32).max
+    dy = np.float32([[top, -top, np.nextafter(np.float32(3.3961775e38), top), 3.3895314e38, 1.0000001, 2.0 ** -100, 0, np.inf, -np.inf, 0]])
+    dy.view(np.uint32)[0, 9] = 0x7f800001   # a NaN whose payload is in the lower half alone
+    x = np.float64([[0.25, 0.5, 2.0 ** -20]])
+    q, e = ref.encode(x)
+    codes = iodf.Codes(t.from_numpy(q).cuda(), t.from_numpy(e).cuda(), 3)
+    got = host(iodf.weight_grad(codes, t.from_numpy(dy).cuda()))
+    x = ref.decode(q, e, 3)[:, :2]
+    assert np.array_equal(got[:9, :2], dy[:, :9].astype(np.float64).T @ x) and np.isnan(got[9, :2]).all()
