@@ -269,7 +269,7 @@ int iodf_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int cols, void*
  * Sums and everything between loads and stores are 32-bit floats; x is taken from h' before it is rounded to the stream's type.
  * w_post NULL: no norm behind the block, n = f. w_pre NULL: none before the next, no x and no u. gate NULL and alpha NULL: 1.
  * Row t reads gate row t / gate_rows (gate_rows 1: a gate for each row; gate_rows >= rows: one gate for all). In a padded row
- * h' = h and u = 0. out_stream may be in_stream (same stride); otherwise outputs overlap no inputs.
+ * h' = h, to the bit, and u = 0, whatever stands in its gate, too. out_stream may be in_stream (same stride); otherwise outputs overlap no inputs.
  * The stream's type is F32 or the block's type; 1 <= cols <= 16384; eps > 0.
  *
  * iodf_join_forward: in_stream = h, in_block = f -> out_stream = h', out_block = u; with xq, not NULL, also the checkpoints of

@@ -116,10 +116,10 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                n[v][i] *= ip;
-                z[v][i] += coef[v][i] * n[v][i];
-            }
+            for (int i = 0; i < 8; ++i) n[v][i] *= ip;
+            if (now)  // the gate of a padded row may be no number either
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[v][i] += coef[v][i] * n[v][i];
             store8((TH*)a.out_stream + out + c[v].c0, c[v].n, z[v]);
             if (a.nq) {
                 if (!c[v].n)
@@ -574,7 +574,7 @@ __global__ __launch_bounds__(FC* FR) void k_join_params(const iodf_join a, const
                 weighted += s;  // the gates are in the sums already, or are 1
             } else {
                 const long long at = (long long)g * cols + c;
-                weighted += a.gate[at] * s;
+                weighted += s == 0 ? 0 : a.gate[at] * s;  // the gate of padded rows alone may be no number
                 a.dgate[at] = (float)(alpha * wp * s);
             }
         }

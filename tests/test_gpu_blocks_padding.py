@@ -69,3 +69,31 @@ def test_join_backward_of_no_rows_gives_zeros(groups, cols):
     g = iodf.join_backward(saved, h, u, *par)
     for got, p in zip(g[2:], par):
         assert t.equal(got, t.zeros_like(p))
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 40), (50, 40), (33, 300), (20, 1111), (9, 9001)])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_join_leaves_a_padded_row_s_gate_out(rows, cols, kind):
+    """A gate for each row, no number where the row is padding: h' is h there to the bit (signs of zeros among them), nothing reaches a gradient."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(rows)
+    live = t.rand(rows, generator=gen, device="cuda") < 0.6
+    live[0] = rows > 1
+    h, f, dh, du = (t.randn((rows, cols), generator=gen, device="cuda").to(getattr(t, kind)) for _ in range(4))
+    h[:, ::3] = -0.0
+    clean = [t.randn(s, generator=gen, device="cuda") for s in ((1,), (rows, cols), (cols,), (cols,))]
+    dirty = [x.clone() for x in clean]
+    dirty[1][~live] = float("nan")
+    dirty[1][~live, ::2] = float("inf")
+    bits = t.int32 if kind == "float32" else t.int16
+
+    def same(a, b):
+        return t.equal(a.view(bits), b.view(bits)) if a.dtype == h.dtype else t.equal(a, b)
+
+    (h1, u1, s1), (h2, u2, s2) = (iodf.join(h, f, *par, live=live) for par in (clean, dirty))
+    assert same(h1, h2) and same(u1, u2) and same(h1[~live], h[~live]) and not u1[~live].any()
+    for a, b in zip((*s1.x[:2], *s1.n[:2], s1.inv_pre, s1.inv_post), (*s2.x[:2], *s2.n[:2], s2.inv_pre, s2.inv_post)):
+        assert t.equal(a, b)
+    g1, g2 = (iodf.join_backward(s1, dh, du, *par, live=live) for par in (clean, dirty))
+    for a, b in zip(g1, g2):
+        assert t.isfinite(a).all() and same(a, b)
