@@ -147,7 +147,7 @@ def _codes(c, name, rows, cols, device):
         _refuse("%s has to be Codes" % name)
     pitch = _pitch(cols)
     q, e, _ = c
-    if c.cols != cols or q.dtype != _torch.int8 or e.dtype != _torch.uint8 or q.shape != (rows, pitch) or e.shape != (rows, pitch // 32) \
+    if not isinstance(q, _Tensor) or not isinstance(e, _Tensor) or c.cols != cols or q.dtype != _torch.int8 or e.dtype != _torch.uint8 or q.shape != (rows, pitch) or e.shape != (rows, pitch // 32) \
             or q.device != device or e.device != device or not q.is_contiguous() or not e.is_contiguous():
         _refuse("%s has to be the codes of %d x %d values on %s" % (name, rows, cols, device))
     return q.data_ptr(), e.data_ptr()
@@ -186,7 +186,7 @@ def unpack(codes, dtype=None):
     dtype = t.bfloat16 if dtype is None else dtype
     if dtype not in (t.bfloat16, t.float32):
         _refuse("codes are unpacked to bfloat16 or float32")
-    if not isinstance(codes, Codes):
+    if not isinstance(codes, Codes) or not isinstance(codes.q, _Tensor) or codes.q.dim() != 2:
         _refuse("codes has to be Codes")
     rows, cols, device = codes.q.shape[0], codes.cols, codes.q.device
     qp, ep = _codes(codes, "codes", rows, cols, device)
@@ -202,8 +202,10 @@ def unpack(codes, dtype=None):
 def _join_params(rows, cols, device, alpha, gate, w_post, w_pre, live):
     gate_rows, gp = rows, 0
     if gate is not None:
+        if not isinstance(gate, _Tensor) or gate.dim() not in (1, 2):
+            _refuse("gate has to be a float32 tensor [cols] or [groups, cols]")
         groups = 1 if gate.dim() == 1 else gate.shape[0]
-        if gate.dim() not in (1, 2) or gate.shape[-1] != cols or groups < 1 and rows or groups > 1 and rows % groups:
+        if gate.shape[-1] != cols or groups < 1 and rows or groups > 1 and rows % groups:
             _refuse("gate is %s: [cols] or [groups, cols] is wanted, groups that divide the %d rows" % (list(gate.shape), rows))
         gate_rows = rows // groups if groups else 0
         gp = _vector(gate, "gate", groups * cols, device)
@@ -251,7 +253,11 @@ def join_backward(saved, dh, du, alpha=None, gate=None, w_post=None, w_pre=None,
     device = dh.device
     if (du is None) != (w_pre is None):
         _refuse("du belongs to w_pre: both or none")
-    block_dtype = du.dtype if du is not None else block_dtype or dh.dtype
+    if not isinstance(saved, JoinSaved):
+        _refuse("saved has to be JoinSaved, which join returns with save=True")
+    block_dtype = getattr(du, "dtype", None) if du is not None else block_dtype or dh.dtype
+    if block_dtype not in _types:
+        _refuse("block_dtype is float32, bfloat16 or float16, not %s" % (block_dtype,))
     tf, sf = _matrix(du, "du", shape, block_dtype, device) if du is not None else (_types[block_dtype], cols)
     gate_rows, ap, gp, wop, wip, lp = _join_params(rows, cols, device, alpha, gate, w_post, w_pre, live)
     xq, xe = _codes(saved.x, "saved.x", rows, cols, device) if w_pre is not None else (0, 0)
@@ -303,6 +309,8 @@ def _glu_backward(saved, dy, act, live, rebuild):
     kind, sd = _matrix(dy, "dy")
     rows, cols = dy.shape
     device = dy.device
+    if not isinstance(saved, GluSaved):
+        _refuse("saved has to be GluSaved, which glu returns with save=True")
     aq, ae = _codes(saved.a, "saved.a", rows, cols, device)
     bq, be = _codes(saved.b, "saved.b", rows, cols, device)
     code, lp = _act(act), _live(live, rows, device)

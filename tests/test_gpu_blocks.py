@@ -688,3 +688,18 @@ def test_weight_grad_of_the_largest_numbers_in_32_bits():
     got = host(iodf.weight_grad(codes, t.from_numpy(dy).cuda()))
     x = ref.decode(q, e, 3)[:, :2]
     assert np.array_equal(got[:9, :2], dy[:, :9].astype(np.float64).T @ x) and np.isnan(got[9, :2]).all()
+
+
+def test_what_is_no_tensor_or_was_not_saved_is_refused():
+    t = torch()
+    x = t.zeros((6, 64), device="cuda")
+    c = iodf.pack(x)
+    for call in (lambda: iodf.join(x, x, gate=0.5), lambda: iodf.join(x, x, gate=x[0, 0]), lambda: iodf.join(x, x, gate=x[None]),
+                 lambda: iodf.join_backward(iodf.join(x, x, save=False)[2], x, None), lambda: iodf.join_backward((c, c, None, None), x, None),
+                 lambda: iodf.join_backward(iodf.JoinSaved(None, c, None, None), x, None, block_dtype=t.float64),
+                 lambda: iodf.join_backward(iodf.JoinSaved(c, c, x[:, 0].contiguous(), None), x, 1.0, w_pre=x[0]),
+                 lambda: iodf.glu_backward(iodf.glu(x, x, save=False)[1], x), lambda: iodf.unpack(iodf.Codes(None, None, 64)),
+                 lambda: iodf.unpack(iodf.Codes(c.q, None, 64)), lambda: iodf.weight_grad(iodf.Codes(None, c.e, 64), x),
+                 lambda: iodf.unpack(iodf.Codes(c.q[0], c.e[0], 64))):
+        with pytest.raises(ValueError, match="iodf"):
+            call()
