@@ -703,3 +703,78 @@ def test_what_is_no_tensor_or_was_not_saved_is_refused():
                  lambda: iodf.unpack(iodf.Codes(c.q[0], c.e[0], 64))):
         with pytest.raises(ValueError, match="iodf"):
             call()
+
+
+def test_the_binding_s_plain_entries_give_the_same_bits():
+    """The C names with addresses and argument blocks, as a caller without torch's operators has them, on a stream of the caller's."""
+    t = torch()
+    rows, cols, out = 300, 200, 136
+    rng, p, live = join_case(6, rows, cols, "f32", "bf16", 3, "some")
+    h, f, lv = dev(p["h"]), dev(p["f"], "bf16"), on_gpu(live)
+    alpha, gate, w_post, w_pre = par = params_on_gpu(p)
+    dy, du, pitch = dev(rng.standard_normal((rows, out)), "bf16"), dev(rng.standard_normal((rows, cols)), "bf16"), 224
+    h2, u, saved = iodf.join(h, f, *par, live=lv, eps=1e-5)
+    grads = iodf.join_backward(saved, h, du, *par, live=lv)
+    y, gated = iodf.glu(f, du, "gelu", live=lv)
+    da, db, yc = iodf.glu_backward(gated, f, "gelu", live=lv)
+    dw = iodf.weight_grad(saved.x, dy, col_scale=w_pre, live=lv)
+    back = iodf.unpack(saved.x)
+    st = t.cuda.Stream()
+    st.wait_stream(t.cuda.current_stream())
+
+    def codes():
+        return iodf.Codes(t.full((rows, pitch), 99, dtype=t.int8, device="cuda"), t.full((rows, pitch // 32), 99, dtype=t.uint8, device="cuda"), cols)
+
+    def at(**tensors):
+        return {k: v.data_ptr() for k, v in tensors.items()}
+
+    def same(got, want):
+        for a, b in zip(got, want):
+            assert t.equal(a, b)
+
+    with t.cuda.stream(st):
+        x, n, ipre, ipost = codes(), codes(), t.empty(rows, device="cuda"), t.empty(rows, device="cuda")
+        o_h, o_u = t.empty_like(h), t.empty_like(f)
+        a = iodf.JoinArgs(rows=rows, gate_rows=rows // 3, cols=cols, stream_type=iodf.IODF_T_F32, block_type=iodf.IODF_T_BF16, eps=1e-5,
+                          in_stream_stride=cols, in_block_stride=cols, out_stream_stride=cols, out_block_stride=cols,
+                          **at(alpha=alpha, gate=gate, w_post=w_post, w_pre=w_pre, live=lv, in_stream=h, in_block=f, out_stream=o_h, out_block=o_u,
+                               xq=x.q, xe=x.e, nq=n.q, ne=n.e, inv_pre=ipre, inv_post=ipost))
+        iodf.iodf_join_forward(a, st.cuda_stream)
+        st.synchronize()
+        same((o_h, o_u, *x[:2], *n[:2], ipre, ipost), (h2, u, *saved.x[:2], *saved.n[:2], saved.inv_pre, saved.inv_post))
+        g = [t.empty_like(v) for v in (h, f, *par)]
+        for name, v in at(in_block=du, out_stream=g[0], out_block=g[1], dalpha=g[2], dgate=g[3], dw_post=g[4], dw_pre=g[5]).items():
+            setattr(a, name, v)
+        work = t.empty(iodf.iodf_join_workspace(a), dtype=t.uint8, device="cuda")
+        iodf.iodf_join_backward(a, work.data_ptr(), work.numel(), st.cuda_stream)
+        st.synchronize()
+        same(g, grads)
+        ca, cb, cy, o_y, o_a, o_b = codes(), codes(), codes(), *(t.empty_like(f) for _ in range(3))
+        a = iodf.GluArgs(rows=rows, cols=cols, type=iodf.IODF_T_BF16, act=iodf.IODF_ACT_GELU, a_stride=cols, b_stride=cols, y_stride=cols, dy_stride=cols,
+                         da_stride=cols, db_stride=cols, **at(live=lv, a=f, b=du, y=o_y, dy=f, da=o_a, db=o_b, aq=ca.q, ae=ca.e, bq=cb.q, be=cb.e,
+                                                              yq=cy.q, ye=cy.e))
+        iodf.iodf_glu_forward(a, st.cuda_stream)
+        iodf.iodf_glu_backward(a, st.cuda_stream)
+        st.synchronize()
+        same((o_y, *ca[:2], *cb[:2], o_a, o_b, *cy[:2]), (y, *gated.a[:2], *gated.b[:2], da, db, *yc[:2]))
+        o_w = t.empty((out, cols), device="cuda")
+        a = iodf.WgradArgs(rows=rows, cols=cols, out=out, dy_type=iodf.IODF_T_BF16, dy_stride=out, dw_stride=cols,
+                           **at(dy=dy, q=x.q, e=x.e, col_scale=w_pre, live=lv, dw=o_w))
+        work = t.empty(iodf.iodf_weight_grad_workspace(a) + 16, dtype=t.uint8, device="cuda")
+        iodf.iodf_weight_grad(a, work.data_ptr(), work.numel(), st.cuda_stream)
+        c, o_v = codes(), t.empty_like(f)
+        iodf.iodf_pack(back.data_ptr(), iodf.IODF_T_BF16, cols, rows, cols, lv.data_ptr(), c.q.data_ptr(), c.e.data_ptr(), st.cuda_stream)
+        iodf.iodf_unpack(x.q.data_ptr(), x.e.data_ptr(), rows, cols, o_v.data_ptr(), iodf.IODF_T_BF16, cols, st.cuda_stream)
+        st.synchronize()
+        again = iodf.pack(back, live=lv)
+        same((o_w, o_v, *c[:2]), (dw, back, *again[:2]))
+    for call, bad in ((iodf.iodf_weight_grad, iodf.WgradArgs(rows=-1)), (iodf.iodf_join_backward, iodf.JoinArgs(rows=-1))):
+        with pytest.raises(iodf.IodfError):
+            call(bad, 0, 0, 0)
+    for call, bad in ((iodf.iodf_join_forward, iodf.JoinArgs(rows=-1)), (iodf.iodf_glu_forward, iodf.GluArgs(rows=-1)),
+                      (iodf.iodf_glu_backward, iodf.GluArgs(rows=-1))):
+        with pytest.raises(iodf.IodfError):
+            call(bad, 0)
+    for call, bad in ((iodf.iodf_join_workspace, iodf.JoinArgs(rows=-1)), (iodf.iodf_weight_grad_workspace, iodf.WgradArgs(rows=-1))):
+        with pytest.raises(iodf.IodfError):
+            call(bad)
