@@ -412,7 +412,7 @@ def _make_functions():
             w, col_scale, live, q, e = ctx.saved_tensors
             dy, to_u, to_weight = rows_first(dy), *ctx.needs_input_grad[:2]
             dw = weight_grad(Codes(q, e, ctx.cols), dy, col_scale=col_scale, live=live).to(ctx.dtype) if to_weight else None
-            return dy @ w if to_u else None, dw, None, None, None
+            return dy @ w.to(dy.dtype) if to_u else None, dw, None, None, None  # autocast may have given the product another type than u's
 
     class GatedProjection(t.autograd.Function):
         @staticmethod
@@ -432,7 +432,7 @@ def _make_functions():
             do = rows_first(do)
             saved = GluSaved(Codes(aq, ae, ctx.cols), Codes(bq, be, ctx.cols))
             to_weight = ctx.needs_input_grad[1]
-            dab, y = _glu_backward(saved, do @ w, ctx.act, live, to_weight)
+            dab, y = _glu_backward(saved, do @ w.to(do.dtype), ctx.act, live, to_weight)
             return dab, weight_grad(y, do, live=live).to(ctx.dtype) if to_weight else None, None, None, None
 
     _functions = (Joined, Projection, GatedProjection)

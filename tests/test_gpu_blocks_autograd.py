@@ -198,3 +198,25 @@ def test_gradients_that_nobody_asked_for_are_not_computed(monkeypatch):
         silent = iodf.gated_projection(a, frozen)
     assert t.equal(silent, iodf.gated_projection(a, frozen).detach()) and not silent.requires_grad
     assert t.equal(silent, iodf.gated_projection(a.detach(), frozen)) and saves == [False, True, False]
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+@pytest.mark.parametrize("inputs", ["float32", "bfloat16"])
+def test_projections_under_autocast(kind, inputs):
+    """The product's type is autocast's, the gradients' are the inputs'; near the product of the same numbers in 64 bits: 16-bit roundings of the
+    operands (half a unit, 2^-9, each), of the product and of its gradient, and codes of a percent or so."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(1)
+    x, a = (t.randn((256, 96), generator=gen, device="cuda").to(getattr(t, inputs)).requires_grad_() for _ in range(2))
+    w, v = t.randn((64, 96), generator=gen, device="cuda").requires_grad_(), t.randn((64, 48), generator=gen, device="cuda").requires_grad_()
+    dy = t.randn((256, 64), generator=gen, device="cuda").to(getattr(t, kind))
+    with t.autocast("cuda", dtype=getattr(t, kind)):
+        y, z = iodf.projection(x, w, iodf.pack(x)), iodf.gated_projection(a, v)
+    assert y.dtype == z.dtype == getattr(t, kind)
+    got = t.autograd.grad((y, z), (x, w, a, v), (dy, dy))
+    wide = [p.detach().double().requires_grad_() for p in (x, w, a, v)]
+    x2, w2, a2, v2 = wide
+    left, right = a2.chunk(2, 1)
+    want = t.autograd.grad((x2 @ w2.t(), (left * t.sigmoid(left) * right) @ v2.t()), wide, (dy.double(), dy.double()))
+    for g, w, p in zip(got, want, (x, w, a, v)):
+        assert g.dtype == p.dtype and (g.double() - w).norm() <= 0.03 * w.norm()
