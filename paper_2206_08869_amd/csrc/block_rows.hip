@@ -23,6 +23,12 @@ __device__ __forceinline__ int team_of() {
     return LPR > 64 ? 0 : LPR == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : threadIdx.x / LPR;
 }
 
+// 1 / sqrt(x) for x > 0. The instruction takes numbers below the normal ones, which a row of zeros and a tiny eps give, for 0.
+__device__ __forceinline__ float inverse_root(float x) {
+    const bool tiny = x < 0x1p-126f;
+    return __builtin_amdgcn_rsqf(tiny ? x * 0x1p24f : x) * (tiny ? 0x1p12f : 1.f);
+}
+
 // coef[c] = alpha * gate[c] * w_post[c]
 __device__ __forceinline__ void load_params(const float* p, int c0, int cols, float v[8], float absent) {
     if (p) {
@@ -110,7 +116,7 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
                 s += c[v].n ? part : 0.f;
             }
             row_sums<LPR, 1>(&s, meet, turn);
-            ip = __builtin_amdgcn_rsqf(s * inv_cols + a.eps);
+            ip = inverse_root(s * inv_cols + a.eps);
         }
         const long long out = (long long)row * a.out_stream_stride;
 #pragma unroll
@@ -139,7 +145,7 @@ __global__ __launch_bounds__(threads_of<LPR>()) void k_join_forward(const iodf_j
                 s += c[v].n ? part : 0.f;
             }
             row_sums<LPR, 1>(&s, meet, turn);
-            const float iq = __builtin_amdgcn_rsqf(s * inv_cols + a.eps);
+            const float iq = inverse_root(s * inv_cols + a.eps);
             const long long uo = (long long)row * a.out_block_stride;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {

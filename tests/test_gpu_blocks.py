@@ -778,3 +778,19 @@ def test_the_binding_s_plain_entries_give_the_same_bits():
     for call, bad in ((iodf.iodf_join_workspace, iodf.JoinArgs(rows=-1)), (iodf.iodf_weight_grad_workspace, iodf.WgradArgs(rows=-1))):
         with pytest.raises(iodf.IodfError):
             call(bad)
+
+
+@pytest.mark.parametrize("eps", [1e-6, 1e-30, 1.2e-38, 1e-38, 1e-40, 1.4e-45])
+@pytest.mark.parametrize("cols", [5, 64, 1111])
+def test_join_of_rows_of_zeros(cols, eps):
+    """Whatever eps > 0 there is: zeros over sqrt(eps) are zeros, and the factors are finite."""
+    t = torch()
+    f, w = t.zeros((3, cols), device="cuda"), t.ones(cols, device="cuda")
+    f[1] = 0.5
+    h, u, saved = iodf.join(t.zeros_like(f), f, w_post=w, w_pre=w, eps=eps)
+    root = np.float64(np.float32(eps)) ** -0.5
+    for got in (saved.inv_post, saved.inv_pre):
+        got = host(got)
+        assert np.abs(got[[0, 2]] / root - 1).max() < 8 * U
+    assert not host(h)[[0, 2]].any() and not host(u)[[0, 2]].any()
+    near(u[1:2], np.full((1, cols), (1 + eps) ** -0.5), "f32", SLACK * U, "u")
