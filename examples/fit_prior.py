@@ -3,7 +3,8 @@
 A flow's prior gives every latent a discretised logistic distribution; the closer its mean and scale, the fewer bits the coder needs. This program
 takes images through `Flow.forward` and trains a residual network that predicts the level-1 latents of a position from the deeper levels' latents
 there, which a decoder has before it (levels are decoded from the deepest one up). The network is a stream of residual blocks with norms around each
-block, a gate and a residual scale; all that its backward pass keeps of them is in 8 bits.
+block, a gate and a residual scale; all that its backward pass keeps of them is in 8 bits. The bits that it prints are what such a prior would need;
+the coder itself keeps to the blob's integer prior, which is the same to the bit everywhere, as a network in bfloat16 is not.
 
     python examples/fit_prior.py --model paper_res32 --images 64 --steps 60
 """

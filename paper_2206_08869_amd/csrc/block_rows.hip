@@ -184,8 +184,10 @@ struct Runs {
 // so that a row meets once, for four sums, and not twice. That sum is also the row's part of dalpha (and alpha may be 0).
 // One vector to a thread, kept as it was loaded and widened again behind the meeting: held as 32-bit floats it would spill. Registers for four
 // waves a SIMD where that spills little, three where rows are 32 bits or a wave's own.
-// 32768 x 4096 in bfloat16: 272 us for 1.35 GB (5.0 TB/s); aligned widths from 512 to 8192: 4.2 to 4.6 TB/s with inputs in 16 bits or a stream in 32;
-// 3.3 to 3.8 TB/s for odd widths, whose vectors straddle lines.
+// 32768 x 4096 in bfloat16: 249 to 272 us for 1.35 GB (5.0 to 5.4 TB/s). TB/s for 2^26 elements, stream and block in bfloat16 / in 32 bits: widths
+// that fill their threads (1024, 1536, 2048, 4096) 4.4, 4.1, 4.2, 4.4 / 4.4, 4.3, 4.8, 4.9; that leave some of them idle (1112: 28 %, 2104: 49 %,
+// 4104: 33 %) 4.0, 3.5, 3.5 / 3.7, 3.8, 4.8. Rows that start at any element, whose vectors straddle lines, cost another 4 to 10 %: 1111, 2100, 4095
+// columns 3.6, 3.2, 4.0 / 3.5, 3.5, 4.7.
 template <typename TH, typename TF, int LPR, bool OWN>
 __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR <= 64 ? 3 : 4) void k_join_backward(
     const iodf_join a, const Runs runs, const int over_h, const int over_u, float* sum_pre, float* sum_post, double* sum_alpha) {
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(threads_of<LPR>(), OWN ? 1 : sizeof(TF) == 4 || LPR
 // The same for rows of more than 8192 columns, two vectors to each of 1024 threads: with 128 registers to a thread (64 KB of a row, its parameters
 // and sums in 256 KB), nothing of a row is held. The vectors are taken one after the other, each fetched while the one before is worked on, once
 // for the sums over the row and once more, out of L2, for the gradients; the columns' sums are in LDS and the parameters are read again.
-// 4096 x 16384: 275 us in bfloat16, 329 us with a stream in 32 bits (2.5 and 2.9 TB/s); rows held in registers, which spilled: 575 and 785.
+// 4096 x 16384: 267 us in bfloat16, 314 us with a stream in 32 bits (2.5 and 3.0 TB/s); rows held in registers, which spilled: 575 and 785.
 template <typename TH, typename TF, bool OWN>
 __global__ __launch_bounds__(1024) void k_join_backward_far(const iodf_join a, const Runs runs, const int over_h, const int over_u, float* sum_pre,
                                                             float* sum_post, double* sum_alpha) {
@@ -512,8 +514,9 @@ __global__ __launch_bounds__(1024) void k_join_backward_far(const iodf_join a, c
 
 // The parameters' gradients from the runs' sums. A workgroup has FC columns and FR threads for each, which share the runs: in the first row of
 // workgroups group by group for dgate = alpha w_post S and dw_post = alpha sum gate S, S a group's sum, in the second one over all runs for
-// dw_pre; a workgroup of the third one adds the runs' parts of dalpha. Sixteen loads of a thread are in flight. 4096 columns, 512 runs: 10.6 us;
-// 1111 columns, 7 gates: 5.4 us.
+// dw_pre; a workgroup of the third one adds the runs' parts of dalpha. Sixteen loads of a thread are in flight. 4096 columns, 512 runs: 10.5 us;
+// 1111 columns, 7 gates: 5.4 us. A column's threads take the groups one after the other, FR at a time, so that many shared gates take long: the
+// whole backward pass of 131072 x 512 in bfloat16 with 1, 1024, 16384 and 65536 gates takes 153, 179, 491 and 1760 us (a gate for each row: 254).
 constexpr int FC = 16, FR = 64;  // a wave has four threads of each column
 
 __device__ __forceinline__ float column_sum(const float* p, int n, int wide, int lane, int lanes) {

@@ -90,8 +90,8 @@ __device__ __forceinline__ void store_outputs(const f32x16 (&acc)[MT][NT], const
 
 // BM x BN outputs to a workgroup of four waves, a quarter to each. Operands come through registers, two tiles ahead: for every type of dy, for
 // layers too small for tiles of 256, and for narrow ones, which are bound by memory. 100000 rows, 1000 x 37 weights: 40 us, 5.1 TB/s;
-// 4096 rows, 1024 x 1024: 30 us and 8 us for the slices' sums; 16384 rows, 4096 x 4096, dy in 32 bits: 1777 us, 930 TFLOP/s of the three
-// parts' products. Tiles of 64 rows instead of 32, half as many barriers: the same within 1 %, 8 % behind for the smallest.
+// 4096 rows, 1024 x 1024: 36 us with the slices' sums; 16384 rows, 4096 x 4096, dy in 32 bits: 1650 us, 1000 TFLOP/s of the three
+// parts' products, in half precision 1222 us, 900 TFLOP/s of two. Tiles of 64 rows instead of 32, half as many barriers: the same within 1 %, 8 % behind for the smallest.
 // Padding (LIVE) is bits in LDS and costs 4 to 9 %: 40.5 us instead of 38.4 at 4096 rows, 1024 x 1024; a byte loaded beside each chunk of dy and of
 // codes cost up to 140 % (20000 rows, 1030 x 1100, 32 bits: 247 us against 566, 229 without padding).
 template <typename TY, int BM, int BN, bool LIVE>
@@ -525,9 +525,11 @@ constexpr TileCost kTiles[] = {{64, 64, 4.3f, 0.26f, 0.17f}, {64, 128, 6.3f, 0.3
 
 // The tile and the number of slices of least estimated time. Large tiles read operands less often, small ones fill the chip with few outputs and
 // end sooner; slices do so with few tiles, at the price of their sums' way through memory (about 0.36 us a megabyte there and back) and of a second
-// launch. Over 18 shapes from 64 x 512 x 512 to 131072 x 512 x 512, timed with every tile and slices in powers of two, the choice is at most 8 %
-// behind the best of them; one fixed rule (the largest tile that fills the chip, slices for 512 workgroups) was up to 2.7 times behind (512 x 2048
-// x 2048: 44 us against 16).
+// launch. Over 18 shapes from 64 x 512 x 512 to 131072 x 512 x 512, timed with every tile and slices in powers of two, dy in bfloat16: at 14 the
+// choice is within 7 % of the best of them, at two (16384 rows, 2048 x 512 and 66 x 896) 11 and 12 % behind, and at two it takes slices where none
+// are better (1000 rows, 130 x 72: 14.0 us against 11.5; 2048 rows, 1024 x 1024: 26.0 against 19.3); with dy in 16 and 32 bits at most 24 and 20 %
+// behind. One fixed rule (the largest tile that fills the chip, slices for 512 workgroups) was up to 2.7 times behind (512 x 2048 x 2048: 44 us
+// against 16). A step with parts of dy takes 1.5 to 1.9 (two) and 1.8 to 2.5 times (three) as long as one without where steps are most of the time.
 Plan plan_of(const iodf_wgrad& a) {
     auto up = [](long long n, long long d) { return (n + d - 1) / d; };
     const float parts = a.dy_type == IODF_T_BF16 ? 1.f : a.dy_type == IODF_T_F16 ? 1.9f : 2.7f;
