@@ -397,9 +397,8 @@ def _make_functions():
 
     class Projection(t.autograd.Function):
         @staticmethod
-        def forward(ctx, u, weight, codes, col_scale, live):
+        def forward(ctx, u, weight, codes, col_scale, live, learns):
             w = weight.to(u.dtype)
-            learns = ctx.needs_input_grad[1]
             if learns and not isinstance(codes, Codes):
                 _refuse("codes has to be Codes")
             ctx.save_for_backward(w, col_scale, live, *(codes[:2] if learns else (None, None)))
@@ -412,7 +411,7 @@ def _make_functions():
             w, col_scale, live, q, e = ctx.saved_tensors
             dy, to_u, to_weight = rows_first(dy), *ctx.needs_input_grad[:2]
             dw = weight_grad(Codes(q, e, ctx.cols), dy, col_scale=col_scale, live=live).to(ctx.dtype) if to_weight else None
-            return dy @ w.to(dy.dtype) if to_u else None, dw, None, None, None  # autocast may have given the product another type than u's
+            return dy @ w.to(dy.dtype) if to_u else None, dw, None, None, None, None  # autocast may have given the product another type than u's
 
     class GatedProjection(t.autograd.Function):
         @staticmethod
@@ -449,7 +448,8 @@ def joined(h, f, alpha=None, gate=None, w_post=None, w_pre=None, live=None, eps=
 
 def projection(u, weight, codes, col_scale=None, live=None):
     """u @ weight.T, differentiable, which keeps no u: the weight's gradient reads codes, which stand for u / col_scale."""
-    return _make_functions()[1].apply(u, weight, codes, col_scale, live)
+    call = _make_functions()[1].apply
+    return call(u, weight, codes, col_scale, live, _torch.is_grad_enabled() and weight.requires_grad)
 
 
 def gated_projection(ab, weight, act="silu", live=None):

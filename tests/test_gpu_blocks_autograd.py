@@ -220,3 +220,13 @@ def test_projections_under_autocast(kind, inputs):
     want = t.autograd.grad((x2 @ w2.t(), (left * t.sigmoid(left) * right) @ v2.t()), wide, (dy.double(), dy.double()))
     for g, w, p in zip(got, want, (x, w, a, v)):
         assert g.dtype == p.dtype and (g.double() - w).norm() <= 0.03 * w.norm()
+
+
+def test_a_projection_that_nothing_is_recorded_of_wants_no_codes():
+    t = torch()
+    u, w = t.randn((4, 32), device="cuda").requires_grad_(), t.randn((8, 32), device="cuda").requires_grad_()
+    with t.no_grad():
+        y = iodf.projection(u, w, None)
+    assert t.equal(y, (u @ w.t()).detach()) and not y.requires_grad
+    got, = t.autograd.grad(iodf.projection(u, w.detach(), None), u, t.ones_like(y))
+    assert t.equal(got, t.ones_like(y) @ w.detach())
