@@ -361,6 +361,82 @@ typedef struct iodf_wgrad {
 int iodf_weight_grad(const iodf_wgrad* args, void* work, int64_t work_bytes, void* stream);
 int iodf_weight_grad_workspace(const iodf_wgrad* args, int64_t* bytes);
 
+/*
+ * The two ends of a training step: the loss over a table of classes, and orthogonalised updates of weights. Memory, streams, rows and padding
+ * are as for the training operators above.
+ *
+ * Softmax cross entropy of rows u [rows][cols] against a table W [classes][cols], both of `type`, without the logits ever being in memory:
+ *   s[t][v] = sum_c u[t][c] W[v][c],  lse[t] = log sum_v exp s[t][v],  loss[t] = lse[t] - s[t][target[t]]
+ * iodf_class_loss_forward: loss, lse (F32 [rows]; 0 in padded rows). dloss, dlse, du and dw are not looked at.
+ * iodf_class_loss_backward: lse as the forward pass gave it, dloss = dL/dloss and dlse = dL/dlse (either may be NULL: 0) ->
+ *   du[t][c] = sum_v g[t][v] W[v][c] and dw[v][c] = sum_t g[t][v] u[t][c] of `type` (either may be NULL: not computed), with
+ *   g[t][v] = (dloss[t] + dlse[t]) exp(s[t][v] - lse[t]) - (v == target[t]) dloss[t].
+ *   It goes over the classes in pieces whose g fits 512 MB. In 16-bit types g is rounded to that type (times a power of two in half precision),
+ *   which is as much as the gradients' own rounding. In F32 numbers are multiplied in two parts of 11 bits each: exact to 2^-22 of the number, or to
+ *   2^-38 of the tensor's largest.
+ * `live` as above: a padded row's u, target, lse, dloss and dlse may be anything; its du is 0. A target outside 0..classes-1 in any other row makes that
+ * row's loss, du and all of dw NaN. Sums are in an order that depends on the sizes alone. With no rows dw is 0.
+ * 0 <= rows <= 2^24, 1 <= classes <= 2^20, 1 <= cols <= 65536, rows and classes times cols <= 2^34. Outputs overlap no inputs.
+ */
+typedef struct iodf_class_loss {
+    int64_t rows;
+    int32_t classes, cols, type, reserved;
+    const void* u;
+    const void* w;
+    int64_t u_stride, w_stride;
+    const int64_t* target;
+    const uint8_t* live;
+    float* loss;
+    float* lse;
+    const float* dloss;
+    const float* dlse;
+    void* du;
+    void* dw;
+    int64_t du_stride, dw_stride;
+} iodf_class_loss;
+int iodf_class_loss_forward(const iodf_class_loss* args, void* work, int64_t work_bytes, void* stream);
+int iodf_class_loss_backward(const iodf_class_loss* args, void* work, int64_t work_bytes, void* stream);
+int iodf_class_loss_workspace(const iodf_class_loss* args, int backward, int64_t* bytes);
+
+/*
+ * A gradient made nearly orthogonal: G [rows][cols] divided by its Frobenius norm + eps, then `steps` times an odd polynomial of its singular values,
+ *   X <- a X + b (X X') X + c (X X')^2 X,
+ * which brings all but the smallest of them near 1 and leaves the singular vectors. `count` matrices at once, in_batch and out_batch elements apart.
+ * coefficients: host memory, a, b, c of each step. For out_type BF16 the numbers that are multiplied are rounded to 11 bits (of X X' only
+ * what lies beside its diagonal; X itself is kept in 22), which shows in the result as less than its own rounding; for F32 and F16 they have 22 bits.
+ * Norms and sums are 32 bits or more. A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN.
+ * 0 <= count <= 4096, 1 <= rows, cols <= 65536, the shorter side at most 16384, count * rows * cols (each rounded up to 64) <= 2^32,
+ * 1 <= steps <= 16. Polynomials that let singular values from 0..1 grow past 64 are refused. out may be in (same type and strides).
+ *
+ * iodf_muon_step: the step of an optimiser around that, for `count` weights of one shape, each a tensor of its own (arrays of pointers, host memory):
+ *   M <- beta M + G,  D = G + beta M (nesterov) or M,  W <- (1 - rate * decay) W - rate * scale * orthogonalise(D)
+ * M F32 with consecutive rows; W and G strided, of their types. Products are as for out_type = weight_type. 0 <= count <= 64. Tensors of one call
+ * do not overlap.
+ */
+enum { IODF_ORTH_MOST = 16, IODF_MUON_MOST = 64 };
+typedef struct iodf_orth {
+    int64_t count, in_batch, out_batch, in_stride, out_stride;
+    int32_t rows, cols, in_type, out_type, steps;
+    float eps;
+    const float* coefficients;
+    const void* in;
+    void* out;
+} iodf_orth;
+int iodf_orthogonalise(const iodf_orth* args, void* work, int64_t work_bytes, void* stream);
+int iodf_orthogonalise_workspace(const iodf_orth* args, int64_t* bytes);
+
+typedef struct iodf_muon {
+    int64_t count, weight_stride, grad_stride;
+    int32_t rows, cols, weight_type, grad_type, steps, nesterov;
+    float eps, rate, beta, decay, scale, reserved;
+    const float* coefficients;
+    void* const* weights;
+    const void* const* grads;
+    float* const* momenta;
+} iodf_muon;
+int iodf_muon_step(const iodf_muon* args, void* work, int64_t work_bytes, void* stream);
+int iodf_muon_workspace(const iodf_muon* args, int64_t* bytes);
+
 /* Read one IODF_Q_* quantity into *out (host). */
 int iodf_query(iodf_ctx* ctx, int what, int64_t* out);
 

@@ -26,10 +26,12 @@ EXPORTS = ["iodf_init", "iodf_forward", "iodf_inverse", "iodf_query", "iodf_free
            "iodf_decode", "iodf_codec_tables", "iodf_tile_patches", "iodf_untile_patches",
            "iodf_conv_probe", "iodf_encode_noalloc", "iodf_conv_probe_timeline", "iodf_pack", "iodf_unpack",
            "iodf_join_forward", "iodf_join_backward", "iodf_join_workspace", "iodf_glu_forward", "iodf_glu_backward",
-           "iodf_weight_grad", "iodf_weight_grad_workspace"]
+           "iodf_weight_grad", "iodf_weight_grad_workspace", "iodf_class_loss_forward", "iodf_class_loss_backward",
+           "iodf_class_loss_workspace", "iodf_orthogonalise", "iodf_orthogonalise_workspace", "iodf_muon_step", "iodf_muon_workspace"]
 
 IODF_T_F32, IODF_T_BF16, IODF_T_F16 = range(3)
 IODF_ACT_RELU, IODF_ACT_SILU, IODF_ACT_GELU = range(3)
+IODF_ORTH_MOST, IODF_MUON_MOST = 16, 64
 
 
 class KernelStat(ctypes.Structure):
@@ -58,6 +60,26 @@ class WgradArgs(ctypes.Structure):
                 ("accumulate", ctypes.c_int32), ("dy", ctypes.c_void_p), ("dy_stride", ctypes.c_int64), ("q", ctypes.c_void_p),
                 ("e", ctypes.c_void_p), ("col_scale", ctypes.c_void_p), ("live", ctypes.c_void_p), ("dw", ctypes.c_void_p),
                 ("dw_stride", ctypes.c_int64)]
+
+
+class ClassLossArgs(ctypes.Structure):
+    _fields_ = ([("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("classes", "cols", "type", "reserved")] +
+                [("u", ctypes.c_void_p), ("w", ctypes.c_void_p), ("u_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64)] +
+                [(n, ctypes.c_void_p) for n in ("target", "live", "loss", "lse", "dloss", "dlse", "du", "dw")] +
+                [("du_stride", ctypes.c_int64), ("dw_stride", ctypes.c_int64)])
+
+
+class OrthArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("count", "in_batch", "out_batch", "in_stride", "out_stride")] +
+                [(n, ctypes.c_int32) for n in ("rows", "cols", "in_type", "out_type", "steps")] + [("eps", ctypes.c_float)] +
+                [(n, ctypes.c_void_p) for n in ("coefficients", "in_", "out")])
+
+
+class MuonArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("count", "weight_stride", "grad_stride")] +
+                [(n, ctypes.c_int32) for n in ("rows", "cols", "weight_type", "grad_type", "steps", "nesterov")] +
+                [(n, ctypes.c_float) for n in ("eps", "rate", "beta", "decay", "scale", "reserved")] +
+                [(n, ctypes.c_void_p) for n in ("coefficients", "weights", "grads", "momenta")])
 
 
 class IodfError(RuntimeError):
@@ -152,6 +174,15 @@ def load_library(build_if_missing=True):
         getattr(L, name).restype = ci
         getattr(L, name).argtypes = [args(kind), vp, i64, vp]
     for name, kind in (("iodf_join_workspace", JoinArgs), ("iodf_weight_grad_workspace", WgradArgs)):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [args(kind), args(i64)]
+    for name, kind in (("iodf_class_loss_forward", ClassLossArgs), ("iodf_class_loss_backward", ClassLossArgs), ("iodf_orthogonalise", OrthArgs),
+                       ("iodf_muon_step", MuonArgs)):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [args(kind), vp, i64, vp]
+    L.iodf_class_loss_workspace.restype = ci
+    L.iodf_class_loss_workspace.argtypes = [args(ClassLossArgs), ci, args(i64)]
+    for name, kind in (("iodf_orthogonalise_workspace", OrthArgs), ("iodf_muon_workspace", MuonArgs)):
         getattr(L, name).restype = ci
         getattr(L, name).argtypes = [args(kind), args(i64)]
     _LIB = L
@@ -287,6 +318,40 @@ def iodf_weight_grad_workspace(args):
 
 def iodf_weight_grad(args, work_ptr, work_bytes, stream):
     _check(load_library().iodf_weight_grad(args, work_ptr, work_bytes, stream))
+
+
+def iodf_class_loss_workspace(args, backward):
+    n = ctypes.c_int64(0)
+    _check(load_library().iodf_class_loss_workspace(args, backward, n))
+    return n.value
+
+
+def iodf_class_loss_forward(args, work_ptr, work_bytes, stream):
+    _check(load_library().iodf_class_loss_forward(args, work_ptr, work_bytes, stream))
+
+
+def iodf_class_loss_backward(args, work_ptr, work_bytes, stream):
+    _check(load_library().iodf_class_loss_backward(args, work_ptr, work_bytes, stream))
+
+
+def iodf_orthogonalise_workspace(args):
+    n = ctypes.c_int64(0)
+    _check(load_library().iodf_orthogonalise_workspace(args, n))
+    return n.value
+
+
+def iodf_orthogonalise(args, work_ptr, work_bytes, stream):
+    _check(load_library().iodf_orthogonalise(args, work_ptr, work_bytes, stream))
+
+
+def iodf_muon_workspace(args):
+    n = ctypes.c_int64(0)
+    _check(load_library().iodf_muon_workspace(args, n))
+    return n.value
+
+
+def iodf_muon_step(args, work_ptr, work_bytes, stream):
+    _check(load_library().iodf_muon_step(args, work_ptr, work_bytes, stream))
 
 
 def iodf_codec_tables():

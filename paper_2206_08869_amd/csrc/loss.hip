@@ -1,0 +1,595 @@
+// Softmax cross entropy of rows against a table of classes, and its gradient: products of 16-bit numbers (products.h) whose logits never reach
+// memory as such.
+//
+// Forward: a workgroup has the logits of a tile of classes and rows in registers and leaves, for each of its rows, their largest and
+// the sum of exponentials relative to it; a second kernel joins the tiles of a row. Backward: the logits once more, from which g = (dloss + dlse) exp(s -
+// lse) - dloss [target] goes to memory in 16 bits, piece by piece of the classes; du += g W and dw = g' u are two more products.
+#include <algorithm>
+
+#include "products.h"
+#include "step.h"
+
+namespace iodf {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr long long kPieceBytes = 512ll << 20;  // of g
+constexpr int kMaxima = 256;                    // partial maxima of a tensor
+
+inline long long up(long long n, long long d) { return (n + d - 1) / d * d; }
+
+// What the kernels need of numbers' sizes, powers of two. Only where numbers have to be moved into the range of half precision.
+struct Scales {
+    float u, w, g;           // what u, W and g are multiplied with
+    float iu, iw, ig;        // and the inverses
+};
+
+// ---- getting operands ready ----
+
+__device__ __forceinline__ float finite_max(float m, float v) {
+    v = fabsf(v);
+    return v < __builtin_inff() && v > m ? v : m;
+}
+__device__ __forceinline__ float block_max(float m, float* meet) {  // 256 threads
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
+    if ((threadIdx.x & 63) == 0) meet[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(meet[0], meet[1]), fmaxf(meet[2], meet[3]));
+    __syncthreads();
+    return m;
+}
+
+struct MaxArgs {
+    const float* u;   // of 32-bit operands; NULL: 16 bits, no need
+    const float* w;
+    long long u_stride, w_stride, rows, classes;
+    int cols;
+    const uint8_t* live;
+    const float* dloss;
+    const float* dlse;
+};
+
+// blockIdx.y: 0 u, 1 W, 2 what g is made of
+__global__ __launch_bounds__(256) void k_maxima(const MaxArgs a, float* maxima) {
+    __shared__ float meet[4];
+    const int what = blockIdx.y;
+    float m = 0.f;
+    if (what == 2) {
+        for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < a.rows; t += (long long)gridDim.x * 256) {
+            if (a.live && !a.live[t]) continue;
+            const float d = a.dloss ? a.dloss[t] : 0.f;
+            m = finite_max(finite_max(m, d), a.dlse ? a.dlse[t] + d : d);
+        }
+    } else if (what == 0 ? a.u : a.w) {
+        const float* const x = what == 0 ? a.u : a.w;
+        const long long stride = what == 0 ? a.u_stride : a.w_stride, rows = what == 0 ? a.rows : a.classes;
+        for (long long t = blockIdx.x; t < rows; t += gridDim.x) {
+            if (what == 0 && a.live && !a.live[t]) continue;
+            for (int c = threadIdx.x; c < a.cols; c += 256) m = finite_max(m, x[t * stride + c]);
+        }
+    }
+    m = block_max(m, meet);
+    if (threadIdx.x == 0) maxima[what * kMaxima + blockIdx.x] = m;
+}
+
+// The power of two that takes numbers up to m to just below 2^15.
+__device__ __forceinline__ float lift(float m, float& inverse) {
+    int e = 0;
+    if (m > 0.f) {
+        frexpf(m, &e);
+        e = min(126, max(-112, 15 - e));
+    }
+    inverse = ldexpf(1.f, -e);
+    return ldexpf(1.f, e);
+}
+
+__global__ __launch_bounds__(256) void k_scales(const float* maxima, int wide, Scales* s) {
+    __shared__ float meet[4];
+    float m[3];
+    for (int k = 0; k < 3; ++k) m[k] = block_max(maxima[k * kMaxima + threadIdx.x], meet);
+    if (threadIdx.x) return;
+    Scales r;
+    r.u = lift(wide ? m[0] : 0.f, r.iu);
+    r.w = lift(wide ? m[1] : 0.f, r.iw);
+    r.g = lift(2.f * m[2], r.ig);
+    *s = r;
+}
+
+// x [rows][cols] -> 16-bit rows of `pitch` with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in two parts of half precision.
+template <typename TX>
+__global__ __launch_bounds__(256) void k_ready(const TX* x, long long stride, long long rows, int cols, int pitch, const uint8_t* live,
+                                               const float* scale, uint16_t* y, long long plane) {
+    const int per = pitch / 8;
+    const float by = sizeof(TX) == 4 ? *scale : 1.f;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (long long)gridDim.x * 256) {
+        const long long t = i / per;
+        const int c = (int)(i - t * per) * 8, n = live && !live[t] ? 0 : cols - c;
+        const Raw8<TX> r = fetch8(x + t * stride + c, n, false);
+        if (sizeof(TX) == 2) {
+            *(u32x4*)(y + t * pitch + c) = u32x4{r.w[0], r.w[1], r.w[2], r.w[3]};
+        } else {
+            float v[8];
+            widen8(r, v);
+            _Float16 hi[8], lo[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float s = v[j] * by;
+                hi[j] = (_Float16)s;
+                const float rest = s - (float)hi[j];
+                lo[j] = fabsf(s) < 60000.f ? (_Float16)rest : (_Float16)0.f;  // an infinity or NaN has no rest
+            }
+            u32x4 w;
+            __builtin_memcpy(&w, hi, 16);
+            *(u32x4*)(y + t * pitch + c) = w;
+            __builtin_memcpy(&w, lo, 16);
+            *(u32x4*)(y + plane + t * pitch + c) = w;
+        }
+    }
+}
+
+// ---- logits ----
+
+struct LogitArgs {
+    Side w, u;
+    int kts;             // tiles along the columns
+    int tm, tn;          // tiles of classes and rows
+    int classes;         // of this piece
+    long long first;     // the piece's first class
+    long long all;       // classes of the table
+    long long rows;
+    const Scales* scales;
+    const int64_t* target;
+    const uint8_t* live;
+    float* tops;         // forward: [tile of classes][rows] largest logit, and the sum of exponentials relative to it
+    float* sums;
+    float* picked;       // [rows] the target's logit
+    const float* lse;    // backward
+    const float* dloss;
+    const float* dlse;
+    uint16_t* g;         // [rows up to a multiple of 256][ld]
+    long long g_ld, g_plane;
+};
+
+template <typename T>
+__device__ __forceinline__ uint16_t bits16(float v) {
+    return __builtin_bit_cast(uint16_t, (T)v);
+}
+
+// Classes are the rows of the matrix instructions, so that a lane holds 16 * MT classes of one row and reduces them in registers.
+template <typename T, int MW, int NW, int MT, int NT, int PAIRS, bool GRAD>
+__global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
+    typedef Products<T, MW, NW, MT, NT, false, false, PAIRS> P;
+    __shared__ __align__(16) uint16_t lds[P::LDS];
+    int tm, tn;
+    place_tile(blockIdx.x, gridDim.x, a.tm, a.tn, tm, tn);
+    const int m0 = tm * P::BM, n0 = tn * P::BN;
+    P p;
+    p.run(a.w, a.u, m0, n0, 0, a.kts, lds);
+
+    const int wm = P::wave_m(), wn = P::wave_n();
+    const float iu = a.scales ? a.scales->iu : 1.f, iw = a.scales ? a.scales->iw : 1.f;
+    if (a.scales) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p.acc[m][n][i] = p.acc[m][n][i] * iu * iw;
+    }
+    if (!GRAD) {
+        float* const meet = (float*)lds;  // [MW][BN][2]
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int col = wn + n * 32 + P::col_of();
+            const long long t = (long long)n0 + col;
+            const int left = a.classes - (m0 + wm);  // classes that exist from the wave's first on
+            float top = -__builtin_inff();
+            if (left < MT * 32) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (m * 32 + P::row_of(i) >= left) p.acc[m][n][i] = -__builtin_inff();
+            }
+            const long long want = t < a.rows ? a.target[t] - a.first - m0 - wm : -1;
+            const int w = want >= 0 && want < min(left, MT * 32) ? (int)want : -1;
+            if (__builtin_amdgcn_ballot_w64(w >= 0)) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (m * 32 + P::row_of(i) == w) a.picked[t] = p.acc[m][n][i];
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    top = fmaxf(top, p.acc[m][n][i]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top > -__builtin_inff() ? top * kLog2e : 0.f;
+            float sum = 0.f;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(p.acc[m][n][i], kLog2e, -base));
+            sum += __shfl_xor(sum, 32);
+            if ((threadIdx.x & 63) < 32) {
+                meet[((wm / (MT * 32)) * P::BN + col) * 2] = top;
+                meet[((wm / (MT * 32)) * P::BN + col) * 2 + 1] = sum;
+            }
+        }
+        __syncthreads();
+        for (int col = threadIdx.x; col < P::BN; col += P::THREADS) {
+            const long long t = (long long)n0 + col;
+            if (t >= a.rows) break;
+            float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < MW; ++k) top = fmaxf(top, meet[(k * P::BN + col) * 2]);
+#pragma unroll
+            for (int k = 0; k < MW; ++k) {
+                const float mine = meet[(k * P::BN + col) * 2], s = meet[(k * P::BN + col) * 2 + 1];
+                sum += mine > -__builtin_inff() ? s * __builtin_amdgcn_exp2f((mine - top) * kLog2e) : s;
+            }
+            a.tops[tm * a.rows + t] = top;
+            a.sums[tm * a.rows + t] = sum;
+        }
+    } else {
+        const float lift = a.scales ? a.scales->g : 1.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const long long t = (long long)n0 + wn + n * 32 + P::col_of();
+            const bool there = t < a.rows && !(a.live && !a.live[t]);
+            float lse = 0.f, up = 0.f, both = 0.f;
+            long long want = -1;
+            if (there) {
+                lse = a.lse[t];
+                up = a.dloss ? a.dloss[t] : 0.f;
+                both = up + (a.dlse ? a.dlse[t] : 0.f);
+                want = a.target[t];
+                if (want < 0 || want >= a.all) up = both = __builtin_nanf("");
+                want -= a.first + m0 + wm;
+            }
+            const int w = want >= 0 && want < MT * 32 ? (int)want : -1;
+            up *= lift, both *= lift;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint16_t hi[4], lo[4];
+                    const int v0 = m * 32 + P::row_of(4 * q);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float s = p.acc[m][n][4 * q + j] - lse;
+                        const float e = PAIRS > 1 ? expf(s) : __builtin_amdgcn_exp2f(s * kLog2e);
+                        float g = both * e - (v0 + j == w ? up : 0.f);
+                        g = there && m0 + wm + v0 + j < a.classes ? g : 0.f;
+                        hi[j] = bits16<T>(g);
+                        if (PAIRS > 1) lo[j] = bits16<T>(fabsf(g) < 60000.f ? g - (float)__builtin_bit_cast(T, hi[j]) : 0.f);
+                    }
+                    uint16_t* const to = a.g + t * a.g_ld + m0 + wm + v0;
+                    *(u32x2*)to = u32x2{hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16};
+                    if (PAIRS > 1) *(u32x2*)(to + a.g_plane) = u32x2{lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16};
+                }
+        }
+    }
+}
+
+// The tiles of a row: LANES threads to a row.
+template <int LANES>
+__global__ __launch_bounds__(256) void k_loss_join(long long rows, int tiles, int classes, const float* tops, const float* sums, const float* picked,
+                                                   const int64_t* target, const uint8_t* live, float* loss, float* lse) {
+    __shared__ float meet[2][256];
+    constexpr int ROWS = 256 / LANES;
+    const int at = threadIdx.x % ROWS, lane = threadIdx.x / ROWS;
+    const long long t = (long long)blockIdx.x * ROWS + at;
+    float top = -__builtin_inff(), sum = 0.f;
+    if (t < rows) {
+        for (int k = lane; k < tiles; k += LANES) top = fmaxf(top, tops[k * rows + t]);
+        meet[0][threadIdx.x] = top;
+    }
+    __syncthreads();
+    if (t < rows) {
+        for (int k = 0; k < LANES; ++k) top = fmaxf(top, meet[0][k * ROWS + at]);
+        for (int k = lane; k < tiles; k += LANES) {
+            const float mine = tops[k * rows + t], s = sums[k * rows + t];
+            sum += mine > -__builtin_inff() ? s * __builtin_amdgcn_exp2f((mine - top) * kLog2e) : s;
+        }
+        meet[1][threadIdx.x] = sum;
+    }
+    __syncthreads();
+    if (lane || t >= rows) return;
+    for (int k = 1; k < LANES; ++k) sum += meet[1][k * ROWS + at];
+    const bool there = !(live && !live[t]);
+    const float l = there ? top + logf(sum) : 0.f;
+    lse[t] = l;
+    const int64_t w = there ? target[t] : 0;
+    loss[t] = !there ? 0.f : w >= 0 && w < classes ? l - picked[t] : __builtin_nanf("");
+}
+
+// ---- gradients ----
+
+struct GradArgs {
+    Side a, b;
+    int kts, per;        // tiles along the sum, and of a slice
+    int tm, tn;
+    long long rows;      // outputs
+    int cols;
+    void* out;
+    long long ld;
+    float* partial;      // not NULL: [slice][rows][cols] sums, added to where `add`
+    int add;
+    const float* down0;  // factors of an output, or NULL
+    const float* down1;
+};
+
+// du = g W (rows of g, sums of W) and dw = g' u (sums of both).
+template <typename T, typename TO, int MW, int NW, int MT, int NT, bool ASUMS, int PAIRS>
+__global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
+    typedef Products<T, MW, NW, MT, NT, ASUMS, true, PAIRS> P;
+    __shared__ __align__(16) uint16_t lds[P::LDS];
+    int tm, tn;
+    place_tile(blockIdx.x, gridDim.x, a.tm, a.tn, tm, tn);
+    const int kt0 = blockIdx.y * a.per, kt1 = min(a.kts, kt0 + a.per);
+    P p;
+    if (kt0 < kt1) {
+        p.run(a.a, a.b, tm * P::BM, tn * P::BN, kt0, kt1, lds);
+    } else {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p.acc[m][n][i] = 0.f;
+    }
+    const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
+    const long long r0 = (long long)tm * P::BM + P::wave_m();
+    const int c0 = tn * P::BN + P::wave_n() + P::col_of();
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const long long r = r0 + m * 32 + P::row_of(i);
+            if (r >= a.rows) continue;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int c = c0 + n * 32;
+                if (c >= a.cols) continue;
+                if (a.partial) {
+                    float* const to = a.partial + ((long long)blockIdx.y * a.rows + r) * a.cols + c;
+                    *to = p.acc[m][n][i] + (a.add ? *to : 0.f);
+                } else {
+                    ((TO*)a.out)[r * a.ld + c] = (TO)(p.acc[m][n][i] * d0 * d1);
+                }
+            }
+        }
+}
+
+// The slices' sums, one after the other.
+template <typename TO>
+__global__ __launch_bounds__(256) void k_grad_join(const float* partial, int slices, long long rows, int cols, TO* out, long long ld, const float* down0,
+                                                   const float* down1) {
+    const float d0 = down0 ? *down0 : 1.f, d1 = down1 ? *down1 : 1.f;
+    const long long n = rows * cols;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        float s = 0.f;
+        for (int k = 0; k < slices; ++k) s += partial[k * n + i];
+        const long long r = i / cols;
+        out[r * ld + (i - r * cols)] = (TO)(s * d0 * d1);
+    }
+}
+
+template <typename TO>
+__global__ __launch_bounds__(256) void k_zero_rows(TO* out, long long rows, int cols, long long ld) {
+    const long long n = rows * cols;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const long long r = i / cols;
+        out[r * ld + (i - r * cols)] = (TO)0.f;
+    }
+}
+
+// ---- plans ----
+
+// The edge of square tiles and the slices of the sum.
+struct Cut {
+    int edge, slices, per;
+};
+Cut cut_of(long long m, long long n, int kts, int most) {
+    auto tiles = [&](int e) { return ((m + e - 1) / e) * ((n + e - 1) / e); };
+    int edge = 256;
+    if (tiles(256) < 256) edge = 128;
+    if (m <= 64 || n <= 64) edge = 64;
+    long long slices = std::max<long long>(1, 512 / tiles(edge));
+    slices = std::min<long long>({slices, (long long)most, std::max(1, kts / 8)});
+    const int per = (int)((kts + slices - 1) / slices);
+    return {edge, (int)((kts + per - 1) / per), per};
+}
+
+struct LossPlan {
+    bool wide, u_ready, w_ready, scaled;  // 32-bit operands; whether u and W are copied; whether there are scales
+    int pitch, kts;
+    int edge, tiles;                      // of the logits' tiles, tiles of classes
+    int planes;
+    long long rows_up, piece;
+    Cut du, dw;
+    // byte offsets into the workspace
+    size_t maxima, scales, u, w, tops, sums, picked, g, du_sums, dw_sums, bytes;
+};
+
+bool in_place(const void* p, long long stride, int cols, bool wide) { return !wide && cols % PK == 0 && stride % 8 == 0 && stride <= (1 << 22) && ((uintptr_t)p & 15) == 0; }
+
+LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
+    LossPlan p{};
+    p.wide = a.type == IODF_T_F32;
+    p.planes = p.wide ? 2 : 1;
+    p.pitch = (int)up(a.cols, PK);
+    p.kts = p.pitch / PK;
+    p.u_ready = !in_place(a.u, a.u_stride, a.cols, p.wide) || (backward && a.live);
+    p.w_ready = !in_place(a.w, a.w_stride, a.cols, p.wide);
+    p.scaled = p.wide || (backward && a.type == IODF_T_F16);
+    p.rows_up = up(a.rows, 256);
+    auto tiles = [&](int e) { return ((a.rows + e - 1) / e) * ((a.classes + e - 1) / e); };
+    p.edge = a.rows <= 64 ? 64 : tiles(256) >= 256 ? 256 : 128;
+    const int bm = p.edge == 64 ? 128 : p.edge;
+    p.tiles = (a.classes + bm - 1) / bm;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t was = at;
+        at += up(bytes, 256);
+        return was;
+    };
+    if (p.scaled) p.maxima = take(3 * kMaxima * 4), p.scales = take(sizeof(Scales));
+    if (p.u_ready) p.u = take((size_t)p.planes * a.rows * p.pitch * 2);
+    if (p.w_ready) p.w = take((size_t)p.planes * a.classes * p.pitch * 2);
+    if (!backward) {
+        p.tops = take((size_t)p.tiles * a.rows * 4), p.sums = take((size_t)p.tiles * a.rows * 4), p.picked = take((size_t)a.rows * 4);
+    } else if (a.rows) {
+        p.piece = std::max<long long>(256, kPieceBytes / (p.rows_up * 2 * p.planes) / 256 * 256);
+        p.piece = std::min(p.piece, up(a.classes, 256));
+        p.g = take((size_t)p.planes * p.rows_up * p.piece * 2);
+        p.du = cut_of(a.rows, a.cols, (int)(p.piece / PK), 64);
+        p.dw = cut_of(std::min<long long>(p.piece, a.classes), a.cols, (int)((a.rows + PK - 1) / PK), 64);
+        if (a.du && (p.du.slices > 1 || p.piece < a.classes)) p.du_sums = take((size_t)p.du.slices * a.rows * a.cols * 4);
+        if (a.dw && p.dw.slices > 1) p.dw_sums = take((size_t)p.dw.slices * std::min<long long>(p.piece, a.classes) * a.cols * 4);
+    }
+    p.bytes = at;
+    return p;
+}
+
+unsigned blocks_for(long long threads) { return (unsigned)std::max<long long>(1, std::min<long long>((threads + 255) / 256, 1 << 16)); }
+
+template <typename TX>
+void ready(const void* x, long long stride, long long rows, int cols, const LossPlan& p, const uint8_t* live, const float* scale, uint16_t* y, hipStream_t st) {
+    k_ready<TX><<<blocks_for(rows * (p.pitch / 8)), 256, 0, st>>>((const TX*)x, stride, rows, cols, p.pitch, live, scale, y, rows * p.pitch);
+}
+
+template <typename T, int PAIRS, bool GRAD>
+void logits(const LogitArgs& a, int edge, hipStream_t st) {
+    LogitArgs r = a;
+    auto go = [&](auto kernel, int bm, int bn, int threads) {
+        r.tm = (a.classes + bm - 1) / bm, r.tn = (int)((a.rows + bn - 1) / bn);
+        kernel<<<(unsigned)r.tm * r.tn, threads, 0, st>>>(r);
+    };
+    if (edge == 256) go(k_logits<T, 2, 4, 4, 2, PAIRS, GRAD>, 256, 256, 512);
+    else if (edge == 128) go(k_logits<T, 2, 2, 2, 2, PAIRS, GRAD>, 128, 128, 256);
+    else go(k_logits<T, 4, 1, 1, 2, PAIRS, GRAD>, 128, 64, 256);
+}
+
+template <typename T, typename TO, bool ASUMS, int PAIRS>
+void gradient(const GradArgs& a, const Cut& c, hipStream_t st) {
+    GradArgs r = a;
+    r.per = c.per;
+    r.tm = (int)((a.rows + c.edge - 1) / c.edge), r.tn = (a.cols + c.edge - 1) / c.edge;
+    const dim3 grid((unsigned)r.tm * r.tn, c.slices);
+    if (c.edge == 256) k_loss_grad<T, TO, 2, 4, 4, 2, ASUMS, PAIRS><<<grid, 512, 0, st>>>(r);
+    else if (c.edge == 128) k_loss_grad<T, TO, 2, 2, 2, 2, ASUMS, PAIRS><<<grid, 256, 0, st>>>(r);
+    else k_loss_grad<T, TO, 2, 2, 1, 1, ASUMS, PAIRS><<<grid, 256, 0, st>>>(r);
+}
+
+template <typename TO>
+void grad_join(const float* partial, int slices, long long rows, int cols, void* out, long long ld, const float* d0, const float* d1, hipStream_t st) {
+    k_grad_join<TO><<<blocks_for(rows * cols), 256, 0, st>>>(partial, slices, rows, cols, (TO*)out, ld, d0, d1);
+}
+
+// Operands ready, scales; the rest of the arguments of the logits.
+template <typename TX>
+LogitArgs prepared(const iodf_class_loss& a, const LossPlan& p, char* work, bool backward, hipStream_t st) {
+    LogitArgs l{};
+    Scales* const s = p.scaled ? (Scales*)(work + p.scales) : nullptr;
+    if (s) {
+        float* const maxima = (float*)(work + p.maxima);
+        const MaxArgs m{p.wide ? (const float*)a.u : nullptr, p.wide ? (const float*)a.w : nullptr, a.u_stride, a.w_stride, a.rows, a.classes, a.cols,
+                        a.live, backward ? a.dloss : nullptr, backward ? a.dlse : nullptr};
+        k_maxima<<<dim3(kMaxima, 3), 256, 0, st>>>(m, maxima);
+        k_scales<<<1, 256, 0, st>>>(maxima, p.wide, s);
+    }
+    l.u = {(const uint16_t*)a.u, 0, a.u_stride, (int)a.rows, (int)a.rows};
+    l.w = {(const uint16_t*)a.w, 0, a.w_stride, a.classes, a.classes};
+    if (p.u_ready) {
+        uint16_t* const y = (uint16_t*)(work + p.u);
+        ready<TX>(a.u, a.u_stride, a.rows, a.cols, p, a.live, s ? &s->u : nullptr, y, st);
+        l.u.p = y, l.u.ld = p.pitch, l.u.plane = a.rows * p.pitch;
+    }
+    if (p.w_ready) {
+        uint16_t* const y = (uint16_t*)(work + p.w);
+        ready<TX>(a.w, a.w_stride, a.classes, a.cols, p, nullptr, s ? &s->w : nullptr, y, st);
+        l.w.p = y, l.w.ld = p.pitch, l.w.plane = (long long)a.classes * p.pitch;
+    }
+    l.kts = p.kts, l.classes = a.classes, l.all = a.classes, l.rows = a.rows, l.scales = s, l.target = a.target, l.live = a.live;
+    return l;
+}
+
+template <typename TX, typename T, int PAIRS>
+hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
+    const LossPlan p = loss_plan(a, false);
+    LogitArgs l = prepared<TX>(a, p, work, false, st);
+    l.tops = (float*)(work + p.tops), l.sums = (float*)(work + p.sums), l.picked = (float*)(work + p.picked);
+    logits<T, PAIRS, false>(l, p.edge, st);
+    if (a.rows >= 4096) k_loss_join<4><<<(unsigned)((a.rows + 63) / 64), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.tops, l.sums, l.picked, a.target, a.live, a.loss, a.lse);
+    else k_loss_join<64><<<(unsigned)((a.rows + 3) / 4), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.tops, l.sums, l.picked, a.target, a.live, a.loss, a.lse);
+    return hipGetLastError();
+}
+
+template <typename TX, typename T, int PAIRS>
+hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
+    if (a.rows == 0) {
+        k_zero_rows<TX><<<blocks_for((long long)a.classes * a.cols), 256, 0, st>>>((TX*)a.dw, a.classes, a.cols, a.dw_stride);
+        return hipGetLastError();
+    }
+    const LossPlan p = loss_plan(a, true);
+    LogitArgs l = prepared<TX>(a, p, work, true, st);
+    const Scales* const s = l.scales;
+    const Side w = l.w;
+    l.lse = a.lse, l.dloss = a.dloss, l.dlse = a.dlse;
+    l.g = (uint16_t*)(work + p.g), l.g_ld = p.piece, l.g_plane = p.rows_up * p.piece;
+    float* const du_sums = p.du.slices > 1 || p.piece < a.classes ? (float*)(work + p.du_sums) : nullptr;
+    float* const dw_sums = p.dw.slices > 1 ? (float*)(work + p.dw_sums) : nullptr;
+    for (long long v0 = 0; v0 < a.classes; v0 += p.piece) {
+        const int n = (int)std::min<long long>(p.piece, a.classes - v0);
+        l.first = v0, l.classes = n;
+        l.w = w, l.w.p += v0 * w.ld, l.w.extent = l.w.depth = n;
+        logits<T, PAIRS, true>(l, p.edge, st);
+        if (a.du) {
+            GradArgs g{};
+            g.a = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
+            g.b = {l.w.p, w.plane, w.ld, a.cols, n};
+            g.kts = (n + PK - 1) / PK, g.rows = a.rows, g.cols = a.cols, g.out = a.du, g.ld = a.du_stride;
+            g.partial = du_sums, g.add = v0 > 0;
+            if (s) g.down0 = &s->ig, g.down1 = &s->iw;
+            gradient<T, TX, false, PAIRS>(g, p.du, st);
+        }
+        if (a.dw) {
+            GradArgs g{};
+            TX* const out = (TX*)a.dw + v0 * a.dw_stride;
+            g.a = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};
+            g.b = {l.u.p, l.u.plane, l.u.ld, a.cols, (int)a.rows};
+            g.kts = (int)((a.rows + PK - 1) / PK), g.rows = n, g.cols = a.cols, g.out = out, g.ld = a.dw_stride;
+            g.partial = dw_sums;
+            if (s) g.down0 = &s->ig, g.down1 = &s->iu;
+            gradient<T, TX, true, PAIRS>(g, p.dw, st);
+            if (dw_sums) grad_join<TX>(dw_sums, p.dw.slices, n, a.cols, out, a.dw_stride, g.down0, g.down1, st);
+        }
+    }
+    if (a.du && du_sums) grad_join<TX>(du_sums, p.du.slices, a.rows, a.cols, a.du, a.du_stride, s ? &s->ig : nullptr, s ? &s->iw : nullptr, st);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t class_loss_workspace(const iodf_class_loss& a, bool backward) { return loss_plan(a, backward).bytes; }
+
+hipError_t launch_class_loss(const iodf_class_loss& a, void* work, hipStream_t st) {
+    return a.type == IODF_T_F32    ? forward<float, _Float16, 3>(a, (char*)work, st)
+           : a.type == IODF_T_BF16 ? forward<__bf16, __bf16, 1>(a, (char*)work, st)
+                                   : forward<_Float16, _Float16, 1>(a, (char*)work, st);
+}
+
+hipError_t launch_class_loss_backward(const iodf_class_loss& a, void* work, hipStream_t st) {
+    return a.type == IODF_T_F32    ? backward<float, _Float16, 3>(a, (char*)work, st)
+           : a.type == IODF_T_BF16 ? backward<__bf16, __bf16, 1>(a, (char*)work, st)
+                                   : backward<_Float16, _Float16, 1>(a, (char*)work, st);
+}
+
+}  // namespace iodf

@@ -1,0 +1,220 @@
+// Matrix products of 16-bit numbers with 32-bit sums, for the ends of a training step (loss.hip, orth.hip):
+//   acc[m][n] = sum_k A(m, k) B(n, k)
+// A workgroup computes BM x BN outputs. Operands go straight from memory to LDS in tiles of 64 along k, a tile ahead of the products, and
+// each may lie in memory either way round:
+//   rows   [m][k], k consecutive: a lane's fragment (eight k of one m) is one LDS read of sixteen bytes
+//   sums   [k][m], m consecutive: the transposing LDS read takes the fragment out of eight rows
+// so that no operand is ever transposed in memory. A number of more bits than 16 is two parts, high and low (planes of the same
+// layout), and the sum of three products: high high, high low, low high.
+#pragma once
+#include "block_dev.h"
+
+namespace iodf {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int PK = 64;  // of a tile along k
+
+// An operand, its base and leading dimension in elements. Rows (or, of a `sums` operand, columns) past `extent` repeat existing ones: they only reach
+// outputs that nobody stores. Along k a `rows` operand is readable up to a multiple of 64; a `sums` operand repeats its last row past `depth`. What
+// stands there must be zero in one of the operands and finite in the other. Rows start at multiples of 16 bytes.
+struct Side {
+    const uint16_t* p;
+    long long plane;  // from the high parts to the low ones
+    long long ld;
+    int extent, depth;
+};
+
+template <typename T> struct Mma;
+template <> struct Mma<__bf16> {
+    static __device__ __forceinline__ f32x16 go(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mma<_Float16> {
+    static __device__ __forceinline__ f32x16 go(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), c, 0, 0, 0);
+    }
+};
+
+// Sixteen bytes a lane from memory to LDS, lane after lane from `lds` on. Written out because the compiler, where it knows of such a load,
+// waits for all of them before any LDS access that may meet one.
+__device__ __forceinline__ void to_lds16(uint32_t lds, const void* base, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+template <int LEFT>
+__device__ __forceinline__ void wait_vm() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+
+// One operand's way through LDS: W rows (or columns) of a tile, THREADS threads.
+template <int W, int THREADS, bool SUMS>
+struct Lane {
+    static constexpr int LOADS = W * 8 / THREADS;      // of sixteen bytes, a thread and tile
+    static constexpr int PER = W / 8;                  // chunks of a row of a `sums` tile
+    uint32_t off[LOADS];                               // bytes from the tile's corner
+    // `first`: where the workgroup's rows (columns) begin
+    __device__ __forceinline__ void init(const Side& s, int first) {
+        const int tid = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int p = i * THREADS + tid;
+            if (!SUMS) {
+                const int r = p / 8, c = (p & 7) ^ (r & 7), at = min(r, s.extent - 1 - first);
+                off[i] = (uint32_t)(at * s.ld + c * 8) * 2;
+            } else {
+                const int c = chunk(p / PER, p % PER);
+                off[i] = (uint32_t)(first + c * 8 < s.extent ? c * 8 : 0) * 2;
+            }
+        }
+    }
+    // Where chunk c of row r lies, and which chunk lies at place c: 64 bytes further a row, so that the four rows that sixteen lanes read together
+    // cover all banks.
+    static __device__ __forceinline__ int chunk(int r, int c) { return PER >= 16 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); }
+    // tile kt (of the plane `part`) to `lds`
+    __device__ __forceinline__ void start(const Side& s, int first, int part, int kt, uint32_t lds) const {
+        const uint16_t* const base = s.p + part * s.plane + (SUMS ? (long long)kt * PK * s.ld + first : (long long)first * s.ld + kt * PK);
+        const uint32_t at = lds + (threadIdx.x / 64) * 1024;
+        if (!SUMS) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) to_lds16(__builtin_amdgcn_readfirstlane(at + i * THREADS * 16), base, off[i]);
+        } else {
+            const int last = s.depth - 1 - kt * PK;  // rows of the tile past it repeat it
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int r = min((i * THREADS + (int)threadIdx.x) / PER, last);
+                to_lds16(__builtin_amdgcn_readfirstlane(at + i * THREADS * 16), base, off[i] + (uint32_t)(r * s.ld) * 2);
+            }
+        }
+    }
+};
+
+// A wave's fragments of `COUNT` blocks of 32 from row (column) `w0` of the tile on.
+template <int W, int COUNT, bool SUMS>
+struct Frags {
+    uint32_t at[SUMS ? COUNT : 4];  // elements
+    __device__ __forceinline__ void init(int w0) {
+        const int lane = threadIdx.x & 63;
+        if (!SUMS) {
+            const int r = w0 + (lane & 31);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) at[s] = r * PK + (((s * 2 + (lane >> 5)) ^ (r & 7)) * 8);
+        } else {
+            const int r = (lane >> 5) * 8 + ((lane >> 2) & 3), c = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+            for (int b = 0; b < COUNT; ++b) at[b] = r * W + Lane<W, 64, true>::chunk(r, (w0 + b * 32 + c) / 8) * 8 + (c & 7);
+        }
+    }
+    __device__ __forceinline__ void read(const uint16_t* tile, int step, s16x8 (&f)[COUNT]) const {
+#pragma unroll
+        for (int b = 0; b < COUNT; ++b) {
+            if (!SUMS) {
+                f[b] = *(const s16x8*)(tile + at[step] + b * 32 * PK);
+            } else {
+                union { s16x4 h[2]; s16x8 v; } u;
+                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + step * 16 * W));
+                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + (step * 16 + 4) * W));
+                f[b] = u.v;
+            }
+        }
+    }
+};
+
+// MW x NW waves of MT x NT blocks of 32 x 32 outputs.
+template <typename T, int MW, int NW, int MT_, int NT_, bool ASUMS, bool BSUMS, int PAIRS>
+struct Products {
+    static constexpr int MT = MT_, NT = NT_, BM = MW * MT * 32, BN = NW * NT * 32, THREADS = MW * NW * 64;
+    static constexpr int STAGE = (BM + BN) * PK;  // elements of a tile of both operands
+    static constexpr int LDS = 2 * STAGE;         // elements of LDS that run() wants
+    f32x16 acc[MT][NT];
+
+    static __device__ __forceinline__ int wave_m() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW * MT * 32; }
+    static __device__ __forceinline__ int wave_n() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW * NT * 32; }
+    // which output of the wave's a lane holds in acc[m][n][i]: row m * 32 + row_of(i), column n * 32 + col_of()
+    static __device__ __forceinline__ int row_of(int i) { return 8 * (i / 4) + 4 * ((threadIdx.x & 63) >> 5) + i % 4; }
+    static __device__ __forceinline__ int col_of() { return threadIdx.x & 31; }
+
+    // Tiles kt0 .. kt1 - 1 (kt1 > kt0) along k, of outputs from (m0, n0) on. Ends with a barrier: LDS is free then.
+    __device__ __forceinline__ void run(const Side& a, const Side& b, int m0, int n0, int kt0, int kt1, uint16_t* lds) {
+        Lane<BM, THREADS, ASUMS> la;
+        Lane<BN, THREADS, BSUMS> lb;
+        Frags<BM, MT, ASUMS> fa;
+        Frags<BN, NT, BSUMS> fb;
+        la.init(a, m0), lb.init(b, n0);
+        fa.init(wave_m()), fb.init(wave_n());
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.f;
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)lds;
+        const int tiles = (kt1 - kt0) * PAIRS;
+        int pair = 0, kt = kt0;  // of the next tile to load
+        auto start = [&](int buf) {
+            la.start(a, m0, PAIRS > 1 && pair == 2, kt, lds0 + buf * STAGE * 2);
+            lb.start(b, n0, PAIRS > 1 && pair == 1, kt, lds0 + (buf * STAGE + BM * PK) * 2);
+            if (++kt == kt1) kt = kt0, ++pair;
+        };
+        auto meet = [] {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        s16x8 xa[2][MT], xb[2][NT];
+        auto read = [&](int set, int buf, int step) {
+            fb.read(lds + buf * STAGE + BM * PK, step, xb[set]);
+            fa.read(lds + buf * STAGE, step, xa[set]);
+        };
+        auto multiply = [&](int set) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[m][n] = Mma<T>::go(xa[set][m], xb[set][n], acc[m][n]);
+        };
+        start(0);
+        meet();
+        if (tiles > 1) start(1);
+        read(0, 0, 0);
+        auto tile = [&](int t, int buf) {
+            read(1, buf, 1);
+            multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
+            read(0, buf, 2);
+            multiply(1);
+            __builtin_amdgcn_sched_barrier(0);
+            read(1, buf, 3);
+            multiply(0);
+            meet();  // this tile has been read by all, the next one has landed
+            __builtin_amdgcn_sched_barrier(0);
+            if (t + 1 < tiles) {
+                if (t + 2 < tiles) start(buf);
+                read(0, buf ^ 1, 0);
+            }
+            multiply(1);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int t = 0;
+        for (; t + 1 < tiles; t += 2) {
+            tile(t, 0);
+            tile(t + 1, 1);
+        }
+        if (t < tiles) tile(t, 0);
+    }
+};
+
+// Which tile of a grid of tm x tn a workgroup takes. Workgroups go round the eight dies (each with an L2 of its own) in turn; a die gets neighbours,
+// in bands four tiles high, so that a panel of either operand is fetched into as few L2s as may be.
+__device__ __forceinline__ void place_tile(unsigned b, unsigned all, unsigned tm, unsigned tn, int& m, int& n) {
+    const unsigned share = all / 8, l = b < share * 8 ? b % 8 * share + b / 8 : b;
+    const unsigned band = l / (4 * tn), in = l - band * 4 * tn, high = min(4u, tm - band * 4);
+    m = (int)(band * 4 + in % high);
+    n = (int)(in / high);
+}
+
+}  // namespace iodf
