@@ -237,6 +237,9 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
             a.sums[tm * a.rows + t] = sum;
         }
     } else {
+        typedef Staged<P, uint16_t, NW> Out;
+        static_assert((PAIRS > 1 ? 2 : 1) * Out::BYTES <= P::LDS * 2, "g passes through the operands' LDS");
+        char* const low = (char*)lds + Out::BYTES;
         const float lift = a.scales ? a.scales->g : 1.f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -254,6 +257,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
             }
             const int w = want >= 0 && want < MT * 32 ? (int)want : -1;
             up *= lift, both *= lift;
+            if (n) __syncthreads();
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -269,10 +273,18 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                         hi[j] = bits16<T>(g);
                         if (PAIRS > 1) lo[j] = bits16<T>(fabsf(g) < 60000.f ? g - (float)__builtin_bit_cast(T, hi[j]) : 0.f);
                     }
-                    uint16_t* const to = a.g + t * a.g_ld + m0 + wm + v0;
-                    *(u32x2*)to = u32x2{hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16};
-                    if (PAIRS > 1) *(u32x2*)(to + a.g_plane) = u32x2{lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16};
+                    Out::put(lds, m, q, hi);
+                    if (PAIRS > 1) Out::put(low, m, q, lo);
                 }
+            __syncthreads();
+            uint16_t* const g = a.g + n0 * a.g_ld + m0;
+#pragma unroll
+            for (int i = 0; i < Out::PER; ++i) {
+                int row, col;
+                Out::where(i, n, row, col);
+                *(u32x4*)(g + row * a.g_ld + col) = Out::take(lds, i);
+                if (PAIRS > 1) *(u32x4*)(g + row * a.g_ld + col + a.g_plane) = Out::take(low, i);
+            }
         }
     }
 }
@@ -312,23 +324,25 @@ __global__ __launch_bounds__(256) void k_loss_join(long long rows, int tiles, in
 // ---- gradients ----
 
 struct GradArgs {
-    Side a, b;
+    Side a, b;           // the side of the outputs' columns, and of their rows
     int kts, per;        // tiles along the sum, and of a slice
     int tm, tn;
     long long rows;      // outputs
     int cols;
     void* out;
     long long ld;
-    float* partial;      // not NULL: [slice][rows][cols] sums, added to where `add`
+    float* partial;      // not NULL: sums [slice][tile] in the order in which lanes hold them, added to where `add`
     int add;
     const float* down0;  // factors of an output, or NULL
     const float* down1;
 };
 
-// du = g W (rows of g, sums of W) and dw = g' u (sums of both).
-template <typename T, typename TO, int MW, int NW, int MT, int NT, bool ASUMS, int PAIRS>
+// du = g W (sums of W, rows of g) and dw = g' u (sums of both). The outputs' columns are the matrix instructions' rows.
+template <typename T, typename TO, int MW, int NW, int MT, int NT, bool BSUMS, int PAIRS>
 __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
-    typedef Products<T, MW, NW, MT, NT, ASUMS, true, PAIRS> P;
+    typedef Products<T, MW, NW, MT, NT, true, BSUMS, PAIRS> P;
+    typedef Staged<P, float, NW> Out;
+    static_assert(Out::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
     __shared__ __align__(16) uint16_t lds[P::LDS];
     int tm, tn;
     place_tile(blockIdx.x, gridDim.x, a.tm, a.tn, tm, tn);
@@ -344,40 +358,75 @@ __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) p.acc[m][n][i] = 0.f;
     }
-    const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
-    const long long r0 = (long long)tm * P::BM + P::wave_m();
-    const int c0 = tn * P::BN + P::wave_n() + P::col_of();
+    if (a.partial) {
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        f32x4* const to = (f32x4*)a.partial + ((long long)blockIdx.y * gridDim.x + tm * a.tn + tn) * (P::BM * P::BN / 4) +
+                          (threadIdx.x >> 6) * (MT * NT * 256) + (threadIdx.x & 63);
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const long long r = r0 + m * 32 + P::row_of(i);
-            if (r >= a.rows) continue;
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int c = c0 + n * 32;
-                if (c >= a.cols) continue;
-                if (a.partial) {
-                    float* const to = a.partial + ((long long)blockIdx.y * a.rows + r) * a.cols + c;
-                    *to = p.acc[m][n][i] + (a.add ? *to : 0.f);
-                } else {
-                    ((TO*)a.out)[r * a.ld + c] = (TO)(p.acc[m][n][i] * d0 * d1);
+                for (int q = 0; q < 4; ++q) {
+                    f32x4 v{p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
+                    f32x4* const at = to + ((m * NT + n) * 4 + q) * 64;
+                    if (a.add) v += *at;
+                    *at = v;
                 }
+        return;
+    }
+    const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
+    const long long r0 = (long long)tn * P::BN;
+    const int c0 = tm * P::BM;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (n) __syncthreads();
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float v[4] = {p.acc[m][n][4 * q] * d0 * d1, p.acc[m][n][4 * q + 1] * d0 * d1, p.acc[m][n][4 * q + 2] * d0 * d1,
+                                    p.acc[m][n][4 * q + 3] * d0 * d1};
+                Out::put(lds, m, q, v);
             }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < Out::PER; ++i) {
+            int row, col;
+            Out::where(i, n, row, col);
+            if (r0 + row >= a.rows || c0 + col >= a.cols) continue;
+            float v[4];
+            const u32x4 w = Out::take(lds, i);
+            __builtin_memcpy(v, &w, 16);
+            put_quad((TO*)a.out + (r0 + row) * a.ld + c0 + col, a.cols - c0 - col, v);
         }
+    }
 }
 
-// The slices' sums, one after the other.
-template <typename TO>
-__global__ __launch_bounds__(256) void k_grad_join(const float* partial, int slices, long long rows, int cols, TO* out, long long ld, const float* down0,
-                                                   const float* down1) {
-    const float d0 = down0 ? *down0 : 1.f, d1 = down1 ? *down1 : 1.f;
-    const long long n = rows * cols;
+// The slices' sums, one after the other, four neighbours of a row to a thread.
+template <typename TO, int MW, int NW, int MT, int NT>
+__global__ __launch_bounds__(256) void k_grad_join(const GradArgs a, int slices) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    constexpr int BM = MW * MT * 32, BN = NW * NT * 32, PER = BM * BN / 4;
+    const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
+    const long long n = (long long)a.tm * a.tn * PER;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        float s = 0.f;
-        for (int k = 0; k < slices; ++k) s += partial[k * n + i];
-        const long long r = i / cols;
-        out[r * ld + (i - r * cols)] = (TO)(s * d0 * d1);
+        const int tile = (int)(i / PER), in = (int)(i % PER), lane = in & 63, q = in >> 6 & 3, block = in >> 8 & (MT * NT - 1), wave = in / (MT * NT * 256);
+        const long long r = (long long)(tile % a.tn) * BN + wave % NW * (NT * 32) + block % NT * 32 + (lane & 31);
+        const int c = tile / a.tn * BM + wave / NW * (MT * 32) + block / NT * 32 + 8 * q + 4 * (lane >> 5);
+        if (r >= a.rows || c >= a.cols) continue;
+        const f32x4* const from = (const f32x4*)a.partial + i;
+        f32x4 s = 0.f;
+        int k = 0;
+        for (; k + 8 <= slices; k += 8) {
+            f32x4 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = from[(k + u) * n];
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+        for (; k < slices; ++k) s += from[k * n];
+        const float v[4] = {s[0] * d0 * d1, s[1] * d0 * d1, s[2] * d0 * d1, s[3] * d0 * d1};
+        put_quad((TO*)a.out + r * a.ld + c, a.cols - c, v);
     }
 }
 
@@ -451,8 +500,9 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.g = take((size_t)p.planes * p.rows_up * p.piece * 2);
         p.du = cut_of(a.rows, a.cols, (int)(p.piece / PK), 64);
         p.dw = cut_of(std::min<long long>(p.piece, a.classes), a.cols, (int)((a.rows + PK - 1) / PK), 64);
-        if (a.du && (p.du.slices > 1 || p.piece < a.classes)) p.du_sums = take((size_t)p.du.slices * a.rows * a.cols * 4);
-        if (a.dw && p.dw.slices > 1) p.dw_sums = take((size_t)p.dw.slices * std::min<long long>(p.piece, a.classes) * a.cols * 4);
+        auto sums = [&](const Cut& c, long long rows) { return (size_t)c.slices * up(rows, c.edge) * up(a.cols, c.edge) * 4; };
+        if (a.du && (p.du.slices > 1 || p.piece < a.classes)) p.du_sums = take(sums(p.du, a.rows));
+        if (a.dw && p.dw.slices > 1) p.dw_sums = take(sums(p.dw, std::min<long long>(p.piece, a.classes)));
     }
     p.bytes = at;
     return p;
@@ -477,20 +527,24 @@ void logits(const LogitArgs& a, int edge, hipStream_t st) {
     else go(k_logits<T, 4, 1, 1, 2, PAIRS, GRAD>, 128, 64, 256);
 }
 
-template <typename T, typename TO, bool ASUMS, int PAIRS>
-void gradient(const GradArgs& a, const Cut& c, hipStream_t st) {
+// One piece's part of a gradient; `last`: its slices are joined.
+template <typename T, typename TO, bool BSUMS, int PAIRS>
+void gradient(const GradArgs& a, const Cut& c, bool last, hipStream_t st) {
     GradArgs r = a;
     r.per = c.per;
-    r.tm = (int)((a.rows + c.edge - 1) / c.edge), r.tn = (a.cols + c.edge - 1) / c.edge;
+    r.tm = (a.cols + c.edge - 1) / c.edge, r.tn = (int)((a.rows + c.edge - 1) / c.edge);
     const dim3 grid((unsigned)r.tm * r.tn, c.slices);
-    if (c.edge == 256) k_loss_grad<T, TO, 2, 4, 4, 2, ASUMS, PAIRS><<<grid, 512, 0, st>>>(r);
-    else if (c.edge == 128) k_loss_grad<T, TO, 2, 2, 2, 2, ASUMS, PAIRS><<<grid, 256, 0, st>>>(r);
-    else k_loss_grad<T, TO, 2, 2, 1, 1, ASUMS, PAIRS><<<grid, 256, 0, st>>>(r);
-}
-
-template <typename TO>
-void grad_join(const float* partial, int slices, long long rows, int cols, void* out, long long ld, const float* d0, const float* d1, hipStream_t st) {
-    k_grad_join<TO><<<blocks_for(rows * cols), 256, 0, st>>>(partial, slices, rows, cols, (TO*)out, ld, d0, d1);
+    const unsigned join = blocks_for((long long)r.tm * r.tn * c.edge * c.edge / 4);
+    if (c.edge == 256) {
+        k_loss_grad<T, TO, 2, 4, 4, 2, BSUMS, PAIRS><<<grid, 512, 0, st>>>(r);
+        if (r.partial && last) k_grad_join<TO, 2, 4, 4, 2><<<join, 256, 0, st>>>(r, c.slices);
+    } else if (c.edge == 128) {
+        k_loss_grad<T, TO, 2, 2, 2, 2, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
+        if (r.partial && last) k_grad_join<TO, 2, 2, 2, 2><<<join, 256, 0, st>>>(r, c.slices);
+    } else {
+        k_loss_grad<T, TO, 2, 2, 1, 1, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
+        if (r.partial && last) k_grad_join<TO, 2, 2, 1, 1><<<join, 256, 0, st>>>(r, c.slices);
+    }
 }
 
 // Operands ready, scales; the rest of the arguments of the logits.
@@ -553,26 +607,23 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
         logits<T, PAIRS, true>(l, p.edge, st);
         if (a.du) {
             GradArgs g{};
-            g.a = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
-            g.b = {l.w.p, w.plane, w.ld, a.cols, n};
+            g.a = {l.w.p, w.plane, w.ld, a.cols, n};
+            g.b = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
             g.kts = (n + PK - 1) / PK, g.rows = a.rows, g.cols = a.cols, g.out = a.du, g.ld = a.du_stride;
             g.partial = du_sums, g.add = v0 > 0;
             if (s) g.down0 = &s->ig, g.down1 = &s->iw;
-            gradient<T, TX, false, PAIRS>(g, p.du, st);
+            gradient<T, TX, false, PAIRS>(g, p.du, v0 + n == a.classes, st);
         }
         if (a.dw) {
             GradArgs g{};
-            TX* const out = (TX*)a.dw + v0 * a.dw_stride;
-            g.a = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};
-            g.b = {l.u.p, l.u.plane, l.u.ld, a.cols, (int)a.rows};
-            g.kts = (int)((a.rows + PK - 1) / PK), g.rows = n, g.cols = a.cols, g.out = out, g.ld = a.dw_stride;
+            g.a = {l.u.p, l.u.plane, l.u.ld, a.cols, (int)a.rows};
+            g.b = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};
+            g.kts = (int)((a.rows + PK - 1) / PK), g.rows = n, g.cols = a.cols, g.out = (TX*)a.dw + v0 * a.dw_stride, g.ld = a.dw_stride;
             g.partial = dw_sums;
             if (s) g.down0 = &s->ig, g.down1 = &s->iu;
-            gradient<T, TX, true, PAIRS>(g, p.dw, st);
-            if (dw_sums) grad_join<TX>(dw_sums, p.dw.slices, n, a.cols, out, a.dw_stride, g.down0, g.down1, st);
+            gradient<T, TX, true, PAIRS>(g, p.dw, true, st);
         }
     }
-    if (a.du && du_sums) grad_join<TX>(du_sums, p.du.slices, a.rows, a.cols, a.du, a.du_stride, s ? &s->ig : nullptr, s ? &s->iw : nullptr, st);
     return hipGetLastError();
 }
 

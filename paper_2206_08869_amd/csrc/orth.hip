@@ -20,7 +20,7 @@ namespace iodf {
 
 namespace {
 
-constexpr int kNormBlocks = 256;  // partial sums of squares of a matrix
+constexpr int kNormBlocks = 1024;  // partial sums of squares of a matrix, at most
 
 inline long long up(long long n, long long d) { return (n + d - 1) / d * d; }
 
@@ -43,32 +43,47 @@ struct Shape {
     int count, rows, cols, rp, cp, s, sp;  // rp, cp, sp: rounded up to 64; s the shorter side
 };
 
-// What goes into the norm and then into X: the gradient, or the momentum's view of it. `first`: the momentum is moved on.
-template <typename TG, bool MUON>
-__device__ __forceinline__ float taken(const Source& src, int k, long long r, int c, int cols, bool first) {
-    if (!MUON) return (float)((const TG*)src.g[0] + k * src.batch + r * src.stride)[c];
-    const float g = (float)((const TG*)src.g[k] + r * src.stride)[c];
-    float* const m = src.m[k] + r * cols + c;
-    float v = *m;
-    if (first) *m = v = fmaf(src.beta, v, g);
-    return src.nesterov ? fmaf(src.beta, v, g) : v;
+// What goes into the norm and then into X, eight neighbours of a row: the gradient, or the momentum's view of it. `first`: the momentum is moved on.
+template <typename TG, bool MUON, bool FIRST>
+__device__ __forceinline__ void taken(const Source& src, int k, int r, int c, int cols, float (&v)[8]) {
+    const int n = cols - c;
+    const TG* const g = (MUON ? (const TG*)src.g[k] : (const TG*)src.g[0] + k * src.batch) + r * src.stride + c;
+    load8(g, n, v);
+    if (!MUON) return;
+    float* const m = src.m[k] + (long long)r * cols + c;
+    float was[8];
+    load8(m, n, was);
+    if (FIRST) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) was[j] = fmaf(src.beta, was[j], v[j]);
+        store8(m, n, was);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = src.nesterov ? fmaf(src.beta, was[j], v[j]) : was[j];
+}
+
+// The sum over 256 threads, in each of them.
+__device__ __forceinline__ double block_sum(double s, double* meet) {
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
+    if ((threadIdx.x & 63) == 0) meet[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return (meet[0] + meet[1]) + (meet[2] + meet[3]);
 }
 
 template <typename TG, bool MUON>
 __global__ __launch_bounds__(256) void k_orth_norm(const Source src, const Shape z, double* sums) {
     __shared__ double meet[4];
-    const int k = blockIdx.y;
+    const int k = blockIdx.y, per = (z.cols + 7) / 8;
     double s = 0.0;
-    for (long long r = blockIdx.x; r < z.rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < z.cols; c += 256) {
-            const double v = taken<TG, MUON>(src, k, r, c, z.cols, true);
-            s += v * v;
-        }
+    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < (unsigned)z.rows * per; i += gridDim.x * 256) {
+        float v[8];
+        taken<TG, MUON, true>(src, k, i / per, i % per * 8, z.cols, v);
 #pragma unroll
-    for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
-    if ((threadIdx.x & 63) == 0) meet[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) sums[k * kNormBlocks + blockIdx.x] = (meet[0] + meet[1]) + (meet[2] + meet[3]);
+        for (int j = 0; j < 8; ++j) s += (double)v[j] * v[j];
+    }
+    s = block_sum(s, meet);
+    if (threadIdx.x == 0) sums[k * gridDim.x + blockIdx.x] = s;
 }
 
 __device__ __forceinline__ void two_parts(float v, _Float16& hi, _Float16& lo) {
@@ -78,22 +93,26 @@ __device__ __forceinline__ void two_parts(float v, _Float16& hi, _Float16& lo) {
 
 // D / (norm + eps), times 2^x_exp, in two parts, with zeros around it.
 template <typename TG, bool MUON>
-__global__ __launch_bounds__(256) void k_orth_start(const Source src, const Shape z, const double* sums, float eps, float lift, _Float16* x, long long plane) {
+__global__ __launch_bounds__(256) void k_orth_start(const Source src, const Shape z, const double* sums, int parts, float eps, float lift, _Float16* x,
+                                                    long long plane) {
     __shared__ double meet[4];
-    const int k = blockIdx.y;
-    double s = threadIdx.x < kNormBlocks ? sums[k * kNormBlocks + threadIdx.x] : 0.0;
+    const int k = blockIdx.y, per = z.cp / 8;
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 256) s += sums[k * parts + i];
+    const double by = (double)lift / (sqrt(block_sum(s, meet)) + (double)eps);
+    x += k * (long long)z.rp * z.cp;
+    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < (unsigned)z.rp * per; i += gridDim.x * 256) {
+        const int r = i / per, c = i % per * 8;
+        float v[8] = {};
+        if (r < z.rows && c < z.cols) taken<TG, MUON, false>(src, k, r, c, z.cols, v);
+        _Float16 hi[8], lo[8];
 #pragma unroll
-    for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
-    if ((threadIdx.x & 63) == 0) meet[threadIdx.x >> 6] = s;
-    __syncthreads();
-    const double by = (double)lift / (sqrt((meet[0] + meet[1]) + (meet[2] + meet[3])) + (double)eps);
-    const long long n = (long long)z.rp * z.cp;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        const int r = (int)(i / z.cp), c = (int)(i - (long long)r * z.cp);
-        _Float16 hi = (_Float16)0.f, lo = (_Float16)0.f;
-        if (r < z.rows && c < z.cols) two_parts((float)(taken<TG, MUON>(src, k, r, c, z.cols, false) * by), hi, lo);
-        x[k * n + i] = hi;
-        x[plane + k * n + i] = lo;
+        for (int j = 0; j < 8; ++j) two_parts(c + j < z.cols ? (float)(v[j] * by) : 0.f, hi[j], lo[j]);
+        u32x4 w;
+        __builtin_memcpy(&w, hi, 16);
+        *(u32x4*)(x + i * 8ll) = w;
+        __builtin_memcpy(&w, lo, 16);
+        *(u32x4*)(x + plane + i * 8ll) = w;
     }
 }
 
@@ -149,44 +168,91 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
     const _Float16* const o = (const _Float16*)x.p;
     float* const d = a.d + (long long)k * a.sp;
     float* const e = a.e + (long long)k * a.sp;
-    const int r0 = ti * P::BM + P::wave_m(), c0 = tj * P::BN + P::wave_n() + P::col_of();
+    // four neighbours of row r, from sums in LDS
+    struct Four {
+        float sum[4], was[4], dr, dc[4];
+        int r, c;
+    };
+    auto fetch = [&](Four& f, int r, int c, u32x4 w) {
+        __builtin_memcpy(f.sum, &w, 16);
+        f.r = r, f.c = c;
+        if (SECOND && r < a.sp && c < a.sp) {
+            load4<PAIRS>(o + (long long)r * a.sp + c, x.plane, f.was);
+            f.dr = d[r];
+            __builtin_memcpy(f.dc, d + c, 16);
+        }
+    };
+    auto finish = [&](const Four& f) {
+        if (f.r >= a.sp || f.c >= a.sp) return;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float sum = f.sum[j] * a.down;
+            const bool diagonal = f.r == f.c + j;
+            if (!SECOND) {
+                if (diagonal) d[f.r] = sum;
+                v[j] = sum * a.lift;
+            } else {
+                const float ov = f.was[j] * a.unlift;
+                if (diagonal) e[f.r] = fmaf(a.c, fmaf(f.dr, f.dr, sum), a.b * f.dr);
+                v[j] = fmaf(a.c, fmaf(f.dr + f.dc[j], ov, sum), a.b * ov) * a.lift;
+            }
+            if (diagonal) v[j] = 0.f;
+        }
+        store4<PAIRS>(out + (long long)f.r * a.sp + f.c, a.plane, v);
+    };
+    typedef Staged<P, float, NW> Out;
+    typedef StagedAcross<P, MW> Mirror;
+    static_assert(Out::BYTES <= P::LDS * 2 && Mirror::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
+    constexpr int AT_ONCE = 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int c = c0 + n * 32;
-        if (c >= a.sp) continue;
-        const float dc = SECOND ? d[c] : 0.f;
+        if (n) __syncthreads();
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int r = r0 + m * 32 + P::row_of(4 * q);
-                if (r >= a.sp) continue;
-                float v[4], was[4];
-                if (SECOND) load4<PAIRS>(o + (long long)c * a.sp + r, x.plane, was);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float sum = p.acc[m][n][4 * q + j] * a.down;
-                    if (!SECOND) {
-                        if (r + j == c) d[c] = sum;
-                        v[j] = sum * a.lift;
-                    } else {
-                        const float ov = was[j] * a.unlift;
-                        if (r + j == c) e[c] = fmaf(a.c, fmaf(dc, dc, sum), a.b * dc);
-                        v[j] = fmaf(a.c, fmaf(dc + d[r + j], ov, sum), a.b * ov) * a.lift;
-                    }
-                    if (r + j == c) v[j] = 0.f;
-                }
-                store4<PAIRS>(out + (long long)c * a.sp + r, a.plane, v);
-                if (ti != tj) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        _Float16 hi, lo;
-                        two_parts(v[j], hi, lo);
-                        out[(long long)(r + j) * a.sp + c] = hi;
-                        if (PAIRS > 1) out[a.plane + (long long)(r + j) * a.sp + c] = lo;
-                    }
-                }
+                const float v[4] = {p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
+                Out::put(lds, m, q, v);
             }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < Out::PER; i += AT_ONCE) {
+            Four f[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                int row, col;
+                Out::where(i + u, n, row, col);
+                fetch(f[u], tj * P::BN + row, ti * P::BM + col, Out::take(lds, i + u));
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) finish(f[u]);
+        }
+    }
+    if (ti == tj) return;  // symmetric: all of it has been stored
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float v[4] = {p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
+                Mirror::put(lds, n, q, v);
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < Mirror::PER; i += AT_ONCE) {
+            Four f[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                int row, col;
+                Mirror::where(i + u, m, row, col);
+                fetch(f[u], ti * P::BM + row, tj * P::BN + col, Mirror::take(lds, i + u));
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) finish(f[u]);
+        }
     }
 }
 
@@ -204,11 +270,15 @@ struct ApplyArgs {
 };
 
 template <typename TO>
-__device__ __forceinline__ void deliver(const Target& t, int k, int r, int c, int cols, const float (&v)[4]) {
+__device__ __forceinline__ void deliver(const Target& t, int k, int r, int c, int n, float (&v)[4]) {
     TO* const to = (t.batch ? (TO*)t.w[0] + k * t.batch : (TO*)t.w[k]) + r * t.stride + c;
+    if (t.update) {
+        float was[4];
+        get_quad(to, n, was);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (c + j < cols) to[j] = (TO)(t.update ? fmaf(t.keep, (float)to[j], t.by * v[j]) : v[j]);
+        for (int j = 0; j < 4; ++j) v[j] = fmaf(t.keep, was[j], t.by * v[j]);
+    }
+    put_quad(to, n, v);
 }
 
 // (a + e) X + B X: columns of X are the rows of the matrix instructions, so that a lane holds four neighbours of a row.
@@ -227,34 +297,56 @@ __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const
 
     const _Float16* const was = (const _Float16*)x.p;
     const float* const e = a.e + (long long)k * a.z.sp;
-    const int c0 = tm * P::BM + P::wave_m(), r0 = tn * P::BN + P::wave_n() + P::col_of();
+    const int rows = a.to ? a.z.rp : a.z.rows, cols = a.to ? a.z.cp : a.z.cols;
+    _Float16* const to = a.to + k * a.x_batch;
+    typedef Staged<P, float, NW> Out;
+    static_assert(Out::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
+    constexpr int AT_ONCE = 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int r = r0 + n * 32;
-        if (r >= (a.to ? a.z.rp : a.z.rows)) continue;
+        if (n) __syncthreads();
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int c = c0 + m * 32 + P::row_of(4 * q);
-                if (c >= (a.to ? a.z.cp : a.z.cols)) continue;
-                float v[4];
-                load4<2>(was + (long long)r * a.z.cp + c, x.plane, v);
+                const float v[4] = {p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
+                Out::put(lds, m, q, v);
+            }
+        __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    v[j] = fmaf(a.a + e[TALL ? c + j : r], v[j] * a.unlift, p.acc[m][n][4 * q + j] * a.down);
+        for (int i = 0; i < Out::PER; i += AT_ONCE) {
+            float x0[AT_ONCE][4], e0[AT_ONCE][4];
+            int r[AT_ONCE], c[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                Out::where(i + u, n, r[u], c[u]);
+                r[u] += tn * P::BN, c[u] += tm * P::BM;
+                if (r[u] >= rows || c[u] >= cols) continue;
+                load4<2>(was + (long long)r[u] * a.z.cp + c[u], x.plane, x0[u]);
+                if (TALL) __builtin_memcpy(e0[u], e + c[u], 16);
+                else e0[u][0] = e0[u][1] = e0[u][2] = e0[u][3] = e[r[u]];
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (r[u] >= rows || c[u] >= cols) continue;
+                float v[4];
+                const u32x4 w = Out::take(lds, i + u);
+                __builtin_memcpy(v, &w, 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = fmaf(a.a + e0[u][j], x0[u][j] * a.unlift, v[j] * a.down);
                 if (a.to) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] *= a.lift;
-                    store4<2>(a.to + k * a.x_batch + (long long)r * a.z.cp + c, a.plane, v);
+                    store4<2>(to + (long long)r[u] * a.z.cp + c[u], a.plane, v);
                 } else if (type == IODF_T_F32) {
-                    deliver<float>(target, k, r, c, a.z.cols, v);
+                    deliver<float>(target, k, r[u], c[u], cols - c[u], v);
                 } else if (type == IODF_T_BF16) {
-                    deliver<__bf16>(target, k, r, c, a.z.cols, v);
+                    deliver<__bf16>(target, k, r[u], c[u], cols - c[u], v);
                 } else {
-                    deliver<_Float16>(target, k, r, c, a.z.cols, v);
+                    deliver<_Float16>(target, k, r[u], c[u], cols - c[u], v);
                 }
             }
+        }
     }
 }
 
@@ -262,6 +354,7 @@ struct OrthPlan {
     Shape z;
     bool tall, parts;          // parts: three products
     int square_edge, apply_edge;
+    int parts_of_norm;
     size_t sums, x0, x1, o, b, d, e, bytes;
 };
 
@@ -283,7 +376,8 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
         return was;
     };
     const size_t x = (size_t)count * p.z.rp * p.z.cp * 2 * 2, s = (size_t)count * p.z.sp * p.z.sp * 2 * (p.parts ? 2 : 1);
-    p.sums = take((size_t)count * kNormBlocks * 8);
+    p.parts_of_norm = (int)std::max<long long>(1, std::min<long long>({kNormBlocks, 2048 / std::max<long long>(1, count), ((long long)rows * ((cols + 7) / 8) + 255) / 256}));
+    p.sums = take((size_t)count * p.parts_of_norm * 8);
     p.x0 = take(x), p.x1 = take(x), p.o = take(s), p.b = take(s);
     p.d = take((size_t)count * p.z.sp * 4), p.e = take((size_t)count * p.z.sp * 4);
     p.bytes = at;
@@ -321,11 +415,11 @@ void begin(const Source& src, int type, const OrthPlan& p, float eps, float lift
     double* const sums = (double*)(work + p.sums);
     _Float16* const x = (_Float16*)(work + p.x0);
     const long long n = (long long)p.z.rp * p.z.cp, plane = n * p.z.count;
-    const dim3 sum_grid(kNormBlocks, p.z.count), grid((unsigned)std::min<long long>((n + 255) / 256, 4096), p.z.count);
+    const dim3 sum_grid(p.parts_of_norm, p.z.count), grid((unsigned)std::min<long long>((n / 8 + 255) / 256, 2048), p.z.count);
     auto go = [&](auto t) {
         typedef decltype(t) TG;
         k_orth_norm<TG, MUON><<<sum_grid, 256, 0, st>>>(src, p.z, sums);
-        k_orth_start<TG, MUON><<<grid, 256, 0, st>>>(src, p.z, sums, eps, lift, x, plane);
+        k_orth_start<TG, MUON><<<grid, 256, 0, st>>>(src, p.z, sums, p.parts_of_norm, eps, lift, x, plane);
     };
     if (type == IODF_T_F32) go(0.f);
     else if (type == IODF_T_BF16) go((__bf16)0.f);

@@ -57,7 +57,8 @@ template <int W, int THREADS, bool SUMS>
 struct Lane {
     static constexpr int LOADS = W * 8 / THREADS;      // of sixteen bytes, a thread and tile
     static constexpr int PER = W / 8;                  // chunks of a row of a `sums` tile
-    uint32_t off[LOADS];                               // bytes from the tile's corner
+    uint32_t off[LOADS];                               // bytes from the tile's corner, of a `sums` tile from the row's start
+    uint32_t ld;
     // `first`: where the workgroup's rows (columns) begin
     __device__ __forceinline__ void init(const Side& s, int first) {
         const int tid = threadIdx.x;
@@ -70,6 +71,7 @@ struct Lane {
             } else {
                 const int c = chunk(p / PER, p % PER);
                 off[i] = (uint32_t)(first + c * 8 < s.extent ? c * 8 : 0) * 2;
+                ld = (uint32_t)s.ld * 2;
             }
         }
     }
@@ -84,11 +86,11 @@ struct Lane {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) to_lds16(__builtin_amdgcn_readfirstlane(at + i * THREADS * 16), base, off[i]);
         } else {
-            const int last = s.depth - 1 - kt * PK;  // rows of the tile past it repeat it
+            const unsigned last = s.depth - 1 - kt * PK;  // rows of the tile past it repeat it
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                const int r = min((i * THREADS + (int)threadIdx.x) / PER, last);
-                to_lds16(__builtin_amdgcn_readfirstlane(at + i * THREADS * 16), base, off[i] + (uint32_t)(r * s.ld) * 2);
+                const unsigned r = min((i * THREADS + threadIdx.x) / PER, last);
+                to_lds16(__builtin_amdgcn_readfirstlane(at + i * THREADS * 16), base, __umul24(r, ld) + off[i]);
             }
         }
     }
@@ -207,6 +209,87 @@ struct Products {
         if (t < tiles) tile(t, 0);
     }
 };
+
+// A workgroup's outputs on their way to memory: what lanes hold as four neighbours of a row here and there goes through LDS and comes out as whole rows, sixteen
+// bytes to a lane. Output rows are the products' columns n, output columns their rows m. Block column n of all waves at a time: NW * 32 rows of BM.
+// Chunks of sixteen bytes are moved about by their row, so that the 32 rows that a wave writes together cover all banks.
+template <class P, typename E, int NW>
+struct Staged {
+    static constexpr int ROWS = NW * 32, CHUNKS = P::BM * (int)sizeof(E) / 16, PER = ROWS * CHUNKS / P::THREADS, OF = 16 / (int)sizeof(E);
+    static constexpr int BYTES = ROWS * CHUNKS * 16;
+    static __device__ __forceinline__ void put(void* lds, int m, int q, const E (&v)[4]) {
+        const int row = P::wave_n() / P::NT + P::col_of(), c = P::wave_m() + m * 32 + P::row_of(4 * q);
+        __builtin_memcpy((char*)lds + (row * CHUNKS + ((c / OF) ^ (row & (CHUNKS - 1) & 31))) * 16 + c % OF * sizeof(E), v, 4 * sizeof(E));
+    }
+    // chunk i of the thread's: its row and first column among the workgroup's outputs, and what it holds
+    static __device__ __forceinline__ void where(int i, int n, int& row, int& col) {
+        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
+        row = (r / 32) * (P::NT * 32) + n * 32 + r % 32;
+        col = k % CHUNKS * OF;
+    }
+    static __device__ __forceinline__ u32x4 take(const void* lds, int i) {
+        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
+        return *(const u32x4*)((const char*)lds + (r * CHUNKS + ((k % CHUNKS) ^ (r & (CHUNKS - 1) & 31))) * 16);
+    }
+};
+
+// The same for the mirror image: output rows are the products' rows m, output columns their columns n. Block row m of all waves at a time.
+template <class P, int MW>
+struct StagedAcross {
+    static constexpr int ROWS = MW * 32, CHUNKS = P::BN / 4, PER = ROWS * CHUNKS / P::THREADS, BYTES = ROWS * CHUNKS * 16;
+    static __device__ __forceinline__ void put(void* lds, int n, int q, const float (&v)[4]) {
+        const int row = P::wave_m() / P::MT + P::row_of(4 * q), c = P::wave_n() + n * 32 + P::col_of();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ((float*)lds)[((row + j) * CHUNKS + ((c / 4) ^ ((row + j) & (CHUNKS - 1) & 31))) * 4 + c % 4] = v[j];
+    }
+    static __device__ __forceinline__ void where(int i, int m, int& row, int& col) {
+        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
+        row = (r / 32) * (P::MT * 32) + m * 32 + r % 32;
+        col = k % CHUNKS * 4;
+    }
+    static __device__ __forceinline__ u32x4 take(const void* lds, int i) {
+        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
+        return *(const u32x4*)((const char*)lds + (r * CHUNKS + ((k % CHUNKS) ^ (r & (CHUNKS - 1) & 31))) * 16);
+    }
+};
+
+// Four neighbours of a row, of which n exist, at any element's address.
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+template <typename T>
+__device__ __forceinline__ void put_quad(T* to, int n, const float (&v)[4]) {
+    T t[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t[j] = (T)v[j];
+    if (n < 4) {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (j < n) to[j] = t[j];
+    } else if (sizeof(T) == 4) {
+        u32x4 w;
+        __builtin_memcpy(&w, t, 4 * sizeof(T));
+        *(u32x4_any*)to = w;
+    } else {
+        u32x2 w;
+        __builtin_memcpy(&w, t, 4 * sizeof(T));
+        *(u32x2_any*)to = w;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void get_quad(const T* from, int n, float (&v)[4]) {
+    T t[4];
+    if (n < 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = j < n ? from[j] : (T)0.f;
+    } else if (sizeof(T) == 4) {
+        const u32x4 w = *(const u32x4_any*)from;
+        __builtin_memcpy(t, &w, 4 * sizeof(T));
+    } else {
+        const u32x2 w = *(const u32x2_any*)from;
+        __builtin_memcpy(t, &w, 4 * sizeof(T));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = (float)t[j];
+}
 
 // Which tile of a grid of tm x tn a workgroup takes. Workgroups go round the eight dies (each with an L2 of its own) in turn; a die gets neighbours,
 // in bands four tiles high, so that a panel of either operand is fetched into as few L2s as may be.
