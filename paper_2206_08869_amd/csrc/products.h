@@ -66,7 +66,7 @@ struct Lane {
         for (int i = 0; i < LOADS; ++i) {
             const int p = i * THREADS + tid;
             if (!SUMS) {
-                const int r = p / 8, c = (p & 7) ^ (r & 7), at = min(r, s.extent - 1 - first);
+                const int r = p / 8, c = (p & 7) ^ (r >> 1 & 7), at = min(r, s.extent - 1 - first);
                 off[i] = (uint32_t)(at * s.ld + c * 8) * 2;
             } else {
                 const int c = chunk(p / PER, p % PER);
@@ -105,7 +105,7 @@ struct Frags {
         if (!SUMS) {
             const int r = w0 + (lane & 31);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) at[s] = r * PK + (((s * 2 + (lane >> 5)) ^ (r & 7)) * 8);
+            for (int s = 0; s < 4; ++s) at[s] = r * PK + (((s * 2 + (lane >> 5)) ^ (r >> 1 & 7)) * 8);
         } else {
             const int r = (lane >> 5) * 8 + ((lane >> 2) & 3), c = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
