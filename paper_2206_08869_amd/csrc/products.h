@@ -7,6 +7,8 @@
 // so that no operand is ever transposed in memory. A number of more bits than 16 is two parts, high and low (planes of the same
 // layout), and the sum of three products: high high, high low, low high.
 #pragma once
+#include <type_traits>
+
 #include "block_dev.h"
 
 namespace iodf {
@@ -57,8 +59,7 @@ template <int W, int THREADS, bool SUMS>
 struct Lane {
     static constexpr int LOADS = W * 8 / THREADS;      // of sixteen bytes, a thread and tile
     static constexpr int PER = W / 8;                  // chunks of a row of a `sums` tile
-    uint32_t off[LOADS];                               // bytes from the tile's corner, of a `sums` tile from the row's start
-    uint32_t ld;
+    uint32_t off[LOADS], ld;                           // bytes from the tile's corner (of a `sums` tile from the row's start), from row to row
     // `first`: where the workgroup's rows (columns) begin
     __device__ __forceinline__ void init(const Side& s, int first) {
         const int tid = threadIdx.x;
@@ -70,29 +71,21 @@ struct Lane {
                 off[i] = (uint32_t)(at * s.ld + c * 8) * 2;
             } else {
                 const int c = chunk(p / PER, p % PER);
-                off[i] = (uint32_t)(first + c * 8 < s.extent ? c * 8 : 0) * 2;
                 ld = (uint32_t)s.ld * 2;
+                off[i] = (uint32_t)(first + c * 8 < s.extent ? c * 8 : 0) * 2;
             }
         }
     }
     // Where chunk c of row r lies, and which chunk lies at place c: 64 bytes further a row, so that the four rows that sixteen lanes read together
     // cover all banks.
     static __device__ __forceinline__ int chunk(int r, int c) { return PER >= 16 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); }
-    // tile kt (of the plane `part`) to `lds`
-    __device__ __forceinline__ void start(const Side& s, int first, int part, int kt, uint32_t lds) const {
-        const uint16_t* const base = s.p + part * s.plane + (SUMS ? (long long)kt * PK * s.ld + first : (long long)first * s.ld + kt * PK);
-        const uint32_t at = lds + (threadIdx.x / 64) * 1024;
-        if (!SUMS) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) to_lds16(__builtin_amdgcn_readfirstlane(at + i * THREADS * 16), base, off[i]);
-        } else {
-            const unsigned last = s.depth - 1 - kt * PK;  // rows of the tile past it repeat it
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const unsigned r = min((i * THREADS + threadIdx.x) / PER, last);
-                to_lds16(__builtin_amdgcn_readfirstlane(at + i * THREADS * 16), base, __umul24(r, ld) + off[i]);
-            }
-        }
+    // tile kt (of the plane `part`): its loads i0 .. i1 - 1, to `lds`, this wave's place in the tile
+    static __device__ __forceinline__ const uint16_t* corner(const Side& s, int first, int part, int kt) {
+        return s.p + part * s.plane + (SUMS ? (long long)kt * PK * s.ld + first : (long long)first * s.ld + kt * PK);
+    }
+    // `last`: the tile's last row that exists along k; rows past it repeat it
+    __device__ __forceinline__ void start(const uint16_t* corner, unsigned last, uint32_t lds, int i) const {
+        to_lds16(lds + i * THREADS * 16, corner, SUMS ? __umul24(min((i * THREADS + threadIdx.x) / PER, last), ld) + off[i] : off[i]);
     }
 };
 
@@ -112,18 +105,12 @@ struct Frags {
             for (int b = 0; b < COUNT; ++b) at[b] = r * W + Lane<W, 64, true>::chunk(r, (w0 + b * 32 + c) / 8) * 8 + (c & 7);
         }
     }
-    __device__ __forceinline__ void read(const uint16_t* tile, int step, s16x8 (&f)[COUNT]) const {
-#pragma unroll
-        for (int b = 0; b < COUNT; ++b) {
-            if (!SUMS) {
-                f[b] = *(const s16x8*)(tile + at[step] + b * 32 * PK);
-            } else {
-                union { s16x4 h[2]; s16x8 v; } u;
-                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + step * 16 * W));
-                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + (step * 16 + 4) * W));
-                f[b] = u.v;
-            }
-        }
+    __device__ __forceinline__ s16x8 read(const uint16_t* tile, int step, int b) const {
+        if (!SUMS) return *(const s16x8*)(tile + at[step] + b * 32 * PK);
+        union { s16x4 h[2]; s16x8 v; } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + step * 16 * W));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + (step * 16 + 4) * W));
+        return u.v;
     }
 };
 
@@ -155,58 +142,86 @@ struct Products {
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.f;
-        const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)lds;
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)lds +
+                              __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
         const int tiles = (kt1 - kt0) * PAIRS;
         int pair = 0, kt = kt0;  // of the next tile to load
-        auto start = [&](int buf) {
-            la.start(a, m0, PAIRS > 1 && pair == 2, kt, lds0 + buf * STAGE * 2);
-            lb.start(b, n0, PAIRS > 1 && pair == 1, kt, lds0 + (buf * STAGE + BM * PK) * 2);
+        const uint16_t *ca, *cb;
+        unsigned left_a, left_b;
+        auto next = [&] {
+            ca = Lane<BM, THREADS, ASUMS>::corner(a, m0, PAIRS > 1 && pair == 2, kt);
+            cb = Lane<BN, THREADS, BSUMS>::corner(b, n0, PAIRS > 1 && pair == 1, kt);
+            left_a = a.depth - 1 - kt * PK, left_b = b.depth - 1 - kt * PK;
             if (++kt == kt1) kt = kt0, ++pair;
         };
+        // loads i0 .. i1 - 1 of the tile's, of both operands; buf: where in LDS (elements) it goes
+        auto start = [&](int buf, int i0, int i1) {
+#pragma unroll
+            for (int i = i0; i < i1; ++i) {
+                if (i < la.LOADS) la.start(ca, left_a, lds0 + buf * 2, i);
+                else lb.start(cb, left_b, lds0 + (buf + BM * PK) * 2, i - la.LOADS);
+            }
+        };
+        constexpr int LOADS = Lane<BM, THREADS, ASUMS>::LOADS + Lane<BN, THREADS, BSUMS>::LOADS;
         auto meet = [] {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
+        // Fragments of the next step are read while this one's are multiplied: a step is MT groups of NT products, with reads (and, once a tile, the loads
+        // of the tile after the next) dealt out between them. Left to itself the compiler gathers reads just before their products.
         s16x8 xa[2][MT], xb[2][NT];
-        auto read = [&](int set, int buf, int step) {
-            fb.read(lds + buf * STAGE + BM * PK, step, xb[set]);
-            fa.read(lds + buf * STAGE, step, xa[set]);
-        };
-        auto multiply = [&](int set) {
+        auto group = [&](int set, int m) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) acc[m][n] = Mma<T>::go(xa[set][m], xb[set][n], acc[m][n]);
+            for (int n = 0; n < NT; ++n) acc[m][n] = Mma<T>::go(xa[set][m], xb[set][n], acc[m][n]);
         };
-        start(0);
-        meet();
-        if (tiles > 1) start(1);
-        read(0, 0, 0);
-        auto tile = [&](int t, int buf) {
-            read(1, buf, 1);
-            multiply(0);
-            __builtin_amdgcn_sched_barrier(0);
-            read(0, buf, 2);
-            multiply(1);
-            __builtin_amdgcn_sched_barrier(0);
-            read(1, buf, 3);
-            multiply(0);
-            meet();  // this tile has been read by all, the next one has landed
-            __builtin_amdgcn_sched_barrier(0);
-            if (t + 1 < tiles) {
-                if (t + 2 < tiles) start(buf);
-                read(0, buf ^ 1, 0);
+        constexpr int READS = MT + NT, BUSY = MT > 1 ? MT - 1 : 1, EACH = (READS + BUSY - 1) / BUSY;  // of a group; the last one has none
+        auto reads = [&](int set, int buf, int step, int m) {
+#pragma unroll
+            for (int i = m * EACH; i < (m + 1) * EACH && i < READS; ++i) {
+                if (i < NT) xb[set][i] = fb.read(lds + buf + BM * PK, step, i);
+                else xa[set][i - NT] = fa.read(lds + buf, step, i - NT);
             }
-            multiply(1);
-            __builtin_amdgcn_sched_barrier(0);
         };
-        int t = 0;
-        for (; t + 1 < tiles; t += 2) {
-            tile(t, 0);
-            tile(t + 1, 1);
+        auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+        auto step = [&](int set, int buf, int of) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                reads(set ^ 1, buf, of, m);
+                group(set, m);
+                fence();
+            }
+        };
+        next();
+        start(0, 0, LOADS);
+        meet();
+        if (tiles > 1) {
+            next();
+            start(STAGE, 0, LOADS);
         }
-        if (t < tiles) tile(t, 0);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) reads(0, 0, 0, m);
+        int buf = 0;
+        for (int t = 0; t < tiles; ++t) {
+            step(0, buf, 1);
+            step(1, buf, 2);
+            step(0, buf, 3);
+            const bool load = t + 2 < tiles;
+            if (load) next();
+            meet();  // this tile has been read by all, the next one has landed
+            fence();
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                reads(0, buf ^ STAGE, 0, m);  // behind the last tile of what is left there
+                if (load) start(buf, m * LOADS / MT, (m + 1) * LOADS / MT);
+                group(1, m);
+                fence();
+            }
+            buf ^= STAGE;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     }
 };
 
