@@ -157,7 +157,7 @@ __device__ __forceinline__ uint16_t bits16(float v) {
     return __builtin_bit_cast(uint16_t, (T)v);
 }
 
-// Classes are the rows of the matrix instructions, so that a lane holds 16 * MT classes of one row and reduces them in registers.
+// Classes are the rows of the matrix instructions, so that a lane holds 4 * MT classes of a row and reduces them in registers.
 template <typename T, int MW, int NW, int MT, int NT, int PAIRS, bool GRAD>
 __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     typedef Products<T, MW, NW, MT, NT, false, false, PAIRS> P;
@@ -169,56 +169,58 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     p.run(a.w, a.u, m0, n0, 0, a.kts, lds);
 
     const int wm = P::wave_m(), wn = P::wave_n();
-    const float iu = a.scales ? a.scales->iu : 1.f, iw = a.scales ? a.scales->iw : 1.f;
     if (a.scales) {
+        const float iu = a.scales->iu, iw = a.scales->iw;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) p.acc[m][n][i] = p.acc[m][n][i] * iu * iw;
+                for (int j = 0; j < 4; ++j) p.acc[m][n][j] = p.acc[m][n][j] * iu * iw;
     }
     if (!GRAD) {
         float* const meet = (float*)lds;  // [MW][BN][2]
+        const int left = a.classes - (m0 + wm);  // classes that exist from the wave's first on
+        if (left < MT * 16) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (m * 16 + P::row_of() + j >= left) p.acc[m][n][j] = -__builtin_inff();
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int col = wn + n * 32 + P::col_of();
+            const int col = wn + n * 16 + P::col_of();
             const long long t = (long long)n0 + col;
-            const int left = a.classes - (m0 + wm);  // classes that exist from the wave's first on
-            float top = -__builtin_inff();
-            if (left < MT * 32) {
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (m * 32 + P::row_of(i) >= left) p.acc[m][n][i] = -__builtin_inff();
-            }
             const long long want = t < a.rows ? a.target[t] - a.first - m0 - wm : -1;
-            const int w = want >= 0 && want < min(left, MT * 32) ? (int)want : -1;
+            const int w = want >= 0 && want < min(left, MT * 16) ? (int)want : -1;
             if (__builtin_amdgcn_ballot_w64(w >= 0)) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (m * 32 + P::row_of(i) == w) a.picked[t] = p.acc[m][n][i];
+                    for (int j = 0; j < 4; ++j)
+                        if (m * 16 + P::row_of() + j == w) a.picked[t] = p.acc[m][n][j];
             }
+            float top = -__builtin_inff();
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    top = fmaxf(top, p.acc[m][n][i]);
-                }
+                for (int j = 0; j < 4; ++j) top = fmaxf(top, p.acc[m][n][j]);
+            top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float base = top > -__builtin_inff() ? top * kLog2e : 0.f;
             float sum = 0.f;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(p.acc[m][n][i], kLog2e, -base));
+                for (int j = 0; j < 4; ++j) sum += __builtin_amdgcn_exp2f(fmaf(p.acc[m][n][j], kLog2e, -base));
+            sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
-            if ((threadIdx.x & 63) < 32) {
-                meet[((wm / (MT * 32)) * P::BN + col) * 2] = top;
-                meet[((wm / (MT * 32)) * P::BN + col) * 2 + 1] = sum;
+            if ((threadIdx.x & 63) < 16) {
+                meet[((wm / (MT * 16)) * P::BN + col) * 2] = top;
+                meet[((wm / (MT * 16)) * P::BN + col) * 2 + 1] = sum;
             }
         }
         __syncthreads();
@@ -242,46 +244,47 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
         char* const low = (char*)lds + Out::BYTES;
         const float lift = a.scales ? a.scales->g : 1.f;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const long long t = (long long)n0 + wn + n * 32 + P::col_of();
-            const bool there = t < a.rows && !(a.live && !a.live[t]);
-            float lse = 0.f, up = 0.f, both = 0.f;
-            long long want = -1;
-            if (there) {
-                lse = a.lse[t];
-                up = a.dloss ? a.dloss[t] : 0.f;
-                both = up + (a.dlse ? a.dlse[t] : 0.f);
-                want = a.target[t];
-                if (want < 0 || want >= a.all) up = both = __builtin_nanf("");
-                want -= a.first + m0 + wm;
-            }
-            const int w = want >= 0 && want < MT * 32 ? (int)want : -1;
-            up *= lift, both *= lift;
-            if (n) __syncthreads();
+        for (int pass = 0; pass < NT / 2; ++pass) {
+            if (pass) __syncthreads();
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int n = 2 * pass; n < 2 * pass + 2; ++n) {
+                const long long t = (long long)n0 + wn + n * 16 + P::col_of();
+                const bool there = t < a.rows && !(a.live && !a.live[t]);
+                float lse = 0.f, up = 0.f, both = 0.f;
+                long long want = -1;
+                if (there) {
+                    lse = a.lse[t];
+                    up = a.dloss ? a.dloss[t] : 0.f;
+                    both = up + (a.dlse ? a.dlse[t] : 0.f);
+                    want = a.target[t];
+                    if (want < 0 || want >= a.all) up = both = __builtin_nanf("");
+                    want -= a.first + m0 + wm;
+                }
+                const int w = want >= 0 && want < MT * 16 ? (int)want : -1;
+                up *= lift, both *= lift;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int m = 0; m < MT; ++m) {
                     uint16_t hi[4], lo[4];
-                    const int v0 = m * 32 + P::row_of(4 * q);
+                    const int v0 = m * 16 + P::row_of();
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float s = p.acc[m][n][4 * q + j] - lse;
+                        const float s = p.acc[m][n][j] - lse;
                         const float e = PAIRS > 1 ? expf(s) : __builtin_amdgcn_exp2f(s * kLog2e);
                         float g = both * e - (v0 + j == w ? up : 0.f);
                         g = there && m0 + wm + v0 + j < a.classes ? g : 0.f;
                         hi[j] = bits16<T>(g);
                         if (PAIRS > 1) lo[j] = bits16<T>(fabsf(g) < 60000.f ? g - (float)__builtin_bit_cast(T, hi[j]) : 0.f);
                     }
-                    Out::put(lds, m, q, hi);
-                    if (PAIRS > 1) Out::put(low, m, q, lo);
+                    Out::put(lds, m, n, hi);
+                    if (PAIRS > 1) Out::put(low, m, n, lo);
                 }
+            }
             __syncthreads();
             uint16_t* const g = a.g + n0 * a.g_ld + m0;
 #pragma unroll
             for (int i = 0; i < Out::PER; ++i) {
                 int row, col;
-                Out::where(i, n, row, col);
+                Out::where(i, pass, row, col);
                 *(u32x4*)(g + row * a.g_ld + col) = Out::take(lds, i);
                 if (PAIRS > 1) *(u32x4*)(g + row * a.g_ld + col + a.g_plane) = Out::take(low, i);
             }
@@ -351,49 +354,39 @@ __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
     if (kt0 < kt1) {
         p.run(a.a, a.b, tm * P::BM, tn * P::BN, kt0, kt1, lds);
     } else {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p.acc[m][n][i] = 0.f;
+        p.clear();
     }
     if (a.partial) {
-        typedef float f32x4 __attribute__((ext_vector_type(4)));
         f32x4* const to = (f32x4*)a.partial + ((long long)blockIdx.y * gridDim.x + tm * a.tn + tn) * (P::BM * P::BN / 4) +
-                          (threadIdx.x >> 6) * (MT * NT * 256) + (threadIdx.x & 63);
+                          (threadIdx.x >> 6) * (MT * NT * 64) + (threadIdx.x & 63);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    f32x4 v{p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
-                    f32x4* const at = to + ((m * NT + n) * 4 + q) * 64;
-                    if (a.add) v += *at;
-                    *at = v;
-                }
+            for (int n = 0; n < NT; ++n) {
+                f32x4* const at = to + (m * NT + n) * 64;
+                *at = a.add ? *at + p.acc[m][n] : p.acc[m][n];
+            }
         return;
     }
     const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
     const long long r0 = (long long)tn * P::BN;
     const int c0 = tm * P::BM;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (n) __syncthreads();
+    for (int pass = 0; pass < NT / 2; ++pass) {
+        if (pass) __syncthreads();
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 2 * pass; n < 2 * pass + 2; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float v[4] = {p.acc[m][n][4 * q] * d0 * d1, p.acc[m][n][4 * q + 1] * d0 * d1, p.acc[m][n][4 * q + 2] * d0 * d1,
-                                    p.acc[m][n][4 * q + 3] * d0 * d1};
-                Out::put(lds, m, q, v);
+            for (int m = 0; m < MT; ++m) {
+                const f32x4 s = p.acc[m][n];
+                const float v[4] = {s[0] * d0 * d1, s[1] * d0 * d1, s[2] * d0 * d1, s[3] * d0 * d1};
+                Out::put(lds, m, n, v);
             }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < Out::PER; ++i) {
             int row, col;
-            Out::where(i, n, row, col);
+            Out::where(i, pass, row, col);
             if (r0 + row >= a.rows || c0 + col >= a.cols) continue;
             float v[4];
             const u32x4 w = Out::take(lds, i);
@@ -406,14 +399,13 @@ __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
 // The slices' sums, one after the other, four neighbours of a row to a thread.
 template <typename TO, int MW, int NW, int MT, int NT>
 __global__ __launch_bounds__(256) void k_grad_join(const GradArgs a, int slices) {
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
-    constexpr int BM = MW * MT * 32, BN = NW * NT * 32, PER = BM * BN / 4;
+    constexpr int BM = MW * MT * 16, BN = NW * NT * 16, PER = BM * BN / 4;
     const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
     const long long n = (long long)a.tm * a.tn * PER;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        const int tile = (int)(i / PER), in = (int)(i % PER), lane = in & 63, q = in >> 6 & 3, block = in >> 8 & (MT * NT - 1), wave = in / (MT * NT * 256);
-        const long long r = (long long)(tile % a.tn) * BN + wave % NW * (NT * 32) + block % NT * 32 + (lane & 31);
-        const int c = tile / a.tn * BM + wave / NW * (MT * 32) + block / NT * 32 + 8 * q + 4 * (lane >> 5);
+        const int tile = (int)(i / PER), in = (int)(i % PER), lane = in & 63, block = in / 64 % (MT * NT), wave = in / (MT * NT * 64);
+        const long long r = (long long)(tile % a.tn) * BN + wave % NW * (NT * 16) + block % NT * 16 + (lane & 15);
+        const int c = tile / a.tn * BM + wave / NW * (MT * 16) + block / NT * 16 + 4 * (lane >> 4);
         if (r >= a.rows || c >= a.cols) continue;
         const f32x4* const from = (const f32x4*)a.partial + i;
         f32x4 s = 0.f;
@@ -522,9 +514,9 @@ void logits(const LogitArgs& a, int edge, hipStream_t st) {
         r.tm = (a.classes + bm - 1) / bm, r.tn = (int)((a.rows + bn - 1) / bn);
         kernel<<<(unsigned)r.tm * r.tn, threads, 0, st>>>(r);
     };
-    if (edge == 256) go(k_logits<T, 2, 4, 4, 2, PAIRS, GRAD>, 256, 256, 512);
-    else if (edge == 128) go(k_logits<T, 2, 2, 2, 2, PAIRS, GRAD>, 128, 128, 256);
-    else go(k_logits<T, 4, 1, 1, 2, PAIRS, GRAD>, 128, 64, 256);
+    if (edge == 256) go(k_logits<T, 2, 4, 8, 4, PAIRS, GRAD>, 256, 256, 512);
+    else if (edge == 128) go(k_logits<T, 2, 2, 4, 4, PAIRS, GRAD>, 128, 128, 256);
+    else go(k_logits<T, 4, 1, 2, 4, PAIRS, GRAD>, 128, 64, 256);
 }
 
 // One piece's part of a gradient; `last`: its slices are joined.
@@ -536,14 +528,14 @@ void gradient(const GradArgs& a, const Cut& c, bool last, hipStream_t st) {
     const dim3 grid((unsigned)r.tm * r.tn, c.slices);
     const unsigned join = blocks_for((long long)r.tm * r.tn * c.edge * c.edge / 4);
     if (c.edge == 256) {
-        k_loss_grad<T, TO, 2, 4, 4, 2, BSUMS, PAIRS><<<grid, 512, 0, st>>>(r);
-        if (r.partial && last) k_grad_join<TO, 2, 4, 4, 2><<<join, 256, 0, st>>>(r, c.slices);
+        k_loss_grad<T, TO, 2, 4, 8, 4, BSUMS, PAIRS><<<grid, 512, 0, st>>>(r);
+        if (r.partial && last) k_grad_join<TO, 2, 4, 8, 4><<<join, 256, 0, st>>>(r, c.slices);
     } else if (c.edge == 128) {
+        k_loss_grad<T, TO, 2, 2, 4, 4, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
+        if (r.partial && last) k_grad_join<TO, 2, 2, 4, 4><<<join, 256, 0, st>>>(r, c.slices);
+    } else {
         k_loss_grad<T, TO, 2, 2, 2, 2, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
         if (r.partial && last) k_grad_join<TO, 2, 2, 2, 2><<<join, 256, 0, st>>>(r, c.slices);
-    } else {
-        k_loss_grad<T, TO, 2, 2, 1, 1, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
-        if (r.partial && last) k_grad_join<TO, 2, 2, 1, 1><<<join, 256, 0, st>>>(r, c.slices);
     }
 }
 

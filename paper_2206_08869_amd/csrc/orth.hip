@@ -206,14 +206,14 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
     static_assert(Out::BYTES <= P::LDS * 2 && Mirror::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
     constexpr int AT_ONCE = 4;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (n) __syncthreads();
+    for (int pass = 0; pass < NT / 2; ++pass) {
+        if (pass) __syncthreads();
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 2 * pass; n < 2 * pass + 2; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float v[4] = {p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
-                Out::put(lds, m, q, v);
+            for (int m = 0; m < MT; ++m) {
+                const float v[4] = {p.acc[m][n][0], p.acc[m][n][1], p.acc[m][n][2], p.acc[m][n][3]};
+                Out::put(lds, m, n, v);
             }
         __syncthreads();
 #pragma unroll
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
                 int row, col;
-                Out::where(i + u, n, row, col);
+                Out::where(i + u, pass, row, col);
                 fetch(f[u], tj * P::BN + row, ti * P::BM + col, Out::take(lds, i + u));
             }
 #pragma unroll
@@ -231,14 +231,14 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
     }
     if (ti == tj) return;  // symmetric: all of it has been stored
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
+    for (int pass = 0; pass < MT / 2; ++pass) {
         __syncthreads();
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int m = 2 * pass; m < 2 * pass + 2; ++m)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float v[4] = {p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
-                Mirror::put(lds, n, q, v);
+            for (int n = 0; n < NT; ++n) {
+                const float v[4] = {p.acc[m][n][0], p.acc[m][n][1], p.acc[m][n][2], p.acc[m][n][3]};
+                Mirror::put(lds, m, n, v);
             }
         __syncthreads();
 #pragma unroll
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
                 int row, col;
-                Mirror::where(i + u, m, row, col);
+                Mirror::where(i + u, pass, row, col);
                 fetch(f[u], ti * P::BM + row, tj * P::BN + col, Mirror::take(lds, i + u));
             }
 #pragma unroll
@@ -303,14 +303,14 @@ __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const
     static_assert(Out::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
     constexpr int AT_ONCE = 4;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (n) __syncthreads();
+    for (int pass = 0; pass < NT / 2; ++pass) {
+        if (pass) __syncthreads();
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 2 * pass; n < 2 * pass + 2; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float v[4] = {p.acc[m][n][4 * q], p.acc[m][n][4 * q + 1], p.acc[m][n][4 * q + 2], p.acc[m][n][4 * q + 3]};
-                Out::put(lds, m, q, v);
+            for (int m = 0; m < MT; ++m) {
+                const float v[4] = {p.acc[m][n][0], p.acc[m][n][1], p.acc[m][n][2], p.acc[m][n][3]};
+                Out::put(lds, m, n, v);
             }
         __syncthreads();
 #pragma unroll
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const
             int r[AT_ONCE], c[AT_ONCE];
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                Out::where(i + u, n, r[u], c[u]);
+                Out::where(i + u, pass, r[u], c[u]);
                 r[u] += tn * P::BN, c[u] += tm * P::BM;
                 if (r[u] >= rows || c[u] >= cols) continue;
                 load4<2>(was + (long long)r[u] * a.z.cp + c[u], x.plane, x0[u]);
@@ -386,28 +386,28 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
 
 template <int MW, int NW, int MT, int NT, bool SUMS, bool SECOND, int PAIRS>
 void square_with(SquareArgs a, int count, int s, hipStream_t st) {
-    constexpr int E = MW * MT * 32;
+    constexpr int E = MW * MT * 16;
     a.tiles = (s + E - 1) / E;
     k_square<MW, NW, MT, NT, SUMS, SECOND, PAIRS><<<dim3((unsigned)(a.tiles * (a.tiles + 1) / 2), count), MW * NW * 64, 0, st>>>(a);
 }
 template <bool SUMS, bool SECOND, int PAIRS>
 void square(const SquareArgs& a, int edge, int count, int s, hipStream_t st) {
-    if (edge == 256) square_with<2, 4, 4, 2, SUMS, SECOND, PAIRS>(a, count, s, st);
-    else if (edge == 128) square_with<2, 2, 2, 2, SUMS, SECOND, PAIRS>(a, count, s, st);
-    else square_with<2, 2, 1, 1, SUMS, SECOND, PAIRS>(a, count, s, st);
+    if (edge == 256) square_with<2, 4, 8, 4, SUMS, SECOND, PAIRS>(a, count, s, st);
+    else if (edge == 128) square_with<2, 2, 4, 4, SUMS, SECOND, PAIRS>(a, count, s, st);
+    else square_with<2, 2, 2, 2, SUMS, SECOND, PAIRS>(a, count, s, st);
 }
 
 template <int MW, int NW, int MT, int NT, bool TALL, int PAIRS>
 void apply_with(ApplyArgs a, const Target& t, int type, hipStream_t st) {
-    constexpr int E = MW * MT * 32;
+    constexpr int E = MW * MT * 16;
     a.tm = (a.z.cols + E - 1) / E, a.tn = (a.z.rows + E - 1) / E;
     k_apply<MW, NW, MT, NT, TALL, PAIRS><<<dim3((unsigned)a.tm * a.tn, a.z.count), MW * NW * 64, 0, st>>>(a, t, type);
 }
 template <bool TALL, int PAIRS>
 void apply(const ApplyArgs& a, int edge, const Target& t, int type, hipStream_t st) {
-    if (edge == 256) apply_with<2, 4, 4, 2, TALL, PAIRS>(a, t, type, st);
-    else if (edge == 128) apply_with<2, 2, 2, 2, TALL, PAIRS>(a, t, type, st);
-    else apply_with<2, 2, 1, 1, TALL, PAIRS>(a, t, type, st);
+    if (edge == 256) apply_with<2, 4, 8, 4, TALL, PAIRS>(a, t, type, st);
+    else if (edge == 128) apply_with<2, 2, 4, 4, TALL, PAIRS>(a, t, type, st);
+    else apply_with<2, 2, 2, 2, TALL, PAIRS>(a, t, type, st);
 }
 
 template <bool MUON>

@@ -13,7 +13,7 @@
 
 namespace iodf {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
@@ -34,13 +34,13 @@ struct Side {
 
 template <typename T> struct Mma;
 template <> struct Mma<__bf16> {
-    static __device__ __forceinline__ f32x16 go(s16x8 a, s16x8 b, f32x16 c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
+    static __device__ __forceinline__ f32x4 go(s16x8 a, s16x8 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
     }
 };
 template <> struct Mma<_Float16> {
-    static __device__ __forceinline__ f32x16 go(s16x8 a, s16x8 b, f32x16 c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), c, 0, 0, 0);
+    static __device__ __forceinline__ f32x4 go(s16x8 a, s16x8 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), c, 0, 0, 0);
     }
 };
 
@@ -76,9 +76,9 @@ struct Lane {
             }
         }
     }
-    // Where chunk c of row r lies, and which chunk lies at place c: 64 bytes further a row, so that the four rows that sixteen lanes read together
-    // cover all banks.
-    static __device__ __forceinline__ int chunk(int r, int c) { return PER >= 16 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); }
+    // Where chunk c of row r lies, and which chunk lies at place c. Thirty-two lanes read 32 bytes each of rows r .. r + 3 and r + 8 .. r + 11 together: 64
+    // bytes further a row and 32 every eight rows, they cover all banks.
+    static __device__ __forceinline__ int chunk(int r, int c) { return c ^ (PER >= 16 ? (r & 3) << 2 : (r & 2) << 1) ^ (r >> 2 & 2); }
     // tile kt (of the plane `part`): its loads i0 .. i1 - 1, to `lds`, this wave's place in the tile
     static __device__ __forceinline__ const uint16_t* corner(const Side& s, int first, int part, int kt) {
         return s.p + part * s.plane + (SUMS ? (long long)kt * PK * s.ld + first : (long long)first * s.ld + kt * PK);
@@ -89,44 +89,51 @@ struct Lane {
     }
 };
 
-// A wave's fragments of `COUNT` blocks of 32 from row (column) `w0` of the tile on.
+// A wave's fragments of `COUNT` blocks of 16 from row (column) `w0` of the tile on: lane l holds eight numbers along k, from 8 * (l / 16) on, of row l % 16.
 template <int W, int COUNT, bool SUMS>
 struct Frags {
-    uint32_t at[SUMS ? COUNT : 4];  // elements
+    uint32_t at[SUMS ? COUNT : 2];  // elements
     __device__ __forceinline__ void init(int w0) {
         const int lane = threadIdx.x & 63;
         if (!SUMS) {
-            const int r = w0 + (lane & 31);
+            const int r = w0 + (lane & 15);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) at[s] = r * PK + (((s * 2 + (lane >> 5)) ^ (r >> 1 & 7)) * 8);
+            for (int s = 0; s < 2; ++s) at[s] = r * PK + (((s * 4 + (lane >> 4)) ^ (r >> 1 & 7)) * 8);
         } else {
-            const int r = (lane >> 5) * 8 + ((lane >> 2) & 3), c = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+            const int r = (lane >> 4) * 8 + ((lane >> 2) & 3), c = (lane & 3) * 4;
 #pragma unroll
-            for (int b = 0; b < COUNT; ++b) at[b] = r * W + Lane<W, 64, true>::chunk(r, (w0 + b * 32 + c) / 8) * 8 + (c & 7);
+            for (int b = 0; b < COUNT; ++b) at[b] = r * W + Lane<W, 64, true>::chunk(r, (w0 + b * 16 + c) / 8) * 8 + (c & 7);
         }
     }
+    // of step `step` (32 along k) of the tile, block b
     __device__ __forceinline__ s16x8 read(const uint16_t* tile, int step, int b) const {
-        if (!SUMS) return *(const s16x8*)(tile + at[step] + b * 32 * PK);
+        if (!SUMS) return *(const s16x8*)(tile + at[step] + b * 16 * PK);
         union { s16x4 h[2]; s16x8 v; } u;
-        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + step * 16 * W));
-        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + (step * 16 + 4) * W));
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + step * 32 * W));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + at[b] + (step * 32 + 4) * W));
         return u.v;
     }
 };
 
-// MW x NW waves of MT x NT blocks of 32 x 32 outputs.
+// MW x NW waves of MT x NT blocks of 16 x 16 outputs.
 template <typename T, int MW, int NW, int MT_, int NT_, bool ASUMS, bool BSUMS, int PAIRS>
 struct Products {
-    static constexpr int MT = MT_, NT = NT_, BM = MW * MT * 32, BN = NW * NT * 32, THREADS = MW * NW * 64;
+    static constexpr int MT = MT_, NT = NT_, BM = MW * MT * 16, BN = NW * NT * 16, THREADS = MW * NW * 64;
     static constexpr int STAGE = (BM + BN) * PK;  // elements of a tile of both operands
     static constexpr int LDS = 2 * STAGE;         // elements of LDS that run() wants
-    f32x16 acc[MT][NT];
+    f32x4 acc[MT][NT];
 
-    static __device__ __forceinline__ int wave_m() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW * MT * 32; }
-    static __device__ __forceinline__ int wave_n() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW * NT * 32; }
-    // which output of the wave's a lane holds in acc[m][n][i]: row m * 32 + row_of(i), column n * 32 + col_of()
-    static __device__ __forceinline__ int row_of(int i) { return 8 * (i / 4) + 4 * ((threadIdx.x & 63) >> 5) + i % 4; }
-    static __device__ __forceinline__ int col_of() { return threadIdx.x & 31; }
+    static __device__ __forceinline__ int wave_m() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW * MT * 16; }
+    static __device__ __forceinline__ int wave_n() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW * NT * 16; }
+    // which outputs of the wave's a lane holds in acc[m][n][0..3]: rows m * 16 + row_of() and the three behind it, column n * 16 + col_of()
+    static __device__ __forceinline__ int row_of() { return (threadIdx.x & 63) / 16 * 4; }
+    static __device__ __forceinline__ int col_of() { return threadIdx.x & 15; }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     // Tiles kt0 .. kt1 - 1 (kt1 > kt0) along k, of outputs from (m0, n0) on. Ends with a barrier: LDS is free then.
     __device__ __forceinline__ void run(const Side& a, const Side& b, int m0, int n0, int kt0, int kt1, uint16_t* lds) {
@@ -136,12 +143,7 @@ struct Products {
         Frags<BN, NT, BSUMS> fb;
         la.init(a, m0), lb.init(b, n0);
         fa.init(wave_m()), fb.init(wave_n());
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.f;
+        clear();
         const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)lds +
                               __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
         const int tiles = (kt1 - kt0) * PAIRS;
@@ -168,30 +170,27 @@ struct Products {
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        // Fragments of the next step are read while this one's are multiplied: a step is MT groups of NT products, with reads (and, once a tile, the loads
-        // of the tile after the next) dealt out between them. Left to itself the compiler gathers reads just before their products.
-        s16x8 xa[2][MT], xb[2][NT];
+        // A tile is two steps of MT groups of NT products. Fragments of the next step are read while this one's are multiplied: those of B and of A's last
+        // SPARE blocks into registers of their own, A's other blocks into the same ones, once their products are on their way. So the last read of a
+        // step has the products of the last two groups to arrive, and all of a tile is read when its second step begins. Reads (and, once a tile, the
+        // loads of the tile after the next) are dealt out by hand: left to itself the compiler gathers reads just before their products.
+        constexpr int SPARE = 2, ROLL = MT - SPARE, BUSY = MT > 1 ? MT / 2 : 1, EACH = (NT + SPARE + BUSY - 1) / BUSY;
+        static_assert(MT >= SPARE, "two blocks of rows at least");
+        s16x8 xa[ROLL > 0 ? ROLL : 1], xs[2][SPARE], xb[2][NT];
+        auto read_a = [&](int buf, int step, int m) { return fa.read(lds + buf, step, m); };
         auto group = [&](int set, int m) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[m][n] = Mma<T>::go(xa[set][m], xb[set][n], acc[m][n]);
+            for (int n = 0; n < NT; ++n) acc[m][n] = Mma<T>::go(m < ROLL ? xa[m < ROLL ? m : 0] : xs[set][m < ROLL ? 0 : m - ROLL], xb[set][n], acc[m][n]);
         };
-        constexpr int READS = MT + NT, BUSY = MT > 1 ? MT - 1 : 1, EACH = (READS + BUSY - 1) / BUSY;  // of a group; the last one has none
-        auto reads = [&](int set, int buf, int step, int m) {
+        auto reads = [&](int set, int buf, int step, int g) {  // of step `step`, before group g of the step before it
 #pragma unroll
-            for (int i = m * EACH; i < (m + 1) * EACH && i < READS; ++i) {
+            for (int i = g * EACH; i < (g + 1) * EACH && i < NT + SPARE; ++i) {
                 if (i < NT) xb[set][i] = fb.read(lds + buf + BM * PK, step, i);
-                else xa[set][i - NT] = fa.read(lds + buf, step, i - NT);
+                else xs[set][i - NT] = read_a(buf, step, ROLL + i - NT);
             }
+            if (g >= 1 && g - 1 < ROLL) xa[g - 1] = read_a(buf, step, g - 1);
         };
         auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-        auto step = [&](int set, int buf, int of) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                reads(set ^ 1, buf, of, m);
-                group(set, m);
-                fence();
-            }
-        };
         next();
         start(0, 0, LOADS);
         meet();
@@ -200,21 +199,24 @@ struct Products {
             start(STAGE, 0, LOADS);
         }
 #pragma unroll
-        for (int m = 0; m < MT; ++m) reads(0, 0, 0, m);
+        for (int g = 0; g <= MT; ++g) reads(0, 0, 0, g);
         int buf = 0;
         for (int t = 0; t < tiles; ++t) {
-            step(0, buf, 1);
-            step(1, buf, 2);
-            step(0, buf, 3);
+#pragma unroll
+            for (int g = 0; g < MT; ++g) {
+                reads(1, buf, 1, g);
+                group(0, g);
+                fence();
+            }
             const bool load = t + 2 < tiles;
             if (load) next();
             meet();  // this tile has been read by all, the next one has landed
             fence();
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                reads(0, buf ^ STAGE, 0, m);  // behind the last tile of what is left there
-                if (load) start(buf, m * LOADS / MT, (m + 1) * LOADS / MT);
-                group(1, m);
+            for (int g = 0; g < MT; ++g) {
+                reads(0, buf ^ STAGE, 0, g);  // behind the last tile of what is left there
+                if (load) start(buf, g * LOADS / MT, (g + 1) * LOADS / MT);
+                group(1, g);
                 fence();
             }
             buf ^= STAGE;
@@ -226,20 +228,21 @@ struct Products {
 };
 
 // A workgroup's outputs on their way to memory: what lanes hold as four neighbours of a row here and there goes through LDS and comes out as whole rows, sixteen
-// bytes to a lane. Output rows are the products' columns n, output columns their rows m. Block column n of all waves at a time: NW * 32 rows of BM.
+// bytes to a lane. Output rows are the products' columns n, output columns their rows m. Two block columns of all waves at a time, pass by pass: NW * 32 rows of BM.
 // Chunks of sixteen bytes are moved about by their row, so that the 32 rows that a wave writes together cover all banks.
 template <class P, typename E, int NW>
 struct Staged {
     static constexpr int ROWS = NW * 32, CHUNKS = P::BM * (int)sizeof(E) / 16, PER = ROWS * CHUNKS / P::THREADS, OF = 16 / (int)sizeof(E);
     static constexpr int BYTES = ROWS * CHUNKS * 16;
-    static __device__ __forceinline__ void put(void* lds, int m, int q, const E (&v)[4]) {
-        const int row = P::wave_n() / P::NT + P::col_of(), c = P::wave_m() + m * 32 + P::row_of(4 * q);
+    // block (m, n); n's own pass is n / 2
+    static __device__ __forceinline__ void put(void* lds, int m, int n, const E (&v)[4]) {
+        const int row = P::wave_n() / P::NT * 2 + n % 2 * 16 + P::col_of(), c = P::wave_m() + m * 16 + P::row_of();
         __builtin_memcpy((char*)lds + (row * CHUNKS + ((c / OF) ^ (row & (CHUNKS - 1) & 31))) * 16 + c % OF * sizeof(E), v, 4 * sizeof(E));
     }
-    // chunk i of the thread's: its row and first column among the workgroup's outputs, and what it holds
-    static __device__ __forceinline__ void where(int i, int n, int& row, int& col) {
+    // chunk i of the thread's in a pass: its row and first column among the workgroup's outputs, and what it holds
+    static __device__ __forceinline__ void where(int i, int pass, int& row, int& col) {
         const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
-        row = (r / 32) * (P::NT * 32) + n * 32 + r % 32;
+        row = (r / 32) * (P::NT * 16) + pass * 32 + r % 32;
         col = k % CHUNKS * OF;
     }
     static __device__ __forceinline__ u32x4 take(const void* lds, int i) {
@@ -248,18 +251,18 @@ struct Staged {
     }
 };
 
-// The same for the mirror image: output rows are the products' rows m, output columns their columns n. Block row m of all waves at a time.
+// The same for the mirror image: output rows are the products' rows m, output columns their columns n. Two block rows of all waves at a time.
 template <class P, int MW>
 struct StagedAcross {
     static constexpr int ROWS = MW * 32, CHUNKS = P::BN / 4, PER = ROWS * CHUNKS / P::THREADS, BYTES = ROWS * CHUNKS * 16;
-    static __device__ __forceinline__ void put(void* lds, int n, int q, const float (&v)[4]) {
-        const int row = P::wave_m() / P::MT + P::row_of(4 * q), c = P::wave_n() + n * 32 + P::col_of();
+    static __device__ __forceinline__ void put(void* lds, int m, int n, const float (&v)[4]) {
+        const int row = P::wave_m() / P::MT * 2 + m % 2 * 16 + P::row_of(), c = P::wave_n() + n * 16 + P::col_of();
 #pragma unroll
         for (int j = 0; j < 4; ++j) ((float*)lds)[((row + j) * CHUNKS + ((c / 4) ^ ((row + j) & (CHUNKS - 1) & 31))) * 4 + c % 4] = v[j];
     }
-    static __device__ __forceinline__ void where(int i, int m, int& row, int& col) {
+    static __device__ __forceinline__ void where(int i, int pass, int& row, int& col) {
         const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
-        row = (r / 32) * (P::MT * 32) + m * 32 + r % 32;
+        row = (r / 32) * (P::MT * 16) + pass * 32 + r % 32;
         col = k % CHUNKS * 4;
     }
     static __device__ __forceinline__ u32x4 take(const void* lds, int i) {
