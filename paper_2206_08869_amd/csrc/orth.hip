@@ -153,11 +153,9 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
     typedef Products<_Float16, MW, NW, MT, NT, SUMS, SUMS, PAIRS> P;
     static_assert(P::BM == P::BN, "tiles of a symmetric product are square");
     __shared__ __align__(16) uint16_t lds[P::LDS];
-    const int l = blockIdx.x, k = blockIdx.y;
-    int ti = (int)((sqrtf(8.f * l + 1.f) - 1.f) * 0.5f);
-    while ((ti + 1) * (ti + 2) / 2 <= l) ++ti;
-    while (ti * (ti + 1) / 2 > l) --ti;
-    const int tj = l - ti * (ti + 1) / 2;
+    const int k = blockIdx.y;
+    int ti, tj;
+    place_triangle(blockIdx.x, gridDim.x, a.tiles, ti, tj);
     Side x = a.x;
     x.p += k * a.x_batch;
     P p;

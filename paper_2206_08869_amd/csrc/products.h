@@ -318,4 +318,19 @@ __device__ __forceinline__ void place_tile(unsigned b, unsigned all, unsigned tm
     n = (int)(in / high);
 }
 
+// The same for the tiles on and below the diagonal of a square of n x n, in bands eight tiles high.
+__device__ __forceinline__ void place_triangle(unsigned b, unsigned all, unsigned n, int& i, int& j) {
+    const unsigned share = all / 8, l = b < share * 8 ? b % 8 * share + b / 8 : b;
+    unsigned r0 = 0;
+    while (r0 + 8 < n && (r0 + 8) * (r0 + 9) / 2 <= l) r0 += 8;
+    const unsigned high = min(8u, n - r0), in = l - r0 * (r0 + 1) / 2;
+    if (in < high * r0) {
+        i = (int)(r0 + in % high), j = (int)(in / high);
+    } else {
+        unsigned k = in - high * r0, r = 0;
+        while (k > r) k -= ++r;
+        i = (int)(r0 + r), j = (int)(r0 + k);
+    }
+}
+
 }  // namespace iodf
