@@ -239,15 +239,16 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
             a.sums[tm * a.rows + t] = sum;
         }
     } else {
-        typedef Staged<P, uint16_t, NW> Out;
+        typedef Staged<P, uint16_t, NW, (PAIRS > 1 ? NT / 2 : NT)> Out;
         static_assert((PAIRS > 1 ? 2 : 1) * Out::BYTES <= P::LDS * 2, "g passes through the operands' LDS");
         char* const low = (char*)lds + Out::BYTES;
         const float lift = a.scales ? a.scales->g : 1.f;
 #pragma unroll
-        for (int pass = 0; pass < NT / 2; ++pass) {
-            if (pass) __syncthreads();
+        for (int pass = 0; pass < Out::PASSES; ++pass) {
+            if (pass) lds_barrier();
+            const Out staged;
 #pragma unroll
-            for (int n = 2 * pass; n < 2 * pass + 2; ++n) {
+            for (int n = pass * (NT / Out::PASSES); n < (pass + 1) * (NT / Out::PASSES); ++n) {
                 const long long t = (long long)n0 + wn + n * 16 + P::col_of();
                 const bool there = t < a.rows && !(a.live && !a.live[t]);
                 float lse = 0.f, up = 0.f, both = 0.f;
@@ -275,18 +276,19 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                         hi[j] = bits16<T>(g);
                         if (PAIRS > 1) lo[j] = bits16<T>(fabsf(g) < 60000.f ? g - (float)__builtin_bit_cast(T, hi[j]) : 0.f);
                     }
-                    Out::put(lds, m, n, hi);
-                    if (PAIRS > 1) Out::put(low, m, n, lo);
+                    staged.put(lds, m, n, hi);
+                    if (PAIRS > 1) staged.put(low, m, n, lo);
                 }
             }
-            __syncthreads();
+            lds_barrier();
             uint16_t* const g = a.g + n0 * a.g_ld + m0;
 #pragma unroll
             for (int i = 0; i < Out::PER; ++i) {
+                if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                 int row, col;
-                Out::where(i, pass, row, col);
-                *(u32x4*)(g + row * a.g_ld + col) = Out::take(lds, i);
-                if (PAIRS > 1) *(u32x4*)(g + row * a.g_ld + col + a.g_plane) = Out::take(low, i);
+                staged.where(i, pass, row, col);
+                *(u32x4*)(g + row * a.g_ld + col) = staged.take(lds, i);
+                if (PAIRS > 1) *(u32x4*)(g + row * a.g_ld + col + a.g_plane) = staged.take(low, i);
             }
         }
     }
@@ -344,7 +346,7 @@ struct GradArgs {
 template <typename T, typename TO, int MW, int NW, int MT, int NT, bool BSUMS, int PAIRS>
 __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
     typedef Products<T, MW, NW, MT, NT, true, BSUMS, PAIRS> P;
-    typedef Staged<P, float, NW> Out;
+    typedef Staged<P, float, NW, 2> Out;
     static_assert(Out::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
     __shared__ __align__(16) uint16_t lds[P::LDS];
     int tm, tn;
@@ -372,24 +374,26 @@ __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
     const long long r0 = (long long)tn * P::BN;
     const int c0 = tm * P::BM;
 #pragma unroll
-    for (int pass = 0; pass < NT / 2; ++pass) {
-        if (pass) __syncthreads();
+    for (int pass = 0; pass < Out::PASSES; ++pass) {
+        if (pass) lds_barrier();
+        const Out staged;
 #pragma unroll
         for (int n = 2 * pass; n < 2 * pass + 2; ++n)
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const f32x4 s = p.acc[m][n];
                 const float v[4] = {s[0] * d0 * d1, s[1] * d0 * d1, s[2] * d0 * d1, s[3] * d0 * d1};
-                Out::put(lds, m, n, v);
+                staged.put(lds, m, n, v);
             }
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int i = 0; i < Out::PER; ++i) {
+            if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
             int row, col;
-            Out::where(i, pass, row, col);
+            staged.where(i, pass, row, col);
             if (r0 + row >= a.rows || c0 + col >= a.cols) continue;
             float v[4];
-            const u32x4 w = Out::take(lds, i);
+            const u32x4 w = staged.take(lds, i);
             __builtin_memcpy(v, &w, 16);
             put_quad((TO*)a.out + (r0 + row) * a.ld + c0 + col, a.cols - c0 - col, v);
         }

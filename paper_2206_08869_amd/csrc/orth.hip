@@ -12,6 +12,8 @@
 // A and A^2 are symmetric: only tiles on and below the diagonal are computed, and stored twice.
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
+#include <cstdlib>
 
 #include "products.h"
 #include "step.h"
@@ -120,6 +122,9 @@ struct SquareArgs {
     Side x;                 // X (first) or O (second), of matrix 0
     long long x_batch;
     int kts, tiles;         // tiles along the sum, tiles of a side
+    int pieces;             // 0: a workgroup has a tile's whole sum
+    long long units;        // tiles along the sums of all tiles
+    float* parts;
     int sp;
     float down;             // what a sum is multiplied with to be X X' or O O
     float lift, unlift;     // powers of two of what is stored; second: of O's inverse
@@ -130,24 +135,129 @@ struct SquareArgs {
     long long plane;
 };
 
-template <int PAIRS>
-__device__ __forceinline__ void store4(_Float16* to, long long plane, const float (&v)[4]) {
-    _Float16 hi[4], lo[4];
+// Four numbers as they lie in memory: what a load that is not waited for yet holds.
+template <int PARTS>
+struct Raw4 {
+    u32x2 w[PARTS];
+    __device__ __forceinline__ void load(const _Float16* from, long long plane) {
+        w[0] = *(const u32x2*)from;
+        if (PARTS > 1) w[PARTS - 1] = *(const u32x2*)(from + plane);
+    }
+    __device__ __forceinline__ float get(int j) const {
+        float v = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) two_parts(v[j], hi[j], lo[j]);
-    __builtin_memcpy(to, hi, 8);
-    if (PAIRS > 1) __builtin_memcpy(to + plane, lo, 8);
-}
-template <int PAIRS>
-__device__ __forceinline__ void load4(const _Float16* from, long long plane, float (&v)[4]) {
-    _Float16 hi[4], lo[4];
-    __builtin_memcpy(hi, from, 8);
-    if (PAIRS > 1) __builtin_memcpy(lo, from + plane, 8);
+        for (int k = 0; k < PARTS; ++k) v += (float)__builtin_bit_cast(_Float16, (uint16_t)(w[k][j / 2] >> j % 2 * 16));
+        return v;
+    }
+};
+
+// Sums of a block of X X' or O O from row m0 and column n0 on -> what is stored of it, and with `mirror` its mirror image (of a tile on the diagonal the
+// block itself is that).
+template <class P, int MW, int NW, bool SECOND, int PAIRS>
+__device__ __forceinline__ void finish_square(const SquareArgs& a, P& p, int k, int m0, int n0, bool mirror, uint16_t* lds) {
+    constexpr int MT = P::MT, NT = P::NT;
+    constexpr int PARTS = PAIRS > 1 ? 2 : 1, AHEAD = MT < 4 ? MT : 4;
+    typedef Staged<P, uint16_t, NW, NT> Out;
+    static_assert(Out::BYTES <= 2 * P::LDS, "outputs pass through the operands' LDS");
+    const long long square = (long long)a.sp * a.sp;
+    uint16_t* const out = (uint16_t*)a.out + k * square;
+    const _Float16* const o = (const _Float16*)a.x.p + k * a.x_batch;  // second
+    float* const d = a.d + (long long)k * a.sp;
+    float* const e = a.e + (long long)k * a.sp;
+    // rows and columns past sp stand in for the last ones where something is read
+    const int r0 = m0 + P::wave_m() + P::row_of(), c0 = n0 + P::wave_n() + P::col_of();
+    float dr[MT][4], dc[NT];
+    if (SECOND) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = (float)hi[j] + (PAIRS > 1 ? (float)lo[j] : 0.f);
+        for (int m = 0; m < MT; ++m) __builtin_memcpy(dr[m], d + min(r0 + m * 16, a.sp - 4), 16);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) dc[n] = d[min(c0 + n * 16, a.sp - 1)];
+    }
+    if (!mirror) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = r0 + m * 16 + j;
+                    if (r != c0 + n * 16 || r >= a.sp) continue;
+                    const float sum = p.acc[m][n][j] * a.down;
+                    if (!SECOND) d[r] = sum;
+                    else e[r] = fmaf(a.c, fmaf(dc[n], dc[n], sum), a.b * dc[n]);
+                }
+    }
+    // Low parts in a pass of their own. What a lane holds is four rows of a column of sums: symmetric, so O is read as four neighbours of a row.
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+        if (part) {
+            lds_barrier();
+            p.anew();
+        }
+        const Out staged;
+        int r0 = m0 + P::wave_m() + P::row_of(), c0 = n0 + P::wave_n() + P::col_of();
+        asm volatile("" : "+v"(r0), "+v"(c0));
+        Raw4<PARTS> was[2][AHEAD];
+        auto load = [&](int i) {  // of blocks i * AHEAD on, column by column
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int m = i * AHEAD % MT + u, n = i * AHEAD / MT;
+                was[i & 1][u].load(o + (long long)min(c0 + n * 16, a.sp - 1) * a.sp + min(r0 + m * 16, a.sp - 4), a.x.plane);
+            }
+        };
+        if (SECOND) load(0);
+#pragma unroll
+        for (int i = 0; i < MT * NT / AHEAD; ++i) {
+            if (SECOND && i + 1 < MT * NT / AHEAD) load(i + 1);
+            __builtin_amdgcn_sched_barrier(0);  // so far ahead and no further, which would not fit the registers
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int m = i * AHEAD % MT + u, n = i * AHEAD / MT;
+                uint16_t v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float w = p.acc[m][n][j] * a.down;
+                    if (SECOND) {
+                        const float ov = was[i & 1][u].get(j) * a.unlift;
+                        w = fmaf(a.c, fmaf(dc[n] + dr[m][j], ov, w), a.b * ov);
+                    }
+                    _Float16 hi, lo;
+                    two_parts(w * a.lift, hi, lo);
+                    v[j] = __builtin_bit_cast(uint16_t, part ? lo : hi);
+                }
+                staged.put(lds, m, n, v);
+            }
+        }
+        if (!mirror) {  // the diagonal is kept as d or e
+            lds_barrier();
+            const int r = max(m0, n0) + (int)threadIdx.x;
+            if (r < min(m0 + P::BM, n0 + P::BN)) *(uint16_t*)((char*)lds + Out::place(r - n0, (r - m0) / 8) + (r - m0) % 8 * 2) = 0;
+        }
+        lds_barrier();
+        uint16_t* const to = out + (part ? a.plane : 0);
+#pragma unroll
+        for (int i = 0; i < Out::PER; ++i) {
+            if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+            int row, col;
+            staged.where(i, 0, row, col);
+            row += n0, col += m0;
+            if (row < a.sp && col < a.sp) *(u32x4*)(to + (long long)row * a.sp + col) = staged.take(lds, i);
+        }
+        if (mirror) {
+#pragma unroll
+            for (int i = 0; i < Out::ACROSS; ++i) {
+                if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                int row, col;
+                staged.where_across(i, row, col);
+                row += m0, col += n0;
+                const s16x8 v = staged.take_across(lds, i);
+                if (row < a.sp && col < a.sp) *(s16x8*)(to + (long long)row * a.sp + col) = v;
+            }
+        }
+    }
 }
 
-// A tile on or below the diagonal of a symmetric product, and its mirror image.
+// A tile on or below the diagonal of a symmetric product, all of its sum.
 template <int MW, int NW, int MT, int NT, bool SUMS, bool SECOND, int PAIRS>
 __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
     typedef Products<_Float16, MW, NW, MT, NT, SUMS, SUMS, PAIRS> P;
@@ -155,103 +265,72 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
     __shared__ __align__(16) uint16_t lds[P::LDS];
     const int k = blockIdx.y;
     int ti, tj;
-    place_triangle(blockIdx.x, gridDim.x, a.tiles, ti, tj);
+    place_triangle(by_die(blockIdx.x, gridDim.x), a.tiles, ti, tj);
     Side x = a.x;
     x.p += k * a.x_batch;
     P p;
     p.run(x, x, ti * P::BM, tj * P::BN, 0, a.kts, lds);
+    finish_square<P, MW, NW, SECOND, PAIRS>(a, p, k, ti * P::BM, tj * P::BN, ti != tj, lds);
+}
 
-    const long long square = (long long)a.sp * a.sp;
-    _Float16* const out = a.out + k * square;
-    const _Float16* const o = (const _Float16*)x.p;
-    float* const d = a.d + (long long)k * a.sp;
-    float* const e = a.e + (long long)k * a.sp;
-    // four neighbours of row r, from sums in LDS
-    struct Four {
-        float sum[4], was[4], dr, dc[4];
-        int r, c;
-    };
-    auto fetch = [&](Four& f, int r, int c, u32x4 w) {
-        __builtin_memcpy(f.sum, &w, 16);
-        f.r = r, f.c = c;
-        if (SECOND && r < a.sp && c < a.sp) {
-            load4<PAIRS>(o + (long long)r * a.sp + c, x.plane, f.was);
-            f.dr = d[r];
-            __builtin_memcpy(f.dc, d + c, 16);
-        }
-    };
-    auto finish = [&](const Four& f) {
-        if (f.r >= a.sp || f.c >= a.sp) return;
-        float v[4];
+// The same where tiles are few or do not go round the compute units evenly: all tiles' steps along their sums are one line, of which every workgroup takes
+// an equal piece, through the ends of tiles. A piece's part of a tile is kept as sums, in the order in which lanes hold them, in place piece + tile, and a
+// second kernel adds a tile's parts up. 4096 x 4096 is 136 tiles of 256: 1.9 compute units to a tile.
+__device__ __forceinline__ long long piece_begin(const SquareArgs& a, long long w) { return w * a.units / a.pieces; }
+__device__ __forceinline__ long long piece_of(const SquareArgs& a, long long unit) { return ((unit + 1) * a.pieces - 1) / a.units; }
+
+template <int MW, int NW, int MT, int NT, bool SUMS, int PAIRS>
+__global__ __launch_bounds__(MW * NW * 64) void k_square_piece(const SquareArgs a) {
+    typedef Products<_Float16, MW, NW, MT, NT, SUMS, SUMS, PAIRS> P;
+    __shared__ __align__(16) uint16_t lds[P::LDS];
+    const int w = by_die(blockIdx.x, gridDim.x);
+    const long long begin = piece_begin(a, w);
+    const int per = a.tiles * (a.tiles + 1) / 2;
+    // the same in all lanes, which the compiler does not see behind a division
+    int left = __builtin_amdgcn_readfirstlane((int)(piece_begin(a, w + 1) - begin)), tile = __builtin_amdgcn_readfirstlane((int)(begin / a.kts));
+    int kt0 = __builtin_amdgcn_readfirstlane((int)(begin - (long long)tile * a.kts));
+    for (; left > 0; ++tile, kt0 = 0) {
+        const int kt1 = min(a.kts, kt0 + left), k = __builtin_amdgcn_readfirstlane(tile / per);
+        int ti, tj;
+        place_triangle(tile - k * per, a.tiles, ti, tj);
+        ti = __builtin_amdgcn_readfirstlane(ti), tj = __builtin_amdgcn_readfirstlane(tj);
+        Side x = a.x;
+        x.p += k * a.x_batch;
+        P p;
+        p.run(x, x, ti * P::BM, tj * P::BN, kt0, kt1, lds);
+        f32x4* const to = (f32x4*)a.parts + ((long long)(w + tile) * (MW * NW) + (threadIdx.x >> 6)) * (MT * NT * 64) + (threadIdx.x & 63);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float sum = f.sum[j] * a.down;
-            const bool diagonal = f.r == f.c + j;
-            if (!SECOND) {
-                if (diagonal) d[f.r] = sum;
-                v[j] = sum * a.lift;
-            } else {
-                const float ov = f.was[j] * a.unlift;
-                if (diagonal) e[f.r] = fmaf(a.c, fmaf(f.dr, f.dr, sum), a.b * f.dr);
-                v[j] = fmaf(a.c, fmaf(f.dr + f.dc[j], ov, sum), a.b * ov) * a.lift;
-            }
-            if (diagonal) v[j] = 0.f;
-        }
-        store4<PAIRS>(out + (long long)f.r * a.sp + f.c, a.plane, v);
-    };
-    typedef Staged<P, float, NW> Out;
-    typedef StagedAcross<P, MW> Mirror;
-    static_assert(Out::BYTES <= P::LDS * 2 && Mirror::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
-    constexpr int AT_ONCE = 4;
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int pass = 0; pass < NT / 2; ++pass) {
-        if (pass) __syncthreads();
-#pragma unroll
-        for (int n = 2 * pass; n < 2 * pass + 2; ++n)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const float v[4] = {p.acc[m][n][0], p.acc[m][n][1], p.acc[m][n][2], p.acc[m][n][3]};
-                Out::put(lds, m, n, v);
-            }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < Out::PER; i += AT_ONCE) {
-            Four f[AT_ONCE];
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                int row, col;
-                Out::where(i + u, pass, row, col);
-                fetch(f[u], tj * P::BN + row, ti * P::BM + col, Out::take(lds, i + u));
-            }
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) finish(f[u]);
-        }
+            for (int n = 0; n < NT; ++n) to[(m * NT + n) * 64] = p.acc[m][n];
+        left -= kt1 - kt0;
     }
-    if (ti == tj) return;  // symmetric: all of it has been stored
+}
+
+// A wave's part of a tile to a workgroup.
+template <int MW, int NW, int MT, int NT, bool SECOND, int PAIRS>
+__global__ __launch_bounds__(64) void k_square_join(const SquareArgs a) {
+    typedef Products<_Float16, 1, 1, MT, NT, false, false, PAIRS> P;
+    constexpr int WAVES = MW * NW;
+    __shared__ __align__(16) uint16_t lds[Staged<P, uint16_t, 1, NT>::BYTES / 2];
+    const int tile = blockIdx.x / WAVES, wave = blockIdx.x % WAVES, per = a.tiles * (a.tiles + 1) / 2, k = tile / per;
+    int ti, tj;
+    place_triangle(tile - k * per, a.tiles, ti, tj);
+    P p;
+    const int first = (int)piece_of(a, (long long)tile * a.kts), last = (int)piece_of(a, (tile + 1ll) * a.kts - 1);
+    const f32x4* from = (const f32x4*)a.parts + ((long long)(first + tile) * WAVES + wave) * (MT * NT * 64) + threadIdx.x;
 #pragma unroll
-    for (int pass = 0; pass < MT / 2; ++pass) {
-        __syncthreads();
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int m = 2 * pass; m < 2 * pass + 2; ++m)
+        for (int n = 0; n < NT; ++n) p.acc[m][n] = from[(m * NT + n) * 64];
+    for (int w = first + 1; w <= last; ++w) {
+        from += WAVES * MT * NT * 64;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float v[4] = {p.acc[m][n][0], p.acc[m][n][1], p.acc[m][n][2], p.acc[m][n][3]};
-                Mirror::put(lds, m, n, v);
-            }
-        __syncthreads();
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < Mirror::PER; i += AT_ONCE) {
-            Four f[AT_ONCE];
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                int row, col;
-                Mirror::where(i + u, pass, row, col);
-                fetch(f[u], ti * P::BM + row, tj * P::BN + col, Mirror::take(lds, i + u));
-            }
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) finish(f[u]);
-        }
+            for (int n = 0; n < NT; ++n) p.acc[m][n] += from[(m * NT + n) * 64];
     }
+    finish_square<P, 1, 1, SECOND, PAIRS>(a, p, k, ti * (MW * P::BM) + wave / NW * P::BM, tj * (NW * P::BN) + wave % NW * P::BN, ti != tj, lds);
 }
 
 struct ApplyArgs {
@@ -267,16 +346,35 @@ struct ApplyArgs {
     float lift;
 };
 
-template <typename TO>
-__device__ __forceinline__ void deliver(const Target& t, int k, int r, int c, int n, float (&v)[4]) {
-    TO* const to = (t.batch ? (TO*)t.w[0] + k * t.batch : (TO*)t.w[k]) + r * t.stride + c;
-    if (t.update) {
-        float was[4];
-        get_quad(to, n, was);
+// A pass of results, to the gradient's place or into the weights. Weights are read eight rows' chunks ahead.
+template <typename TO, class Out>
+__device__ __forceinline__ void deliver(const Target& t, int k, const Shape& z, int r0, int c0, int pass, const void* lds) {
+    constexpr int AT_ONCE = 4;
+    const Out staged;
+    TO* const to = t.batch ? (TO*)t.w[0] + k * t.batch : (TO*)t.w[k];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = fmaf(t.keep, was[j], t.by * v[j]);
+    for (int i = 0; i < Out::PER; i += AT_ONCE) {
+        float was[AT_ONCE][4];
+        int r[AT_ONCE], c[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            staged.where(i + u, pass, r[u], c[u]);
+            r[u] += r0, c[u] += c0;
+            if (t.update && r[u] < z.rows && c[u] < z.cols) get_quad(to + r[u] * t.stride + c[u], z.cols - c[u], was[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (r[u] >= z.rows || c[u] >= z.cols) continue;
+            float v[4];
+            const u32x4 w = staged.take(lds, i + u);
+            __builtin_memcpy(v, &w, 16);
+            if (t.update) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = fmaf(t.keep, was[u][j], t.by * v[j]);
+            }
+            put_quad(to + r[u] * t.stride + c[u], z.cols - c[u], v);
+        }
     }
-    put_quad(to, n, v);
 }
 
 // (a + e) X + B X: columns of X are the rows of the matrix instructions, so that a lane holds four neighbours of a row.
@@ -295,65 +393,128 @@ __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const
 
     const _Float16* const was = (const _Float16*)x.p;
     const float* const e = a.e + (long long)k * a.z.sp;
-    const int rows = a.to ? a.z.rp : a.z.rows, cols = a.to ? a.z.cp : a.z.cols;
-    _Float16* const to = a.to + k * a.x_batch;
-    typedef Staged<P, float, NW> Out;
-    static_assert(Out::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
-    constexpr int AT_ONCE = 4;
+    // in place: what the sums are to be. Columns and rows past the matrix stand in for the last ones where something is read.
+    const int c0 = tm * P::BM, r0 = tn * P::BN, cl = c0 + P::wave_m() + P::row_of(), rl = r0 + P::wave_n() + P::col_of();
+    float ec[MT][4];
+    if (TALL) {
 #pragma unroll
-    for (int pass = 0; pass < NT / 2; ++pass) {
-        if (pass) __syncthreads();
+        for (int m = 0; m < MT; ++m) __builtin_memcpy(ec[m], e + min(cl + m * 16, a.z.cp - 4), 16);
+    }
+    constexpr int AHEAD = MT < 4 ? MT : 4;
+    Raw4<2> x0[2][AHEAD];
+    auto load = [&](int i) {  // of blocks i * AHEAD on, column by column
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int m = i * AHEAD % MT + u, n = i * AHEAD / MT;
+            x0[i & 1][u].load(was + (long long)min(rl + n * 16, a.z.rp - 1) * a.z.cp + min(cl + m * 16, a.z.cp - 4), x.plane);
+        }
+    };
+    float er[NT];
+    if (!TALL) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) er[n] = e[min(rl + n * 16, a.z.rp - 1)];
+    }
+    load(0);
+#pragma unroll
+    for (int i = 0; i < MT * NT / AHEAD; ++i) {
+        if (i + 1 < MT * NT / AHEAD) load(i + 1);
+        __builtin_amdgcn_sched_barrier(0);  // so far ahead and no further, which would not fit the registers
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int m = i * AHEAD % MT + u, n = i * AHEAD / MT;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                p.acc[m][n][j] = fmaf(a.a + (TALL ? ec[m][j] : er[n]), x0[i & 1][u].get(j) * a.unlift, p.acc[m][n][j] * a.down);
+        }
+    }
+    if (a.to) {
+        typedef Staged<P, uint16_t, NW, NT> Out;
+        static_assert(Out::BYTES <= 2 * P::LDS, "outputs pass through the operands' LDS");
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            if (part) {
+                lds_barrier();
+                p.anew();
+            }
+            const Out staged;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    uint16_t v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        _Float16 hi, lo;
+                        two_parts(p.acc[m][n][j] * a.lift, hi, lo);
+                        v[j] = __builtin_bit_cast(uint16_t, part ? lo : hi);
+                    }
+                    staged.put(lds, m, n, v);
+                }
+            lds_barrier();
+            uint16_t* const to = (uint16_t*)a.to + k * a.x_batch + (part ? a.plane : 0);
+#pragma unroll
+            for (int i = 0; i < Out::PER; ++i) {
+                if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                int row, col;
+                staged.where(i, 0, row, col);
+                row += r0, col += c0;
+                if (row < a.z.rp && col < a.z.cp) *(u32x4*)(to + (long long)row * a.z.cp + col) = staged.take(lds, i);
+            }
+        }
+        return;
+    }
+    typedef Staged<P, float, NW, 2> Out;
+    static_assert(Out::BYTES <= 2 * P::LDS, "outputs pass through the operands' LDS");
+#pragma unroll
+    for (int pass = 0; pass < Out::PASSES; ++pass) {
+        if (pass) lds_barrier();
+        const Out staged;
 #pragma unroll
         for (int n = 2 * pass; n < 2 * pass + 2; ++n)
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const float v[4] = {p.acc[m][n][0], p.acc[m][n][1], p.acc[m][n][2], p.acc[m][n][3]};
-                Out::put(lds, m, n, v);
+                staged.put(lds, m, n, v);
             }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < Out::PER; i += AT_ONCE) {
-            float x0[AT_ONCE][4], e0[AT_ONCE][4];
-            int r[AT_ONCE], c[AT_ONCE];
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                Out::where(i + u, pass, r[u], c[u]);
-                r[u] += tn * P::BN, c[u] += tm * P::BM;
-                if (r[u] >= rows || c[u] >= cols) continue;
-                load4<2>(was + (long long)r[u] * a.z.cp + c[u], x.plane, x0[u]);
-                if (TALL) __builtin_memcpy(e0[u], e + c[u], 16);
-                else e0[u][0] = e0[u][1] = e0[u][2] = e0[u][3] = e[r[u]];
-            }
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                if (r[u] >= rows || c[u] >= cols) continue;
-                float v[4];
-                const u32x4 w = Out::take(lds, i + u);
-                __builtin_memcpy(v, &w, 16);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = fmaf(a.a + e0[u][j], x0[u][j] * a.unlift, v[j] * a.down);
-                if (a.to) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] *= a.lift;
-                    store4<2>(to + (long long)r[u] * a.z.cp + c[u], a.plane, v);
-                } else if (type == IODF_T_F32) {
-                    deliver<float>(target, k, r[u], c[u], cols - c[u], v);
-                } else if (type == IODF_T_BF16) {
-                    deliver<__bf16>(target, k, r[u], c[u], cols - c[u], v);
-                } else {
-                    deliver<_Float16>(target, k, r[u], c[u], cols - c[u], v);
-                }
-            }
-        }
+        lds_barrier();
+        if (type == IODF_T_F32) deliver<float, Out>(target, k, a.z, r0, c0, pass, lds);
+        else if (type == IODF_T_BF16) deliver<__bf16, Out>(target, k, a.z, r0, c0, pass, lds);
+        else deliver<_Float16, Out>(target, k, a.z, r0, c0, pass, lds);
     }
+}
+
+// A square product's tiles, and how many workgroups go through them piece by piece (0: one to a tile).
+struct Cut {
+    int edge, tiles, pieces;
+};
+
+Cut cut_of(long long count, int s, int kts, int products) {
+    if (const char* f = getenv("ORTH_CUT")) { int e, q; sscanf(f, "%d,%d", &e, &q); return {e, (s + e - 1) / e, q}; }
+    Cut best{};
+    float least = 0.f;
+    for (const int edge : {256, 128, 64}) {
+        const int n = (s + edge - 1) / edge;
+        const long long tiles = count * n * (n + 1) / 2, units = tiles * kts;
+        const int at_once = edge == 256 ? 256 : 512;
+        const float step = edge == 256 ? 1.1f : edge == 128 ? 0.8f : 0.6f, out = 8e-6f * edge * edge;  // microseconds, of a tile along the sum; megabytes
+        auto take = [&](float t, int pieces) {
+            if (!best.edge || t < least) least = t, best = {edge, n, pieces};
+        };
+        take(4.f + step * kts * products * ((tiles + at_once - 1) / at_once), 0);
+        if (edge == 64) continue;
+        const int pieces = (int)std::min<long long>(at_once, std::max<long long>(1, units / 4));
+        take(10.f + step * products * ((units + pieces - 1) / pieces) + 0.3f * out * (tiles + pieces), pieces);
+    }
+    return best;
 }
 
 struct OrthPlan {
     Shape z;
     bool tall, parts;          // parts: three products
-    int square_edge, apply_edge;
+    Cut first, second;
+    int apply_edge;
     int parts_of_norm;
-    size_t sums, x0, x1, o, b, d, e, bytes;
+    size_t sums, x0, x1, o, b, d, e, pieces, bytes;
 };
 
 OrthPlan orth_plan(long long count, int rows, int cols, int type) {
@@ -363,9 +524,9 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     p.tall = rows > cols;
     p.parts = type != IODF_T_BF16;
     auto tiles = [&](long long n, int e) { return (n + e - 1) / e; };
-    auto square = [&](int e) { return count * tiles(p.z.s, e) * (tiles(p.z.s, e) + 1) / 2; };
     auto apply = [&](int e) { return count * tiles(rows, e) * tiles(cols, e); };
-    p.square_edge = square(256) >= 200 ? 256 : square(128) >= 200 ? 128 : 64;
+    p.first = cut_of(count, p.z.s, (p.tall ? p.z.rp : p.z.cp) / PK, p.parts ? 3 : 1);
+    p.second = cut_of(count, p.z.s, p.z.sp / PK, p.parts ? 3 : 1);
     p.apply_edge = apply(256) >= 200 ? 256 : apply(128) >= 200 ? 128 : 64;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -378,21 +539,30 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     p.sums = take((size_t)count * p.parts_of_norm * 8);
     p.x0 = take(x), p.x1 = take(x), p.o = take(s), p.b = take(s);
     p.d = take((size_t)count * p.z.sp * 4), p.e = take((size_t)count * p.z.sp * 4);
+    size_t most = 0;
+    for (const Cut& c : {p.first, p.second})
+        if (c.pieces) most = std::max(most, (size_t)(count * c.tiles * (c.tiles + 1) / 2 + c.pieces) * c.edge * c.edge * 4);
+    p.pieces = take(most);
     p.bytes = at;
     return p;
 }
 
 template <int MW, int NW, int MT, int NT, bool SUMS, bool SECOND, int PAIRS>
-void square_with(SquareArgs a, int count, int s, hipStream_t st) {
-    constexpr int E = MW * MT * 16;
-    a.tiles = (s + E - 1) / E;
-    k_square<MW, NW, MT, NT, SUMS, SECOND, PAIRS><<<dim3((unsigned)(a.tiles * (a.tiles + 1) / 2), count), MW * NW * 64, 0, st>>>(a);
+void square_with(SquareArgs a, const Cut& cut, int count, hipStream_t st) {
+    const int per = cut.tiles * (cut.tiles + 1) / 2;
+    a.tiles = cut.tiles, a.pieces = cut.pieces, a.units = (long long)count * per * a.kts;
+    if (cut.pieces == 0) {
+        k_square<MW, NW, MT, NT, SUMS, SECOND, PAIRS><<<dim3((unsigned)per, count), MW * NW * 64, 0, st>>>(a);
+        return;
+    }
+    k_square_piece<MW, NW, MT, NT, SUMS, PAIRS><<<(unsigned)cut.pieces, MW * NW * 64, 0, st>>>(a);
+    k_square_join<MW, NW, MT, NT, SECOND, PAIRS><<<(unsigned)(count * per * MW * NW), 64, 0, st>>>(a);
 }
 template <bool SUMS, bool SECOND, int PAIRS>
-void square(const SquareArgs& a, int edge, int count, int s, hipStream_t st) {
-    if (edge == 256) square_with<2, 4, 8, 4, SUMS, SECOND, PAIRS>(a, count, s, st);
-    else if (edge == 128) square_with<2, 2, 4, 4, SUMS, SECOND, PAIRS>(a, count, s, st);
-    else square_with<2, 2, 2, 2, SUMS, SECOND, PAIRS>(a, count, s, st);
+void square(const SquareArgs& a, const Cut& cut, int count, hipStream_t st) {
+    if (cut.edge == 256) square_with<2, 4, 8, 4, SUMS, SECOND, PAIRS>(a, cut, count, st);
+    else if (cut.edge == 128) square_with<2, 2, 4, 4, SUMS, SECOND, PAIRS>(a, cut, count, st);
+    else square_with<2, 2, 2, 2, SUMS, SECOND, PAIRS>(a, cut, count, st);
 }
 
 template <int MW, int NW, int MT, int NT, bool TALL, int PAIRS>
@@ -436,12 +606,12 @@ void polynomials(const OrthPlan& p, const OrthSteps& s, char* work, const Target
         q.x = {(const uint16_t*)x, plane, p.z.cp, TALL ? p.z.cp : p.z.rp, TALL ? p.z.rp : p.z.cp};
         q.x_batch = xn, q.sp = p.z.sp, q.d = d, q.e = e, q.plane = square_n * p.z.count;
         q.kts = (TALL ? p.z.rp : p.z.cp) / PK;
-        q.down = 1.f / (xl * xl), q.lift = ol, q.out = o;
-        square<TALL, false, PAIRS>(q, p.square_edge, p.z.count, p.z.s, st);
+        q.down = 1.f / (xl * xl), q.lift = ol, q.out = o, q.parts = (float*)(work + p.pieces);
+        square<TALL, false, PAIRS>(q, p.first, p.z.count, st);
         q.x = {(const uint16_t*)o, square_n * p.z.count, p.z.sp, p.z.sp, p.z.sp};
         q.x_batch = square_n, q.kts = p.z.sp / PK;
         q.down = 1.f / (ol * ol), q.unlift = 1.f / ol, q.lift = bl, q.b = s.b[i], q.c = s.c[i], q.out = b;
-        square<false, true, PAIRS>(q, p.square_edge, p.z.count, p.z.s, st);
+        square<false, true, PAIRS>(q, p.second, p.z.count, st);
         ApplyArgs a{};
         a.x = {(const uint16_t*)x, plane, p.z.cp, TALL ? p.z.rp : p.z.cp, TALL ? p.z.cp : p.z.rp};
         a.b = {(const uint16_t*)b, square_n * p.z.count, p.z.sp, p.z.sp, p.z.sp};

@@ -54,6 +54,20 @@ __device__ __forceinline__ void wait_vm() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
 }
 
+// A barrier that waits for LDS only: stores on their way to memory are left there.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// An address that is the same in all lanes, in scalar registers also where the compiler does not see that it is.
+template <typename T>
+__device__ __forceinline__ T* uniform(T* p) {
+    const uint64_t a = (uint64_t)(uintptr_t)p;
+    return (T*)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)a));
+}
+
 // One operand's way through LDS: W rows (or columns) of a tile, THREADS threads.
 template <int W, int THREADS, bool SUMS>
 struct Lane {
@@ -135,6 +149,14 @@ struct Products {
             for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
+    // What has been computed from acc is not kept for what comes: it is computed again, since it would not fit the registers.
+    __device__ __forceinline__ void anew() {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(acc[m][n]));
+    }
+
     // Tiles kt0 .. kt1 - 1 (kt1 > kt0) along k, of outputs from (m0, n0) on. Ends with a barrier: LDS is free then.
     __device__ __forceinline__ void run(const Side& a, const Side& b, int m0, int n0, int kt0, int kt1, uint16_t* lds) {
         Lane<BM, THREADS, ASUMS> la;
@@ -151,8 +173,8 @@ struct Products {
         const uint16_t *ca, *cb;
         unsigned left_a, left_b;
         auto next = [&] {
-            ca = Lane<BM, THREADS, ASUMS>::corner(a, m0, PAIRS > 1 && pair == 2, kt);
-            cb = Lane<BN, THREADS, BSUMS>::corner(b, n0, PAIRS > 1 && pair == 1, kt);
+            ca = uniform(Lane<BM, THREADS, ASUMS>::corner(a, m0, PAIRS > 1 && pair == 2, kt));
+            cb = uniform(Lane<BN, THREADS, BSUMS>::corner(b, n0, PAIRS > 1 && pair == 1, kt));
             left_a = a.depth - 1 - kt * PK, left_b = b.depth - 1 - kt * PK;
             if (++kt == kt1) kt = kt0, ++pair;
         };
@@ -221,53 +243,50 @@ struct Products {
             }
             buf ^= STAGE;
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        lds_barrier();
     }
 };
 
 // A workgroup's outputs on their way to memory: what lanes hold as four neighbours of a row here and there goes through LDS and comes out as whole rows, sixteen
-// bytes to a lane. Output rows are the products' columns n, output columns their rows m. Two block columns of all waves at a time, pass by pass: NW * 32 rows of BM.
-// Chunks of sixteen bytes are moved about by their row, so that the 32 rows that a wave writes together cover all banks.
-template <class P, typename E, int NW>
+// bytes to a lane. Output rows are the products' columns n, output columns their rows m. N of the NT block columns of all waves at a time, pass by pass.
+// Chunks of sixteen bytes are moved about by their row, so that the rows that a wave writes together cover all banks.
+template <class P, typename E, int NW, int N>
 struct Staged {
-    static constexpr int ROWS = NW * 32, CHUNKS = P::BM * (int)sizeof(E) / 16, PER = ROWS * CHUNKS / P::THREADS, OF = 16 / (int)sizeof(E);
-    static constexpr int BYTES = ROWS * CHUNKS * 16;
-    // block (m, n); n's own pass is n / 2
-    static __device__ __forceinline__ void put(void* lds, int m, int n, const E (&v)[4]) {
-        const int row = P::wave_n() / P::NT * 2 + n % 2 * 16 + P::col_of(), c = P::wave_m() + m * 16 + P::row_of();
-        __builtin_memcpy((char*)lds + (row * CHUNKS + ((c / OF) ^ (row & (CHUNKS - 1) & 31))) * 16 + c % OF * sizeof(E), v, 4 * sizeof(E));
+    // Of its own for every use: what one has computed for its places is not kept in registers for the next.
+    unsigned tid;
+    __device__ __forceinline__ Staged() : tid(threadIdx.x) { asm volatile("" : "+v"(tid)); }
+    static constexpr int ROWS = NW * N * 16, CHUNKS = P::BM * (int)sizeof(E) / 16, PER = ROWS * CHUNKS / P::THREADS, OF = 16 / (int)sizeof(E);
+    static constexpr int BYTES = ROWS * CHUNKS * 16, PASSES = P::NT / N;
+    static __device__ __forceinline__ int place(int row, int chunk) { return (row * CHUNKS + (chunk ^ (row & (CHUNKS - 1) & 31))) * 16; }
+    // block (m, n), in pass n / N
+    __device__ __forceinline__ void put(void* lds, int m, int n, const E (&v)[4]) const {
+        const int row = P::wave_n() / P::NT * N + n % N * 16 + (tid & 15), c = P::wave_m() + m * 16 + (tid & 63) / 16 * 4;
+        __builtin_memcpy((char*)lds + place(row, c / OF) + c % OF * sizeof(E), v, 4 * sizeof(E));
     }
     // chunk i of the thread's in a pass: its row and first column among the workgroup's outputs, and what it holds
-    static __device__ __forceinline__ void where(int i, int pass, int& row, int& col) {
-        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
-        row = (r / 32) * (P::NT * 16) + pass * 32 + r % 32;
+    __device__ __forceinline__ void where(int i, int pass, int& row, int& col) const {
+        const int k = i * P::THREADS + tid, r = k / CHUNKS;
+        row = r / (N * 16) * (P::NT * 16) + pass * (N * 16) + r % (N * 16);
         col = k % CHUNKS * OF;
     }
-    static __device__ __forceinline__ u32x4 take(const void* lds, int i) {
-        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
-        return *(const u32x4*)((const char*)lds + (r * CHUNKS + ((k % CHUNKS) ^ (r & (CHUNKS - 1) & 31))) * 16);
+    __device__ __forceinline__ u32x4 take(const void* lds, int i) const {
+        const int k = i * P::THREADS + tid, r = k / CHUNKS;
+        return *(const u32x4*)((const char*)lds + place(r, k % CHUNKS));
     }
-};
-
-// The same for the mirror image: output rows are the products' rows m, output columns their columns n. Two block rows of all waves at a time.
-template <class P, int MW>
-struct StagedAcross {
-    static constexpr int ROWS = MW * 32, CHUNKS = P::BN / 4, PER = ROWS * CHUNKS / P::THREADS, BYTES = ROWS * CHUNKS * 16;
-    static __device__ __forceinline__ void put(void* lds, int m, int n, const float (&v)[4]) {
-        const int row = P::wave_m() / P::MT * 2 + m % 2 * 16 + P::row_of(), c = P::wave_n() + n * 16 + P::col_of();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) ((float*)lds)[((row + j) * CHUNKS + ((c / 4) ^ ((row + j) & (CHUNKS - 1) & 31))) * 4 + c % 4] = v[j];
+    // The mirror image of 16-bit outputs, in one pass (N = NT), by the transposing read: eight neighbours of a row, which is one of the products' rows m.
+    static constexpr int ACROSS = ROWS * P::BM / 8 / P::THREADS;
+    __device__ __forceinline__ void where_across(int i, int& row, int& col) const {
+        const int lane = tid & 63, block = i * (P::THREADS / 64) + (tid >> 6);
+        row = block % (P::BM / 16) * 16 + (lane & 15);
+        col = block / (P::BM / 16) * 32 + (lane >> 4) * 8;
     }
-    static __device__ __forceinline__ void where(int i, int pass, int& row, int& col) {
-        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
-        row = (r / 32) * (P::MT * 16) + pass * 32 + r % 32;
-        col = k % CHUNKS * 4;
-    }
-    static __device__ __forceinline__ u32x4 take(const void* lds, int i) {
-        const int k = i * P::THREADS + threadIdx.x, r = k / CHUNKS;
-        return *(const u32x4*)((const char*)lds + (r * CHUNKS + ((k % CHUNKS) ^ (r & (CHUNKS - 1) & 31))) * 16);
+    __device__ __forceinline__ s16x8 take_across(const void* lds, int i) const {
+        const int lane = tid & 63, block = i * (P::THREADS / 64) + (tid >> 6);
+        const int m = block % (P::BM / 16) * 16 + (lane & 3) * 4, n = block / (P::BM / 16) * 32 + (lane >> 4) * 8 + (lane >> 2 & 3);
+        union { s16x4 h[2]; s16x8 v; } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((const char*)lds + place(n, m / 8) + m % 8 * 2));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((const char*)lds + place(n + 4, m / 8) + m % 8 * 2));
+        return u.v;
     }
 };
 
@@ -309,18 +328,21 @@ __device__ __forceinline__ void get_quad(const T* from, int n, float (&v)[4]) {
     for (int j = 0; j < 4; ++j) v[j] = (float)t[j];
 }
 
-// Which tile of a grid of tm x tn a workgroup takes. Workgroups go round the eight dies (each with an L2 of its own) in turn; a die gets neighbours,
-// in bands four tiles high, so that a panel of either operand is fetched into as few L2s as may be.
+// Workgroups go round the eight dies (each with an L2 of its own) in turn: numbers with which a die gets neighbours.
+__device__ __forceinline__ unsigned by_die(unsigned b, unsigned all) {
+    const unsigned share = all / 8;
+    return b < share * 8 ? b % 8 * share + b / 8 : b;
+}
+// Which tile of a grid of tm x tn a workgroup takes, in bands four tiles high, so that a panel of either operand is fetched into as few L2s as may be.
 __device__ __forceinline__ void place_tile(unsigned b, unsigned all, unsigned tm, unsigned tn, int& m, int& n) {
-    const unsigned share = all / 8, l = b < share * 8 ? b % 8 * share + b / 8 : b;
+    const unsigned l = by_die(b, all);
     const unsigned band = l / (4 * tn), in = l - band * 4 * tn, high = min(4u, tm - band * 4);
     m = (int)(band * 4 + in % high);
     n = (int)(in / high);
 }
 
-// The same for the tiles on and below the diagonal of a square of n x n, in bands eight tiles high.
-__device__ __forceinline__ void place_triangle(unsigned b, unsigned all, unsigned n, int& i, int& j) {
-    const unsigned share = all / 8, l = b < share * 8 ? b % 8 * share + b / 8 : b;
+// Tile l of those on and below the diagonal of a square of n x n, in bands eight tiles high.
+__device__ __forceinline__ void place_triangle(unsigned l, unsigned n, int& i, int& j) {
     unsigned r0 = 0;
     while (r0 + 8 < n && (r0 + 8) * (r0 + 9) / 2 <= l) r0 += 8;
     const unsigned high = min(8u, n - r0), in = l - r0 * (r0 + 1) / 2;
