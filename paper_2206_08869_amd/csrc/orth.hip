@@ -12,8 +12,6 @@
 // A and A^2 are symmetric: only tiles on and below the diagonal are computed, and stored twice.
 #include <algorithm>
 #include <cmath>
-#include <cstdio>
-#include <cstdlib>
 
 #include "products.h"
 #include "step.h"
@@ -156,7 +154,7 @@ struct Raw4 {
 template <class P, int MW, int NW, bool SECOND, int PAIRS>
 __device__ __forceinline__ void finish_square(const SquareArgs& a, P& p, int k, int m0, int n0, bool mirror, uint16_t* lds) {
     constexpr int MT = P::MT, NT = P::NT;
-    constexpr int PARTS = PAIRS > 1 ? 2 : 1, AHEAD = MT < 4 ? MT : 4;
+    constexpr int PARTS = PAIRS > 1 ? 2 : 1, AHEAD = MT % 4 == 0 ? 4 : MT % 3 == 0 ? 3 : MT;
     typedef Staged<P, uint16_t, NW, NT> Out;
     static_assert(Out::BYTES <= 2 * P::LDS, "outputs pass through the operands' LDS");
     const long long square = (long long)a.sp * a.sp;
@@ -319,16 +317,22 @@ __global__ __launch_bounds__(64) void k_square_join(const SquareArgs a) {
     P p;
     const int first = (int)piece_of(a, (long long)tile * a.kts), last = (int)piece_of(a, (tile + 1ll) * a.kts - 1);
     const f32x4* from = (const f32x4*)a.parts + ((long long)(first + tile) * WAVES + wave) * (MT * NT * 64) + threadIdx.x;
+    constexpr int PART = WAVES * MT * NT * 64, AT_ONCE = 64 / (MT * NT);  // parts in flight, 256 registers
+    p.clear();
+    for (int w = first; w <= last; w += AT_ONCE, from += AT_ONCE * PART) {
+        f32x4 v[AT_ONCE][MT * NT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (w + u <= last) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) p.acc[m][n] = from[(m * NT + n) * 64];
-    for (int w = first + 1; w <= last; ++w) {
-        from += WAVES * MT * NT * 64;
+                for (int i = 0; i < MT * NT; ++i) v[u][i] = from[u * PART + i * 64];
+            }
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (w + u <= last) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) p.acc[m][n] += from[(m * NT + n) * 64];
+                for (int i = 0; i < MT * NT; ++i) p.acc[i / NT][i % NT] += v[u][i];
+            }
     }
     finish_square<P, 1, 1, SECOND, PAIRS>(a, p, k, ti * (MW * P::BM) + wave / NW * P::BM, tj * (NW * P::BN) + wave % NW * P::BN, ti != tj, lds);
 }
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const
 #pragma unroll
         for (int m = 0; m < MT; ++m) __builtin_memcpy(ec[m], e + min(cl + m * 16, a.z.cp - 4), 16);
     }
-    constexpr int AHEAD = MT < 4 ? MT : 4;
+    constexpr int AHEAD = MT % 4 == 0 ? 4 : MT % 3 == 0 ? 3 : MT;
     Raw4<2> x0[2][AHEAD];
     auto load = [&](int i) {  // of blocks i * AHEAD on, column by column
 #pragma unroll
@@ -488,22 +492,28 @@ struct Cut {
     int edge, tiles, pieces;
 };
 
-Cut cut_of(long long count, int s, int kts, int products) {
-    if (const char* f = getenv("ORTH_CUT")) { int e, q; sscanf(f, "%d,%d", &e, &q); return {e, (s + e - 1) / e, q}; }
+Cut cut_of(long long count, int s, int kts, int products, bool sums) {
     Cut best{};
     float least = 0.f;
-    for (const int edge : {256, 128, 64}) {
+    auto take = [&](float t, const Cut& c) {
+        if (!best.edge || t < least) least = t, best = c;
+    };
+    const float steps = (float)kts * products;
+    for (const int edge : {256, 192, 64}) {  // whole tiles
         const int n = (s + edge - 1) / edge;
+        const float tiles = (float)count * n * (n + 1) / 2;
+        if (edge == 64) take(3.f + steps * std::max(0.5f, 0.23f * tiles / 256.f), {edge, n, 0});
+        else take(15.f + (edge == 256 ? 1.13f : 0.7f) * steps * std::ceil(tiles / 256.f), {edge, n, 0});
+    }
+    for (const int edge : {256, 128}) {  // pieces
+        const int n = (s + edge - 1) / edge, most = edge == 256 ? 256 : 512;
         const long long tiles = count * n * (n + 1) / 2, units = tiles * kts;
-        const int at_once = edge == 256 ? 256 : 512;
-        const float step = edge == 256 ? 1.1f : edge == 128 ? 0.8f : 0.6f, out = 8e-6f * edge * edge;  // microseconds, of a tile along the sum; megabytes
-        auto take = [&](float t, int pieces) {
-            if (!best.edge || t < least) least = t, best = {edge, n, pieces};
-        };
-        take(4.f + step * kts * products * ((tiles + at_once - 1) / at_once), 0);
-        if (edge == 64) continue;
-        const int pieces = (int)std::min<long long>(at_once, std::max<long long>(1, units / 4));
-        take(10.f + step * products * ((units + pieces - 1) / pieces) + 0.3f * out * (tiles + pieces), pieces);
+        for (int pieces = most; pieces >= 8; pieces /= 2) {
+            if (pieces > units || pieces < tiles / 2) continue;
+            const float step = edge == 256 ? 1.13f : (sums ? 0.75f : 0.45f) * (pieces > 256 ? 2.f : pieces > 128 ? 1.3f : 1.f);
+            const float parts = (float)pieces / tiles + 1.f, moved = (float)(pieces + tiles) * edge * edge * 8e-6f;
+            take(step * products * std::ceil((float)units / pieces) + 10.f + 0.4f * parts * edge / 128 + 0.15f * moved, {edge, n, pieces});
+        }
     }
     return best;
 }
@@ -525,9 +535,9 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     p.parts = type != IODF_T_BF16;
     auto tiles = [&](long long n, int e) { return (n + e - 1) / e; };
     auto apply = [&](int e) { return count * tiles(rows, e) * tiles(cols, e); };
-    p.first = cut_of(count, p.z.s, (p.tall ? p.z.rp : p.z.cp) / PK, p.parts ? 3 : 1);
-    p.second = cut_of(count, p.z.s, p.z.sp / PK, p.parts ? 3 : 1);
-    p.apply_edge = apply(256) >= 200 ? 256 : apply(128) >= 200 ? 128 : 64;
+    p.first = cut_of(count, p.z.s, (p.tall ? p.z.rp : p.z.cp) / PK, p.parts ? 3 : 1, p.tall);
+    p.second = cut_of(count, p.z.s, p.z.sp / PK, p.parts ? 3 : 1, false);
+    p.apply_edge = apply(256) >= 130 ? 256 : apply(128) >= 200 ? 128 : 64;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;
@@ -547,22 +557,24 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     return p;
 }
 
-template <int MW, int NW, int MT, int NT, bool SUMS, bool SECOND, int PAIRS>
+template <bool WHOLE, int MW, int NW, int MT, int NT, bool SUMS, bool SECOND, int PAIRS>
 void square_with(SquareArgs a, const Cut& cut, int count, hipStream_t st) {
     const int per = cut.tiles * (cut.tiles + 1) / 2;
     a.tiles = cut.tiles, a.pieces = cut.pieces, a.units = (long long)count * per * a.kts;
-    if (cut.pieces == 0) {
+    if constexpr (WHOLE) {
         k_square<MW, NW, MT, NT, SUMS, SECOND, PAIRS><<<dim3((unsigned)per, count), MW * NW * 64, 0, st>>>(a);
-        return;
+    } else {
+        k_square_piece<MW, NW, MT, NT, SUMS, PAIRS><<<(unsigned)cut.pieces, MW * NW * 64, 0, st>>>(a);
+        k_square_join<MW, NW, MT, NT, SECOND, PAIRS><<<(unsigned)(count * per * MW * NW), 64, 0, st>>>(a);
     }
-    k_square_piece<MW, NW, MT, NT, SUMS, PAIRS><<<(unsigned)cut.pieces, MW * NW * 64, 0, st>>>(a);
-    k_square_join<MW, NW, MT, NT, SECOND, PAIRS><<<(unsigned)(count * per * MW * NW), 64, 0, st>>>(a);
 }
 template <bool SUMS, bool SECOND, int PAIRS>
 void square(const SquareArgs& a, const Cut& cut, int count, hipStream_t st) {
-    if (cut.edge == 256) square_with<2, 4, 8, 4, SUMS, SECOND, PAIRS>(a, cut, count, st);
-    else if (cut.edge == 128) square_with<2, 2, 4, 4, SUMS, SECOND, PAIRS>(a, cut, count, st);
-    else square_with<2, 2, 2, 2, SUMS, SECOND, PAIRS>(a, cut, count, st);
+    if (cut.pieces && cut.edge == 256) square_with<false, 2, 4, 8, 4, SUMS, SECOND, PAIRS>(a, cut, count, st);
+    else if (cut.pieces) square_with<false, 2, 2, 4, 4, SUMS, SECOND, PAIRS>(a, cut, count, st);
+    else if (cut.edge == 256) square_with<true, 2, 4, 8, 4, SUMS, SECOND, PAIRS>(a, cut, count, st);
+    else if (cut.edge == 192) square_with<true, 2, 4, 6, 3, SUMS, SECOND, PAIRS>(a, cut, count, st);
+    else square_with<true, 2, 2, 2, 2, SUMS, SECOND, PAIRS>(a, cut, count, st);
 }
 
 template <int MW, int NW, int MT, int NT, bool TALL, int PAIRS>

@@ -92,7 +92,7 @@ struct Lane {
     }
     // Where chunk c of row r lies, and which chunk lies at place c. Thirty-two lanes read 32 bytes each of rows r .. r + 3 and r + 8 .. r + 11 together: 64
     // bytes further a row and 32 every eight rows, they cover all banks.
-    static __device__ __forceinline__ int chunk(int r, int c) { return c ^ (PER >= 16 ? (r & 3) << 2 : (r & 2) << 1) ^ (r >> 2 & 2); }
+    static __device__ __forceinline__ int chunk(int r, int c) { return c ^ (PER % 16 == 0 ? (r & 3) << 2 : (r & 2) << 1) ^ (r >> 2 & 2); }
     // tile kt (of the plane `part`): its loads i0 .. i1 - 1, to `lds`, this wave's place in the tile
     static __device__ __forceinline__ const uint16_t* corner(const Side& s, int first, int part, int kt) {
         return s.p + part * s.plane + (SUMS ? (long long)kt * PK * s.ld + first : (long long)first * s.ld + kt * PK);
@@ -257,7 +257,8 @@ struct Staged {
     __device__ __forceinline__ Staged() : tid(threadIdx.x) { asm volatile("" : "+v"(tid)); }
     static constexpr int ROWS = NW * N * 16, CHUNKS = P::BM * (int)sizeof(E) / 16, PER = ROWS * CHUNKS / P::THREADS, OF = 16 / (int)sizeof(E);
     static constexpr int BYTES = ROWS * CHUNKS * 16, PASSES = P::NT / N;
-    static __device__ __forceinline__ int place(int row, int chunk) { return (row * CHUNKS + (chunk ^ (row & (CHUNKS - 1) & 31))) * 16; }
+    static constexpr int MOVE = (CHUNKS & -CHUNKS) < 32 ? (CHUNKS & -CHUNKS) - 1 : 31;
+    static __device__ __forceinline__ int place(int row, int chunk) { return (row * CHUNKS + (chunk ^ (row & MOVE))) * 16; }
     // block (m, n), in pass n / N
     __device__ __forceinline__ void put(void* lds, int m, int n, const E (&v)[4]) const {
         const int row = P::wave_n() / P::NT * N + n % N * 16 + (tid & 15), c = P::wave_m() + m * 16 + (tid & 63) / 16 * 4;

@@ -525,3 +525,20 @@ def test_plain_entries_give_the_bits_of_the_torch_calls(name):
     work = t.empty(need, dtype=t.uint8, device="cuda")
     iodf.iodf_muon_step(a, work.data_ptr(), need, st)
     assert t.equal(w1, w2) and t.equal(m1, m2)
+
+
+@pytest.mark.parametrize("count,rows,cols,name", [(8, 1344, 1400, "bf16"), (1, 700, 8200, "bf16"), (3, 1500, 1344, "f32"), (1, 4100, 4096, "bf16")])
+def test_orthogonalise_every_kind_of_tile(count, rows, cols, name):
+    """Shapes whose square products are cut into tiles of 192 and 256 and into pieces of tiles, against 64 bits on the card."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(4)
+    g = t.randn((count, rows, cols), generator=gen, device="cuda") * t.exp(0.4 * t.randn((cols,), generator=gen, device="cuda"))
+    r = iodf.orthogonalise(g, dtype=dtype(name))
+    for k in {0, count - 1}:
+        x = g[k].double() / g[k].double().norm()
+        x = x.t().contiguous() if rows > cols else x
+        for _ in range(5):
+            m = x @ x.t().contiguous()
+            x = 3.4445 * x + (-4.7750 * m + 2.0315 * m @ m) @ x
+        x = x.t() if rows > cols else x
+        assert (r[k].double() - x).norm() <= {"bf16": 2.0 ** -9 + 4 * 2.0 ** -12, "f32": 4e-6}[name] * x.norm()
