@@ -15,7 +15,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr long long kPieceBytes = 512ll << 20;  // of g
-constexpr int kMaxima = 256;                    // partial maxima of a tensor
+constexpr int kMaxima = 1024;                   // partial maxima of a tensor, at most
 
 inline long long up(long long n, long long d) { return (n + d - 1) / d * d; }
 
@@ -51,27 +51,34 @@ struct MaxArgs {
     const float* dlse;
 };
 
-// blockIdx.y: 0 u, 1 W, 2 what g is made of
+// Of each workgroup's share; blockIdx.y: 0 what g is made of, 1 u, 2 W.
 __global__ __launch_bounds__(256) void k_maxima(const MaxArgs a, float* maxima) {
     __shared__ float meet[4];
     const int what = blockIdx.y;
     float m = 0.f;
-    if (what == 2) {
+    if (what == 0) {
         for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < a.rows; t += (long long)gridDim.x * 256) {
             if (a.live && !a.live[t]) continue;
             const float d = a.dloss ? a.dloss[t] : 0.f;
             m = finite_max(finite_max(m, d), a.dlse ? a.dlse[t] + d : d);
         }
-    } else if (what == 0 ? a.u : a.w) {
-        const float* const x = what == 0 ? a.u : a.w;
-        const long long stride = what == 0 ? a.u_stride : a.w_stride, rows = what == 0 ? a.rows : a.classes;
-        for (long long t = blockIdx.x; t < rows; t += gridDim.x) {
-            if (what == 0 && a.live && !a.live[t]) continue;
-            for (int c = threadIdx.x; c < a.cols; c += 256) m = finite_max(m, x[t * stride + c]);
+    } else {
+        const float* const x = what == 1 ? a.u : a.w;
+        const uint8_t* const live = what == 1 ? a.live : nullptr;
+        const long long stride = what == 1 ? a.u_stride : a.w_stride, rows = what == 1 ? a.rows : a.classes;
+        const int per = (a.cols + 7) / 8;
+        for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (long long)gridDim.x * 256) {
+            const long long t = i / per;
+            const int c = (int)(i - t * per) * 8;
+            if (live && !live[t]) continue;
+            float v[8];
+            load8(x + t * stride + c, a.cols - c, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = finite_max(m, v[j]);
         }
     }
     m = block_max(m, meet);
-    if (threadIdx.x == 0) maxima[what * kMaxima + blockIdx.x] = m;
+    if (threadIdx.x == 0) maxima[what * gridDim.x + blockIdx.x] = m;
 }
 
 // The power of two that takes numbers up to m to just below 2^15.
@@ -85,30 +92,47 @@ __device__ __forceinline__ float lift(float m, float& inverse) {
     return ldexpf(1.f, e);
 }
 
-__global__ __launch_bounds__(256) void k_scales(const float* maxima, int wide, Scales* s) {
-    __shared__ float meet[4];
-    float m[3];
-    for (int k = 0; k < 3; ++k) m[k] = block_max(maxima[k * kMaxima + threadIdx.x], meet);
-    if (threadIdx.x) return;
-    Scales r;
-    r.u = lift(wide ? m[0] : 0.f, r.iu);
-    r.w = lift(wide ? m[1] : 0.f, r.iw);
-    r.g = lift(2.f * m[2], r.ig);
-    *s = r;
-}
+struct ReadyArgs {
+    const void* x[2];      // u and W
+    uint16_t* y[2];        // NULL: stays where it is
+    long long stride[2], rows[2];
+    const uint8_t* live;   // of u's rows
+    int cols, pitch;
+    const float* maxima;   // NULL: no scales
+    int parts, wide;       // partial maxima of a tensor; u's and W's are there too
+    Scales* scales;
+};
 
-// x [rows][cols] -> 16-bit rows of `pitch` with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in two parts of half precision.
+// Rows of `pitch` 16-bit numbers with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in two parts of half precision. And the scales,
+// which every workgroup takes from the maxima by itself.
 template <typename TX>
-__global__ __launch_bounds__(256) void k_ready(const TX* x, long long stride, long long rows, int cols, int pitch, const uint8_t* live,
-                                               const float* scale, uint16_t* y, long long plane) {
-    const int per = pitch / 8;
-    const float by = sizeof(TX) == 4 ? *scale : 1.f;
+__global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
+    __shared__ float meet[4];
+    const int which = blockIdx.y, per = a.pitch / 8;
+    float by = 1.f;
+    if (a.maxima) {
+        float m[3] = {};
+        for (int k = 0; k < (a.wide ? 3 : 1); ++k) {
+            for (int i = threadIdx.x; i < a.parts; i += 256) m[k] = fmaxf(m[k], a.maxima[k * a.parts + i]);
+            m[k] = block_max(m[k], meet);
+        }
+        Scales r;
+        r.g = lift(2.f * m[0], r.ig);
+        r.u = lift(m[1], r.iu);
+        r.w = lift(m[2], r.iw);
+        if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *a.scales = r;
+        by = which ? r.w : r.u;
+    }
+    uint16_t* const y = a.y[which];
+    if (!y) return;
+    const long long rows = a.rows[which], stride = a.stride[which], plane = rows * a.pitch;
+    const uint8_t* const live = which ? nullptr : a.live;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (long long)gridDim.x * 256) {
         const long long t = i / per;
-        const int c = (int)(i - t * per) * 8, n = live && !live[t] ? 0 : cols - c;
-        const Raw8<TX> r = fetch8(x + t * stride + c, n, false);
+        const int c = (int)(i - t * per) * 8, n = live && !live[t] ? 0 : a.cols - c;
+        const Raw8<TX> r = fetch8((const TX*)a.x[which] + t * stride + c, n, false);
         if (sizeof(TX) == 2) {
-            *(u32x4*)(y + t * pitch + c) = u32x4{r.w[0], r.w[1], r.w[2], r.w[3]};
+            *(u32x4*)(y + t * a.pitch + c) = u32x4{r.w[0], r.w[1], r.w[2], r.w[3]};
         } else {
             float v[8];
             widen8(r, v);
@@ -122,14 +146,16 @@ __global__ __launch_bounds__(256) void k_ready(const TX* x, long long stride, lo
             }
             u32x4 w;
             __builtin_memcpy(&w, hi, 16);
-            *(u32x4*)(y + t * pitch + c) = w;
+            *(u32x4*)(y + t * a.pitch + c) = w;
             __builtin_memcpy(&w, lo, 16);
-            *(u32x4*)(y + plane + t * pitch + c) = w;
+            *(u32x4*)(y + plane + t * a.pitch + c) = w;
         }
     }
 }
 
 // ---- logits ----
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct LogitArgs {
     Side w, u;
@@ -142,8 +168,7 @@ struct LogitArgs {
     const Scales* scales;
     const int64_t* target;
     const uint8_t* live;
-    float* tops;         // forward: [tile of classes][rows] largest logit, and the sum of exponentials relative to it
-    float* sums;
+    f32x2* parts;        // forward: [tile of classes][rows] largest logit, and the sum of exponentials relative to it
     float* picked;       // [rows] the target's logit
     const float* lse;    // backward
     const float* dloss;
@@ -235,8 +260,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                 const float mine = meet[(k * P::BN + col) * 2], s = meet[(k * P::BN + col) * 2 + 1];
                 sum += mine > -__builtin_inff() ? s * __builtin_amdgcn_exp2f((mine - top) * kLog2e) : s;
             }
-            a.tops[tm * a.rows + t] = top;
-            a.sums[tm * a.rows + t] = sum;
+            a.parts[tm * a.rows + t] = f32x2{top, sum};
         }
     } else {
         typedef Staged<P, uint16_t, NW, (PAIRS > 1 ? NT / 2 : NT)> Out;
@@ -294,33 +318,36 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     }
 }
 
+// (top, sum of exponentials relative to it) of two sets of logits, of either of which there may be none.
+__device__ __forceinline__ f32x2 merged(f32x2 a, f32x2 b) {
+    const float top = fmaxf(a[0], b[0]), base = top > -__builtin_inff() ? top : 0.f;
+    return f32x2{top, a[1] * __builtin_amdgcn_exp2f((a[0] - base) * kLog2e) + b[1] * __builtin_amdgcn_exp2f((b[0] - base) * kLog2e)};
+}
+
 // The tiles of a row: LANES threads to a row.
 template <int LANES>
-__global__ __launch_bounds__(256) void k_loss_join(long long rows, int tiles, int classes, const float* tops, const float* sums, const float* picked,
-                                                   const int64_t* target, const uint8_t* live, float* loss, float* lse) {
-    __shared__ float meet[2][256];
-    constexpr int ROWS = 256 / LANES;
+__global__ __launch_bounds__(256) void k_loss_join(long long rows, int tiles, int classes, const f32x2* parts, const float* picked, const int64_t* target,
+                                                   const uint8_t* live, float* loss, float* lse) {
+    __shared__ f32x2 meet[256];
+    constexpr int ROWS = 256 / LANES, AT_ONCE = 8;
     const int at = threadIdx.x % ROWS, lane = threadIdx.x / ROWS;
     const long long t = (long long)blockIdx.x * ROWS + at;
-    float top = -__builtin_inff(), sum = 0.f;
+    f32x2 all{-__builtin_inff(), 0.f};
     if (t < rows) {
-        for (int k = lane; k < tiles; k += LANES) top = fmaxf(top, tops[k * rows + t]);
-        meet[0][threadIdx.x] = top;
-    }
-    __syncthreads();
-    if (t < rows) {
-        for (int k = 0; k < LANES; ++k) top = fmaxf(top, meet[0][k * ROWS + at]);
-        for (int k = lane; k < tiles; k += LANES) {
-            const float mine = tops[k * rows + t], s = sums[k * rows + t];
-            sum += mine > -__builtin_inff() ? s * __builtin_amdgcn_exp2f((mine - top) * kLog2e) : s;
+        for (int k = lane; k < tiles; k += AT_ONCE * LANES) {
+            f32x2 v[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) v[i] = k + i * LANES < tiles ? parts[(k + i * LANES) * rows + t] : f32x2{-__builtin_inff(), 0.f};
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) all = merged(all, v[i]);
         }
-        meet[1][threadIdx.x] = sum;
     }
+    meet[threadIdx.x] = all;
     __syncthreads();
     if (lane || t >= rows) return;
-    for (int k = 1; k < LANES; ++k) sum += meet[1][k * ROWS + at];
+    for (int k = 1; k < LANES; ++k) all = merged(all, meet[k * ROWS + at]);
     const bool there = !(live && !live[t]);
-    const float l = there ? top + logf(sum) : 0.f;
+    const float l = there ? all[0] + logf(all[1]) : 0.f;
     lse[t] = l;
     const int64_t w = there ? target[t] : 0;
     loss[t] = !there ? 0.f : w >= 0 && w < classes ? l - picked[t] : __builtin_nanf("");
@@ -437,30 +464,61 @@ __global__ __launch_bounds__(256) void k_zero_rows(TO* out, long long rows, int 
 
 // ---- plans ----
 
-// The edge of square tiles and the slices of the sum.
+// A product's tiles and the slices of its sum.
 struct Cut {
     int edge, slices, per;
 };
-Cut cut_of(long long m, long long n, int kts, int most) {
-    auto tiles = [&](int e) { return ((m + e - 1) / e) * ((n + e - 1) / e); };
-    int edge = 256;
-    if (tiles(256) < 256) edge = 128;
-    if (m <= 64 || n <= 64) edge = 64;
-    long long slices = std::max<long long>(1, 512 / tiles(edge));
-    slices = std::min<long long>({slices, (long long)most, std::max(1, kts / 8)});
-    const int per = (int)((kts + slices - 1) / slices);
-    return {edge, (int)((kts + per - 1) / per), per};
+
+// Microseconds that workgroups of a kind take to a tile (64 along the sum), all of them, on 256 compute units.
+float step_of(int edge, float workgroups) {
+    const float each = std::ceil(workgroups) / 256.f;
+    if (edge == 256) return 1.13f * std::ceil(each);
+    if (edge == 128) return each <= 1.f ? 0.6f : 0.85f * std::ceil(each / 2.f);
+    return std::max(0.5f, 0.23f * each);
+}
+
+// The kind of tile and number of slices of least estimated time. Large tiles read operands less often, small ones and slices fill the chip when outputs are
+// few, slices at the price of their sums' way through memory and of a second launch.
+Cut cut_of(long long m, long long n, int kts, int products, bool kept) {
+    Cut best{};
+    float least = 0.f;
+    const int planes = products > 1 ? 2 : 1;
+    for (const int edge : {256, 128, 64}) {
+        const long long tm = (m + edge - 1) / edge, tn = (n + edge - 1) / edge, tiles = tm * tn;
+        const float read = (float)kts * PK * 2 * planes * (float)(m * tn + n * tm) / 7e6f;
+        for (int slices = 1; slices <= 256 && (slices == 1 || kts / slices >= 2); slices *= 2) {
+            const int per = (kts + slices - 1) / slices;
+            const float outputs = (float)tiles * edge * edge;
+            float t = 8.f + std::max(read, per * products * step_of(edge, (float)tiles * slices));
+            t += slices > 1 || kept ? 5.f + outputs * 8.f * slices / 5e6f : outputs * 4.f / 5e6f;
+            if (!best.edge || t < least) least = t, best = {edge, (kts + per - 1) / per, per};
+        }
+    }
+    return best;
+}
+
+// The kind of tile of the logits: classes x rows, 128 x 64 among them for few rows.
+int logits_edge(long long classes, long long rows, int kts, int products) {
+    int best = 0;
+    float least = 0.f;
+    for (const int edge : {256, 128, 64}) {
+        const float tiles = (float)((classes + edge - 1) / edge) * (float)((rows + edge - 1) / edge);
+        const float t = edge * 0.04f + kts * products * step_of(edge, tiles);
+        if (!best || t < least) least = t, best = edge;
+    }
+    return best;
 }
 
 struct LossPlan {
     bool wide, u_ready, w_ready, scaled;  // 32-bit operands; whether u and W are copied; whether there are scales
     int pitch, kts;
     int edge, tiles;                      // of the logits' tiles, tiles of classes
+    int maxima_parts;
     int planes;
     long long rows_up, piece;
     Cut du, dw;
     // byte offsets into the workspace
-    size_t maxima, scales, u, w, tops, sums, picked, g, du_sums, dw_sums, bytes;
+    size_t maxima, scales, u, w, parts, picked, g, du_sums, dw_sums, bytes;
 };
 
 bool in_place(const void* p, long long stride, int cols, bool wide) { return !wide && cols % PK == 0 && stride % 8 == 0 && stride <= (1 << 22) && ((uintptr_t)p & 15) == 0; }
@@ -475,41 +533,36 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     p.w_ready = !in_place(a.w, a.w_stride, a.cols, p.wide);
     p.scaled = p.wide || (backward && a.type == IODF_T_F16);
     p.rows_up = up(a.rows, 256);
-    auto tiles = [&](int e) { return ((a.rows + e - 1) / e) * ((a.classes + e - 1) / e); };
-    p.edge = a.rows <= 64 ? 64 : tiles(256) >= 256 ? 256 : 128;
-    const int bm = p.edge == 64 ? 128 : p.edge;
-    p.tiles = (a.classes + bm - 1) / bm;
+    p.edge = logits_edge(a.classes, a.rows, p.kts, p.wide ? 3 : 1);
+    p.tiles = (a.classes + p.edge - 1) / p.edge;
+    p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, ((p.wide ? std::max<long long>(a.rows, a.classes) * p.pitch / 8 : a.rows) + 511) / 512));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;
         at += up(bytes, 256);
         return was;
     };
-    if (p.scaled) p.maxima = take(3 * kMaxima * 4), p.scales = take(sizeof(Scales));
+    if (p.scaled) p.maxima = take((size_t)3 * p.maxima_parts * 4), p.scales = take(sizeof(Scales));
     if (p.u_ready) p.u = take((size_t)p.planes * a.rows * p.pitch * 2);
     if (p.w_ready) p.w = take((size_t)p.planes * a.classes * p.pitch * 2);
     if (!backward) {
-        p.tops = take((size_t)p.tiles * a.rows * 4), p.sums = take((size_t)p.tiles * a.rows * 4), p.picked = take((size_t)a.rows * 4);
+        p.parts = take((size_t)p.tiles * a.rows * 8), p.picked = take((size_t)a.rows * 4);
     } else if (a.rows) {
         p.piece = std::max<long long>(256, kPieceBytes / (p.rows_up * 2 * p.planes) / 256 * 256);
         p.piece = std::min(p.piece, up(a.classes, 256));
         p.g = take((size_t)p.planes * p.rows_up * p.piece * 2);
-        p.du = cut_of(a.rows, a.cols, (int)(p.piece / PK), 64);
-        p.dw = cut_of(std::min<long long>(p.piece, a.classes), a.cols, (int)((a.rows + PK - 1) / PK), 64);
+        const long long here = std::min<long long>(p.piece, a.classes);
+        p.du = cut_of(a.cols, a.rows, (int)((here + PK - 1) / PK), p.wide ? 3 : 1, here < a.classes);
+        p.dw = cut_of(a.cols, here, (int)((a.rows + PK - 1) / PK), p.wide ? 3 : 1, false);
         auto sums = [&](const Cut& c, long long rows) { return (size_t)c.slices * up(rows, c.edge) * up(a.cols, c.edge) * 4; };
         if (a.du && (p.du.slices > 1 || p.piece < a.classes)) p.du_sums = take(sums(p.du, a.rows));
-        if (a.dw && p.dw.slices > 1) p.dw_sums = take(sums(p.dw, std::min<long long>(p.piece, a.classes)));
+        if (a.dw && p.dw.slices > 1) p.dw_sums = take(sums(p.dw, here));
     }
     p.bytes = at;
     return p;
 }
 
 unsigned blocks_for(long long threads) { return (unsigned)std::max<long long>(1, std::min<long long>((threads + 255) / 256, 1 << 16)); }
-
-template <typename TX>
-void ready(const void* x, long long stride, long long rows, int cols, const LossPlan& p, const uint8_t* live, const float* scale, uint16_t* y, hipStream_t st) {
-    k_ready<TX><<<blocks_for(rows * (p.pitch / 8)), 256, 0, st>>>((const TX*)x, stride, rows, cols, p.pitch, live, scale, y, rows * p.pitch);
-}
 
 template <typename T, int PAIRS, bool GRAD>
 void logits(const LogitArgs& a, int edge, hipStream_t st) {
@@ -520,7 +573,7 @@ void logits(const LogitArgs& a, int edge, hipStream_t st) {
     };
     if (edge == 256) go(k_logits<T, 2, 4, 8, 4, PAIRS, GRAD>, 256, 256, 512);
     else if (edge == 128) go(k_logits<T, 2, 2, 4, 4, PAIRS, GRAD>, 128, 128, 256);
-    else go(k_logits<T, 4, 1, 2, 4, PAIRS, GRAD>, 128, 64, 256);
+    else go(k_logits<T, 2, 2, 2, 2, PAIRS, GRAD>, 64, 64, 256);
 }
 
 // One piece's part of a gradient; `last`: its slices are joined.
@@ -548,24 +601,22 @@ template <typename TX>
 LogitArgs prepared(const iodf_class_loss& a, const LossPlan& p, char* work, bool backward, hipStream_t st) {
     LogitArgs l{};
     Scales* const s = p.scaled ? (Scales*)(work + p.scales) : nullptr;
+    float* const maxima = s ? (float*)(work + p.maxima) : nullptr;
     if (s) {
-        float* const maxima = (float*)(work + p.maxima);
-        const MaxArgs m{p.wide ? (const float*)a.u : nullptr, p.wide ? (const float*)a.w : nullptr, a.u_stride, a.w_stride, a.rows, a.classes, a.cols,
+        const MaxArgs m{(const float*)a.u, (const float*)a.w, a.u_stride, a.w_stride, a.rows, a.classes, a.cols,
                         a.live, backward ? a.dloss : nullptr, backward ? a.dlse : nullptr};
-        k_maxima<<<dim3(kMaxima, 3), 256, 0, st>>>(m, maxima);
-        k_scales<<<1, 256, 0, st>>>(maxima, p.wide, s);
+        k_maxima<<<dim3(p.maxima_parts, p.wide ? 3 : 1), 256, 0, st>>>(m, maxima);
     }
     l.u = {(const uint16_t*)a.u, 0, a.u_stride, (int)a.rows, (int)a.rows};
     l.w = {(const uint16_t*)a.w, 0, a.w_stride, a.classes, a.classes};
-    if (p.u_ready) {
-        uint16_t* const y = (uint16_t*)(work + p.u);
-        ready<TX>(a.u, a.u_stride, a.rows, a.cols, p, a.live, s ? &s->u : nullptr, y, st);
-        l.u.p = y, l.u.ld = p.pitch, l.u.plane = a.rows * p.pitch;
-    }
-    if (p.w_ready) {
-        uint16_t* const y = (uint16_t*)(work + p.w);
-        ready<TX>(a.w, a.w_stride, a.classes, a.cols, p, nullptr, s ? &s->w : nullptr, y, st);
-        l.w.p = y, l.w.ld = p.pitch, l.w.plane = (long long)a.classes * p.pitch;
+    ReadyArgs r{};
+    r.x[0] = a.u, r.x[1] = a.w, r.stride[0] = a.u_stride, r.stride[1] = a.w_stride, r.rows[0] = a.rows, r.rows[1] = a.classes;
+    r.live = a.live, r.cols = a.cols, r.pitch = p.pitch, r.maxima = maxima, r.parts = p.maxima_parts, r.wide = p.wide, r.scales = s;
+    if (p.u_ready) r.y[0] = (uint16_t*)(work + p.u), l.u.p = r.y[0], l.u.ld = p.pitch, l.u.plane = a.rows * p.pitch;
+    if (p.w_ready) r.y[1] = (uint16_t*)(work + p.w), l.w.p = r.y[1], l.w.ld = p.pitch, l.w.plane = (long long)a.classes * p.pitch;
+    if (s || p.u_ready || p.w_ready) {
+        const long long most = std::max<long long>(p.u_ready ? a.rows : 0, p.w_ready ? a.classes : 0) * (p.pitch / 8);
+        k_ready<TX><<<dim3(std::min(blocks_for(most), 4096u), p.w_ready ? 2 : 1), 256, 0, st>>>(r);
     }
     l.kts = p.kts, l.classes = a.classes, l.all = a.classes, l.rows = a.rows, l.scales = s, l.target = a.target, l.live = a.live;
     return l;
@@ -575,10 +626,14 @@ template <typename TX, typename T, int PAIRS>
 hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
     const LossPlan p = loss_plan(a, false);
     LogitArgs l = prepared<TX>(a, p, work, false, st);
-    l.tops = (float*)(work + p.tops), l.sums = (float*)(work + p.sums), l.picked = (float*)(work + p.picked);
+    l.parts = (f32x2*)(work + p.parts), l.picked = (float*)(work + p.picked);
     logits<T, PAIRS, false>(l, p.edge, st);
-    if (a.rows >= 4096) k_loss_join<4><<<(unsigned)((a.rows + 63) / 64), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.tops, l.sums, l.picked, a.target, a.live, a.loss, a.lse);
-    else k_loss_join<64><<<(unsigned)((a.rows + 3) / 4), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.tops, l.sums, l.picked, a.target, a.live, a.loss, a.lse);
+    auto join = [&](auto kernel, int rows) {
+        kernel<<<(unsigned)((a.rows + rows - 1) / rows), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.parts, l.picked, a.target, a.live, a.loss, a.lse);
+    };
+    if (a.rows < 2048) join(k_loss_join<64>, 4);
+    else if (a.rows < 65536) join(k_loss_join<16>, 16);
+    else join(k_loss_join<4>, 64);
     return hipGetLastError();
 }
 
