@@ -5,6 +5,7 @@
 // the sum of exponentials relative to it; a second kernel joins the tiles of a row. Backward: the logits once more, from which g = (dloss + dlse) exp(s -
 // lse) - dloss [target] goes to memory in 16 bits, piece by piece of the classes; du += g W and dw = g' u are two more products.
 #include <algorithm>
+#include <type_traits>
 
 #include "products.h"
 #include "step.h"
@@ -182,6 +183,133 @@ __device__ __forceinline__ uint16_t bits16(float v) {
     return __builtin_bit_cast(uint16_t, (T)v);
 }
 
+// (top, sum of exponentials relative to it) of two sets of logits, of either of which there may be none.
+__device__ __forceinline__ f32x2 merged(f32x2 a, f32x2 b) {
+    const float top = fmaxf(a[0], b[0]), base = top > -__builtin_inff() ? top : 0.f;
+    return f32x2{top, a[1] * __builtin_amdgcn_exp2f((a[0] - base) * kLog2e) + b[1] * __builtin_amdgcn_exp2f((b[0] - base) * kLog2e)};
+}
+
+// ---- few rows ----
+
+struct FewArgs {
+    const void* w;       // where it lies: any stride and element
+    const void* u;
+    long long w_stride, u_stride;
+    int classes, cols, rows, groups;  // groups: of 32 classes to a workgroup
+    const int64_t* target;
+    f32x2* parts;
+    float* picked;
+};
+
+// Sixteen bytes along k of a row, of which n elements exist.
+template <typename TX>
+__device__ __forceinline__ u32x4 along(const TX* p, int n) {
+    constexpr int E = 16 / (int)sizeof(TX);
+    if (n >= E) return *(const u32x4_any*)p;
+    TX t[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) t[j] = j < n ? p[j] : (TX)0.f;
+    u32x4 w;
+    __builtin_memcpy(&w, t, 16);
+    return w;
+}
+template <typename TX>
+__device__ __forceinline__ f32x4 product(u32x4 w, u32x4 u, f32x4 c) {
+    return Mma<TX>::go(__builtin_bit_cast(s16x8, w), __builtin_bit_cast(s16x8, u), c);
+}
+template <>
+__device__ __forceinline__ f32x4 product<float>(u32x4 w, u32x4 u, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[j]), __uint_as_float(u[j]), c, 0, 0, 0);
+    return c;
+}
+
+// Rows that do not fill a tile, of a table that would have to be copied for tiles: it is read once, as it lies, straight into registers, 32 classes to a workgroup whose four waves share out the
+// columns. NB blocks of 16 rows. Which columns a lane holds is the same for both operands and otherwise of no matter: in 32 bits four neighbours
+// are four products of the 32-bit matrix instruction.
+template <typename TX, int NB>
+__global__ __launch_bounds__(256) void k_few(const FewArgs a) {
+    constexpr int E = 16 / (int)sizeof(TX), STEP = 4 * E, AT_ONCE = NB <= 2 ? 4 : 2, SPAN = STEP * AT_ONCE;
+    __shared__ f32x4 meet[4][2][NB][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, k = lane / 16 * E;
+    f32x2 all[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) all[n] = f32x2{-__builtin_inff(), 0.f};
+    for (int group = 0; group < a.groups; ++group) {
+        const int c0 = (blockIdx.x * a.groups + group) * 32;
+        if (c0 >= a.classes) break;
+        const TX* w[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) w[b] = (const TX*)a.w + min(c0 + b * 16 + r, a.classes - 1) * a.w_stride + k;
+        const TX* u[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) u[n] = (const TX*)a.u + min(n * 16 + r, a.rows - 1) * a.u_stride + k;
+        f32x4 acc[2][NB];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto span = [&](int k0, auto inside) {
+            u32x4 wf[2][AT_ONCE], uf[NB][AT_ONCE];
+#pragma unroll
+            for (int s = 0; s < AT_ONCE; ++s) {
+                const int at = k0 + s * STEP, left = inside ? E : a.cols - at - k;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) wf[b][s] = along(w[b] + at, left);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) uf[n][s] = along(u[n] + at, left);
+            }
+#pragma unroll
+            for (int s = 0; s < AT_ONCE; ++s)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) acc[b][n] = product<TX>(wf[b][s], uf[n][s], acc[b][n]);
+        };
+        int k0 = wave * SPAN;
+        for (; k0 + SPAN <= a.cols; k0 += 4 * SPAN) span(k0, std::true_type());
+        if (k0 < a.cols) span(k0, std::false_type());
+        if (group) __syncthreads();
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) meet[wave][b][n][lane] = acc[b][n];
+        __syncthreads();
+#pragma unroll
+        for (int n = wave; n < NB; n += 4) {  // the waves share out the blocks of rows
+            const int t = n * 16 + r;
+            const long long want = t < a.rows ? a.target[t] - c0 : -1;
+            float v[8], top = -__builtin_inff();
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const f32x4 s = (meet[0][b][n][lane] + meet[1][b][n][lane]) + (meet[2][b][n][lane] + meet[3][b][n][lane]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = b * 16 + lane / 16 * 4 + j;
+                    v[b * 4 + j] = c0 + c < a.classes ? s[j] : -__builtin_inff();
+                    if (want == c && c0 + c < a.classes) a.picked[t] = s[j];
+                    top = fmaxf(top, v[b * 4 + j]);
+                }
+            }
+            const float base = top > -__builtin_inff() ? top : 0.f;
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f((v[j] - base) * kLog2e);
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+                if (i == n) all[i] = merged(all[i], f32x2{top, sum});
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        if (n % 4 != wave) continue;
+        f32x2 v = all[n];
+        v = merged(v, f32x2{__shfl_xor(v[0], 16), __shfl_xor(v[1], 16)});
+        v = merged(v, f32x2{__shfl_xor(v[0], 32), __shfl_xor(v[1], 32)});
+        if (lane < 16 && n * 16 + r < a.rows) a.parts[(long long)blockIdx.x * a.rows + n * 16 + r] = v;
+    }
+}
+
 // Classes are the rows of the matrix instructions, so that a lane holds 4 * MT classes of a row and reduces them in registers.
 template <typename T, int MW, int NW, int MT, int NT, int PAIRS, bool GRAD>
 __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
@@ -316,12 +444,6 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
             }
         }
     }
-}
-
-// (top, sum of exponentials relative to it) of two sets of logits, of either of which there may be none.
-__device__ __forceinline__ f32x2 merged(f32x2 a, f32x2 b) {
-    const float top = fmaxf(a[0], b[0]), base = top > -__builtin_inff() ? top : 0.f;
-    return f32x2{top, a[1] * __builtin_amdgcn_exp2f((a[0] - base) * kLog2e) + b[1] * __builtin_amdgcn_exp2f((b[0] - base) * kLog2e)};
 }
 
 // The tiles of a row: LANES threads to a row.
@@ -485,11 +607,11 @@ Cut cut_of(long long m, long long n, int kts, int products, bool kept) {
     const int planes = products > 1 ? 2 : 1;
     for (const int edge : {256, 128, 64}) {
         const long long tm = (m + edge - 1) / edge, tn = (n + edge - 1) / edge, tiles = tm * tn;
-        const float read = (float)kts * PK * 2 * planes * (float)(m * tn + n * tm) / 7e6f;
+        const float read = (float)kts * PK * 2 * planes * (float)(m * tn + n * tm) / 11e6f;
         for (int slices = 1; slices <= 256 && (slices == 1 || kts / slices >= 2); slices *= 2) {
             const int per = (kts + slices - 1) / slices;
             const float outputs = (float)tiles * edge * edge;
-            float t = 8.f + std::max(read, per * products * step_of(edge, (float)tiles * slices));
+            float t = 2.f + 0.05f * edge + std::max(read, per * products * step_of(edge, (float)tiles * slices));
             t += slices > 1 || kept ? 5.f + outputs * 8.f * slices / 5e6f : outputs * 4.f / 5e6f;
             if (!best.edge || t < least) least = t, best = {edge, (kts + per - 1) / per, per};
         }
@@ -512,6 +634,7 @@ int logits_edge(long long classes, long long rows, int kts, int products) {
 struct LossPlan {
     bool wide, u_ready, w_ready, scaled;  // 32-bit operands; whether u and W are copied; whether there are scales
     int pitch, kts;
+    int few, groups;                      // blocks of 16 rows of k_few (0: tiles), groups of classes to its workgroups
     int edge, tiles;                      // of the logits' tiles, tiles of classes
     int maxima_parts;
     int planes;
@@ -535,6 +658,13 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     p.rows_up = up(a.rows, 256);
     p.edge = logits_edge(a.classes, a.rows, p.kts, p.wide ? 3 : 1);
     p.tiles = (a.classes + p.edge - 1) / p.edge;
+    if (!backward && p.w_ready && a.rows <= (p.wide ? 64 : 32)) {
+        const int blocks = (int)((a.rows + 15) / 16), groups = (a.classes + 31) / 32;
+        p.few = blocks <= 1 ? 1 : blocks <= 2 ? 2 : 4;
+        p.groups = (groups + 2047) / 2048;
+        p.tiles = (groups + p.groups - 1) / p.groups;
+        p.u_ready = p.w_ready = p.scaled = false;
+    }
     p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, ((p.wide ? std::max<long long>(a.rows, a.classes) * p.pitch / 8 : a.rows) + 511) / 512));
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -627,7 +757,15 @@ hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
     const LossPlan p = loss_plan(a, false);
     LogitArgs l = prepared<TX>(a, p, work, false, st);
     l.parts = (f32x2*)(work + p.parts), l.picked = (float*)(work + p.picked);
-    logits<T, PAIRS, false>(l, p.edge, st);
+    if (p.few) {
+        const FewArgs f{a.w, a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.groups, a.target, l.parts, l.picked};
+        auto go = [&](auto kernel) { kernel<<<(unsigned)p.tiles, 256, 0, st>>>(f); };
+        if (p.few == 1) go(k_few<TX, 1>);
+        else if (p.few == 2) go(k_few<TX, 2>);
+        else if constexpr (sizeof(TX) == 4) go(k_few<TX, 4>);
+    } else {
+        logits<T, PAIRS, false>(l, p.edge, st);
+    }
     auto join = [&](auto kernel, int rows) {
         kernel<<<(unsigned)((a.rows + rows - 1) / rows), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.parts, l.picked, a.target, a.live, a.loss, a.lse);
     };
