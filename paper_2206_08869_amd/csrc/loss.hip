@@ -119,6 +119,11 @@ __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
         }
         Scales r;
         r.g = lift(2.f * m[0], r.ig);
+        if (m[0] > 0.f) {  // and to make the largest a power of two, see lift_of
+            int e;
+            const float rest = frexpf(m[0], &e);
+            r.g /= rest, r.ig *= rest;
+        }
         r.u = lift(m[1], r.iu);
         r.w = lift(m[2], r.iw);
         if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *a.scales = r;
@@ -174,6 +179,7 @@ struct LogitArgs {
     const float* lse;    // backward
     const float* dloss;
     const float* dlse;
+    float* inverse;      // without scales: of what g is multiplied with
     uint16_t* g;         // [rows up to a multiple of 256][ld]
     long long g_ld, g_plane;
 };
@@ -310,18 +316,58 @@ __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
     }
 }
 
+// g is rounded to 16 bits, and in most programs dloss is the same number in every row: what the rounding does to it would be the same everywhere, and not
+// average out. So g is multiplied with the number from 1 to 2 that makes the first row's dloss (or, where that is 0, what its probabilities are multiplied
+// with) a power of two. The same in all waves; the row's number is asked for first and used behind the products.
+__device__ __forceinline__ float lift_ask(const LogitArgs& a) {
+    const int t = threadIdx.x & 63;
+    if (a.scales || t >= a.rows || (a.live && !a.live[t])) return 0.f;
+    const float v = a.dloss ? fabsf(a.dloss[t]) : 0.f;
+    return v == 0.f && a.dlse ? fabsf(a.dlse[t]) : v;
+}
+__device__ __forceinline__ float lift_of(float asked, float& inverse) {
+    const unsigned long long some = __builtin_amdgcn_ballot_w64(asked > 0.f && asked < __builtin_inff());
+    inverse = 1.f;
+    if (some) {
+        int e;
+        inverse = frexpf(__shfl(asked, __builtin_ctzll(some)), &e);
+    }
+    return 1.f / inverse;
+}
+
 // Classes are the rows of the matrix instructions, so that a lane holds 4 * MT classes of a row and reduces them in registers.
-template <typename T, int MW, int NW, int MT, int NT, int PAIRS, bool GRAD>
+template <typename T, int MW, int NW, int MT, int NT, int PAIRS, int PARTS>
 __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     typedef Products<T, MW, NW, MT, NT, false, false, PAIRS> P;
     __shared__ __align__(16) uint16_t lds[P::LDS];
     int tm, tn;
     place_tile(blockIdx.x, gridDim.x, a.tm, a.tn, tm, tn);
     const int m0 = tm * P::BM, n0 = tn * P::BN;
+    const int wm = P::wave_m(), wn = P::wave_n();
+    // what the rows' gradients need, asked for in front of the products
+    float lse[NT], up[NT], both[NT], asked = 0.f;
+    int want[NT];  // the target, counted from the wave's first class; -1: elsewhere, -2: no such row, or padding
+    if (PARTS) {
+        asked = lift_ask(a);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const long long t = (long long)n0 + wn + n * 16 + P::col_of();
+            const bool there = t < a.rows && !(a.live && !a.live[t]);
+            lse[n] = up[n] = both[n] = 0.f, want[n] = -2;
+            if (there) {
+                want[n] = -1;
+                lse[n] = a.lse[t];
+                up[n] = a.dloss ? a.dloss[t] : 0.f;
+                both[n] = up[n] + (a.dlse ? a.dlse[t] : 0.f);
+                const long long target = a.target[t], from = a.first + m0 + wm;
+                if (target < 0 || target >= a.all) up[n] = both[n] = __builtin_nanf("");
+                if (target >= from && target < from + MT * 16) want[n] = (int)(target - from);
+            }
+        }
+    }
     P p;
     p.run(a.w, a.u, m0, n0, 0, a.kts, lds);
 
-    const int wm = P::wave_m(), wn = P::wave_n();
     if (a.scales) {
         const float iu = a.scales->iu, iw = a.scales->iw;
 #pragma unroll
@@ -331,7 +377,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p.acc[m][n][j] = p.acc[m][n][j] * iu * iw;
     }
-    if (!GRAD) {
+    if (PARTS == 0) {
         float* const meet = (float*)lds;  // [MW][BN][2]
         const int left = a.classes - (m0 + wm);  // classes that exist from the wave's first on
         if (left < MT * 16) {
@@ -391,45 +437,34 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
             a.parts[tm * a.rows + t] = f32x2{top, sum};
         }
     } else {
-        typedef Staged<P, uint16_t, NW, (PAIRS > 1 ? NT / 2 : NT)> Out;
-        static_assert((PAIRS > 1 ? 2 : 1) * Out::BYTES <= P::LDS * 2, "g passes through the operands' LDS");
+        typedef Staged<P, uint16_t, NW, (PARTS > 1 ? NT / 2 : NT)> Out;
+        static_assert((PARTS > 1 ? 2 : 1) * Out::BYTES <= P::LDS * 2, "g passes through the operands' LDS");
         char* const low = (char*)lds + Out::BYTES;
-        const float lift = a.scales ? a.scales->g : 1.f;
+        float inverse;
+        const float own = lift_of(asked, inverse), lift = a.scales ? a.scales->g : own;
+        if (!a.scales && blockIdx.x + threadIdx.x == 0) *a.inverse = inverse;
 #pragma unroll
         for (int pass = 0; pass < Out::PASSES; ++pass) {
             if (pass) lds_barrier();
             const Out staged;
 #pragma unroll
             for (int n = pass * (NT / Out::PASSES); n < (pass + 1) * (NT / Out::PASSES); ++n) {
-                const long long t = (long long)n0 + wn + n * 16 + P::col_of();
-                const bool there = t < a.rows && !(a.live && !a.live[t]);
-                float lse = 0.f, up = 0.f, both = 0.f;
-                long long want = -1;
-                if (there) {
-                    lse = a.lse[t];
-                    up = a.dloss ? a.dloss[t] : 0.f;
-                    both = up + (a.dlse ? a.dlse[t] : 0.f);
-                    want = a.target[t];
-                    if (want < 0 || want >= a.all) up = both = __builtin_nanf("");
-                    want -= a.first + m0 + wm;
-                }
-                const int w = want >= 0 && want < MT * 16 ? (int)want : -1;
-                up *= lift, both *= lift;
+                const float gu = up[n] * lift, gb = both[n] * lift;
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     uint16_t hi[4], lo[4];
                     const int v0 = m * 16 + P::row_of();
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float s = p.acc[m][n][j] - lse;
+                        const float s = p.acc[m][n][j] - lse[n];
                         const float e = PAIRS > 1 ? expf(s) : __builtin_amdgcn_exp2f(s * kLog2e);
-                        float g = both * e - (v0 + j == w ? up : 0.f);
-                        g = there && m0 + wm + v0 + j < a.classes ? g : 0.f;
+                        float g = gb * e - (v0 + j == want[n] ? gu : 0.f);
+                        g = want[n] != -2 && m0 + wm + v0 + j < a.classes ? g : 0.f;
                         hi[j] = bits16<T>(g);
-                        if (PAIRS > 1) lo[j] = bits16<T>(fabsf(g) < 60000.f ? g - (float)__builtin_bit_cast(T, hi[j]) : 0.f);
+                        if (PARTS > 1) lo[j] = bits16<T>(fabsf(g) < 60000.f ? g - (float)__builtin_bit_cast(T, hi[j]) : 0.f);
                     }
                     staged.put(lds, m, n, hi);
-                    if (PAIRS > 1) staged.put(low, m, n, lo);
+                    if (PARTS > 1) staged.put(low, m, n, lo);
                 }
             }
             lds_barrier();
@@ -440,7 +475,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                 int row, col;
                 staged.where(i, pass, row, col);
                 *(u32x4*)(g + row * a.g_ld + col) = staged.take(lds, i);
-                if (PAIRS > 1) *(u32x4*)(g + row * a.g_ld + col + a.g_plane) = staged.take(low, i);
+                if (PARTS > 1) *(u32x4*)(g + row * a.g_ld + col + a.g_plane) = staged.take(low, i);
             }
         }
     }
@@ -601,11 +636,12 @@ float step_of(int edge, float workgroups) {
 
 // The kind of tile and number of slices of least estimated time. Large tiles read operands less often, small ones and slices fill the chip when outputs are
 // few, slices at the price of their sums' way through memory and of a second launch.
-Cut cut_of(long long m, long long n, int kts, int products, bool kept) {
+Cut cut_of(long long m, long long n, int kts, int products, bool kept, int most) {
     Cut best{};
     float least = 0.f;
     const int planes = products > 1 ? 2 : 1;
     for (const int edge : {256, 128, 64}) {
+        if (edge > most) continue;
         const long long tm = (m + edge - 1) / edge, tn = (n + edge - 1) / edge, tiles = tm * tn;
         const float read = (float)kts * PK * 2 * planes * (float)(m * tn + n * tm) / 11e6f;
         for (int slices = 1; slices <= 256 && (slices == 1 || kts / slices >= 2); slices *= 2) {
@@ -620,10 +656,11 @@ Cut cut_of(long long m, long long n, int kts, int products, bool kept) {
 }
 
 // The kind of tile of the logits: classes x rows, 128 x 64 among them for few rows.
-int logits_edge(long long classes, long long rows, int kts, int products) {
+int logits_edge(long long classes, long long rows, int kts, int products, int most) {
     int best = 0;
     float least = 0.f;
     for (const int edge : {256, 128, 64}) {
+        if (edge > most) continue;
         const float tiles = (float)((classes + edge - 1) / edge) * (float)((rows + edge - 1) / edge);
         const float t = edge * 0.04f + kts * products * step_of(edge, tiles);
         if (!best || t < least) least = t, best = edge;
@@ -633,6 +670,7 @@ int logits_edge(long long classes, long long rows, int kts, int products) {
 
 struct LossPlan {
     bool wide, u_ready, w_ready, scaled;  // 32-bit operands; whether u and W are copied; whether there are scales
+    bool fine;                            // g in two parts though the operands have one
     int pitch, kts;
     int few, groups;                      // blocks of 16 rows of k_few (0: tiles), groups of classes to its workgroups
     int edge, tiles;                      // of the logits' tiles, tiles of classes
@@ -655,8 +693,11 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     p.u_ready = !in_place(a.u, a.u_stride, a.cols, p.wide) || (backward && a.live);
     p.w_ready = !in_place(a.w, a.w_stride, a.cols, p.wide);
     p.scaled = p.wide || (backward && a.type == IODF_T_F16);
+    // Sums of few numbers do not average the rounding of g to 16 bits: it would make gradients 1.6 times as far off as their own last rounding (14 rows, 7
+    // classes: 2.7e-3 for 1.7e-3). A second part costs a second product, which is time only where products are most of it.
+    p.fine = backward && !p.wide && (a.rows <= 256 || a.classes <= 16 || 2.0 * a.rows * a.classes * a.cols <= 4e9);
     p.rows_up = up(a.rows, 256);
-    p.edge = logits_edge(a.classes, a.rows, p.kts, p.wide ? 3 : 1);
+    p.edge = logits_edge(a.classes, a.rows, p.kts, p.wide ? 3 : 1, p.fine ? 128 : 256);
     p.tiles = (a.classes + p.edge - 1) / p.edge;
     if (!backward && p.w_ready && a.rows <= (p.wide ? 64 : 32)) {
         const int blocks = (int)((a.rows + 15) / 16), groups = (a.classes + 31) / 32;
@@ -672,18 +713,21 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         at += up(bytes, 256);
         return was;
     };
-    if (p.scaled) p.maxima = take((size_t)3 * p.maxima_parts * 4), p.scales = take(sizeof(Scales));
+    if (p.scaled) p.maxima = take((size_t)3 * p.maxima_parts * 4);
+    if (p.scaled || backward) p.scales = take(sizeof(Scales));
     if (p.u_ready) p.u = take((size_t)p.planes * a.rows * p.pitch * 2);
     if (p.w_ready) p.w = take((size_t)p.planes * a.classes * p.pitch * 2);
     if (!backward) {
         p.parts = take((size_t)p.tiles * a.rows * 8), p.picked = take((size_t)a.rows * 4);
     } else if (a.rows) {
-        p.piece = std::max<long long>(256, kPieceBytes / (p.rows_up * 2 * p.planes) / 256 * 256);
+        const int g_planes = p.wide || p.fine ? 2 : 1;
+        p.piece = std::max<long long>(256, kPieceBytes / (p.rows_up * 2 * g_planes) / 256 * 256);
         p.piece = std::min(p.piece, up(a.classes, 256));
-        p.g = take((size_t)p.planes * p.rows_up * p.piece * 2);
+        p.g = take((size_t)g_planes * p.rows_up * p.piece * 2);
         const long long here = std::min<long long>(p.piece, a.classes);
-        p.du = cut_of(a.cols, a.rows, (int)((here + PK - 1) / PK), p.wide ? 3 : 1, here < a.classes);
-        p.dw = cut_of(a.cols, here, (int)((a.rows + PK - 1) / PK), p.wide ? 3 : 1, false);
+        const int products = p.wide ? 3 : p.fine ? 2 : 1;
+        p.du = cut_of(a.cols, a.rows, (int)((here + PK - 1) / PK), products, here < a.classes, p.fine ? 128 : 256);
+        p.dw = cut_of(a.cols, here, (int)((a.rows + PK - 1) / PK), products, false, p.fine ? 128 : 256);
         auto sums = [&](const Cut& c, long long rows) { return (size_t)c.slices * up(rows, c.edge) * up(a.cols, c.edge) * 4; };
         if (a.du && (p.du.slices > 1 || p.piece < a.classes)) p.du_sums = take(sums(p.du, a.rows));
         if (a.dw && p.dw.slices > 1) p.dw_sums = take(sums(p.dw, here));
@@ -694,16 +738,18 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
 
 unsigned blocks_for(long long threads) { return (unsigned)std::max<long long>(1, std::min<long long>((threads + 255) / 256, 1 << 16)); }
 
-template <typename T, int PAIRS, bool GRAD>
+template <typename T, int PAIRS, int PARTS>
 void logits(const LogitArgs& a, int edge, hipStream_t st) {
     LogitArgs r = a;
     auto go = [&](auto kernel, int bm, int bn, int threads) {
         r.tm = (a.classes + bm - 1) / bm, r.tn = (int)((a.rows + bn - 1) / bn);
         kernel<<<(unsigned)r.tm * r.tn, threads, 0, st>>>(r);
     };
-    if (edge == 256) go(k_logits<T, 2, 4, 8, 4, PAIRS, GRAD>, 256, 256, 512);
-    else if (edge == 128) go(k_logits<T, 2, 2, 4, 4, PAIRS, GRAD>, 128, 128, 256);
-    else go(k_logits<T, 2, 2, 2, 2, PAIRS, GRAD>, 64, 64, 256);
+    if constexpr (PAIRS > 1 || PARTS < 2) {
+        if (edge == 256) return go(k_logits<T, 2, 4, 8, 4, PAIRS, PARTS>, 256, 256, 512);
+    }
+    if (edge == 128) go(k_logits<T, 2, 2, 4, 4, PAIRS, PARTS>, 128, 128, 256);
+    else go(k_logits<T, 2, 2, 2, 2, PAIRS, PARTS>, 64, 64, 256);
 }
 
 // One piece's part of a gradient; `last`: its slices are joined.
@@ -715,8 +761,10 @@ void gradient(const GradArgs& a, const Cut& c, bool last, hipStream_t st) {
     const dim3 grid((unsigned)r.tm * r.tn, c.slices);
     const unsigned join = blocks_for((long long)r.tm * r.tn * c.edge * c.edge / 4);
     if (c.edge == 256) {
-        k_loss_grad<T, TO, 2, 4, 8, 4, BSUMS, PAIRS><<<grid, 512, 0, st>>>(r);
-        if (r.partial && last) k_grad_join<TO, 2, 4, 8, 4><<<join, 256, 0, st>>>(r, c.slices);
+        if constexpr (PAIRS != 2) {
+            k_loss_grad<T, TO, 2, 4, 8, 4, BSUMS, PAIRS><<<grid, 512, 0, st>>>(r);
+            if (r.partial && last) k_grad_join<TO, 2, 4, 8, 4><<<join, 256, 0, st>>>(r, c.slices);
+        }
     } else if (c.edge == 128) {
         k_loss_grad<T, TO, 2, 2, 4, 4, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
         if (r.partial && last) k_grad_join<TO, 2, 2, 4, 4><<<join, 256, 0, st>>>(r, c.slices);
@@ -764,7 +812,7 @@ hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
         else if (p.few == 2) go(k_few<TX, 2>);
         else if constexpr (sizeof(TX) == 4) go(k_few<TX, 4>);
     } else {
-        logits<T, PAIRS, false>(l, p.edge, st);
+        logits<T, PAIRS, 0>(l, p.edge, st);
     }
     auto join = [&](auto kernel, int rows) {
         kernel<<<(unsigned)((a.rows + rows - 1) / rows), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.parts, l.picked, a.target, a.live, a.loss, a.lse);
@@ -786,22 +834,30 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
     const Scales* const s = l.scales;
     const Side w = l.w;
     l.lse = a.lse, l.dloss = a.dloss, l.dlse = a.dlse;
-    l.g = (uint16_t*)(work + p.g), l.g_ld = p.piece, l.g_plane = p.rows_up * p.piece;
+    l.inverse = (float*)(work + p.scales), l.g = (uint16_t*)(work + p.g), l.g_ld = p.piece, l.g_plane = p.rows_up * p.piece;
     float* const du_sums = p.du.slices > 1 || p.piece < a.classes ? (float*)(work + p.du_sums) : nullptr;
     float* const dw_sums = p.dw.slices > 1 ? (float*)(work + p.dw_sums) : nullptr;
     for (long long v0 = 0; v0 < a.classes; v0 += p.piece) {
         const int n = (int)std::min<long long>(p.piece, a.classes - v0);
         l.first = v0, l.classes = n;
         l.w = w, l.w.p += v0 * w.ld, l.w.extent = l.w.depth = n;
-        logits<T, PAIRS, true>(l, p.edge, st);
+        if constexpr (PAIRS > 1) logits<T, PAIRS, 2>(l, p.edge, st);
+        else if (p.fine) logits<T, 1, 2>(l, p.edge, st);
+        else logits<T, 1, 1>(l, p.edge, st);
+        // with g in two parts where the operand has one
+        auto part = [&](const GradArgs& g, auto bsums, const Cut& c, bool last) {
+            if constexpr (PAIRS > 1) gradient<T, TX, bsums, 3>(g, c, last, st);
+            else if (p.fine) gradient<T, TX, bsums, 2>(g, c, last, st);
+            else gradient<T, TX, bsums, 1>(g, c, last, st);
+        };
         if (a.du) {
             GradArgs g{};
             g.a = {l.w.p, w.plane, w.ld, a.cols, n};
             g.b = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
             g.kts = (n + PK - 1) / PK, g.rows = a.rows, g.cols = a.cols, g.out = a.du, g.ld = a.du_stride;
             g.partial = du_sums, g.add = v0 > 0;
-            if (s) g.down0 = &s->ig, g.down1 = &s->iw;
-            gradient<T, TX, false, PAIRS>(g, p.du, v0 + n == a.classes, st);
+            g.down0 = s ? &s->ig : l.inverse, g.down1 = s ? &s->iw : nullptr;
+            part(g, std::false_type(), p.du, v0 + n == a.classes);
         }
         if (a.dw) {
             GradArgs g{};
@@ -809,8 +865,8 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
             g.b = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};
             g.kts = (int)((a.rows + PK - 1) / PK), g.rows = n, g.cols = a.cols, g.out = (TX*)a.dw + v0 * a.dw_stride, g.ld = a.dw_stride;
             g.partial = dw_sums;
-            if (s) g.down0 = &s->ig, g.down1 = &s->iu;
-            gradient<T, TX, true, PAIRS>(g, p.dw, true, st);
+            g.down0 = s ? &s->ig : l.inverse, g.down1 = s ? &s->iu : nullptr;
+            part(g, std::true_type(), p.dw, true);
         }
     }
     return hipGetLastError();

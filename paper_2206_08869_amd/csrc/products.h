@@ -5,7 +5,7 @@
 //   rows   [m][k], k consecutive: a lane's fragment (eight k of one m) is one LDS read of sixteen bytes
 //   sums   [k][m], m consecutive: the transposing LDS read takes the fragment out of eight rows
 // so that no operand is ever transposed in memory. A number of more bits than 16 is two parts, high and low (planes of the same
-// layout), and the sum of three products: high high, high low, low high.
+// layout), and the sum of three products: high high, high low, low high; or of two where only B has low parts.
 #pragma once
 #include <type_traits>
 
