@@ -5,7 +5,8 @@
 //   rows   [m][k], k consecutive: a lane's fragment (eight k of one m) is one LDS read of sixteen bytes
 //   sums   [k][m], m consecutive: the transposing LDS read takes the fragment out of eight rows
 // so that no operand is ever transposed in memory. A number of more bits than 16 is two parts, high and low (planes of the same
-// layout), and the sum of three products: high high, high low, low high; or of two where only B has low parts.
+// layout), and the sum of three products: high low, low high, high high (the small ones first, while the sums
+// that they are rounded to are small too); or of two where only B has low parts.
 #pragma once
 #include <type_traits>
 
@@ -173,8 +174,8 @@ struct Products {
         const uint16_t *ca, *cb;
         unsigned left_a, left_b;
         auto next = [&] {
-            ca = uniform(Lane<BM, THREADS, ASUMS>::corner(a, m0, PAIRS > 1 && pair == 2, kt));
-            cb = uniform(Lane<BN, THREADS, BSUMS>::corner(b, n0, PAIRS > 1 && pair == 1, kt));
+            ca = uniform(Lane<BM, THREADS, ASUMS>::corner(a, m0, PAIRS > 2 && pair == 1, kt));
+            cb = uniform(Lane<BN, THREADS, BSUMS>::corner(b, n0, PAIRS > 1 && pair == 0, kt));
             left_a = a.depth - 1 - kt * PK, left_b = b.depth - 1 - kt * PK;
             if (++kt == kt1) kt = kt0, ++pair;
         };
