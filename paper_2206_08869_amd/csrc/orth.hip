@@ -381,6 +381,18 @@ __device__ __forceinline__ void deliver(const Target& t, int k, const Shape& z, 
     }
 }
 
+template <typename TO>
+__device__ __forceinline__ void deliver_quad(const Target& t, int k, int r, int c, int n, float (&v)[4]) {
+    TO* const to = (t.batch ? (TO*)t.w[0] + k * t.batch : (TO*)t.w[k]) + r * t.stride + c;
+    if (t.update) {
+        float was[4];
+        get_quad(to, n, was);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = fmaf(t.keep, was[j], t.by * v[j]);
+    }
+    put_quad(to, n, v);
+}
+
 // (a + e) X + B X: columns of X are the rows of the matrix instructions, so that a lane holds four neighbours of a row.
 template <int MW, int NW, int MT, int NT, bool TALL, int PAIRS>
 __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const Target target, const int type) {
@@ -487,6 +499,199 @@ __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const
     }
 }
 
+// ---- a short side of at most 64 ----
+
+struct SlimArgs {
+    _Float16* x;            // [matrix][rp][cp] in two parts; every workgroup changes its own blocks
+    long long plane;
+    Shape z;
+    int groups, per;        // workgroups to a matrix, blocks of 64 along the longer side to a workgroup
+    const float* from;      // [matrix][workgroup][64][64], parts of X X' times 2^(2 x_exp)
+    float* to;
+    float a, b, c;
+    float unlift, square;   // inverses of X's power of two and of its square
+    float o_lift, b_lift;
+    float lift;             // the next X's
+};
+
+// A step with one launch: a workgroup adds up A's parts, has A^2 and b A + c A^2 in LDS, applies it to its own blocks of X, and adds what these give to the
+// next A. FIRST: only that; LAST: the result goes to `target`. What bounds it is the launch and about a dozen dependent trips to memory and LDS: 128 matrices
+// of 64 x 64 take as long as one.
+template <bool TALL, int PAIRS, int KIND>
+__global__ __launch_bounds__(256) void k_slim(const SlimArgs a, const Target target, const int type) {
+    constexpr int FIRST = 0, LAST = 2, PARTS = PAIRS > 1 ? 2 : 1, S = 64;
+    // X as its product reads it, and the next X as its own square does
+    __shared__ __align__(16) uint16_t o[PARTS][S * S], m[PARTS][S * S], x[2][S * S], y[2][S * S];
+    __shared__ __align__(16) float d[S], e[S];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, low = lane & 15, q = wave * 16 + lane / 16 * 4;
+    const int k = blockIdx.y, g = blockIdx.x;
+    auto in_rows = [](int r, int c) { return r * S + ((c / 8) ^ (r >> 1 & 7)) * 8 + c % 8; };
+    auto in_sums = [](int r, int c) { return r * S + Lane<S, 64, true>::chunk(r, c / 8) * 8 + c % 8; };
+    auto rows = [&](const uint16_t* t, int r0, int step) { return *(const s16x8*)(t + in_rows(r0 + low, step * 32 + lane / 16 * 8)); };
+    auto sums = [&](const uint16_t* t, int c0, int step) {
+        const int r = step * 32 + lane / 16 * 8 + (lane >> 2 & 3), c = c0 + (lane & 3) * 4;
+        union { s16x4 h[2]; s16x8 v; } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + in_sums(r, c)));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + in_sums(r + 4, c)));
+        return u.v;
+    };
+    // acc[n] += rows q .. q + 3 of one operand by columns 16 n + low of the other, fragments by plane, block and step; small products first
+    auto multiply = [&](f32x4 (&acc)[4], auto left, auto right) {
+#pragma unroll
+        for (int p = PAIRS > 1 ? 0 : 2; p < 3; ++p)
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                const s16x8 l = left(p == 1, step);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) acc[n] = Mma<_Float16>::go(l, right(p == 0, n, step), acc[n]);
+            }
+    };
+    auto put4 = [](uint16_t (*t)[S * S], int parts, int at, const float (&v)[4]) {
+        _Float16 hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) two_parts(v[j], hi[j], lo[j]);
+        __builtin_memcpy(&t[0][at], hi, 8);
+        if (parts > 1) __builtin_memcpy(&t[parts - 1][at], lo, 8);
+    };
+    auto get = [](const uint16_t (*t)[S * S], int parts, int at, float (&v)[4]) {
+        _Float16 hi[4], lo[4];
+        __builtin_memcpy(hi, &t[0][at], 8);
+        if (parts > 1) __builtin_memcpy(lo, &t[parts - 1][at], 8);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (float)hi[j] + (parts > 1 ? (float)lo[j] : 0.f);
+    };
+
+    // this workgroup's blocks of X, sixteen bytes at a time: asked for a block ahead
+    const long long n = (long long)a.z.rp * a.z.cp;
+    uint16_t* const xs = (uint16_t*)a.x + k * n;
+    const int first = g * a.per, last = min((TALL ? a.z.rp : a.z.cp) / S, first + a.per);
+    u32x4 raw[2][2];
+    auto place = [&](int block, int i) {  // of chunk i of the thread's, in memory
+        const int r = (i * 256 + tid) / 8, c = (i * 256 + tid) % 8 * 8;
+        return TALL ? (long long)(block * S + r) * a.z.cp + c : (long long)r * a.z.cp + block * S + c;
+    };
+    auto ask = [&](int block) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) raw[p][i] = *(const u32x4*)(xs + p * a.plane + place(block, i));
+    };
+    ask(first);
+
+    if (KIND != FIRST) {
+        f32x4 s[4] = {};
+        const float* from = a.from + (long long)k * a.groups * S * S + tid * 4;
+        for (int w = 0; w < a.groups; w += 4) {
+            f32x4 v[4][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[u][i] = w + u < a.groups ? *(const f32x4*)(from + (w + u) * S * S + i * 1024) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] += v[u][i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 16 + tid / 16, c = tid % 16 * 4;
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = s[i][j] * a.square;
+                if (r == c + j) d[r] = v[j];
+                v[j] = r == c + j ? 0.f : v[j] * a.o_lift;
+            }
+            put4(o, PARTS, in_rows(r, c), v);
+        }
+        __syncthreads();
+        f32x4 acc[4] = {};
+        multiply(acc, [&](int p, int step) { return rows(o[p * (PARTS - 1)], wave * 16, step); },
+                 [&](int p, int b, int step) { return rows(o[p * (PARTS - 1)], b * 16, step); });
+        const float down = 1.f / (a.o_lift * a.o_lift), un = 1.f / a.o_lift;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {  // symmetric: four rows of a column are four neighbours of a row
+            const int r = b * 16 + low;
+            float was[4], v[4];
+            get(o, PARTS, in_rows(r, q), was);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float sum = acc[b][j] * down, ov = was[j] * un;
+                if (r == q + j) e[r] = fmaf(a.c, fmaf(d[r], d[r], sum), a.b * d[r]);
+                v[j] = r == q + j ? 0.f : fmaf(a.c, fmaf(d[r] + d[q + j], ov, sum), a.b * ov) * a.b_lift;
+            }
+            put4(m, PARTS, in_rows(r, q), v);
+        }
+    }
+    f32x4 next[4] = {};
+    const float down = a.unlift / a.b_lift;
+    for (int block = first; block < last; ++block) {
+        __syncthreads();
+        uint16_t (*const into)[S * S] = KIND == FIRST ? y : x;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = (i * 256 + tid) / 8, c = (i * 256 + tid) % 8 * 8;
+                *(u32x4*)&into[p][(KIND == FIRST) != TALL ? in_rows(r, c) : in_sums(r, c)] = raw[p][i];
+            }
+        if (block + 1 < last) ask(block + 1);
+        __syncthreads();
+        if (KIND != FIRST) {
+            // outputs q .. q + 3 of a row of X's memory, 16 b + low
+            f32x4 acc[4] = {};
+            if (TALL)
+                multiply(acc, [&](int p, int step) { return rows(m[p * (PARTS - 1)], wave * 16, step); },
+                         [&](int p, int b, int step) { return rows(x[p], b * 16, step); });
+            else
+                multiply(acc, [&](int p, int step) { return sums(x[p], wave * 16, step); },
+                         [&](int p, int b, int step) { return rows(m[p * (PARTS - 1)], b * 16, step); });
+            float v[4][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int r = b * 16 + low;
+                get(x, 2, TALL ? in_rows(r, q) : in_sums(r, q), v[b]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[b][j] = fmaf(a.a + e[TALL ? q + j : r], v[b][j] * a.unlift, acc[b][j] * down) * (KIND == LAST ? 1.f : a.lift);
+                if (KIND != LAST) put4(y, 2, TALL ? in_sums(r, q) : in_rows(r, q), v[b]);
+            }
+            if (KIND == LAST) {
+                float* const t = (float*)y;  // rows of 64 numbers, to be delivered as they lie
+#pragma unroll
+                for (int b = 0; b < 4; ++b) __builtin_memcpy(t + (b * 16 + low) * S + (q ^ (low & 7) * 4), v[b], 16);
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = i * 16 + tid / 16, c = tid % 16 * 4, row = TALL ? block * S + r : r, col = TALL ? c : block * S + c;
+                    if (row >= a.z.rows || col >= a.z.cols) continue;
+                    float w[4];
+                    __builtin_memcpy(w, t + r * S + (c ^ (r & 7) * 4), 16);
+                    if (type == IODF_T_F32) deliver_quad<float>(target, k, row, col, a.z.cols - col, w);
+                    else if (type == IODF_T_BF16) deliver_quad<__bf16>(target, k, row, col, a.z.cols - col, w);
+                    else deliver_quad<_Float16>(target, k, row, col, a.z.cols - col, w);
+                }
+                continue;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = (i * 256 + tid) / 8, c = (i * 256 + tid) % 8 * 8;
+                    *(u32x4*)(xs + p * a.plane + place(block, i)) = *(const u32x4*)&y[p][TALL ? in_sums(r, c) : in_rows(r, c)];
+                }
+        }
+        if (TALL)
+            multiply(next, [&](int p, int step) { return sums(y[p], wave * 16, step); }, [&](int p, int b, int step) { return sums(y[p], b * 16, step); });
+        else
+            multiply(next, [&](int p, int step) { return rows(y[p], wave * 16, step); }, [&](int p, int b, int step) { return rows(y[p], b * 16, step); });
+    }
+    if (KIND == LAST) return;
+    float* const to = a.to + ((long long)k * a.groups + g) * S * S;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) *(f32x4*)(to + (b * 16 + low) * S + q) = next[b];
+}
+
 // A square product's tiles, and how many workgroups go through them piece by piece (0: one to a tile).
 struct Cut {
     int edge, tiles, pieces;
@@ -521,6 +726,7 @@ Cut cut_of(long long count, int s, int kts, int products, bool sums) {
 struct OrthPlan {
     Shape z;
     bool tall, parts;          // parts: three products
+    int groups, per;           // of k_slim, 0: not by it
     Cut first, second;
     int apply_edge;
     int parts_of_norm;
@@ -535,6 +741,11 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     p.parts = type != IODF_T_BF16;
     auto tiles = [&](long long n, int e) { return (n + e - 1) / e; };
     auto apply = [&](int e) { return count * tiles(rows, e) * tiles(cols, e); };
+    if (p.z.s <= 64) {
+        const int blocks = std::max(p.z.rp, p.z.cp) / 64;
+        p.per = (blocks + 31) / 32;
+        p.groups = (blocks + p.per - 1) / p.per;
+    }
     p.first = cut_of(count, p.z.s, (p.tall ? p.z.rp : p.z.cp) / PK, p.parts ? 3 : 1, p.tall);
     p.second = cut_of(count, p.z.s, p.z.sp / PK, p.parts ? 3 : 1, false);
     p.apply_edge = apply(256) >= 130 ? 256 : apply(128) >= 200 ? 128 : 64;
@@ -547,7 +758,13 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     const size_t x = (size_t)count * p.z.rp * p.z.cp * 2 * 2, s = (size_t)count * p.z.sp * p.z.sp * 2 * (p.parts ? 2 : 1);
     p.parts_of_norm = (int)std::max<long long>(1, std::min<long long>({kNormBlocks, 2048 / std::max<long long>(1, count), ((long long)rows * ((cols + 7) / 8) + 255) / 256}));
     p.sums = take((size_t)count * p.parts_of_norm * 8);
-    p.x0 = take(x), p.x1 = take(x), p.o = take(s), p.b = take(s);
+    p.x0 = take(x);
+    if (p.groups) {
+        p.pieces = take((size_t)2 * count * p.groups * 64 * 64 * 4);
+        p.bytes = at;
+        return p;
+    }
+    p.x1 = take(x), p.o = take(s), p.b = take(s);
     p.d = take((size_t)count * p.z.sp * 4), p.e = take((size_t)count * p.z.sp * 4);
     size_t most = 0;
     for (const Cut& c : {p.first, p.second})
@@ -635,7 +852,30 @@ void polynomials(const OrthPlan& p, const OrthSteps& s, char* work, const Target
     }
 }
 
+template <bool TALL, int PAIRS>
+void slim(const OrthPlan& p, const OrthSteps& s, char* work, const Target& target, int type, hipStream_t st) {
+    SlimArgs a{};
+    a.x = (_Float16*)(work + p.x0), a.plane = (long long)p.z.rp * p.z.cp * p.z.count, a.z = p.z, a.groups = p.groups, a.per = p.per;
+    float *parts = (float*)(work + p.pieces), *other = parts + (long long)p.z.count * p.groups * 64 * 64;
+    const dim3 grid(p.groups, p.z.count);
+    a.to = parts, a.b_lift = 1.f;
+    k_slim<TALL, PAIRS, 0><<<grid, 256, 0, st>>>(a, target, type);
+    for (int i = 0; i < s.n; ++i) {
+        a.from = parts, a.to = other, a.a = s.a[i], a.b = s.b[i], a.c = s.c[i];
+        a.unlift = ldexpf(1.f, -s.x_exp[i]), a.square = a.unlift * a.unlift, a.lift = ldexpf(1.f, s.x_exp[i + 1]);
+        a.o_lift = ldexpf(1.f, s.a_exp[i]), a.b_lift = ldexpf(1.f, s.b_exp[i]);
+        if (i + 1 < s.n) k_slim<TALL, PAIRS, 1><<<grid, 256, 0, st>>>(a, target, type);
+        else k_slim<TALL, PAIRS, 2><<<grid, 256, 0, st>>>(a, target, type);
+        std::swap(parts, other);
+    }
+}
+
 hipError_t run(const OrthPlan& p, const OrthSteps& s, char* work, const Target& t, int type, hipStream_t st) {
+    if (p.groups) {
+        if (p.tall) p.parts ? slim<true, 3>(p, s, work, t, type, st) : slim<true, 1>(p, s, work, t, type, st);
+        else p.parts ? slim<false, 3>(p, s, work, t, type, st) : slim<false, 1>(p, s, work, t, type, st);
+        return hipGetLastError();
+    }
     if (p.tall) p.parts ? polynomials<true, 3>(p, s, work, t, type, st) : polynomials<true, 1>(p, s, work, t, type, st);
     else p.parts ? polynomials<false, 3>(p, s, work, t, type, st) : polynomials<false, 1>(p, s, work, t, type, st);
     return hipGetLastError();
