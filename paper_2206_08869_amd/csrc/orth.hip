@@ -12,6 +12,7 @@
 // A and A^2 are symmetric: only tiles on and below the diagonal are computed, and stored twice.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "products.h"
 #include "step.h"
@@ -71,19 +72,25 @@ __device__ __forceinline__ double block_sum(double s, double* meet) {
     return (meet[0] + meet[1]) + (meet[2] + meet[3]);
 }
 
+// The sum of squares of every `all`-th eight neighbours, from the one that `at` counts.
 template <typename TG, bool MUON>
-__global__ __launch_bounds__(256) void k_orth_norm(const Source src, const Shape z, double* sums) {
-    __shared__ double meet[4];
-    const int k = blockIdx.y, per = (z.cols + 7) / 8;
+__device__ __forceinline__ double squares(const Source& src, const Shape& z, int k, unsigned at, unsigned all) {
+    const unsigned per = (z.cols + 7) / 8;
     double s = 0.0;
-    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < (unsigned)z.rows * per; i += gridDim.x * 256) {
+    for (unsigned i = at; i < z.rows * per; i += all) {
         float v[8];
         taken<TG, MUON, true>(src, k, i / per, i % per * 8, z.cols, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s += (double)v[j] * v[j];
     }
-    s = block_sum(s, meet);
-    if (threadIdx.x == 0) sums[k * gridDim.x + blockIdx.x] = s;
+    return s;
+}
+
+template <typename TG, bool MUON>
+__global__ __launch_bounds__(256) void k_orth_norm(const Source src, const Shape z, double* sums) {
+    __shared__ double meet[4];
+    const double s = block_sum(squares<TG, MUON>(src, z, blockIdx.y, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256), meet);
+    if (threadIdx.x == 0) sums[blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
 
 __device__ __forceinline__ void two_parts(float v, _Float16& hi, _Float16& lo) {
@@ -91,17 +98,12 @@ __device__ __forceinline__ void two_parts(float v, _Float16& hi, _Float16& lo) {
     lo = fabsf(v) < 60000.f ? (_Float16)(v - (float)hi) : (_Float16)0.f;  // an infinity or NaN has no rest
 }
 
-// D / (norm + eps), times 2^x_exp, in two parts, with zeros around it.
+// D times `by` in two parts, with zeros around it: every `all`-th eight neighbours.
 template <typename TG, bool MUON>
-__global__ __launch_bounds__(256) void k_orth_start(const Source src, const Shape z, const double* sums, int parts, float eps, float lift, _Float16* x,
-                                                    long long plane) {
-    __shared__ double meet[4];
-    const int k = blockIdx.y, per = z.cp / 8;
-    double s = 0.0;
-    for (int i = threadIdx.x; i < parts; i += 256) s += sums[k * parts + i];
-    const double by = (double)lift / (sqrt(block_sum(s, meet)) + (double)eps);
+__device__ __forceinline__ void start_x(const Source& src, const Shape& z, int k, double by, _Float16* x, long long plane, unsigned at, unsigned all) {
+    const unsigned per = z.cp / 8;
     x += k * (long long)z.rp * z.cp;
-    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < (unsigned)z.rp * per; i += gridDim.x * 256) {
+    for (unsigned i = at; i < z.rp * per; i += all) {
         const int r = i / per, c = i % per * 8;
         float v[8] = {};
         if (r < z.rows && c < z.cols) taken<TG, MUON, false>(src, k, r, c, z.cols, v);
@@ -114,6 +116,16 @@ __global__ __launch_bounds__(256) void k_orth_start(const Source src, const Shap
         __builtin_memcpy(&w, lo, 16);
         *(u32x4*)(x + plane + i * 8ll) = w;
     }
+}
+
+template <typename TG, bool MUON>
+__global__ __launch_bounds__(256) void k_orth_start(const Source src, const Shape z, const double* sums, int parts, float eps, float lift, _Float16* x,
+                                                    long long plane) {
+    __shared__ double meet[4];
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 256) s += sums[blockIdx.y * parts + i];
+    const double by = (double)lift / (sqrt(block_sum(s, meet)) + (double)eps);
+    start_x<TG, MUON>(src, z, blockIdx.y, by, x, plane, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 struct SquareArgs {
@@ -508,18 +520,18 @@ struct SlimArgs {
     int groups, per;        // workgroups to a matrix, blocks of 64 along the longer side to a workgroup
     const float* from;      // [matrix][workgroup][64][64], parts of X X' times 2^(2 x_exp)
     float* to;
-    float a, b, c;
-    float unlift, square;   // inverses of X's power of two and of its square
-    float o_lift, b_lift;
-    float lift;             // the next X's
+    OrthSteps steps;
 };
 
-// A step with one launch: a workgroup adds up A's parts, has A^2 and b A + c A^2 in LDS, applies it to its own blocks of X, and adds what these give to the
-// next A. FIRST: only that; LAST: the result goes to `target`. What bounds it is the launch and about a dozen dependent trips to memory and LDS: 128 matrices
-// of 64 x 64 take as long as one.
-template <bool TALL, int PAIRS, int KIND>
-__global__ __launch_bounds__(256) void k_slim(const SlimArgs a, const Target target, const int type) {
-    constexpr int FIRST = 0, LAST = 2, PARTS = PAIRS > 1 ? 2 : 1, S = 64;
+// A workgroup adds up A's parts, has A^2 and b A + c A^2 in LDS, applies it to its own blocks of X, and adds what these give to the next A. That is a step
+// with one launch (KIND STEP; FIRST: only the first A; LAST: the result goes to `target`), and where a workgroup has a whole matrix (ALL: at most 256 along
+// the longer side) all steps with one, norm and start included. What bounds it is the launch and a dozen dependent trips to memory and LDS a step.
+enum { SLIM_FIRST, SLIM_STEP, SLIM_LAST, SLIM_ALL };
+
+template <bool TALL, int PAIRS, int KIND, bool MUON>
+__global__ __launch_bounds__(256) void k_slim(const SlimArgs a, const int step, const Source src, const int in_type, const float eps, const Target target,
+                                              const int type) {
+    constexpr int PARTS = PAIRS > 1 ? 2 : 1, S = 64;
     // X as its product reads it, and the next X as its own square does
     __shared__ __align__(16) uint16_t o[PARTS][S * S], m[PARTS][S * S], x[2][S * S], y[2][S * S];
     __shared__ __align__(16) float d[S], e[S];
@@ -576,117 +588,161 @@ __global__ __launch_bounds__(256) void k_slim(const SlimArgs a, const Target tar
 #pragma unroll
             for (int i = 0; i < 2; ++i) raw[p][i] = *(const u32x4*)(xs + p * a.plane + place(block, i));
     };
+    if (KIND == SLIM_ALL) {
+        __shared__ double meet[4];
+        auto begin = [&](auto t) {
+            typedef decltype(t) TG;
+            const double by = (double)ldexpf(1.f, a.steps.x_exp[0]) / (sqrt(block_sum(squares<TG, MUON>(src, a.z, k, tid, 256), meet)) + (double)eps);
+            start_x<TG, MUON>(src, a.z, k, by, a.x, a.plane, tid, 256);
+        };
+        if (in_type == IODF_T_F32) begin(0.f);
+        else if (in_type == IODF_T_BF16) begin((__bf16)0.f);
+        else begin((_Float16)0.f);
+        __syncthreads();
+    }
     ask(first);
 
-    if (KIND != FIRST) {
-        f32x4 s[4] = {};
-        const float* from = a.from + (long long)k * a.groups * S * S + tid * 4;
-        for (int w = 0; w < a.groups; w += 4) {
-            f32x4 v[4][4];
+    const bool stays = KIND == SLIM_ALL && a.per == 1;  // X never leaves LDS
+    // four neighbours of A's row r
+    auto put_a = [&](int r, int c, const f32x4& s, float square, float lift) {
+        float v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[u][i] = w + u < a.groups ? *(const f32x4*)(from + (w + u) * S * S + i * 1024) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] += v[u][i];
+        for (int j = 0; j < 4; ++j) {
+            v[j] = s[j] * square;
+            if (r == c + j) d[r] = v[j];
+            v[j] = r == c + j ? 0.f : v[j] * lift;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = i * 16 + tid / 16, c = tid % 16 * 4;
-            float v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = s[i][j] * a.square;
-                if (r == c + j) d[r] = v[j];
-                v[j] = r == c + j ? 0.f : v[j] * a.o_lift;
-            }
-            put4(o, PARTS, in_rows(r, c), v);
-        }
-        __syncthreads();
-        f32x4 acc[4] = {};
-        multiply(acc, [&](int p, int step) { return rows(o[p * (PARTS - 1)], wave * 16, step); },
-                 [&](int p, int b, int step) { return rows(o[p * (PARTS - 1)], b * 16, step); });
-        const float down = 1.f / (a.o_lift * a.o_lift), un = 1.f / a.o_lift;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {  // symmetric: four rows of a column are four neighbours of a row
-            const int r = b * 16 + low;
-            float was[4], v[4];
-            get(o, PARTS, in_rows(r, q), was);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float sum = acc[b][j] * down, ov = was[j] * un;
-                if (r == q + j) e[r] = fmaf(a.c, fmaf(d[r], d[r], sum), a.b * d[r]);
-                v[j] = r == q + j ? 0.f : fmaf(a.c, fmaf(d[r] + d[q + j], ov, sum), a.b * ov) * a.b_lift;
-            }
-            put4(m, PARTS, in_rows(r, q), v);
-        }
-    }
+        put4(o, PARTS, in_rows(r, c), v);
+    };
     f32x4 next[4] = {};
-    const float down = a.unlift / a.b_lift;
-    for (int block = first; block < last; ++block) {
-        __syncthreads();
-        uint16_t (*const into)[S * S] = KIND == FIRST ? y : x;
+    // step i; `begin`: only the first A
+    auto pass = [&](int i, auto begin, auto end) {
+        const float unlift = begin ? 0.f : ldexpf(1.f, -a.steps.x_exp[i]), lift = ldexpf(1.f, a.steps.x_exp[i + 1]);
+        const float o_lift = begin ? 0.f : ldexpf(1.f, a.steps.a_exp[i]), b_lift = begin ? 1.f : ldexpf(1.f, a.steps.b_exp[i]);
+        const float ca = begin ? 0.f : a.steps.a[i], cb = begin ? 0.f : a.steps.b[i], cc = begin ? 0.f : a.steps.c[i];
+        if (!begin) {
+            if (KIND == SLIM_ALL) {  // symmetric: four rows of a column are four neighbours of a row
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+                for (int b = 0; b < 4; ++b) put_a(b * 16 + low, q, next[b], unlift * unlift, o_lift);
+            } else {
+                f32x4 s[4] = {};
+                const float* from = a.from + (long long)k * a.groups * S * S + tid * 4;
+                for (int w = 0; w < a.groups; w += 8) {
+                    f32x4 v[8][4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = (i * 256 + tid) / 8, c = (i * 256 + tid) % 8 * 8;
-                *(u32x4*)&into[p][(KIND == FIRST) != TALL ? in_rows(r, c) : in_sums(r, c)] = raw[p][i];
-            }
-        if (block + 1 < last) ask(block + 1);
-        __syncthreads();
-        if (KIND != FIRST) {
-            // outputs q .. q + 3 of a row of X's memory, 16 b + low
-            f32x4 acc[4] = {};
-            if (TALL)
-                multiply(acc, [&](int p, int step) { return rows(m[p * (PARTS - 1)], wave * 16, step); },
-                         [&](int p, int b, int step) { return rows(x[p], b * 16, step); });
-            else
-                multiply(acc, [&](int p, int step) { return sums(x[p], wave * 16, step); },
-                         [&](int p, int b, int step) { return rows(m[p * (PARTS - 1)], b * 16, step); });
-            float v[4][4];
+                    for (int u = 0; u < 8; ++u)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int r = b * 16 + low;
-                get(x, 2, TALL ? in_rows(r, q) : in_sums(r, q), v[b]);
+                        for (int j = 0; j < 4; ++j) v[u][j] = w + u < a.groups ? *(const f32x4*)(from + (w + u) * S * S + j * 1024) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[b][j] = fmaf(a.a + e[TALL ? q + j : r], v[b][j] * a.unlift, acc[b][j] * down) * (KIND == LAST ? 1.f : a.lift);
-                if (KIND != LAST) put4(y, 2, TALL ? in_sums(r, q) : in_rows(r, q), v[b]);
-            }
-            if (KIND == LAST) {
-                float* const t = (float*)y;  // rows of 64 numbers, to be delivered as they lie
+                    for (int u = 0; u < 8; ++u)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) __builtin_memcpy(t + (b * 16 + low) * S + (q ^ (low & 7) * 4), v[b], 16);
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = i * 16 + tid / 16, c = tid % 16 * 4, row = TALL ? block * S + r : r, col = TALL ? c : block * S + c;
-                    if (row >= a.z.rows || col >= a.z.cols) continue;
-                    float w[4];
-                    __builtin_memcpy(w, t + r * S + (c ^ (r & 7) * 4), 16);
-                    if (type == IODF_T_F32) deliver_quad<float>(target, k, row, col, a.z.cols - col, w);
-                    else if (type == IODF_T_BF16) deliver_quad<__bf16>(target, k, row, col, a.z.cols - col, w);
-                    else deliver_quad<_Float16>(target, k, row, col, a.z.cols - col, w);
+                        for (int j = 0; j < 4; ++j) s[j] += v[u][j];
                 }
-                continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) put_a(j * 16 + tid / 16, tid % 16 * 4, s[j], unlift * unlift, o_lift);
             }
-            __syncthreads();
+            lds_barrier();
+            f32x4 acc[4] = {};
+            multiply(acc, [&](int p, int step) { return rows(o[p * (PARTS - 1)], wave * 16, step); },
+                     [&](int p, int b, int step) { return rows(o[p * (PARTS - 1)], b * 16, step); });
+            const float down = 1.f / (o_lift * o_lift), un = 1.f / o_lift;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {  // symmetric again
+                const int r = b * 16 + low;
+                float was[4], v[4];
+                get(o, PARTS, in_rows(r, q), was);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float sum = acc[b][j] * down, ov = was[j] * un;
+                    if (r == q + j) e[r] = fmaf(cc, fmaf(d[r], d[r], sum), cb * d[r]);
+                    v[j] = r == q + j ? 0.f : fmaf(cc, fmaf(d[r] + d[q + j], ov, sum), cb * ov) * b_lift;
+                }
+                put4(m, PARTS, in_rows(r, q), v);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) next[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float down = unlift / b_lift;
+        for (int block = first; block < last; ++block) {
+            lds_barrier();
+            uint16_t (*const into)[S * S] = begin ? y : x;
 #pragma unroll
             for (int p = 0; p < 2; ++p)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int r = (i * 256 + tid) / 8, c = (i * 256 + tid) % 8 * 8;
-                    *(u32x4*)(xs + p * a.plane + place(block, i)) = *(const u32x4*)&y[p][TALL ? in_sums(r, c) : in_rows(r, c)];
+                    u32x4 w = raw[p][i];
+                    if (stays && !begin) w = *(const u32x4*)&y[p][TALL ? in_sums(r, c) : in_rows(r, c)];
+                    *(u32x4*)&into[p][begin != TALL ? in_rows(r, c) : in_sums(r, c)] = w;
                 }
+            if (block + 1 < last) ask(block + 1);
+            lds_barrier();
+            if (!begin) {
+                // outputs q .. q + 3 of a row of X's memory, 16 b + low
+                f32x4 acc[4] = {};
+                if (TALL)
+                    multiply(acc, [&](int p, int step) { return rows(m[p * (PARTS - 1)], wave * 16, step); },
+                             [&](int p, int b, int step) { return rows(x[p], b * 16, step); });
+                else
+                    multiply(acc, [&](int p, int step) { return sums(x[p], wave * 16, step); },
+                             [&](int p, int b, int step) { return rows(m[p * (PARTS - 1)], b * 16, step); });
+                float v[4][4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int r = b * 16 + low;
+                    get(x, 2, TALL ? in_rows(r, q) : in_sums(r, q), v[b]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[b][j] = fmaf(ca + e[TALL ? q + j : r], v[b][j] * unlift, acc[b][j] * down) * (end ? 1.f : lift);
+                    if (!end) put4(y, 2, TALL ? in_sums(r, q) : in_rows(r, q), v[b]);
+                }
+                if (end) {
+                    float* const t = (float*)y;  // rows of 64 numbers, to be delivered as they lie
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) __builtin_memcpy(t + (b * 16 + low) * S + (q ^ (low & 7) * 4), v[b], 16);
+                    lds_barrier();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = i * 16 + tid / 16, c = tid % 16 * 4, row = TALL ? block * S + r : r, col = TALL ? c : block * S + c;
+                        if (row >= a.z.rows || col >= a.z.cols) continue;
+                        float w[4];
+                        __builtin_memcpy(w, t + r * S + (c ^ (r & 7) * 4), 16);
+                        if (type == IODF_T_F32) deliver_quad<float>(target, k, row, col, a.z.cols - col, w);
+                        else if (type == IODF_T_BF16) deliver_quad<__bf16>(target, k, row, col, a.z.cols - col, w);
+                        else deliver_quad<_Float16>(target, k, row, col, a.z.cols - col, w);
+                    }
+                    continue;
+                }
+                lds_barrier();
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int r = (i * 256 + tid) / 8, c = (i * 256 + tid) % 8 * 8;
+                        if (!stays) *(u32x4*)(xs + p * a.plane + place(block, i)) = *(const u32x4*)&y[p][TALL ? in_sums(r, c) : in_rows(r, c)];
+                    }
+            }
+            if (TALL)
+                multiply(next, [&](int p, int step) { return sums(y[p], wave * 16, step); }, [&](int p, int b, int step) { return sums(y[p], b * 16, step); });
+            else
+                multiply(next, [&](int p, int step) { return rows(y[p], wave * 16, step); }, [&](int p, int b, int step) { return rows(y[p], b * 16, step); });
         }
-        if (TALL)
-            multiply(next, [&](int p, int step) { return sums(y[p], wave * 16, step); }, [&](int p, int b, int step) { return sums(y[p], b * 16, step); });
-        else
-            multiply(next, [&](int p, int step) { return rows(y[p], wave * 16, step); }, [&](int p, int b, int step) { return rows(y[p], b * 16, step); });
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if (KIND == SLIM_LAST) return pass(step, no, yes);
+    if (KIND == SLIM_STEP) pass(step, no, no);
+    else pass(-1, yes, no);
+    if (KIND == SLIM_ALL) {
+        for (int i = 0; i < a.steps.n; ++i) {
+            if (!stays) {
+                __syncthreads();  // X is in memory
+                ask(first);
+            }
+            if (i + 1 < a.steps.n) pass(i, no, no);
+            else pass(i, no, yes);
+        }
+        return;
     }
-    if (KIND == LAST) return;
     float* const to = a.to + ((long long)k * a.groups + g) * S * S;
 #pragma unroll
     for (int b = 0; b < 4; ++b) *(f32x4*)(to + (b * 16 + low) * S + q) = next[b];
@@ -743,7 +799,7 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     auto apply = [&](int e) { return count * tiles(rows, e) * tiles(cols, e); };
     if (p.z.s <= 64) {
         const int blocks = std::max(p.z.rp, p.z.cp) / 64;
-        p.per = (blocks + 31) / 32;
+        p.per = blocks <= 4 ? blocks : blocks <= 32 ? (blocks + 15) / 16 : (blocks + 31) / 32;
         p.groups = (blocks + p.per - 1) / p.per;
     }
     p.first = cut_of(count, p.z.s, (p.tall ? p.z.rp : p.z.cp) / PK, p.parts ? 3 : 1, p.tall);
@@ -855,19 +911,28 @@ void polynomials(const OrthPlan& p, const OrthSteps& s, char* work, const Target
 template <bool TALL, int PAIRS>
 void slim(const OrthPlan& p, const OrthSteps& s, char* work, const Target& target, int type, hipStream_t st) {
     SlimArgs a{};
-    a.x = (_Float16*)(work + p.x0), a.plane = (long long)p.z.rp * p.z.cp * p.z.count, a.z = p.z, a.groups = p.groups, a.per = p.per;
+    a.x = (_Float16*)(work + p.x0), a.plane = (long long)p.z.rp * p.z.cp * p.z.count, a.z = p.z, a.groups = p.groups, a.per = p.per, a.steps = s;
     float *parts = (float*)(work + p.pieces), *other = parts + (long long)p.z.count * p.groups * 64 * 64;
     const dim3 grid(p.groups, p.z.count);
-    a.to = parts, a.b_lift = 1.f;
-    k_slim<TALL, PAIRS, 0><<<grid, 256, 0, st>>>(a, target, type);
+    const Source none{};
+    a.to = parts;
+    k_slim<TALL, PAIRS, SLIM_FIRST, false><<<grid, 256, 0, st>>>(a, -1, none, 0, 0.f, target, type);
     for (int i = 0; i < s.n; ++i) {
-        a.from = parts, a.to = other, a.a = s.a[i], a.b = s.b[i], a.c = s.c[i];
-        a.unlift = ldexpf(1.f, -s.x_exp[i]), a.square = a.unlift * a.unlift, a.lift = ldexpf(1.f, s.x_exp[i + 1]);
-        a.o_lift = ldexpf(1.f, s.a_exp[i]), a.b_lift = ldexpf(1.f, s.b_exp[i]);
-        if (i + 1 < s.n) k_slim<TALL, PAIRS, 1><<<grid, 256, 0, st>>>(a, target, type);
-        else k_slim<TALL, PAIRS, 2><<<grid, 256, 0, st>>>(a, target, type);
+        a.from = parts, a.to = other;
+        if (i + 1 < s.n) k_slim<TALL, PAIRS, SLIM_STEP, false><<<grid, 256, 0, st>>>(a, i, none, 0, 0.f, target, type);
+        else k_slim<TALL, PAIRS, SLIM_LAST, false><<<grid, 256, 0, st>>>(a, i, none, 0, 0.f, target, type);
         std::swap(parts, other);
     }
+}
+
+template <bool MUON>
+hipError_t all_at_once(const Source& src, int in_type, const OrthPlan& p, const OrthSteps& s, float eps, char* work, const Target& target, int type, hipStream_t st) {
+    SlimArgs a{};
+    a.x = (_Float16*)(work + p.x0), a.plane = (long long)p.z.rp * p.z.cp * p.z.count, a.z = p.z, a.groups = 1, a.per = p.per, a.steps = s;
+    auto go = [&](auto kernel) { kernel<<<dim3(1, p.z.count), 256, 0, st>>>(a, 0, src, in_type, eps, target, type); };
+    if (p.tall) p.parts ? go(k_slim<true, 3, SLIM_ALL, MUON>) : go(k_slim<true, 1, SLIM_ALL, MUON>);
+    else p.parts ? go(k_slim<false, 3, SLIM_ALL, MUON>) : go(k_slim<false, 1, SLIM_ALL, MUON>);
+    return hipGetLastError();
 }
 
 hipError_t run(const OrthPlan& p, const OrthSteps& s, char* work, const Target& t, int type, hipStream_t st) {
@@ -883,8 +948,8 @@ hipError_t run(const OrthPlan& p, const OrthSteps& s, char* work, const Target& 
 
 }  // namespace
 
-// How large singular values, and with them every entry of X, of A and of b A + c A^2, can get: 0..1 at first, then as the polynomials say, looked at in
-// 4096 places, two percent added for what lies between them and for roundings.
+// How large singular values, and with them every entry of X, of A and of b A + c A^2, can get: 0..1 at first, then as the polynomials say, two percent
+// added for roundings.
 bool orth_steps(int steps, const float* co, OrthSteps& s) {
     if (steps < 1 || steps > IODF_ORTH_MOST || !co) return false;
     s.n = steps;
@@ -893,11 +958,22 @@ bool orth_steps(int steps, const float* co, OrthSteps& s) {
     for (int i = 0; i < steps; ++i) {
         const double a = co[3 * i], b = co[3 * i + 1], c = co[3 * i + 2];
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        // in x = v^2: the polynomial turns where a + 3 b x + 5 c x^2 = 0, b x + c x^2 at -b / 2 c
+        const double end = most * most;
         double next = 0.0, beside = 0.0;
-        for (int k = 0; k <= 4096; ++k) {
-            const double v = most * k / 4096, v2 = v * v;
-            next = std::max(next, std::fabs(v * (a + v2 * (b + v2 * c))));
-            beside = std::max(beside, std::fabs(v2 * (b + v2 * c)));
+        auto look = [&](double x) {
+            if (!(x >= 0.0 && x <= end)) return;
+            next = std::max(next, std::fabs(std::sqrt(x) * (a + x * (b + x * c))));
+            beside = std::max(beside, std::fabs(x * (b + x * c)));
+        };
+        look(end);
+        if (c != 0.0) {
+            const double root = std::sqrt(9.0 * b * b - 20.0 * a * c);  // NaN: it does not turn
+            look((-3.0 * b + root) / (10.0 * c));
+            look((-3.0 * b - root) / (10.0 * c));
+            look(-b / (2.0 * c));
+        } else if (b != 0.0) {
+            look(-a / (3.0 * b));
         }
         s.a[i] = (float)a, s.b[i] = (float)b, s.c[i] = (float)c;
         s.x_exp[i] = lift(most), s.a_exp[i] = lift(most * most), s.b_exp[i] = lift(1.02 * beside);
@@ -917,6 +993,7 @@ hipError_t launch_orthogonalise(const iodf_orth& a, const OrthSteps& s, void* wo
     src.g[0] = a.in, src.stride = a.in_stride, src.batch = a.in_batch;
     Target t{};
     t.w[0] = a.out, t.stride = a.out_stride, t.batch = a.out_batch;
+    if (p.groups == 1) return all_at_once<false>(src, a.in_type, p, s, a.eps, (char*)work, t, a.out_type, st);
     begin<false>(src, a.in_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
     return run(p, s, (char*)work, t, a.out_type, st);
 }
@@ -929,6 +1006,7 @@ hipError_t launch_muon_step(const iodf_muon& a, const OrthSteps& s, void* work, 
     src.stride = a.grad_stride, src.beta = a.beta, src.nesterov = a.nesterov;
     t.stride = a.weight_stride, t.update = 1;
     t.keep = (float)(1.0 - (double)a.rate * a.decay), t.by = (float)(-(double)a.rate * a.scale);
+    if (p.groups == 1) return all_at_once<true>(src, a.grad_type, p, s, a.eps, (char*)work, t, a.weight_type, st);
     begin<true>(src, a.grad_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
     return run(p, s, (char*)work, t, a.weight_type, st);
 }
