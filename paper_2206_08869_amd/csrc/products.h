@@ -134,8 +134,12 @@ struct Frags {
 template <typename T, int MW, int NW, int MT_, int NT_, bool ASUMS, bool BSUMS, int PAIRS>
 struct Products {
     static constexpr int MT = MT_, NT = NT_, BM = MW * MT * 16, BN = NW * NT * 16, THREADS = MW * NW * 64;
-    static constexpr int STAGE = (BM + BN) * PK;  // elements of a tile of both operands
-    static constexpr int LDS = 2 * STAGE;         // elements of LDS that run() wants
+    // Small tiles have both parts of both operands in LDS at a time, which takes two loads for three products; large ones, which would not fit, go over
+    // the sum once for each product.
+    static constexpr bool BOTH = PAIRS > 1 && BM <= 128 && BN <= 128;
+    static constexpr int NA = BOTH && PAIRS > 2 ? 2 : 1, NB = BOTH ? 2 : 1;  // parts in LDS
+    static constexpr int STAGE = (NA * BM + NB * BN) * PK;                   // elements of a tile of both operands
+    static constexpr int LDS = 2 * STAGE;                                    // elements of LDS that run() wants
     f32x4 acc[MT][NT];
 
     static __device__ __forceinline__ int wave_m() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW * MT * 16; }
@@ -169,13 +173,15 @@ struct Products {
         clear();
         const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)lds +
                               __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
-        const int tiles = (kt1 - kt0) * PAIRS;
+        const int tiles = (kt1 - kt0) * (BOTH ? 1 : PAIRS);
         int pair = 0, kt = kt0;  // of the next tile to load
-        const uint16_t *ca, *cb;
+        const uint16_t *ca[NA], *cb[NB];
         unsigned left_a, left_b;
         auto next = [&] {
-            ca = uniform(Lane<BM, THREADS, ASUMS>::corner(a, m0, PAIRS > 2 && pair == 1, kt));
-            cb = uniform(Lane<BN, THREADS, BSUMS>::corner(b, n0, PAIRS > 1 && pair == 0, kt));
+#pragma unroll
+            for (int p = 0; p < NA; ++p) ca[p] = uniform(Lane<BM, THREADS, ASUMS>::corner(a, m0, BOTH ? p : PAIRS > 2 && pair == 1, kt));
+#pragma unroll
+            for (int p = 0; p < NB; ++p) cb[p] = uniform(Lane<BN, THREADS, BSUMS>::corner(b, n0, BOTH ? p : PAIRS > 1 && pair == 0, kt));
             left_a = a.depth - 1 - kt * PK, left_b = b.depth - 1 - kt * PK;
             if (++kt == kt1) kt = kt0, ++pair;
         };
@@ -183,11 +189,12 @@ struct Products {
         auto start = [&](int buf, int i0, int i1) {
 #pragma unroll
             for (int i = i0; i < i1; ++i) {
-                if (i < la.LOADS) la.start(ca, left_a, lds0 + buf * 2, i);
-                else lb.start(cb, left_b, lds0 + (buf + BM * PK) * 2, i - la.LOADS);
+                const int j = i - NA * la.LOADS;
+                if (j < 0) la.start(ca[i / la.LOADS], left_a, lds0 + (buf + i / la.LOADS * BM * PK) * 2, i % la.LOADS);
+                else lb.start(cb[j / lb.LOADS], left_b, lds0 + (buf + (NA * BM + j / lb.LOADS * BN) * PK) * 2, j % lb.LOADS);
             }
         };
-        constexpr int LOADS = Lane<BM, THREADS, ASUMS>::LOADS + Lane<BN, THREADS, BSUMS>::LOADS;
+        constexpr int LOADS = NA * Lane<BM, THREADS, ASUMS>::LOADS + NB * Lane<BN, THREADS, BSUMS>::LOADS;
         auto meet = [] {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
@@ -199,19 +206,33 @@ struct Products {
         // loads of the tile after the next) are dealt out by hand: left to itself the compiler gathers reads just before their products.
         constexpr int SPARE = 2, ROLL = MT - SPARE, BUSY = MT > 1 ? MT / 2 : 1, EACH = (NT + SPARE + BUSY - 1) / BUSY;
         static_assert(MT >= SPARE, "two blocks of rows at least");
-        s16x8 xa[ROLL > 0 ? ROLL : 1], xs[2][SPARE], xb[2][NT];
-        auto read_a = [&](int buf, int step, int m) { return fa.read(lds + buf, step, m); };
+        s16x8 xa[NA][ROLL > 0 ? ROLL : 1], xs[2][NA][SPARE], xb[2][NB][NT];
+        f32x4 low[BOTH ? MT : 1][BOTH ? NT : 1] = {};  // the small products' sums
         auto group = [&](int set, int m) {
+            auto of_a = [&](int p) { return m < ROLL ? xa[p][m < ROLL ? m : 0] : xs[set][p][m < ROLL ? 0 : m - ROLL]; };
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[m][n] = Mma<T>::go(m < ROLL ? xa[m < ROLL ? m : 0] : xs[set][m < ROLL ? 0 : m - ROLL], xb[set][n], acc[m][n]);
+            for (int n = 0; n < NT; ++n) {
+                if (BOTH) low[BOTH ? m : 0][BOTH ? n : 0] = Mma<T>::go(of_a(0), xb[set][NB - 1][n], low[BOTH ? m : 0][BOTH ? n : 0]);
+                if (NA > 1) low[BOTH ? m : 0][BOTH ? n : 0] = Mma<T>::go(of_a(NA - 1), xb[set][0][n], low[BOTH ? m : 0][BOTH ? n : 0]);
+                acc[m][n] = Mma<T>::go(of_a(0), xb[set][0][n], acc[m][n]);
+            }
         };
+        auto read_a = [&](int buf, int step, int p, int m) { return fa.read(lds + buf + p * BM * PK, step, m); };
         auto reads = [&](int set, int buf, int step, int g) {  // of step `step`, before group g of the step before it
 #pragma unroll
             for (int i = g * EACH; i < (g + 1) * EACH && i < NT + SPARE; ++i) {
-                if (i < NT) xb[set][i] = fb.read(lds + buf + BM * PK, step, i);
-                else xs[set][i - NT] = read_a(buf, step, ROLL + i - NT);
+                if (i < NT) {
+#pragma unroll
+                    for (int p = 0; p < NB; ++p) xb[set][p][i] = fb.read(lds + buf + (NA * BM + p * BN) * PK, step, i);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < NA; ++p) xs[set][p][i - NT] = read_a(buf, step, p, ROLL + i - NT);
+                }
             }
-            if (g >= 1 && g - 1 < ROLL) xa[g - 1] = read_a(buf, step, g - 1);
+            if (g >= 1 && g - 1 < ROLL) {
+#pragma unroll
+                for (int p = 0; p < NA; ++p) xa[p][g - 1] = read_a(buf, step, p, g - 1);
+            }
         };
         auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
         next();
@@ -243,6 +264,12 @@ struct Products {
                 fence();
             }
             buf ^= STAGE;
+        }
+        if (BOTH) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[m][n] += low[BOTH ? m : 0][BOTH ? n : 0];
         }
         lds_barrier();
     }
