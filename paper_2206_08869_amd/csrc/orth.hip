@@ -763,15 +763,15 @@ Cut cut_of(long long count, int s, int kts, int products, bool sums) {
     for (const int edge : {256, 192, 64}) {  // whole tiles
         const int n = (s + edge - 1) / edge;
         const float tiles = (float)count * n * (n + 1) / 2;
-        if (edge == 64) take(3.f + steps * std::max(0.5f, 0.23f * tiles / 256.f), {edge, n, 0});
+        if (edge == 64) take(3.f + steps * std::max(products > 1 ? 0.24f : 0.5f, (products > 1 ? 0.25f : 0.23f) * tiles / 256.f), {edge, n, 0});
         else take(15.f + (edge == 256 ? 1.13f : 0.7f) * steps * std::ceil(tiles / 256.f), {edge, n, 0});
     }
     for (const int edge : {256, 128}) {  // pieces
-        const int n = (s + edge - 1) / edge, most = edge == 256 ? 256 : 512;
+        const int n = (s + edge - 1) / edge, most = edge == 256 || products > 1 ? 256 : 512;
         const long long tiles = count * n * (n + 1) / 2, units = tiles * kts;
         for (int pieces = most; pieces >= 8; pieces /= 2) {
             if (pieces > units || pieces < tiles / 2) continue;
-            const float step = edge == 256 ? 1.13f : (sums ? 0.75f : 0.45f) * (pieces > 256 ? 2.f : pieces > 128 ? 1.3f : 1.f);
+            const float step = edge == 256 ? (sums ? 1.9f : 1.5f) : (sums ? 0.75f : 0.45f) * (products > 1 ? 0.67f : 1.f) * (pieces > 256 ? 2.f : pieces > 128 ? 1.3f : 1.f);
             const float parts = (float)pieces / tiles + 1.f, moved = (float)(pieces + tiles) * edge * edge * 8e-6f;
             take(step * products * std::ceil((float)units / pieces) + 10.f + 0.4f * parts * edge / 128 + 0.15f * moved, {edge, n, pieces});
         }
