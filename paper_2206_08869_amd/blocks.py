@@ -102,7 +102,7 @@ def _matrix(x, name, shape=None, dtype=None, device=None, recorded=True):
     if not isinstance(x, _Tensor) or x.dim() != 2 or x.dtype not in _types or not x.is_cuda:
         _refuse("%s has to be a float32, bfloat16 or float16 [rows, cols] tensor on the GPU" % name)
     if x.requires_grad and recorded and _torch.is_grad_enabled():
-        _refuse("%s requires a gradient, and this call records no graph: take joined, projection or gated_projection, or torch.no_grad()" % name)
+        _refuse("%s requires a gradient, and this call records no graph: take joined, projection, gated_projection or classified, or torch.no_grad()" % name)
     r, c = x.shape
     if shape is not None and (r, c) != shape:
         _refuse("%s is %s, not %s" % (name, [r, c], list(shape)))

@@ -461,7 +461,8 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                         float g = gb * e - (v0 + j == want[n] ? gu : 0.f);
                         g = want[n] != -2 && m0 + wm + v0 + j < a.classes ? g : 0.f;
                         hi[j] = bits16<T>(g);
-                        if (PARTS > 1) lo[j] = bits16<T>(fabsf(g) < 60000.f ? g - (float)__builtin_bit_cast(T, hi[j]) : 0.f);
+                        const float whole = (float)__builtin_bit_cast(T, hi[j]);
+                        if (PARTS > 1) lo[j] = bits16<T>(fabsf(whole) < __builtin_inff() ? g - whole : 0.f);
                     }
                     staged.put(lds, m, n, hi);
                     if (PARTS > 1) staged.put(low, m, n, lo);

@@ -86,8 +86,12 @@ int iodf_orthogonalise(const iodf_orth* a, void* work, int64_t work_bytes, void*
     if (a->count == 0) return IODF_OK;
     if (!work || !words(work, 16) || work_bytes < need) return IODF_E_ARG;
     if (!a_tensor(a->in, a->in_type, a->in_stride, a->cols) || !a_tensor(a->out, a->out_type, a->out_stride, a->cols)) return IODF_E_ARG;
-    if (a->count > 1 && (a->in_batch < 1 || a->out_batch < (a->rows - 1) * a->out_stride + a->cols || a->in_batch > (1ll << 40) || a->out_batch > (1ll << 40)))
-        return IODF_E_ARG;
+    if (a->count > 1) {
+        if (a->in_batch < 1 || a->out_batch < 1 || a->in_batch > (1ll << 40) || a->out_batch > (1ll << 40)) return IODF_E_ARG;
+        // one behind the other, or side by side between the rows of the first
+        if (a->out_batch < (a->rows - 1) * a->out_stride + a->cols && (a->out_batch < a->cols || (a->count - 1) * a->out_batch + a->cols > a->out_stride))
+            return IODF_E_ARG;
+    }
     iodf_orth run = *a;
     if (a->count == 1) run.in_batch = run.out_batch = 1;  // one matrix: they are multiplied with 0
     return report_hip(launch_orthogonalise(run, s, work, (hipStream_t)stream));

@@ -129,7 +129,8 @@ def _make_classified():
 
 def classified(u, weight, target, live=None):
     """class_loss as a differentiable call -> ClassLoss, whose loss and lse both have gradients (a penalty on lse keeps logits from drifting). What the
-    backward pass keeps of a row is u and 4 bytes. weight may have another type than u (a 32-bit original of 16-bit products): it is rounded to u's."""
+    backward pass keeps of a row is u and 4 bytes. weight may have another type than u (a 32-bit original of 16-bit products): it is rounded to u's, and the
+    backward pass keeps that copy. As with any differentiable call, no eager graph of the same leaves may live while a backward pass is captured."""
     return ClassLoss(*(_classified or _make_classified()).apply(u, weight, target, live))
 
 
@@ -169,17 +170,55 @@ def _sheets(x, name, shape=None):
             _refuse("%s has to be a float32, bfloat16 or float16 tensor on the GPU" % name)
         return kind, 0, x.shape[1], x.shape[2], 0, x.shape[2]
     kind, stride = _k._matrix(x[0], name)
-    batch = x.stride(0)
-    if x.shape[0] > 1 and batch < (x.shape[1] - 1) * stride + x.shape[2]:
-        _refuse("the matrices of %s overlap" % name)
-    return kind, x.shape[0], x.shape[1], x.shape[2], batch, stride
+    (count, rows, cols), batch = x.shape, x.stride(0)
+    if count > 1 and batch < (rows - 1) * stride + cols and (batch < cols or (count - 1) * batch + cols > stride):
+        _refuse("the matrices of %s overlap" % name)  # neither one behind the other nor side by side between the rows of the first
+    return kind, count, rows, cols, batch, stride
+
+
+def _place(x, stride):
+    """Address, rows, and bytes from row to row and of a row, of a [rows, cols] tensor."""
+    size = x.element_size()
+    return x.data_ptr(), x.shape[0], stride * size, x.shape[1] * size
+
+
+def _meet(p, q):
+    """Whether two places have memory in common, as far as that is easy to say: of different row strides wherever their ranges meet."""
+    (at, rows, stride, cols), (other, _, other_stride, other_cols) = sorted((p, q))
+    if other - at >= (rows - 1) * stride + cols:
+        return False
+    row, col = divmod(other - at, stride)
+    return stride != other_stride or col < cols or (col + other_cols > stride and row + 1 < rows)
+
+
+def _whole(x, count, rows, cols, batch, stride):
+    """The place of several matrices: side by side they count as rows that are as wide as all of them, otherwise, if they are not the rows of one, as one row."""
+    size = x.element_size()
+    if count == 1 or batch < (rows - 1) * stride + cols:
+        return x.data_ptr(), rows, stride * size, ((count - 1) * batch + cols) * size
+    if batch == rows * stride:
+        return x.data_ptr(), count * rows, stride * size, cols * size
+    whole = ((count - 1) * batch + (rows - 1) * stride + cols) * size
+    return x.data_ptr(), 1, whole, whole
+
+
+def _apart(changed, read):
+    """Refuses tensors, given by their places, of which one that is changed has memory in common with another."""
+    places = sorted([(p, True) for p in changed] + [(p, False) for p in read])
+    end, near = 0, False
+    for (at, rows, stride, cols), _ in places:
+        near = near or at < end
+        end = max(end, at + (rows - 1) * stride + cols)
+    if near and any((x or y) and _meet(p, q) for i, (p, x) in enumerate(places) for q, y in places[:i]):
+        _refuse("a tensor is there twice, or overlaps another")
 
 
 def orthogonalise(g, steps=5, coefficients=QUINTIC, eps=1e-7, dtype=None, out=None):
     """g / (its Frobenius norm + eps), `steps` times an odd polynomial of its singular values: nearly the orthogonal matrix next to it.
 
     g [rows, cols], or [count, rows, cols] for several of one shape. coefficients: (a, b, c) of X <- a X + b XX'X + c (XX')^2 X, or one triple for each
-    step. dtype: the result's, g's if None; bfloat16 takes a third of the work of float32 and float16. out may be g."""
+    step. dtype: the result's, g's if None; bfloat16 takes a third of the work of float32 and float16. out may be g. At most 4096 matrices, whose shorter side
+    is at most 16384 and longer one at most 65536."""
     t = _k._torch if _native else _setup()
     kind, count, rows, cols, batch, stride = _sheets(g, "g")
     numbers = _polynomials(steps, coefficients)
@@ -193,6 +232,8 @@ def orthogonalise(g, steps=5, coefficients=QUINTIC, eps=1e-7, dtype=None, out=No
     to, _, _, _, out_batch, out_stride = _sheets(out, "out", tuple(g.shape))
     if min(rows, cols) < 1:
         _refuse("g has to have rows and columns")
+    if given and count and (g.data_ptr(), kind, batch, stride) != (out.data_ptr(), to, out_batch, out_stride):
+        _apart([_whole(out, count, rows, cols, out_batch, out_stride)], [_whole(g, count, rows, cols, batch, stride)])
     block = _ORTH.pack(count, batch, out_batch, stride, out_stride, rows, cols, kind, to, steps, eps, ctypes.addressof(numbers), g.data_ptr(),
                        out.data_ptr())
     _run("orthogonalise", "orthogonalise_workspace", block, g.device)
@@ -241,9 +282,7 @@ def muon_step(weights, grads, momenta, rate, beta=0.95, nesterov=True, decay=0.0
     rows, cols = shape
     if rows < 1 or not all(m.is_contiguous() for m in momenta):
         _refuse("weights have to have rows, and momenta to be contiguous")
-    changed = [x.data_ptr() for x in weights + momenta]
-    if len(set(changed)) < len(changed) or set(changed) & {g.data_ptr() for g in grads}:
-        _refuse("a tensor is there twice")
+    _apart([_place(w, sw) for w in weights] + [_place(m, cols) for m in momenta], [_place(g, sg) for g in grads])
     scale = math.sqrt(max(1.0, rows / cols)) if scale is None else scale
     numbers, most = _polynomials(steps, coefficients), _b.IODF_MUON_MOST
     for at in range(0, len(weights), most):

@@ -542,3 +542,119 @@ def test_orthogonalise_every_kind_of_tile(count, rows, cols, name):
             x = 3.4445 * x + (-4.7750 * m + 2.0315 * m @ m) @ x
         x = x.t() if rows > cols else x
         assert (r[k].double() - x).norm() <= {"bf16": 2.0 ** -9 + 4 * 2.0 ** -12, "f32": 4e-6}[name] * x.norm()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,classes,cols", [(40, 300, 96), (900, 40, 130)])
+def test_class_loss_gradients_of_scaled_losses(name, rows, classes, cols):
+    """2^16 times dloss: 2^16 times the gradients, to the bit (of bf16, and of f16 what fits it), also where products of g exceed half precision's range."""
+    t = torch()
+    u, w, target, d = on_card(rows, classes, cols, name, 8)
+    lse = iodf.class_loss(u, w, target).lse
+    d = d * (1.0 if name == "bf16" else 2.0 ** -16)
+    for less, more in zip(iodf.class_loss_backward(u, w, target, lse, d * 3), iodf.class_loss_backward(u, w, target, lse, d * 3 * 65536)):
+        if name == "bf16":
+            assert t.equal(less.float() * 65536, more.float())
+        else:  # less has numbers below the normal range
+            assert ((less.float() * 65536 - more.float()).abs() <= 2.0 ** -25 * 65536 + more.float().abs() * 2.0 ** -11).all()
+
+
+@pytest.mark.parametrize("to", NAMES)
+def test_orthogonalise_side_by_side(to):
+    """[rows, count, cols] turned to [count, rows, cols], from and to."""
+    t = torch()
+    rng = np.random.default_rng(17)
+    g = dev(as_type(gradient(rng, 50 * 3, 70), to), to).view(50, 3, 70)
+    want = iodf.orthogonalise(g.transpose(0, 1).contiguous())
+    assert t.equal(iodf.orthogonalise(g.transpose(0, 1)), want)
+    out = t.full((50, 4, 70), float("nan"), dtype=g.dtype, device="cuda")
+    iodf.orthogonalise(g.transpose(0, 1), out=out[:, :3].transpose(0, 1))
+    assert t.equal(out[:, :3].transpose(0, 1), want) and out[:, 3].isnan().all()
+    iodf.orthogonalise(g.transpose(0, 1), out=g.transpose(0, 1))
+    assert t.equal(g.transpose(0, 1), want)
+
+
+def test_tensors_that_overlap_are_refused():
+    t = torch()
+    x = t.randn((3, 60, 80), device="cuda")
+    before = x.clone()
+    flat = x.view(-1)
+    for g, out in ((x[0, :40], x[0, 20:]), (x[:2], x[1:]), (x[0, :, :50], x[0, :, 30:]), (x[0, :59], flat[1:4721].view(59, 80)),
+                   (x[0, :30], x[0].view(t.bfloat16)[:30, :80]), (x[:, :, :50], x[:, :, 30:])):
+        with pytest.raises(ValueError, match="overlap"):
+            iodf.orthogonalise(g, out=out)
+    assert t.equal(x, before)
+    m = [t.zeros((20, 80), device="cuda") for _ in range(2)]
+    g = [t.randn((20, 80), device="cuda") for _ in range(2)]
+    for w, grads, momenta in (([x[0, :20], x[0, 10:30]], g, m), ([x[0, :20], x[0, 20:40]], [x[0, 5:25], g[1]], m), ([x[0, :20], x[0, 20:40]], g, [m[0], m[0]]),
+                              ([x[0, :20]], [x[0, :20]], m[:1])):
+        with pytest.raises(ValueError, match="overlap"):
+            iodf.muon_step(w, grads, momenta, 0.1)
+    assert t.equal(x, before) and not any(k.any() for k in m)
+    # side by side, one gradient for both, and neighbours are fine: the bits of tensors of their own
+    halves, own = [x[0, :20, :40], x[0, :20, 40:]], [x[0, :20, :40].clone(), x[0, :20, 40:].clone()]
+    d, m1, m2 = g[0][:, :40], [t.zeros((20, 40), device="cuda") for _ in range(2)], [t.zeros((20, 40), device="cuda") for _ in range(2)]
+    iodf.muon_step(halves, [d, d], m1, 0.1)
+    for k in range(2):
+        iodf.muon_step(own[k], d.contiguous(), m2[k], 0.1)
+        assert t.equal(halves[k], own[k]) and t.equal(m1[k], m2[k])
+    y = t.randn((2, 30, 40), device="cuda")
+    want = iodf.orthogonalise(y[0])
+    assert t.equal(iodf.orthogonalise(y[0], out=y[1]), want)
+
+
+def test_classified_captured_with_its_backward_pass():
+    """Loss, gradients and the step of a weight as a captured graph, the leaves used in it alone; eager runs on copies between the replays."""
+    t = torch()
+    u0, w0, target, _ = on_card(200, 90, 64, "bf16", 9)
+    expanded = t.full((1,), 1.0 / 200, device="cuda").expand(200)
+
+    def once(u, w, m):
+        u, w = u.detach().requires_grad_(), w.detach().requires_grad_()
+        r = iodf.classified(u, w, target)
+        du, dw = t.autograd.grad([r.loss, r.lse], [u, w], [expanded, 0.01 * expanded])
+        with t.no_grad():
+            new = w.detach().clone()
+            iodf.muon_step(new, dw, m, 0.1)
+        return r.loss.detach(), du, dw, new
+
+    want = once(u0, w0, t.zeros((90, 64), device="cuda"))
+    m = t.zeros((90, 64), device="cuda")
+    side = t.cuda.Stream()
+    side.wait_stream(t.cuda.current_stream())
+    with t.cuda.stream(side):
+        once(u0, w0, m)
+    t.cuda.current_stream().wait_stream(side)
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        got = once(u0, w0, m)
+    for _ in range(3):
+        m.zero_()
+        for x in got:
+            x.fill_(0)
+        graph.replay()
+        eager = once(u0, w0, t.zeros((90, 64), device="cuda"))
+        t.cuda.synchronize()
+        assert all(t.equal(a, b) for a, b in zip(got, want)) and all(t.equal(a, b) for a, b in zip(eager, want))
+
+
+def test_two_streams_at_once():
+    """The same calls on two streams at a time, with workspaces of their own: the bits of calls one after the other."""
+    t = torch()
+    sets = [on_card(500, 700, 256, "bf16", s) for s in (11, 12)]
+    g = [t.randn((300, 260), device="cuda") for _ in sets]
+
+    def once(k):
+        u, w, target, d = sets[k]
+        r = iodf.class_loss(u, w, target)
+        return (*r, *iodf.class_loss_backward(u, w, target, r.lse, d), iodf.orthogonalise(g[k]))
+
+    want = [once(k) for k in range(2)]
+    t.cuda.synchronize()
+    streams, got = [t.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(10):
+        for k, s in enumerate(streams):
+            with t.cuda.stream(s):
+                got[k].append(once(k))
+    t.cuda.synchronize()
+    assert all(t.equal(a, b) for k in range(2) for run in got[k] for a, b in zip(run, want[k]))
