@@ -67,13 +67,12 @@ __global__ __launch_bounds__(256) void k_maxima(const MaxArgs a, float* maxima) 
         const float* const x = what == 1 ? a.u : a.w;
         const uint8_t* const live = what == 1 ? a.live : nullptr;
         const long long stride = what == 1 ? a.u_stride : a.w_stride, rows = what == 1 ? a.rows : a.classes;
-        const int per = (a.cols + 7) / 8;
-        for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (long long)gridDim.x * 256) {
-            const long long t = i / per;
-            const int c = (int)(i - t * per) * 8;
+        const unsigned per = (a.cols + 7) / 8, n = (unsigned)(rows * per);  // fits, as rows times cols is 2^34 at most
+        for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+            const unsigned t = i / per, c = (i - t * per) * 8;
             if (live && !live[t]) continue;
             float v[8];
-            load8(x + t * stride + c, a.cols - c, v);
+            load8(x + t * stride + c, a.cols - (int)c, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = finite_max(m, v[j]);
         }
@@ -105,15 +104,17 @@ struct ReadyArgs {
 };
 
 // Rows of `pitch` 16-bit numbers with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in two parts of half precision. And the scales,
-// which every workgroup takes from the maxima by itself.
+// which workgroups take from the maxima by themselves.
 template <typename TX>
 __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
     __shared__ float meet[4];
-    const int which = blockIdx.y, per = a.pitch / 8;
+    const int which = blockIdx.y;
+    const unsigned per = a.pitch / 8;
     float by = 1.f;
-    if (a.maxima) {
+    if (a.maxima && (a.wide || blockIdx.x + blockIdx.y == 0)) {
         float m[3] = {};
         for (int k = 0; k < (a.wide ? 3 : 1); ++k) {
+            if (k != which + 1 && blockIdx.x + blockIdx.y) continue;  // only the first workgroup needs all of them
             for (int i = threadIdx.x; i < a.parts; i += 256) m[k] = fmaxf(m[k], a.maxima[k * a.parts + i]);
             m[k] = block_max(m[k], meet);
         }
@@ -133,15 +134,29 @@ __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
     if (!y) return;
     const long long rows = a.rows[which], stride = a.stride[which], plane = rows * a.pitch;
     const uint8_t* const live = which ? nullptr : a.live;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (long long)gridDim.x * 256) {
-        const long long t = i / per;
-        const int c = (int)(i - t * per) * 8, n = live && !live[t] ? 0 : a.cols - c;
-        const Raw8<TX> r = fetch8((const TX*)a.x[which] + t * stride + c, n, false);
-        if (sizeof(TX) == 2) {
-            *(u32x4*)(y + t * a.pitch + c) = u32x4{r.w[0], r.w[1], r.w[2], r.w[3]};
-        } else {
+    const unsigned all = (unsigned)(rows * per);  // fits, as rows times cols is 2^34 at most
+    const unsigned step = gridDim.x * 256;
+    constexpr int AT_ONCE = 2;  // in flight
+    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < all; i += AT_ONCE * step) {
+        Raw8<TX> raw[AT_ONCE];
+        long long to[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const unsigned at = min(i + k * step, all - 1);
+            const long long t = at / per;
+            const int c = (int)(at % per) * 8;
+            raw[k] = fetch8((const TX*)a.x[which] + t * stride + c, live && !live[t] ? 0 : a.cols - c, false);
+            to[k] = t * a.pitch + c;
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (i + k * step >= all) break;
+            if (sizeof(TX) == 2) {
+                *(u32x4*)(y + to[k]) = u32x4{raw[k].w[0], raw[k].w[1], raw[k].w[2], raw[k].w[3]};
+                continue;
+            }
             float v[8];
-            widen8(r, v);
+            widen8(raw[k], v);
             _Float16 hi[8], lo[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -152,9 +167,9 @@ __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
             }
             u32x4 w;
             __builtin_memcpy(&w, hi, 16);
-            *(u32x4*)(y + t * a.pitch + c) = w;
+            *(u32x4*)(y + to[k]) = w;
             __builtin_memcpy(&w, lo, 16);
-            *(u32x4*)(y + plane + t * a.pitch + c) = w;
+            *(u32x4*)(y + plane + to[k]) = w;
         }
     }
 }
@@ -182,6 +197,9 @@ struct LogitArgs {
     float* inverse;      // without scales: of what g is multiplied with
     uint16_t* g;         // [rows up to a multiple of 256][ld]
     long long g_ld, g_plane;
+    int per;             // tiles along the columns of a slice
+    int slices;
+    f32x4* sums;         // [slice][tile], in the order in which lanes hold them
 };
 
 template <typename T>
@@ -335,8 +353,11 @@ __device__ __forceinline__ float lift_of(float asked, float& inverse) {
     return 1.f / inverse;
 }
 
-// Classes are the rows of the matrix instructions, so that a lane holds 4 * MT classes of a row and reduces them in registers.
-template <typename T, int MW, int NW, int MT, int NT, int PAIRS, int PARTS>
+// Classes are the rows of the matrix instructions, so that a lane holds 4 * MT classes of a row and reduces them in registers. Where tiles are few and
+// columns many the columns are split: SLICE leaves a slice's sums, JOIN adds them up and goes on.
+enum { WHOLE, SLICE, JOIN };
+
+template <typename T, int MW, int NW, int MT, int NT, int PAIRS, int PARTS, int KIND>
 __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     typedef Products<T, MW, NW, MT, NT, false, false, PAIRS> P;
     __shared__ __align__(16) uint16_t lds[P::LDS];
@@ -347,7 +368,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     // what the rows' gradients need, asked for in front of the products
     float lse[NT], up[NT], both[NT], asked = 0.f;
     int want[NT];  // the target, counted from the wave's first class; -1: elsewhere, -2: no such row, or padding
-    if (PARTS) {
+    if (PARTS && KIND != SLICE) {
         asked = lift_ask(a);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -366,7 +387,35 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
         }
     }
     P p;
-    p.run(a.w, a.u, m0, n0, 0, a.kts, lds);
+    f32x4* const sums = a.sums + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * (P::BM * P::BN / 4) + (threadIdx.x >> 6) * (MT * NT * 64) + (threadIdx.x & 63);
+    if (KIND == WHOLE) {
+        p.run(a.w, a.u, m0, n0, 0, a.kts, lds);
+    } else if (KIND == SLICE) {
+        const int kt0 = blockIdx.y * a.per;
+        p.run(a.w, a.u, m0, n0, kt0, min(a.kts, kt0 + a.per), lds);
+#pragma unroll
+        for (int i = 0; i < MT * NT; ++i) sums[i * 64] = p.acc[i / NT][i % NT];
+        return;
+    } else {
+        constexpr int AT_ONCE = 32 / (MT * NT);
+        const long long next = (long long)gridDim.x * (P::BM * P::BN / 4);
+        p.clear();
+        for (int k = 0; k < a.slices; k += AT_ONCE) {
+            f32x4 v[AT_ONCE][MT * NT];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (k + u < a.slices) {
+#pragma unroll
+                    for (int i = 0; i < MT * NT; ++i) v[u][i] = sums[(k + u) * next + i * 64];
+                }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (k + u < a.slices) {
+#pragma unroll
+                    for (int i = 0; i < MT * NT; ++i) p.acc[i / NT][i % NT] += v[u][i];
+                }
+        }
+    }
 
     if (a.scales) {
         const float iu = a.scales->iu, iw = a.scales->iw;
@@ -527,16 +576,16 @@ struct GradArgs {
     const float* down1;
 };
 
-// du = g W (sums of W, rows of g) and dw = g' u (sums of both). The outputs' columns are the matrix instructions' rows.
-template <typename T, typename TO, int MW, int NW, int MT, int NT, bool BSUMS, int PAIRS>
-__global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
-    typedef Products<T, MW, NW, MT, NT, true, BSUMS, PAIRS> P;
+// A tile of du = g W (sums of W, rows of g) or dw = g' u (sums of both). The outputs' columns are the matrix instructions' rows.
+template <class P, typename TO, int NW>
+__device__ __forceinline__ void grad_tile(const GradArgs& a, unsigned block, uint16_t* lds) {
+    constexpr int MT = P::MT, NT = P::NT;
     typedef Staged<P, float, NW, 2> Out;
     static_assert(Out::BYTES <= P::LDS * 2, "outputs pass through the operands' LDS");
-    __shared__ __align__(16) uint16_t lds[P::LDS];
+    const unsigned tiles = (unsigned)a.tm * a.tn, slice = block / tiles;
     int tm, tn;
-    place_tile(blockIdx.x, gridDim.x, a.tm, a.tn, tm, tn);
-    const int kt0 = blockIdx.y * a.per, kt1 = min(a.kts, kt0 + a.per);
+    place_tile(block - slice * tiles, tiles, a.tm, a.tn, tm, tn);
+    const int kt0 = slice * a.per, kt1 = min(a.kts, kt0 + a.per);
     P p;
     if (kt0 < kt1) {
         p.run(a.a, a.b, tm * P::BM, tn * P::BN, kt0, kt1, lds);
@@ -544,7 +593,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
         p.clear();
     }
     if (a.partial) {
-        f32x4* const to = (f32x4*)a.partial + ((long long)blockIdx.y * gridDim.x + tm * a.tn + tn) * (P::BM * P::BN / 4) +
+        f32x4* const to = (f32x4*)a.partial + ((long long)slice * tiles + tm * a.tn + tn) * (P::BM * P::BN / 4) +
                           (threadIdx.x >> 6) * (MT * NT * 64) + (threadIdx.x & 63);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -585,9 +634,22 @@ __global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs a) {
     }
 }
 
-// The slices' sums, one after the other, four neighbours of a row to a thread.
+// `first` workgroups for du's tiles and slices, the others for dw's: neither fills the chip by itself where rows and classes are few.
+template <typename T, typename TO, int MW, int NW, int MT, int NT, int PAIRS>
+__global__ __launch_bounds__(MW * NW * 64) void k_loss_grad(const GradArgs du, const GradArgs dw, const unsigned first) {
+    typedef Products<T, MW, NW, MT, NT, true, false, PAIRS> DU;
+    typedef Products<T, MW, NW, MT, NT, true, true, PAIRS> DW;
+    __shared__ __align__(16) uint16_t lds[DU::LDS];
+    if (blockIdx.x < first) grad_tile<DU, TO, NW>(du, blockIdx.x, lds);
+    else grad_tile<DW, TO, NW>(dw, blockIdx.x - first, lds);
+}
+
+// The slices' sums, one after the other, four neighbours of a row to a thread, of du, dw or both: which have slices.
 template <typename TO, int MW, int NW, int MT, int NT>
-__global__ __launch_bounds__(256) void k_grad_join(const GradArgs a, int slices) {
+__global__ __launch_bounds__(256) void k_grad_join(const GradArgs du, const GradArgs dw, int slices_du, int slices_dw) {
+    const bool second = !slices_du || blockIdx.y;
+    const GradArgs& a = second ? dw : du;
+    const int slices = second ? slices_dw : slices_du;
     constexpr int BM = MW * MT * 16, BN = NW * NT * 16, PER = BM * BN / 4;
     const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
     const long long n = (long long)a.tm * a.tn * PER;
@@ -627,44 +689,77 @@ struct Cut {
     int edge, slices, per;
 };
 
-// Microseconds that workgroups of a kind take to a tile (64 along the sum), all of them, on 256 compute units.
-float step_of(int edge, float workgroups) {
-    const float each = std::ceil(workgroups) / 256.f;
-    if (edge == 256) return 1.13f * std::ceil(each);
-    if (edge == 128) return each <= 1.f ? 0.6f : 0.85f * std::ceil(each / 2.f);
-    return std::max(0.5f, 0.23f * each);
+// Microseconds that workgroups of a kind take, all of them, on 256 compute units, each `per` tiles (64 along the sum) of `products`: those that fit LDS at a
+// time go along together, then the next ones do. Times of a tile and (7, 5, 1.5) of the way to the first products and from the last ones are fitted to
+// calls of two to a hundred thousand rows and classes, which they say within a fifth.
+float time_of(int edge, float workgroups, int per, int products) {
+    const float most = edge == 256 ? 1.f : edge == 128 ? (products > 1 ? 1.f : 2.f) : products > 2 ? 2.f : products > 1 ? 3.f : 4.f;
+    const float each = workgroups / 256.f, at_once = std::min(most, std::max(1.f, each));
+    const float rounds = edge > 64 ? std::ceil(each / most) : std::max(1.f, each / most);
+    const float step = edge == 256 ? 1.13f : edge == 128 ? (products > 1 ? 0.6f : at_once > 1.f ? 0.85f : 0.6f)
+                       : products > 1 ? std::max(0.25f, 0.23f * at_once) : std::max(0.5f, 0.23f * at_once);
+    return rounds * ((edge == 256 ? 7.f : edge == 128 ? 5.f : 1.5f) + per * products * step);
 }
 
-// The kind of tile and number of slices of least estimated time. Large tiles read operands less often, small ones and slices fill the chip when outputs are
-// few, slices at the price of their sums' way through memory and of a second launch.
-Cut cut_of(long long m, long long n, int kts, int products, bool kept, int most) {
-    Cut best{};
+// What a gradient's product is: outputs m x n, tiles along its sum, and whether its sums go through memory anyway. m of 0: there is none.
+struct Task {
+    long long m, n;
+    int kts;
+    bool kept;
+};
+
+// The kind of tile and number of slices of least estimated time, of one product or of two in one launch. Large tiles read operands less often, small ones and
+// slices fill the chip when outputs are few, slices at the price of their sums' way through memory and of a second launch.
+float cut_of(const Task* tasks, int count, Cut* cuts, int products, int most) {
     float least = 0.f;
     const int planes = products > 1 ? 2 : 1;
     for (const int edge : {256, 128, 64}) {
         if (edge > most) continue;
-        const long long tm = (m + edge - 1) / edge, tn = (n + edge - 1) / edge, tiles = tm * tn;
-        const float read = (float)kts * PK * 2 * planes * (float)(m * tn + n * tm) / 11e6f;
-        for (int slices = 1; slices <= 256 && (slices == 1 || kts / slices >= 2); slices *= 2) {
-            const int per = (kts + slices - 1) / slices;
-            const float outputs = (float)tiles * edge * edge;
-            float t = 2.f + 0.05f * edge + std::max(read, per * products * step_of(edge, (float)tiles * slices));
-            t += slices > 1 || kept ? 5.f + outputs * 8.f * slices / 5e6f : outputs * 4.f / 5e6f;
-            if (!best.edge || t < least) least = t, best = {edge, (kts + per - 1) / per, per};
+        struct { long long tiles; float read, outputs; } t[2] = {};
+        for (int i = 0; i < count; ++i) {
+            const Task& k = tasks[i];
+            const long long tm = (k.m + edge - 1) / edge, tn = (k.n + edge - 1) / edge;
+            const float once = (float)(k.m + k.n) / 5e6f, again = (float)(k.m * (tn - 1) + k.n * (tm - 1)) / 11e6f;
+            t[i] = {tm * tn, (float)k.kts * PK * 2 * planes * (once + again), (float)(tm * tn) * edge * edge};
         }
+        auto per_of = [&](int i, int slices) { return (tasks[i].kts + slices - 1) / slices; };
+        auto may = [&](int i, int slices) { return slices == 1 || (slices <= 256 && tasks[i].kts / slices >= 2); };
+        for (int s0 = 1; may(0, s0); s0 *= 2)
+            for (int s1 = 1; count > 1 ? may(1, s1) : s1 == 1; s1 *= 2) {
+                const int per = count > 1 ? std::max(per_of(0, s0), per_of(1, s1)) : per_of(0, s0);
+                const float workgroups = (float)(t[0].tiles * s0 + (count > 1 ? t[1].tiles * s1 : 0));
+                float time = std::max(t[0].read + t[1].read, time_of(edge, workgroups, per, products));
+                bool join = false;
+                for (int i = 0; i < count; ++i) {
+                    const int slices = i ? s1 : s0;
+                    if (slices > 1 || tasks[i].kept) join = true, time += t[i].outputs * 8.f * slices / 5e6f + 0.035f * slices;
+                    else time += t[i].outputs * 4.f / 5e6f;
+                }
+                if (join) time += 5.f;
+                if (least > 0.f && time >= least) continue;
+                least = time;
+                for (int i = 0; i < count; ++i) {
+                    const int p = per_of(i, i ? s1 : s0);
+                    cuts[i] = {edge, (tasks[i].kts + p - 1) / p, p};
+                }
+            }
     }
-    return best;
+    return least;
 }
 
-// The kind of tile of the logits: classes x rows, 128 x 64 among them for few rows.
-int logits_edge(long long classes, long long rows, int kts, int products, int most) {
-    int best = 0;
+// The kind of tile of the logits, classes x rows, and the slices of the columns.
+Cut logits_cut(long long classes, long long rows, int kts, int products, int most) {
+    Cut best{};
     float least = 0.f;
     for (const int edge : {256, 128, 64}) {
         if (edge > most) continue;
         const float tiles = (float)((classes + edge - 1) / edge) * (float)((rows + edge - 1) / edge);
-        const float t = edge * 0.04f + kts * products * step_of(edge, tiles);
-        if (!best || t < least) least = t, best = edge;
+        for (int slices = 1; slices == 1 || (edge < 256 && slices <= 64 && kts / slices >= 2); slices *= 2) {
+            const int per = (kts + slices - 1) / slices;
+            float t = time_of(edge, tiles * slices, per, products);
+            if (slices > 1) t += 6.f + tiles * edge * edge * 8.f * slices / 5e6f;
+            if (!best.edge || t < least) least = t, best = {edge, (kts + per - 1) / per, per};
+        }
     }
     return best;
 }
@@ -674,13 +769,15 @@ struct LossPlan {
     bool fine;                            // g in two parts though the operands have one
     int pitch, kts;
     int few, groups;                      // blocks of 16 rows of k_few (0: tiles), groups of classes to its workgroups
-    int edge, tiles;                      // of the logits' tiles, tiles of classes
+    Cut logits;
+    int tiles;                            // of classes
     int maxima_parts;
     int planes;
     long long rows_up, piece;
     Cut du, dw;
+    bool together;                        // du's and dw's products in one launch
     // byte offsets into the workspace
-    size_t maxima, scales, u, w, parts, picked, g, du_sums, dw_sums, bytes;
+    size_t maxima, scales, u, w, sums, parts, picked, g, du_sums, dw_sums, bytes;
 };
 
 bool in_place(const void* p, long long stride, int cols, bool wide) { return !wide && cols % PK == 0 && stride % 8 == 0 && stride <= (1 << 22) && ((uintptr_t)p & 15) == 0; }
@@ -698,8 +795,8 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     // classes: 2.7e-3 for 1.7e-3). A second part costs a second product, which is time only where products are most of it.
     p.fine = backward && !p.wide && (a.rows <= 256 || a.classes <= 16 || 2.0 * a.rows * a.classes * a.cols <= 4e9);
     p.rows_up = up(a.rows, 256);
-    p.edge = logits_edge(a.classes, a.rows, p.kts, p.wide ? 3 : 1, p.fine ? 128 : 256);
-    p.tiles = (a.classes + p.edge - 1) / p.edge;
+    p.logits = logits_cut(a.classes, a.rows, p.kts, p.wide ? 3 : 1, p.fine ? 128 : 256);
+    p.tiles = (a.classes + p.logits.edge - 1) / p.logits.edge;
     if (!backward && p.w_ready && a.rows <= (p.wide ? 64 : 32)) {
         const int blocks = (int)((a.rows + 15) / 16), groups = (a.classes + 31) / 32;
         p.few = blocks <= 1 ? 1 : blocks <= 2 ? 2 : 4;
@@ -718,6 +815,7 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     if (p.scaled || backward) p.scales = take(sizeof(Scales));
     if (p.u_ready) p.u = take((size_t)p.planes * a.rows * p.pitch * 2);
     if (p.w_ready) p.w = take((size_t)p.planes * a.classes * p.pitch * 2);
+    if (!p.few && p.logits.slices > 1) p.sums = take((size_t)p.logits.slices * p.tiles * up(a.rows, p.logits.edge) * p.logits.edge * 4);
     if (!backward) {
         p.parts = take((size_t)p.tiles * a.rows * 8), p.picked = take((size_t)a.rows * 4);
     } else if (a.rows) {
@@ -727,8 +825,13 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.g = take((size_t)g_planes * p.rows_up * p.piece * 2);
         const long long here = std::min<long long>(p.piece, a.classes);
         const int products = p.wide ? 3 : p.fine ? 2 : 1;
-        p.du = cut_of(a.cols, a.rows, (int)((here + PK - 1) / PK), products, here < a.classes, p.fine ? 128 : 256);
-        p.dw = cut_of(a.cols, here, (int)((a.rows + PK - 1) / PK), products, false, p.fine ? 128 : 256);
+        const Task tasks[2] = {{a.cols, a.rows, (int)((here + PK - 1) / PK), here < a.classes}, {a.cols, here, (int)((a.rows + PK - 1) / PK), false}};
+        const int most = p.fine ? 128 : 256;
+        Cut cuts[2];
+        float alone = 0.f;
+        if (a.du) alone += cut_of(tasks, 1, &p.du, products, most);
+        if (a.dw) alone += cut_of(tasks + 1, 1, &p.dw, products, most);
+        if (a.du && a.dw && cut_of(tasks, 2, cuts, products, most) < alone) p.together = true, p.du = cuts[0], p.dw = cuts[1];
         auto sums = [&](const Cut& c, long long rows) { return (size_t)c.slices * up(rows, c.edge) * up(a.cols, c.edge) * 4; };
         if (a.du && (p.du.slices > 1 || p.piece < a.classes)) p.du_sums = take(sums(p.du, a.rows));
         if (a.dw && p.dw.slices > 1) p.dw_sums = take(sums(p.dw, here));
@@ -740,39 +843,51 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
 unsigned blocks_for(long long threads) { return (unsigned)std::max<long long>(1, std::min<long long>((threads + 255) / 256, 1 << 16)); }
 
 template <typename T, int PAIRS, int PARTS>
-void logits(const LogitArgs& a, int edge, hipStream_t st) {
+void logits(const LogitArgs& a, const Cut& cut, hipStream_t st) {
     LogitArgs r = a;
-    auto go = [&](auto kernel, int bm, int bn, int threads) {
-        r.tm = (a.classes + bm - 1) / bm, r.tn = (int)((a.rows + bn - 1) / bn);
-        kernel<<<(unsigned)r.tm * r.tn, threads, 0, st>>>(r);
+    r.slices = cut.slices, r.per = cut.per;
+    r.tm = (a.classes + cut.edge - 1) / cut.edge, r.tn = (int)((a.rows + cut.edge - 1) / cut.edge);
+    const unsigned tiles = (unsigned)r.tm * r.tn;
+    auto go = [&](auto whole, auto slice, auto join) {
+        if (cut.slices <= 1) {
+            whole<<<tiles, 256, 0, st>>>(r);
+        } else {
+            slice<<<dim3(tiles, cut.slices), 256, 0, st>>>(r);
+            join<<<tiles, 256, 0, st>>>(r);
+        }
     };
     if constexpr (PAIRS > 1 || PARTS < 2) {
-        if (edge == 256) return go(k_logits<T, 2, 4, 8, 4, PAIRS, PARTS>, 256, 256, 512);
+        if (cut.edge == 256) {
+            k_logits<T, 2, 4, 8, 4, PAIRS, PARTS, WHOLE><<<tiles, 512, 0, st>>>(r);
+            return;
+        }
     }
-    if (edge == 128) go(k_logits<T, 2, 2, 4, 4, PAIRS, PARTS>, 128, 128, 256);
-    else go(k_logits<T, 2, 2, 2, 2, PAIRS, PARTS>, 64, 64, 256);
+    if (cut.edge == 128) go(k_logits<T, 2, 2, 4, 4, PAIRS, PARTS, WHOLE>, k_logits<T, 2, 2, 4, 4, PAIRS, 0, SLICE>, k_logits<T, 2, 2, 4, 4, PAIRS, PARTS, JOIN>);
+    else go(k_logits<T, 2, 2, 2, 2, PAIRS, PARTS, WHOLE>, k_logits<T, 2, 2, 2, 2, PAIRS, 0, SLICE>, k_logits<T, 2, 2, 2, 2, PAIRS, PARTS, JOIN>);
 }
 
-// One piece's part of a gradient; `last`: its slices are joined.
-template <typename T, typename TO, bool BSUMS, int PAIRS>
-void gradient(const GradArgs& a, const Cut& c, bool last, hipStream_t st) {
-    GradArgs r = a;
-    r.per = c.per;
-    r.tm = (a.cols + c.edge - 1) / c.edge, r.tn = (int)((a.rows + c.edge - 1) / c.edge);
-    const dim3 grid((unsigned)r.tm * r.tn, c.slices);
-    const unsigned join = blocks_for((long long)r.tm * r.tn * c.edge * c.edge / 4);
-    if (c.edge == 256) {
-        if constexpr (PAIRS != 2) {
-            k_loss_grad<T, TO, 2, 4, 8, 4, BSUMS, PAIRS><<<grid, 512, 0, st>>>(r);
-            if (r.partial && last) k_grad_join<TO, 2, 4, 8, 4><<<join, 256, 0, st>>>(r, c.slices);
-        }
-    } else if (c.edge == 128) {
-        k_loss_grad<T, TO, 2, 2, 4, 4, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
-        if (r.partial && last) k_grad_join<TO, 2, 2, 4, 4><<<join, 256, 0, st>>>(r, c.slices);
-    } else {
-        k_loss_grad<T, TO, 2, 2, 2, 2, BSUMS, PAIRS><<<grid, 256, 0, st>>>(r);
-        if (r.partial && last) k_grad_join<TO, 2, 2, 2, 2><<<join, 256, 0, st>>>(r, c.slices);
+// A piece's part of du, of dw or of both, whose tiles are alike then. Slices are joined where `joined` says of how many.
+template <typename T, typename TO, int PAIRS>
+void gradients(GradArgs du, GradArgs dw, const Cut* cut_du, const Cut* cut_dw, const int (&joined)[2], hipStream_t st) {
+    unsigned blocks[2] = {}, most = 0;
+    const int edge = (cut_du ? cut_du : cut_dw)->edge;
+    auto place = [&](GradArgs& r, const Cut* c, int i) {
+        if (!c) return;
+        r.per = c->per;
+        r.tm = (r.cols + edge - 1) / edge, r.tn = (int)((r.rows + edge - 1) / edge);
+        blocks[i] = (unsigned)r.tm * r.tn * c->slices;
+        if (joined[i]) most = std::max(most, blocks_for((long long)r.tm * r.tn * edge * edge / 4));
+    };
+    place(du, cut_du, 0), place(dw, cut_dw, 1);
+    auto go = [&](auto kernel, auto join, int threads) {
+        kernel<<<blocks[0] + blocks[1], threads, 0, st>>>(du, dw, blocks[0]);
+        if (most) join<<<dim3(most, joined[0] && joined[1] ? 2 : 1), 256, 0, st>>>(du, dw, joined[0], joined[1]);
+    };
+    if constexpr (PAIRS != 2) {
+        if (edge == 256) return go(k_loss_grad<T, TO, 2, 4, 8, 4, PAIRS>, k_grad_join<TO, 2, 4, 8, 4>, 512);
     }
+    if (edge == 128) go(k_loss_grad<T, TO, 2, 2, 4, 4, PAIRS>, k_grad_join<TO, 2, 2, 4, 4>, 256);
+    else go(k_loss_grad<T, TO, 2, 2, 2, 2, PAIRS>, k_grad_join<TO, 2, 2, 2, 2>, 256);
 }
 
 // Operands ready, scales; the rest of the arguments of the logits.
@@ -795,9 +910,10 @@ LogitArgs prepared(const iodf_class_loss& a, const LossPlan& p, char* work, bool
     if (p.w_ready) r.y[1] = (uint16_t*)(work + p.w), l.w.p = r.y[1], l.w.ld = p.pitch, l.w.plane = (long long)a.classes * p.pitch;
     if (s || p.u_ready || p.w_ready) {
         const long long most = std::max<long long>(p.u_ready ? a.rows : 0, p.w_ready ? a.classes : 0) * (p.pitch / 8);
-        k_ready<TX><<<dim3(std::min(blocks_for(most), 4096u), p.w_ready ? 2 : 1), 256, 0, st>>>(r);
+        k_ready<TX><<<dim3(std::min(blocks_for(most), 1024u), p.w_ready ? 2 : 1), 256, 0, st>>>(r);
     }
     l.kts = p.kts, l.classes = a.classes, l.all = a.classes, l.rows = a.rows, l.scales = s, l.target = a.target, l.live = a.live;
+    l.sums = (f32x4*)(work + p.sums);
     return l;
 }
 
@@ -813,7 +929,7 @@ hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
         else if (p.few == 2) go(k_few<TX, 2>);
         else if constexpr (sizeof(TX) == 4) go(k_few<TX, 4>);
     } else {
-        logits<T, PAIRS, 0>(l, p.edge, st);
+        logits<T, PAIRS, 0>(l, p.logits, st);
     }
     auto join = [&](auto kernel, int rows) {
         kernel<<<(unsigned)((a.rows + rows - 1) / rows), 256, 0, st>>>(a.rows, p.tiles, a.classes, l.parts, l.picked, a.target, a.live, a.loss, a.lse);
@@ -836,38 +952,40 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
     const Side w = l.w;
     l.lse = a.lse, l.dloss = a.dloss, l.dlse = a.dlse;
     l.inverse = (float*)(work + p.scales), l.g = (uint16_t*)(work + p.g), l.g_ld = p.piece, l.g_plane = p.rows_up * p.piece;
-    float* const du_sums = p.du.slices > 1 || p.piece < a.classes ? (float*)(work + p.du_sums) : nullptr;
-    float* const dw_sums = p.dw.slices > 1 ? (float*)(work + p.dw_sums) : nullptr;
+    float* const du_sums = a.du && (p.du.slices > 1 || p.piece < a.classes) ? (float*)(work + p.du_sums) : nullptr;
+    float* const dw_sums = a.dw && p.dw.slices > 1 ? (float*)(work + p.dw_sums) : nullptr;
     for (long long v0 = 0; v0 < a.classes; v0 += p.piece) {
         const int n = (int)std::min<long long>(p.piece, a.classes - v0);
         l.first = v0, l.classes = n;
         l.w = w, l.w.p += v0 * w.ld, l.w.extent = l.w.depth = n;
-        if constexpr (PAIRS > 1) logits<T, PAIRS, 2>(l, p.edge, st);
-        else if (p.fine) logits<T, 1, 2>(l, p.edge, st);
-        else logits<T, 1, 1>(l, p.edge, st);
-        // with g in two parts where the operand has one
-        auto part = [&](const GradArgs& g, auto bsums, const Cut& c, bool last) {
-            if constexpr (PAIRS > 1) gradient<T, TX, bsums, 3>(g, c, last, st);
-            else if (p.fine) gradient<T, TX, bsums, 2>(g, c, last, st);
-            else gradient<T, TX, bsums, 1>(g, c, last, st);
+        if constexpr (PAIRS > 1) logits<T, PAIRS, 2>(l, p.logits, st);
+        else if (p.fine) logits<T, 1, 2>(l, p.logits, st);
+        else logits<T, 1, 1>(l, p.logits, st);
+        GradArgs du{}, dw{};
+        const bool last = v0 + n == a.classes;
+        du.a = {l.w.p, w.plane, w.ld, a.cols, n};
+        du.b = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
+        du.kts = (n + PK - 1) / PK, du.rows = a.rows, du.cols = a.cols, du.out = a.du, du.ld = a.du_stride;
+        du.partial = du_sums, du.add = v0 > 0;
+        du.down0 = s ? &s->ig : l.inverse, du.down1 = s ? &s->iw : nullptr;
+        dw.a = {l.u.p, l.u.plane, l.u.ld, a.cols, (int)a.rows};
+        dw.b = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};
+        dw.kts = (int)((a.rows + PK - 1) / PK), dw.rows = n, dw.cols = a.cols, dw.out = (TX*)a.dw + v0 * a.dw_stride, dw.ld = a.dw_stride;
+        dw.partial = dw_sums;
+        dw.down0 = s ? &s->ig : l.inverse, dw.down1 = s ? &s->iu : nullptr;
+        const int join_du = du_sums && last ? p.du.slices : 0, join_dw = dw_sums ? p.dw.slices : 0;
+        auto go = [&](const Cut* cut_du, const Cut* cut_dw) {
+            const int joined[2] = {cut_du ? join_du : 0, cut_dw ? join_dw : 0};
+            // with g in two parts where the operand has one
+            if constexpr (PAIRS > 1) gradients<T, TX, 3>(du, dw, cut_du, cut_dw, joined, st);
+            else if (p.fine) gradients<T, TX, 2>(du, dw, cut_du, cut_dw, joined, st);
+            else gradients<T, TX, 1>(du, dw, cut_du, cut_dw, joined, st);
         };
-        if (a.du) {
-            GradArgs g{};
-            g.a = {l.w.p, w.plane, w.ld, a.cols, n};
-            g.b = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
-            g.kts = (n + PK - 1) / PK, g.rows = a.rows, g.cols = a.cols, g.out = a.du, g.ld = a.du_stride;
-            g.partial = du_sums, g.add = v0 > 0;
-            g.down0 = s ? &s->ig : l.inverse, g.down1 = s ? &s->iw : nullptr;
-            part(g, std::false_type(), p.du, v0 + n == a.classes);
-        }
-        if (a.dw) {
-            GradArgs g{};
-            g.a = {l.u.p, l.u.plane, l.u.ld, a.cols, (int)a.rows};
-            g.b = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};
-            g.kts = (int)((a.rows + PK - 1) / PK), g.rows = n, g.cols = a.cols, g.out = (TX*)a.dw + v0 * a.dw_stride, g.ld = a.dw_stride;
-            g.partial = dw_sums;
-            g.down0 = s ? &s->ig : l.inverse, g.down1 = s ? &s->iu : nullptr;
-            part(g, std::true_type(), p.dw, true);
+        if (p.together) {
+            go(&p.du, &p.dw);
+        } else {
+            if (a.du) go(&p.du, nullptr);
+            if (a.dw) go(nullptr, &p.dw);
         }
     }
     return hipGetLastError();

@@ -658,3 +658,12 @@ def test_two_streams_at_once():
                 got[k].append(once(k))
     t.cuda.synchronize()
     assert all(t.equal(a, b) for k in range(2) for run in got[k] for a, b in zip(run, want[k]))
+
+
+@pytest.mark.parametrize("rows,classes,cols", [(3, 79, 8064), (2, 1031, 7360), (60, 200, 4100), (150, 140, 2050)])
+@pytest.mark.parametrize("name", NAMES)
+def test_class_loss_of_few_logits_and_long_rows(rows, classes, cols, name):
+    """The columns are split among workgroups: forward, gradients, padding."""
+    u, w, target, live, rng = some(rows, classes, cols, name, seed=3, dead=0.2)
+    check_forward(u, w, target, live, name)
+    check_backward(u, w, target, live, name, *upstream(rng, rows, "both"))
