@@ -1,8 +1,9 @@
 """MI355X-native integer-only discrete-flow inference (arXiv 2206.08869).
 
 Python surface = the C ABI of libiodf (include/iodf.h) plus a small convenience
-class, the training operators of residual blocks on torch tensors (blocks.py), and the loss and the updates of a training step (step.py). Importing the package does not load the library; the first call does, and
-raises if it has not been built.
+class, the training operators of residual blocks on torch tensors (blocks.py), and the loss and
+the updates of a training step (step.py). Importing the package does not load the library; the
+first call does, and raises if it has not been built.
 """
 from .binding import (Flow, IodfError, build_library, load_library, iodf_init, iodf_forward, iodf_inverse,
                       iodf_query, iodf_free, iodf_profile_begin, iodf_profile_end, iodf_prior_cf, iodf_encode, iodf_encode_noalloc,

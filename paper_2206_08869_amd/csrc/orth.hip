@@ -86,6 +86,7 @@ __device__ __forceinline__ double squares(const Source& src, const Shape& z, int
     return s;
 }
 
+// Memory bounds it: 4096 x 8192 in bfloat16 with momenta 55 us (6.1 TB/s, the last-level cache helping), 4096 x 4096 of 32 bits 13.4.
 template <typename TG, bool MUON>
 __global__ __launch_bounds__(256) void k_orth_norm(const Source src, const Shape z, double* sums) {
     __shared__ double meet[4];
@@ -118,6 +119,7 @@ __device__ __forceinline__ void start_x(const Source& src, const Shape& z, int k
     }
 }
 
+// As k_orth_norm: 60 us and 26.
 template <typename TG, bool MUON>
 __global__ __launch_bounds__(256) void k_orth_start(const Source src, const Shape z, const double* sums, int parts, float eps, float lift, _Float16* x,
                                                     long long plane) {
@@ -267,7 +269,8 @@ __device__ __forceinline__ void finish_square(const SquareArgs& a, P& p, int k, 
     }
 }
 
-// A tile on or below the diagonal of a symmetric product, all of its sum.
+// A tile on or below the diagonal of a symmetric product, all of its sum. 4096 x 4096 is 136 tiles of 256, one round of 92 us on half the compute units, or 253 of
+// 192, one round of 71 on all of them (the second product 98 and 75). Of that a tile's way in and out is 15 us.
 template <int MW, int NW, int MT, int NT, bool SUMS, bool SECOND, int PAIRS>
 __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
     typedef Products<_Float16, MW, NW, MT, NT, SUMS, SUMS, PAIRS> P;
@@ -285,7 +288,8 @@ __global__ __launch_bounds__(MW * NW * 64) void k_square(const SquareArgs a) {
 
 // The same where tiles are few or do not go round the compute units evenly: all tiles' steps along their sums are one line, of which every workgroup takes
 // an equal piece, through the ends of tiles. A piece's part of a tile is kept as sums, in the order in which lanes hold them, in place piece + tile, and a
-// second kernel adds a tile's parts up. 4096 x 4096 is 136 tiles of 256: 1.9 compute units to a tile.
+// second kernel adds a tile's parts up. The 4096 x 4096 above takes 75 and 29 us this way, more than tiles of 192; 1111 x 520 in
+// 32 bits 10.9 and 10 where tiles of 64 take 16.4. It is for few tiles of long sums: 700 x 8200, 6 tiles of 256 with 128 steps.
 __device__ __forceinline__ long long piece_begin(const SquareArgs& a, long long w) { return w * a.units / a.pieces; }
 __device__ __forceinline__ long long piece_of(const SquareArgs& a, long long unit) { return ((unit + 1) * a.pieces - 1) / a.units; }
 
@@ -405,6 +409,8 @@ __device__ __forceinline__ void deliver_quad(const Target& t, int k, int r, int 
     put_quad(to, n, v);
 }
 
+// 4096 x 4096: 132 to 136 us (1010 to 1040 TFLOP/s) of which 97 are the products at the rate of long sums: every compute unit has one tile, so that nothing covers
+// its first loads, and its 64 KB of X in two parts read and written.
 // (a + e) X + B X: columns of X are the rows of the matrix instructions, so that a lane holds four neighbours of a row.
 template <int MW, int NW, int MT, int NT, bool TALL, int PAIRS>
 __global__ __launch_bounds__(MW * NW * 64) void k_apply(const ApplyArgs a, const Target target, const int type) {
@@ -525,7 +531,8 @@ struct SlimArgs {
 
 // A workgroup adds up A's parts, has A^2 and b A + c A^2 in LDS, applies it to its own blocks of X, and adds what these give to the next A. That is a step
 // with one launch (KIND STEP; FIRST: only the first A; LAST: the result goes to `target`), and where a workgroup has a whole matrix (ALL: at most 256 along
-// the longer side) all steps with one, norm and start included. What bounds it is the launch and a dozen dependent trips to memory and LDS a step.
+// the longer side) all steps with one, norm and start included. What bounds it is the launch and a dozen dependent trips to memory and LDS a step. As three
+// launches a step 64 x 300 and 64 x 64 take 85 us, here 51 and 22.
 enum { SLIM_FIRST, SLIM_STEP, SLIM_LAST, SLIM_ALL };
 
 template <bool TALL, int PAIRS, int KIND, bool MUON>
@@ -748,11 +755,162 @@ __global__ __launch_bounds__(256) void k_slim(const SlimArgs a, const int step, 
     for (int b = 0; b < 4; ++b) *(f32x4*)(to + (b * 16 + low) * S + q) = next[b];
 }
 
+// ---- one block of 128 x 128 ----
+
+// A matrix of 65 to 128 rows and columns, all of it in a workgroup's LDS with zeros around it, X in two parts and A, then b A + c A^2, in the place of each other.
+// Norm, start and all steps in one launch; tall ones go as the others do, which in a square of zeros is the same. What bounds it is LDS: a step reads a megabyte of
+// fragments (three with both parts), and the dependent ways between them. 128 x 128 in bfloat16 51 us, as three launches a step 69.
+template <int PAIRS, bool MUON>
+__global__ __launch_bounds__(512) void k_block(const Shape z, const OrthSteps steps, const Source src, const int in_type, const float eps, const Target target,
+                                               const int type) {
+    constexpr int PARTS = PAIRS > 1 ? 2 : 1, S = 128;
+    __shared__ __align__(16) uint16_t a[PARTS][S * S], x[2][S * S];
+    __shared__ __align__(16) float d[S], e[S];
+    __shared__ double meet[8];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, low = lane & 15, q = wave * 16 + lane / 16 * 4, k = blockIdx.x;
+    auto at = [](int r, int c) { return r * S + ((c / 8) ^ (r >> 1 & 7)) * 8 + c % 8; };
+    auto rows = [&](const uint16_t* t, int r0, int step) { return *(const s16x8*)(t + at(r0 + low, step * 32 + lane / 16 * 8)); };
+    auto sums = [&](const uint16_t* t, int c0, int step) {
+        const int r = step * 32 + lane / 16 * 8 + (lane >> 2 & 3), c = c0 + (lane & 3) * 4;
+        union { s16x4 h[2]; s16x8 v; } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + at(r, c)));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + at(r + 4, c)));
+        return u.v;
+    };
+    // four neighbours q .. q + 3 of row 16 b + low, small products first
+    f32x4 acc[8];
+    auto multiply = [&](auto left, auto right) {
+#pragma unroll
+        for (int b = 0; b < 8; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = PAIRS > 1 ? 0 : 2; p < 3; ++p)
+#pragma unroll
+            for (int step = 0; step < S / 32; ++step) {
+                const s16x8 l = left(p == 1, step);
+#pragma unroll
+                for (int b = 0; b < 8; ++b) acc[b] = Mma<_Float16>::go(l, right(p == 0, b, step), acc[b]);
+            }
+    };
+    auto put4 = [](uint16_t (*t)[S * S], int parts, int to, const float (&v)[4]) {
+        _Float16 hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) two_parts(v[j], hi[j], lo[j]);
+        __builtin_memcpy(&t[0][to], hi, 8);
+        if (parts > 1) __builtin_memcpy(&t[parts - 1][to], lo, 8);
+    };
+    auto get4 = [](const uint16_t (*t)[S * S], int parts, int from, float (&v)[4]) {
+        _Float16 hi[4], lo[4];
+        __builtin_memcpy(hi, &t[0][from], 8);
+        if (parts > 1) __builtin_memcpy(lo, &t[parts - 1][from], 8);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (float)hi[j] + (parts > 1 ? (float)lo[j] : 0.f);
+    };
+    auto begin = [&](auto t) {
+        typedef decltype(t) TG;
+        double s = squares<TG, MUON>(src, z, k, tid, 512);
+#pragma unroll
+        for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
+        if (lane == 0) meet[wave] = s;
+        __syncthreads();  // momenta are in memory, too
+        s = 0.0;
+        for (int w = 0; w < 8; ++w) s += meet[w];
+        const double by = (double)ldexpf(1.f, steps.x_exp[0]) / (sqrt(s) + (double)eps);
+#pragma unroll
+        for (int i = 0; i < S * S / 8 / 512; ++i) {
+            const int r = (i * 512 + tid) / (S / 8), c = (i * 512 + tid) % (S / 8) * 8;
+            float v[8] = {};
+            if (r < z.rows && c < z.cols) taken<TG, MUON, false>(src, k, r, c, z.cols, v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = c + h * 4 + j < z.cols ? (float)(v[h * 4 + j] * by) : 0.f;
+                put4(x, 2, at(r, c + h * 4), w);
+            }
+        }
+        __syncthreads();
+    };
+    if (in_type == IODF_T_F32) begin(0.f);
+    else if (in_type == IODF_T_BF16) begin((__bf16)0.f);
+    else begin((_Float16)0.f);
+    for (int i = 0; i < steps.n; ++i) {
+        const bool end = i + 1 == steps.n;
+        const float unlift = ldexpf(1.f, -steps.x_exp[i]), lift = end ? 1.f : ldexpf(1.f, steps.x_exp[i + 1]);
+        const float o_lift = ldexpf(1.f, steps.a_exp[i]), b_lift = ldexpf(1.f, steps.b_exp[i]), ca = steps.a[i], cb = steps.b[i], cc = steps.c[i];
+        multiply([&](int p, int step) { return rows(x[p], wave * 16, step); }, [&](int p, int b, int step) { return rows(x[p], b * 16, step); });
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {  // symmetric: four rows of a column are four neighbours of a row
+            const int r = b * 16 + low;
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = acc[b][j] * (unlift * unlift);
+                if (r == q + j) d[r] = v[j];
+                v[j] = r == q + j ? 0.f : v[j] * o_lift;
+            }
+            put4(a, PARTS, at(r, q), v);
+        }
+        lds_barrier();
+        multiply([&](int p, int step) { return rows(a[p * (PARTS - 1)], wave * 16, step); },
+                 [&](int p, int b, int step) { return rows(a[p * (PARTS - 1)], b * 16, step); });
+        const float down = 1.f / (o_lift * o_lift), un = 1.f / o_lift;
+        float v[8][4];
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+            const int r = b * 16 + low;
+            get4(a, PARTS, at(r, q), v[b]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float sum = acc[b][j] * down, ov = v[b][j] * un;
+                if (r == q + j) e[r] = fmaf(cc, fmaf(d[r], d[r], sum), cb * d[r]);
+                v[b][j] = r == q + j ? 0.f : fmaf(cc, fmaf(d[r] + d[q + j], ov, sum), cb * ov) * b_lift;
+            }
+        }
+        lds_barrier();  // A has been read by all
+#pragma unroll
+        for (int b = 0; b < 8; ++b) put4(a, PARTS, at(b * 16 + low, q), v[b]);
+        lds_barrier();
+        multiply([&](int p, int step) { return sums(x[p], wave * 16, step); }, [&](int p, int b, int step) { return rows(a[p * (PARTS - 1)], b * 16, step); });
+        const float back = unlift / b_lift;
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+            const int r = b * 16 + low;
+            get4(x, 2, at(r, q), v[b]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[b][j] = fmaf(ca + e[r], v[b][j] * unlift, acc[b][j] * back) * lift;
+        }
+        lds_barrier();  // X has been read by all
+        if (!end) {
+#pragma unroll
+            for (int b = 0; b < 8; ++b) put4(x, 2, at(b * 16 + low, q), v[b]);
+            lds_barrier();
+            continue;
+        }
+        float* const t = (float*)x;  // rows of 128 numbers, to be delivered as they lie
+#pragma unroll
+        for (int b = 0; b < 8; ++b) __builtin_memcpy(t + (b * 16 + low) * S + (q ^ (low & 7) * 4), v[b], 16);
+        lds_barrier();
+#pragma unroll
+        for (int n = 0; n < S * S / 4 / 512; ++n) {
+            const int r = n * 16 + tid / 32, c = tid % 32 * 4;
+            if (r >= z.rows || c >= z.cols) continue;
+            float w[4];
+            __builtin_memcpy(w, t + r * S + (c ^ (r & 7) * 4), 16);
+            if (type == IODF_T_F32) deliver_quad<float>(target, k, r, c, z.cols - c, w);
+            else if (type == IODF_T_BF16) deliver_quad<__bf16>(target, k, r, c, z.cols - c, w);
+            else deliver_quad<_Float16>(target, k, r, c, z.cols - c, w);
+        }
+    }
+}
+
 // A square product's tiles, and how many workgroups go through them piece by piece (0: one to a tile).
 struct Cut {
     int edge, tiles, pieces;
 };
 
+// Estimated times in us, from these measurements (4096 x 4096, 8192 x 2048, 2048 x 512 eight times, 1111 x 520, 777 x 333 three times): a step along a tile's sum and
+// product takes 1.13 with tiles of 256, 0.7 of 192, 0.23 to 0.25 a tile of 64 and compute unit; a piece's 1.5 to 1.9 and 0.3 to 0.75, and joining goes by the sums moved. Of
+// three products 2048 x 512 eight times takes 131 us with tiles of 256, 94 of 192, 34.5 of 64, 28 + 14 in pieces of 128.
 Cut cut_of(long long count, int s, int kts, int products, bool sums) {
     Cut best{};
     float least = 0.f;
@@ -782,6 +940,7 @@ Cut cut_of(long long count, int s, int kts, int products, bool sums) {
 struct OrthPlan {
     Shape z;
     bool tall, parts;          // parts: three products
+    bool block;                // by k_block
     int groups, per;           // of k_slim, 0: not by it
     Cut first, second;
     int apply_edge;
@@ -804,6 +963,8 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     }
     p.first = cut_of(count, p.z.s, (p.tall ? p.z.rp : p.z.cp) / PK, p.parts ? 3 : 1, p.tall);
     p.second = cut_of(count, p.z.s, p.z.sp / PK, p.parts ? 3 : 1, false);
+    // Tiles of 256, 128, 64, us: 4096 x 4096 133, 167, 213; 8192 x 2048 86, 99, 125; 2048 x 512 eight times, three products 60, 44, 52; 1111 x 520 57, 27, 17 and
+    // 777 x 333 three times 48, 22, 14: the largest tiles that half fill the chip, or three quarters of it.
     p.apply_edge = apply(256) >= 130 ? 256 : apply(128) >= 200 ? 128 : 64;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -814,6 +975,11 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     const size_t x = (size_t)count * p.z.rp * p.z.cp * 2 * 2, s = (size_t)count * p.z.sp * p.z.sp * 2 * (p.parts ? 2 : 1);
     p.parts_of_norm = (int)std::max<long long>(1, std::min<long long>({kNormBlocks, 2048 / std::max<long long>(1, count), ((long long)rows * ((cols + 7) / 8) + 255) / 256}));
     p.sums = take((size_t)count * p.parts_of_norm * 8);
+    p.block = p.z.s > 64 && std::max(rows, cols) <= 128;
+    if (p.block) {
+        p.bytes = at;
+        return p;
+    }
     p.x0 = take(x);
     if (p.groups) {
         p.pieces = take((size_t)2 * count * p.groups * 64 * 64 * 4);
@@ -927,6 +1093,11 @@ void slim(const OrthPlan& p, const OrthSteps& s, char* work, const Target& targe
 
 template <bool MUON>
 hipError_t all_at_once(const Source& src, int in_type, const OrthPlan& p, const OrthSteps& s, float eps, char* work, const Target& target, int type, hipStream_t st) {
+    if (p.block) {
+        auto go = [&](auto kernel) { kernel<<<p.z.count, 512, 0, st>>>(p.z, s, src, in_type, eps, target, type); };
+        p.parts ? go(k_block<3, MUON>) : go(k_block<1, MUON>);
+        return hipGetLastError();
+    }
     SlimArgs a{};
     a.x = (_Float16*)(work + p.x0), a.plane = (long long)p.z.rp * p.z.cp * p.z.count, a.z = p.z, a.groups = 1, a.per = p.per, a.steps = s;
     auto go = [&](auto kernel) { kernel<<<dim3(1, p.z.count), 256, 0, st>>>(a, 0, src, in_type, eps, target, type); };
@@ -993,7 +1164,7 @@ hipError_t launch_orthogonalise(const iodf_orth& a, const OrthSteps& s, void* wo
     src.g[0] = a.in, src.stride = a.in_stride, src.batch = a.in_batch;
     Target t{};
     t.w[0] = a.out, t.stride = a.out_stride, t.batch = a.out_batch;
-    if (p.groups == 1) return all_at_once<false>(src, a.in_type, p, s, a.eps, (char*)work, t, a.out_type, st);
+    if (p.block || p.groups == 1) return all_at_once<false>(src, a.in_type, p, s, a.eps, (char*)work, t, a.out_type, st);
     begin<false>(src, a.in_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
     return run(p, s, (char*)work, t, a.out_type, st);
 }
@@ -1006,7 +1177,7 @@ hipError_t launch_muon_step(const iodf_muon& a, const OrthSteps& s, void* work, 
     src.stride = a.grad_stride, src.beta = a.beta, src.nesterov = a.nesterov;
     t.stride = a.weight_stride, t.update = 1;
     t.keep = (float)(1.0 - (double)a.rate * a.decay), t.by = (float)(-(double)a.rate * a.scale);
-    if (p.groups == 1) return all_at_once<true>(src, a.grad_type, p, s, a.eps, (char*)work, t, a.weight_type, st);
+    if (p.block || p.groups == 1) return all_at_once<true>(src, a.grad_type, p, s, a.eps, (char*)work, t, a.weight_type, st);
     begin<true>(src, a.grad_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
     return run(p, s, (char*)work, t, a.weight_type, st);
 }

@@ -7,6 +7,10 @@
 // so that no operand is ever transposed in memory. A number of more bits than 16 is two parts, high and low (planes of the same
 // layout), and the sum of three products: high low, low high, high high (the small ones first, while the sums
 // that they are rounded to are small too); or of two where only B has low parts.
+//
+// Tiles of 256 x 256 with eight waves are bound by power: logits of 8192 rows, 65536 classes and 4096 columns run at 1390 to 1440 TFLOP/s with random numbers
+// and at 1754 with zeros. The 16 x 16 x 32 instruction moves fewer sums for an operation than the 32 x 32 x 16 one, which made 1430 of 1305. Reads that meet
+// no bank twice, and reads and loads dealt out between the products by hand, were 3 percent each.
 #pragma once
 #include <type_traits>
 

@@ -667,3 +667,40 @@ def test_class_loss_of_few_logits_and_long_rows(rows, classes, cols, name):
     u, w, target, live, rng = some(rows, classes, cols, name, seed=3, dead=0.2)
     check_forward(u, w, target, live, name)
     check_backward(u, w, target, live, name, *upstream(rng, rows, "both"))
+
+
+@pytest.mark.parametrize("rows,cols", [(65, 65), (128, 128), (128, 65), (70, 127), (100, 101)])
+@pytest.mark.parametrize("to", NAMES)
+def test_orthogonalise_one_block(rows, cols, to):
+    """Matrices that fit a workgroup's LDS: several, tall and wide, strided and in place; the step of an optimiser the same."""
+    t = torch()
+    rng = np.random.default_rng(rows + cols)
+    g = np.stack([as_type(gradient(rng, rows, cols), to) for _ in range(3)])
+    wide = t.full((3, rows + 1, cols + 3), float("nan"), dtype=dtype(to), device="cuda")
+    view = wide[:, 1:, 2:-1]
+    view.copy_(dev(g.reshape(-1, cols), to).view(3, rows, cols))
+    given = view.clone()
+    iodf.orthogonalise(view, out=view)
+    assert wide.isnan().sum() == wide.numel() - view.numel()
+    for x, y in zip(g, view):
+        check_orth(y, x, to)
+    w = [t.zeros((rows, cols), device="cuda", dtype=dtype(to)) for _ in range(3)]
+    m = [t.zeros((rows, cols), device="cuda") for _ in range(3)]
+    iodf.muon_step(w, list(given), m, 1.0, beta=0.0, nesterov=False, scale=-1.0)
+    for k in range(3):
+        assert t.equal(m[k], given[k].float()) and t.equal(w[k], view[k])
+
+
+@pytest.mark.parametrize("rows,cols", [(128, 128), (70, 100)])
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("grad", NAMES)
+def test_muon_step_one_block(rows, cols, name, grad):
+    rng = np.random.default_rng(19)
+    w, g, m = as_type(rng.standard_normal((rows, cols)) / np.sqrt(cols), name), as_type(gradient(rng, rows, cols), grad), as_type(gradient(rng, rows, cols), "f32")
+    wt, mt = dev(w, name), dev(m)
+    iodf.muon_step(wt, dev(g, grad), mt, 0.05, beta=0.9, decay=0.2, scale=0.7)
+    new = np.float64(np.float32(0.9)) * m + g
+    near(mt, new, "f32", 2 * U * (np.abs(m) + np.abs(g)), "momentum")
+    step, off = ref.orthogonalise(g + 0.9 * new, parts=name != "bf16")
+    want = (1 - 0.05 * 0.2) * w - 0.05 * 0.7 * step
+    assert np.linalg.norm(host(wt) - want) <= np.linalg.norm(half_unit(name, want)) + 0.05 * 0.7 * off + 4 * U * np.linalg.norm(w)
