@@ -798,13 +798,17 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     p.u_ready = !in_place(a.u, a.u_stride, a.cols, p.wide) || (backward && a.live);
     p.w_ready = !in_place(a.w, a.w_stride, a.cols, p.wide);
     p.scaled = p.wide || (backward && a.type == IODF_T_F16);
-    // Sums of few numbers do not average the rounding of g to 16 bits: it would make gradients 1.6 times as far off as their own last rounding (14 rows, 7
-    // classes: 2.7e-3 for 1.7e-3). A second part costs a second product, which is time only where products are most of it.
-    p.fine = backward && !p.wide && (a.rows <= 256 || a.classes <= 16 || 2.0 * a.rows * a.classes * a.cols <= 4e9);
+    // Where a few numbers g make up a gradient, the rounding to 16 bits makes it up to twice as far off as its own last rounding does: of few rows (1 row, 79857
+    // classes: 2.0 times), few classes (100000 rows, 14 classes: 1.4), few numbers altogether (14 rows, 7 classes: 1.6) or few columns, where products cost least
+    // (23726 rows, 2091 classes of 11 columns: 1.5); 200 rows, 300 classes of 8000 columns 1.26 times, 21 rows, 40000 classes of 3000 1.17. A second part costs a
+    // second product: 256 rows, 4000 classes of 512 columns 28 us for 22, 32000 classes of 4096 columns 607 for 339.
+    p.fine = backward && !p.wide && (a.rows <= 16 || a.classes <= 32 || a.cols <= 128 || a.rows * a.classes <= 65536);
     p.rows_up = up(a.rows, 256);
     p.logits = logits_cut(a.classes, a.rows, p.kts, p.wide ? 3 : 1, p.fine ? 128 : 256);
     p.tiles = (a.classes + p.logits.edge - 1) / p.logits.edge;
-    if (!backward && p.w_ready && a.rows <= (p.wide ? 64 : 32)) {
+    // us by k_few and by a copy and tiles, 32000 classes of 1111 columns: in 32 bits 32 and 108 for a row, 47 and 110 for 32, 75 and 114 for 64; in bfloat16 29 and
+    // 42 for a row, 37 and 43 for 16, 57 and 43 for 32.
+    if (!backward && p.w_ready && a.rows <= (p.wide ? 64 : 16)) {
         const int blocks = (int)((a.rows + 15) / 16), groups = (a.classes + 31) / 32;
         p.few = blocks <= 1 ? 1 : blocks <= 2 ? 2 : 4;
         p.groups = (groups + 2047) / 2048;
@@ -933,8 +937,7 @@ hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
         const FewArgs f{a.w, a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.groups, a.target, l.parts, l.picked};
         auto go = [&](auto kernel) { kernel<<<(unsigned)p.tiles, 256, 0, st>>>(f); };
         if (p.few == 1) go(k_few<TX, 1>);
-        else if (p.few == 2) go(k_few<TX, 2>);
-        else if constexpr (sizeof(TX) == 4) go(k_few<TX, 4>);
+        else if constexpr (sizeof(TX) == 4) p.few == 2 ? go(k_few<TX, 2>) : go(k_few<TX, 4>);
     } else {
         logits<T, PAIRS, 0>(l, p.logits, st);
     }
