@@ -225,6 +225,11 @@ struct FewArgs {
     const int64_t* target;
     f32x2* parts;
     float* picked;
+    float* g;            // gradients: [classes][16], the other two are not looked at then
+    const uint8_t* live;
+    const float* lse;
+    const float* dloss;
+    const float* dlse;
 };
 
 // Sixteen bytes along k of a row, of which n elements exist.
@@ -253,7 +258,7 @@ __device__ __forceinline__ f32x4 product<float>(u32x4 w, u32x4 u, f32x4 c) {
 // Rows that do not fill a tile, of a table that would have to be copied for tiles: it is read once, as it lies, straight into registers, 32 classes to a workgroup whose four waves share out the
 // columns. NB blocks of 16 rows. Which columns a lane holds is the same for both operands and otherwise of no matter: in 32 bits four neighbours
 // are four products of the 32-bit matrix instruction.
-template <typename TX, int NB>
+template <typename TX, int NB, bool GRAD>
 __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
     constexpr int E = 16 / (int)sizeof(TX), STEP = 4 * E, AT_ONCE = NB <= 2 ? 4 : 2, SPAN = STEP * AT_ONCE;
     __shared__ f32x4 meet[4][2][NB][64];
@@ -305,6 +310,22 @@ __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
         for (int n = wave; n < NB; n += 4) {  // the waves share out the blocks of rows
             const int t = n * 16 + r;
             const long long want = t < a.rows ? a.target[t] - c0 : -1;
+            if (GRAD) {
+                const bool there = t < a.rows && !(a.live && !a.live[t]);
+                const float lse = there ? a.lse[t] : 0.f;
+                float up = there && a.dloss ? a.dloss[t] : 0.f, both = up + (there && a.dlse ? a.dlse[t] : 0.f);
+                if (there && (want < -c0 || want >= a.classes - c0)) up = both = __builtin_nanf("");
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const f32x4 s = (meet[0][b][n][lane] + meet[1][b][n][lane]) + (meet[2][b][n][lane] + meet[3][b][n][lane]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int c = b * 16 + lane / 16 * 4 + j;
+                        if (c0 + c < a.classes) a.g[(c0 + c) * 16ll + r] = there ? both * expf(s[j] - lse) - (want == c ? up : 0.f) : 0.f;
+                    }
+                }
+                continue;
+            }
             float v[8], top = -__builtin_inff();
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -326,6 +347,7 @@ __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
                 if (i == n) all[i] = merged(all[i], f32x2{top, sum});
         }
     }
+    if (GRAD) return;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         if (n % 4 != wave) continue;
@@ -334,6 +356,82 @@ __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
         v = merged(v, f32x2{__shfl_xor(v[0], 32), __shfl_xor(v[1], 32)});
         if (lane < 16 && n * 16 + r < a.rows) a.parts[(long long)blockIdx.x * a.rows + n * 16 + r] = v;
     }
+}
+
+struct FewGradArgs {
+    const float* w;
+    const float* u;
+    long long w_stride, u_stride;
+    int classes, cols, rows, per;  // per: classes to a wave
+    const uint8_t* live;
+    const float* g;
+    float* du;                     // NULL: not asked for, as dw
+    float* dw;
+    long long du_stride, dw_stride;
+    float* sums;                   // [workgroup along the classes][R][cols], rounded up to 256
+    int slices, pitch;
+};
+
+// Gradients of up to sixteen rows in 32 bits: a wave has 256 columns of u and of du in registers, goes through its classes, adds g W to du, and writes g' u to dw.
+// Nothing is copied or scaled for it, and memory bounds it: with the logits before it W is read twice and dw written, 24000 classes of 6592 columns 427 us (4.4 TB/s).
+template <int R>
+__global__ __launch_bounds__(256) void k_few_grad(const FewGradArgs a) {
+    constexpr int AT_ONCE = 4;
+    __shared__ f32x4 meet[3][R][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = blockIdx.x * 256 + lane * 4, n = a.cols - c;
+    float u[R][4], du[R][4] = {};
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        u[t][0] = u[t][1] = u[t][2] = u[t][3] = 0.f;
+        if (t < a.rows && n > 0 && !(a.live && !a.live[t])) get_quad(a.u + t * a.u_stride + c, n, u[t]);
+    }
+    const int v0 = ((int)blockIdx.y * 4 + wave) * a.per, v1 = min(a.classes, v0 + a.per);
+    for (int v = v0; v < v1; v += AT_ONCE) {
+        float w[AT_ONCE][4] = {};
+        if (a.du && n > 0) {
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) get_quad(a.w + min(v + k, a.classes - 1) * a.w_stride + c, n, w[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (v + k >= v1) break;
+            const float* const g = a.g + (v + k) * 16ll;
+            float out[4] = {};
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                const float gt = g[t];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) du[t][j] = fmaf(gt, w[k][j], du[t][j]), out[j] = fmaf(gt, u[t][j], out[j]);
+            }
+            if (a.dw && n > 0) put_quad(a.dw + (v + k) * a.dw_stride + c, n, out);
+        }
+    }
+    if (!a.du) return;
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+        if (wave) meet[wave - 1][t][lane] = f32x4{du[t][0], du[t][1], du[t][2], du[t][3]};
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        const f32x4 s = (f32x4{du[t][0], du[t][1], du[t][2], du[t][3]} + meet[0][t][lane]) + (meet[1][t][lane] + meet[2][t][lane]);
+        *(f32x4*)(a.sums + ((long long)blockIdx.y * R + t) * a.pitch + c) = s;
+    }
+}
+
+// The workgroups' sums: 64 columns of a row to a workgroup, sixteen threads to four columns.
+__global__ __launch_bounds__(256) void k_few_join(const FewGradArgs a, const int per_slice) {
+    __shared__ f32x4 meet[256];
+    const int c = blockIdx.x * 64 + threadIdx.x % 16 * 4, t = blockIdx.y;
+    f32x4 s{0.f, 0.f, 0.f, 0.f};
+    for (int k = threadIdx.x / 16; k < a.slices; k += 16) s += *(const f32x4*)(a.sums + ((long long)k * per_slice + t) * a.pitch + c);
+    meet[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x >= 16 || c >= a.cols) return;
+    for (int k = 1; k < 16; ++k) s += meet[k * 16 + threadIdx.x];
+    const bool there = !(a.live && !a.live[t]);
+    const float v[4] = {there ? s[0] : 0.f, there ? s[1] : 0.f, there ? s[2] : 0.f, there ? s[3] : 0.f};
+    put_quad(a.du + t * a.du_stride + c, a.cols - c, v);
 }
 
 // g is rounded to 16 bits, and in most programs dloss is the same number in every row: what the rounding does to it would be the same everywhere, and not
@@ -776,6 +874,7 @@ struct LossPlan {
     bool fine;                            // g in two parts though the operands have one
     int pitch, kts;
     int few, groups;                      // blocks of 16 rows of k_few (0: tiles), groups of classes to its workgroups
+    int few_rows, few_per, few_slices;    // backward: R of k_few_grad, classes to a wave, workgroups along the classes
     Cut logits;
     int tiles;                            // of classes
     int maxima_parts;
@@ -814,6 +913,21 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.groups = (groups + 2047) / 2048;
         p.tiles = (groups + p.groups - 1) / p.groups;
         p.u_ready = p.w_ready = p.scaled = false;
+    }
+    // us by k_few and k_few_grad and by tiles, in 32 bits: 24000 classes of 6592 columns 427 and 863 for a row, 538 and 910 for 16; 32000 of 1111 112 and 220, 135 and 221;
+    // 50 of 100 20 and 25. In bfloat16, where tiles read W as it lies, 363 and 405, 115 and 113, 20 and 21 for a row: not by these.
+    if (backward && p.wide && a.rows && a.rows <= 16) {
+        const int groups = (a.classes + 31) / 32, across = (a.cols + 255) / 256, waves = std::max(1, 512 / across) * 4;
+        p.few = 1;
+        p.groups = (groups + 2047) / 2048;
+        p.tiles = (groups + p.groups - 1) / p.groups;
+        p.few_rows = a.rows <= 2 ? 2 : a.rows <= 4 ? 4 : a.rows <= 8 ? 8 : 16;
+        p.few_per = std::max(4, (a.classes + waves - 1) / waves);
+        p.few_slices = (a.classes + 4 * p.few_per - 1) / (4 * p.few_per);
+        const size_t g = (size_t)up((long long)a.classes * 16 * 4, 256);
+        p.g = 0, p.du_sums = g;
+        p.bytes = g + (a.du ? (size_t)p.few_slices * p.few_rows * across * 256 * 4 : 0);
+        return p;
     }
     p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, ((p.wide ? std::max<long long>(a.rows, a.classes) * p.pitch / 8 : a.rows) + 511) / 512));
     size_t at = 0;
@@ -934,10 +1048,10 @@ hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
     LogitArgs l = prepared<TX>(a, p, work, false, st);
     l.parts = (f32x2*)(work + p.parts), l.picked = (float*)(work + p.picked);
     if (p.few) {
-        const FewArgs f{a.w, a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.groups, a.target, l.parts, l.picked};
+        const FewArgs f{a.w, a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.groups, a.target, l.parts, l.picked, nullptr, nullptr, nullptr, nullptr, nullptr};
         auto go = [&](auto kernel) { kernel<<<(unsigned)p.tiles, 256, 0, st>>>(f); };
-        if (p.few == 1) go(k_few<TX, 1>);
-        else if constexpr (sizeof(TX) == 4) p.few == 2 ? go(k_few<TX, 2>) : go(k_few<TX, 4>);
+        if (p.few == 1) go(k_few<TX, 1, false>);
+        else if constexpr (sizeof(TX) == 4) p.few == 2 ? go(k_few<TX, 2, false>) : go(k_few<TX, 4, false>);
     } else {
         logits<T, PAIRS, 0>(l, p.logits, st);
     }
@@ -950,6 +1064,21 @@ hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
     return hipGetLastError();
 }
 
+hipError_t few_backward(const iodf_class_loss& a, const LossPlan& p, char* work, hipStream_t st) {
+    const FewArgs f{a.w, a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.groups, a.target, nullptr, nullptr, (float*)(work + p.g), a.live, a.lse, a.dloss, a.dlse};
+    k_few<float, 1, true><<<(unsigned)p.tiles, 256, 0, st>>>(f);
+    const int across = (a.cols + 255) / 256;
+    const FewGradArgs g{(const float*)a.w, (const float*)a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.few_per, a.live, f.g, (float*)a.du, (float*)a.dw, a.du_stride, a.dw_stride,
+                        (float*)(work + p.du_sums), p.few_slices, across * 256};
+    auto go = [&](auto kernel) { kernel<<<dim3(across, p.few_slices), 256, 0, st>>>(g); };
+    if (p.few_rows == 2) go(k_few_grad<2>);
+    else if (p.few_rows == 4) go(k_few_grad<4>);
+    else if (p.few_rows == 8) go(k_few_grad<8>);
+    else go(k_few_grad<16>);
+    if (a.du) k_few_join<<<dim3((a.cols + 63) / 64, (unsigned)a.rows), 256, 0, st>>>(g, p.few_rows);
+    return hipGetLastError();
+}
+
 template <typename TX, typename T, int PAIRS>
 hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
     if (a.rows == 0) {
@@ -957,6 +1086,9 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
         return hipGetLastError();
     }
     const LossPlan p = loss_plan(a, true);
+    if constexpr (PAIRS > 1) {
+        if (p.few) return few_backward(a, p, work, st);
+    }
     LogitArgs l = prepared<TX>(a, p, work, true, st);
     const Scales* const s = l.scales;
     const Side w = l.w;

@@ -963,9 +963,10 @@ OrthPlan orth_plan(long long count, int rows, int cols, int type) {
     }
     p.first = cut_of(count, p.z.s, (p.tall ? p.z.rp : p.z.cp) / PK, p.parts ? 3 : 1, p.tall);
     p.second = cut_of(count, p.z.s, p.z.sp / PK, p.parts ? 3 : 1, false);
-    // Tiles of 256, 128, 64, us: 4096 x 4096 133, 167, 213; 8192 x 2048 86, 99, 125; 2048 x 512 eight times, three products 60, 44, 52; 1111 x 520 57, 27, 17 and
-    // 777 x 333 three times 48, 22, 14: the largest tiles that half fill the chip, or three quarters of it.
-    p.apply_edge = apply(256) >= 130 ? 256 : apply(128) >= 200 ? 128 : 64;
+    // Tiles of 256 where they half fill the chip, else of 64. us with 256, 128 and 64, a product: 4096 x 4096 133, 167, 213; 8192 x 2048 86, 99, 125; 2048 x 512 eight
+    // times 41, 26, 28; 1024 x 4096 48, 25, 22. Three: 4096 x 4096 339, 467, 514; 3000 x 1500 twice 120, 139, 122; 2048 x 512 eight times 62, 52, 49; 2048 x 2048 143,
+    // 70, 75; 277 x 1329 eight times 48, 36, 20; 1111 x 520 57, 24, 11.
+    p.apply_edge = apply(256) >= 130 ? 256 : 64;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;
@@ -1025,7 +1026,6 @@ void apply_with(ApplyArgs a, const Target& t, int type, hipStream_t st) {
 template <bool TALL, int PAIRS>
 void apply(const ApplyArgs& a, int edge, const Target& t, int type, hipStream_t st) {
     if (edge == 256) apply_with<2, 4, 8, 4, TALL, PAIRS>(a, t, type, st);
-    else if (edge == 128) apply_with<2, 2, 4, 4, TALL, PAIRS>(a, t, type, st);
     else apply_with<2, 2, 2, 2, TALL, PAIRS>(a, t, type, st);
 }
 

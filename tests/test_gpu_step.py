@@ -704,3 +704,30 @@ def test_muon_step_one_block(rows, cols, name, grad):
     step, off = ref.orthogonalise(g + 0.9 * new, parts=name != "bf16")
     want = (1 - 0.05 * 0.2) * w - 0.05 * 0.7 * step
     assert np.linalg.norm(host(wt) - want) <= np.linalg.norm(half_unit(name, want)) + 0.05 * 0.7 * off + 4 * U * np.linalg.norm(w)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 5, 9, 16, 17])
+@pytest.mark.parametrize("classes,cols", [(1, 3), (77, 259), (4100, 1030)])
+def test_class_loss_gradients_of_few_rows(rows, classes, cols):
+    """In 32 bits a table is read as it lies: strided, any element, padded rows of anything, one gradient or both."""
+    t = torch()
+    u, w, target, live, rng = some(rows, classes, cols, "f32", seed=23, dead=0.3)
+    up = upstream(rng, rows, "both")
+    du, dw = check_backward(u, w, target, live, "f32", *up)
+    assert t.equal(check_backward(u, w, target, live, "f32", *up, need=(True, False))[0], du)
+    assert t.equal(check_backward(u, w, target, live, "f32", *up, need=(False, True))[1], dw)
+    wide = t.full((classes, cols + 3), float("nan"), device="cuda")
+    wide[:, 1:cols + 1] = dev(w)
+    lse = dev(ref.loss(u, w, target, live)[1].astype(np.float32))
+    su, st = spoiled(u, target, live)
+    again = iodf.class_loss_backward(dev(su), wide[:, 1:cols + 1], long(st), lse, dev(up[0]), dev(up[1]), live=on_gpu(live))
+    assert t.equal(again[0], du) and t.equal(again[1], dw)
+
+
+def test_class_loss_gradients_of_few_rows_and_no_class():
+    t = torch()
+    u, w, target, _, rng = some(5, 90, 33, "f32", seed=29)
+    lse = dev(ref.loss(u, w, target, None)[1].astype(np.float32))
+    target[2], target[4] = 90, -1
+    du, dw = iodf.class_loss_backward(dev(u), dev(w), long(target), lse, t.ones(5, device="cuda"))
+    assert du[[2, 4]].isnan().all() and du[[0, 1, 3]].isfinite().all() and dw.isnan().all()
