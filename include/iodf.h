@@ -373,8 +373,9 @@ int iodf_weight_grad_workspace(const iodf_wgrad* args, int64_t* bytes);
  *   g[t][v] = (dloss[t] + dlse[t]) exp(s[t][v] - lse[t]) - (v == target[t]) dloss[t].
  *   It goes over the classes in pieces whose g fits 512 MB (256 classes at least). In 16-bit types g is rounded to that type after it is multiplied so that
  *   the first of the gradients that are not 0 is a power of two (in half precision the largest); where few of them make up a gradient (16 rows, 32
- *   classes, 128 columns or 2^16 of them) it has two parts, so that gradients are as far off as their own rounding. In F32 numbers are multiplied in two
- *   parts of 11 bits each, exact to 2^-22 of the number, or to 2^-38 of the tensor's largest; of up to 16 rows as they are.
+ *   classes, 128 columns or 2^16 of them) it has two parts, so that gradients are as far off as their own rounding. In F32 numbers are multiplied
+ *   exactly but for what is 2^-25 of a product and less, however large or small others are. The forward pass multiplies F32 numbers of more than 64 rows in two
+ *   parts of 11 bits each, exact to 2^-22 of the number, or to 2^-38 of the tensor's largest.
  * `live` as above: a padded row's u, target, lse, dloss and dlse may be anything; its du is 0. A target outside 0..classes-1 in any other row makes that
  * row's loss, du and all of dw NaN. Sums are in an order that depends on the sizes alone. With no rows dw is 0.
  * 0 <= rows <= 2^24, 1 <= classes <= 2^20, 1 <= cols <= 65536, rows and classes times cols <= 2^34, rows times classes <= 2^38. Outputs overlap no

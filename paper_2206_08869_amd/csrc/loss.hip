@@ -1,6 +1,10 @@
 // Softmax cross entropy of rows against a table of classes, and its gradient: products of 16-bit numbers (products.h) whose logits never reach
 // memory as such.
 //
+// 32-bit operands: the gradients' sums go over rows and over classes, so that no power of two a row, class or tensor would do for all that a sum has in it, and numbers are
+// three parts of bfloat16, whose range is theirs: six products. 4096 rows, 32768 classes of 1024 columns 4.66 ms; two parts of half precision and three products, which a
+// number 10^8 times the others leaves 12 bits, took 2.23.
+//
 // Forward: a workgroup has the logits of a tile of classes and rows in registers and leaves, for each of its rows, their largest and
 // the sum of exponentials relative to it; a second kernel joins the tiles of a row. Backward: the logits once more, from which g = (dloss + dlse) exp(s -
 // lse) - dloss [target] goes to memory in 16 bits, piece by piece of the classes; du += g W and dw = g' u are two more products.
@@ -20,7 +24,8 @@ constexpr int kMaxima = 1024;                   // partial maxima of a tensor, a
 
 inline long long up(long long n, long long d) { return (n + d - 1) / d * d; }
 
-// What the kernels need of numbers' sizes, powers of two. Only where numbers have to be moved into the range of half precision.
+// What the kernels need of numbers' sizes, powers of two. Only where numbers have to be moved into the range of half precision: 32-bit logits of the forward
+// pass, g of half precision.
 struct Scales {
     float u, w, g;           // what u, W and g are multiplied with
     float iu, iw, ig;        // and the inverses
@@ -99,23 +104,35 @@ struct ReadyArgs {
     const uint8_t* live;   // of u's rows
     int cols, pitch;
     const float* maxima;   // NULL: no scales
-    int parts, wide;       // partial maxima of a tensor; u's and W's are there too
+    int parts;             // partial maxima of a tensor; with two parts u's and W's are there too
     Scales* scales;
 };
 
-// Rows of `pitch` 16-bit numbers with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in two parts of half precision. And the scales,
-// which workgroups take from the maxima by themselves. So
+// v in three parts of bfloat16, whose sum it is (but for parts below the smallest numbers there are): whatever its size, an infinity or NaN as the first of them.
+__device__ __forceinline__ void three_parts(float v, uint16_t (&part)[3]) {
+    constexpr uint32_t MOST = 0x7f7f0000;  // the largest, where rounding would make an infinity
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        float h = (float)(__bf16)v;
+        if (p == 0 && fabsf(h) > __uint_as_float(MOST) && fabsf(v) < __builtin_inff()) h = copysignf(__uint_as_float(MOST), v);
+        part[p] = (uint16_t)(__float_as_uint(h) >> 16);
+        v = fabsf(h) < __builtin_inff() ? v - h : 0.f;
+    }
+}
+
+// Rows of `pitch` 16-bit numbers with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in two parts of half precision (the forward pass) or three of bfloat16.
+// And the scales, which workgroups take from the maxima by themselves. So
 // there are at most 1024 of them for a tensor, with two chunks in flight a thread: the same rows 18 us (5.5 TB/s) where 4096 took 30, each with its 2 us for
 // the maxima.
-template <typename TX>
+template <typename TX, int PARTS>
 __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
     __shared__ float meet[4];
     const int which = blockIdx.y;
     const unsigned per = a.pitch / 8;
     float by = 1.f;
-    if (a.maxima && (a.wide || blockIdx.x + blockIdx.y == 0)) {
+    if (PARTS < 3 && a.maxima && (PARTS == 2 || blockIdx.x + blockIdx.y == 0)) {
         float m[3] = {};
-        for (int k = 0; k < (a.wide ? 3 : 1); ++k) {
+        for (int k = 0; k < (PARTS == 2 ? 3 : 1); ++k) {
             if (k != which + 1 && blockIdx.x + blockIdx.y) continue;  // only the first workgroup needs all of them
             for (int i = threadIdx.x; i < a.parts; i += 256) m[k] = fmaxf(m[k], a.maxima[k * a.parts + i]);
             m[k] = block_max(m[k], meet);
@@ -153,25 +170,31 @@ __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             if (i + k * step >= all) break;
-            if (sizeof(TX) == 2) {
+            if (PARTS == 1) {
                 *(u32x4*)(y + to[k]) = u32x4{raw[k].w[0], raw[k].w[1], raw[k].w[2], raw[k].w[3]};
                 continue;
             }
             float v[8];
             widen8(raw[k], v);
-            _Float16 hi[8], lo[8];
+            uint16_t part[3][8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float s = v[j] * by;
-                hi[j] = (_Float16)s;
-                const float rest = s - (float)hi[j];
-                lo[j] = fabsf(s) < 60000.f ? (_Float16)rest : (_Float16)0.f;  // an infinity or NaN has no rest
+                if (PARTS == 2) {
+                    const float s = v[j] * by;
+                    const _Float16 hi = (_Float16)s, lo = fabsf(s) < 60000.f ? (_Float16)(s - (float)hi) : (_Float16)0.f;  // an infinity or NaN has no rest
+                    part[0][j] = __builtin_bit_cast(uint16_t, hi), part[1][j] = __builtin_bit_cast(uint16_t, lo);
+                } else {
+                    uint16_t of[3];
+                    three_parts(v[j], of);
+                    part[0][j] = of[0], part[1][j] = of[1], part[2][j] = of[2];
+                }
             }
-            u32x4 w;
-            __builtin_memcpy(&w, hi, 16);
-            *(u32x4*)(y + to[k]) = w;
-            __builtin_memcpy(&w, lo, 16);
-            *(u32x4*)(y + plane + to[k]) = w;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                u32x4 w;
+                __builtin_memcpy(&w, part[p], 16);
+                *(u32x4*)(y + p * plane + to[k]) = w;
+            }
         }
     }
 }
@@ -471,7 +494,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     float lse[NT], up[NT], both[NT], asked = 0.f;
     int want[NT];  // the target, counted from the wave's first class; -1: elsewhere, -2: no such row, or padding
     if (PARTS && KIND != SLICE) {
-        asked = lift_ask(a);
+        if (PARTS < 3) asked = lift_ask(a);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const long long t = (long long)n0 + wn + n * 16 + P::col_of();
@@ -528,7 +551,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p.acc[m][n][j] = p.acc[m][n][j] * iu * iw;
     }
-    if (PARTS == 0) {
+    if constexpr (PARTS == 0) {
         float* const meet = (float*)lds;  // [MW][BN][2]
         const int left = a.classes - (m0 + wm);  // classes that exist from the wave's first on
         if (left < MT * 16) {
@@ -588,12 +611,11 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
             a.parts[tm * a.rows + t] = f32x2{top, sum};
         }
     } else {
-        typedef Staged<P, uint16_t, NW, (PARTS > 1 ? NT / 2 : NT)> Out;
-        static_assert((PARTS > 1 ? 2 : 1) * Out::BYTES <= P::LDS * 2, "g passes through the operands' LDS");
-        char* const low = (char*)lds + Out::BYTES;
+        typedef Staged<P, uint16_t, NW, (PARTS > 2 ? 1 : PARTS > 1 ? NT / 2 : NT)> Out;
+        static_assert(PARTS * Out::BYTES <= P::LDS * 2, "g passes through the operands' LDS");
         float inverse;
-        const float own = lift_of(asked, inverse), lift = a.scales ? a.scales->g : own;
-        if (!a.scales && blockIdx.x + threadIdx.x == 0) *a.inverse = inverse;
+        const float own = lift_of(asked, inverse), lift = PARTS > 2 ? 1.f : a.scales ? a.scales->g : own;
+        if (PARTS < 3 && !a.scales && blockIdx.x + threadIdx.x == 0) *a.inverse = inverse;
 #pragma unroll
         for (int pass = 0; pass < Out::PASSES; ++pass) {
             if (pass) lds_barrier();
@@ -603,7 +625,7 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                 const float gu = up[n] * lift, gb = both[n] * lift;
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    uint16_t hi[4], lo[4];
+                    uint16_t part[PARTS][4];
                     const int v0 = m * 16 + P::row_of();
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -611,12 +633,18 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                         const float e = PAIRS > 1 ? expf(s) : __builtin_amdgcn_exp2f(s * kLog2e);
                         float g = gb * e - (v0 + j == want[n] ? gu : 0.f);
                         g = want[n] != -2 && m0 + wm + v0 + j < a.classes ? g : 0.f;
-                        hi[j] = bits16<T>(g);
-                        const float whole = (float)__builtin_bit_cast(T, hi[j]);
-                        if (PARTS > 1) lo[j] = bits16<T>(fabsf(whole) < __builtin_inff() ? g - whole : 0.f);
+                        if constexpr (PARTS > 2) {
+                            uint16_t of[3];
+                            three_parts(g, of);
+                            part[0][j] = of[0], part[1][j] = of[1], part[2][j] = of[2];
+                        } else {
+                            part[0][j] = bits16<T>(g);
+                            const float whole = (float)__builtin_bit_cast(T, part[0][j]);
+                            if constexpr (PARTS > 1) part[1][j] = bits16<T>(fabsf(whole) < __builtin_inff() ? g - whole : 0.f);
+                        }
                     }
-                    staged.put(lds, m, n, hi);
-                    if (PARTS > 1) staged.put(low, m, n, lo);
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) staged.put((char*)lds + q * Out::BYTES, m, n, part[q]);
                 }
             }
             lds_barrier();
@@ -626,8 +654,8 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                 if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                 int row, col;
                 staged.where(i, pass, row, col);
-                *(u32x4*)(g + row * a.g_ld + col) = staged.take(lds, i);
-                if (PARTS > 1) *(u32x4*)(g + row * a.g_ld + col + a.g_plane) = staged.take(low, i);
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) *(u32x4*)(g + row * a.g_ld + col + q * a.g_plane) = staged.take((char*)lds + q * Out::BYTES, i);
             }
         }
     }
@@ -675,8 +703,7 @@ struct GradArgs {
     long long ld;
     float* partial;      // not NULL: sums [slice][tile] in the order in which lanes hold them, added to where `add`
     int add;
-    const float* down0;  // factors of an output, or NULL
-    const float* down1;
+    const float* down;   // factor of an output, or NULL
 };
 
 // A tile of du = g W (sums of W, rows of g) or dw = g' u (sums of both). The outputs' columns are the matrix instructions' rows.
@@ -707,7 +734,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, unsigned block, uin
             }
         return;
     }
-    const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
+    const float down = a.down ? *a.down : 1.f;
     const long long r0 = (long long)tn * P::BN;
     const int c0 = tm * P::BM;
 #pragma unroll
@@ -719,7 +746,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, unsigned block, uin
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const f32x4 s = p.acc[m][n];
-                const float v[4] = {s[0] * d0 * d1, s[1] * d0 * d1, s[2] * d0 * d1, s[3] * d0 * d1};
+                const float v[4] = {s[0] * down, s[1] * down, s[2] * down, s[3] * down};
                 staged.put(lds, m, n, v);
             }
         lds_barrier();
@@ -756,7 +783,7 @@ __global__ __launch_bounds__(256) void k_grad_join(const GradArgs du, const Grad
     const GradArgs& a = second ? dw : du;
     const int slices = second ? slices_dw : slices_du;
     constexpr int BM = MW * MT * 16, BN = NW * NT * 16, PER = BM * BN / 4;
-    const float d0 = a.down0 ? *a.down0 : 1.f, d1 = a.down1 ? *a.down1 : 1.f;
+    const float down = a.down ? *a.down : 1.f;
     const long long n = (long long)a.tm * a.tn * PER;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
         const int tile = (int)(i / PER), in = (int)(i % PER), lane = in & 63, block = in / 64 % (MT * NT), wave = in / (MT * NT * 64);
@@ -773,7 +800,7 @@ __global__ __launch_bounds__(256) void k_grad_join(const GradArgs du, const Grad
             s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
         for (; k < slices; ++k) s += from[k * n];
-        const float v[4] = {s[0] * d0 * d1, s[1] * d0 * d1, s[2] * d0 * d1, s[3] * d0 * d1};
+        const float v[4] = {s[0] * down, s[1] * down, s[2] * down, s[3] * down};
         put_quad((TO*)a.out + r * a.ld + c, a.cols - c, v);
     }
 }
@@ -796,12 +823,14 @@ struct Cut {
 
 // Microseconds that workgroups of a kind take, all of them, on 256 compute units, each `per` tiles (64 along the sum) of `products`: those that fit LDS at a
 // time go along together, then the next ones do. Times of a tile and (7, 5, 1.5) of the way to the first products and from the last ones are fitted to
-// calls of two to a hundred thousand rows and classes, which they say within a fifth.
+// calls of two to a hundred thousand rows and classes, which they say within a fifth. Of six products tiles of 128 go over the sum once for each, as of one, and
+// of tiles of 64 one fits LDS at a time.
 float time_of(int edge, float workgroups, int per, int products) {
-    const float most = edge == 256 ? 1.f : edge == 128 ? (products > 1 ? 1.f : 2.f) : products > 2 ? 2.f : products > 1 ? 3.f : 4.f;
+    const bool apart = products == 1 || products > 3;
+    const float most = edge == 256 ? 1.f : edge == 128 ? (apart ? 2.f : 1.f) : products > 3 ? 1.f : products > 2 ? 2.f : products > 1 ? 3.f : 4.f;
     const float each = workgroups / 256.f, at_once = std::min(most, std::max(1.f, each));
     const float rounds = edge > 64 ? std::ceil(each / most) : std::max(1.f, each / most);
-    const float step = edge == 256 ? 1.13f : edge == 128 ? (products > 1 ? 0.6f : at_once > 1.f ? 0.85f : 0.6f)
+    const float step = edge == 256 ? 1.13f : edge == 128 ? (apart && (products > 1 || at_once > 1.f) ? 0.85f : 0.6f)
                        : products > 1 ? std::max(0.25f, 0.23f * at_once) : std::max(0.5f, 0.23f * at_once);
     return rounds * ((edge == 256 ? 7.f : edge == 128 ? 5.f : 1.5f) + per * products * step);
 }
@@ -817,7 +846,7 @@ struct Task {
 // slices fill the chip when outputs are few, slices at the price of their sums' way through memory and of a second launch.
 float cut_of(const Task* tasks, int count, Cut* cuts, int products, int most) {
     float least = 0.f;
-    const int planes = products > 1 ? 2 : 1;
+    const int planes = products > 3 ? 3 : products > 1 ? 2 : 1;
     for (const int edge : {256, 128, 64}) {
         if (edge > most) continue;
         struct { long long tiles; float read, outputs; } t[2] = {};
@@ -891,19 +920,19 @@ bool in_place(const void* p, long long stride, int cols, bool wide) { return !wi
 LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     LossPlan p{};
     p.wide = a.type == IODF_T_F32;
-    p.planes = p.wide ? 2 : 1;
+    p.planes = !p.wide ? 1 : backward ? 3 : 2;
     p.pitch = (int)up(a.cols, PK);
     p.kts = p.pitch / PK;
     p.u_ready = !in_place(a.u, a.u_stride, a.cols, p.wide) || (backward && a.live);
     p.w_ready = !in_place(a.w, a.w_stride, a.cols, p.wide);
-    p.scaled = p.wide || (backward && a.type == IODF_T_F16);
+    p.scaled = backward ? a.type == IODF_T_F16 : p.wide;
     // Where a few numbers g make up a gradient, the rounding to 16 bits makes it up to twice as far off as its own last rounding does: of few rows (1 row, 79857
     // classes: 2.0 times), few classes (100000 rows, 14 classes: 1.4), few numbers altogether (14 rows, 7 classes: 1.6) or few columns, where products cost least
     // (23726 rows, 2091 classes of 11 columns: 1.5); 200 rows, 300 classes of 8000 columns 1.26 times, 21 rows, 40000 classes of 3000 1.17. A second part costs a
     // second product: 256 rows, 4000 classes of 512 columns 28 us for 22, 32000 classes of 4096 columns 607 for 339.
     p.fine = backward && !p.wide && (a.rows <= 16 || a.classes <= 32 || a.cols <= 128 || a.rows * a.classes <= 65536);
     p.rows_up = up(a.rows, 256);
-    p.logits = logits_cut(a.classes, a.rows, p.kts, p.wide ? 3 : 1, p.fine ? 128 : 256);
+    p.logits = logits_cut(a.classes, a.rows, p.kts, !p.wide ? 1 : backward ? 6 : 3, p.fine ? 128 : 256);
     p.tiles = (a.classes + p.logits.edge - 1) / p.logits.edge;
     // us by k_few and by a copy and tiles, 32000 classes of 1111 columns: in 32 bits 32 and 108 for a row, 47 and 110 for 32, 75 and 114 for 64; in bfloat16 29 and
     // 42 for a row, 37 and 43 for 16, 57 and 43 for 32.
@@ -929,7 +958,7 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.bytes = g + (a.du ? (size_t)p.few_slices * p.few_rows * across * 256 * 4 : 0);
         return p;
     }
-    p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, ((p.wide ? std::max<long long>(a.rows, a.classes) * p.pitch / 8 : a.rows) + 511) / 512));
+    p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, ((backward ? a.rows : std::max<long long>(a.rows, a.classes) * p.pitch / 8) + 511) / 512));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;
@@ -944,12 +973,12 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     if (!backward) {
         p.parts = take((size_t)p.tiles * a.rows * 8), p.picked = take((size_t)a.rows * 4);
     } else if (a.rows) {
-        const int g_planes = p.wide || p.fine ? 2 : 1;
+        const int g_planes = p.wide ? 3 : p.fine ? 2 : 1;
         p.piece = std::max<long long>(256, kPieceBytes / (p.rows_up * 2 * g_planes) / 256 * 256);
         p.piece = std::min(p.piece, up(a.classes, 256));
         p.g = take((size_t)g_planes * p.rows_up * p.piece * 2);
         const long long here = std::min<long long>(p.piece, a.classes);
-        const int products = p.wide ? 3 : p.fine ? 2 : 1;
+        const int products = p.wide ? 6 : p.fine ? 2 : 1;
         const Task tasks[2] = {{a.cols, a.rows, (int)((here + PK - 1) / PK), here < a.classes}, {a.cols, here, (int)((a.rows + PK - 1) / PK), false}};
         const int most = p.fine ? 128 : 256;
         Cut cuts[2];
@@ -1024,18 +1053,20 @@ LogitArgs prepared(const iodf_class_loss& a, const LossPlan& p, char* work, bool
     if (s) {
         const MaxArgs m{(const float*)a.u, (const float*)a.w, a.u_stride, a.w_stride, a.rows, a.classes, a.cols,
                         a.live, backward ? a.dloss : nullptr, backward ? a.dlse : nullptr};
-        k_maxima<<<dim3(p.maxima_parts, p.wide ? 3 : 1), 256, 0, st>>>(m, maxima);
+        k_maxima<<<dim3(p.maxima_parts, backward ? 1 : 3), 256, 0, st>>>(m, maxima);
     }
     l.u = {(const uint16_t*)a.u, 0, a.u_stride, (int)a.rows, (int)a.rows};
     l.w = {(const uint16_t*)a.w, 0, a.w_stride, a.classes, a.classes};
     ReadyArgs r{};
     r.x[0] = a.u, r.x[1] = a.w, r.stride[0] = a.u_stride, r.stride[1] = a.w_stride, r.rows[0] = a.rows, r.rows[1] = a.classes;
-    r.live = a.live, r.cols = a.cols, r.pitch = p.pitch, r.maxima = maxima, r.parts = p.maxima_parts, r.wide = p.wide, r.scales = s;
+    r.live = a.live, r.cols = a.cols, r.pitch = p.pitch, r.maxima = maxima, r.parts = p.maxima_parts, r.scales = s;
     if (p.u_ready) r.y[0] = (uint16_t*)(work + p.u), l.u.p = r.y[0], l.u.ld = p.pitch, l.u.plane = a.rows * p.pitch;
     if (p.w_ready) r.y[1] = (uint16_t*)(work + p.w), l.w.p = r.y[1], l.w.ld = p.pitch, l.w.plane = (long long)a.classes * p.pitch;
     if (s || p.u_ready || p.w_ready) {
         const long long most = std::max<long long>(p.u_ready ? a.rows : 0, p.w_ready ? a.classes : 0) * (p.pitch / 8);
-        k_ready<TX><<<dim3(std::min(blocks_for(most), 1024u), p.w_ready ? 2 : 1), 256, 0, st>>>(r);
+        const dim3 grid(std::min(blocks_for(most), 1024u), p.w_ready ? 2 : 1);
+        if constexpr (sizeof(TX) == 2) k_ready<TX, 1><<<grid, 256, 0, st>>>(r);
+        else backward ? k_ready<TX, 3><<<grid, 256, 0, st>>>(r) : k_ready<TX, 2><<<grid, 256, 0, st>>>(r);
     }
     l.kts = p.kts, l.classes = a.classes, l.all = a.classes, l.rows = a.rows, l.scales = s, l.target = a.target, l.live = a.live;
     l.sums = (f32x4*)(work + p.sums);
@@ -1100,7 +1131,7 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
         const int n = (int)std::min<long long>(p.piece, a.classes - v0);
         l.first = v0, l.classes = n;
         l.w = w, l.w.p += v0 * w.ld, l.w.extent = l.w.depth = n;
-        if constexpr (PAIRS > 1) logits<T, PAIRS, 2>(l, p.logits, st);
+        if constexpr (PAIRS > 1) logits<T, PAIRS, 3>(l, p.logits, st);
         else if (p.fine) logits<T, 1, 2>(l, p.logits, st);
         else logits<T, 1, 1>(l, p.logits, st);
         GradArgs du{}, dw{};
@@ -1109,17 +1140,17 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
         du.b = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
         du.kts = (n + PK - 1) / PK, du.rows = a.rows, du.cols = a.cols, du.out = a.du, du.ld = a.du_stride;
         du.partial = du_sums, du.add = v0 > 0;
-        du.down0 = s ? &s->ig : l.inverse, du.down1 = s ? &s->iw : nullptr;
+        du.down = p.wide ? nullptr : s ? &s->ig : l.inverse;
         dw.a = {l.u.p, l.u.plane, l.u.ld, a.cols, (int)a.rows};
         dw.b = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};
         dw.kts = (int)((a.rows + PK - 1) / PK), dw.rows = n, dw.cols = a.cols, dw.out = (TX*)a.dw + v0 * a.dw_stride, dw.ld = a.dw_stride;
         dw.partial = dw_sums;
-        dw.down0 = s ? &s->ig : l.inverse, dw.down1 = s ? &s->iu : nullptr;
+        dw.down = du.down;
         const int join_du = du_sums && last ? p.du.slices : 0, join_dw = dw_sums ? p.dw.slices : 0;
         auto go = [&](const Cut* cut_du, const Cut* cut_dw) {
             const int joined[2] = {cut_du ? join_du : 0, cut_dw ? join_dw : 0};
             // with g in two parts where the operand has one
-            if constexpr (PAIRS > 1) gradients<T, TX, 3>(du, dw, cut_du, cut_dw, joined, st);
+            if constexpr (PAIRS > 1) gradients<T, TX, PAIRS>(du, dw, cut_du, cut_dw, joined, st);
             else if (p.fine) gradients<T, TX, 2>(du, dw, cut_du, cut_dw, joined, st);
             else gradients<T, TX, 1>(du, dw, cut_du, cut_dw, joined, st);
         };
@@ -1144,7 +1175,7 @@ hipError_t launch_class_loss(const iodf_class_loss& a, void* work, hipStream_t s
 }
 
 hipError_t launch_class_loss_backward(const iodf_class_loss& a, void* work, hipStream_t st) {
-    return a.type == IODF_T_F32    ? backward<float, _Float16, 3>(a, (char*)work, st)
+    return a.type == IODF_T_F32    ? backward<float, __bf16, 6>(a, (char*)work, st)
            : a.type == IODF_T_BF16 ? backward<__bf16, __bf16, 1>(a, (char*)work, st)
                                    : backward<_Float16, _Float16, 1>(a, (char*)work, st);
 }

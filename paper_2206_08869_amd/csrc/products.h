@@ -6,7 +6,8 @@
 //   sums   [k][m], m consecutive: the transposing LDS read takes the fragment out of eight rows
 // so that no operand is ever transposed in memory. A number of more bits than 16 is two parts, high and low (planes of the same
 // layout), and the sum of three products: high low, low high, high high (the small ones first, while the sums
-// that they are rounded to are small too); or of two where only B has low parts.
+// that they are rounded to are small too); or of two where only B has low parts. A 32-bit number of any size is three parts in bfloat16, exactly, and six products: those
+// left out are 2^-25 of the whole and less.
 //
 // Tiles of 256 x 256 with eight waves are bound by power: logits of 8192 rows, 65536 classes and 4096 columns run at 1390 to 1440 TFLOP/s with random numbers
 // and at 1754 with zeros. The 16 x 16 x 32 instruction moves fewer sums for an operation than the 32 x 32 x 16 one, which made 1430 of 1305. Reads that meet
@@ -138,10 +139,13 @@ struct Frags {
 template <typename T, int MW, int NW, int MT_, int NT_, bool ASUMS, bool BSUMS, int PAIRS>
 struct Products {
     static constexpr int MT = MT_, NT = NT_, BM = MW * MT * 16, BN = NW * NT * 16, THREADS = MW * NW * 64;
-    // Small tiles have both parts of both operands in LDS at a time, which takes two loads for three products; large ones, which would not fit, go over
+    // Small tiles have all parts of both operands in LDS at a time, which takes two loads for three products; large ones, which would not fit, go over
     // the sum once for each product.
-    static constexpr bool BOTH = PAIRS > 1 && BM <= 128 && BN <= 128;
-    static constexpr int NA = BOTH && PAIRS > 2 ? 2 : 1, NB = BOTH ? 2 : 1;  // parts in LDS
+    static constexpr bool BOTH = PAIRS > 1 && BM <= (PAIRS > 3 ? 64 : 128) && BN <= (PAIRS > 3 ? 64 : 128);
+    static constexpr int NA = !BOTH || PAIRS == 2 ? 1 : PAIRS > 3 ? 3 : 2, NB = !BOTH ? 1 : PAIRS > 3 ? 3 : 2;  // parts in LDS
+    // of A and of B in a product: (0 2) (1 1) (2 0) (0 1) (1 0) (0 0), the last three or two of them
+    static __device__ __forceinline__ constexpr int part_a(int pair) { return PAIRS == 2 ? 0 : 0x010210 >> 4 * (pair + 6 - (PAIRS > 3 ? 6 : 3)) & 3; }
+    static __device__ __forceinline__ constexpr int part_b(int pair) { return PAIRS == 2 ? 1 - pair : 0x001012 >> 4 * (pair + 6 - (PAIRS > 3 ? 6 : 3)) & 3; }
     static constexpr int STAGE = (NA * BM + NB * BN) * PK;                   // elements of a tile of both operands
     static constexpr int LDS = 2 * STAGE;                                    // elements of LDS that run() wants
     f32x4 acc[MT][NT];
@@ -183,9 +187,9 @@ struct Products {
         unsigned left_a, left_b;
         auto next = [&] {
 #pragma unroll
-            for (int p = 0; p < NA; ++p) ca[p] = uniform(Lane<BM, THREADS, ASUMS>::corner(a, m0, BOTH ? p : PAIRS > 2 && pair == 1, kt));
+            for (int p = 0; p < NA; ++p) ca[p] = uniform(Lane<BM, THREADS, ASUMS>::corner(a, m0, BOTH ? p : PAIRS > 1 ? part_a(pair) : 0, kt));
 #pragma unroll
-            for (int p = 0; p < NB; ++p) cb[p] = uniform(Lane<BN, THREADS, BSUMS>::corner(b, n0, BOTH ? p : PAIRS > 1 && pair == 0, kt));
+            for (int p = 0; p < NB; ++p) cb[p] = uniform(Lane<BN, THREADS, BSUMS>::corner(b, n0, BOTH ? p : PAIRS > 1 ? part_b(pair) : 0, kt));
             left_a = a.depth - 1 - kt * PK, left_b = b.depth - 1 - kt * PK;
             if (++kt == kt1) kt = kt0, ++pair;
         };
@@ -216,8 +220,11 @@ struct Products {
             auto of_a = [&](int p) { return m < ROLL ? xa[p][m < ROLL ? m : 0] : xs[set][p][m < ROLL ? 0 : m - ROLL]; };
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                if (BOTH) low[BOTH ? m : 0][BOTH ? n : 0] = Mma<T>::go(of_a(0), xb[set][NB - 1][n], low[BOTH ? m : 0][BOTH ? n : 0]);
-                if (NA > 1) low[BOTH ? m : 0][BOTH ? n : 0] = Mma<T>::go(of_a(NA - 1), xb[set][0][n], low[BOTH ? m : 0][BOTH ? n : 0]);
+                if (BOTH) {
+#pragma unroll
+                    for (int pair = 0; pair < PAIRS - 1; ++pair)
+                        low[BOTH ? m : 0][BOTH ? n : 0] = Mma<T>::go(of_a(BOTH ? part_a(pair) : 0), xb[set][BOTH ? part_b(pair) : 0][n], low[BOTH ? m : 0][BOTH ? n : 0]);
+                }
                 acc[m][n] = Mma<T>::go(of_a(0), xb[set][0][n], acc[m][n]);
             }
         };

@@ -1,0 +1,50 @@
+"""The loss over a table of classes and its gradients where numbers are far apart: loud rows, classes and columns, upstream gradients at the ends of the
+range, padding in front, numbers that are no numbers beside padded rows."""
+import numpy as np
+import pytest
+
+import paper_2206_08869_amd as iodf
+import step_ref as ref
+from test_gpu_blocks import as_type, dev, half_unit, host, near, on_gpu, torch
+from test_gpu_step import NAMES, check_forward, long, some, upstream
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def gradients(u, w, target, live, name, dloss, dlse):
+    lse = ref.loss(u, w, target, live)[1].astype(np.float32)
+    got = iodf.class_loss_backward(dev(u, name), dev(w, name), long(target), dev(lse), *(None if d is None else dev(d) for d in (dloss, dlse)), live=on_gpu(live))
+    return got, lse.astype(np.float64)
+
+
+@pytest.mark.parametrize("rows,classes,cols", [(150, 270, 96), (600, 900, 264), (20, 3000, 130), (300, 40, 520)])
+def test_class_loss_gradients_of_loud_numbers(rows, classes, cols):
+    """32 bits: one number of a row, one of a class and a whole column are far louder than all others, each where the other tensor has nothing or next to nothing: what they
+    meet is exact, and what they do not meet is as near as its own numbers make it."""
+    u, w, target, _, rng = some(rows, classes, cols, "f32", seed=34)
+    w[:, 1], u[:, 2] = 0, 0
+    u[rows // 2, 1], w[classes // 2, 2] = 1e10, 1e12
+    u[:, 3], w[:, 3] = as_type(u[:, 3] * 1e9, "f32"), as_type(w[:, 3] * 1e-9, "f32")
+    up = upstream(rng, rows, "both")
+    up[0][rows // 3], up[1][rows // 3] = 1e6, 1e6
+    got, lse = gradients(u, w, target, None, "f32", *up)
+    du, dw, eu, ew = ref.gradients_by_the_parts(u, w, target, lse, *up, None, U)
+    near(got[0], du, "f32", eu, "du")
+    near(got[1], dw, "f32", ew, "dweight")
+
+
+def test_class_loss_gradients_without_a_diverged_row():
+    """32 bits: a live row whose upstream gradient is 0 may be as loud as it likes."""
+    u, w, target, _, rng = some(200, 300, 96, "f32", seed=35)
+    up = upstream(rng, 200, "both")
+    for row, by in ((3, 1e8), (77, 1e25)):
+        u[row] = as_type(u[row] * by, "f32")
+        up[0][row] = up[1][row] = 0
+    got, lse = gradients(u, w, target, None, "f32", *up)
+    rest = np.ones(200, bool)
+    rest[[3, 77]] = False
+    du, dw, eu, ew = ref.gradients_by_the_parts(u[rest], w, target[rest], lse[rest], up[0][rest], up[1][rest], None, U)
+    near(got[0][torch().from_numpy(rest).cuda()], du, "f32", eu, "du")
+    near(got[1], dw, "f32", ew, "dweight")
+    assert not got[0][[3, 77]].any()
