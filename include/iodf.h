@@ -375,7 +375,7 @@ int iodf_weight_grad_workspace(const iodf_wgrad* args, int64_t* bytes);
  *   the first of the gradients that are not 0 is a power of two (in half precision the largest); where few of them make up a gradient (16 rows, 32
  *   classes, 128 columns or 2^16 of them) it has two parts, so that gradients are as far off as their own rounding. In F32 numbers are multiplied
  *   exactly but for what is 2^-25 of a product and less, however large or small others are. The forward pass multiplies F32 numbers of more than 64 rows in two
- *   parts of 11 bits each, exact to 2^-22 of the number, or to 2^-38 of the tensor's largest.
+ *   parts of 11 bits each, exact to 2^-22 of the number, or to 2^-51 of its own row's or class's largest.
  * `live` as above: a padded row's u, target, lse, dloss and dlse may be anything; its du is 0. A target outside 0..classes-1 in any other row makes that
  * row's loss, du and all of dw NaN. Sums are in an order that depends on the sizes alone. With no rows dw is 0.
  * 0 <= rows <= 2^24, 1 <= classes <= 2^20, 1 <= cols <= 65536, rows and classes times cols <= 2^34, rows times classes <= 2^38. Outputs overlap no

@@ -2,7 +2,8 @@
 // memory as such.
 //
 // 32-bit operands: the gradients' sums go over rows and over classes, so that no power of two a row, class or tensor would do for all that a sum has in it, and numbers are
-// three parts of bfloat16, whose range is theirs: six products. 4096 rows, 32768 classes of 1024 columns 4.66 ms; two parts of half precision and three products, which a
+// three parts of bfloat16, whose range is theirs: six products. A logit's sum is over columns, and logits of the forward pass are of two parts of half precision with a power of two
+// for each row and each class, three products. 4096 rows, 32768 classes of 1024 columns 4.66 ms; two parts of half precision and three products, which a
 // number 10^8 times the others leaves 12 bits, took 2.23.
 //
 // Forward: a workgroup has the logits of a tile of classes and rows in registers and leaves, for each of its rows, their largest and
@@ -24,11 +25,9 @@ constexpr int kMaxima = 1024;                   // partial maxima of a tensor, a
 
 inline long long up(long long n, long long d) { return (n + d - 1) / d * d; }
 
-// What the kernels need of numbers' sizes, powers of two. Only where numbers have to be moved into the range of half precision: 32-bit logits of the forward
-// pass, g of half precision.
+// What g of half precision is multiplied with, and the inverse.
 struct Scales {
-    float u, w, g;           // what u, W and g are multiplied with
-    float iu, iw, ig;        // and the inverses
+    float g, ig;
 };
 
 // ---- getting operands ready ----
@@ -47,43 +46,17 @@ __device__ __forceinline__ float block_max(float m, float* meet) {  // 256 threa
     return m;
 }
 
-struct MaxArgs {
-    const float* u;   // of 32-bit operands; NULL: 16 bits, no need
-    const float* w;
-    long long u_stride, w_stride, rows, classes;
-    int cols;
-    const uint8_t* live;
-    const float* dloss;
-    const float* dlse;
-};
-
-// Of each workgroup's share; blockIdx.y: 0 what g is made of, 1 u, 2 W. Memory bounds it: 1023 and 10007 rows of 1111 numbers 9.6 us, 5.1 TB/s.
-__global__ __launch_bounds__(256) void k_maxima(const MaxArgs a, float* maxima) {
+// The largest number that g is made of, of each workgroup's share. 1000 rows 3 us, the launch.
+__global__ __launch_bounds__(256) void k_maxima(long long rows, const uint8_t* live, const float* dloss, const float* dlse, float* maxima) {
     __shared__ float meet[4];
-    const int what = blockIdx.y;
     float m = 0.f;
-    if (what == 0) {
-        for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < a.rows; t += (long long)gridDim.x * 256) {
-            if (a.live && !a.live[t]) continue;
-            const float d = a.dloss ? a.dloss[t] : 0.f;
-            m = finite_max(finite_max(m, d), a.dlse ? a.dlse[t] + d : d);
-        }
-    } else {
-        const float* const x = what == 1 ? a.u : a.w;
-        const uint8_t* const live = what == 1 ? a.live : nullptr;
-        const long long stride = what == 1 ? a.u_stride : a.w_stride, rows = what == 1 ? a.rows : a.classes;
-        const unsigned per = (a.cols + 7) / 8, n = (unsigned)(rows * per);  // fits, as rows times cols is 2^34 at most
-        for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
-            const unsigned t = i / per, c = (i - t * per) * 8;
-            if (live && !live[t]) continue;
-            float v[8];
-            load8(x + t * stride + c, a.cols - (int)c, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = finite_max(m, v[j]);
-        }
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < rows; t += (long long)gridDim.x * 256) {
+        if (live && !live[t]) continue;
+        const float d = dloss ? dloss[t] : 0.f;
+        m = finite_max(finite_max(m, d), dlse ? dlse[t] + d : d);
     }
     m = block_max(m, meet);
-    if (threadIdx.x == 0) maxima[what * gridDim.x + blockIdx.x] = m;
+    if (threadIdx.x == 0) maxima[blockIdx.x] = m;
 }
 
 // The power of two that takes numbers up to m to just below 2^15.
@@ -104,7 +77,7 @@ struct ReadyArgs {
     const uint8_t* live;   // of u's rows
     int cols, pitch;
     const float* maxima;   // NULL: no scales
-    int parts;             // partial maxima of a tensor; with two parts u's and W's are there too
+    int parts;             // partial maxima
     Scales* scales;
 };
 
@@ -120,34 +93,25 @@ __device__ __forceinline__ void three_parts(float v, uint16_t (&part)[3]) {
     }
 }
 
-// Rows of `pitch` 16-bit numbers with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in two parts of half precision (the forward pass) or three of bfloat16.
-// And the scales, which workgroups take from the maxima by themselves. So
-// there are at most 1024 of them for a tensor, with two chunks in flight a thread: the same rows 18 us (5.5 TB/s) where 4096 took 30, each with its 2 us for
-// the maxima.
+// Rows of `pitch` 16-bit numbers with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in three parts of bfloat16. And the scales of g. At most
+// 1024 workgroups for a tensor, with two chunks in flight a thread.
 template <typename TX, int PARTS>
 __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
     __shared__ float meet[4];
     const int which = blockIdx.y;
     const unsigned per = a.pitch / 8;
-    float by = 1.f;
-    if (PARTS < 3 && a.maxima && (PARTS == 2 || blockIdx.x + blockIdx.y == 0)) {
-        float m[3] = {};
-        for (int k = 0; k < (PARTS == 2 ? 3 : 1); ++k) {
-            if (k != which + 1 && blockIdx.x + blockIdx.y) continue;  // only the first workgroup needs all of them
-            for (int i = threadIdx.x; i < a.parts; i += 256) m[k] = fmaxf(m[k], a.maxima[k * a.parts + i]);
-            m[k] = block_max(m[k], meet);
-        }
+    if (a.maxima && blockIdx.x + blockIdx.y == 0) {
+        float m = 0.f;
+        for (int i = threadIdx.x; i < a.parts; i += 256) m = fmaxf(m, a.maxima[i]);
+        m = block_max(m, meet);
         Scales r;
-        r.g = lift(2.f * m[0], r.ig);
-        if (m[0] > 0.f) {  // and to make the largest a power of two, see lift_of
+        r.g = lift(2.f * m, r.ig);
+        if (m > 0.f) {  // and to make the largest a power of two, see lift_of
             int e;
-            const float rest = frexpf(m[0], &e);
+            const float rest = frexpf(m, &e);
             r.g /= rest, r.ig *= rest;
         }
-        r.u = lift(m[1], r.iu);
-        r.w = lift(m[2], r.iw);
-        if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *a.scales = r;
-        by = which ? r.w : r.u;
+        if (threadIdx.x == 0) *a.scales = r;
     }
     uint16_t* const y = a.y[which];
     if (!y) return;
@@ -179,15 +143,9 @@ __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
             uint16_t part[3][8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (PARTS == 2) {
-                    const float s = v[j] * by;
-                    const _Float16 hi = (_Float16)s, lo = fabsf(s) < 60000.f ? (_Float16)(s - (float)hi) : (_Float16)0.f;  // an infinity or NaN has no rest
-                    part[0][j] = __builtin_bit_cast(uint16_t, hi), part[1][j] = __builtin_bit_cast(uint16_t, lo);
-                } else {
-                    uint16_t of[3];
-                    three_parts(v[j], of);
-                    part[0][j] = of[0], part[1][j] = of[1], part[2][j] = of[2];
-                }
+                uint16_t of[3];
+                three_parts(v[j], of);
+                part[0][j] = of[0], part[1][j] = of[1], part[2][j] = of[2];
             }
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
@@ -197,6 +155,77 @@ __global__ __launch_bounds__(256) void k_ready(const ReadyArgs a) {
             }
         }
     }
+}
+
+constexpr int kShift = 12;  // low parts of the forward pass are held times 2^12
+
+struct RowsArgs {
+    const float* x[2];     // u and W
+    uint16_t* y[2];
+    int* e[2];             // [row] the power of two that its numbers are of
+    long long stride[2], rows[2];
+    unsigned first;        // workgroups of u, those of W behind them
+    const uint8_t* live;   // of u's rows
+    int cols, pitch;
+};
+
+// 32-bit rows in two parts of half precision, times the power of two that takes a row's largest number to just below 2^15. The low part of that may be 8, and is held
+// times 2^12: so numbers keep 22 bits down to 2^-29 of the row's largest, and what is left below is 2^-51 of it. SPAN threads to a row, which keep 32 of its numbers each and read
+// what is longer twice. 1023 and 10007 rows of 1111 numbers 24 us, 4.2 TB/s.
+template <int SPAN>
+__global__ __launch_bounds__(256) void k_rows(const RowsArgs a) {
+    __shared__ float meet[4];
+    constexpr int KEEP = 4;
+    const int which = blockIdx.x >= a.first, lane = threadIdx.x % SPAN;
+    const long long t = (long long)(blockIdx.x - (which ? a.first : 0)) * (256 / SPAN) + threadIdx.x / SPAN;
+    if (SPAN < 256 && t >= a.rows[which]) return;
+    const float* const x = a.x[which] + t * a.stride[which];
+    const int n = !which && a.live && !a.live[t] ? 0 : a.cols;
+    Raw8<float> keep[KEEP];
+    float m = 0.f;
+    auto look = [&](const Raw8<float>& raw) {
+        float v[8];
+        widen8(raw, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = finite_max(m, v[j]);
+    };
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) keep[k] = fetch8(x + (k * SPAN + lane) * 8, n - (k * SPAN + lane) * 8, false);
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) look(keep[k]);
+    for (int c = (KEEP * SPAN + lane) * 8; c < n; c += SPAN * 8) look(fetch8(x + c, n - c, false));
+    if (SPAN < 256) {
+#pragma unroll
+        for (int k = 1; k < SPAN; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
+    } else {
+        m = block_max(m, meet);
+    }
+    int e = 15;
+    if (m > 0.f) frexpf(m, &e);
+    e -= 15;
+    if (lane == 0) a.e[which][t] = e;
+    const long long plane = a.rows[which] * a.pitch;
+    uint16_t* const y = a.y[which] + t * a.pitch;
+    auto put = [&](const Raw8<float>& raw, int c) {
+        float v[8];
+        widen8(raw, v);
+        _Float16 hi[8], lo[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float s = ldexpf(v[j], -e);
+            hi[j] = (_Float16)s;
+            lo[j] = fabsf(s) < 60000.f ? (_Float16)((s - (float)hi[j]) * (1 << kShift)) : (_Float16)0.f;  // an infinity or NaN has no rest
+        }
+        u32x4 w;
+        __builtin_memcpy(&w, hi, 16);
+        *(u32x4*)(y + c) = w;
+        __builtin_memcpy(&w, lo, 16);
+        *(u32x4*)(y + plane + c) = w;
+    };
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+        if ((k * SPAN + lane) * 8 < a.pitch) put(keep[k], (k * SPAN + lane) * 8);
+    for (int c = (KEEP * SPAN + lane) * 8; c < a.pitch; c += SPAN * 8) put(fetch8(x + c, n - c, false), c);
 }
 
 // ---- logits ----
@@ -211,6 +240,8 @@ struct LogitArgs {
     long long first;     // the piece's first class
     long long all;       // classes of the table
     long long rows;
+    const int* u_exp;    // [rows], [classes] powers of two that 32-bit operands are of, or NULL
+    const int* w_exp;
     const Scales* scales;
     const int64_t* target;
     const uint8_t* live;
@@ -484,7 +515,7 @@ enum { WHOLE, SLICE, JOIN };
 
 template <typename T, int MW, int NW, int MT, int NT, int PAIRS, int PARTS, int KIND>
 __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
-    typedef Products<T, MW, NW, MT, NT, false, false, PAIRS> P;
+    typedef Products<T, MW, NW, MT, NT, false, false, PAIRS, PAIRS == 3 ? kShift : 0> P;
     __shared__ __align__(16) uint16_t lds[P::LDS];
     int tm, tn;
     place_tile(blockIdx.x, gridDim.x, a.tm, a.tn, tm, tn);
@@ -542,14 +573,19 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
         }
     }
 
-    if (a.scales) {
-        const float iu = a.scales->iu, iw = a.scales->iw;
+    if (PAIRS == 3) {  // the workspace goes on to the tiles' ends
+        int eu[NT];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 0; n < NT; ++n) eu[n] = a.u_exp[n0 + wn + n * 16 + P::col_of()];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            int ew[4];
+            __builtin_memcpy(ew, a.w_exp + m0 + wm + m * 16 + P::row_of(), 16);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) p.acc[m][n][j] = p.acc[m][n][j] * iu * iw;
+                for (int j = 0; j < 4; ++j) p.acc[m][n][j] = ldexpf(p.acc[m][n][j], eu[n] + ew[j]);
+        }
     }
     if constexpr (PARTS == 0) {
         float* const meet = (float*)lds;  // [MW][BN][2]
@@ -899,7 +935,7 @@ Cut logits_cut(long long classes, long long rows, int kts, int products, int mos
 }
 
 struct LossPlan {
-    bool wide, u_ready, w_ready, scaled;  // 32-bit operands; whether u and W are copied; whether there are scales
+    bool wide, u_ready, w_ready, scaled;  // 32-bit operands; whether u and W are copied; whether there are scales of g
     bool fine;                            // g in two parts though the operands have one
     int pitch, kts;
     int few, groups;                      // blocks of 16 rows of k_few (0: tiles), groups of classes to its workgroups
@@ -912,7 +948,7 @@ struct LossPlan {
     Cut du, dw;
     bool together;                        // du's and dw's products in one launch
     // byte offsets into the workspace
-    size_t maxima, scales, u, w, sums, parts, picked, g, du_sums, dw_sums, bytes;
+    size_t maxima, scales, u_exp, w_exp, u, w, sums, parts, picked, g, du_sums, dw_sums, bytes;
 };
 
 bool in_place(const void* p, long long stride, int cols, bool wide) { return !wide && cols % PK == 0 && stride % 8 == 0 && stride <= (1 << 22) && ((uintptr_t)p & 15) == 0; }
@@ -925,7 +961,7 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     p.kts = p.pitch / PK;
     p.u_ready = !in_place(a.u, a.u_stride, a.cols, p.wide) || (backward && a.live);
     p.w_ready = !in_place(a.w, a.w_stride, a.cols, p.wide);
-    p.scaled = backward ? a.type == IODF_T_F16 : p.wide;
+    p.scaled = backward && a.type == IODF_T_F16;
     // Where a few numbers g make up a gradient, the rounding to 16 bits makes it up to twice as far off as its own last rounding does: of few rows (1 row, 79857
     // classes: 2.0 times), few classes (100000 rows, 14 classes: 1.4), few numbers altogether (14 rows, 7 classes: 1.6) or few columns, where products cost least
     // (23726 rows, 2091 classes of 11 columns: 1.5); 200 rows, 300 classes of 8000 columns 1.26 times, 21 rows, 40000 classes of 3000 1.17. A second part costs a
@@ -941,7 +977,7 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.few = blocks <= 1 ? 1 : blocks <= 2 ? 2 : 4;
         p.groups = (groups + 2047) / 2048;
         p.tiles = (groups + p.groups - 1) / p.groups;
-        p.u_ready = p.w_ready = p.scaled = false;
+        p.u_ready = p.w_ready = false;
     }
     // us by k_few and k_few_grad and by tiles, in 32 bits: 24000 classes of 6592 columns 427 and 863 for a row, 538 and 910 for 16; 32000 of 1111 112 and 220, 135 and 221;
     // 50 of 100 20 and 25. In bfloat16, where tiles read W as it lies, 363 and 405, 115 and 113, 20 and 21 for a row: not by these.
@@ -958,15 +994,16 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.bytes = g + (a.du ? (size_t)p.few_slices * p.few_rows * across * 256 * 4 : 0);
         return p;
     }
-    p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, ((backward ? a.rows : std::max<long long>(a.rows, a.classes) * p.pitch / 8) + 511) / 512));
+    p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, (a.rows + 511) / 512));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;
         at += up(bytes, 256);
         return was;
     };
-    if (p.scaled) p.maxima = take((size_t)3 * p.maxima_parts * 4);
-    if (p.scaled || backward) p.scales = take(sizeof(Scales));
+    if (p.scaled) p.maxima = take((size_t)p.maxima_parts * 4);
+    if (backward) p.scales = take(sizeof(Scales));
+    if (p.wide && !backward && !p.few) p.u_exp = take((size_t)p.rows_up * 4), p.w_exp = take((size_t)up(a.classes, 256) * 4);
     if (p.u_ready) p.u = take((size_t)p.planes * a.rows * p.pitch * 2);
     if (p.w_ready) p.w = take((size_t)p.planes * a.classes * p.pitch * 2);
     if (!p.few && p.logits.slices > 1) p.sums = take((size_t)p.logits.slices * p.tiles * up(a.rows, p.logits.edge) * p.logits.edge * 4);
@@ -1050,11 +1087,7 @@ LogitArgs prepared(const iodf_class_loss& a, const LossPlan& p, char* work, bool
     LogitArgs l{};
     Scales* const s = p.scaled ? (Scales*)(work + p.scales) : nullptr;
     float* const maxima = s ? (float*)(work + p.maxima) : nullptr;
-    if (s) {
-        const MaxArgs m{(const float*)a.u, (const float*)a.w, a.u_stride, a.w_stride, a.rows, a.classes, a.cols,
-                        a.live, backward ? a.dloss : nullptr, backward ? a.dlse : nullptr};
-        k_maxima<<<dim3(p.maxima_parts, backward ? 1 : 3), 256, 0, st>>>(m, maxima);
-    }
+    if (s) k_maxima<<<p.maxima_parts, 256, 0, st>>>(a.rows, a.live, a.dloss, a.dlse, maxima);
     l.u = {(const uint16_t*)a.u, 0, a.u_stride, (int)a.rows, (int)a.rows};
     l.w = {(const uint16_t*)a.w, 0, a.w_stride, a.classes, a.classes};
     ReadyArgs r{};
@@ -1062,11 +1095,21 @@ LogitArgs prepared(const iodf_class_loss& a, const LossPlan& p, char* work, bool
     r.live = a.live, r.cols = a.cols, r.pitch = p.pitch, r.maxima = maxima, r.parts = p.maxima_parts, r.scales = s;
     if (p.u_ready) r.y[0] = (uint16_t*)(work + p.u), l.u.p = r.y[0], l.u.ld = p.pitch, l.u.plane = a.rows * p.pitch;
     if (p.w_ready) r.y[1] = (uint16_t*)(work + p.w), l.w.p = r.y[1], l.w.ld = p.pitch, l.w.plane = (long long)a.classes * p.pitch;
-    if (s || p.u_ready || p.w_ready) {
-        const long long most = std::max<long long>(p.u_ready ? a.rows : 0, p.w_ready ? a.classes : 0) * (p.pitch / 8);
-        const dim3 grid(std::min(blocks_for(most), 1024u), p.w_ready ? 2 : 1);
-        if constexpr (sizeof(TX) == 2) k_ready<TX, 1><<<grid, 256, 0, st>>>(r);
-        else backward ? k_ready<TX, 3><<<grid, 256, 0, st>>>(r) : k_ready<TX, 2><<<grid, 256, 0, st>>>(r);
+    const long long most = std::max<long long>(p.u_ready ? a.rows : 0, p.w_ready ? a.classes : 0) * (p.pitch / 8);
+    const dim3 grid(std::min(blocks_for(most), 1024u), p.w_ready ? 2 : 1);
+    if constexpr (sizeof(TX) == 2) {
+        if (s || p.u_ready || p.w_ready) k_ready<TX, 1><<<grid, 256, 0, st>>>(r);
+    } else if (backward) {
+        k_ready<TX, 3><<<grid, 256, 0, st>>>(r);
+    } else if (!p.few) {
+        RowsArgs h{};
+        int* const e[2] = {(int*)(work + p.u_exp), (int*)(work + p.w_exp)};
+        for (int i = 0; i < 2; ++i) h.x[i] = (const float*)r.x[i], h.y[i] = r.y[i], h.e[i] = e[i], h.stride[i] = r.stride[i], h.rows[i] = r.rows[i];
+        h.live = a.live, h.cols = a.cols, h.pitch = p.pitch, l.u_exp = e[0], l.w_exp = e[1];
+        const int at_once = p.pitch <= 256 ? 32 : p.pitch <= 2048 ? 4 : 1;  // rows to a workgroup
+        h.first = (unsigned)((a.rows + at_once - 1) / at_once);
+        const unsigned blocks = h.first + (unsigned)((a.classes + at_once - 1) / at_once);
+        at_once == 32 ? k_rows<8><<<blocks, 256, 0, st>>>(h) : at_once == 4 ? k_rows<64><<<blocks, 256, 0, st>>>(h) : k_rows<256><<<blocks, 256, 0, st>>>(h);
     }
     l.kts = p.kts, l.classes = a.classes, l.all = a.classes, l.rows = a.rows, l.scales = s, l.target = a.target, l.live = a.live;
     l.sums = (f32x4*)(work + p.sums);

@@ -135,8 +135,8 @@ struct Frags {
     }
 };
 
-// MW x NW waves of MT x NT blocks of 16 x 16 outputs.
-template <typename T, int MW, int NW, int MT_, int NT_, bool ASUMS, bool BSUMS, int PAIRS>
+// MW x NW waves of MT x NT blocks of 16 x 16 outputs. Low parts are held times 2^SHIFT.
+template <typename T, int MW, int NW, int MT_, int NT_, bool ASUMS, bool BSUMS, int PAIRS, int SHIFT = 0>
 struct Products {
     static constexpr int MT = MT_, NT = NT_, BM = MW * MT * 16, BN = NW * NT * 16, THREADS = MW * NW * 64;
     // Small tiles have all parts of both operands in LDS at a time, which takes two loads for three products; large ones, which would not fit, go over
@@ -256,7 +256,14 @@ struct Products {
 #pragma unroll
         for (int g = 0; g <= MT; ++g) reads(0, 0, 0, g);
         int buf = 0;
+        constexpr float DOWN = 1.f / (1 << SHIFT);
         for (int t = 0; t < tiles; ++t) {
+            if (SHIFT && !BOTH && t == (PAIRS - 1) * (kt1 - kt0)) {  // the small products are done
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[m][n] *= DOWN;
+            }
 #pragma unroll
             for (int g = 0; g < MT; ++g) {
                 reads(1, buf, 1, g);
@@ -280,7 +287,7 @@ struct Products {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[m][n] += low[BOTH ? m : 0][BOTH ? n : 0];
+                for (int n = 0; n < NT; ++n) acc[m][n] += SHIFT ? low[BOTH ? m : 0][BOTH ? n : 0] * DOWN : low[BOTH ? m : 0][BOTH ? n : 0];
         }
         lds_barrier();
     }

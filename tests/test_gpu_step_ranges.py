@@ -12,6 +12,39 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 
 
+def test_class_loss_rows_do_not_see_how_loud_others_are():
+    """32 bits: a row's logits are as near as its own numbers make them."""
+    u, w, target, _, _ = some(200, 300, 96, "f32", seed=31)
+    for row, by in ((7, 1e8), (90, -1e8), (40, 1e-25)):
+        u[row] = as_type(u[row] * by, "f32")
+    check_forward(u, w, target, None, "f32")
+
+
+def test_class_loss_classes_do_not_see_how_loud_others_are():
+    """Some classes are loud in columns where half the rows have nothing, another is so everywhere and has no probability."""
+    u, w, target, _, _ = some(200, 300, 96, "f32", seed=32)
+    w[:, 5] = 0
+    w[11, 5], w[250, 5] = 1e8, 3e7
+    u[::2, 5] = 0
+    u[1::2, 5] = -1
+    target[np.isin(target, (11, 250))] = 3
+    check_forward(u, w, target, None, "f32")
+    u[:, 7], w[100], target[target == 100] = -1, 0, 101
+    w[100, 7] = 1e30
+    r = iodf.class_loss(dev(u), dev(w), long(target))
+    rest = np.arange(300) != 100
+    loss, lse, s = ref.loss(u, w[rest], target - (target > 100))
+    slack = ref.logit_slack(u, w[rest]) + 64 * U * (1 + np.abs(lse) + np.abs(s).max(1))
+    near(r.lse, lse, "f32", slack, "lse")
+    near(r.loss, loss, "f32", 2 * slack, "loss")
+
+
+def test_class_loss_loud_columns_of_small_weights():
+    u, w, target, _, _ = some(150, 200, 96, "f32", seed=33)
+    u[:, 3], w[:, 3] = as_type(u[:, 3] * 1e8, "f32"), as_type(w[:, 3] * 1e-8, "f32")
+    check_forward(u, w, target, None, "f32")
+
+
 def gradients(u, w, target, live, name, dloss, dlse):
     lse = ref.loss(u, w, target, live)[1].astype(np.float32)
     got = iodf.class_loss_backward(dev(u, name), dev(w, name), long(target), dev(lse), *(None if d is None else dev(d) for d in (dloss, dlse)), live=on_gpu(live))
