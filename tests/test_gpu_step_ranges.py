@@ -39,6 +39,16 @@ def test_class_loss_classes_do_not_see_how_loud_others_are():
     near(r.loss, loss, "f32", 2 * slack, "loss")
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [300, 2000])
+def test_class_loss_of_huge_logits(name, classes):
+    """Logits whose 24 bits end above 1."""
+    u, w, target, _, _ = some(200, classes, 96, name, seed=40)
+    for row, by in ((7, 1e12), (90, 1e20), (199, 1e30)):
+        u[row] = as_type(u[row] * by, name)
+    check_forward(u, w, target, None, name)
+
+
 def test_class_loss_loud_columns_of_small_weights():
     u, w, target, _, _ = some(150, 200, 96, "f32", seed=33)
     u[:, 3], w[:, 3] = as_type(u[:, 3] * 1e8, "f32"), as_type(w[:, 3] * 1e-8, "f32")
