@@ -375,7 +375,7 @@ __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int c = b * 16 + lane / 16 * 4 + j;
-                        if (c0 + c < a.classes) a.g[(c0 + c) * 16ll + r] = there ? both * expf(s[j] - lse) - (want == c ? up : 0.f) : 0.f;
+                        if (c0 + c < a.classes) a.g[(c0 + c) * 16ll + r] = there ? both * expf(s[j] - lse > 0.f ? 0.f : s[j] - lse) - (want == c ? up : 0.f) : 0.f;
                     }
                 }
                 continue;
@@ -665,7 +665,8 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                     const int v0 = m * 16 + P::row_of();
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float s = p.acc[m][n][j] - lse[n];
+                        float s = p.acc[m][n][j] - lse[n];
+                        s = s > 0.f ? 0.f : s;  // no probability is past 1; of huge logits the two passes' roundings are, and 0 times their exponential is not 0
                         const float e = PAIRS > 1 ? expf(s) : __builtin_amdgcn_exp2f(s * kLog2e);
                         float g = gb * e - (v0 + j == want[n] ? gu : 0.f);
                         g = want[n] != -2 && m0 + wm + v0 + j < a.classes ? g : 0.f;

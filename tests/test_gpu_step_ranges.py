@@ -91,3 +91,21 @@ def test_class_loss_gradients_without_a_diverged_row():
     near(got[0][torch().from_numpy(rest).cuda()], du, "f32", eu, "du")
     near(got[1], dw, "f32", ew, "dweight")
     assert not got[0][[3, 77]].any()
+
+
+@pytest.mark.parametrize("rows", [12, 300])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_rows_without_upstream_gradient_stay_out_whatever_their_logits(name, rows):
+    """Logits so large that the two passes' roundings of them lie a thousand apart: a probability is at most 1 for all that, and nothing times it is nothing."""
+    u, w, target, _, rng = some(rows, 400, 200, name, seed=39)
+    up = upstream(rng, rows, "both")
+    rest = np.ones(rows, bool)
+    for row, by in ((0, 1e10), (rows // 4, 1e15), (rows - 1, 1e25)):
+        u[row] = as_type(u[row] * by, name)
+        up[0][row] = up[1][row] = 0
+        rest[row] = False
+    got, lse = gradients(u, w, target, None, name, *up)
+    du, dw, eu, ew = ref.loss_backward(u[rest], w, target[rest], lse[rest], up[0][rest], up[1][rest], None, name)
+    near(got[0][torch().from_numpy(rest).cuda()], du, name, eu, "du")
+    near(got[1], dw, name, ew, "dweight")
+    assert not got[0][torch().from_numpy(~rest).cuda()].any()
