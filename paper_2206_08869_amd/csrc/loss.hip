@@ -489,20 +489,29 @@ __global__ __launch_bounds__(256) void k_few_join(const FewGradArgs a, const int
 }
 
 // g is rounded to 16 bits, and in most programs dloss is the same number in every row: what the rounding does to it would be the same everywhere, and not
-// average out. So g is multiplied with the number from 1 to 2 that makes the first row's dloss (or, where that is 0, what its probabilities are multiplied
-// with) a power of two. The same in all waves; the row's number is asked for first and used behind the products.
-__device__ __forceinline__ float lift_ask(const LogitArgs& a) {
-    const int t = threadIdx.x & 63;
-    if (a.scales || t >= a.rows || (a.live && !a.live[t])) return 0.f;
-    const float v = a.dloss ? fabsf(a.dloss[t]) : 0.f;
-    return v == 0.f && a.dlse ? fabsf(a.dlse[t]) : v;
+// average out. So g is multiplied with the number from 1 to 2 that makes a row's dloss (or, where that is 0, what its probabilities are multiplied
+// with) a power of two: the first that is not 0 of 256 rows spread evenly over all, since those at the beginning may be padding. The same in all waves; the rows' numbers are
+// asked for first and used behind the products.
+constexpr int kAsked = 4;
+__device__ __forceinline__ void lift_ask(const LogitArgs& a, float (&asked)[kAsked]) {
+#pragma unroll
+    for (int k = 0; k < kAsked; ++k) {
+        const long long i = k * 64 + (threadIdx.x & 63), t = a.rows > 64 * kAsked ? i * a.rows / (64 * kAsked) : i;
+        asked[k] = 0.f;
+        if (a.scales || t >= a.rows || (a.live && !a.live[t])) continue;
+        const float v = a.dloss ? fabsf(a.dloss[t]) : 0.f;
+        asked[k] = v == 0.f && a.dlse ? fabsf(a.dlse[t]) : v;
+    }
 }
-__device__ __forceinline__ float lift_of(float asked, float& inverse) {
-    const unsigned long long some = __builtin_amdgcn_ballot_w64(asked > 0.f && asked < __builtin_inff());
+__device__ __forceinline__ float lift_of(const float (&asked)[kAsked], float& inverse) {
     inverse = 1.f;
-    if (some) {
-        int e;
-        inverse = frexpf(__shfl(asked, __builtin_ctzll(some)), &e);
+#pragma unroll
+    for (int k = kAsked - 1; k >= 0; --k) {
+        const unsigned long long some = __builtin_amdgcn_ballot_w64(asked[k] > 0.f && asked[k] < __builtin_inff());
+        if (some) {
+            int e;
+            inverse = frexpf(__shfl(asked[k], __builtin_ctzll(some)), &e);
+        }
     }
     return 1.f / inverse;
 }
@@ -522,10 +531,10 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     const int m0 = tm * P::BM, n0 = tn * P::BN;
     const int wm = P::wave_m(), wn = P::wave_n();
     // what the rows' gradients need, asked for in front of the products
-    float lse[NT], up[NT], both[NT], asked = 0.f;
+    float lse[NT], up[NT], both[NT], asked[kAsked];
     int want[NT];  // the target, counted from the wave's first class; -1: elsewhere, -2: no such row, or padding
     if (PARTS && KIND != SLICE) {
-        if (PARTS < 3) asked = lift_ask(a);
+        if (PARTS < 3) lift_ask(a, asked);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const long long t = (long long)n0 + wn + n * 16 + P::col_of();
@@ -649,9 +658,13 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
     } else {
         typedef Staged<P, uint16_t, NW, (PARTS > 2 ? 1 : PARTS > 1 ? NT / 2 : NT)> Out;
         static_assert(PARTS * Out::BYTES <= P::LDS * 2, "g passes through the operands' LDS");
-        float inverse;
-        const float own = lift_of(asked, inverse), lift = PARTS > 2 ? 1.f : a.scales ? a.scales->g : own;
-        if (PARTS < 3 && !a.scales && blockIdx.x + threadIdx.x == 0) *a.inverse = inverse;
+        float lift = 1.f;
+        if (PARTS < 3) {
+            float inverse;
+            lift = lift_of(asked, inverse);
+            if (a.scales) lift = a.scales->g;
+            else if (blockIdx.x + threadIdx.x == 0) *a.inverse = inverse;
+        }
 #pragma unroll
         for (int pass = 0; pass < Out::PASSES; ++pass) {
             if (pass) lds_barrier();

@@ -93,6 +93,29 @@ def test_class_loss_gradients_without_a_diverged_row():
     assert not got[0][[3, 77]].any()
 
 
+@pytest.mark.parametrize("quiet", ["padded", "masked"])
+@pytest.mark.parametrize("rows", [400, 2000])
+def test_class_loss_gradient_s_rounding_is_not_the_same_in_all_rows(quiet, rows):
+    """bfloat16, the same dloss in every row but the first hundred, half way between two neighbours: multiplied so that it is a power of two, gradients that are dloss
+    itself are exact, and a result is off by its own rounding alone. The rows' targets have next to no probability and another class has next to all."""
+    rng = np.random.default_rng(36)
+    classes, cols, d = 400, 200, (1 + 2.0 ** -8) * 2.0 ** -9
+    w = as_type(rng.standard_normal((classes, cols)), "bf16")
+    sure, target = rng.integers(0, classes, rows), rng.integers(0, classes, rows)
+    target = np.where(sure == target, (target + 1) % classes, target)
+    u = as_type(w[sure], "bf16")  # a logit of 200, others far below
+    dloss = np.full(rows, d)
+    live = None
+    if quiet == "padded":
+        live = np.arange(rows) >= 100
+    else:
+        dloss[:100] = 0
+    got, lse = gradients(u, w, target, live, "bf16", dloss, None)
+    du, dw, _, _ = ref.loss_backward(u, w, target, lse, dloss, None, live, "f32")
+    for a, b in zip(got, (du, dw)):
+        assert np.linalg.norm(host(a) - b) <= 1.01 * np.linalg.norm(half_unit("bf16", b))
+
+
 @pytest.mark.parametrize("rows", [12, 300])
 @pytest.mark.parametrize("name", ["f32", "bf16"])
 def test_rows_without_upstream_gradient_stay_out_whatever_their_logits(name, rows):
