@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256) void k_few_join(const FewGradArgs a, const int
 }
 
 // g is rounded to 16 bits, and in most programs dloss is the same number in every row: what the rounding does to it would be the same everywhere, and not
-// average out. So g is multiplied with the number from 1 to 2 that makes a row's dloss (or, where that is 0, what its probabilities are multiplied
+// average out. So g is multiplied with the number from 1/2 to 1 that makes a row's dloss (or, where that is 0, what its probabilities are multiplied
 // with) a power of two: the first that is not 0 of 256 rows spread evenly over all, since those at the beginning may be padding. The same in all waves; the rows' numbers are
 // asked for first and used behind the products.
 constexpr int kAsked = 4;
@@ -510,7 +510,7 @@ __device__ __forceinline__ float lift_of(const float (&asked)[kAsked], float& in
         const unsigned long long some = __builtin_amdgcn_ballot_w64(asked[k] > 0.f && asked[k] < __builtin_inff());
         if (some) {
             int e;
-            inverse = frexpf(__shfl(asked[k], __builtin_ctzll(some)), &e);
+            inverse = 2.f * frexpf(__shfl(asked[k], __builtin_ctzll(some)), &e);
         }
     }
     return 1.f / inverse;

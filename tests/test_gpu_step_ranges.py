@@ -116,6 +116,19 @@ def test_class_loss_gradient_s_rounding_is_not_the_same_in_all_rows(quiet, rows)
         assert np.linalg.norm(host(a) - b) <= 1.01 * np.linalg.norm(half_unit("bf16", b))
 
 
+def test_class_loss_gradients_at_the_end_of_the_range():
+    """bfloat16: dloss near the largest number of 32 bits."""
+    u, w, target, _, _ = some(400, 300, 200, "bf16", seed=37)
+    dloss = np.full(400, np.float64(np.float32(1e30)))
+    dloss[5] = dloss[0] = np.float64(np.float32(2.5e38))
+    w = as_type(w * 2.0 ** -10, "bf16")
+    u = as_type(u * 2.0 ** -10, "bf16")
+    (a, b), lse = gradients(u, w, target, None, "bf16", dloss, None)
+    du, dw, eu, ew = ref.loss_backward(u, w, target, lse, dloss, None, None, "bf16")
+    near(a, du, "bf16", eu, "du")
+    near(b, dw, "bf16", ew, "dweight")
+
+
 @pytest.mark.parametrize("rows", [12, 300])
 @pytest.mark.parametrize("name", ["f32", "bf16"])
 def test_rows_without_upstream_gradient_stay_out_whatever_their_logits(name, rows):
