@@ -754,6 +754,7 @@ struct GradArgs {
     float* partial;      // not NULL: sums [slice][tile] in the order in which lanes hold them, added to where `add`
     int add;
     const float* down;   // factor of an output, or NULL
+    const uint8_t* live; // of du's rows: a padded one's g is 0, which times an infinity in W would be NaN
 };
 
 // A tile of du = g W (sums of W, rows of g) or dw = g' u (sums of both). The outputs' columns are the matrix instructions' rows.
@@ -807,7 +808,8 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, unsigned block, uin
             staged.where(i, pass, row, col);
             if (r0 + row >= a.rows || c0 + col >= a.cols) continue;
             float v[4];
-            const u32x4 w = staged.take(lds, i);
+            u32x4 w = staged.take(lds, i);
+            if (a.live && !a.live[r0 + row]) w = u32x4{0, 0, 0, 0};
             __builtin_memcpy(v, &w, 16);
             put_quad((TO*)a.out + (r0 + row) * a.ld + c0 + col, a.cols - c0 - col, v);
         }
@@ -850,6 +852,7 @@ __global__ __launch_bounds__(256) void k_grad_join(const GradArgs du, const Grad
             s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
         for (; k < slices; ++k) s += from[k * n];
+        if (a.live && !a.live[r]) s = 0.f;
         const float v[4] = {s[0] * down, s[1] * down, s[2] * down, s[3] * down};
         put_quad((TO*)a.out + r * a.ld + c, a.cols - c, v);
     }
@@ -1196,7 +1199,7 @@ hipError_t backward(const iodf_class_loss& a, char* work, hipStream_t st) {
         du.a = {l.w.p, w.plane, w.ld, a.cols, n};
         du.b = {l.g, l.g_plane, l.g_ld, (int)p.rows_up, (int)p.rows_up};
         du.kts = (n + PK - 1) / PK, du.rows = a.rows, du.cols = a.cols, du.out = a.du, du.ld = a.du_stride;
-        du.partial = du_sums, du.add = v0 > 0;
+        du.partial = du_sums, du.add = v0 > 0, du.live = a.live;
         du.down = p.wide ? nullptr : s ? &s->ig : l.inverse;
         dw.a = {l.u.p, l.u.plane, l.u.ld, a.cols, (int)a.rows};
         dw.b = {l.g, l.g_plane, l.g_ld, (int)p.piece, (int)p.rows_up};

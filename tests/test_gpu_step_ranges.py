@@ -129,6 +129,17 @@ def test_class_loss_gradients_at_the_end_of_the_range():
     near(b, dw, "bf16", ew, "dweight")
 
 
+@pytest.mark.parametrize("rows,classes,cols", [(9, 300, 96), (150, 270, 96), (300, 513, 200), (40, 200, 4100)])
+@pytest.mark.parametrize("name", NAMES)
+def test_padded_rows_have_no_gradient_whatever_the_table_holds(rows, classes, cols, name):
+    u, w, target, live, _ = some(rows, classes, cols, name, seed=38, dead=0.4)
+    live[0], live[-1] = True, False
+    w[classes // 2, 1], w[classes - 1, 2] = np.inf, np.nan
+    t = torch()
+    du, _ = iodf.class_loss_backward(dev(u, name), dev(w, name), long(target), t.ones(rows, device="cuda"), t.ones(rows, device="cuda"), live=on_gpu(live))
+    assert not host(du)[~live].any() and not np.isfinite(host(du)[live]).all()
+
+
 @pytest.mark.parametrize("rows", [12, 300])
 @pytest.mark.parametrize("name", ["f32", "bf16"])
 def test_rows_without_upstream_gradient_stay_out_whatever_their_logits(name, rows):
