@@ -377,7 +377,8 @@ int iodf_weight_grad_workspace(const iodf_wgrad* args, int64_t* bytes);
  *   exactly but for what is 2^-25 of a product and less, however large or small others are. The forward pass multiplies F32 numbers of more than 64 rows in two
  *   parts of 11 bits each, exact to 2^-22 of the number, or to 2^-51 of its own row's or class's largest.
  * `live` as above: a padded row's u, target, lse, dloss and dlse may be anything; its du is 0. A target outside 0..classes-1 in any other row makes that
- * row's loss, du and all of dw NaN. Sums are in an order that depends on the sizes alone. With no rows dw is 0.
+ * row's loss, du and all of dw NaN. Sums are in an order that depends on the sizes and the type, not on which gradients are asked
+ * for, and in the forward pass of up to 16 rows of 16 bits on whether w's columns are a multiple of 64 and its rows start at multiples of 16 bytes. With no rows dw is 0.
  * 0 <= rows <= 2^24, 1 <= classes <= 2^20, 1 <= cols <= 65536, rows and classes times cols <= 2^34, rows times classes <= 2^38. Outputs overlap no
  * inputs. The workspace depends on sizes, type, strides, on which of the pointers are NULL and on how u and w are aligned: it is asked for with the same
  * arguments.

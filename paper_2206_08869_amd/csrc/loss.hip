@@ -1035,11 +1035,10 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         const int products = p.wide ? 6 : p.fine ? 2 : 1;
         const Task tasks[2] = {{a.cols, a.rows, (int)((here + PK - 1) / PK), here < a.classes}, {a.cols, here, (int)((a.rows + PK - 1) / PK), false}};
         const int most = p.fine ? 128 : 256;
+        // As for both, whichever are asked for: a gradient has the same bits with the other and without.
         Cut cuts[2];
-        float alone = 0.f;
-        if (a.du) alone += cut_of(tasks, 1, &p.du, products, most);
-        if (a.dw) alone += cut_of(tasks + 1, 1, &p.dw, products, most);
-        if (a.du && a.dw && cut_of(tasks, 2, cuts, products, most) < alone) p.together = true, p.du = cuts[0], p.dw = cuts[1];
+        const float alone = cut_of(tasks, 1, &p.du, products, most) + cut_of(tasks + 1, 1, &p.dw, products, most);
+        if (cut_of(tasks, 2, cuts, products, most) < alone) p.together = a.du && a.dw, p.du = cuts[0], p.dw = cuts[1];
         auto sums = [&](const Cut& c, long long rows) { return (size_t)c.slices * up(rows, c.edge) * up(a.cols, c.edge) * 4; };
         if (a.du && (p.du.slices > 1 || p.piece < a.classes)) p.du_sums = take(sums(p.du, a.rows));
         if (a.dw && p.dw.slices > 1) p.dw_sums = take(sums(p.dw, here));

@@ -6,7 +6,7 @@ import pytest
 import paper_2206_08869_amd as iodf
 import step_ref as ref
 from test_gpu_blocks import as_type, dev, half_unit, host, near, on_gpu, torch
-from test_gpu_step import NAMES, check_forward, long, some, upstream
+from test_gpu_step import NAMES, check_forward, long, on_card, some, upstream
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -156,3 +156,14 @@ def test_rows_without_upstream_gradient_stay_out_whatever_their_logits(name, row
     near(got[0][torch().from_numpy(rest).cuda()], du, name, eu, "du")
     near(got[1], dw, name, ew, "dweight")
     assert not got[0][torch().from_numpy(~rest).cuda()].any()
+
+
+@pytest.mark.parametrize("rows,classes,cols,name", [(2049, 3001, 768, "bf16"), (4096, 8192, 320, "bf16"), (600, 5003, 264, "f32"), (600, 5003, 264, "f16"),
+                                                   (20, 9000, 130, "f32"), (5000, 40, 700, "bf16")])
+def test_a_gradient_has_the_same_bits_with_the_other_and_without(rows, classes, cols, name):
+    t = torch()
+    u, w, target, d = on_card(rows, classes, cols, name, 41)
+    lse = iodf.class_loss(u, w, target).lse
+    both = iodf.class_loss_backward(u, w, target, lse, d)
+    assert t.equal(iodf.class_loss_backward(u, w, target, lse, d, need=(True, False))[0], both[0])
+    assert t.equal(iodf.class_loss_backward(u, w, target, lse, d, need=(False, True))[1], both[1])
