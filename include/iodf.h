@@ -411,12 +411,13 @@ int iodf_class_loss_workspace(const iodf_class_loss* args, int backward, int64_t
  * what lies beside its diagonal; X itself is kept in 22), which shows in the result as less than its own rounding; for F32 and F16 they have 22 bits.
  * Norms and sums are 32 bits or more. A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN.
  * 0 <= count <= 4096, 1 <= rows, cols <= 65536, the shorter side at most 16384, count * rows * cols (each rounded up to 64) <= 2^32,
- * 1 <= steps <= 16. Polynomials that let singular values from 0..1 grow past 64 are refused. out may be in (same type and strides).
+ * 1 <= steps <= 16, eps above 0. Polynomials that let singular values from 0..1 grow past 64 are refused. out may be in (same type and strides). As many matrices go together as have 2^26
+ * elements, one at least: the workspace is about 1 GB at most, but for a matrix that wants more by itself.
  *
  * iodf_muon_step: the step of an optimiser around that, for `count` weights of one shape, each a tensor of its own (arrays of pointers, host memory):
  *   M <- beta M + G,  D = G + beta M (nesterov) or M,  W <- (1 - rate * decay) W - rate * scale * orthogonalise(D)
- * M F32 with consecutive rows; W and G strided, of their types. Products are as for out_type = weight_type. 0 <= count <= 64. Tensors of one call
- * do not overlap.
+ * M F32 with consecutive rows; W and G strided, of their types. Products are as for out_type = weight_type. 0 <= count <= 64, whatever their
+ * size together. Tensors of one call do not overlap.
  */
 enum { IODF_ORTH_MOST = 16, IODF_MUON_MOST = 64 };
 typedef struct iodf_orth {

@@ -1155,31 +1155,58 @@ bool orth_steps(int steps, const float* co, OrthSteps& s) {
     return true;
 }
 
-size_t orth_workspace(const iodf_orth& a) { return orth_plan(a.count, a.rows, a.cols, a.out_type).bytes; }
-size_t muon_workspace(const iodf_muon& a) { return orth_plan(a.count, a.rows, a.cols, a.weight_type).bytes; }
+// How many matrices go together: those whose scratch, 16 bytes an element and less, stays within a gigabyte or so, one at least. Fewer would not fill the chip, more do not make it
+// fuller: 2^26 elements are 1024 tiles of 256.
+static long long together(long long count, int rows, int cols) {
+    return std::max<long long>(1, std::min<long long>(count, (1ll << 26) / (up(rows, PK) * up(cols, PK))));
+}
+static size_t workspace(long long count, int rows, int cols, int type) {
+    const long long most = together(count, rows, cols);
+    return std::max(orth_plan(most, rows, cols, type).bytes, count % most ? orth_plan(count % most, rows, cols, type).bytes : 0);
+}
+
+size_t orth_workspace(const iodf_orth& a) { return workspace(a.count, a.rows, a.cols, a.out_type); }
+size_t muon_workspace(const iodf_muon& a) { return workspace(a.count, a.rows, a.cols, a.weight_type); }
 
 hipError_t launch_orthogonalise(const iodf_orth& a, const OrthSteps& s, void* work, hipStream_t st) {
-    const OrthPlan p = orth_plan(a.count, a.rows, a.cols, a.out_type);
-    Source src{};
-    src.g[0] = a.in, src.stride = a.in_stride, src.batch = a.in_batch;
-    Target t{};
-    t.w[0] = a.out, t.stride = a.out_stride, t.batch = a.out_batch;
-    if (p.block || p.groups == 1) return all_at_once<false>(src, a.in_type, p, s, a.eps, (char*)work, t, a.out_type, st);
-    begin<false>(src, a.in_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
-    return run(p, s, (char*)work, t, a.out_type, st);
+    const long long most = together(a.count, a.rows, a.cols);
+    auto size_of = [](int type) { return type == IODF_T_F32 ? 4 : 2; };
+    hipError_t rc = hipSuccess;
+    for (long long at = 0; at < a.count && rc == hipSuccess; at += most) {
+        const OrthPlan p = orth_plan(std::min(most, a.count - at), a.rows, a.cols, a.out_type);
+        Source src{};
+        src.g[0] = (const char*)a.in + at * a.in_batch * size_of(a.in_type), src.stride = a.in_stride, src.batch = a.in_batch;
+        Target t{};
+        t.w[0] = (char*)a.out + at * a.out_batch * size_of(a.out_type), t.stride = a.out_stride, t.batch = a.out_batch;
+        if (p.block || p.groups == 1) {
+            rc = all_at_once<false>(src, a.in_type, p, s, a.eps, (char*)work, t, a.out_type, st);
+        } else {
+            begin<false>(src, a.in_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
+            rc = run(p, s, (char*)work, t, a.out_type, st);
+        }
+    }
+    return rc;
 }
 
 hipError_t launch_muon_step(const iodf_muon& a, const OrthSteps& s, void* work, hipStream_t st) {
-    const OrthPlan p = orth_plan(a.count, a.rows, a.cols, a.weight_type);
-    Source src{};
-    Target t{};
-    for (int k = 0; k < a.count; ++k) src.g[k] = a.grads[k], src.m[k] = a.momenta[k], t.w[k] = a.weights[k];
-    src.stride = a.grad_stride, src.beta = a.beta, src.nesterov = a.nesterov;
-    t.stride = a.weight_stride, t.update = 1;
-    t.keep = (float)(1.0 - (double)a.rate * a.decay), t.by = (float)(-(double)a.rate * a.scale);
-    if (p.block || p.groups == 1) return all_at_once<true>(src, a.grad_type, p, s, a.eps, (char*)work, t, a.weight_type, st);
-    begin<true>(src, a.grad_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
-    return run(p, s, (char*)work, t, a.weight_type, st);
+    const long long most = together(a.count, a.rows, a.cols);
+    hipError_t rc = hipSuccess;
+    for (long long at = 0; at < a.count && rc == hipSuccess; at += most) {
+        const OrthPlan p = orth_plan(std::min(most, a.count - at), a.rows, a.cols, a.weight_type);
+        Source src{};
+        Target t{};
+        for (int k = 0; k < p.z.count; ++k) src.g[k] = a.grads[at + k], src.m[k] = a.momenta[at + k], t.w[k] = a.weights[at + k];
+        src.stride = a.grad_stride, src.beta = a.beta, src.nesterov = a.nesterov;
+        t.stride = a.weight_stride, t.update = 1;
+        t.keep = (float)(1.0 - (double)a.rate * a.decay), t.by = (float)(-(double)a.rate * a.scale);
+        if (p.block || p.groups == 1) {
+            rc = all_at_once<true>(src, a.grad_type, p, s, a.eps, (char*)work, t, a.weight_type, st);
+        } else {
+            begin<true>(src, a.grad_type, p, a.eps, ldexpf(1.f, s.x_exp[0]), (char*)work, st);
+            rc = run(p, s, (char*)work, t, a.weight_type, st);
+        }
+    }
+    return rc;
 }
 
 }  // namespace iodf

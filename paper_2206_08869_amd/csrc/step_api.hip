@@ -98,7 +98,7 @@ int iodf_orthogonalise(const iodf_orth* a, void* work, int64_t work_bytes, void*
 }
 
 int iodf_muon_workspace(const iodf_muon* a, int64_t* bytes) {
-    if (!a || !bytes || !a_type(a->weight_type) || !a_type(a->grad_type) || a->count > kMaxUpdates || !check_orth_sizes(a->count, a->rows, a->cols, a->eps))
+    if (!a || !bytes || !a_type(a->weight_type) || !a_type(a->grad_type) || a->count < 0 || a->count > kMaxUpdates || !check_orth_sizes(1, a->rows, a->cols, a->eps))
         return IODF_E_ARG;
     *bytes = a->count ? (int64_t)muon_workspace(*a) : 0;
     return IODF_OK;

@@ -167,3 +167,15 @@ def test_a_gradient_has_the_same_bits_with_the_other_and_without(rows, classes, 
     both = iodf.class_loss_backward(u, w, target, lse, d)
     assert t.equal(iodf.class_loss_backward(u, w, target, lse, d, need=(True, False))[0], both[0])
     assert t.equal(iodf.class_loss_backward(u, w, target, lse, d, need=(False, True))[1], both[1])
+
+
+def test_many_large_matrices_go_a_few_at_a_time():
+    """2^26 elements at a time: the bits of calls with as many."""
+    t = torch()
+    gen = t.Generator("cuda").manual_seed(42)
+    g = t.randn((5, 4096, 4096), generator=gen, device="cuda").bfloat16()
+    got = iodf.orthogonalise(g)
+    assert t.equal(got[:4], iodf.orthogonalise(g[:4])) and t.equal(got[4:], iodf.orthogonalise(g[4:]))
+    w, m = [t.zeros_like(x) for x in g], [t.zeros((4096, 4096), device="cuda") for _ in g]
+    iodf.muon_step(w, list(g), m, 1.0, beta=0.0, nesterov=False, scale=-1.0)
+    assert all(t.equal(a, b) for a, b in zip(w, got)) and all(t.equal(a, b.float()) for a, b in zip(m, g))

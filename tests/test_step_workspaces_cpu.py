@@ -1,0 +1,21 @@
+"""Scratch of the loss over a table of classes and of orthogonalised updates, which the library answers without a GPU: bounded however many and large the tensors."""
+import ctypes
+
+import pytest
+
+import paper_2206_08869_amd as iodf
+from test_step_cpu import buf, lib, loss_args, muon_args, orth_args  # noqa: F401
+
+GB = 1 << 30
+
+
+@pytest.mark.parametrize("kind", [0, 1, 2])
+@pytest.mark.parametrize("rows,cols,most", [(8192, 8192, 2 * GB), (8192, 16384, 3 * GB), (2048, 512, 2 * GB), (64, 65536, 2 * GB), (4100, 4096, 2 * GB), (100, 100, 2 * GB)])
+def test_updates_of_long_lists_take_a_bounded_workspace(lib, buf, rows, cols, most, kind):  # noqa: F811
+    n, one = ctypes.c_int64(0), ctypes.c_int64(0)
+    a = dict(rows=rows, cols=cols, weight_type=kind, weight_stride=cols, grad_stride=cols)
+    assert lib.iodf_muon_workspace(muon_args(buf[1], count=64, **a), n) == 0
+    assert 0 < n.value <= most
+    assert lib.iodf_muon_workspace(muon_args(buf[1], count=1, **a), one) == 0 and one.value <= n.value
+    o = orth_args(buf[1], count=32, rows=rows, cols=cols, out_type=kind, in_stride=cols, out_stride=cols, in_batch=rows * cols, out_batch=rows * cols)
+    assert lib.iodf_orthogonalise_workspace(o, n) == 0 and 0 < n.value <= most
