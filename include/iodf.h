@@ -371,7 +371,7 @@ int iodf_weight_grad_workspace(const iodf_wgrad* args, int64_t* bytes);
  * iodf_class_loss_backward: lse as the forward pass gave it, dloss = dL/dloss and dlse = dL/dlse (either may be NULL: 0) ->
  *   du[t][c] = sum_v g[t][v] W[v][c] and dw[v][c] = sum_t g[t][v] u[t][c] of `type` (either may be NULL: not computed), with
  *   g[t][v] = (dloss[t] + dlse[t]) exp(s[t][v] - lse[t]) - (v == target[t]) dloss[t], the exponential being 1 at most.
- *   It goes over the classes in pieces whose g fits 512 MB (256 classes at least). In 16-bit types g is rounded to that type after it is multiplied so that
+ *   It goes over the classes in pieces whose g fits 512 MB (a tile's 64 to 256 classes at least). In 16-bit types g is rounded to that type after it is multiplied so that
  *   the first dloss that is not 0, of 64 rows spread over all, is a power of two (in half precision the largest); where few of them make up a gradient (16 rows, 32
  *   classes, 128 columns or 2^16 of them) it has two parts, so that gradients are as far off as their own rounding. In F32 numbers are multiplied
  *   exactly but for what is 2^-25 of a product and less, however large or small others are. The forward pass multiplies F32 numbers of more than 64 rows in two

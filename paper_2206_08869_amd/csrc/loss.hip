@@ -251,7 +251,7 @@ struct LogitArgs {
     const float* dloss;
     const float* dlse;
     float* inverse;      // without scales: of what g is multiplied with
-    uint16_t* g;         // [rows up to a multiple of 256][ld]
+    uint16_t* g;         // [rows up to the tiles' end][ld]
     long long g_ld, g_plane;
     int per;             // tiles along the columns of a slice
     int slices;
@@ -984,9 +984,11 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     // (23726 rows, 2091 classes of 11 columns: 1.5); 200 rows, 300 classes of 8000 columns 1.26 times, 21 rows, 40000 classes of 3000 1.17. A second part costs a
     // second product: 256 rows, 4000 classes of 512 columns 28 us for 22, 32000 classes of 4096 columns 607 for 339.
     p.fine = backward && !p.wide && (a.rows <= 16 || a.classes <= 32 || a.cols <= 128 || a.rows * a.classes <= 65536);
-    p.rows_up = up(a.rows, 256);
-    p.logits = logits_cut(a.classes, a.rows, p.kts, !p.wide ? 1 : backward ? 6 : 3, p.fine ? 128 : 256);
+    // g of few classes is not made wider than a tile of them
+    const int most = backward && a.classes <= 64 ? 64 : backward && (p.fine || a.classes <= 128) ? 128 : 256;
+    p.logits = logits_cut(a.classes, a.rows, p.kts, !p.wide ? 1 : backward ? 6 : 3, most);
     p.tiles = (a.classes + p.logits.edge - 1) / p.logits.edge;
+    p.rows_up = up(a.rows, p.logits.edge);
     // us by k_few and by a copy and tiles, 32000 classes of 1111 columns: in 32 bits 32 and 108 for a row, 47 and 110 for 32, 75 and 114 for 64; in bfloat16 29 and
     // 42 for a row, 37 and 43 for 16, 57 and 43 for 32.
     if (!backward && p.w_ready && a.rows <= (p.wide ? 64 : 16)) {
@@ -1020,7 +1022,7 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     };
     if (p.scaled) p.maxima = take((size_t)p.maxima_parts * 4);
     if (backward) p.scales = take(sizeof(Scales));
-    if (p.wide && !backward && !p.few) p.u_exp = take((size_t)p.rows_up * 4), p.w_exp = take((size_t)up(a.classes, 256) * 4);
+    if (p.wide && !backward && !p.few) p.u_exp = take((size_t)p.rows_up * 4), p.w_exp = take((size_t)p.tiles * p.logits.edge * 4);
     if (p.u_ready) p.u = take((size_t)p.planes * a.rows * p.pitch * 2);
     if (p.w_ready) p.w = take((size_t)p.planes * a.classes * p.pitch * 2);
     if (!p.few && p.logits.slices > 1) p.sums = take((size_t)p.logits.slices * p.tiles * up(a.rows, p.logits.edge) * p.logits.edge * 4);
@@ -1028,8 +1030,9 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.parts = take((size_t)p.tiles * a.rows * 8), p.picked = take((size_t)a.rows * 4);
     } else if (a.rows) {
         const int g_planes = p.wide ? 3 : p.fine ? 2 : 1;
-        p.piece = std::max<long long>(256, kPieceBytes / (p.rows_up * 2 * g_planes) / 256 * 256);
-        p.piece = std::min(p.piece, up(a.classes, 256));
+        const long long edge = p.logits.edge;  // whole tiles: products read up to a multiple of 64 along their sums
+        p.piece = std::max(edge, kPieceBytes / (p.rows_up * 2 * g_planes) / edge * edge);
+        p.piece = std::min(p.piece, up(a.classes, edge));
         p.g = take((size_t)g_planes * p.rows_up * p.piece * 2);
         const long long here = std::min<long long>(p.piece, a.classes);
         const int products = p.wide ? 6 : p.fine ? 2 : 1;

@@ -19,3 +19,14 @@ def test_updates_of_long_lists_take_a_bounded_workspace(lib, buf, rows, cols, mo
     assert lib.iodf_muon_workspace(muon_args(buf[1], count=1, **a), one) == 0 and one.value <= n.value
     o = orth_args(buf[1], count=32, rows=rows, cols=cols, out_type=kind, in_stride=cols, out_stride=cols, in_batch=rows * cols, out_batch=rows * cols)
     assert lib.iodf_orthogonalise_workspace(o, n) == 0 and 0 < n.value <= most
+
+
+@pytest.mark.parametrize("rows,classes", [(1 << 20, 14), (1 << 24, 2), (1 << 24, 1), (300, 5), (1 << 17, 60)])
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_gradients_over_a_few_classes_take_what_they_read(lib, buf, rows, classes, kind):  # noqa: F811
+    """64 classes, which is what a product reads along its sum, in all parts, beside the copy of 16 columns as 64 of them; not 256 classes."""
+    n = ctypes.c_int64(0)
+    a = loss_args(1 << 20, rows=rows, classes=classes, cols=16, type=kind, u_stride=16, w_stride=16, du_stride=16, dw_stride=16)
+    assert lib.iodf_class_loss_workspace(a, 1, n) == 0
+    parts_of_g, parts_of_u, up = (3, 3, rows + 63) if kind == 0 else (2, 1, rows + 63)
+    assert n.value <= up * 64 * 2 * (parts_of_g + parts_of_u) + (16 << 20)
