@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "block_dev.h"
+#include "plan.h"
 
 namespace iodf {
 
@@ -25,8 +26,6 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-constexpr int PK = 64;  // of a tile along k
 
 // An operand, its base and leading dimension in elements. Rows (or, of a `sums` operand, columns) past `extent` repeat existing ones: they only reach
 // outputs that nobody stores. Along k a `rows` operand is readable up to a multiple of 64; a `sums` operand repeats its last row past `depth`. What
