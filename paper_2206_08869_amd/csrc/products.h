@@ -54,10 +54,6 @@ template <> struct Mma<_Float16> {
 __device__ __forceinline__ void to_lds16(uint32_t lds, const void* base, uint32_t off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
-template <int LEFT>
-__device__ __forceinline__ void wait_vm() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
-}
 
 // A barrier that waits for LDS only: stores on their way to memory are left there.
 __device__ __forceinline__ void lds_barrier() {
