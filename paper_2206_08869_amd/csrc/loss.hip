@@ -271,7 +271,7 @@ struct FewArgs {
     const int64_t* target;
     f32x2* parts;
     float* picked;
-    float* g;            // gradients: [classes][16], the other two are not looked at then
+    float* g;            // gradients: [classes][rows up to a multiple of 16], the other two are not looked at then
     const uint8_t* live;
     const float* lse;
     const float* dloss;
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int c = b * 16 + lane / 16 * 4 + j;
-                        if (c0 + c < a.classes) a.g[(c0 + c) * 16ll + r] = there ? both * expf(s[j] - lse > 0.f ? 0.f : s[j] - lse) - (want == c ? up : 0.f) : 0.f;
+                        if (c0 + c < a.classes) a.g[(c0 + c) * (NB * 16ll) + n * 16 + r] = there ? both * expf(s[j] - lse > 0.f ? 0.f : s[j] - lse) - (want == c ? up : 0.f) : 0.f;
                     }
                 }
                 continue;
@@ -404,6 +404,28 @@ __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
     }
 }
 
+// C neighbours of a row of which n exist, at any element's address.
+template <typename Cols, int C>
+__device__ __forceinline__ Cols get_cols(const float* from, int n) {
+    typedef Cols Any __attribute__((aligned(4)));
+    Cols v;
+    if (n >= C) return *(const Any*)from;
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = j < n ? from[j] : 0.f;
+    return v;
+}
+template <typename Cols, int C>
+__device__ __forceinline__ void put_cols(float* to, int n, Cols v) {
+    typedef Cols Any __attribute__((aligned(4)));
+    if (n >= C) {
+        *(Any*)to = v;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < C - 1; ++j)
+        if (j < n) to[j] = v[j];
+}
+
 struct FewGradArgs {
     const float* w;
     const float* u;
@@ -418,51 +440,47 @@ struct FewGradArgs {
     int slices, pitch;
 };
 
-// Gradients of up to sixteen rows in 32 bits: a wave has 256 columns of u and of du in registers, goes through its classes, adds g W to du, and writes g' u to dw.
+// Gradients of up to 32 rows in 32 bits: a wave has 256 columns of u and of du in registers (128 of more than sixteen rows), goes through its classes, adds g W to du, and writes g' u to dw.
 // Nothing is copied or scaled for it, and memory bounds it: with the logits before it W is read twice and dw written, 24000 classes of 6592 columns 427 us (4.4 TB/s).
 template <int R>
 __global__ __launch_bounds__(256) void k_few_grad(const FewGradArgs a) {
-    constexpr int AT_ONCE = 4;
-    __shared__ f32x4 meet[3][R][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = blockIdx.x * 256 + lane * 4, n = a.cols - c;
-    float u[R][4], du[R][4] = {};
+    constexpr int AT_ONCE = 4, C = R > 16 ? 2 : 4, OF = R > 16 ? R : 16;  // columns of a lane, numbers of a class in g
+    typedef float Cols __attribute__((ext_vector_type(C)));
+    __shared__ Cols meet[3][R][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = blockIdx.x * (64 * C) + lane * C, n = a.cols - c;
+    Cols u[R], du[R] = {};
 #pragma unroll
-    for (int t = 0; t < R; ++t) {
-        u[t][0] = u[t][1] = u[t][2] = u[t][3] = 0.f;
-        if (t < a.rows && n > 0 && !(a.live && !a.live[t])) get_quad(a.u + t * a.u_stride + c, n, u[t]);
-    }
+    for (int t = 0; t < R; ++t) u[t] = t < a.rows && n > 0 && !(a.live && !a.live[t]) ? get_cols<Cols, C>(a.u + t * a.u_stride + c, n) : Cols(0.f);
     const int v0 = ((int)blockIdx.y * 4 + wave) * a.per, v1 = min(a.classes, v0 + a.per);
     for (int v = v0; v < v1; v += AT_ONCE) {
-        float w[AT_ONCE][4] = {};
+        Cols w[AT_ONCE] = {};
         if (a.du && n > 0) {
 #pragma unroll
-            for (int k = 0; k < AT_ONCE; ++k) get_quad(a.w + min(v + k, a.classes - 1) * a.w_stride + c, n, w[k]);
+            for (int k = 0; k < AT_ONCE; ++k) w[k] = get_cols<Cols, C>(a.w + min(v + k, a.classes - 1) * a.w_stride + c, n);
         }
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             if (v + k >= v1) break;
-            const float* const g = a.g + (v + k) * 16ll;
-            float out[4] = {};
+            const float* const g = a.g + (v + k) * (long long)OF;
+            Cols out = {};
 #pragma unroll
             for (int t = 0; t < R; ++t) {
                 const float gt = g[t];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) du[t][j] = fmaf(gt, w[k][j], du[t][j]), out[j] = fmaf(gt, u[t][j], out[j]);
+                for (int j = 0; j < C; ++j) du[t][j] = fmaf(gt, w[k][j], du[t][j]), out[j] = fmaf(gt, u[t][j], out[j]);
             }
-            if (a.dw && n > 0) put_quad(a.dw + (v + k) * a.dw_stride + c, n, out);
+            if (a.dw && n > 0) put_cols<Cols, C>(a.dw + (v + k) * a.dw_stride + c, n, out);
         }
     }
     if (!a.du) return;
 #pragma unroll
     for (int t = 0; t < R; ++t)
-        if (wave) meet[wave - 1][t][lane] = f32x4{du[t][0], du[t][1], du[t][2], du[t][3]};
+        if (wave) meet[wave - 1][t][lane] = du[t];
     __syncthreads();
     if (wave) return;
 #pragma unroll
-    for (int t = 0; t < R; ++t) {
-        const f32x4 s = (f32x4{du[t][0], du[t][1], du[t][2], du[t][3]} + meet[0][t][lane]) + (meet[1][t][lane] + meet[2][t][lane]);
-        *(f32x4*)(a.sums + ((long long)blockIdx.y * R + t) * a.pitch + c) = s;
-    }
+    for (int t = 0; t < R; ++t)
+        *(Cols*)(a.sums + ((long long)blockIdx.y * R + t) * a.pitch + c) = (du[t] + meet[0][t][lane]) + (meet[1][t][lane] + meet[2][t][lane]);
 }
 
 // The workgroups' sums: 64 columns of a row to a workgroup, sixteen threads to four columns.
@@ -970,15 +988,17 @@ hipError_t forward(const iodf_class_loss& a, char* work, hipStream_t st) {
 
 hipError_t few_backward(const iodf_class_loss& a, const LossPlan& p, char* work, hipStream_t st) {
     const FewArgs f{a.w, a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.groups, a.target, nullptr, nullptr, (float*)(work + p.g), a.live, a.lse, a.dloss, a.dlse};
-    k_few<float, 1, true><<<(unsigned)p.tiles, 256, 0, st>>>(f);
-    const int across = (a.cols + 255) / 256;
+    if (p.few == 1) k_few<float, 1, true><<<(unsigned)p.tiles, 256, 0, st>>>(f);
+    else k_few<float, 2, true><<<(unsigned)p.tiles, 256, 0, st>>>(f);
+    const int span = p.few == 1 ? 256 : 128, across = (a.cols + span - 1) / span;
     const FewGradArgs g{(const float*)a.w, (const float*)a.u, a.w_stride, a.u_stride, a.classes, a.cols, (int)a.rows, p.few_per, a.live, f.g, (float*)a.du, (float*)a.dw, a.du_stride, a.dw_stride,
-                        (float*)(work + p.du_sums), p.few_slices, across * 256};
+                        (float*)(work + p.du_sums), p.few_slices, across * span};
     auto go = [&](auto kernel) { kernel<<<dim3(across, p.few_slices), 256, 0, st>>>(g); };
     if (p.few_rows == 2) go(k_few_grad<2>);
     else if (p.few_rows == 4) go(k_few_grad<4>);
     else if (p.few_rows == 8) go(k_few_grad<8>);
-    else go(k_few_grad<16>);
+    else if (p.few_rows == 16) go(k_few_grad<16>);
+    else go(k_few_grad<32>);
     if (a.du) k_few_join<<<dim3((a.cols + 63) / 64, (unsigned)a.rows), 256, 0, st>>>(g, p.few_rows);
     return hipGetLastError();
 }

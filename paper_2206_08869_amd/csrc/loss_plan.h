@@ -148,19 +148,20 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
         p.tiles = (groups + p.groups - 1) / p.groups;
         p.u_ready = p.w_ready = false;
     }
-    // us by k_few and k_few_grad and by tiles, in 32 bits: 24000 classes of 6592 columns 427 and 863 for a row, 538 and 910 for 16; 32000 of 1111 112 and 220, 135 and 221;
-    // 50 of 100 20 and 25. In bfloat16, where tiles read W as it lies, 363 and 405, 115 and 113, 20 and 21 for a row: not by these.
-    if (backward && p.wide && a.rows && a.rows <= 16) {
-        const int groups = (a.classes + 31) / 32, across = (a.cols + 255) / 256, waves = std::max(1, 512 / across) * 4;
-        p.few = 1;
+    // us by k_few and k_few_grad and by tiles, in 32 bits: 24000 classes of 6592 columns 427 and 1088 for a row, 538 and 1088 for 16, 887 and 1088 for 17; 32000 of 1111 188 and 273 for 32;
+    // 300 of 96 17 and 19 for 17. With more than 16 rows not where a few classes have long rows, whose sums k_few does not split as well: 100 of 5000 41 and 26 for 24. In bfloat16,
+    // where tiles read W as it lies, 363 and 405, 115 and 113, 20 and 21 for a row: not by these.
+    if (backward && p.wide && a.rows && (a.rows <= 16 || (a.rows <= 32 && a.cols <= 4ll * a.classes))) {
+        p.few = a.rows <= 16 ? 1 : 2;
+        const int groups = (a.classes + 31) / 32, span = p.few == 1 ? 256 : 128, across = (a.cols + span - 1) / span, waves = std::max(1, 512 / across) * 4;
         p.groups = (groups + 2047) / 2048;
         p.tiles = (groups + p.groups - 1) / p.groups;
-        p.few_rows = a.rows <= 2 ? 2 : a.rows <= 4 ? 4 : a.rows <= 8 ? 8 : 16;
+        p.few_rows = a.rows <= 2 ? 2 : a.rows <= 4 ? 4 : a.rows <= 8 ? 8 : a.rows <= 16 ? 16 : 32;
         p.few_per = std::max(4, (a.classes + waves - 1) / waves);
         p.few_slices = (a.classes + 4 * p.few_per - 1) / (4 * p.few_per);
-        const size_t g = (size_t)up((long long)a.classes * 16 * 4, 256);
+        const size_t g = (size_t)up((long long)a.classes * p.few * 16 * 4, 256);
         p.g = 0, p.du_sums = g;
-        p.bytes = g + (a.du ? (size_t)p.few_slices * p.few_rows * across * 256 * 4 : 0);
+        p.bytes = g + (a.du ? (size_t)p.few_slices * p.few_rows * across * span * 4 : 0);
         return p;
     }
     p.maxima_parts = (int)std::max<long long>(1, std::min<long long>(kMaxima, (a.rows + 511) / 512));

@@ -21,7 +21,8 @@ LOSS_CALLS = [
     (8, 32, 64, "f16", 0, 1, 0), (1, 360, 64, "f32", 1, 1, 1), (4, 104, 64, "f32", 1, 1, 0), (20, 32, 64, "f32", 0, 1, 1),
     (8, 45, 115, "f32", 0, 1, 1), (1, 45, 1600, "f16", 0, 0, 1), (1, 58, 1280, "bf16", 0, 0, 1), (6, 233, 64, "bf16", 0, 0, 1),
     (1, 83, 1401, "f16", 1, 1, 0), (4, 466, 64, "f16", 0, 0, 1), (36, 193, 22, "f32", 0, 0, 0), (1, 262, 616, "bf16", 0, 1, 1),
-    (16, 248, 64, "f32", 1, 0, 1), (5, 844, 64, "f32", 1, 1, 0), (120, 100, 23, "f32", 0, 1, 0), (6, 50, 982, "bf16", 1, 1, 0),
+    (16, 248, 64, "f32", 1, 0, 1), (27, 5003, 301, "f32", 1, 1, 0),
+    (35, 28277, 78, "f32", 1, 1, 0), (5, 844, 64, "f32", 1, 1, 0), (120, 100, 23, "f32", 0, 1, 0), (6, 50, 982, "bf16", 1, 1, 0),
     (75, 30, 951, "f32", 0, 1, 1), (1464, 64, 131, "f16", 1, 1, 0), (70, 956, 192, "bf16", 1, 1, 1), (18, 8923, 477, "f32", 1, 0, 0),
     (4303, 38, 832, "f32", 1, 1, 1), (1495, 6451, 20, "f32", 0, 0, 0), (24658, 33, 318, "f32", 1, 1, 1), (32454, 83, 112, "bf16", 1, 0, 0),
     (13032, 1072, 25, "f16", 0, 1, 1), (131, 26886, 105, "f16", 1, 0, 1), (69, 30237, 192, "f32", 0, 1, 1), (837, 6732, 72, "f16", 1, 0, 0),
