@@ -373,7 +373,7 @@ int iodf_weight_grad_workspace(const iodf_wgrad* args, int64_t* bytes);
  *   g[t][v] = (dloss[t] + dlse[t]) exp(s[t][v] - lse[t]) - (v == target[t]) dloss[t], the exponential being 1 at most.
  *   It goes over the classes in pieces whose g fits 512 MB (a tile's 64 to 256 classes at least). In 16-bit types g is rounded to that type after it is multiplied so that
  *   the first dloss that is not 0, of 64 rows spread over all, is a power of two (in half precision the largest); where few of them make up a gradient (16 rows, 32
- *   classes, 128 columns or 2^16 of them) it has two parts, so that gradients are as far off as their own rounding. In F32 numbers are multiplied
+ *   classes, 128 columns or 2^16 of them) it has two parts, so that gradients are off by hardly more than their own rounding; elsewhere by 1.1 to 1.3 times that. In F32 numbers are multiplied
  *   exactly but for what is 2^-25 of a product and less, however large or small others are. The forward pass multiplies F32 numbers of more than 64 rows in two
  *   parts of 11 bits each, exact to 2^-22 of the number, or to 2^-51 of its own row's or class's largest.
  * `live` as above: a padded row's u, target, lse, dloss and dlse may be anything; its du is 0. A target outside 0..classes-1 in any other row makes that
@@ -408,7 +408,8 @@ int iodf_class_loss_workspace(const iodf_class_loss* args, int backward, int64_t
  *   X <- a X + b (X X') X + c (X X')^2 X,
  * which brings all but the smallest of them near 1 and leaves the singular vectors. `count` matrices at once, in_batch and out_batch elements apart.
  * coefficients: host memory, a, b, c of each step. For out_type BF16 the numbers that are multiplied are rounded to 11 bits (of X X' only
- * what lies beside its diagonal; X itself is kept in 22), which shows in the result as less than its own rounding; for F32 and F16 they have 22 bits.
+ * what lies beside its diagonal; X itself is kept in 22), which shows in the result as less than its own rounding; for F32 and F16 they have 22 bits, or are exact to 2^-38
+ * where 1 is X's norm (a G far below eps has little left).
  * Norms and sums are 32 bits or more. A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN.
  * 0 <= count <= 4096, 1 <= rows, cols <= 65536, the shorter side at most 16384, count * rows * cols (each rounded up to 64) <= 2^32,
  * 1 <= steps <= 16, eps above 0. Polynomials that let singular values from 0..1 grow past 64 are refused. out may be in (same type and strides). As many matrices go together as have 2^26

@@ -139,7 +139,7 @@ LossPlan loss_plan(const iodf_class_loss& a, bool backward) {
     p.logits = logits_cut(a.classes, a.rows, p.kts, !p.wide ? 1 : backward ? 6 : 3, most);
     p.tiles = (a.classes + p.logits.edge - 1) / p.logits.edge;
     p.rows_up = up(a.rows, p.logits.edge);
-    // us by k_few and by a copy and tiles, 32000 classes of 1111 columns: in 32 bits 32 and 108 for a row, 47 and 110 for 32, 75 and 114 for 64; in bfloat16 29 and
+    // us by k_few and by a copy and tiles, 32000 classes of 1111 columns: in 32 bits 32 and 77 for a row, 49 and 76 for 32, 78 and 76 for 64; in bfloat16 29 and
     // 42 for a row, 37 and 43 for 16, 57 and 43 for 32.
     if (!backward && p.w_ready && a.rows <= (p.wide ? 64 : 16)) {
         const int blocks = (int)((a.rows + 15) / 16), groups = (a.classes + 31) / 32;

@@ -68,7 +68,8 @@ def _loss_inputs(u, weight, target, live):
 def class_loss(u, weight, target, live=None):
     """lse = log sum_v exp(u . weight[v]) and loss = lse - u . weight[target] of each row -> ClassLoss, 0 in padded rows.
 
-    u [rows, cols] and weight [classes, cols] have one type. No logits are kept; a target that is no class makes its row's loss NaN."""
+    u [rows, cols] and weight [classes, cols] have one type. No logits are kept; a target that is no class makes its row's loss NaN. In 16 bits products are exact and sums have 32
+    bits. In float32 more than 64 rows are multiplied in 22 bits of each number, or down to 2^-51 of its row's or class's largest; no row sees how large the others are."""
     t = _k._torch if _native else _setup()
     kind, su, sw, rows, cols, device, lp = _loss_inputs(u, weight, target, live)
     loss, lse = t.empty(rows, dtype=_k._f32, device=device), t.empty(rows, dtype=_k._f32, device=device)
@@ -81,7 +82,9 @@ def class_loss(u, weight, target, live=None):
 def class_loss_backward(u, weight, target, lse, dloss, dlse=None, live=None, need=(True, True)):
     """dL/dloss and dL/dlse (float32 [rows]; either may be None) -> (dL/du, dL/dweight), in the tensors' type; lse as class_loss gave it.
 
-    The logits are computed again, a piece of the classes at a time. need: which of the two are wanted, the others are None."""
+    The logits are computed again, a piece of the classes at a time. need: which of the two are wanted, the others are None; a gradient's bits do not depend on it.
+    What the logits' gradient is rounded to on its way goes by the tensors' type: 16 bits, in two parts where few of them make up a gradient; in float32 all of its 24 bits, as all products
+    have, whatever the numbers' sizes (six products of 16 bits, so about a sixth of bfloat16's rate)."""
     t = _k._torch if _native else _setup()
     kind, su, sw, rows, cols, device, lp = _loss_inputs(u, weight, target, live)
     if lse is None:
@@ -217,7 +220,7 @@ def orthogonalise(g, steps=5, coefficients=QUINTIC, eps=1e-7, dtype=None, out=No
     """g / (its Frobenius norm + eps), `steps` times an odd polynomial of its singular values: nearly the orthogonal matrix next to it.
 
     g [rows, cols], or [count, rows, cols] for several of one shape. coefficients: (a, b, c) of X <- a X + b XX'X + c (XX')^2 X, or one triple for each
-    step. dtype: the result's, g's if None; bfloat16 takes a third of the work of float32 and float16. out may be g. At most 4096 matrices, whose shorter side
+    step. dtype: the result's, g's if None; bfloat16 takes a third of the work of float32 and float16, with 11 bits of what is multiplied instead of 22. out may be g. At most 4096 matrices, whose shorter side
     is at most 16384 and longer one at most 65536, of 2^32 elements together (sides rounded up to multiples of 64); eps is above 0."""
     t = _k._torch if _native else _setup()
     kind, count, rows, cols, batch, stride = _sheets(g, "g")
@@ -268,7 +271,8 @@ def muon_step(weights, grads, momenta, rate, beta=0.95, nesterov=True, decay=0.0
     m <- beta m + g, w <- (1 - rate decay) w - rate scale orthogonalise(g + beta m, or m without nesterov).
 
     momenta are contiguous float32 tensors, zeros before the first step. scale None: sqrt(max(1, rows / cols)). The numbers are part of a captured graph.
-    The products are those of a result in the weights' type: bfloat16 weights take a third of the work of the others."""
+    The products are those of a result in the weights' type: bfloat16 weights take a third of the work of the others, with 11 bits of what is multiplied instead of 22 whatever the
+    gradients' type. A list may be as long as it likes: as many weights go together as have 2^26 elements."""
     t = _k._torch if _native else _setup()
     weights, grads, momenta = _each(weights, "weights"), _each(grads, "grads"), _each(momenta, "momenta")
     if not len(weights) == len(grads) == len(momenta):

@@ -179,3 +179,21 @@ def test_many_large_matrices_go_a_few_at_a_time():
     w, m = [t.zeros_like(x) for x in g], [t.zeros((4096, 4096), device="cuda") for _ in g]
     iodf.muon_step(w, list(g), m, 1.0, beta=0.0, nesterov=False, scale=-1.0)
     assert all(t.equal(a, b) for a, b in zip(w, got)) and all(t.equal(a, b.float()) for a, b in zip(m, g))
+
+
+@pytest.mark.parametrize("rows,classes,cols,name", [(300, 400, 200, "f32"), (300, 400, 200, "bf16"), (20, 5000, 130, "f32"), (1000, 80, 300, "f32"), (40, 90, 64, "bf16")])
+def test_class_loss_gradients_of_classes_that_are_no_targets(rows, classes, cols, name):
+    """Their gradients are probabilities alone, here 1e-8 to 1e-15 of the others', and as near in themselves as those are."""
+    u, w, target, _, rng = some(rows, classes, cols, name, seed=43)
+    rare = np.arange(classes) % 3 == 1
+    u[:, 0], w[:, 0] = 1, 0
+    w[rare, 0] = -as_type(rng.uniform(18, 34, rare.sum()), name)
+    target[rare[target]] = 0
+    up = (np.full(rows, np.float64(np.float32(1.0 / rows))), None)
+    got, lse = gradients(u, w, target, None, name, *up)
+    step = U if name == "f32" else 2.0 ** -16 if cols <= 128 else 2.0 ** -8
+    du, dw, eu, ew = ref.gradients_by_the_parts(u, w, target, lse, *up, None, step)
+    assert 0 < np.abs(dw[rare]).max() < 1e-6 * np.abs(dw[~rare]).max()
+    for a, b, off in ((got[0], du, eu), (got[1], dw, ew)):
+        near(a, b, name, off + 1.01 * (half_unit(name, np.abs(b) + off) - half_unit(name, b)), "gradient")
+    assert np.linalg.norm(host(got[1])[rare] - dw[rare]) <= {"f32": 1e-5, "bf16": 2.0 ** -8}[name] * np.linalg.norm(dw[rare])
