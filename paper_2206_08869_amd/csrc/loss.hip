@@ -73,16 +73,20 @@ struct ReadyArgs {
     Scales* scales;
 };
 
-// v in three parts of bfloat16, whose sum it is (but for parts below the smallest numbers there are): whatever its size, an infinity or NaN as the first of them.
+// v in three parts of bfloat16, whose sum it is (but for parts below the smallest numbers there are), whatever its size. An infinity is the last part: that is multiplied with first parts alone, which
+// are 0 where the other number is, while others may be 0 where it is not, and 0 times an infinity is none.
 __device__ __forceinline__ void three_parts(float v, uint16_t (&part)[3]) {
     constexpr uint32_t MOST = 0x7f7f0000;  // the largest, where rounding would make an infinity
+    const bool endless = fabsf(v) == __builtin_inff();
+    float left = endless ? 0.f : v;
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
-        float h = (float)(__bf16)v;
-        if (p == 0 && fabsf(h) > __uint_as_float(MOST) && fabsf(v) < __builtin_inff()) h = copysignf(__uint_as_float(MOST), v);
+        float h = (float)(__bf16)left;
+        if (p == 0 && fabsf(h) == __builtin_inff()) h = copysignf(__uint_as_float(MOST), v);
         part[p] = (uint16_t)(__float_as_uint(h) >> 16);
-        v = fabsf(h) < __builtin_inff() ? v - h : 0.f;
+        left = fabsf(h) < __builtin_inff() ? left - h : 0.f;  // NaN has no rest
     }
+    if (endless) part[2] = (uint16_t)(__float_as_uint(v) >> 16);
 }
 
 // Rows of `pitch` 16-bit numbers with zeros behind, and padded rows as zeros: as they are, or 32-bit numbers in three parts of bfloat16. And the scales of g. At most
@@ -205,8 +209,9 @@ __global__ __launch_bounds__(256) void k_rows(const RowsArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float s = ldexpf(v[j], -e);
-            hi[j] = (_Float16)s;
-            lo[j] = fabsf(s) < 60000.f ? (_Float16)((s - (float)hi[j]) * (1 << kShift)) : (_Float16)0.f;  // an infinity or NaN has no rest
+            const bool endless = fabsf(s) == __builtin_inff();  // all of it in the low part, as in three_parts
+            hi[j] = endless ? (_Float16)0.f : (_Float16)s;
+            lo[j] = (_Float16)((s - (float)hi[j]) * (1 << kShift));
         }
         u32x4 w;
         __builtin_memcpy(&w, hi, 16);

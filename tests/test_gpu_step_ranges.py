@@ -5,8 +5,8 @@ import pytest
 
 import paper_2206_08869_amd as iodf
 import step_ref as ref
-from test_gpu_blocks import as_type, dev, half_unit, host, near, on_gpu, torch
-from test_gpu_step import NAMES, check_forward, long, on_card, some, upstream
+from test_gpu_blocks import as_type, dev, dtype, half_unit, host, near, on_gpu, torch
+from test_gpu_step import NAMES, check_forward, long, on_card, some, spoiled, upstream
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -197,3 +197,51 @@ def test_class_loss_gradients_of_classes_that_are_no_targets(rows, classes, cols
     for a, b, off in ((got[0], du, eu), (got[1], dw, ew)):
         near(a, b, name, off + 1.01 * (half_unit(name, np.abs(b) + off) - half_unit(name, b)), "gradient")
     assert np.linalg.norm(host(got[1])[rare] - dw[rare]) <= {"f32": 1e-5, "bf16": 2.0 ** -8}[name] * np.linalg.norm(dw[rare])
+
+
+MASKED = [(9, 300, 96), (100, 300, 96), (30, 300, 96), (300, 513, 200), (40, 200, 4100), (500, 600, 264)]
+
+
+@pytest.mark.parametrize("rows,classes,cols", MASKED)
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("mask", ["infinity", "lowest"])
+def test_classes_masked_through_a_column_of_ones(rows, classes, cols, name, mask):
+    """A mask of minus infinity, or of the type's lowest number, in a column of the table that every row multiplies with 1: those classes have no probability and the others are as without
+    them. An infinity times g, which is 0 there, makes that column of du NaN, and nothing else."""
+    t = torch()
+    u, w, target, live, rng = some(rows, classes, cols, name, seed=44, dead=0.2)
+    live[0] = True
+    masked = np.arange(classes) % 4 == 2
+    masked[-1] = True
+    target[masked[target]] = 0
+    u[:, 5], w[:, 5] = 1, 0
+    rest = np.flatnonzero(~masked)
+    w[masked, 5] = -np.inf if mask == "infinity" else float(t.finfo(dtype(name)).min)
+    place = np.cumsum(~masked) - 1
+    loss, lse, s = ref.loss(u, w[rest], place[target], live)
+    su, st = spoiled(u, target, live)
+    r = iodf.class_loss(dev(su, name), dev(w, name), long(st), live=on_gpu(live))
+    slack = ref.logit_slack(u, w[rest], live) + 64 * U * (1 + np.abs(lse) + np.abs(s).max(1))
+    near(r.lse, lse, "f32", slack, "lse")
+    near(r.loss, loss, "f32", 2 * slack, "loss")
+    up = upstream(rng, rows, "both")
+    lse32 = lse.astype(np.float32)
+    got = iodf.class_loss_backward(dev(su, name), dev(w, name), long(st), dev(lse32), dev(up[0]), dev(up[1]), live=on_gpu(live))
+    du, dw, eu, ew = ref.loss_backward(u, w[rest], place[target], lse32.astype(np.float64), *up, live, name)
+    columns = np.arange(cols) != 5
+    more = lambda b, off: off + 1.01 * (half_unit(name, np.abs(b) + off) - half_unit(name, b))  # noqa: E731
+    near(got[0][:, t.from_numpy(columns).cuda()], du[:, columns], name, more(du, eu)[:, columns], "du")
+    near(got[1][t.from_numpy(rest).cuda()], dw, name, more(dw, ew), "dweight")
+    assert not got[1][t.from_numpy(masked).cuda()].any() and (mask == "infinity" or not got[0][:, 5].isnan().any())
+
+
+@pytest.mark.parametrize("rows,classes,cols", [(10, 90, 64), (80, 90, 64), (300, 513, 200)])
+@pytest.mark.parametrize("name", NAMES)
+def test_a_row_that_is_no_number_has_a_gradient_that_is_none(rows, classes, cols, name):
+    u, w, target, _, rng = some(rows, classes, cols, name, seed=45)
+    u[4, 9] = np.nan
+    t = torch()
+    lse = iodf.class_loss(dev(u, name), dev(w, name), long(target)).lse
+    du, dw = iodf.class_loss_backward(dev(u, name), dev(w, name), long(target), lse, t.full((rows,), 0.1, device="cuda"))
+    rest = np.arange(rows) != 4
+    assert np.isnan(host(du)[4]).all() and np.isfinite(host(du)[rest]).all() and np.isnan(host(dw)).all()
