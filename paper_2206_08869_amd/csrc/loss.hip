@@ -1,10 +1,11 @@
 // Softmax cross entropy of rows against a table of classes, and its gradient: products of 16-bit numbers (products.h) whose logits never reach
 // memory as such.
 //
-// 32-bit operands: the gradients' sums go over rows and over classes, so that no power of two of a row, class or tensor would do for all that a sum has in it. A class that is hardly a target
-// has probabilities alone for its gradient, 1e-9 and less of the largest number of g, and what updates weights by the size of their gradients goes by those too. So there numbers are three parts of bfloat16,
-// whose range is theirs: six products. 4096 rows, 32768 classes of 1024 columns 4.7 ms; two parts of half precision and three products, which leave a number of 2^-27 of the largest 12 bits, took 2.2. A logit's
-// sum is over columns, and logits of the forward pass are of two parts of half precision with a power of two for each row and each class, three products.
+// 32-bit operands: the gradients' sums go over rows and over classes, so that no power of two of a row, class or tensor would do for all that a sum has in it. A class that is
+// hardly a target has probabilities alone for its gradient, 1e-9 and less of the largest number of g, and what updates weights by the size of their gradients goes by those
+// too. So there numbers are three parts of bfloat16, whose range is theirs: six products. 4096 rows, 32768 classes of 1024 columns 4.7 ms; two parts of half precision and
+// three products, which leave a number of 2^-27 of the largest 12 bits, took 2.2. A logit's sum is over columns, and logits of the forward pass are of two parts of half
+// precision with a power of two for each row and each class, three products.
 //
 // Forward: a workgroup has the logits of a tile of classes and rows in registers and leaves, for each of its rows, their largest and
 // the sum of exponentials relative to it; a second kernel joins the tiles of a row. Backward: the logits once more, from which g = (dloss + dlse) exp(s -
@@ -73,8 +74,8 @@ struct ReadyArgs {
     Scales* scales;
 };
 
-// v in three parts of bfloat16, whose sum it is (but for parts below the smallest numbers there are), whatever its size. An infinity is the last part: that is multiplied with first parts alone, which
-// are 0 where the other number is, while others may be 0 where it is not, and 0 times an infinity is none.
+// v in three parts of bfloat16, whose sum it is (but for parts below the smallest numbers there are), whatever its size. An infinity is the last part: that is multiplied with
+// first parts alone, which are 0 where the other number is, while others may be 0 where it is not, and 0 times an infinity is none.
 __device__ __forceinline__ void three_parts(float v, uint16_t (&part)[3]) {
     constexpr uint32_t MOST = 0x7f7f0000;  // the largest, where rounding would make an infinity
     const bool endless = fabsf(v) == __builtin_inff();
@@ -306,9 +307,9 @@ __device__ __forceinline__ f32x4 product<float>(u32x4 w, u32x4 u, f32x4 c) {
     return c;
 }
 
-// Rows that do not fill a tile, of a table that would have to be copied for tiles: it is read once, as it lies, straight into registers, 32 classes to a workgroup whose four waves share out the
-// columns. NB blocks of 16 rows. Which columns a lane holds is the same for both operands and otherwise of no matter: in 32 bits four neighbours
-// are four products of the 32-bit matrix instruction.
+// Rows that do not fill a tile, of a table that would have to be copied for tiles: it is read once, as it lies, straight into registers, 32 classes to a workgroup whose four
+// waves share out the columns. NB blocks of 16 rows. Which columns a lane holds is the same for both operands and otherwise of no matter: in 32 bits four neighbours are four
+// products of the 32-bit matrix instruction.
 template <typename TX, int NB, bool GRAD>
 __global__ __launch_bounds__(256) void k_few(const FewArgs a) {
     constexpr int E = 16 / (int)sizeof(TX), STEP = 4 * E, AT_ONCE = NB <= 2 ? 4 : 2, SPAN = STEP * AT_ONCE;
@@ -686,7 +687,8 @@ __global__ __launch_bounds__(MW * NW * 64) void k_logits(const LogitArgs a) {
                     const int v0 = m * 16 + P::row_of();
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float s = __builtin_elementwise_minimum(p.acc[m][n][j] - lse[n], 0.f);  // no probability is past 1; of huge logits the two passes' roundings are, and 0 times their exponential is not 0
+                        // no probability is past 1; of huge logits the two passes' roundings are, and 0 times their exponential is not 0
+                        const float s = __builtin_elementwise_minimum(p.acc[m][n][j] - lse[n], 0.f);
                         const float e = PAIRS > 1 ? expf(s) : __builtin_amdgcn_exp2f(s * kLog2e);
                         float g = gb * e - (v0 + j == want[n] ? gu : 0.f);
                         g = want[n] != -2 && m0 + wm + v0 + j < a.classes ? g : 0.f;

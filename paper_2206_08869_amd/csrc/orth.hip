@@ -750,10 +750,9 @@ __global__ __launch_bounds__(256) void k_slim(const SlimArgs a, const int step, 
 
 // ---- one block of 128 x 128 ----
 
-// A matrix of 65 to 128 rows and columns, all of it in a workgroup's LDS with zeros around it, X in two parts and A, then b A + c A^2, in the place of each other.
-// Norm, start and all steps in one launch; tall ones go as the others do, which in a square of zeros is the same. A step reads a megabyte of
-// fragments (three with both parts): LDS is busy for half of the time, the matrix units for an eighth, and the rest is the dependent ways between three products. 128 x 128 in bfloat16 51 us, as
-// three launches a step 69.
+// A matrix of 65 to 128 rows and columns, all of it in a workgroup's LDS with zeros around it, X in two parts and A, then b A + c A^2, in the place of each other. Norm, start
+// and all steps in one launch; tall ones go as the others do, which in a square of zeros is the same. A step reads a megabyte of fragments (three with both parts): LDS is busy
+// for half of the time, the matrix units for an eighth, and the rest is the dependent ways between three products. 128 x 128 in bfloat16 51 us, as three launches a step 69.
 template <int PAIRS, bool MUON>
 __global__ __launch_bounds__(512) void k_block(const Shape z, const OrthSteps steps, const Source src, const int in_type, const float eps, const Target target,
                                                const int type) {

@@ -220,8 +220,9 @@ def orthogonalise(g, steps=5, coefficients=QUINTIC, eps=1e-7, dtype=None, out=No
     """g / (its Frobenius norm + eps), `steps` times an odd polynomial of its singular values: nearly the orthogonal matrix next to it.
 
     g [rows, cols], or [count, rows, cols] for several of one shape. coefficients: (a, b, c) of X <- a X + b XX'X + c (XX')^2 X, or one triple for each
-    step. dtype: the result's, g's if None; bfloat16 takes a third of the work of float32 and float16, with 11 bits of what is multiplied instead of 22. out may be g. At most 4096 matrices, whose shorter side
-    is at most 16384 and longer one at most 65536, of 2^32 elements together (sides rounded up to multiples of 64); eps is above 0."""
+    step. dtype: the result's, g's if None; bfloat16 takes a third of the work of float32 and float16, with 11 bits of what is multiplied instead of 22.
+    out may be g. At most 4096 matrices, whose shorter side is at most 16384 and longer one at most 65536, of 2^32 elements together (sides rounded up to
+    multiples of 64); eps is above 0."""
     t = _k._torch if _native else _setup()
     kind, count, rows, cols, batch, stride = _sheets(g, "g")
     numbers = _polynomials(steps, coefficients)
